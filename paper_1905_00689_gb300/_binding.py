@@ -39,7 +39,10 @@ EXPORTS = (
     "lstm_approx_sync", "lstm_approx_get_mask", "lstm_approx_last_error", "lstm_approx_destroy",
     "lstm_approx_query", "lstm_approx_set_option", "lstm_approx_phase_times", "lstm_approx_run_static",
     "lstm_approx_plan", "lstm_approx_get_term", "lstm_approx_dense_run", "lstm_approx_dense_workspace_bytes",
-    "lstm_approx_dense_set_launch_order",
+    "lstm_approx_dense_set_launch_order", "lstm_approx_rms_norm", "lstm_approx_rms_norm_backward",
+    "lstm_approx_rms_norm_workspace_bytes", "lstm_approx_gated_scan", "lstm_approx_gated_scan_backward",
+    "lstm_approx_gated_scan_workspace_bytes", "lstm_approx_gated_step", "lstm_approx_w4_quantize",
+    "lstm_approx_w4_matvec",
 )
 
 _lib = None
@@ -83,10 +86,23 @@ def load(path: str = LIB_PATH):
                                           ctypes.c_char_p, I]
     lib.lstm_approx_dense_workspace_bytes.argtypes = [I, I, I]
     lib.lstm_approx_dense_set_launch_order.argtypes = [I]
+    # the operators of include/lstm_approx_ops.h; each ends in (stream, msg, msg_len)
+    F, Z, end = ctypes.c_float, ctypes.c_size_t, [P, ctypes.c_char_p, I]
+    lib.lstm_approx_rms_norm.argtypes = [I, I, P, LL, P, LL, P, F, LL, I, P, P, P, P] + end
+    lib.lstm_approx_rms_norm_backward.argtypes = [I, P, LL, P, LL, P, P, P, LL, LL, I, P, P, P, Z] + end
+    lib.lstm_approx_rms_norm_workspace_bytes.argtypes = [LL, I]
+    lib.lstm_approx_gated_scan.argtypes = [I, P, P, P, P, F, P, P, P, I, I, I, P, P, P, P] + end
+    lib.lstm_approx_gated_scan_backward.argtypes = ([I, P, P, P, P, P, P, F, P, P, P, I, I, I, P, P, P, P, P, P, P, Z]
+                                                    + end)
+    lib.lstm_approx_gated_scan_workspace_bytes.argtypes = [I, I, I]
+    lib.lstm_approx_gated_step.argtypes = [I, P, LL, P, LL, P, LL, P, F, P, I, P, P, I, I, P] + end
+    lib.lstm_approx_w4_quantize.argtypes = [I, P, LL, I, I, I, P, LL, P, I, P] + end
+    lib.lstm_approx_w4_matvec.argtypes = [I, P, LL, P, I, P, LL, P, I, P, P, I, I, I, I, P, I] + end
     for name in EXPORTS:
-        if name not in ("lstm_approx_last_error", "lstm_approx_destroy", "lstm_approx_dense_workspace_bytes"):
+        if name.endswith("_workspace_bytes"):
+            getattr(lib, name).restype = ctypes.c_size_t
+        elif name not in ("lstm_approx_last_error", "lstm_approx_destroy"):
             getattr(lib, name).restype = ctypes.c_int
-    lib.lstm_approx_dense_workspace_bytes.restype = ctypes.c_size_t
     _lib = lib
     return lib
 
