@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import threading
 from typing import Optional
 
 import torch
@@ -25,6 +26,10 @@ _CODES = {torch.float32: OP_FP32, torch.bfloat16: OP_BF16, torch.float16: OP_FP1
 _MSG_LEN = 256
 
 
+_F32, _I32, _U8, _E4M3 = torch.float32, torch.int32, torch.uint8, torch.float8_e4m3fn
+_held = threading.local()
+
+
 def _need(ok: bool, text: str) -> None:
     if not ok:
         raise ValueError(text)
@@ -32,13 +37,13 @@ def _need(ok: bool, text: str) -> None:
 
 def _check(t, name: str, dev: int, dtype, shape) -> int:
     """The address of a tensor of this device, type and shape whose last axis is contiguous."""
-    if t.get_device() != dev or dev < 0:
-        raise ValueError(f"{name} must be on the CUDA device of the other tensors")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on the CUDA device of the other tensors")
+    if not t.is_contiguous() and t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name}'s last axis must be contiguous")
     return t.data_ptr()
 
@@ -47,10 +52,10 @@ def _dense(t, name: str, dev: int, dtype, shape) -> Optional[int]:
     """_check of a contiguous tensor; None passes NULL."""
     if t is None:
         return None
-    p = _check(t, name, dev, dtype, shape)
-    if not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _check(t, name, dev, dtype, shape)
         raise ValueError(f"{name} must be contiguous")
-    return p
+    return t.data_ptr()
 
 
 def _code(t, name: str) -> int:
@@ -94,16 +99,18 @@ _HERE = contextlib.nullcontext()
 
 def _on(dev: int, stream, tensors):
     """The context in which a call launches and allocates."""
-    if stream is None and dev == torch.cuda.current_device():
+    if stream is None and dev == torch._C._cuda_getDevice():
         return _HERE
     return _elsewhere(dev, stream, tensors)
 
 
-def _call(name: str, *args) -> None:
-    """lib.name(*args, current stream, msg): raises what it reports."""
-    msg = ctypes.create_string_buffer(_MSG_LEN)
-    raw = torch.cuda.current_stream().cuda_stream
-    rc = getattr(load(), name)(*args, raw, msg, _MSG_LEN)
+def _call(dev: int, name: str, *args) -> None:
+    """lib.name(*args, current stream of dev, msg): raises what it reports."""
+    try:
+        msg = _held.msg
+    except AttributeError:
+        msg = _held.msg = ctypes.create_string_buffer(_MSG_LEN)
+    rc = getattr(load(), name)(*args, torch._C._cuda_getCurrentRawStream(dev), msg, _MSG_LEN)
     if rc != OK:
         raise LSTMApproxError(rc, msg.value.decode())
 
@@ -132,14 +139,14 @@ def _norm(x, weight, residual, eps, group, out, scales, residual_out, rstd, stre
             groups = shape[:-1] + (max(1, -(-D // group)),)
             if scales is None:
                 scales = torch.empty(groups, dtype=torch.float32, device=x.device)
-            _dense(scales, "scales", dev, torch.float32, groups)
+            _dense(scales, "scales", dev, _F32, groups)
         kind = torch.float8_e4m3fn if group else x.dtype
         if out is None:
             out = torch.empty(shape, dtype=kind, device=x.device)
-        _call("lstm_approx_rms_norm", code, group, px, pitch, pres, res_pitch,
-              _dense(weight, "weight", dev, torch.float32, (D,)), eps, rows, D, _dense(out, "out", dev, kind, shape),
+        _call(dev, "lstm_approx_rms_norm", code, group, px, pitch, pres, res_pitch,
+              _dense(weight, "weight", dev, _F32, (D,)), eps, rows, D, _dense(out, "out", dev, kind, shape),
               None if scales is None else scales.data_ptr(), _dense(residual_out, "residual_out", dev, x.dtype, shape),
-              _dense(rstd, "rstd", dev, torch.float32, shape[:-1]))
+              _dense(rstd, "rstd", dev, _F32, shape[:-1]))
     return out, scales, residual_out
 
 
@@ -184,12 +191,12 @@ def rms_norm_backward(dy, s, weight, rstd, dsum=None, *, dx=None, dweight=None, 
         if workspace is None:
             need = load().lstm_approx_rms_norm_workspace_bytes(rows, D)
             workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dy.device)
-        _call("lstm_approx_rms_norm_backward", code, _check(dy, "dy", dev, dy.dtype, shape), _pitch(dy, "dy"),
-              _check(s, "s", dev, dy.dtype, shape), _pitch(s, "s"), _dense(weight, "weight", dev, torch.float32, (D,)),
-              _dense(rstd, "rstd", dev, torch.float32, shape[:-1]),
+        _call(dev, "lstm_approx_rms_norm_backward", code, _check(dy, "dy", dev, dy.dtype, shape), _pitch(dy, "dy"),
+              _check(s, "s", dev, dy.dtype, shape), _pitch(s, "s"), _dense(weight, "weight", dev, _F32, (D,)),
+              _dense(rstd, "rstd", dev, _F32, shape[:-1]),
               None if dsum is None else _check(dsum, "dsum", dev, dy.dtype, shape),
               0 if dsum is None else _pitch(dsum, "dsum"), rows, D, _dense(dx, "dx", dev, dy.dtype, shape),
-              _dense(dweight, "dweight", dev, torch.float32, (D,)), workspace.data_ptr(), workspace.nbytes)
+              _dense(dweight, "dweight", dev, _F32, (D,)), workspace.data_ptr(), workspace.nbytes)
     return dx, dweight
 
 
@@ -225,10 +232,10 @@ def gated_scan(x, r, i, decay, h0=None, *, c: float = 8.0, lengths=None, reset=N
             y = torch.empty(shape, dtype=x.dtype, device=x.device)
         if h_last is None:
             h_last = torch.empty(B, D, dtype=torch.float32, device=x.device)
-        f32 = torch.float32
+        f32 = _F32
         px, pr, pi, py = (_check(t, n, dev, x.dtype, shape) for t, n in ((x, "x"), (r, "r"), (i, "i"), (y, "y")))
-        _call("lstm_approx_gated_scan", code, px, pr, pi, _dense(decay, "decay", dev, f32, (D,)), c,
-              _dense(h0, "h0", dev, f32, (B, D)), _dense(lengths, "lengths", dev, torch.int32, (B,)),
+        _call(dev, "lstm_approx_gated_scan", code, px, pr, pi, _dense(decay, "decay", dev, f32, (D,)), c,
+              _dense(h0, "h0", dev, f32, (B, D)), _dense(lengths, "lengths", dev, _I32, (B,)),
               _reset(reset, dev, (T, B)), T, B, D, py, _strides(x, r, i, y), _dense(h_last, "h_last", dev, f32, (B, D)),
               _dense(states, "states", dev, f32, (-(-T // SCAN_CHUNK), B, D)))
     return y, h_last
@@ -248,7 +255,7 @@ def gated_scan_backward(dy, x, r, i, decay, states, dh_last=None, *, c: float = 
     """
     dev, code = _cuda(x, "x"), _code(x, "x")
     _need(x.dim() == 3, "x must be [T, B, D]")
-    shape, f32 = x.shape, torch.float32
+    shape, f32 = x.shape, _F32
     T, B, D = shape
     with _on(dev, stream, (dy, x, r, i, decay, states, dh_last, lengths, reset, dx, dr, di, ddecay, dh0, workspace)):
         dx, dr, di = (torch.empty(shape, dtype=x.dtype, device=x.device) if t is None else t for t in (dx, dr, di))
@@ -262,10 +269,10 @@ def gated_scan_backward(dy, x, r, i, decay, states, dh_last=None, *, c: float = 
         pdy, px, pr, pi, pdx, pdr, pdi = (
             _check(t, n, dev, x.dtype, shape)
             for t, n in ((dy, "dy"), (x, "x"), (r, "r"), (i, "i"), (dx, "dx"), (dr, "dr"), (di, "di")))
-        _call("lstm_approx_gated_scan_backward", code, pdy, _dense(dh_last, "dh_last", dev, f32, (B, D)), px, pr, pi,
+        _call(dev, "lstm_approx_gated_scan_backward", code, pdy, _dense(dh_last, "dh_last", dev, f32, (B, D)), px, pr, pi,
               _dense(decay, "decay", dev, f32, (D,)), c,
               _dense(states, "states", dev, f32, (-(-T // SCAN_CHUNK), B, D)),
-              _dense(lengths, "lengths", dev, torch.int32, (B,)), _reset(reset, dev, (T, B)), T, B, D, pdx, pdr, pdi,
+              _dense(lengths, "lengths", dev, _I32, (B,)), _reset(reset, dev, (T, B)), T, B, D, pdx, pdr, pdi,
               _strides(dy, x, r, i, dx, dr, di), _dense(ddecay, "ddecay", dev, f32, (D,)),
               _dense(dh0, "dh0", dev, f32, (B, D)), workspace.data_ptr(), workspace.nbytes)
     return dx, dr, di, ddecay, dh0
@@ -279,15 +286,15 @@ def gated_step(x, r, i, decay, state, *, c: float = 8.0, slots=None, reset=None,
     """
     dev, code = _cuda(x, "x"), _code(x, "x")
     _need(x.dim() == 2 and state.dim() == 2, "x must be [B, D] and state [n_slots, D]")
-    shape, f32 = x.shape, torch.float32
+    shape, f32 = x.shape, _F32
     B, D = shape
     with _on(dev, stream, (x, r, i, decay, state, slots, reset, y)):
         if y is None:
             y = torch.empty(shape, dtype=x.dtype, device=x.device)
-        _call("lstm_approx_gated_step", code, _check(x, "x", dev, x.dtype, shape), x.stride(0),
+        _call(dev, "lstm_approx_gated_step", code, _check(x, "x", dev, x.dtype, shape), x.stride(0),
               _check(r, "r", dev, x.dtype, shape), r.stride(0), _check(i, "i", dev, x.dtype, shape), i.stride(0),
               _dense(decay, "decay", dev, f32, (D,)), c, _dense(state, "state", dev, f32, (state.shape[0], D)),
-              state.shape[0], _dense(slots, "slots", dev, torch.int32, (B,)), _reset(reset, dev, (B,)), B, D,
+              state.shape[0], _dense(slots, "slots", dev, _I32, (B,)), _reset(reset, dev, (B,)), B, D,
               _dense(y, "y", dev, x.dtype, shape))
     return y
 
@@ -330,7 +337,7 @@ def w4_quantize(w, group: int = 128, *, scale_dtype=torch.float16, stream=None) 
         q = torch.empty(N, -(-K // 32) * 16, dtype=torch.uint8, device=w.device)
         scale = torch.empty(N, G, dtype=scale_dtype, device=w.device)
         zero = torch.empty(N, G, dtype=torch.uint8, device=w.device)
-        _call("lstm_approx_w4_quantize", code, _check(w, "w", dev, w.dtype, w.shape), w.stride(0), N, K, group,
+        _call(dev, "lstm_approx_w4_quantize", code, _check(w, "w", dev, w.dtype, w.shape), w.stride(0), N, K, group,
               q.data_ptr(), q.shape[1], scale.data_ptr(), _code(scale, "scale"), zero.data_ptr())
         return W4Weight(q, scale, zero, K, group)
 
@@ -362,7 +369,7 @@ def w4_matvec(x, w: W4Weight, *, x_scale=None, bias=None, out=None, out_dtype=No
             out_dtype = out_dtype or (torch.bfloat16 if code == OP_E4M3 else x.dtype)
             out = torch.empty(lead + (N,), dtype=out_dtype, device=x.device)
         y_code = _code(out, "out")
-        _call("lstm_approx_w4_matvec", code, _check(x, "x", dev, x.dtype, shape), _pitch(x, "x"),
+        _call(dev, "lstm_approx_w4_matvec", code, _check(x, "x", dev, x.dtype, shape), _pitch(x, "x"),
               None if x_scale is None else x_scale.data_ptr(), x_group, w.q.data_ptr(), w.pitch, w.scale.data_ptr(),
               w.code, None if w.zero is None else w.zero.data_ptr(), _dense(bias, "bias", dev, torch.float32, (N,)),
               M, N, K, w.group, _dense(out, "out", dev, out.dtype, lead + (N,)), y_code)

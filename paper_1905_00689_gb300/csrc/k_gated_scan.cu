@@ -13,6 +13,13 @@
 // and each warp goes over its 8 timesteps once more from the state it starts
 // with.  a_t and m_t sigma(i_t) x_t are computed once and stay in registers.
 //
+// Few streams over few channels leave most of the GPU idle in that form, so the
+// blocks of a cluster of up to 16 share a stream's 64 channels: block k of n
+// takes tiles k, n + k, ..., writes its tile's (A, U) into every block's shared
+// memory, and after one cluster barrier per n tiles each block joins all of
+// them in order.  That keeps the sequence at one pass over memory in one
+// launch, with no flags in memory and no waits but the barrier.
+//
 // Backward, with p_t = k_t a_t g_t the gradient of h_{t-1}:
 //   g_t = dy_t + p_{t+1}  (p after the last timestep: dh_last; before the first: dh0)
 //   dx = g m si,  di = g m x si (1 - si)                       (si = sigma(i))
@@ -51,41 +58,75 @@ __device__ __forceinline__ float softplus_ratio_f(float d) {
   return sp > 0.0f ? sig / sp : 1.0f;
 }
 
-// 1 - e^t for t <= 0: above -0.35 by its Taylor series to t^8 (the first
-// term left out is t^8 / 9! < 7e-10 of the first), which has no cancellation.
-__device__ __forceinline__ float one_minus_exp(float t) {
-  float p = 1.0f / 40320.0f;
-  p = fmaf(p, t, 1.0f / 5040.0f);
-  p = fmaf(p, t, 1.0f / 720.0f);
-  p = fmaf(p, t, 1.0f / 120.0f);
-  p = fmaf(p, t, 1.0f / 24.0f);
-  p = fmaf(p, t, 1.0f / 6.0f);
-  p = fmaf(p, t, 0.5f);
-  p = fmaf(p, t, 1.0f);
-  return t > -0.35f ? -t * p : 1.0f - ex2_approx(t * kLog2E);
-}
-
-__device__ __forceinline__ float sqrt_approx(float x) {
+// x for x <= 60, else 60; NaN stays NaN.
+__device__ __forceinline__ float at_most_60(float x) {
   float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("min.NaN.f32 %0, %1, 0f42700000;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float rsqrt_approx(float x) {
+  float r;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 
+// The gates of a lane's two channels (pairs of fp32, two per instruction where
+// there is one for two): sigma(r), sigma(i), 1 - a and 1 - a^2, from which a
+// and m follow.  rate = c softplus(decay); far: -log a may be above 0.35.
+//
+// Both sigmoids come from one reciprocal of the product of their denominators
+// (the special-function unit, four operations to a channel, is what the scan
+// meets next after memory); so that the product stays finite, e^-z is taken at
+// most 2^60, which moves a sigmoid below 9e-19 up to that.
+//
+// 1 - a = 1 - e^-t by its Taylor series to t^8 for t <= 0.35 (the first term
+// left out is below 7e-10 of the first): no cancellation, a = 1 - (1 - a) comes
+// out correctly rounded, which matters where a state decays over hundreds of
+// timesteps, and 1 - a^2 = (1 - a)(2 - (1 - a)) keeps its digits.
 struct Gates {
-  float sr, si, la, a, m;
+  uint64_t sr, si, low, m2;
 };
-// rate = -c softplus(decay)
-__device__ __forceinline__ Gates gates_of(float r, float i, float rate) {
+__device__ __forceinline__ uint64_t both(float v) { return f32x2(v, v); }
+__device__ __forceinline__ Gates gates_of(uint64_t r, uint64_t i, uint64_t rate, bool far) {
+  float r0, r1, i0, i1;
+  f32x2_split(mul2(r, both(-kLog2E)), r0, r1);
+  f32x2_split(mul2(i, both(-kLog2E)), i0, i1);
+  const uint64_t dr = add2(f32x2(ex2_approx(at_most_60(r0)), ex2_approx(at_most_60(r1))), both(1.0f));
+  const uint64_t di = add2(f32x2(ex2_approx(at_most_60(i0)), ex2_approx(at_most_60(i1))), both(1.0f));
+  float d0, d1;
+  f32x2_split(mul2(dr, di), d0, d1);
+  const uint64_t inv = f32x2(rcp_approx(d0), rcp_approx(d1));
   Gates g;
-  g.sr = sigmoid_f(r);
-  g.si = sigmoid_f(i);
-  g.la = rate * g.sr;
-  // a = 1 - (1 - a) and m^2 = (1 - a)(1 + a): a decay near 1, which acts over
-  // hundreds of timesteps, comes out correctly rounded, and m keeps its digits
-  const float low = one_minus_exp(g.la);
-  g.a = 1.0f - low;
-  g.m = sqrt_approx(low * (1.0f + g.a));
+  g.sr = mul2(inv, di);
+  g.si = mul2(inv, dr);
+  const uint64_t t = mul2(rate, g.sr);
+  uint64_t p = both(-1.0f / 40320.0f);
+  p = fma2(p, t, both(1.0f / 5040.0f));
+  p = fma2(p, t, both(-1.0f / 720.0f));
+  p = fma2(p, t, both(1.0f / 120.0f));
+  p = fma2(p, t, both(-1.0f / 24.0f));
+  p = fma2(p, t, both(1.0f / 6.0f));
+  p = fma2(p, t, both(-0.5f));
+  p = fma2(p, t, both(1.0f));
+  g.low = mul2(t, p);
+  if (far) {
+    float t0, t1, l0, l1;
+    f32x2_split(t, t0, t1);
+    f32x2_split(g.low, l0, l1);
+    if (t0 > 0.35f) l0 = 1.0f - ex2_approx(-t0 * kLog2E);
+    if (t1 > 0.35f) l1 = 1.0f - ex2_approx(-t1 * kLog2E);
+    g.low = f32x2(l0, l1);
+  }
+  g.m2 = mul2(g.low, fma2(g.low, both(-1.0f), both(2.0f)));
   return g;
+}
+
+// m = sqrt(m2) and 1 / m, the latter at most 2^63 (m2 = 0 gives m = 0).
+__device__ __forceinline__ void root_of(uint64_t m2, uint64_t& m, uint64_t& inv_m) {
+  float a, b;
+  f32x2_split(m2, a, b);
+  inv_m = f32x2(rsqrt_approx(fmaxf(a, 1.17549435e-38f)), rsqrt_approx(fmaxf(b, 1.17549435e-38f)));
+  m = mul2(m2, inv_m);
 }
 
 // The pair of channels (ch, ch + 1) at p; kVec: both exist and lie in one
@@ -105,9 +146,68 @@ __device__ __forceinline__ void store_pair(T* p, int left, float a, float b) {
   }
 }
 
+// A lane's two channels of one staged timestep.
+template <typename T>
+__device__ __forceinline__ uint64_t staged_pair(const T* p) {
+  if constexpr (sizeof(T) == 4) {
+    return *reinterpret_cast<const uint64_t*>(p);
+  } else {
+    const float2 f = Pair<T>::get(*reinterpret_cast<const typename Pair<T>::Raw*>(p));
+    return f32x2(f.x, f.y);
+  }
+}
+
 struct Strides {
   long long t, b;
 };
+
+// How a tile comes into shared memory: by asynchronous copies of kCopy bytes
+// where every address is a multiple of it (16: everything aligned, D a multiple
+// of 8; 4: an even D, or 32-bit values), else value by value (2).
+//
+// A warp stages its own 8 timesteps of a tile, [kSteps][64] for each tensor,
+// and reads nothing else, so its copies need no barrier of the block.
+// Timesteps past `len` and channels past D come out as zeros, nothing of
+// theirs is read.
+template <typename T, int kCopy>
+__device__ __forceinline__ void stage(T* dst, const T* src, long long stride, int ts, int len, int ch0, int D) {
+  const int lane = threadIdx.x & 31;
+  if constexpr (kCopy >= 4) {
+    constexpr int kPer = kCopy / (int)sizeof(T);          // values of a copy
+    constexpr int kRow = kLanes / kPer;                   // copies of a row
+    constexpr int kRows = kRow >= 32 ? 1 : 32 / kRow;     // rows of one turn of the warp
+    constexpr int kTurns = kRow >= 32 ? kRow / 32 : 1;    // turns of one row
+#pragma unroll
+    for (int s = 0; s < kSteps; s += kRows) {
+#pragma unroll
+      for (int q = 0; q < kTurns; ++q) {
+        const int row = s + lane / kRow % kRows, col = (lane % kRow + 32 * q) * kPer;
+        const bool in = ts + row < len && ch0 + col < D;
+        const T* from = in ? src + (ts + row) * stride + col : src;
+        const uint32_t to = smem_u32(dst + row * kLanes + col);
+        if constexpr (kCopy == 16)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(in ? 16 : 0) : "memory");
+        else
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(in ? 4 : 0) : "memory");
+      }
+    }
+  } else {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int col = lane + 32 * q;
+        dst[s * kLanes + col] = ts + s < len && ch0 + col < D ? src[(ts + s) * stride + col] : from_f32<T>(0.0f);
+      }
+    }
+  }
+}
+__device__ __forceinline__ void stage_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void stage_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+  __syncwarp();
+}
 
 struct ScanArgs {
   const void *x, *r, *i;
@@ -118,7 +218,7 @@ struct ScanArgs {
   const float* h0;
   const int* lengths;
   const unsigned char* reset;
-  int T, B, D, slabs;
+  int T, B, D, slabs, cluster;
   float* h_last;
   float* states;
 };
@@ -135,85 +235,201 @@ __device__ __forceinline__ unsigned reset_bits(const unsigned char* reset, int t
   return __ballot_sync(0xffffffffu, on);
 }
 
-// One warp's run: state after it = cut ? U : A h + U.
-struct Run {
-  float2 A[kWarps][32], U[kWarps][32];
+constexpr int kMaxCluster = 16;
+
+// Runs of several timesteps, of the warps of a tile or the tiles of a
+// cluster's blocks: state after run k = cut[k] ? U : A h + U.
+struct Runs {
+  ulonglong2* AU;  // [runs][32]: A and U of a lane's two channels
+  unsigned* cut;   // [runs]
+};
+struct WarpRuns {
+  ulonglong2 AU[kWarps][32];
   unsigned cut[kWarps];
 };
+__device__ __forceinline__ Runs runs_of(WarpRuns& w) { return {&w.AU[0][0], w.cut}; }
 
-template <typename T, bool kVec>
-__global__ void __launch_bounds__(kWarps * 32) gated_scan_kernel(const ScanArgs a) {
-  __shared__ Run runs[2];
+// h after run k.
+__device__ __forceinline__ uint64_t after(const Runs& r, int k, uint64_t h) {
+  const ulonglong2 v = r.AU[k * 32 + (threadIdx.x & 31)];
+  return r.cut[k] != 0 ? v.y : fma2(v.x, h, v.y);
+}
+
+// The exchange buffer of parity `turn` behind the staged tiles: a run for each block of the cluster.
+__device__ __forceinline__ Runs tile_runs(unsigned char* base, int cluster, int turn) {
+  ulonglong2* AU = reinterpret_cast<ulonglong2*>(base);
+  unsigned* cut = reinterpret_cast<unsigned*>(AU + 2 * cluster * 32);
+  return {AU + turn * cluster * 32, cut + turn * cluster};
+}
+__host__ __device__ constexpr size_t exchange_bytes(int cluster) {
+  return cluster > 1 ? (size_t)2 * cluster * (32 * sizeof(ulonglong2) + sizeof(unsigned)) : 0;
+}
+
+// Writes this block's tile run into slot `rank` of `mine` in every block of the
+// cluster, one block to a warp (the blocks past the eighth in a second turn).
+__device__ __forceinline__ void send_run(const Runs& mine, int rank, int size, ulonglong2 run, bool cut) {
+  const int lane = threadIdx.x & 31;
+  for (int to = threadIdx.x >> 5; to < size; to += kWarps) {
+    const uint32_t at = mapa_shared(smem_u32(mine.AU + rank * 32 + lane), to);
+    asm volatile("st.shared::cluster.v2.u64 [%0], {%1, %2};" ::"r"(at), "l"(run.x), "l"(run.y) : "memory");
+    if (lane == 0) {
+      const uint32_t c = mapa_shared(smem_u32(mine.cut + rank), to);
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(c), "r"((unsigned)cut) : "memory");
+    }
+  }
+}
+
+// Tiles in flight or in use at once, of kTensors tensors: as many as let two
+// blocks share an SM's shared memory (32-bit values backward, and forward in a
+// cluster of 16: one block).
+template <typename T, int kTensors>
+constexpr int kStages = sizeof(T) == 4 || kTensors == 4 ? 2 : 3;
+template <typename T, int kTensors>
+constexpr size_t kStageBytes = (size_t)kTensors * kTile * kLanes * sizeof(T);
+
+__device__ __forceinline__ uint64_t load_f32x2(const float* p, int left) {
+  return f32x2(left > 0 ? p[0] : 0.0f, left > 1 ? p[1] : 0.0f);
+}
+__device__ __forceinline__ void store_f32x2(float* p, int left, uint64_t v) {
+  float a, b;
+  f32x2_split(v, a, b);
+  if (left > 0) p[0] = a;
+  if (left > 1) p[1] = b;
+}
+
+// c softplus(decay) of a lane's channels, zero for one that does not exist.
+__device__ __forceinline__ uint64_t rate_of(const float* decay, int left, float c) {
+  return f32x2(left > 0 ? c * softplus_f(decay[0]) : 0.0f, left > 1 ? c * softplus_f(decay[1]) : 0.0f);
+}
+// Whether -log a of some lane may be above 0.35.
+__device__ __forceinline__ bool any_far(uint64_t rate) {
+  float r0, r1;
+  f32x2_split(rate, r0, r1);
+  return __any_sync(0xffffffffu, !(r0 <= 0.35f && r1 <= 0.35f));
+}
+
+template <typename T, int kCopy>
+__global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const ScanArgs a) {
+  extern __shared__ __align__(16) unsigned char staged[];
+  __shared__ WarpRuns runs[2];
+  constexpr int kN = kStages<T, 3>;
+  unsigned char* exchange = staged + kN * kStageBytes<T, 3>;
+  constexpr bool kVec = kCopy >= 2 * (int)sizeof(T);  // a lane's two channels of y in one store
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int slab = blockIdx.x % a.slabs, b = blockIdx.x / a.slabs;
-  const int ch = slab * kLanes + 2 * lane, left = a.D - ch;  // channels of this lane that exist: min(left, 2)
-  const bool any = left > 0;
+  const int rank = blockIdx.x % a.cluster, item = blockIdx.x / a.cluster;
+  const int slab = item % a.slabs, b = item / a.slabs;
+  const int ch0 = slab * kLanes, ch = ch0 + 2 * lane, left = a.D - ch;  // channels of this lane that exist: min(left, 2)
   const int len = length_of(a.lengths, b, a.T);
-  const T* x = static_cast<const T*>(a.x) + b * a.sx.b + ch;
-  const T* r = static_cast<const T*>(a.r) + b * a.sr.b + ch;
-  const T* in = static_cast<const T*>(a.i) + b * a.si.b + ch;
+  const T* x = static_cast<const T*>(a.x) + b * a.sx.b + ch0;
+  const T* r = static_cast<const T*>(a.r) + b * a.sr.b + ch0;
+  const T* in = static_cast<const T*>(a.i) + b * a.si.b + ch0;
   T* y = static_cast<T*>(a.y) + b * a.sy.b + ch;
   const long long state_at = (long long)b * a.D + ch;
-  float2 rate = make_float2(0.0f, 0.0f), h = make_float2(0.0f, 0.0f);
-  if (any) {
-    const float2 d = load_pair<float, false>(a.decay + ch, left);
-    rate = make_float2(-a.c * softplus_f(d.x), -a.c * softplus_f(d.y));
-    if (a.h0) h = load_pair<float, false>(a.h0 + state_at, left);
-  }
-  int turn = 0;
-  for (int t0 = 0; t0 < a.T; t0 += kTile, turn ^= 1) {
-    const int ts = t0 + warp * kSteps;
+  const int stride = a.cluster * kTile;
+  auto buffer = [&](int n) { return reinterpret_cast<T*>(staged + n * kStageBytes<T, 3>) + warp * kSteps * kLanes; };
+  auto fetch = [&](int n, int first) {  // this warp's part of the tile that starts at `first` + rank tiles, if there is one
+    T* to = buffer(n);
+    const int ts = first + rank * kTile + warp * kSteps;
+    if (ts < len) {
+      stage<T, kCopy>(to, x, a.sx.t, ts, len, ch0, a.D);
+      stage<T, kCopy>(to + kTile * kLanes, r, a.sr.t, ts, len, ch0, a.D);
+      stage<T, kCopy>(to + 2 * kTile * kLanes, in, a.si.t, ts, len, ch0, a.D);
+    }
+    stage_commit();
+  };
+#pragma unroll
+  for (int n = 0; n < kN - 1; ++n) fetch(n, n * stride);
+  const uint64_t rate = rate_of(a.decay + ch, left, a.c);
+  const bool far = any_far(rate);
+  uint64_t h = a.h0 ? load_f32x2(a.h0 + state_at, left) : 0ull;
+  // shared memory of another block is written only after that block has started
+  if (a.cluster > 1) cluster_sync_all();
+  int turn = 0, at = 0, next = kN - 1;  // parity of the exchange buffers; stage in use, stage to fill
+  // every block of the cluster makes the same number of turns (they meet in the barrier)
+  for (int first = 0; first < a.T; first += stride, turn ^= 1) {
+    const int t0 = first + rank * kTile, ts = t0 + warp * kSteps;
     const unsigned resets = reset_bits(a.reset, ts, len, b, a.B);
-    float2 A[kSteps], U[kSteps];
-    float2 xs[kSteps], rs[kSteps], is[kSteps];
+    const T* here = buffer(at) + 2 * lane;
+    stage_wait<kN - 2>();
+    fetch(next, first + (kN - 1) * stride);  // into the stage that the last turn read
+    at = at + 1 == kN ? 0 : at + 1;
+    next = next + 1 == kN ? 0 : next + 1;
+    uint64_t A[kSteps], U[kSteps], PA = both(1.0f), PU = 0ull;
+    const bool whole = ts + kSteps <= len;
+    if (ts < len) {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        const T* p = here + s * kLanes;
+        const Gates g = gates_of(staged_pair<T>(p + kTile * kLanes), staged_pair<T>(p + 2 * kTile * kLanes), rate, far);
+        uint64_t m, inv_m;
+        root_of(g.m2, m, inv_m);
+        A[s] = fma2(g.low, both(-1.0f), both(1.0f));
+        U[s] = mul2(mul2(m, g.si), staged_pair<T>(p));
+      }
+      if (!whole) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+          if (ts + s >= len) A[s] = both(1.0f), U[s] = 0ull;
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) A[s] = both(1.0f), U[s] = 0ull;
+    }
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-      xs[s] = rs[s] = is[s] = make_float2(0.0f, 0.0f);
-      if (any && ts + s < len) {
-        xs[s] = load_pair<T, kVec>(x + (ts + s) * a.sx.t, left);
-        rs[s] = load_pair<T, kVec>(r + (ts + s) * a.sr.t, left);
-        is[s] = load_pair<T, kVec>(in + (ts + s) * a.si.t, left);
+      if (resets >> s & 1u) PU = 0ull;
+      PU = fma2(A[s], PU, U[s]);
+      PA = mul2(PA, A[s]);
+    }
+    runs[turn].AU[warp][lane] = make_ulonglong2(PA, PU);  // the other parity's may still be read
+    if (lane == 0) runs[turn].cut[warp] = resets;
+    __syncthreads();
+    const Runs run = runs_of(runs[turn]), tiles = tile_runs(exchange, a.cluster, turn);
+    if (a.cluster > 1) {
+      ulonglong2 all = make_ulonglong2(both(1.0f), 0ull);
+      bool cut = false;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        all.x = mul2(all.x, run.AU[w * 32 + lane].x);
+        all.y = after(run, w, all.y);
+        cut = cut || run.cut[w] != 0;
+      }
+      send_run(tiles, rank, a.cluster, all, cut);
+      cluster_sync_all();
+    }
+    uint64_t hs = h;  // the state before this block's tile, then before this warp's timesteps
+    if (a.cluster > 1) {
+      for (int k = 0; k < a.cluster; ++k) {
+        if (k == rank) hs = h;
+        h = after(tiles, k, h);
       }
     }
-    float2 PA = make_float2(1.0f, 1.0f), PU = make_float2(0.0f, 0.0f);
+    if (a.states && warp == 0 && t0 < a.T)
+      store_f32x2(a.states + (long long)(t0 / kTile) * a.B * a.D + state_at, left, hs);
+    if (a.cluster > 1) {
+      for (int w = 0; w < warp; ++w) hs = after(run, w, hs);
+    } else {
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        if (w == warp) hs = h;
+        h = after(run, w, h);
+      }
+    }
+    T* to = y + ts * a.sy.t;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-      const Gates g0 = gates_of(rs[s].x, is[s].x, rate.x), g1 = gates_of(rs[s].y, is[s].y, rate.y);
-      const bool live = ts + s < len, cut = resets >> s & 1u;
-      A[s] = live ? make_float2(g0.a, g1.a) : make_float2(1.0f, 1.0f);
-      U[s] = live ? make_float2(g0.m * g0.si * xs[s].x, g1.m * g1.si * xs[s].y) : make_float2(0.0f, 0.0f);
-      PU.x = cut ? U[s].x : fmaf(A[s].x, PU.x, U[s].x);
-      PU.y = cut ? U[s].y : fmaf(A[s].y, PU.y, U[s].y);
-      PA.x *= A[s].x;
-      PA.y *= A[s].y;
-    }
-    Run& run = runs[turn];  // the other one may still be read
-    run.A[warp][lane] = PA;
-    run.U[warp][lane] = PU;
-    if (lane == 0) run.cut[warp] = resets;
-    __syncthreads();
-    float2 hs = h;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float2 wa = run.A[w][lane], wu = run.U[w][lane];
-      const bool cut = run.cut[w] != 0;
-      if (w == warp) hs = h;
-      h.x = cut ? wu.x : fmaf(wa.x, h.x, wu.x);
-      h.y = cut ? wu.y : fmaf(wa.y, h.y, wu.y);
-    }
-    if (a.states && warp == 0 && any)
-      store_pair<float, false>(a.states + (long long)(t0 / kTile) * a.B * a.D + state_at, left, hs.x, hs.y);
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const bool cut = resets >> s & 1u;
-      hs.x = cut ? U[s].x : fmaf(A[s].x, hs.x, U[s].x);
-      hs.y = cut ? U[s].y : fmaf(A[s].y, hs.y, U[s].y);
-      const bool live = ts + s < len;
-      if (any && ts + s < a.T)
-        store_pair<T, kVec>(y + (ts + s) * a.sy.t, left, live ? hs.x : 0.0f, live ? hs.y : 0.0f);
+      if (resets >> s & 1u) hs = 0ull;
+      hs = fma2(A[s], hs, U[s]);
+      float h0, h1;
+      f32x2_split(hs, h0, h1);
+      if (!whole && ts + s >= len) h0 = h1 = 0.0f;
+      if (left > 0 && (whole || ts + s < a.T)) store_pair<T, kVec>(to, left, h0, h1);
+      to += a.sy.t;
     }
   }
-  if (warp == 0 && any) store_pair<float, false>(a.h_last + state_at, left, h.x, h.y);
+  if (warp == 0 && rank == 0) store_f32x2(a.h_last + state_at, left, h);
+  // no block leaves while another may still write into its shared memory
+  if (a.cluster > 1) cluster_sync_all();
 }
 
 struct ScanBackwardArgs {
@@ -226,137 +442,189 @@ struct ScanBackwardArgs {
   const float* states;
   const int* lengths;
   const unsigned char* reset;
-  int T, B, D, slabs;
+  int T, B, D, slabs, cluster;
   float* dh0;
-  float* partial;  // [B][D]: sum of E over the stream's timesteps
+  float* partial;  // [B][cluster][D]: each block's sum of E over its timesteps
 };
 
-template <typename T, bool kVec>
-__global__ void __launch_bounds__(kWarps * 32) gated_scan_backward_kernel(const ScanBackwardArgs a) {
-  __shared__ Run runs[2];
-  __shared__ float2 back[2][kWarps][32];  // V of p -> A p + V (A: as forward)
+template <typename T, int kCopy>
+__global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_scan_backward_kernel(const ScanBackwardArgs a) {
+  extern __shared__ __align__(16) unsigned char staged[];
+  __shared__ WarpRuns runs[2];  // h -> A h + U
+  __shared__ WarpRuns back[2];  // p -> A p + V
+  constexpr int kN = kStages<T, 4>;
+  unsigned char* exchange = staged + kN * kStageBytes<T, 4>;
+  constexpr bool kVec = kCopy >= 2 * (int)sizeof(T);
+  constexpr int kOne = kTile * kLanes;  // values of one staged tensor
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int slab = blockIdx.x % a.slabs, b = blockIdx.x / a.slabs;
-  const int ch = slab * kLanes + 2 * lane, left = a.D - ch;
-  const bool any = left > 0;
+  const int rank = blockIdx.x % a.cluster, item = blockIdx.x / a.cluster;
+  const int slab = item % a.slabs, b = item / a.slabs;
+  const int ch0 = slab * kLanes, ch = ch0 + 2 * lane, left = a.D - ch;
   const int len = length_of(a.lengths, b, a.T);
-  const T* dy = static_cast<const T*>(a.dy) + b * a.sdy.b + ch;
-  const T* x = static_cast<const T*>(a.x) + b * a.sx.b + ch;
-  const T* r = static_cast<const T*>(a.r) + b * a.sr.b + ch;
-  const T* in = static_cast<const T*>(a.i) + b * a.si.b + ch;
+  const T* dy = static_cast<const T*>(a.dy) + b * a.sdy.b + ch0;
+  const T* x = static_cast<const T*>(a.x) + b * a.sx.b + ch0;
+  const T* r = static_cast<const T*>(a.r) + b * a.sr.b + ch0;
+  const T* in = static_cast<const T*>(a.i) + b * a.si.b + ch0;
   T* dx = static_cast<T*>(a.dx) + b * a.sdx.b + ch;
   T* dr = static_cast<T*>(a.dr) + b * a.sdr.b + ch;
   T* di = static_cast<T*>(a.di) + b * a.sdi.b + ch;
   const long long state_at = (long long)b * a.D + ch;
-  float2 rate = make_float2(0.0f, 0.0f), p = make_float2(0.0f, 0.0f), sum = make_float2(0.0f, 0.0f);
-  if (any) {
-    const float2 d = load_pair<float, false>(a.decay + ch, left);
-    rate = make_float2(-a.c * softplus_f(d.x), -a.c * softplus_f(d.y));
-    if (a.dh_last) p = load_pair<float, false>(a.dh_last + state_at, left);
-  }
-  int turn = 0;
-  for (int t0 = (a.T - 1) / kTile * kTile; t0 >= 0 && a.T > 0; t0 -= kTile, turn ^= 1) {
-    const int ts = t0 + warp * kSteps;
+  const int stride = a.cluster * kTile;
+  auto buffer = [&](int n) { return reinterpret_cast<T*>(staged + n * kStageBytes<T, 4>) + warp * kSteps * kLanes; };
+  auto fetch = [&](int n, int first) {
+    T* to = buffer(n);
+    const int ts = first + rank * kTile + warp * kSteps;
+    if (first >= 0 && ts < len) {
+      stage<T, kCopy>(to, x, a.sx.t, ts, len, ch0, a.D);
+      stage<T, kCopy>(to + kOne, r, a.sr.t, ts, len, ch0, a.D);
+      stage<T, kCopy>(to + 2 * kOne, in, a.si.t, ts, len, ch0, a.D);
+      stage<T, kCopy>(to + 3 * kOne, dy, a.sdy.t, ts, len, ch0, a.D);
+    }
+    stage_commit();
+  };
+  const int last = a.T > 0 ? (a.T - 1) / stride * stride : -1;
+#pragma unroll
+  for (int n = 0; n < kN - 1; ++n) fetch(n, last - n * stride);
+  const uint64_t rate = rate_of(a.decay + ch, left, a.c);
+  const bool far = any_far(rate);
+  uint64_t p = a.dh_last ? load_f32x2(a.dh_last + state_at, left) : 0ull, sum = 0ull;
+  if (a.cluster > 1) cluster_sync_all();
+  int turn = 0, at = 0, next = kN - 1;
+  for (int first = last; first >= 0; first -= stride, turn ^= 1) {
+    const int t0 = first + rank * kTile, ts = t0 + warp * kSteps;
     const unsigned resets = reset_bits(a.reset, ts, len, b, a.B);
-    float2 ys[kSteps], xs[kSteps], rs[kSteps], is[kSteps];
+    const T* here = buffer(at) + 2 * lane;
+    uint64_t h = t0 < a.T ? load_f32x2(a.states + (long long)(t0 / kTile) * a.B * a.D + state_at, left) : 0ull;
+    stage_wait<kN - 2>();
+    fetch(next, first - (kN - 1) * stride);
+    at = at + 1 == kN ? 0 : at + 1;
+    next = next + 1 == kN ? 0 : next + 1;
+    const bool whole = ts + kSteps <= len;
+    uint64_t low[kSteps], sr[kSteps], si[kSteps], U[kSteps], PA = both(1.0f), PU = 0ull, PV = 0ull;
+    if (ts < len) {
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      ys[s] = xs[s] = rs[s] = is[s] = make_float2(0.0f, 0.0f);
-      if (any && ts + s < len) {
-        xs[s] = load_pair<T, kVec>(x + (ts + s) * a.sx.t, left);
-        rs[s] = load_pair<T, kVec>(r + (ts + s) * a.sr.t, left);
-        is[s] = load_pair<T, kVec>(in + (ts + s) * a.si.t, left);
-        ys[s] = load_pair<T, kVec>(dy + (ts + s) * a.sdy.t, left);
+      for (int s = 0; s < kSteps; ++s) {
+        const T* q = here + s * kLanes;
+        const Gates g = gates_of(staged_pair<T>(q + kOne), staged_pair<T>(q + 2 * kOne), rate, far);
+        uint64_t m, inv_m;
+        root_of(g.m2, m, inv_m);
+        low[s] = g.low;
+        sr[s] = g.sr;
+        si[s] = g.si;
+        U[s] = mul2(mul2(m, g.si), staged_pair<T>(q));
+      }
+      if (!whole) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+          if (ts + s >= len) low[s] = U[s] = 0ull;
+      }
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        const uint64_t A = fma2(low[s], both(-1.0f), both(1.0f));
+        if (resets >> s & 1u) PU = 0ull;
+        PU = fma2(A, PU, U[s]);
+        PA = mul2(PA, A);
+      }
+#pragma unroll
+      for (int s = kSteps - 1; s >= 0; --s) {  // staged dy is zero past the stream's length
+        const uint64_t A = fma2(low[s], both(-1.0f), both(1.0f));
+        PV = mul2(A, add2(PV, staged_pair<T>(here + 3 * kOne + s * kLanes)));
+        if (resets >> s & 1u) PV = 0ull;
       }
     }
-    float2 h = make_float2(0.0f, 0.0f);
-    if (any) h = load_pair<float, false>(a.states + (long long)(t0 / kTile) * a.B * a.D + state_at, left);
-    float2 A[kSteps], U[kSteps];
-    float2 PA = make_float2(1.0f, 1.0f), PU = make_float2(0.0f, 0.0f), PV = make_float2(0.0f, 0.0f);
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const Gates g0 = gates_of(rs[s].x, is[s].x, rate.x), g1 = gates_of(rs[s].y, is[s].y, rate.y);
-      const bool live = ts + s < len, cut = resets >> s & 1u;
-      A[s] = live ? make_float2(g0.a, g1.a) : make_float2(1.0f, 1.0f);
-      U[s] = live ? make_float2(g0.m * g0.si * xs[s].x, g1.m * g1.si * xs[s].y) : make_float2(0.0f, 0.0f);
-      PU.x = cut ? U[s].x : fmaf(A[s].x, PU.x, U[s].x);
-      PU.y = cut ? U[s].y : fmaf(A[s].y, PU.y, U[s].y);
-      PA.x *= A[s].x;
-      PA.y *= A[s].y;
-    }
-#pragma unroll
-    for (int s = kSteps - 1; s >= 0; --s) {
-      const bool cut = resets >> s & 1u;
-      PV.x = cut ? 0.0f : A[s].x * (ys[s].x + PV.x);
-      PV.y = cut ? 0.0f : A[s].y * (ys[s].y + PV.y);
-    }
-    Run& run = runs[turn];
-    run.A[warp][lane] = PA;
-    run.U[warp][lane] = PU;
-    back[turn][warp][lane] = PV;
-    if (lane == 0) run.cut[warp] = resets;
+    runs[turn].AU[warp][lane] = make_ulonglong2(PA, PU);
+    back[turn].AU[warp][lane] = make_ulonglong2(PA, PV);
+    if (lane == 0) runs[turn].cut[warp] = back[turn].cut[warp] = resets;
     __syncthreads();
-    for (int w = 0; w < warp; ++w) {
-      const float2 wa = run.A[w][lane], wu = run.U[w][lane];
-      const bool cut = run.cut[w] != 0;
-      h.x = cut ? wu.x : fmaf(wa.x, h.x, wu.x);
-      h.y = cut ? wu.y : fmaf(wa.y, h.y, wu.y);
-    }
-    float2 ps = p;
+    const Runs run = runs_of(runs[turn]), rev = runs_of(back[turn]), tiles = tile_runs(exchange, a.cluster, turn);
+    if (a.cluster > 1) {
+      ulonglong2 all = make_ulonglong2(both(1.0f), 0ull);
+      bool cut = false;
 #pragma unroll
-    for (int w = kWarps - 1; w >= 0; --w) {
-      const float2 wa = run.A[w][lane], wv = back[turn][w][lane];
-      const bool cut = run.cut[w] != 0;
-      if (w == warp) ps = p;
-      p.x = cut ? wv.x : fmaf(wa.x, p.x, wv.x);
-      p.y = cut ? wv.y : fmaf(wa.y, p.y, wv.y);
-    }
-    float2 before[kSteps];
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const bool cut = resets >> s & 1u;
-      before[s] = cut ? make_float2(0.0f, 0.0f) : h;
-      h.x = cut ? U[s].x : fmaf(A[s].x, h.x, U[s].x);
-      h.y = cut ? U[s].y : fmaf(A[s].y, h.y, U[s].y);
-    }
-#pragma unroll
-    for (int s = kSteps - 1; s >= 0; --s) {
-      const bool live = ts + s < len, cut = resets >> s & 1u;
-      float gx[2], gr[2], gi[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float rr = e ? rs[s].y : rs[s].x, ii = e ? is[s].y : is[s].x, xx = e ? xs[s].y : xs[s].x;
-        const float hh = e ? before[s].y : before[s].x, dd = e ? ys[s].y : ys[s].x;
-        float& pp = e ? ps.y : ps.x;
-        const Gates g = gates_of(rr, ii, e ? rate.y : rate.x);
-        const float grad = dd + pp;
-        if (live) pp = cut ? 0.0f : g.a * grad;
-        const float q = g.m > 0.0f ? -g.la * rcp_approx(g.m) : 0.0f;
-        const float E = grad * g.a * fmaf(g.la, hh, g.si * xx * g.a * q);
-        const float gm = grad * g.m * g.si;
-        gx[e] = live ? gm : 0.0f;
-        gr[e] = live ? E * (1.0f - g.sr) : 0.0f;
-        gi[e] = live ? gm * xx * (1.0f - g.si) : 0.0f;
-        if (live) (e ? sum.y : sum.x) += E;
+      for (int w = kWarps - 1; w >= 0; --w) {
+        all.x = mul2(all.x, rev.AU[w * 32 + lane].x);
+        all.y = after(rev, w, all.y);
+        cut = cut || rev.cut[w] != 0;
       }
-      if (any && ts + s < a.T) {
-        store_pair<T, kVec>(dx + (ts + s) * a.sdx.t, left, gx[0], gx[1]);
-        store_pair<T, kVec>(dr + (ts + s) * a.sdr.t, left, gr[0], gr[1]);
-        store_pair<T, kVec>(di + (ts + s) * a.sdi.t, left, gi[0], gi[1]);
+      send_run(tiles, rank, a.cluster, all, cut);
+      cluster_sync_all();
+    }
+    for (int w = 0; w < warp; ++w) h = after(run, w, h);
+    uint64_t ps = p;  // p after this block's tile, then after this warp's timesteps
+    if (a.cluster > 1) {
+      for (int k = a.cluster - 1; k >= 0; --k) {
+        if (k == rank) ps = p;
+        p = after(tiles, k, p);
+      }
+      for (int w = kWarps - 1; w > warp; --w) ps = after(rev, w, ps);
+    } else {
+#pragma unroll
+      for (int w = kWarps - 1; w >= 0; --w) {
+        if (w == warp) ps = p;
+        p = after(rev, w, p);
+      }
+    }
+    if (ts < len) {
+      // U becomes the state before each timestep
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        if (resets >> s & 1u) h = 0ull;
+        const uint64_t u = U[s];
+        U[s] = h;
+        h = fma2(fma2(low[s], both(-1.0f), both(1.0f)), h, u);
+      }
+#pragma unroll
+      for (int s = kSteps - 1; s >= 0; --s) {
+        if (!whole && ts + s >= len) {
+          if (left > 0 && ts + s < a.T) {
+            store_pair<T, kVec>(dx + (ts + s) * a.sdx.t, left, 0.0f, 0.0f);
+            store_pair<T, kVec>(dr + (ts + s) * a.sdr.t, left, 0.0f, 0.0f);
+            store_pair<T, kVec>(di + (ts + s) * a.sdi.t, left, 0.0f, 0.0f);
+          }
+          continue;
+        }
+        const uint64_t A = fma2(low[s], both(-1.0f), both(1.0f));
+        const uint64_t xs = staged_pair<T>(here + s * kLanes);
+        const uint64_t g = add2(ps, staged_pair<T>(here + 3 * kOne + s * kLanes));
+        const uint64_t ga = mul2(g, A);
+        ps = resets >> s & 1u ? 0ull : ga;
+        uint64_t m, inv_m;
+        root_of(mul2(low[s], fma2(low[s], both(-1.0f), both(2.0f))), m, inv_m);
+        const uint64_t t = mul2(rate, sr[s]);  // -log a
+        // E = g a (si x a (t / m) - t h)
+        const uint64_t sx = mul2(si[s], xs);
+        const uint64_t E = mul2(ga, mul2(t, fma2(mul2(sx, A), inv_m, mul2(U[s], both(-1.0f)))));
+        const uint64_t gm = mul2(g, mul2(m, si[s]));
+        const uint64_t gr = mul2(E, fma2(sr[s], both(-1.0f), both(1.0f)));
+        const uint64_t gi = mul2(mul2(gm, xs), fma2(si[s], both(-1.0f), both(1.0f)));
+        sum = add2(sum, E);
+        float v0, v1;
+        if (left > 0) {
+          f32x2_split(gm, v0, v1);
+          store_pair<T, kVec>(dx + (ts + s) * a.sdx.t, left, v0, v1);
+          f32x2_split(gr, v0, v1);
+          store_pair<T, kVec>(dr + (ts + s) * a.sdr.t, left, v0, v1);
+          f32x2_split(gi, v0, v1);
+          store_pair<T, kVec>(di + (ts + s) * a.sdi.t, left, v0, v1);
+        }
+      }
+    } else if (left > 0) {
+      for (int t = ts; t < min(ts + kSteps, a.T); ++t) {
+        store_pair<T, kVec>(dx + t * a.sdx.t, left, 0.0f, 0.0f);
+        store_pair<T, kVec>(dr + t * a.sdr.t, left, 0.0f, 0.0f);
+        store_pair<T, kVec>(di + t * a.sdi.t, left, 0.0f, 0.0f);
       }
     }
   }
   __syncthreads();
-  back[0][warp][lane] = sum;
+  runs[0].AU[warp][lane].x = sum;
   __syncthreads();
-  if (warp == 0 && any) {
-    for (int w = 1; w < kWarps; ++w) {
-      sum.x += back[0][w][lane].x;
-      sum.y += back[0][w][lane].y;
-    }
-    store_pair<float, false>(a.partial + state_at, left, sum.x, sum.y);
-    store_pair<float, false>(a.dh0 + state_at, left, p.x, p.y);
+  if (warp == 0) {
+    for (int w = 1; w < kWarps; ++w) sum = add2(sum, runs[0].AU[w][lane].x);
+    store_f32x2(a.partial + ((long long)b * a.cluster + rank) * a.D + ch, left, sum);
+    if (rank == 0) store_f32x2(a.dh0 + state_at, left, p);
   }
+  if (a.cluster > 1) cluster_sync_all();
 }
 
 // ddecay from partial [n][D], summed in a fixed order.
@@ -395,8 +663,7 @@ template <typename T, bool kVec>
 __global__ void __launch_bounds__(256) gated_step_kernel(const StepArgs a) {
   const int ch = 2 * (blockIdx.x * blockDim.x + threadIdx.x), left = a.D - ch;
   if (left <= 0) return;
-  const float2 d = load_pair<float, false>(a.decay + ch, left);
-  const float2 rate = make_float2(-a.c * softplus_f(d.x), -a.c * softplus_f(d.y));
+  const uint64_t rate = rate_of(a.decay + ch, left, a.c);
   for (int b = blockIdx.y; b < a.B; b += gridDim.y) {
     T* y = static_cast<T*>(a.y) + (long long)b * a.D + ch;
     const int slot = a.slots ? a.slots[b] : b;
@@ -408,26 +675,73 @@ __global__ void __launch_bounds__(256) gated_step_kernel(const StepArgs a) {
     const float2 r = load_pair<T, kVec>(static_cast<const T*>(a.r) + b * a.r_pitch + ch, left);
     const float2 i = load_pair<T, kVec>(static_cast<const T*>(a.i) + b * a.i_pitch + ch, left);
     float* st = a.state + (long long)slot * a.D + ch;
-    const bool cut = a.reset && a.reset[b] != 0;
-    const float2 h = load_pair<float, false>(st, left);
-    const Gates g0 = gates_of(r.x, i.x, rate.x), g1 = gates_of(r.y, i.y, rate.y);
-    const float u0 = g0.m * g0.si * x.x, u1 = g1.m * g1.si * x.y;
-    const float h0 = cut ? u0 : fmaf(g0.a, h.x, u0), h1 = cut ? u1 : fmaf(g1.a, h.y, u1);
-    store_pair<float, false>(st, left, h0, h1);
+    uint64_t h = load_f32x2(st, left);
+    if (a.reset && a.reset[b] != 0) h = 0ull;
+    const Gates g = gates_of(f32x2(r.x, r.y), f32x2(i.x, i.y), rate, true);
+    uint64_t m, inv_m;
+    root_of(g.m2, m, inv_m);
+    h = fma2(fma2(g.low, both(-1.0f), both(1.0f)), h, mul2(mul2(m, g.si), f32x2(x.x, x.y)));
+    store_f32x2(st, left, h);
+    float h0, h1;
+    f32x2_split(h, h0, h1);
     store_pair<T, kVec>(y, left, h0, h1);
   }
 }
 
-bool pair_ok(const void* p, size_t es, const Strides& s) {
-  return op_aligned(p, 2 * es) && s.t % 2 == 0 && s.b % 2 == 0;
+bool aligned_to(size_t bytes, const void* p, size_t es, const Strides& s) {
+  return op_aligned(p, bytes) && s.t * es % bytes == 0 && s.b * es % bytes == 0;
+}
+
+// The widest copy (see `stage`) that every tensor's addresses allow.
+int copy_bytes(int D, size_t es, const void* const* p, const Strides* s, int n) {
+  auto all = [&](size_t bytes) {
+    for (int k = 0; k < n; ++k)
+      if (!aligned_to(bytes, p[k], es, s[k])) return false;
+    return D * es % bytes == 0;
+  };
+  return all(16) ? 16 : (all(4) ? 4 : 2);
 }
 
 int check_sizes(int dtype, int T, int B, int D, float c, char* msg, int msg_len) {
   if (!op_float_dtype(dtype)) return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "dtype %d", dtype);
-  if (T < 0 || B < 0 || D < 1 || T > 0x7fffff00 || (long long)B * ((D + kLanes - 1) / kLanes) > 0x7fffffffll)
+  if (T < 0 || B < 0 || D < 1 || T > 0x7fffff00 || (long long)B * ((D + kLanes - 1) / kLanes) > 0x7fffffffll || (long long)B * kMaxCluster > 0x7fffffffll)
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "need T, B >= 0, D >= 1 and B ceil(D / 64) below 2^31");
   if (!(c > 0.0f)) return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "c must be positive");
   return LSTM_APPROX_OK;
+}
+
+// Blocks of a cluster that share a stream's 64 channels: doubled while the
+// blocks are fewer than two to an SM and each still has a tile to itself.
+int cluster_size(int T, int B, int D) {
+  const long long items = (long long)B * ((D + kLanes - 1) / kLanes);
+  int n = 1;
+  while (n < kMaxCluster && items * n < 2 * 152 && (long long)n * kTile < T) n *= 2;
+  return n;
+}
+
+template <typename T, int kCopy, int kTensors, typename A>
+cudaError_t launch_scan(void (*kern)(A), int cluster, int blocks, cudaStream_t s, const A& args) {
+  static thread_local DeviceSet ready;  // of the one kernel that this instance launches
+  constexpr size_t smem = kStages<T, kTensors> * kStageBytes<T, kTensors>;
+  constexpr int most = (int)(smem + exchange_bytes(kMaxCluster));
+  const cudaError_t e = once_per_device(&ready, [&] {
+    const cudaError_t e1 = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return e1 != cudaSuccess ? e1 : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+  });
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(kWarps * 32);
+  cfg.dynamicSmemBytes = smem + exchange_bytes(cluster);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kern, args);
 }
 
 // Strides of n tensors: HOST [2n], or all contiguous [T][B][D].
@@ -461,21 +775,25 @@ extern "C" int lstm_approx_gated_scan(int dtype, const void* x, const void* r, c
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "strides must not be negative");
   if (int rc = op_check_device(msg, msg_len)) return rc;
   if (B == 0) return LSTM_APPROX_OK;
-  const int slabs = (D + kLanes - 1) / kLanes;
-  ScanArgs a{x, r, i, y, st[0], st[1], st[2], st[3], decay, c, h0, lengths, reset, T, B, D, slabs, h_last, states};
-  const bool vec = D % 2 == 0 && pair_ok(x, es, st[0]) && pair_ok(r, es, st[1]) && pair_ok(i, es, st[2]) &&
-                   pair_ok(y, es, st[3]);
+  const int slabs = (D + kLanes - 1) / kLanes, n = cluster_size(T, B, D);
+  ScanArgs a{x, r, i, y, st[0], st[1], st[2], st[3], decay, c, h0, lengths, reset, T, B, D, slabs, n,
+             h_last, states};
+  const void* tensors[4] = {x, r, i, y};
+  const int copy = copy_bytes(D, es, tensors, st, 4);
   const cudaError_t e = op_for_type(dtype, [&](auto* t) {
     using E = std::remove_pointer_t<decltype(t)>;
-    return op_launch(vec ? gated_scan_kernel<E, true> : gated_scan_kernel<E, false>, dim3(slabs * B),
-                     dim3(kWarps * 32), 0, static_cast<cudaStream_t>(cuda_stream), a);
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    if (copy == 16) return launch_scan<E, 16, 3>(gated_scan_kernel<E, 16>, n, slabs * B * n, s, a);
+    if (copy == 4) return launch_scan<E, 4, 3>(gated_scan_kernel<E, 4>, n, slabs * B * n, s, a);
+    if constexpr (sizeof(E) == 2) return launch_scan<E, 2, 3>(gated_scan_kernel<E, 2>, n, slabs * B * n, s, a);
+    return cudaErrorInvalidValue;  // 32-bit values are always copied
   });
   return op_launched(e, "scan launch", msg, msg_len);
 }
 
 extern "C" size_t lstm_approx_gated_scan_workspace_bytes(int T, int B, int D) {
   if (T < 0 || B < 0 || D < 1) return 0;
-  return ((size_t)B * D * sizeof(float) + 15) / 16 * 16 + 16;
+  return ((size_t)B * cluster_size(T, B, D) * D * sizeof(float) + 15) / 16 * 16 + 16;
 }
 
 extern "C" int lstm_approx_gated_scan_backward(int dtype, const void* dy, const float* dh_last, const void* x,
@@ -505,22 +823,24 @@ extern "C" int lstm_approx_gated_scan_backward(int dtype, const void* dy, const 
   if (int rc = op_check_device(msg, msg_len)) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   float* partial = static_cast<float*>(workspace);
+  const int n = cluster_size(T, B, D);
   if (B > 0) {
     const int slabs = (D + kLanes - 1) / kLanes;
     ScanBackwardArgs a{dy,    x,     r,      i,       dx,    dr, di, st[0], st[1], st[2], st[3], st[4], st[5], st[6],
-                       dh_last, decay, c, states, lengths, reset, T,  B,  D,     slabs, dh0,   partial};
-    const bool vec = D % 2 == 0 && pair_ok(dy, es, st[0]) && pair_ok(x, es, st[1]) && pair_ok(r, es, st[2]) &&
-                     pair_ok(i, es, st[3]) && pair_ok(dx, es, st[4]) && pair_ok(dr, es, st[5]) &&
-                     pair_ok(di, es, st[6]);
+                       dh_last, decay, c, states, lengths, reset, T,  B,  D,     slabs, n, dh0,   partial};
+    const void* tensors[7] = {dy, x, r, i, dx, dr, di};
+    const int copy = copy_bytes(D, es, tensors, st, 7);
     const cudaError_t e = op_for_type(dtype, [&](auto* t) {
       using E = std::remove_pointer_t<decltype(t)>;
-      return op_launch(vec ? gated_scan_backward_kernel<E, true> : gated_scan_backward_kernel<E, false>,
-                       dim3(slabs * B), dim3(kWarps * 32), 0, s, a);
+      if (copy == 16) return launch_scan<E, 16, 4>(gated_scan_backward_kernel<E, 16>, n, slabs * B * n, s, a);
+      if (copy == 4) return launch_scan<E, 4, 4>(gated_scan_backward_kernel<E, 4>, n, slabs * B * n, s, a);
+      if constexpr (sizeof(E) == 2) return launch_scan<E, 2, 4>(gated_scan_backward_kernel<E, 2>, n, slabs * B * n, s, a);
+      return cudaErrorInvalidValue;
     });
     if (int rc = op_launched(e, "scan backward launch", msg, msg_len)) return rc;
   }
   const cudaError_t e = op_launch(decay_gradient_kernel, dim3((D + 31) / 32), dim3(32, 32), 0, s,
-                                  static_cast<const float*>(partial), B, D, decay, ddecay);
+                                  static_cast<const float*>(partial), B * n, D, decay, ddecay);
   return op_launched(e, "decay gradient launch", msg, msg_len);
 }
 
@@ -541,8 +861,8 @@ extern "C" int lstm_approx_gated_step(int dtype, const void* x, long long x_pitc
   if (int rc = op_check_device(msg, msg_len)) return rc;
   if (B == 0) return LSTM_APPROX_OK;
   StepArgs a{x, r, i, x_pitch, r_pitch, i_pitch, decay, c, state, n_slots, slots, reset, B, D, y};
-  const bool vec = D % 2 == 0 && pair_ok(x, es, {0, x_pitch}) && pair_ok(r, es, {0, r_pitch}) &&
-                   pair_ok(i, es, {0, i_pitch}) && op_aligned(y, 2 * es);
+  const bool vec = D % 2 == 0 && aligned_to(2 * es, x, es, {0, x_pitch}) && aligned_to(2 * es, r, es, {0, r_pitch}) &&
+                   aligned_to(2 * es, i, es, {0, i_pitch}) && op_aligned(y, 2 * es);
   const int threads = D >= 512 ? 256 : 64;
   const dim3 grid((D + 2 * threads - 1) / (2 * threads), std::min(B, 65535));
   const cudaError_t e = op_for_type(dtype, [&](auto* t) {

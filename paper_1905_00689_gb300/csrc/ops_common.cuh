@@ -10,7 +10,7 @@
 #include <cstdio>
 
 #include "../../include/lstm_approx_ops.h"
-#include "device_set.h"
+#include "internal.h"
 
 namespace lstm_approx_impl {
 
