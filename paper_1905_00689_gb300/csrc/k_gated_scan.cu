@@ -58,58 +58,75 @@ __device__ __forceinline__ float softplus_ratio_f(float d) {
   return sp > 0.0f ? sig / sp : 1.0f;
 }
 
-// x for x <= 60, else 60; NaN stays NaN.
-__device__ __forceinline__ float at_most_60(float x) {
-  float r;
-  asm("min.NaN.f32 %0, %1, 0f42700000;" : "=f"(r) : "f"(x));
-  return r;
-}
 __device__ __forceinline__ float rsqrt_approx(float x) {
   float r;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+__device__ __forceinline__ float sqrt_approx(float x) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ uint64_t both(float v) { return f32x2(v, v); }
+__device__ __forceinline__ uint64_t sub2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// The constants of the loops below, kept in registers: an instruction on two
+// values takes no immediate, and left to itself the compiler forms the pairs
+// anew at every use (a third of all instructions).
+struct Constants {
+  uint64_t one, minus_log2e, c1, c2, c3, c4;
+};
+__device__ __forceinline__ uint64_t held(float v) {
+  uint64_t r;
+  asm volatile("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ Constants constants() {
+  return {held(1.0f), held(-kLog2E), held(-0.5f), held(1.0f / 6.0f), held(-1.0f / 24.0f), held(1.0f / 120.0f)};
+}
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t z, const Constants& k) {
+  float a, b;
+  f32x2_split(mul2(z, k.minus_log2e), a, b);
+  f32x2_split(add2(f32x2(ex2_approx(a), ex2_approx(b)), k.one), a, b);
+  return f32x2(rcp_approx(a), rcp_approx(b));
+}
 
 // The gates of a lane's two channels (pairs of fp32, two per instruction where
-// there is one for two): sigma(r), sigma(i), 1 - a and 1 - a^2, from which a
-// and m follow.  rate = c softplus(decay); far: -log a may be above 0.35.
+// there is one for two): sigma(r), sigma(i) and 1 - a, from which a and m
+// follow.  rate = c softplus(decay), the largest -log a; far: it is above 1/8.
 //
-// Both sigmoids come from one reciprocal of the product of their denominators
-// (the special-function unit, four operations to a channel, is what the scan
-// meets next after memory); so that the product stays finite, e^-z is taken at
-// most 2^60, which moves a sigmoid below 9e-19 up to that.
-//
-// 1 - a = 1 - e^-t by its Taylor series to t^8 for t <= 0.35 (the first term
-// left out is below 7e-10 of the first): no cancellation, a = 1 - (1 - a) comes
-// out correctly rounded, which matters where a state decays over hundreds of
-// timesteps, and 1 - a^2 = (1 - a)(2 - (1 - a)) keeps its digits.
+// 1 - a = 1 - e^-t by its Taylor series: no cancellation, a = 1 - (1 - a)
+// comes out correctly rounded, which matters where a state decays over hundreds
+// of timesteps, and 1 - a^2 = (1 - a)(1 + a) keeps its digits.  Up to t = 1/8
+// (decays down to 0.88 where the gate is open) five terms do (the sixth is
+// below 4.3e-8 of the first); beyond, eight up to t = 0.35 (the ninth is below
+// 7e-10), and the exponential itself above that.
 struct Gates {
-  uint64_t sr, si, low, m2;
+  uint64_t sr, si, low;
 };
-__device__ __forceinline__ uint64_t both(float v) { return f32x2(v, v); }
-__device__ __forceinline__ Gates gates_of(uint64_t r, uint64_t i, uint64_t rate, bool far) {
-  float r0, r1, i0, i1;
-  f32x2_split(mul2(r, both(-kLog2E)), r0, r1);
-  f32x2_split(mul2(i, both(-kLog2E)), i0, i1);
-  const uint64_t dr = add2(f32x2(ex2_approx(at_most_60(r0)), ex2_approx(at_most_60(r1))), both(1.0f));
-  const uint64_t di = add2(f32x2(ex2_approx(at_most_60(i0)), ex2_approx(at_most_60(i1))), both(1.0f));
-  float d0, d1;
-  f32x2_split(mul2(dr, di), d0, d1);
-  const uint64_t inv = f32x2(rcp_approx(d0), rcp_approx(d1));
+template <bool kFar>
+__device__ __forceinline__ Gates gates_of(uint64_t r, uint64_t i, uint64_t rate, const Constants& k) {
   Gates g;
-  g.sr = mul2(inv, di);
-  g.si = mul2(inv, dr);
+  g.sr = sigmoid2(r, k);
+  g.si = sigmoid2(i, k);
   const uint64_t t = mul2(rate, g.sr);
-  uint64_t p = both(-1.0f / 40320.0f);
-  p = fma2(p, t, both(1.0f / 5040.0f));
-  p = fma2(p, t, both(-1.0f / 720.0f));
-  p = fma2(p, t, both(1.0f / 120.0f));
-  p = fma2(p, t, both(-1.0f / 24.0f));
-  p = fma2(p, t, both(1.0f / 6.0f));
-  p = fma2(p, t, both(-0.5f));
-  p = fma2(p, t, both(1.0f));
+  uint64_t p = k.c4;
+  if constexpr (kFar) {
+    p = both(-1.0f / 40320.0f);
+    p = fma2(p, t, both(1.0f / 5040.0f));
+    p = fma2(p, t, both(-1.0f / 720.0f));
+    p = fma2(p, t, k.c4);
+  }
+  p = fma2(p, t, k.c3);
+  p = fma2(p, t, k.c2);
+  p = fma2(p, t, k.c1);
+  p = fma2(p, t, k.one);
   g.low = mul2(t, p);
-  if (far) {
+  if constexpr (kFar) {
     float t0, t1, l0, l1;
     f32x2_split(t, t0, t1);
     f32x2_split(g.low, l0, l1);
@@ -117,16 +134,23 @@ __device__ __forceinline__ Gates gates_of(uint64_t r, uint64_t i, uint64_t rate,
     if (t1 > 0.35f) l1 = 1.0f - ex2_approx(-t1 * kLog2E);
     g.low = f32x2(l0, l1);
   }
-  g.m2 = mul2(g.low, fma2(g.low, both(-1.0f), both(2.0f)));
   return g;
 }
-
-// m = sqrt(m2) and 1 / m, the latter at most 2^63 (m2 = 0 gives m = 0).
-__device__ __forceinline__ void root_of(uint64_t m2, uint64_t& m, uint64_t& inv_m) {
+__device__ __forceinline__ uint64_t decay_of(uint64_t low, const Constants& k) { return sub2(k.one, low); }
+// 1 - a^2
+__device__ __forceinline__ uint64_t m2_of(uint64_t low, uint64_t a, const Constants& k) {
+  return mul2(low, add2(a, k.one));
+}
+__device__ __forceinline__ uint64_t sqrt2(uint64_t v) {
   float a, b;
-  f32x2_split(m2, a, b);
-  inv_m = f32x2(rsqrt_approx(fmaxf(a, 1.17549435e-38f)), rsqrt_approx(fmaxf(b, 1.17549435e-38f)));
-  m = mul2(m2, inv_m);
+  f32x2_split(v, a, b);
+  return f32x2(sqrt_approx(a), sqrt_approx(b));
+}
+// 1 / sqrt(v), at most 2^63
+__device__ __forceinline__ uint64_t rsqrt2(uint64_t v) {
+  float a, b;
+  f32x2_split(add2(v, both(1.17549435e-38f)), a, b);
+  return f32x2(rsqrt_approx(a), rsqrt_approx(b));
 }
 
 // The pair of channels (ch, ch + 1) at p; kVec: both exist and lie in one
@@ -177,19 +201,29 @@ __device__ __forceinline__ void stage(T* dst, const T* src, long long stride, in
     constexpr int kRow = kLanes / kPer;                   // copies of a row
     constexpr int kRows = kRow >= 32 ? 1 : 32 / kRow;     // rows of one turn of the warp
     constexpr int kTurns = kRow >= 32 ? kRow / 32 : 1;    // turns of one row
+    const int row0 = kRow >= 32 ? 0 : lane / kRow;
+    auto copy = [&](uint32_t to, const T* from, int bytes) {
+      if constexpr (kCopy == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+      else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+    };
+    const T* from = src + (ts + row0) * stride + lane % kRow * kPer;
+    const uint32_t to = smem_u32(dst + row0 * kLanes + lane % kRow * kPer);
+    const bool whole = ts + kSteps <= len && ch0 + kLanes <= D;
 #pragma unroll
     for (int s = 0; s < kSteps; s += kRows) {
 #pragma unroll
       for (int q = 0; q < kTurns; ++q) {
-        const int row = s + lane / kRow % kRows, col = (lane % kRow + 32 * q) * kPer;
-        const bool in = ts + row < len && ch0 + col < D;
-        const T* from = in ? src + (ts + row) * stride + col : src;
-        const uint32_t to = smem_u32(dst + row * kLanes + col);
-        if constexpr (kCopy == 16)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(in ? 16 : 0) : "memory");
-        else
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(in ? 4 : 0) : "memory");
+        const uint32_t at = to + (s * kLanes + 32 * q * kPer) * (int)sizeof(T);
+        if (whole) {
+          copy(at, from + 32 * q * kPer, kCopy);
+        } else {
+          const bool in = ts + s + row0 < len && ch0 + (lane % kRow + 32 * q) * kPer < D;
+          copy(at, in ? from + 32 * q * kPer : src, in ? kCopy : 0);
+        }
       }
+      from += kRows * stride;
     }
   } else {
 #pragma unroll
@@ -249,10 +283,11 @@ struct WarpRuns {
 };
 __device__ __forceinline__ Runs runs_of(WarpRuns& w) { return {&w.AU[0][0], w.cut}; }
 
-// h after run k.
-__device__ __forceinline__ uint64_t after(const Runs& r, int k, uint64_t h) {
+// h after run k; cuts: some run may have a reset.
+__device__ __forceinline__ uint64_t after(const Runs& r, int k, uint64_t h, bool cuts) {
   const ulonglong2 v = r.AU[k * 32 + (threadIdx.x & 31)];
-  return r.cut[k] != 0 ? v.y : fma2(v.x, h, v.y);
+  if (cuts && r.cut[k] != 0) h = 0ull;
+  return fma2(v.x, h, v.y);
 }
 
 // The exchange buffer of parity `turn` behind the staged tiles: a run for each block of the cluster.
@@ -297,15 +332,50 @@ __device__ __forceinline__ void store_f32x2(float* p, int left, uint64_t v) {
   if (left > 1) p[1] = b;
 }
 
+template <typename T, bool kVec>
+__device__ __forceinline__ void store_both(T* p, int left, uint64_t v) {
+  float a, b;
+  f32x2_split(v, a, b);
+  store_pair<T, kVec>(p, left, a, b);
+}
+
+// a_t and m_t sigma(i_t) x_t of a warp's staged timesteps.
+template <typename T, bool kFar>
+__device__ __forceinline__ void form_runs(const T* here, uint64_t rate, const Constants& k, uint64_t (&A)[kSteps],
+                                          uint64_t (&U)[kSteps]) {
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const T* p = here + s * kLanes;
+    const Gates g =
+        gates_of<kFar>(staged_pair<T>(p + kTile * kLanes), staged_pair<T>(p + 2 * kTile * kLanes), rate, k);
+    A[s] = decay_of(g.low, k);
+    U[s] = mul2(mul2(sqrt2(m2_of(g.low, A[s], k)), g.si), staged_pair<T>(p));
+  }
+}
+
+// The run of a warp's timesteps (kCuts: with resets at the set bits).
+template <bool kCuts>
+__device__ __forceinline__ ulonglong2 join_steps(const uint64_t (&A)[kSteps], const uint64_t (&U)[kSteps], unsigned resets,
+                                                 const Constants& k) {
+  uint64_t PA = k.one, PU = 0ull;
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    if (kCuts && (resets >> s & 1u)) PU = 0ull;
+    PU = fma2(A[s], PU, U[s]);
+    PA = mul2(PA, A[s]);
+  }
+  return make_ulonglong2(PA, PU);
+}
+
 // c softplus(decay) of a lane's channels, zero for one that does not exist.
 __device__ __forceinline__ uint64_t rate_of(const float* decay, int left, float c) {
   return f32x2(left > 0 ? c * softplus_f(decay[0]) : 0.0f, left > 1 ? c * softplus_f(decay[1]) : 0.0f);
 }
-// Whether -log a of some lane may be above 0.35.
+// Whether -log a of some lane may be above 1/8.
 __device__ __forceinline__ bool any_far(uint64_t rate) {
   float r0, r1;
   f32x2_split(rate, r0, r1);
-  return __any_sync(0xffffffffu, !(r0 <= 0.35f && r1 <= 0.35f));
+  return __any_sync(0xffffffffu, !(r0 <= 0.125f && r1 <= 0.125f));
 }
 
 template <typename T, int kCopy>
@@ -326,6 +396,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const ScanAr
   T* y = static_cast<T*>(a.y) + b * a.sy.b + ch;
   const long long state_at = (long long)b * a.D + ch;
   const int stride = a.cluster * kTile;
+  const bool cuts = a.reset != nullptr;
   auto buffer = [&](int n) { return reinterpret_cast<T*>(staged + n * kStageBytes<T, 3>) + warp * kSteps * kLanes; };
   auto fetch = [&](int n, int first) {  // this warp's part of the tile that starts at `first` + rank tiles, if there is one
     T* to = buffer(n);
@@ -341,6 +412,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const ScanAr
   for (int n = 0; n < kN - 1; ++n) fetch(n, n * stride);
   const uint64_t rate = rate_of(a.decay + ch, left, a.c);
   const bool far = any_far(rate);
+  const Constants k = constants();
   uint64_t h = a.h0 ? load_f32x2(a.h0 + state_at, left) : 0ull;
   // shared memory of another block is written only after that block has started
   if (a.cluster > 1) cluster_sync_all();
@@ -354,44 +426,30 @@ __global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const ScanAr
     fetch(next, first + (kN - 1) * stride);  // into the stage that the last turn read
     at = at + 1 == kN ? 0 : at + 1;
     next = next + 1 == kN ? 0 : next + 1;
-    uint64_t A[kSteps], U[kSteps], PA = both(1.0f), PU = 0ull;
-    const bool whole = ts + kSteps <= len;
-    if (ts < len) {
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const T* p = here + s * kLanes;
-        const Gates g = gates_of(staged_pair<T>(p + kTile * kLanes), staged_pair<T>(p + 2 * kTile * kLanes), rate, far);
-        uint64_t m, inv_m;
-        root_of(g.m2, m, inv_m);
-        A[s] = fma2(g.low, both(-1.0f), both(1.0f));
-        U[s] = mul2(mul2(m, g.si), staged_pair<T>(p));
-      }
-      if (!whole) {
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s)
-          if (ts + s >= len) A[s] = both(1.0f), U[s] = 0ull;
-      }
-    } else {
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) A[s] = both(1.0f), U[s] = 0ull;
+    uint64_t A[kSteps], U[kSteps];
+    const bool whole = ts + kSteps <= len;  // and `some` of its timesteps are the stream's
+    const bool some = ts < len;
+    if (some) {
+      if (far) form_runs<T, true>(here, rate, k, A, U);
+      else form_runs<T, false>(here, rate, k, A, U);
     }
+    if (!whole) {
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      if (resets >> s & 1u) PU = 0ull;
-      PU = fma2(A[s], PU, U[s]);
-      PA = mul2(PA, A[s]);
+      for (int s = 0; s < kSteps; ++s)
+        if (ts + s >= len) A[s] = k.one, U[s] = 0ull;
     }
-    runs[turn].AU[warp][lane] = make_ulonglong2(PA, PU);  // the other parity's may still be read
+    const ulonglong2 PR = resets ? join_steps<true>(A, U, resets, k) : join_steps<false>(A, U, 0u, k);
+    runs[turn].AU[warp][lane] = PR;  // the other parity's may still be read
     if (lane == 0) runs[turn].cut[warp] = resets;
     __syncthreads();
     const Runs run = runs_of(runs[turn]), tiles = tile_runs(exchange, a.cluster, turn);
     if (a.cluster > 1) {
-      ulonglong2 all = make_ulonglong2(both(1.0f), 0ull);
+      ulonglong2 all = make_ulonglong2(k.one, 0ull);
       bool cut = false;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         all.x = mul2(all.x, run.AU[w * 32 + lane].x);
-        all.y = after(run, w, all.y);
+        all.y = after(run, w, all.y, cuts);
         cut = cut || run.cut[w] != 0;
       }
       send_run(tiles, rank, a.cluster, all, cut);
@@ -399,32 +457,42 @@ __global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const ScanAr
     }
     uint64_t hs = h;  // the state before this block's tile, then before this warp's timesteps
     if (a.cluster > 1) {
-      for (int k = 0; k < a.cluster; ++k) {
-        if (k == rank) hs = h;
-        h = after(tiles, k, h);
+      for (int n = 0; n < a.cluster; ++n) {
+        if (n == rank) hs = h;
+        h = after(tiles, n, h, cuts);
       }
     }
     if (a.states && warp == 0 && t0 < a.T)
       store_f32x2(a.states + (long long)(t0 / kTile) * a.B * a.D + state_at, left, hs);
     if (a.cluster > 1) {
-      for (int w = 0; w < warp; ++w) hs = after(run, w, hs);
+      for (int w = 0; w < warp; ++w) hs = after(run, w, hs, cuts);
     } else {
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         if (w == warp) hs = h;
-        h = after(run, w, h);
+        h = after(run, w, h, cuts);
       }
     }
-    T* to = y + ts * a.sy.t;
+    if (resets) {
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      if (resets >> s & 1u) hs = 0ull;
-      hs = fma2(A[s], hs, U[s]);
-      float h0, h1;
-      f32x2_split(hs, h0, h1);
-      if (!whole && ts + s >= len) h0 = h1 = 0.0f;
-      if (left > 0 && (whole || ts + s < a.T)) store_pair<T, kVec>(to, left, h0, h1);
-      to += a.sy.t;
+      for (int s = 0; s < kSteps; ++s) {
+        if (resets >> s & 1u) hs = 0ull;
+        hs = U[s] = fma2(A[s], hs, U[s]);
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) hs = U[s] = fma2(A[s], hs, U[s]);
+    }
+    if (left > 0) {
+      T* to = y + ts * a.sy.t;
+      if (whole) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s, to += a.sy.t) store_both<T, kVec>(to, left, U[s]);
+      } else {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s, to += a.sy.t)
+          if (ts + s < a.T) store_both<T, kVec>(to, left, ts + s < len ? U[s] : 0ull);
+      }
     }
   }
   if (warp == 0 && rank == 0) store_f32x2(a.h_last + state_at, left, h);
@@ -446,6 +514,62 @@ struct ScanBackwardArgs {
   float* dh0;
   float* partial;  // [B][cluster][D]: each block's sum of E over its timesteps
 };
+
+// 1 - a_t, the gates and m_t sigma(i_t) x_t of a warp's staged timesteps.
+template <typename T, bool kFar>
+__device__ __forceinline__ void form_gates(const T* here, uint64_t rate, const Constants& k, uint64_t (&low)[kSteps],
+                                           uint64_t (&sr)[kSteps], uint64_t (&si)[kSteps], uint64_t (&U)[kSteps]) {
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const T* p = here + s * kLanes;
+    const Gates g =
+        gates_of<kFar>(staged_pair<T>(p + kTile * kLanes), staged_pair<T>(p + 2 * kTile * kLanes), rate, k);
+    low[s] = g.low;
+    sr[s] = g.sr;
+    si[s] = g.si;
+    U[s] = mul2(mul2(sqrt2(m2_of(g.low, decay_of(g.low, k), k)), g.si), staged_pair<T>(p));
+  }
+}
+
+// The runs of a warp's timesteps, h -> A h + U forward and p -> A p + V back
+// (staged dy is zero past the stream's length).
+template <typename T, bool kCuts>
+__device__ __forceinline__ void join_both(const T* here, const uint64_t (&low)[kSteps], const uint64_t (&U)[kSteps],
+                                          unsigned resets, const Constants& k, uint64_t& PA, uint64_t& PU, uint64_t& PV) {
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const uint64_t A = decay_of(low[s], k);
+    if (kCuts && (resets >> s & 1u)) PU = 0ull;
+    PU = fma2(A, PU, U[s]);
+    PA = mul2(PA, A);
+  }
+#pragma unroll
+  for (int s = kSteps - 1; s >= 0; --s) {
+    PV = mul2(decay_of(low[s], k), add2(PV, staged_pair<T>(here + 3 * kTile * kLanes + s * kLanes)));
+    if (kCuts && (resets >> s & 1u)) PV = 0ull;
+  }
+}
+
+struct Gradients {
+  uint64_t x, r, i, E;
+};
+// The gradients of the staged timestep at `here`, from p after it, which
+// becomes p before it; h: the state before it.
+template <typename T>
+__device__ __forceinline__ Gradients gradients_of(const T* here, uint64_t low, uint64_t sr, uint64_t si, uint64_t h,
+                                                  uint64_t rate, const Constants& k, uint64_t& p) {
+  const uint64_t A = decay_of(low, k), xs = staged_pair<T>(here);
+  const uint64_t g = add2(p, staged_pair<T>(here + 3 * kTile * kLanes));
+  p = mul2(g, A);
+  const uint64_t m2 = m2_of(low, A, k), inv_m = rsqrt2(m2);
+  const uint64_t t = mul2(rate, sr);  // -log a
+  Gradients d;
+  d.E = mul2(mul2(p, t), sub2(mul2(mul2(mul2(si, xs), A), inv_m), h));  // g a t (si x a / m - h)
+  d.x = mul2(g, mul2(mul2(m2, inv_m), si));
+  d.r = mul2(d.E, sub2(k.one, sr));
+  d.i = mul2(mul2(d.x, xs), sub2(k.one, si));
+  return d;
+}
 
 template <typename T, int kCopy>
 __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_scan_backward_kernel(const ScanBackwardArgs a) {
@@ -470,6 +594,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
   T* di = static_cast<T*>(a.di) + b * a.sdi.b + ch;
   const long long state_at = (long long)b * a.D + ch;
   const int stride = a.cluster * kTile;
+  const bool cuts = a.reset != nullptr;
   auto buffer = [&](int n) { return reinterpret_cast<T*>(staged + n * kStageBytes<T, 4>) + warp * kSteps * kLanes; };
   auto fetch = [&](int n, int first) {
     T* to = buffer(n);
@@ -487,6 +612,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
   for (int n = 0; n < kN - 1; ++n) fetch(n, last - n * stride);
   const uint64_t rate = rate_of(a.decay + ch, left, a.c);
   const bool far = any_far(rate);
+  const Constants k = constants();
   uint64_t p = a.dh_last ? load_f32x2(a.dh_last + state_at, left) : 0ull, sum = 0ull;
   if (a.cluster > 1) cluster_sync_all();
   int turn = 0, at = 0, next = kN - 1;
@@ -500,37 +626,18 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
     at = at + 1 == kN ? 0 : at + 1;
     next = next + 1 == kN ? 0 : next + 1;
     const bool whole = ts + kSteps <= len;
-    uint64_t low[kSteps], sr[kSteps], si[kSteps], U[kSteps], PA = both(1.0f), PU = 0ull, PV = 0ull;
-    if (ts < len) {
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const T* q = here + s * kLanes;
-        const Gates g = gates_of(staged_pair<T>(q + kOne), staged_pair<T>(q + 2 * kOne), rate, far);
-        uint64_t m, inv_m;
-        root_of(g.m2, m, inv_m);
-        low[s] = g.low;
-        sr[s] = g.sr;
-        si[s] = g.si;
-        U[s] = mul2(mul2(m, g.si), staged_pair<T>(q));
-      }
+    const bool some = ts < len;
+    uint64_t low[kSteps], sr[kSteps], si[kSteps], U[kSteps], PA = k.one, PU = 0ull, PV = 0ull;
+    if (some) {
+      if (far) form_gates<T, true>(here, rate, k, low, sr, si, U);
+      else form_gates<T, false>(here, rate, k, low, sr, si, U);
       if (!whole) {
 #pragma unroll
         for (int s = 0; s < kSteps; ++s)
           if (ts + s >= len) low[s] = U[s] = 0ull;
       }
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const uint64_t A = fma2(low[s], both(-1.0f), both(1.0f));
-        if (resets >> s & 1u) PU = 0ull;
-        PU = fma2(A, PU, U[s]);
-        PA = mul2(PA, A);
-      }
-#pragma unroll
-      for (int s = kSteps - 1; s >= 0; --s) {  // staged dy is zero past the stream's length
-        const uint64_t A = fma2(low[s], both(-1.0f), both(1.0f));
-        PV = mul2(A, add2(PV, staged_pair<T>(here + 3 * kOne + s * kLanes)));
-        if (resets >> s & 1u) PV = 0ull;
-      }
+      if (resets) join_both<T, true>(here, low, U, resets, k, PA, PU, PV);
+      else join_both<T, false>(here, low, U, 0u, k, PA, PU, PV);
     }
     runs[turn].AU[warp][lane] = make_ulonglong2(PA, PU);
     back[turn].AU[warp][lane] = make_ulonglong2(PA, PV);
@@ -538,74 +645,82 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
     __syncthreads();
     const Runs run = runs_of(runs[turn]), rev = runs_of(back[turn]), tiles = tile_runs(exchange, a.cluster, turn);
     if (a.cluster > 1) {
-      ulonglong2 all = make_ulonglong2(both(1.0f), 0ull);
+      ulonglong2 all = make_ulonglong2(k.one, 0ull);
       bool cut = false;
 #pragma unroll
       for (int w = kWarps - 1; w >= 0; --w) {
         all.x = mul2(all.x, rev.AU[w * 32 + lane].x);
-        all.y = after(rev, w, all.y);
+        all.y = after(rev, w, all.y, cuts);
         cut = cut || rev.cut[w] != 0;
       }
       send_run(tiles, rank, a.cluster, all, cut);
       cluster_sync_all();
     }
-    for (int w = 0; w < warp; ++w) h = after(run, w, h);
+    for (int w = 0; w < warp; ++w) h = after(run, w, h, cuts);
     uint64_t ps = p;  // p after this block's tile, then after this warp's timesteps
     if (a.cluster > 1) {
-      for (int k = a.cluster - 1; k >= 0; --k) {
-        if (k == rank) ps = p;
-        p = after(tiles, k, p);
+      for (int n = a.cluster - 1; n >= 0; --n) {
+        if (n == rank) ps = p;
+        p = after(tiles, n, p, cuts);
       }
-      for (int w = kWarps - 1; w > warp; --w) ps = after(rev, w, ps);
+      for (int w = kWarps - 1; w > warp; --w) ps = after(rev, w, ps, cuts);
     } else {
 #pragma unroll
       for (int w = kWarps - 1; w >= 0; --w) {
         if (w == warp) ps = p;
-        p = after(rev, w, p);
+        p = after(rev, w, p, cuts);
       }
     }
-    if (ts < len) {
+    if (some) {
       // U becomes the state before each timestep
+      if (resets) {
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        if (resets >> s & 1u) h = 0ull;
-        const uint64_t u = U[s];
-        U[s] = h;
-        h = fma2(fma2(low[s], both(-1.0f), both(1.0f)), h, u);
-      }
-#pragma unroll
-      for (int s = kSteps - 1; s >= 0; --s) {
-        if (!whole && ts + s >= len) {
-          if (left > 0 && ts + s < a.T) {
-            store_pair<T, kVec>(dx + (ts + s) * a.sdx.t, left, 0.0f, 0.0f);
-            store_pair<T, kVec>(dr + (ts + s) * a.sdr.t, left, 0.0f, 0.0f);
-            store_pair<T, kVec>(di + (ts + s) * a.sdi.t, left, 0.0f, 0.0f);
-          }
-          continue;
+        for (int s = 0; s < kSteps; ++s) {
+          if (resets >> s & 1u) h = 0ull;
+          const uint64_t u = U[s];
+          U[s] = h;
+          h = fma2(decay_of(low[s], k), h, u);
         }
-        const uint64_t A = fma2(low[s], both(-1.0f), both(1.0f));
-        const uint64_t xs = staged_pair<T>(here + s * kLanes);
-        const uint64_t g = add2(ps, staged_pair<T>(here + 3 * kOne + s * kLanes));
-        const uint64_t ga = mul2(g, A);
-        ps = resets >> s & 1u ? 0ull : ga;
-        uint64_t m, inv_m;
-        root_of(mul2(low[s], fma2(low[s], both(-1.0f), both(2.0f))), m, inv_m);
-        const uint64_t t = mul2(rate, sr[s]);  // -log a
-        // E = g a (si x a (t / m) - t h)
-        const uint64_t sx = mul2(si[s], xs);
-        const uint64_t E = mul2(ga, mul2(t, fma2(mul2(sx, A), inv_m, mul2(U[s], both(-1.0f)))));
-        const uint64_t gm = mul2(g, mul2(m, si[s]));
-        const uint64_t gr = mul2(E, fma2(sr[s], both(-1.0f), both(1.0f)));
-        const uint64_t gi = mul2(mul2(gm, xs), fma2(si[s], both(-1.0f), both(1.0f)));
-        sum = add2(sum, E);
-        float v0, v1;
-        if (left > 0) {
-          f32x2_split(gm, v0, v1);
-          store_pair<T, kVec>(dx + (ts + s) * a.sdx.t, left, v0, v1);
-          f32x2_split(gr, v0, v1);
-          store_pair<T, kVec>(dr + (ts + s) * a.sdr.t, left, v0, v1);
-          f32x2_split(gi, v0, v1);
-          store_pair<T, kVec>(di + (ts + s) * a.sdi.t, left, v0, v1);
+      } else {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const uint64_t u = U[s];
+          U[s] = h;
+          h = fma2(decay_of(low[s], k), h, u);
+        }
+      }
+      // from the warp's last timestep back
+      T* to_x = dx + (ts + kSteps - 1) * a.sdx.t;
+      T* to_r = dr + (ts + kSteps - 1) * a.sdr.t;
+      T* to_i = di + (ts + kSteps - 1) * a.sdi.t;
+      if (whole && left > 0) {
+#pragma unroll
+        for (int s = kSteps - 1; s >= 0; --s) {
+          const Gradients g = gradients_of<T>(here + s * kLanes, low[s], sr[s], si[s], U[s], rate, k, ps);
+          if (resets && (resets >> s & 1u)) ps = 0ull;
+          sum = add2(sum, g.E);
+          store_both<T, kVec>(to_x, left, g.x);
+          store_both<T, kVec>(to_r, left, g.r);
+          store_both<T, kVec>(to_i, left, g.i);
+          to_x -= a.sdx.t;
+          to_r -= a.sdr.t;
+          to_i -= a.sdi.t;
+        }
+      } else {
+#pragma unroll
+        for (int s = kSteps - 1; s >= 0; --s) {
+          Gradients g = {0ull, 0ull, 0ull, 0ull};
+          if (ts + s < len) g = gradients_of<T>(here + s * kLanes, low[s], sr[s], si[s], U[s], rate, k, ps);
+          if (resets >> s & 1u) ps = 0ull;
+          sum = add2(sum, g.E);
+          if (left > 0 && ts + s < a.T) {
+            store_both<T, kVec>(to_x, left, g.x);
+            store_both<T, kVec>(to_r, left, g.r);
+            store_both<T, kVec>(to_i, left, g.i);
+          }
+          to_x -= a.sdx.t;
+          to_r -= a.sdr.t;
+          to_i -= a.sdi.t;
         }
       }
     } else if (left > 0) {
@@ -664,6 +779,7 @@ __global__ void __launch_bounds__(256) gated_step_kernel(const StepArgs a) {
   const int ch = 2 * (blockIdx.x * blockDim.x + threadIdx.x), left = a.D - ch;
   if (left <= 0) return;
   const uint64_t rate = rate_of(a.decay + ch, left, a.c);
+  const Constants k = constants();
   for (int b = blockIdx.y; b < a.B; b += gridDim.y) {
     T* y = static_cast<T*>(a.y) + (long long)b * a.D + ch;
     const int slot = a.slots ? a.slots[b] : b;
@@ -677,10 +793,9 @@ __global__ void __launch_bounds__(256) gated_step_kernel(const StepArgs a) {
     float* st = a.state + (long long)slot * a.D + ch;
     uint64_t h = load_f32x2(st, left);
     if (a.reset && a.reset[b] != 0) h = 0ull;
-    const Gates g = gates_of(f32x2(r.x, r.y), f32x2(i.x, i.y), rate, true);
-    uint64_t m, inv_m;
-    root_of(g.m2, m, inv_m);
-    h = fma2(fma2(g.low, both(-1.0f), both(1.0f)), h, mul2(mul2(m, g.si), f32x2(x.x, x.y)));
+    const Gates g = gates_of<true>(f32x2(r.x, r.y), f32x2(i.x, i.y), rate, k);
+    const uint64_t A = decay_of(g.low, k);
+    h = fma2(A, h, mul2(mul2(sqrt2(m2_of(g.low, A, k)), g.si), f32x2(x.x, x.y)));
     store_f32x2(st, left, h);
     float h0, h1;
     f32x2_split(h, h0, h1);
@@ -710,12 +825,13 @@ int check_sizes(int dtype, int T, int B, int D, float c, char* msg, int msg_len)
   return LSTM_APPROX_OK;
 }
 
-// Blocks of a cluster that share a stream's 64 channels: doubled while the
-// blocks are fewer than two to an SM and each still has a tile to itself.
+// Blocks of a cluster that share a stream's 64 channels: doubled while all
+// blocks still run at once (two to an SM; clusters of 8 or 16 leave some of a
+// processor group's slots empty) and each has a tile to itself.
 int cluster_size(int T, int B, int D) {
   const long long items = (long long)B * ((D + kLanes - 1) / kLanes);
   int n = 1;
-  while (n < kMaxCluster && items * n < 2 * 152 && (long long)n * kTile < T) n *= 2;
+  while (n < kMaxCluster && items * 2 * n <= 256 && (long long)n * kTile < T) n *= 2;
   return n;
 }
 
