@@ -210,20 +210,22 @@ __device__ __forceinline__ void stage(T* dst, const T* src, long long stride, in
     };
     const T* from = src + (ts + row0) * stride + lane % kRow * kPer;
     const uint32_t to = smem_u32(dst + row0 * kLanes + lane % kRow * kPer);
-    const bool whole = ts + kSteps <= len && ch0 + kLanes <= D;
+    if (ts + kSteps <= len && ch0 + kLanes <= D) {
 #pragma unroll
-    for (int s = 0; s < kSteps; s += kRows) {
+      for (int s = 0; s < kSteps; s += kRows, from += kRows * stride) {
 #pragma unroll
-      for (int q = 0; q < kTurns; ++q) {
-        const uint32_t at = to + (s * kLanes + 32 * q * kPer) * (int)sizeof(T);
-        if (whole) {
-          copy(at, from + 32 * q * kPer, kCopy);
-        } else {
+        for (int q = 0; q < kTurns; ++q)
+          copy(to + (s * kLanes + 32 * q * kPer) * (int)sizeof(T), from + 32 * q * kPer, kCopy);
+      }
+    } else {
+#pragma unroll 1
+      for (int s = 0; s < kSteps; s += kRows, from += kRows * stride) {
+#pragma unroll
+        for (int q = 0; q < kTurns; ++q) {
           const bool in = ts + s + row0 < len && ch0 + (lane % kRow + 32 * q) * kPer < D;
-          copy(at, in ? from + 32 * q * kPer : src, in ? kCopy : 0);
+          copy(to + (s * kLanes + 32 * q * kPer) * (int)sizeof(T), in ? from + 32 * q * kPer : src, in ? kCopy : 0);
         }
       }
-      from += kRows * stride;
     }
   } else {
 #pragma unroll
@@ -263,7 +265,6 @@ __device__ __forceinline__ int length_of(const int* lengths, int b, int T) {
 
 // Bit s: reset at timestep ts + s of this warp (the same in all lanes).
 __device__ __forceinline__ unsigned reset_bits(const unsigned char* reset, int ts, int len, int b, int B) {
-  if (!reset) return 0u;
   const int lane = threadIdx.x & 31, t = ts + lane;
   const bool on = lane < kSteps && t < len && reset[(long long)t * B + b] != 0;
   return __ballot_sync(0xffffffffu, on);
@@ -283,10 +284,11 @@ struct WarpRuns {
 };
 __device__ __forceinline__ Runs runs_of(WarpRuns& w) { return {&w.AU[0][0], w.cut}; }
 
-// h after run k; cuts: some run may have a reset.
-__device__ __forceinline__ uint64_t after(const Runs& r, int k, uint64_t h, bool cuts) {
+// h after run k; kCuts: some run may have a reset.
+template <bool kCuts>
+__device__ __forceinline__ uint64_t after(const Runs& r, int k, uint64_t h) {
   const ulonglong2 v = r.AU[k * 32 + (threadIdx.x & 31)];
-  if (cuts && r.cut[k] != 0) h = 0ull;
+  if (kCuts && r.cut[k] != 0) h = 0ull;
   return fma2(v.x, h, v.y);
 }
 
@@ -318,7 +320,7 @@ __device__ __forceinline__ void send_run(const Runs& mine, int rank, int size, u
 // blocks share an SM's shared memory (32-bit values backward, and forward in a
 // cluster of 16: one block).
 template <typename T, int kTensors>
-constexpr int kStages = sizeof(T) == 4 || kTensors == 4 ? 2 : 3;
+constexpr int kStages = 2;
 template <typename T, int kTensors>
 constexpr size_t kStageBytes = (size_t)kTensors * kTile * kLanes * sizeof(T);
 
@@ -378,8 +380,8 @@ __device__ __forceinline__ bool any_far(uint64_t rate) {
   return __any_sync(0xffffffffu, !(r0 <= 0.125f && r1 <= 0.125f));
 }
 
-template <typename T, int kCopy>
-__global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const ScanArgs a) {
+template <typename T, int kCopy, bool kCuts>
+__global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 2 : 3) gated_scan_kernel(const ScanArgs a) {
   extern __shared__ __align__(16) unsigned char staged[];
   __shared__ WarpRuns runs[2];
   constexpr int kN = kStages<T, 3>;
@@ -396,7 +398,6 @@ __global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const ScanAr
   T* y = static_cast<T*>(a.y) + b * a.sy.b + ch;
   const long long state_at = (long long)b * a.D + ch;
   const int stride = a.cluster * kTile;
-  const bool cuts = a.reset != nullptr;
   auto buffer = [&](int n) { return reinterpret_cast<T*>(staged + n * kStageBytes<T, 3>) + warp * kSteps * kLanes; };
   auto fetch = [&](int n, int first) {  // this warp's part of the tile that starts at `first` + rank tiles, if there is one
     T* to = buffer(n);
@@ -420,7 +421,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const ScanAr
   // every block of the cluster makes the same number of turns (they meet in the barrier)
   for (int first = 0; first < a.T; first += stride, turn ^= 1) {
     const int t0 = first + rank * kTile, ts = t0 + warp * kSteps;
-    const unsigned resets = reset_bits(a.reset, ts, len, b, a.B);
+    const unsigned resets = kCuts ? reset_bits(a.reset, ts, len, b, a.B) : 0u;
     const T* here = buffer(at) + 2 * lane;
     stage_wait<kN - 2>();
     fetch(next, first + (kN - 1) * stride);  // into the stage that the last turn read
@@ -449,7 +450,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const ScanAr
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         all.x = mul2(all.x, run.AU[w * 32 + lane].x);
-        all.y = after(run, w, all.y, cuts);
+        all.y = after<kCuts>(run, w, all.y);
         cut = cut || run.cut[w] != 0;
       }
       send_run(tiles, rank, a.cluster, all, cut);
@@ -459,18 +460,18 @@ __global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const ScanAr
     if (a.cluster > 1) {
       for (int n = 0; n < a.cluster; ++n) {
         if (n == rank) hs = h;
-        h = after(tiles, n, h, cuts);
+        h = after<kCuts>(tiles, n, h);
       }
     }
     if (a.states && warp == 0 && t0 < a.T)
       store_f32x2(a.states + (long long)(t0 / kTile) * a.B * a.D + state_at, left, hs);
     if (a.cluster > 1) {
-      for (int w = 0; w < warp; ++w) hs = after(run, w, hs, cuts);
+      for (int w = 0; w < warp; ++w) hs = after<kCuts>(run, w, hs);
     } else {
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         if (w == warp) hs = h;
-        h = after(run, w, h, cuts);
+        h = after<kCuts>(run, w, h);
       }
     }
     if (resets) {
@@ -571,7 +572,7 @@ __device__ __forceinline__ Gradients gradients_of(const T* here, uint64_t low, u
   return d;
 }
 
-template <typename T, int kCopy>
+template <typename T, int kCopy, bool kCuts>
 __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_scan_backward_kernel(const ScanBackwardArgs a) {
   extern __shared__ __align__(16) unsigned char staged[];
   __shared__ WarpRuns runs[2];  // h -> A h + U
@@ -594,7 +595,6 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
   T* di = static_cast<T*>(a.di) + b * a.sdi.b + ch;
   const long long state_at = (long long)b * a.D + ch;
   const int stride = a.cluster * kTile;
-  const bool cuts = a.reset != nullptr;
   auto buffer = [&](int n) { return reinterpret_cast<T*>(staged + n * kStageBytes<T, 4>) + warp * kSteps * kLanes; };
   auto fetch = [&](int n, int first) {
     T* to = buffer(n);
@@ -618,7 +618,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
   int turn = 0, at = 0, next = kN - 1;
   for (int first = last; first >= 0; first -= stride, turn ^= 1) {
     const int t0 = first + rank * kTile, ts = t0 + warp * kSteps;
-    const unsigned resets = reset_bits(a.reset, ts, len, b, a.B);
+    const unsigned resets = kCuts ? reset_bits(a.reset, ts, len, b, a.B) : 0u;
     const T* here = buffer(at) + 2 * lane;
     uint64_t h = t0 < a.T ? load_f32x2(a.states + (long long)(t0 / kTile) * a.B * a.D + state_at, left) : 0ull;
     stage_wait<kN - 2>();
@@ -650,25 +650,25 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
 #pragma unroll
       for (int w = kWarps - 1; w >= 0; --w) {
         all.x = mul2(all.x, rev.AU[w * 32 + lane].x);
-        all.y = after(rev, w, all.y, cuts);
+        all.y = after<kCuts>(rev, w, all.y);
         cut = cut || rev.cut[w] != 0;
       }
       send_run(tiles, rank, a.cluster, all, cut);
       cluster_sync_all();
     }
-    for (int w = 0; w < warp; ++w) h = after(run, w, h, cuts);
+    for (int w = 0; w < warp; ++w) h = after<kCuts>(run, w, h);
     uint64_t ps = p;  // p after this block's tile, then after this warp's timesteps
     if (a.cluster > 1) {
       for (int n = a.cluster - 1; n >= 0; --n) {
         if (n == rank) ps = p;
-        p = after(tiles, n, p, cuts);
+        p = after<kCuts>(tiles, n, p);
       }
-      for (int w = kWarps - 1; w > warp; --w) ps = after(rev, w, ps, cuts);
+      for (int w = kWarps - 1; w > warp; --w) ps = after<kCuts>(rev, w, ps);
     } else {
 #pragma unroll
       for (int w = kWarps - 1; w >= 0; --w) {
         if (w == warp) ps = p;
-        p = after(rev, w, p, cuts);
+        p = after<kCuts>(rev, w, p);
       }
     }
     if (some) {
@@ -835,7 +835,7 @@ int cluster_size(int T, int B, int D) {
   return n;
 }
 
-template <typename T, int kCopy, int kTensors, typename A>
+template <typename T, int kCopy, bool kCuts, int kTensors, typename A>
 cudaError_t launch_scan(void (*kern)(A), int cluster, int blocks, cudaStream_t s, const A& args) {
   static thread_local DeviceSet ready;  // of the one kernel that this instance launches
   constexpr size_t smem = kStages<T, kTensors> * kStageBytes<T, kTensors>;
@@ -899,10 +899,14 @@ extern "C" int lstm_approx_gated_scan(int dtype, const void* x, const void* r, c
   const cudaError_t e = op_for_type(dtype, [&](auto* t) {
     using E = std::remove_pointer_t<decltype(t)>;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    if (copy == 16) return launch_scan<E, 16, 3>(gated_scan_kernel<E, 16>, n, slabs * B * n, s, a);
-    if (copy == 4) return launch_scan<E, 4, 3>(gated_scan_kernel<E, 4>, n, slabs * B * n, s, a);
-    if constexpr (sizeof(E) == 2) return launch_scan<E, 2, 3>(gated_scan_kernel<E, 2>, n, slabs * B * n, s, a);
-    return cudaErrorInvalidValue;  // 32-bit values are always copied
+    auto go = [&](auto bytes) {
+      constexpr int kCopy = decltype(bytes)::value;
+      return reset ? launch_scan<E, kCopy, true, 3>(gated_scan_kernel<E, kCopy, true>, n, slabs * B * n, s, a)
+                   : launch_scan<E, kCopy, false, 3>(gated_scan_kernel<E, kCopy, false>, n, slabs * B * n, s, a);
+    };
+    if (copy == 16) return go(std::integral_constant<int, 16>());
+    if (copy == 4 || sizeof(E) == 4) return go(std::integral_constant<int, 4>());
+    return go(std::integral_constant<int, sizeof(E) == 4 ? 4 : 2>());  // 32-bit values are always copied
   });
   return op_launched(e, "scan launch", msg, msg_len);
 }
@@ -948,10 +952,15 @@ extern "C" int lstm_approx_gated_scan_backward(int dtype, const void* dy, const 
     const int copy = copy_bytes(D, es, tensors, st, 7);
     const cudaError_t e = op_for_type(dtype, [&](auto* t) {
       using E = std::remove_pointer_t<decltype(t)>;
-      if (copy == 16) return launch_scan<E, 16, 4>(gated_scan_backward_kernel<E, 16>, n, slabs * B * n, s, a);
-      if (copy == 4) return launch_scan<E, 4, 4>(gated_scan_backward_kernel<E, 4>, n, slabs * B * n, s, a);
-      if constexpr (sizeof(E) == 2) return launch_scan<E, 2, 4>(gated_scan_backward_kernel<E, 2>, n, slabs * B * n, s, a);
-      return cudaErrorInvalidValue;
+      auto go = [&](auto bytes) {
+        constexpr int kCopy = decltype(bytes)::value;
+        return reset
+                   ? launch_scan<E, kCopy, true, 4>(gated_scan_backward_kernel<E, kCopy, true>, n, slabs * B * n, s, a)
+                   : launch_scan<E, kCopy, false, 4>(gated_scan_backward_kernel<E, kCopy, false>, n, slabs * B * n, s, a);
+      };
+      if (copy == 16) return go(std::integral_constant<int, 16>());
+      if (copy == 4 || sizeof(E) == 4) return go(std::integral_constant<int, 4>());
+      return go(std::integral_constant<int, sizeof(E) == 4 ? 4 : 2>());
     });
     if (int rc = op_launched(e, "scan backward launch", msg, msg_len)) return rc;
   }
