@@ -132,13 +132,22 @@ size_t lstm_approx_rms_norm_workspace_bytes(long long rows, int D);
  *             where it has none); may be h0 itself
  *   states    [ceil(T / LSTM_APPROX_SCAN_CHUNK)][B][D] fp32, or NULL: the state
  *             before every chunk's first timestep, kept for the backward pass
+ *   workspace at least lstm_approx_gated_scan_workspace_bytes(T, B, D) bytes,
+ *             16-byte aligned, not shared by calls in flight
+ *
+ * A sequence longer than a chunk is split over blocks that run at once and pass
+ * its state on through the workspace (a cooperative launch: ECUDA where the
+ * device cannot hold it).  Should a wait for another block's part run out (2 s;
+ * on a device that works, none does), what depends on that part is NaN.
  */
 #define LSTM_APPROX_SCAN_CHUNK 64
 int lstm_approx_gated_scan(int dtype, const void *x, const void *r, const void *i, const float *decay,
                            float c, const float *h0, const int32_t *lengths,
                            const unsigned char *reset, int T, int B, int D, void *y,
-                           const long long *strides, float *h_last, float *states, void *cuda_stream,
-                           char *msg, int msg_len);
+                           const long long *strides, float *h_last, float *states, void *workspace,
+                           size_t workspace_bytes, void *cuda_stream, char *msg, int msg_len);
+/* Workspace bytes of the call above and of the next; 0 for invalid sizes. */
+size_t lstm_approx_gated_scan_workspace_bytes(int T, int B, int D);
 
 /*
  * Gradients of the recurrence.  With g_t the gradient of h_t (dy_t and what
@@ -163,8 +172,6 @@ int lstm_approx_gated_scan_backward(int dtype, const void *dy, const float *dh_l
                                     void *dr, void *di, const long long *strides, float *ddecay,
                                     float *dh0, void *workspace, size_t workspace_bytes,
                                     void *cuda_stream, char *msg, int msg_len);
-/* Workspace bytes of the call above; 0 for invalid sizes. */
-size_t lstm_approx_gated_scan_workspace_bytes(int T, int B, int D);
 
 /*
  * One timestep of the recurrence for B streams, states updated in place:

@@ -213,7 +213,7 @@ def gated_scan_states(T: int, B: int, D: int, device=None):
 
 
 def gated_scan(x, r, i, decay, h0=None, *, c: float = 8.0, lengths=None, reset=None, y=None, h_last=None,
-               states=None, stream=None):
+               states=None, workspace=None, stream=None):
     """The recurrence h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigma(i_t) x_t,
     a_t = exp(-c softplus(decay) sigma(r_t)), over x, r, i [T, B, D] (any t and
     b strides): returns (y, h_last), y_t = h_t in x's type, h_last [B, D] fp32.
@@ -227,18 +227,25 @@ def gated_scan(x, r, i, decay, h0=None, *, c: float = 8.0, lengths=None, reset=N
     _need(x.dim() == 3, "x must be [T, B, D]")
     shape = x.shape
     T, B, D = shape
-    with _on(dev, stream, (x, r, i, decay, h0, lengths, reset, y, h_last, states)):
+    with _on(dev, stream, (x, r, i, decay, h0, lengths, reset, y, h_last, states, workspace)):
         if y is None:
             y = torch.empty(shape, dtype=x.dtype, device=x.device)
         if h_last is None:
-            h_last = torch.empty(B, D, dtype=torch.float32, device=x.device)
+            h_last = torch.empty(B, D, dtype=_F32, device=x.device)
+        if workspace is None:
+            workspace = _scan_workspace(T, B, D, x.device)
         f32 = _F32
         px, pr, pi, py = (_check(t, n, dev, x.dtype, shape) for t, n in ((x, "x"), (r, "r"), (i, "i"), (y, "y")))
         _call(dev, "lstm_approx_gated_scan", code, px, pr, pi, _dense(decay, "decay", dev, f32, (D,)), c,
               _dense(h0, "h0", dev, f32, (B, D)), _dense(lengths, "lengths", dev, _I32, (B,)),
               _reset(reset, dev, (T, B)), T, B, D, py, _strides(x, r, i, y), _dense(h_last, "h_last", dev, f32, (B, D)),
-              _dense(states, "states", dev, f32, (-(-T // SCAN_CHUNK), B, D)))
+              _dense(states, "states", dev, f32, (-(-T // SCAN_CHUNK), B, D)), workspace.data_ptr(), workspace.nbytes)
     return y, h_last
+
+
+def _scan_workspace(T: int, B: int, D: int, device):
+    need = load().lstm_approx_gated_scan_workspace_bytes(T, B, D)
+    return torch.empty(max(need, 16), dtype=_U8, device=device)
 
 
 def _reset(reset, dev, shape):
@@ -264,8 +271,7 @@ def gated_scan_backward(dy, x, r, i, decay, states, dh_last=None, *, c: float = 
         if dh0 is None:
             dh0 = torch.empty(B, D, dtype=f32, device=x.device)
         if workspace is None:
-            need = load().lstm_approx_gated_scan_workspace_bytes(T, B, D)
-            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=x.device)
+            workspace = _scan_workspace(T, B, D, x.device)
         pdy, px, pr, pi, pdx, pdr, pdi = (
             _check(t, n, dev, x.dtype, shape)
             for t, n in ((dy, "dy"), (x, "x"), (r, "r"), (i, "i"), (dx, "dx"), (dr, "dr"), (di, "di")))

@@ -13,12 +13,22 @@
 // and each warp goes over its 8 timesteps once more from the state it starts
 // with.  a_t and m_t sigma(i_t) x_t are computed once and stay in registers.
 //
-// Few streams over few channels leave most of the GPU idle in that form, so the
-// blocks of a cluster of up to 16 share a stream's 64 channels: block k of n
-// takes tiles k, n + k, ..., writes its tile's (A, U) into every block's shared
-// memory, and after one cluster barrier per n tiles each block joins all of
-// them in order.  That keeps the sequence at one pass over memory in one
-// launch, with no flags in memory and no waits but the barrier.
+// The tiles of all streams and channels are tasks, in the order of time, that
+// go round the blocks of one wave (a cooperative launch, so that all of them
+// run at once).  A task forms its tile's run while the tiles before it are
+// formed by other blocks, and learns the state it starts with through memory:
+// every tile writes its (A, U), and the last of each group of up to 16 tiles the
+// state after it; a tile takes the state before its group and joins the runs of
+// the group's tiles before its own, in their order.  What joins what depends on
+// the shape alone.  So the sequence is read once, the work is even whatever the
+// shape, and the chain through a sequence has one link per 1024 timesteps.
+// (With the blocks of a cluster of up to 16 along T, joined through distributed
+// shared memory, 8192 x 1 x 2048 bf16 took 57 us and 20000 x 1 x 512 fp32 111:
+// too few warps run at once, and clusters do not fill the last wave.)
+//
+// The exchanged words are their own flags: a first kernel fills the exchange
+// with a NaN pattern that no result has, and a reader takes a word once it
+// differs.  Every wait ends after 2 s at the latest, with that NaN as the value.
 //
 // Backward, with p_t = k_t a_t g_t the gradient of h_{t-1}:
 //   g_t = dy_t + p_{t+1}  (p after the last timestep: dh_last; before the first: dh0)
@@ -245,20 +255,6 @@ __device__ __forceinline__ void stage_wait() {
   __syncwarp();
 }
 
-struct ScanArgs {
-  const void *x, *r, *i;
-  void* y;
-  Strides sx, sr, si, sy;
-  const float* decay;
-  float c;
-  const float* h0;
-  const int* lengths;
-  const unsigned char* reset;
-  int T, B, D, slabs, cluster;
-  float* h_last;
-  float* states;
-};
-
 __device__ __forceinline__ int length_of(const int* lengths, int b, int T) {
   return lengths ? min(max(lengths[b], 0), T) : T;
 }
@@ -270,56 +266,186 @@ __device__ __forceinline__ unsigned reset_bits(const unsigned char* reset, int t
   return __ballot_sync(0xffffffffu, on);
 }
 
-constexpr int kMaxCluster = 16;
+// ---- tasks and the exchange between tiles -----------------------------------
 
-// Runs of several timesteps, of the warps of a tile or the tiles of a
-// cluster's blocks: state after run k = cut[k] ? U : A h + U.
-struct Runs {
-  ulonglong2* AU;  // [runs][32]: A and U of a lane's two channels
-  unsigned* cut;   // [runs]
+constexpr int kMaxGroup = 16;                       // tiles of a group
+constexpr unsigned kNotYet = 0xffffffffu;           // a word of the exchange before it is written
+constexpr unsigned long long kWaitNs = 2000000000;  // longest wait for one
+
+// One tile of 64 channels of one stream; `order` counts tiles in the direction of the scan.
+struct Task {
+  int slab, b, order;
 };
-struct WarpRuns {
-  ulonglong2 AU[kWarps][32];
-  unsigned cut[kWarps];
+struct Tasks {
+  int T, B, D;
+  int slabs, tiles;  // of a stream's channels, of the sequence (one at least)
+  int group;         // tiles of a group: a function of the shape
+  long long count;   // slabs * B * tiles
 };
-__device__ __forceinline__ Runs runs_of(WarpRuns& w) { return {&w.AU[0][0], w.cut}; }
-
-// h after run k; kCuts: some run may have a reset.
-template <bool kCuts>
-__device__ __forceinline__ uint64_t after(const Runs& r, int k, uint64_t h) {
-  const ulonglong2 v = r.AU[k * 32 + (threadIdx.x & 31)];
-  if (kCuts && r.cut[k] != 0) h = 0ull;
-  return fma2(v.x, h, v.y);
+// Shapes with few streams and channels have many tiles of one sequence in flight at once (about three blocks to an
+// SM share them); where there are more sequences than blocks a tile's predecessor is done long before.
+inline Tasks tasks_of(int T, int B, int D) {
+  Tasks t{T, B, D, (D + kLanes - 1) / kLanes, std::max(1, (T + kTile - 1) / kTile), 1, 0};
+  const long long items = (long long)t.slabs * B;
+  t.count = items * t.tiles;
+  while (t.group < kMaxGroup && items * t.group < 3 * 152) t.group *= 2;
+  return t;
 }
-
-// The exchange buffer of parity `turn` behind the staged tiles: a run for each block of the cluster.
-__device__ __forceinline__ Runs tile_runs(unsigned char* base, int cluster, int turn) {
-  ulonglong2* AU = reinterpret_cast<ulonglong2*>(base);
-  unsigned* cut = reinterpret_cast<unsigned*>(AU + 2 * cluster * 32);
-  return {AU + turn * cluster * 32, cut + turn * cluster};
+// Tasks go round the blocks in the order slab (fastest), stream, tile.
+__device__ __forceinline__ Task task_at(const Tasks& t, long long id) {
+  return {(int)(id % t.slabs), (int)(id / t.slabs % t.B), (int)(id / t.slabs / t.B)};
 }
-__host__ __device__ constexpr size_t exchange_bytes(int cluster) {
-  return cluster > 1 ? (size_t)2 * cluster * (32 * sizeof(ulonglong2) + sizeof(unsigned)) : 0;
-}
-
-// Writes this block's tile run into slot `rank` of `mine` in every block of the
-// cluster, one block to a warp (the blocks past the eighth in a second turn).
-__device__ __forceinline__ void send_run(const Runs& mine, int rank, int size, ulonglong2 run, bool cut) {
-  const int lane = threadIdx.x & 31;
-  for (int to = threadIdx.x >> 5; to < size; to += kWarps) {
-    const uint32_t at = mapa_shared(smem_u32(mine.AU + rank * 32 + lane), to);
-    asm volatile("st.shared::cluster.v2.u64 [%0], {%1, %2};" ::"r"(at), "l"(run.x), "l"(run.y) : "memory");
-    if (lane == 0) {
-      const uint32_t c = mapa_shared(smem_u32(mine.cut + rank), to);
-      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(c), "r"((unsigned)cut) : "memory");
-    }
+// The task `step` (itself a task's place) further on.
+__device__ __forceinline__ Task advance(const Tasks& t, Task at, Task step) {
+  at.slab += step.slab;
+  at.b += step.b;
+  at.order += step.order;
+  if (at.slab >= t.slabs) {
+    at.slab -= t.slabs;
+    ++at.b;
   }
+  if (at.b >= t.B) {
+    at.b -= t.B;
+    ++at.order;
+  }
+  return at;
 }
 
-// Tiles in flight or in use at once, of kTensors tensors: as many as let two
-// blocks share an SM's shared memory (32-bit values backward, and forward in a
-// cluster of 16: one block).
-template <typename T, int kTensors>
+// The exchange in memory: c softplus(decay) [slabs * 64], then each tile's run [tiles][items][32] (16 bytes for a
+// lane's two channels), then the state before each group but the first [groups - 1][items][32] (8 bytes).
+struct Exchange {
+  float* rate;
+  ulonglong2* runs;
+  uint64_t* states;
+};
+__host__ __device__ inline Exchange exchange_of(void* base, const Tasks& t) {
+  Exchange e;
+  e.rate = static_cast<float*>(base);
+  e.runs = reinterpret_cast<ulonglong2*>(e.rate + (long long)t.slabs * kLanes);
+  e.states = reinterpret_cast<uint64_t*>(e.runs + t.count * 32);
+  return e;
+}
+inline size_t exchange_words(const Tasks& t) {  // of the runs and states (none for a single tile)
+  if (t.tiles == 1) return 0;
+  const long long items = (long long)t.slabs * t.B, groups = (t.tiles + t.group - 1) / t.group;
+  return (size_t)(t.count * 32 * 4 + (groups - 1) * items * 32 * 2);
+}
+inline size_t exchange_bytes(const Tasks& t) { return ((size_t)t.slabs * kLanes + exchange_words(t)) * 4; }
+
+// Fills the exchange and forms the rates, once per call.
+__global__ void __launch_bounds__(256) scan_prepare_kernel(const float* decay, float c, int D, int rates, float* rate,
+                                                           uint4* fill, long long n) {
+  const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < rates) rate[i] = i < D ? c * softplus_f(decay[i]) : 0.0f;
+  for (long long k = i; k < n; k += (long long)gridDim.x * blockDim.x)
+    fill[k] = make_uint4(kNotYet, kNotYet, kNotYet, kNotYet);
+}
+
+__device__ __forceinline__ unsigned as_result(unsigned w) { return w == kNotYet ? 0x7fffffffu : w; }
+__device__ __forceinline__ void publish(uint64_t* p, uint64_t v) {
+  asm volatile("st.relaxed.gpu.global.v2.u32 [%0], {%1, %2};" ::"l"(p), "r"(as_result((unsigned)v)),
+               "r"(as_result((unsigned)(v >> 32)))
+               : "memory");
+}
+__device__ __forceinline__ void publish(ulonglong2* p, ulonglong2 v) {
+  asm volatile("st.relaxed.gpu.global.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(as_result((unsigned)v.x)),
+               "r"(as_result((unsigned)(v.x >> 32))), "r"(as_result((unsigned)v.y)),
+               "r"(as_result((unsigned)(v.y >> 32)))
+               : "memory");
+}
+// Polls until every lane's words are there, or the wait has run out: then the pattern itself, a NaN, is returned.
+template <typename F>
+__device__ __forceinline__ void wait_for_words(F ready) {
+  if (__all_sync(0xffffffffu, ready())) return;
+  const unsigned long long t0 = global_timer_ns();
+  while (!__all_sync(0xffffffffu, ready()))
+    if (__any_sync(0xffffffffu, global_timer_ns() - t0 > kWaitNs)) return;
+}
+__device__ __forceinline__ uint64_t receive(const uint64_t* p) {
+  unsigned a, b;
+  wait_for_words([&] {
+    asm volatile("ld.relaxed.gpu.global.v2.u32 {%0, %1}, [%2];" : "=r"(a), "=r"(b) : "l"(p) : "memory");
+    return a != kNotYet && b != kNotYet;
+  });
+  return (uint64_t)b << 32 | a;
+}
+__device__ __forceinline__ ulonglong2 receive(const ulonglong2* p) {
+  unsigned a, b, c, d;
+  wait_for_words([&] {
+    asm volatile("ld.relaxed.gpu.global.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(a), "=r"(b), "=r"(c), "=r"(d)
+                 : "l"(p)
+                 : "memory");
+    return a != kNotYet && b != kNotYet && c != kNotYet && d != kNotYet;
+  });
+  return make_ulonglong2((uint64_t)b << 32 | a, (uint64_t)d << 32 | c);
+}
+
+// A run with a reset in it leads to U whatever the state before: its A (both channels') is -1, which no product of
+// decays is.
+template <bool kCuts>
+__device__ __forceinline__ uint64_t after(ulonglong2 run, uint64_t h) {
+  if (kCuts && (int)(unsigned)run.x < 0) h = 0ull;
+  return fma2(run.x, h, run.y);
+}
+// The run of `first` and then `second`.
+template <bool kCuts>
+__device__ __forceinline__ ulonglong2 join(ulonglong2 first, ulonglong2 second) {
+  const bool cut = kCuts && ((int)(unsigned)first.x < 0 || (int)(unsigned)second.x < 0);
+  return make_ulonglong2(cut ? both(-1.0f) : mul2(first.x, second.x), after<kCuts>(second, first.y));
+}
+
+struct Join {                             // shared memory of a block
+  ulonglong2 runs[2][kWarps][32];         // of the warps of a tile, by parity of the turn
+  ulonglong2 before[kMaxGroup - 1][32];   // of the group's tiles before this one
+  uint64_t start[32];                     // the state before the group
+};
+
+// Brings what a task needs from other tiles into shared memory, one run to a warp, and this tile's run out to them;
+// `mine`: the warps' runs of this tile, in the direction of the scan from warp `w0` in steps of `dw`.  Returns this
+// tile's run in warp 0.  The block meets in a barrier before and after.
+template <bool kCuts>
+__device__ __forceinline__ ulonglong2 exchange_runs(const Tasks& t, const Exchange& e, const Task& at, Join& sm,
+                                                    const ulonglong2 (&mine)[kWarps][32], int w0, int dw, uint64_t first) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long items = (long long)t.slabs * t.B, item = (long long)at.b * t.slabs + at.slab;
+  const int place = at.order % t.group, group = at.order / t.group;
+  ulonglong2 all = make_ulonglong2(0ull, 0ull);
+  if (warp == 0) {
+    all = mine[w0][lane];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) all = join<kCuts>(all, mine[w0 + dw * w][lane]);
+    if (place != t.group - 1 && at.order != t.tiles - 1) publish(e.runs + (at.order * items + item) * 32 + lane, all);
+  }
+  if (warp == kWarps - 1) sm.start[lane] = group == 0 ? first : receive(e.states + ((group - 1) * items + item) * 32 + lane);
+  for (int q = warp; q < place; q += kWarps)
+    sm.before[q][lane] = receive(e.runs + ((long long)(at.order - place + q) * items + item) * 32 + lane);
+  return all;
+}
+// The state before a tile, after exchange_runs and the barrier.
+template <bool kCuts>
+__device__ __forceinline__ uint64_t state_before(const Tasks& t, const Task& at, const Join& sm) {
+  const int lane = threadIdx.x & 31, place = at.order % t.group;
+  uint64_t h = sm.start[lane];
+  for (int q = 0; q < place; ++q) h = after<kCuts>(sm.before[q][lane], h);
+  return h;
+}
+
+struct ScanArgs {
+  const void *x, *r, *i;
+  void* y;
+  Strides sx, sr, si, sy;
+  const float* h0;
+  const int* lengths;
+  const unsigned char* reset;
+  Tasks tasks;
+  Exchange exchange;
+  float* h_last;
+  float* states;
+};
+
+// A task's tile is used while the next one's arrives: 16-bit values leave room
+// for three blocks to an SM forward and two backward, 32-bit ones two and one.
 constexpr int kStages = 2;
 template <typename T, int kTensors>
 constexpr size_t kStageBytes = (size_t)kTensors * kTile * kLanes * sizeof(T);
@@ -355,18 +481,18 @@ __device__ __forceinline__ void form_runs(const T* here, uint64_t rate, const Co
   }
 }
 
-// The run of a warp's timesteps (kCuts: with resets at the set bits).
+// The run of a warp's timesteps (kCuts: with resets at the set bits, one at least).
 template <bool kCuts>
-__device__ __forceinline__ ulonglong2 join_steps(const uint64_t (&A)[kSteps], const uint64_t (&U)[kSteps], unsigned resets,
-                                                 const Constants& k) {
-  uint64_t PA = k.one, PU = 0ull;
+__device__ __forceinline__ ulonglong2 join_steps(const uint64_t (&A)[kSteps], const uint64_t (&U)[kSteps],
+                                                 unsigned resets) {
+  uint64_t PA = A[0], PU = U[0];
 #pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
+  for (int s = 1; s < kSteps; ++s) {
     if (kCuts && (resets >> s & 1u)) PU = 0ull;
     PU = fma2(A[s], PU, U[s]);
     PA = mul2(PA, A[s]);
   }
-  return make_ulonglong2(PA, PU);
+  return make_ulonglong2(kCuts ? both(-1.0f) : PA, PU);
 }
 
 // c softplus(decay) of a lane's channels, zero for one that does not exist.
@@ -383,55 +509,45 @@ __device__ __forceinline__ bool any_far(uint64_t rate) {
 template <typename T, int kCopy, bool kCuts>
 __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 2 : 3) gated_scan_kernel(const ScanArgs a) {
   extern __shared__ __align__(16) unsigned char staged[];
-  __shared__ WarpRuns runs[2];
-  constexpr int kN = kStages<T, 3>;
-  unsigned char* exchange = staged + kN * kStageBytes<T, 3>;
+  __shared__ Join sm;
   constexpr bool kVec = kCopy >= 2 * (int)sizeof(T);  // a lane's two channels of y in one store
+  constexpr int kOne = kTile * kLanes;                // values of one staged tensor
+  const Tasks& t = a.tasks;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = blockIdx.x % a.cluster, item = blockIdx.x / a.cluster;
-  const int slab = item % a.slabs, b = item / a.slabs;
-  const int ch0 = slab * kLanes, ch = ch0 + 2 * lane, left = a.D - ch;  // channels of this lane that exist: min(left, 2)
-  const int len = length_of(a.lengths, b, a.T);
-  const T* x = static_cast<const T*>(a.x) + b * a.sx.b + ch0;
-  const T* r = static_cast<const T*>(a.r) + b * a.sr.b + ch0;
-  const T* in = static_cast<const T*>(a.i) + b * a.si.b + ch0;
-  T* y = static_cast<T*>(a.y) + b * a.sy.b + ch;
-  const long long state_at = (long long)b * a.D + ch;
-  const int stride = a.cluster * kTile;
+  // this warp's part of a task's tile into stage n
   auto buffer = [&](int n) { return reinterpret_cast<T*>(staged + n * kStageBytes<T, 3>) + warp * kSteps * kLanes; };
-  auto fetch = [&](int n, int first) {  // this warp's part of the tile that starts at `first` + rank tiles, if there is one
+  auto fetch = [&](int n, const Task& at) {
     T* to = buffer(n);
-    const int ts = first + rank * kTile + warp * kSteps;
+    const int ts = at.order * kTile + warp * kSteps, ch0 = at.slab * kLanes;
+    const int len = length_of(a.lengths, at.b, t.T);
     if (ts < len) {
-      stage<T, kCopy>(to, x, a.sx.t, ts, len, ch0, a.D);
-      stage<T, kCopy>(to + kTile * kLanes, r, a.sr.t, ts, len, ch0, a.D);
-      stage<T, kCopy>(to + 2 * kTile * kLanes, in, a.si.t, ts, len, ch0, a.D);
+      stage<T, kCopy>(to, static_cast<const T*>(a.x) + at.b * a.sx.b + ch0, a.sx.t, ts, len, ch0, t.D);
+      stage<T, kCopy>(to + kOne, static_cast<const T*>(a.r) + at.b * a.sr.b + ch0, a.sr.t, ts, len, ch0, t.D);
+      stage<T, kCopy>(to + 2 * kOne, static_cast<const T*>(a.i) + at.b * a.si.b + ch0, a.si.t, ts, len, ch0, t.D);
     }
     stage_commit();
   };
-#pragma unroll
-  for (int n = 0; n < kN - 1; ++n) fetch(n, n * stride);
-  const uint64_t rate = rate_of(a.decay + ch, left, a.c);
-  const bool far = any_far(rate);
+  Task at = task_at(t, blockIdx.x);
+  const Task step = task_at(t, gridDim.x);
+  fetch(0, at);
   const Constants k = constants();
-  uint64_t h = a.h0 ? load_f32x2(a.h0 + state_at, left) : 0ull;
-  // shared memory of another block is written only after that block has started
-  if (a.cluster > 1) cluster_sync_all();
-  int turn = 0, at = 0, next = kN - 1;  // parity of the exchange buffers; stage in use, stage to fill
-  // every block of the cluster makes the same number of turns (they meet in the barrier)
-  for (int first = 0; first < a.T; first += stride, turn ^= 1) {
-    const int t0 = first + rank * kTile, ts = t0 + warp * kSteps;
-    const unsigned resets = kCuts ? reset_bits(a.reset, ts, len, b, a.B) : 0u;
-    const T* here = buffer(at) + 2 * lane;
-    stage_wait<kN - 2>();
-    fetch(next, first + (kN - 1) * stride);  // into the stage that the last turn read
-    at = at + 1 == kN ? 0 : at + 1;
-    next = next + 1 == kN ? 0 : next + 1;
+  int turn = 0;
+  for (; at.order < t.tiles; turn ^= 1) {
+    const Task next = advance(t, at, step);
+    const uint64_t rate = *reinterpret_cast<const uint64_t*>(a.exchange.rate + at.slab * kLanes + 2 * lane);
+    __syncwarp();  // the lanes are done with the stage that the next tile goes to
+    if (next.order < t.tiles) fetch(turn ^ 1, next);
+    else stage_commit();
+    const int ch = at.slab * kLanes + 2 * lane, left = t.D - ch;  // channels of this lane that exist: min(left, 2)
+    const int ts = at.order * kTile + warp * kSteps, len = length_of(a.lengths, at.b, t.T);
+    const long long state_at = (long long)at.b * t.D + ch;
+    const unsigned resets = kCuts ? reset_bits(a.reset, ts, len, at.b, t.B) : 0u;
+    const bool whole = ts + kSteps <= len;
+    const T* here = buffer(turn) + 2 * lane;
+    stage_wait<1>();
     uint64_t A[kSteps], U[kSteps];
-    const bool whole = ts + kSteps <= len;  // and `some` of its timesteps are the stream's
-    const bool some = ts < len;
-    if (some) {
-      if (far) form_runs<T, true>(here, rate, k, A, U);
+    if (ts < len) {
+      if (any_far(rate)) form_runs<T, true>(here, rate, k, A, U);
       else form_runs<T, false>(here, rate, k, A, U);
     }
     if (!whole) {
@@ -439,66 +555,45 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 2 : 3) gated_sca
       for (int s = 0; s < kSteps; ++s)
         if (ts + s >= len) A[s] = k.one, U[s] = 0ull;
     }
-    const ulonglong2 PR = resets ? join_steps<true>(A, U, resets, k) : join_steps<false>(A, U, 0u, k);
-    runs[turn].AU[warp][lane] = PR;  // the other parity's may still be read
-    if (lane == 0) runs[turn].cut[warp] = resets;
+    sm.runs[turn][warp][lane] = kCuts && resets ? join_steps<true>(A, U, resets) : join_steps<false>(A, U, 0u);
     __syncthreads();
-    const Runs run = runs_of(runs[turn]), tiles = tile_runs(exchange, a.cluster, turn);
-    if (a.cluster > 1) {
-      ulonglong2 all = make_ulonglong2(k.one, 0ull);
-      bool cut = false;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        all.x = mul2(all.x, run.AU[w * 32 + lane].x);
-        all.y = after<kCuts>(run, w, all.y);
-        cut = cut || run.cut[w] != 0;
-      }
-      send_run(tiles, rank, a.cluster, all, cut);
-      cluster_sync_all();
+    uint64_t first = 0ull;
+    if (warp == kWarps - 1 && at.order < t.group && a.h0) first = load_f32x2(a.h0 + state_at, left);
+    const ulonglong2 tile = exchange_runs<kCuts>(t, a.exchange, at, sm, sm.runs[turn], 0, 1, first);
+    __syncthreads();
+    uint64_t h = state_before<kCuts>(t, at, sm);
+    if (warp == 0) {
+      const uint64_t end = after<kCuts>(tile, h);
+      if (at.order == t.tiles - 1) store_f32x2(a.h_last + state_at, left, end);
+      else if (at.order % t.group == t.group - 1)
+        publish(a.exchange.states + ((long long)(at.order / t.group) * t.slabs * t.B + at.b * t.slabs + at.slab) * 32 + lane, end);
+      if (a.states && at.order * kTile < t.T)
+        store_f32x2(a.states + (long long)at.order * t.B * t.D + state_at, left, h);
     }
-    uint64_t hs = h;  // the state before this block's tile, then before this warp's timesteps
-    if (a.cluster > 1) {
-      for (int n = 0; n < a.cluster; ++n) {
-        if (n == rank) hs = h;
-        h = after<kCuts>(tiles, n, h);
-      }
-    }
-    if (a.states && warp == 0 && t0 < a.T)
-      store_f32x2(a.states + (long long)(t0 / kTile) * a.B * a.D + state_at, left, hs);
-    if (a.cluster > 1) {
-      for (int w = 0; w < warp; ++w) hs = after<kCuts>(run, w, hs);
-    } else {
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        if (w == warp) hs = h;
-        h = after<kCuts>(run, w, h);
-      }
-    }
-    if (resets) {
+    for (int w = 0; w < warp; ++w) h = after<kCuts>(sm.runs[turn][w][lane], h);
+    if (kCuts && resets) {
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
-        if (resets >> s & 1u) hs = 0ull;
-        hs = U[s] = fma2(A[s], hs, U[s]);
+        if (resets >> s & 1u) h = 0ull;
+        h = U[s] = fma2(A[s], h, U[s]);
       }
     } else {
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) hs = U[s] = fma2(A[s], hs, U[s]);
+      for (int s = 0; s < kSteps; ++s) h = U[s] = fma2(A[s], h, U[s]);
     }
     if (left > 0) {
-      T* to = y + ts * a.sy.t;
+      T* to = static_cast<T*>(a.y) + at.b * a.sy.b + ch + ts * a.sy.t;
       if (whole) {
 #pragma unroll
         for (int s = 0; s < kSteps; ++s, to += a.sy.t) store_both<T, kVec>(to, left, U[s]);
       } else {
 #pragma unroll
         for (int s = 0; s < kSteps; ++s, to += a.sy.t)
-          if (ts + s < a.T) store_both<T, kVec>(to, left, ts + s < len ? U[s] : 0ull);
+          if (ts + s < t.T) store_both<T, kVec>(to, left, ts + s < len ? U[s] : 0ull);
       }
     }
+    at = next;
   }
-  if (warp == 0 && rank == 0) store_f32x2(a.h_last + state_at, left, h);
-  // no block leaves while another may still write into its shared memory
-  if (a.cluster > 1) cluster_sync_all();
 }
 
 struct ScanBackwardArgs {
@@ -506,14 +601,13 @@ struct ScanBackwardArgs {
   void *dx, *dr, *di;
   Strides sdy, sx, sr, si, sdx, sdr, sdi;
   const float* dh_last;
-  const float* decay;
-  float c;
   const float* states;
   const int* lengths;
   const unsigned char* reset;
-  int T, B, D, slabs, cluster;
+  Tasks tasks;
+  Exchange exchange;
   float* dh0;
-  float* partial;  // [B][cluster][D]: each block's sum of E over its timesteps
+  float* partial;  // [tiles][B][slabs * 64]: each tile's sum of E
 };
 
 // 1 - a_t, the gates and m_t sigma(i_t) x_t of a warp's staged timesteps.
@@ -533,7 +627,7 @@ __device__ __forceinline__ void form_gates(const T* here, uint64_t rate, const C
 }
 
 // The runs of a warp's timesteps, h -> A h + U forward and p -> A p + V back
-// (staged dy is zero past the stream's length).
+// (staged dy is zero past the stream's length; kCuts: one reset at least).
 template <typename T, bool kCuts>
 __device__ __forceinline__ void join_both(const T* here, const uint64_t (&low)[kSteps], const uint64_t (&U)[kSteps],
                                           unsigned resets, const Constants& k, uint64_t& PA, uint64_t& PU, uint64_t& PV) {
@@ -549,6 +643,7 @@ __device__ __forceinline__ void join_both(const T* here, const uint64_t (&low)[k
     PV = mul2(decay_of(low[s], k), add2(PV, staged_pair<T>(here + 3 * kTile * kLanes + s * kLanes)));
     if (kCuts && (resets >> s & 1u)) PV = 0ull;
   }
+  if (kCuts) PA = both(-1.0f);
 }
 
 struct Gradients {
@@ -575,105 +670,90 @@ __device__ __forceinline__ Gradients gradients_of(const T* here, uint64_t low, u
 template <typename T, int kCopy, bool kCuts>
 __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_scan_backward_kernel(const ScanBackwardArgs a) {
   extern __shared__ __align__(16) unsigned char staged[];
-  __shared__ WarpRuns runs[2];  // h -> A h + U
-  __shared__ WarpRuns back[2];  // p -> A p + V
-  constexpr int kN = kStages<T, 4>;
-  unsigned char* exchange = staged + kN * kStageBytes<T, 4>;
+  __shared__ Join sm;                             // p -> A p + V
+  __shared__ ulonglong2 ahead[2][kWarps][32];     // h -> A h + U
+  __shared__ uint64_t sums[kWarps][32];           // E over each warp's timesteps of the last task
   constexpr bool kVec = kCopy >= 2 * (int)sizeof(T);
-  constexpr int kOne = kTile * kLanes;  // values of one staged tensor
+  constexpr int kOne = kTile * kLanes;
+  const Tasks& t = a.tasks;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = blockIdx.x % a.cluster, item = blockIdx.x / a.cluster;
-  const int slab = item % a.slabs, b = item / a.slabs;
-  const int ch0 = slab * kLanes, ch = ch0 + 2 * lane, left = a.D - ch;
-  const int len = length_of(a.lengths, b, a.T);
-  const T* dy = static_cast<const T*>(a.dy) + b * a.sdy.b + ch0;
-  const T* x = static_cast<const T*>(a.x) + b * a.sx.b + ch0;
-  const T* r = static_cast<const T*>(a.r) + b * a.sr.b + ch0;
-  const T* in = static_cast<const T*>(a.i) + b * a.si.b + ch0;
-  T* dx = static_cast<T*>(a.dx) + b * a.sdx.b + ch;
-  T* dr = static_cast<T*>(a.dr) + b * a.sdr.b + ch;
-  T* di = static_cast<T*>(a.di) + b * a.sdi.b + ch;
-  const long long state_at = (long long)b * a.D + ch;
-  const int stride = a.cluster * kTile;
   auto buffer = [&](int n) { return reinterpret_cast<T*>(staged + n * kStageBytes<T, 4>) + warp * kSteps * kLanes; };
-  auto fetch = [&](int n, int first) {
+  auto fetch = [&](int n, const Task& at) {
     T* to = buffer(n);
-    const int ts = first + rank * kTile + warp * kSteps;
-    if (first >= 0 && ts < len) {
-      stage<T, kCopy>(to, x, a.sx.t, ts, len, ch0, a.D);
-      stage<T, kCopy>(to + kOne, r, a.sr.t, ts, len, ch0, a.D);
-      stage<T, kCopy>(to + 2 * kOne, in, a.si.t, ts, len, ch0, a.D);
-      stage<T, kCopy>(to + 3 * kOne, dy, a.sdy.t, ts, len, ch0, a.D);
+    const int ts = (t.tiles - 1 - at.order) * kTile + warp * kSteps, ch0 = at.slab * kLanes;
+    const int len = length_of(a.lengths, at.b, t.T);
+    if (ts < len) {
+      stage<T, kCopy>(to, static_cast<const T*>(a.x) + at.b * a.sx.b + ch0, a.sx.t, ts, len, ch0, t.D);
+      stage<T, kCopy>(to + kOne, static_cast<const T*>(a.r) + at.b * a.sr.b + ch0, a.sr.t, ts, len, ch0, t.D);
+      stage<T, kCopy>(to + 2 * kOne, static_cast<const T*>(a.i) + at.b * a.si.b + ch0, a.si.t, ts, len, ch0, t.D);
+      stage<T, kCopy>(to + 3 * kOne, static_cast<const T*>(a.dy) + at.b * a.sdy.b + ch0, a.sdy.t, ts, len, ch0, t.D);
     }
     stage_commit();
   };
-  const int last = a.T > 0 ? (a.T - 1) / stride * stride : -1;
+  auto add_up = [&](const Task& at) {  // the sums of a finished task into its partial
+    uint64_t v = sums[0][lane];
 #pragma unroll
-  for (int n = 0; n < kN - 1; ++n) fetch(n, last - n * stride);
-  const uint64_t rate = rate_of(a.decay + ch, left, a.c);
-  const bool far = any_far(rate);
+    for (int w = 1; w < kWarps; ++w) v = add2(v, sums[w][lane]);
+    const long long row = (long long)(t.tiles - 1 - at.order) * t.B + at.b;
+    *reinterpret_cast<uint64_t*>(a.partial + (row * t.slabs + at.slab) * kLanes + 2 * lane) = v;
+  };
+  Task at = task_at(t, blockIdx.x), done = at;
+  const Task step = task_at(t, gridDim.x);
+  fetch(0, at);
   const Constants k = constants();
-  uint64_t p = a.dh_last ? load_f32x2(a.dh_last + state_at, left) : 0ull, sum = 0ull;
-  if (a.cluster > 1) cluster_sync_all();
-  int turn = 0, at = 0, next = kN - 1;
-  for (int first = last; first >= 0; first -= stride, turn ^= 1) {
-    const int t0 = first + rank * kTile, ts = t0 + warp * kSteps;
-    const unsigned resets = kCuts ? reset_bits(a.reset, ts, len, b, a.B) : 0u;
-    const T* here = buffer(at) + 2 * lane;
-    uint64_t h = t0 < a.T ? load_f32x2(a.states + (long long)(t0 / kTile) * a.B * a.D + state_at, left) : 0ull;
-    stage_wait<kN - 2>();
-    fetch(next, first - (kN - 1) * stride);
-    at = at + 1 == kN ? 0 : at + 1;
-    next = next + 1 == kN ? 0 : next + 1;
-    const bool whole = ts + kSteps <= len;
-    const bool some = ts < len;
+  int turn = 0;
+  bool any = false;
+  for (; at.order < t.tiles; turn ^= 1) {
+    const Task next = advance(t, at, step);
+    const uint64_t rate = *reinterpret_cast<const uint64_t*>(a.exchange.rate + at.slab * kLanes + 2 * lane);
+    __syncwarp();
+    if (next.order < t.tiles) fetch(turn ^ 1, next);
+    else stage_commit();
+    const int tile = t.tiles - 1 - at.order;
+    const int ch = at.slab * kLanes + 2 * lane, left = t.D - ch;
+    const int ts = tile * kTile + warp * kSteps, len = length_of(a.lengths, at.b, t.T);
+    const long long state_at = (long long)at.b * t.D + ch;
+    const unsigned resets = kCuts ? reset_bits(a.reset, ts, len, at.b, t.B) : 0u;
+    const bool whole = ts + kSteps <= len, some = ts < len;
+    const T* here = buffer(turn) + 2 * lane;
+    uint64_t h = some ? load_f32x2(a.states + (long long)tile * t.B * t.D + state_at, left) : 0ull;
+    stage_wait<1>();
     uint64_t low[kSteps], sr[kSteps], si[kSteps], U[kSteps], PA = k.one, PU = 0ull, PV = 0ull;
     if (some) {
-      if (far) form_gates<T, true>(here, rate, k, low, sr, si, U);
+      if (any_far(rate)) form_gates<T, true>(here, rate, k, low, sr, si, U);
       else form_gates<T, false>(here, rate, k, low, sr, si, U);
       if (!whole) {
 #pragma unroll
         for (int s = 0; s < kSteps; ++s)
           if (ts + s >= len) low[s] = U[s] = 0ull;
       }
-      if (resets) join_both<T, true>(here, low, U, resets, k, PA, PU, PV);
+      if (kCuts && resets) join_both<T, true>(here, low, U, resets, k, PA, PU, PV);
       else join_both<T, false>(here, low, U, 0u, k, PA, PU, PV);
     }
-    runs[turn].AU[warp][lane] = make_ulonglong2(PA, PU);
-    back[turn].AU[warp][lane] = make_ulonglong2(PA, PV);
-    if (lane == 0) runs[turn].cut[warp] = back[turn].cut[warp] = resets;
+    ahead[turn][warp][lane] = make_ulonglong2(PA, PU);
+    sm.runs[turn][warp][lane] = make_ulonglong2(PA, PV);
     __syncthreads();
-    const Runs run = runs_of(runs[turn]), rev = runs_of(back[turn]), tiles = tile_runs(exchange, a.cluster, turn);
-    if (a.cluster > 1) {
-      ulonglong2 all = make_ulonglong2(k.one, 0ull);
-      bool cut = false;
-#pragma unroll
-      for (int w = kWarps - 1; w >= 0; --w) {
-        all.x = mul2(all.x, rev.AU[w * 32 + lane].x);
-        all.y = after<kCuts>(rev, w, all.y);
-        cut = cut || rev.cut[w] != 0;
-      }
-      send_run(tiles, rank, a.cluster, all, cut);
-      cluster_sync_all();
+    if (warp == 1 && any) add_up(done);
+    uint64_t first = 0ull;
+    if (warp == kWarps - 1 && at.order < t.group && a.dh_last) first = load_f32x2(a.dh_last + state_at, left);
+    const ulonglong2 run = exchange_runs<kCuts>(t, a.exchange, at, sm, sm.runs[turn], kWarps - 1, -1, first);
+    for (int w = 0; w < warp; ++w) h = after<kCuts>(ahead[turn][w][lane], h);
+    __syncthreads();
+    uint64_t p = state_before<kCuts>(t, at, sm);
+    if (warp == 0) {
+      const uint64_t end = after<kCuts>(run, p);
+      if (at.order == t.tiles - 1) store_f32x2(a.dh0 + state_at, left, end);
+      else if (at.order % t.group == t.group - 1)
+        publish(a.exchange.states + ((long long)(at.order / t.group) * t.slabs * t.B + at.b * t.slabs + at.slab) * 32 + lane, end);
     }
-    for (int w = 0; w < warp; ++w) h = after<kCuts>(run, w, h);
-    uint64_t ps = p;  // p after this block's tile, then after this warp's timesteps
-    if (a.cluster > 1) {
-      for (int n = a.cluster - 1; n >= 0; --n) {
-        if (n == rank) ps = p;
-        p = after<kCuts>(tiles, n, p);
-      }
-      for (int w = kWarps - 1; w > warp; --w) ps = after<kCuts>(rev, w, ps);
-    } else {
-#pragma unroll
-      for (int w = kWarps - 1; w >= 0; --w) {
-        if (w == warp) ps = p;
-        p = after<kCuts>(rev, w, p);
-      }
-    }
+    for (int w = kWarps - 1; w > warp; --w) p = after<kCuts>(sm.runs[turn][w][lane], p);
+    T* dx = static_cast<T*>(a.dx) + at.b * a.sdx.b + ch;
+    T* dr = static_cast<T*>(a.dr) + at.b * a.sdr.b + ch;
+    T* di = static_cast<T*>(a.di) + at.b * a.sdi.b + ch;
+    uint64_t sum = 0ull;
     if (some) {
       // U becomes the state before each timestep
-      if (resets) {
+      if (kCuts && resets) {
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
           if (resets >> s & 1u) h = 0ull;
@@ -696,8 +776,8 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
       if (whole && left > 0) {
 #pragma unroll
         for (int s = kSteps - 1; s >= 0; --s) {
-          const Gradients g = gradients_of<T>(here + s * kLanes, low[s], sr[s], si[s], U[s], rate, k, ps);
-          if (resets && (resets >> s & 1u)) ps = 0ull;
+          const Gradients g = gradients_of<T>(here + s * kLanes, low[s], sr[s], si[s], U[s], rate, k, p);
+          if (kCuts && (resets >> s & 1u)) p = 0ull;
           sum = add2(sum, g.E);
           store_both<T, kVec>(to_x, left, g.x);
           store_both<T, kVec>(to_r, left, g.r);
@@ -710,10 +790,10 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
 #pragma unroll
         for (int s = kSteps - 1; s >= 0; --s) {
           Gradients g = {0ull, 0ull, 0ull, 0ull};
-          if (ts + s < len) g = gradients_of<T>(here + s * kLanes, low[s], sr[s], si[s], U[s], rate, k, ps);
-          if (resets >> s & 1u) ps = 0ull;
+          if (ts + s < len) g = gradients_of<T>(here + s * kLanes, low[s], sr[s], si[s], U[s], rate, k, p);
+          if (kCuts && (resets >> s & 1u)) p = 0ull;
           sum = add2(sum, g.E);
-          if (left > 0 && ts + s < a.T) {
+          if (left > 0 && ts + s < t.T) {
             store_both<T, kVec>(to_x, left, g.x);
             store_both<T, kVec>(to_r, left, g.r);
             store_both<T, kVec>(to_i, left, g.i);
@@ -724,32 +804,31 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
         }
       }
     } else if (left > 0) {
-      for (int t = ts; t < min(ts + kSteps, a.T); ++t) {
-        store_pair<T, kVec>(dx + t * a.sdx.t, left, 0.0f, 0.0f);
-        store_pair<T, kVec>(dr + t * a.sdr.t, left, 0.0f, 0.0f);
-        store_pair<T, kVec>(di + t * a.sdi.t, left, 0.0f, 0.0f);
+      for (int n = ts; n < min(ts + kSteps, t.T); ++n) {
+        store_pair<T, kVec>(dx + n * a.sdx.t, left, 0.0f, 0.0f);
+        store_pair<T, kVec>(dr + n * a.sdr.t, left, 0.0f, 0.0f);
+        store_pair<T, kVec>(di + n * a.sdi.t, left, 0.0f, 0.0f);
       }
     }
+    sums[warp][lane] = sum;
+    done = at;
+    any = true;
+    at = next;
   }
   __syncthreads();
-  runs[0].AU[warp][lane].x = sum;
-  __syncthreads();
-  if (warp == 0) {
-    for (int w = 1; w < kWarps; ++w) sum = add2(sum, runs[0].AU[w][lane].x);
-    store_f32x2(a.partial + ((long long)b * a.cluster + rank) * a.D + ch, left, sum);
-    if (rank == 0) store_f32x2(a.dh0 + state_at, left, p);
-  }
-  if (a.cluster > 1) cluster_sync_all();
+  if (warp == 1 && any) add_up(done);
 }
 
-// ddecay from partial [n][D], summed in a fixed order.
-__global__ void __launch_bounds__(1024) decay_gradient_kernel(const float* partial, int n, int D, const float* decay,
-                                                              float* ddecay) {
+// ddecay from partial [n][pitch], summed in a fixed order.
+__global__ void __launch_bounds__(1024) decay_gradient_kernel(const float* partial, int n, int pitch, int D,
+                                                              const float* decay, float* ddecay) {
   __shared__ float acc[32][33];
   const int col = blockIdx.x * 32 + threadIdx.x;
   float v = 0.0f;
-  if (col < D)
-    for (int k = threadIdx.y; k < n; k += 32) v += partial[(long long)k * D + col];
+  if (col < D) {
+#pragma unroll 4
+    for (int k = threadIdx.y; k < n; k += 32) v += partial[(long long)k * pitch + col];
+  }
   acc[threadIdx.y][threadIdx.x] = v;
   __syncthreads();
   v = acc[threadIdx.x][threadIdx.y];
@@ -819,45 +898,54 @@ int copy_bytes(int D, size_t es, const void* const* p, const Strides* s, int n) 
 
 int check_sizes(int dtype, int T, int B, int D, float c, char* msg, int msg_len) {
   if (!op_float_dtype(dtype)) return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "dtype %d", dtype);
-  if (T < 0 || B < 0 || D < 1 || T > 0x7fffff00 || (long long)B * ((D + kLanes - 1) / kLanes) > 0x7fffffffll || (long long)B * kMaxCluster > 0x7fffffffll)
-    return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "need T, B >= 0, D >= 1 and B ceil(D / 64) below 2^31");
+  if (T < 0 || B < 0 || D < 1 || D > 0x7fffff00 || T > 0x7fffff00 ||
+      (double)B * ((D + kLanes - 1) / kLanes) * (T / kTile + 1) > 2147483647.0)
+    return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "need T, B >= 0, D >= 1 and fewer than 2^31 tiles of 64 x 64 values");
   if (!(c > 0.0f)) return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "c must be positive");
   return LSTM_APPROX_OK;
 }
 
-// Blocks of a cluster that share a stream's 64 channels: doubled while all
-// blocks still run at once (two to an SM; clusters of 8 or 16 leave some of a
-// processor group's slots empty) and each has a tile to itself.
-int cluster_size(int T, int B, int D) {
-  const long long items = (long long)B * ((D + kLanes - 1) / kLanes);
-  int n = 1;
-  while (n < kMaxCluster && items * 2 * n <= 256 && (long long)n * kTile < T) n *= 2;
-  return n;
-}
-
 template <typename T, int kCopy, bool kCuts, int kTensors, typename A>
-cudaError_t launch_scan(void (*kern)(A), int cluster, int blocks, cudaStream_t s, const A& args) {
+cudaError_t launch_scan(void (*kern)(A), cudaStream_t s, const A& args) {
   static thread_local DeviceSet ready;  // of the one kernel that this instance launches
-  constexpr size_t smem = kStages<T, kTensors> * kStageBytes<T, kTensors>;
-  constexpr int most = (int)(smem + exchange_bytes(kMaxCluster));
-  const cudaError_t e = once_per_device(&ready, [&] {
-    const cudaError_t e1 = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    return e1 != cudaSuccess ? e1 : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+  static thread_local int resident[64];
+  constexpr size_t smem = kStages * kStageBytes<T, kTensors>;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && dev >= 64) e = cudaErrorInvalidDevice;
+  if (e != cudaSuccess) return e;
+  e = once_per_device(&ready, [&] {
+    cudaError_t e1 = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    int per = 0, sms = 0;
+    if (e1 == cudaSuccess) e1 = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, kWarps * 32, smem);
+    if (e1 == cudaSuccess) e1 = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    resident[dev] = per * sms;
+    return e1;
   });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(blocks);
+  cfg.gridDim = dim3((unsigned)std::min<long long>(args.tasks.count, resident[dev]));
   cfg.blockDim = dim3(kWarps * 32);
-  cfg.dynamicSmemBytes = smem + exchange_bytes(cluster);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = cluster;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
+  attr[0].id = cudaLaunchAttributeCooperative;  // all blocks at once: they wait for one another's tiles
+  attr[0].val.cooperative = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 1 : 0;
+  cfg.numAttrs = args.tasks.tiles > 1 ? 1 : 0;  // (a single tile waits for none)
   return cudaLaunchKernelEx(&cfg, kern, args);
+}
+
+cudaError_t launch_prepare(const float* decay, float c, const Tasks& t, const Exchange& e, cudaStream_t s) {
+  const long long fill = (long long)(exchange_words(t) / 4), rates = (long long)t.slabs * kLanes;
+  const long long blocks = std::max((rates + 255) / 256, std::min<long long>((fill + 1023) / 1024, 4 * 152));
+  return op_launch(scan_prepare_kernel, dim3((unsigned)blocks), dim3(256), 0, s, decay, c, t.D, (int)rates, e.rate,
+                   reinterpret_cast<uint4*>(e.runs), fill);
+}
+
+// Exchange, then the backward pass's partial sums.
+size_t workspace_bytes_of(const Tasks& t) {
+  return (exchange_bytes(t) + (size_t)t.tiles * t.B * t.slabs * kLanes * sizeof(float) + 15) / 16 * 16 + 16;
 }
 
 // Strides of n tensors: HOST [2n], or all contiguous [T][B][D].
@@ -874,14 +962,20 @@ bool read_strides(const long long* strides, int n, int B, int D, Strides* out) {
 
 using namespace lstm_approx_impl;
 
+extern "C" size_t lstm_approx_gated_scan_workspace_bytes(int T, int B, int D) {
+  if (check_sizes(LSTM_APPROX_OP_FP32, T, B, D, 1.0f, nullptr, 0)) return 0;
+  return workspace_bytes_of(tasks_of(T, B, D));
+}
+
 extern "C" int lstm_approx_gated_scan(int dtype, const void* x, const void* r, const void* i, const float* decay,
                                       float c, const float* h0, const int32_t* lengths, const unsigned char* reset,
                                       int T, int B, int D, void* y, const long long* strides, float* h_last,
-                                      float* states, void* cuda_stream, char* msg, int msg_len) {
+                                      float* states, void* workspace, size_t workspace_bytes, void* cuda_stream,
+                                      char* msg, int msg_len) {
   if (msg && msg_len > 0) msg[0] = '\0';
   if (int rc = check_sizes(dtype, T, B, D, c, msg, msg_len)) return rc;
-  if (B > 0 && (!decay || !h_last || (T > 0 && (!x || !r || !i || !y))))
-    return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "x, r, i, decay, y and h_last must not be NULL");
+  if (B > 0 && (!decay || !h_last || !workspace || (T > 0 && (!x || !r || !i || !y))))
+    return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "x, r, i, decay, y, h_last and workspace must not be NULL");
   const size_t es = op_dtype_bytes(dtype);
   if (!op_aligned(x, es) || !op_aligned(r, es) || !op_aligned(i, es) || !op_aligned(y, es) || !op_aligned(decay, 4) ||
       !op_aligned(h0, 4) || !op_aligned(lengths, 4) || !op_aligned(h_last, 4) || !op_aligned(states, 4))
@@ -889,31 +983,31 @@ extern "C" int lstm_approx_gated_scan(int dtype, const void* x, const void* r, c
   Strides st[4];
   if (!read_strides(strides, 4, B, D, st))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "strides must not be negative");
+  const Tasks tasks = tasks_of(T, B, D);
+  const size_t need = workspace_bytes_of(tasks);
+  if (B > 0 && (!op_aligned(workspace, 16) || workspace_bytes < need))
+    return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "needs a 16-byte aligned workspace of %zu bytes", need);
   if (int rc = op_check_device(msg, msg_len)) return rc;
   if (B == 0) return LSTM_APPROX_OK;
-  const int slabs = (D + kLanes - 1) / kLanes, n = cluster_size(T, B, D);
-  ScanArgs a{x, r, i, y, st[0], st[1], st[2], st[3], decay, c, h0, lengths, reset, T, B, D, slabs, n,
-             h_last, states};
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  const Exchange exchange = exchange_of(workspace, tasks);
+  cudaError_t e = launch_prepare(decay, c, tasks, exchange, s);
+  if (int rc = op_launched(e, "scan preparation launch", msg, msg_len)) return rc;
+  ScanArgs a{x, r, i, y, st[0], st[1], st[2], st[3], h0, lengths, reset, tasks, exchange, h_last, states};
   const void* tensors[4] = {x, r, i, y};
   const int copy = copy_bytes(D, es, tensors, st, 4);
-  const cudaError_t e = op_for_type(dtype, [&](auto* t) {
+  e = op_for_type(dtype, [&](auto* t) {
     using E = std::remove_pointer_t<decltype(t)>;
-    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     auto go = [&](auto bytes) {
       constexpr int kCopy = decltype(bytes)::value;
-      return reset ? launch_scan<E, kCopy, true, 3>(gated_scan_kernel<E, kCopy, true>, n, slabs * B * n, s, a)
-                   : launch_scan<E, kCopy, false, 3>(gated_scan_kernel<E, kCopy, false>, n, slabs * B * n, s, a);
+      return reset ? launch_scan<E, kCopy, true, 3>(gated_scan_kernel<E, kCopy, true>, s, a)
+                   : launch_scan<E, kCopy, false, 3>(gated_scan_kernel<E, kCopy, false>, s, a);
     };
     if (copy == 16) return go(std::integral_constant<int, 16>());
-    if (copy == 4 || sizeof(E) == 4) return go(std::integral_constant<int, 4>());
+    if (copy == 4) return go(std::integral_constant<int, 4>());
     return go(std::integral_constant<int, sizeof(E) == 4 ? 4 : 2>());  // 32-bit values are always copied
   });
   return op_launched(e, "scan launch", msg, msg_len);
-}
-
-extern "C" size_t lstm_approx_gated_scan_workspace_bytes(int T, int B, int D) {
-  if (T < 0 || B < 0 || D < 1) return 0;
-  return ((size_t)B * cluster_size(T, B, D) * D * sizeof(float) + 15) / 16 * 16 + 16;
 }
 
 extern "C" int lstm_approx_gated_scan_backward(int dtype, const void* dy, const float* dh_last, const void* x,
@@ -937,35 +1031,37 @@ extern "C" int lstm_approx_gated_scan_backward(int dtype, const void* dy, const 
   Strides st[7];
   if (!read_strides(strides, 7, B, D, st))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "strides must not be negative");
-  const size_t need = lstm_approx_gated_scan_workspace_bytes(T, B, D);
+  const Tasks tasks = tasks_of(T, B, D);
+  const size_t need = workspace_bytes_of(tasks);
   if (!op_aligned(workspace, 16) || workspace_bytes < need)
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "needs a 16-byte aligned workspace of %zu bytes", need);
   if (int rc = op_check_device(msg, msg_len)) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  float* partial = static_cast<float*>(workspace);
-  const int n = cluster_size(T, B, D);
+  const Exchange exchange = exchange_of(workspace, tasks);
+  float* partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + exchange_bytes(tasks));
   if (B > 0) {
-    const int slabs = (D + kLanes - 1) / kLanes;
-    ScanBackwardArgs a{dy,    x,     r,      i,       dx,    dr, di, st[0], st[1], st[2], st[3], st[4], st[5], st[6],
-                       dh_last, decay, c, states, lengths, reset, T,  B,  D,     slabs, n, dh0,   partial};
+    cudaError_t e = launch_prepare(decay, c, tasks, exchange, s);
+    if (int rc = op_launched(e, "scan preparation launch", msg, msg_len)) return rc;
+    ScanBackwardArgs a{dy,    x,       r,      i,       dx,    dr,    di,       st[0], st[1],  st[2], st[3], st[4],
+                       st[5], st[6],   dh_last, states, lengths, reset, tasks, exchange, dh0, partial};
     const void* tensors[7] = {dy, x, r, i, dx, dr, di};
     const int copy = copy_bytes(D, es, tensors, st, 7);
-    const cudaError_t e = op_for_type(dtype, [&](auto* t) {
+    e = op_for_type(dtype, [&](auto* t) {
       using E = std::remove_pointer_t<decltype(t)>;
       auto go = [&](auto bytes) {
         constexpr int kCopy = decltype(bytes)::value;
-        return reset
-                   ? launch_scan<E, kCopy, true, 4>(gated_scan_backward_kernel<E, kCopy, true>, n, slabs * B * n, s, a)
-                   : launch_scan<E, kCopy, false, 4>(gated_scan_backward_kernel<E, kCopy, false>, n, slabs * B * n, s, a);
+        return reset ? launch_scan<E, kCopy, true, 4>(gated_scan_backward_kernel<E, kCopy, true>, s, a)
+                     : launch_scan<E, kCopy, false, 4>(gated_scan_backward_kernel<E, kCopy, false>, s, a);
       };
       if (copy == 16) return go(std::integral_constant<int, 16>());
-      if (copy == 4 || sizeof(E) == 4) return go(std::integral_constant<int, 4>());
+      if (copy == 4) return go(std::integral_constant<int, 4>());
       return go(std::integral_constant<int, sizeof(E) == 4 ? 4 : 2>());
     });
     if (int rc = op_launched(e, "scan backward launch", msg, msg_len)) return rc;
   }
   const cudaError_t e = op_launch(decay_gradient_kernel, dim3((D + 31) / 32), dim3(32, 32), 0, s,
-                                  static_cast<const float*>(partial), B * n, D, decay, ddecay);
+                                  static_cast<const float*>(partial), tasks.tiles * B, tasks.slabs * kLanes, D, decay,
+                                  ddecay);
   return op_launched(e, "decay gradient launch", msg, msg_len);
 }
 

@@ -357,7 +357,7 @@ def test_scan_in_a_graph(cuda_device):
 
 
 FORWARD = dict(dtype=0, x=64, r=64, i=64, decay=64, c=8.0, h0=None, lengths=None, reset=None, T=2, B=2, D=8, y=64,
-               strides=None, last=64, states=None)
+               strides=None, last=64, states=None, ws=64, nbytes=1 << 20)
 BACKWARD = dict(dtype=0, dy=64, dl=None, x=64, r=64, i=64, decay=64, c=8.0, states=64, lengths=None, reset=None, T=2,
                 B=2, D=8, dx=64, dr=64, di=64, strides=None, ddecay=64, dh0=64, ws=64, nbytes=1 << 20)
 STEP = dict(dtype=0, x=64, xp=8, r=64, rp=8, i=64, ip=8, decay=64, c=8.0, state=64, n=2, slots=None, reset=None, B=2, D=8,
@@ -365,7 +365,7 @@ STEP = dict(dtype=0, x=64, xp=8, r=64, rp=8, i=64, ip=8, decay=64, c=8.0, state=
 BAD = ([(FORWARD, "gated_scan", b) for b in (
             dict(dtype=3), dict(x=None), dict(r=None), dict(i=None), dict(decay=None), dict(y=None), dict(last=None),
             dict(T=-1), dict(B=-1), dict(D=0), dict(c=0.0), dict(c=float("nan")), dict(x=66), dict(dtype=1, y=65),
-            dict(h0=66), dict(lengths=65), dict(states=66), dict(decay=2), dict(strides="negative"))]
+            dict(h0=66), dict(lengths=65), dict(states=66), dict(decay=2), dict(ws=None), dict(ws=72), dict(nbytes=16), dict(strides="negative"))]
        + [(BACKWARD, "gated_scan_backward", b) for b in (
             dict(dtype=-1), dict(dy=None), dict(states=None), dict(dx=None), dict(dr=None), dict(di=None),
             dict(ddecay=None), dict(dh0=None), dict(ws=None), dict(ws=72), dict(nbytes=16), dict(T=-1), dict(D=0),
