@@ -73,11 +73,6 @@ __device__ __forceinline__ float rsqrt_approx(float x) {
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ float sqrt_approx(float x) {
-  float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 __device__ __forceinline__ uint64_t both(float v) { return f32x2(v, v); }
 __device__ __forceinline__ uint64_t sub2(uint64_t a, uint64_t b) {
   uint64_t r;
@@ -151,12 +146,7 @@ __device__ __forceinline__ uint64_t decay_of(uint64_t low, const Constants& k) {
 __device__ __forceinline__ uint64_t m2_of(uint64_t low, uint64_t a, const Constants& k) {
   return mul2(low, add2(a, k.one));
 }
-__device__ __forceinline__ uint64_t sqrt2(uint64_t v) {
-  float a, b;
-  f32x2_split(v, a, b);
-  return f32x2(sqrt_approx(a), sqrt_approx(b));
-}
-// 1 / sqrt(v), at most 2^63
+// 1 / sqrt(v), at most 2^63 (so that v / sqrt(v) is 0 at 0)
 __device__ __forceinline__ uint64_t rsqrt2(uint64_t v) {
   float a, b;
   f32x2_split(add2(v, both(1.17549435e-38f)), a, b);
@@ -204,50 +194,54 @@ struct Strides {
 // Timesteps past `len` and channels past D come out as zeros, nothing of
 // theirs is read.
 template <typename T, int kCopy>
-__device__ __forceinline__ void stage(T* dst, const T* src, long long stride, int ts, int len, int ch0, int D) {
-  const int lane = threadIdx.x & 31;
-  if constexpr (kCopy >= 4) {
-    constexpr int kPer = kCopy / (int)sizeof(T);          // values of a copy
-    constexpr int kRow = kLanes / kPer;                   // copies of a row
-    constexpr int kRows = kRow >= 32 ? 1 : 32 / kRow;     // rows of one turn of the warp
-    constexpr int kTurns = kRow >= 32 ? kRow / 32 : 1;    // turns of one row
-    const int row0 = kRow >= 32 ? 0 : lane / kRow;
-    auto copy = [&](uint32_t to, const T* from, int bytes) {
-      if constexpr (kCopy == 16)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
-      else
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
-    };
-    const T* from = src + (ts + row0) * stride + lane % kRow * kPer;
-    const uint32_t to = smem_u32(dst + row0 * kLanes + lane % kRow * kPer);
-    if (ts + kSteps <= len && ch0 + kLanes <= D) {
+struct Stage {
+  static constexpr int kPer = kCopy >= 4 ? kCopy / (int)sizeof(T) : 1;  // values of a copy
+  static constexpr int kRow = kLanes / kPer;                            // copies of a row
+  static constexpr int kRows = kRow >= 32 ? 1 : 32 / kRow;              // rows of one turn of the warp
+  static constexpr int kTurns = kRow >= 32 ? kRow / 32 : 1;             // turns of one row
+  static __device__ __forceinline__ int row0() { return kRow >= 32 ? 0 : (threadIdx.x & 31) / kRow; }
+  static __device__ __forceinline__ int col0() { return (threadIdx.x & 31) % kRow * kPer; }
+
+  // Byte offset of this lane's first copy from a tile's first value.
+  static __device__ __forceinline__ long long lane_offset(long long stride) {
+    return ((long long)((threadIdx.x >> 5) * kSteps + row0()) * stride + col0()) * (int)sizeof(T);
+  }
+  static __device__ __forceinline__ void copy(T* to, const char* from, bool in) {
+    if constexpr (kCopy == 16)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(in ? 16 : 0)
+                   : "memory");
+    else if constexpr (kCopy == 4)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(in ? 4 : 0)
+                   : "memory");
+    else
+      *to = in ? *reinterpret_cast<const T*>(from) : from_f32<T>(0.0f);
+  }
+  // dst: the warp's [kSteps][64]; tile: the tile's first value; rows, cols: how many of the warp's timesteps and the
+  // tile's channels exist.
+  static __device__ __forceinline__ void run(T* dst, const void* tile, long long offset, long long stride, int rows, int cols) {
+    const char* from = static_cast<const char*>(tile) + offset;
+    T* to = dst + row0() * kLanes + col0();
+    const long long step = kRows * stride * (int)sizeof(T);
+    if (rows >= kSteps && cols >= kLanes) {
 #pragma unroll
-      for (int s = 0; s < kSteps; s += kRows, from += kRows * stride) {
+      for (int s = 0; s < kSteps; s += kRows, from += step) {
 #pragma unroll
         for (int q = 0; q < kTurns; ++q)
-          copy(to + (s * kLanes + 32 * q * kPer) * (int)sizeof(T), from + 32 * q * kPer, kCopy);
+          copy(to + s * kLanes + 32 * q * kPer, from + 32 * q * kPer * (int)sizeof(T), true);
       }
     } else {
 #pragma unroll 1
-      for (int s = 0; s < kSteps; s += kRows, from += kRows * stride) {
+      for (int s = 0; s < kSteps; s += kRows, from += step) {
 #pragma unroll
         for (int q = 0; q < kTurns; ++q) {
-          const bool in = ts + s + row0 < len && ch0 + (lane % kRow + 32 * q) * kPer < D;
-          copy(to + (s * kLanes + 32 * q * kPer) * (int)sizeof(T), in ? from + 32 * q * kPer : src, in ? kCopy : 0);
+          const bool in = s + row0() < rows && col0() + 32 * q * kPer < cols;
+          copy(to + s * kLanes + 32 * q * kPer,
+               in ? from + 32 * q * kPer * (int)sizeof(T) : static_cast<const char*>(tile), in);
         }
       }
     }
-  } else {
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const int col = lane + 32 * q;
-        dst[s * kLanes + col] = ts + s < len && ch0 + col < D ? src[(ts + s) * stride + col] : from_f32<T>(0.0f);
-      }
-    }
   }
-}
+};
 __device__ __forceinline__ void stage_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void stage_wait() {
@@ -279,16 +273,17 @@ struct Task {
 struct Tasks {
   int T, B, D;
   int slabs, tiles;  // of a stream's channels, of the sequence (one at least)
-  int group;         // tiles of a group: a function of the shape
+  int group_log2;    // of the tiles of a group: a function of the shape
   long long count;   // slabs * B * tiles
 };
 // Shapes with few streams and channels have many tiles of one sequence in flight at once (about three blocks to an
 // SM share them); where there are more sequences than blocks a tile's predecessor is done long before.
 inline Tasks tasks_of(int T, int B, int D) {
-  Tasks t{T, B, D, (D + kLanes - 1) / kLanes, std::max(1, (T + kTile - 1) / kTile), 1, 0};
+  Tasks t{T, B, D, (D + kLanes - 1) / kLanes, std::max(1, (T + kTile - 1) / kTile), 0, 0};
   const long long items = (long long)t.slabs * B;
   t.count = items * t.tiles;
-  while (t.group < kMaxGroup && items * t.group < 3 * 152) t.group *= 2;
+  t.group_log2 = 0;
+  while ((1 << t.group_log2) < kMaxGroup && items << t.group_log2 < 3 * 152) ++t.group_log2;
   return t;
 }
 // Tasks go round the blocks in the order slab (fastest), stream, tile.
@@ -311,6 +306,44 @@ __device__ __forceinline__ Task advance(const Tasks& t, Task at, Task step) {
   return at;
 }
 
+// A task's place in its group, and whether it is the last there.
+__device__ __forceinline__ int place_of(const Tasks& t, const Task& at) { return at.order & ((1 << t.group_log2) - 1); }
+__device__ __forceinline__ bool ends_group(const Tasks& t, const Task& at) {
+  return place_of(t, at) == (1 << t.group_log2) - 1;
+}
+
+// What the block's warps need of a task, worked out by one of them two tasks ahead.
+struct Plan {
+  Task at;
+  int len;              // of the stream
+  char* tensors[7];     // the tile's first value in each tensor
+};
+// Tensors of a call as the kernels take them.
+template <int N>
+struct Tensors {
+  char* base[N];
+  Strides strides[N];
+};
+// Called by one warp (all its lanes).
+template <typename T, int N>
+__device__ __forceinline__ void make_plan(Plan& plan, const Tasks& t, const Tensors<N>& tensors, const int* lengths,
+                                          const Task& at, bool back) {
+  const int lane = threadIdx.x & 31;
+  if (at.order >= t.tiles) {
+    if (lane == 0) plan.at = at;
+    return;
+  }
+  const int tile = back ? t.tiles - 1 - at.order : at.order;
+  if (lane < N) {
+    const Strides& st = tensors.strides[lane];
+    plan.tensors[lane] =
+        tensors.base[lane] + (at.b * st.b + (long long)tile * kTile * st.t + at.slab * kLanes) * (long long)sizeof(T);
+  } else if (lane == N) {
+    plan.at = at;
+    plan.len = length_of(lengths, at.b, t.T);
+  }
+}
+
 // The exchange in memory: c softplus(decay) [slabs * 64], then each tile's run [tiles][items][32] (16 bytes for a
 // lane's two channels), then the state before each group but the first [groups - 1][items][32] (8 bytes).
 struct Exchange {
@@ -327,7 +360,7 @@ __host__ __device__ inline Exchange exchange_of(void* base, const Tasks& t) {
 }
 inline size_t exchange_words(const Tasks& t) {  // of the runs and states (none for a single tile)
   if (t.tiles == 1) return 0;
-  const long long items = (long long)t.slabs * t.B, groups = (t.tiles + t.group - 1) / t.group;
+  const long long items = (long long)t.slabs * t.B, groups = (t.tiles - 1) / (1 << t.group_log2) + 1;
   return (size_t)(t.count * 32 * 4 + (groups - 1) * items * 32 * 2);
 }
 inline size_t exchange_bytes(const Tasks& t) { return ((size_t)t.slabs * kLanes + exchange_words(t)) * 4; }
@@ -409,13 +442,13 @@ __device__ __forceinline__ ulonglong2 exchange_runs(const Tasks& t, const Exchan
                                                     const ulonglong2 (&mine)[kWarps][32], int w0, int dw, uint64_t first) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long items = (long long)t.slabs * t.B, item = (long long)at.b * t.slabs + at.slab;
-  const int place = at.order % t.group, group = at.order / t.group;
+  const int place = place_of(t, at), group = at.order >> t.group_log2;
   ulonglong2 all = make_ulonglong2(0ull, 0ull);
   if (warp == 0) {
     all = mine[w0][lane];
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) all = join<kCuts>(all, mine[w0 + dw * w][lane]);
-    if (place != t.group - 1 && at.order != t.tiles - 1) publish(e.runs + (at.order * items + item) * 32 + lane, all);
+    if (!ends_group(t, at) && at.order != t.tiles - 1) publish(e.runs + (at.order * items + item) * 32 + lane, all);
   }
   if (warp == kWarps - 1) sm.start[lane] = group == 0 ? first : receive(e.states + ((group - 1) * items + item) * 32 + lane);
   for (int q = warp; q < place; q += kWarps)
@@ -425,16 +458,14 @@ __device__ __forceinline__ ulonglong2 exchange_runs(const Tasks& t, const Exchan
 // The state before a tile, after exchange_runs and the barrier.
 template <bool kCuts>
 __device__ __forceinline__ uint64_t state_before(const Tasks& t, const Task& at, const Join& sm) {
-  const int lane = threadIdx.x & 31, place = at.order % t.group;
+  const int lane = threadIdx.x & 31, place = place_of(t, at);
   uint64_t h = sm.start[lane];
   for (int q = 0; q < place; ++q) h = after<kCuts>(sm.before[q][lane], h);
   return h;
 }
 
 struct ScanArgs {
-  const void *x, *r, *i;
-  void* y;
-  Strides sx, sr, si, sy;
+  Tensors<4> io;  // x, r, i, y
   const float* h0;
   const int* lengths;
   const unsigned char* reset;
@@ -477,7 +508,8 @@ __device__ __forceinline__ void form_runs(const T* here, uint64_t rate, const Co
     const Gates g =
         gates_of<kFar>(staged_pair<T>(p + kTile * kLanes), staged_pair<T>(p + 2 * kTile * kLanes), rate, k);
     A[s] = decay_of(g.low, k);
-    U[s] = mul2(mul2(sqrt2(m2_of(g.low, A[s], k)), g.si), staged_pair<T>(p));
+    const uint64_t m2 = m2_of(g.low, A[s], k);
+    U[s] = mul2(mul2(mul2(m2, rsqrt2(m2)), g.si), staged_pair<T>(p));
   }
 }
 
@@ -510,36 +542,45 @@ template <typename T, int kCopy, bool kCuts>
 __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 2 : 3) gated_scan_kernel(const ScanArgs a) {
   extern __shared__ __align__(16) unsigned char staged[];
   __shared__ Join sm;
+  __shared__ Plan plans[3];  // of this task and the next two
   constexpr bool kVec = kCopy >= 2 * (int)sizeof(T);  // a lane's two channels of y in one store
   constexpr int kOne = kTile * kLanes;                // values of one staged tensor
   const Tasks& t = a.tasks;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  using St = Stage<T, kCopy>;
+  long long offset[3];
+#pragma unroll
+  for (int n = 0; n < 3; ++n) offset[n] = St::lane_offset(a.io.strides[n].t);
   // this warp's part of a task's tile into stage n
   auto buffer = [&](int n) { return reinterpret_cast<T*>(staged + n * kStageBytes<T, 3>) + warp * kSteps * kLanes; };
-  auto fetch = [&](int n, const Task& at) {
-    T* to = buffer(n);
-    const int ts = at.order * kTile + warp * kSteps, ch0 = at.slab * kLanes;
-    const int len = length_of(a.lengths, at.b, t.T);
-    if (ts < len) {
-      stage<T, kCopy>(to, static_cast<const T*>(a.x) + at.b * a.sx.b + ch0, a.sx.t, ts, len, ch0, t.D);
-      stage<T, kCopy>(to + kOne, static_cast<const T*>(a.r) + at.b * a.sr.b + ch0, a.sr.t, ts, len, ch0, t.D);
-      stage<T, kCopy>(to + 2 * kOne, static_cast<const T*>(a.i) + at.b * a.si.b + ch0, a.si.t, ts, len, ch0, t.D);
+  auto fetch = [&](int n, const Plan& plan) {
+    const int rows = plan.len - plan.at.order * kTile - warp * kSteps, cols = t.D - plan.at.slab * kLanes;
+    if (rows > 0) {
+      T* to = buffer(n);
+#pragma unroll
+      for (int m = 0; m < 3; ++m) St::run(to + m * kOne, plan.tensors[m], offset[m], a.io.strides[m].t, rows, cols);
     }
-    stage_commit();
   };
-  Task at = task_at(t, blockIdx.x);
   const Task step = task_at(t, gridDim.x);
-  fetch(0, at);
+  Task ahead = advance(t, task_at(t, blockIdx.x), step);  // the furthest task with a plan
+  if (warp == 2) {
+    make_plan<T>(plans[0], t, a.io, a.lengths, task_at(t, blockIdx.x), false);
+    make_plan<T>(plans[1], t, a.io, a.lengths, ahead, false);
+  }
+  __syncthreads();
+  fetch(0, plans[0]);
+  stage_commit();
   const Constants k = constants();
-  int turn = 0;
-  for (; at.order < t.tiles; turn ^= 1) {
-    const Task next = advance(t, at, step);
+  int turn = 0, now = 0;
+  for (; plans[now].at.order < t.tiles; turn ^= 1) {
+    const Plan &plan = plans[now], &next = plans[now == 2 ? 0 : now + 1];
+    const Task at = plan.at;
     const uint64_t rate = *reinterpret_cast<const uint64_t*>(a.exchange.rate + at.slab * kLanes + 2 * lane);
     __syncwarp();  // the lanes are done with the stage that the next tile goes to
-    if (next.order < t.tiles) fetch(turn ^ 1, next);
-    else stage_commit();
+    if (next.at.order < t.tiles) fetch(turn ^ 1, next);
+    stage_commit();
     const int ch = at.slab * kLanes + 2 * lane, left = t.D - ch;  // channels of this lane that exist: min(left, 2)
-    const int ts = at.order * kTile + warp * kSteps, len = length_of(a.lengths, at.b, t.T);
+    const int ts = at.order * kTile + warp * kSteps, len = plan.len;
     const long long state_at = (long long)at.b * t.D + ch;
     const unsigned resets = kCuts ? reset_bits(a.reset, ts, len, at.b, t.B) : 0u;
     const bool whole = ts + kSteps <= len;
@@ -558,15 +599,19 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 2 : 3) gated_sca
     sm.runs[turn][warp][lane] = kCuts && resets ? join_steps<true>(A, U, resets) : join_steps<false>(A, U, 0u);
     __syncthreads();
     uint64_t first = 0ull;
-    if (warp == kWarps - 1 && at.order < t.group && a.h0) first = load_f32x2(a.h0 + state_at, left);
+    if (warp == kWarps - 1 && at.order >> t.group_log2 == 0 && a.h0) first = load_f32x2(a.h0 + state_at, left);
     const ulonglong2 tile = exchange_runs<kCuts>(t, a.exchange, at, sm, sm.runs[turn], 0, 1, first);
+    if (warp == 2) {
+      ahead = advance(t, ahead, step);
+      make_plan<T>(plans[now == 0 ? 2 : now - 1], t, a.io, a.lengths, ahead, false);
+    }
     __syncthreads();
     uint64_t h = state_before<kCuts>(t, at, sm);
     if (warp == 0) {
       const uint64_t end = after<kCuts>(tile, h);
       if (at.order == t.tiles - 1) store_f32x2(a.h_last + state_at, left, end);
-      else if (at.order % t.group == t.group - 1)
-        publish(a.exchange.states + ((long long)(at.order / t.group) * t.slabs * t.B + at.b * t.slabs + at.slab) * 32 + lane, end);
+      else if (ends_group(t, at))
+        publish(a.exchange.states + ((long long)(at.order >> t.group_log2) * t.slabs * t.B + at.b * t.slabs + at.slab) * 32 + lane, end);
       if (a.states && at.order * kTile < t.T)
         store_f32x2(a.states + (long long)at.order * t.B * t.D + state_at, left, h);
     }
@@ -582,24 +627,23 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 2 : 3) gated_sca
       for (int s = 0; s < kSteps; ++s) h = U[s] = fma2(A[s], h, U[s]);
     }
     if (left > 0) {
-      T* to = static_cast<T*>(a.y) + at.b * a.sy.b + ch + ts * a.sy.t;
+      const long long sy = a.io.strides[3].t;
+      T* to = reinterpret_cast<T*>(plan.tensors[3]) + warp * kSteps * sy + 2 * lane;
       if (whole) {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s, to += a.sy.t) store_both<T, kVec>(to, left, U[s]);
+        for (int s = 0; s < kSteps; ++s, to += sy) store_both<T, kVec>(to, left, U[s]);
       } else {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s, to += a.sy.t)
+        for (int s = 0; s < kSteps; ++s, to += sy)
           if (ts + s < t.T) store_both<T, kVec>(to, left, ts + s < len ? U[s] : 0ull);
       }
     }
-    at = next;
+    now = now == 2 ? 0 : now + 1;
   }
 }
 
 struct ScanBackwardArgs {
-  const void *dy, *x, *r, *i;
-  void *dx, *dr, *di;
-  Strides sdy, sx, sr, si, sdx, sdr, sdi;
+  Tensors<7> io;  // x, r, i, dy, dx, dr, di
   const float* dh_last;
   const float* states;
   const int* lengths;
@@ -622,7 +666,8 @@ __device__ __forceinline__ void form_gates(const T* here, uint64_t rate, const C
     low[s] = g.low;
     sr[s] = g.sr;
     si[s] = g.si;
-    U[s] = mul2(mul2(sqrt2(m2_of(g.low, decay_of(g.low, k), k)), g.si), staged_pair<T>(p));
+    const uint64_t m2 = m2_of(g.low, decay_of(g.low, k), k);
+    U[s] = mul2(mul2(mul2(m2, rsqrt2(m2)), g.si), staged_pair<T>(p));
   }
 }
 
@@ -673,22 +718,24 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
   __shared__ Join sm;                             // p -> A p + V
   __shared__ ulonglong2 ahead[2][kWarps][32];     // h -> A h + U
   __shared__ uint64_t sums[kWarps][32];           // E over each warp's timesteps of the last task
+  __shared__ Plan plans[3];
   constexpr bool kVec = kCopy >= 2 * (int)sizeof(T);
   constexpr int kOne = kTile * kLanes;
   const Tasks& t = a.tasks;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  using St = Stage<T, kCopy>;
+  long long offset[4];
+#pragma unroll
+  for (int n = 0; n < 4; ++n) offset[n] = St::lane_offset(a.io.strides[n].t);
   auto buffer = [&](int n) { return reinterpret_cast<T*>(staged + n * kStageBytes<T, 4>) + warp * kSteps * kLanes; };
-  auto fetch = [&](int n, const Task& at) {
-    T* to = buffer(n);
-    const int ts = (t.tiles - 1 - at.order) * kTile + warp * kSteps, ch0 = at.slab * kLanes;
-    const int len = length_of(a.lengths, at.b, t.T);
-    if (ts < len) {
-      stage<T, kCopy>(to, static_cast<const T*>(a.x) + at.b * a.sx.b + ch0, a.sx.t, ts, len, ch0, t.D);
-      stage<T, kCopy>(to + kOne, static_cast<const T*>(a.r) + at.b * a.sr.b + ch0, a.sr.t, ts, len, ch0, t.D);
-      stage<T, kCopy>(to + 2 * kOne, static_cast<const T*>(a.i) + at.b * a.si.b + ch0, a.si.t, ts, len, ch0, t.D);
-      stage<T, kCopy>(to + 3 * kOne, static_cast<const T*>(a.dy) + at.b * a.sdy.b + ch0, a.sdy.t, ts, len, ch0, t.D);
+  auto fetch = [&](int n, const Plan& plan) {
+    const int rows = plan.len - (t.tiles - 1 - plan.at.order) * kTile - warp * kSteps;
+    const int cols = t.D - plan.at.slab * kLanes;
+    if (rows > 0) {
+      T* to = buffer(n);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) St::run(to + m * kOne, plan.tensors[m], offset[m], a.io.strides[m].t, rows, cols);
     }
-    stage_commit();
   };
   auto add_up = [&](const Task& at) {  // the sums of a finished task into its partial
     uint64_t v = sums[0][lane];
@@ -697,21 +744,28 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
     const long long row = (long long)(t.tiles - 1 - at.order) * t.B + at.b;
     *reinterpret_cast<uint64_t*>(a.partial + (row * t.slabs + at.slab) * kLanes + 2 * lane) = v;
   };
-  Task at = task_at(t, blockIdx.x), done = at;
   const Task step = task_at(t, gridDim.x);
-  fetch(0, at);
+  Task done = task_at(t, blockIdx.x), ahead_task = advance(t, done, step);
+  if (warp == 2) {
+    make_plan<T>(plans[0], t, a.io, a.lengths, done, true);
+    make_plan<T>(plans[1], t, a.io, a.lengths, ahead_task, true);
+  }
+  __syncthreads();
+  fetch(0, plans[0]);
+  stage_commit();
   const Constants k = constants();
-  int turn = 0;
+  int turn = 0, now = 0;
   bool any = false;
-  for (; at.order < t.tiles; turn ^= 1) {
-    const Task next = advance(t, at, step);
+  for (; plans[now].at.order < t.tiles; turn ^= 1) {
+    const Plan &plan = plans[now], &next = plans[now == 2 ? 0 : now + 1];
+    const Task at = plan.at;
     const uint64_t rate = *reinterpret_cast<const uint64_t*>(a.exchange.rate + at.slab * kLanes + 2 * lane);
     __syncwarp();
-    if (next.order < t.tiles) fetch(turn ^ 1, next);
-    else stage_commit();
+    if (next.at.order < t.tiles) fetch(turn ^ 1, next);
+    stage_commit();
     const int tile = t.tiles - 1 - at.order;
     const int ch = at.slab * kLanes + 2 * lane, left = t.D - ch;
-    const int ts = tile * kTile + warp * kSteps, len = length_of(a.lengths, at.b, t.T);
+    const int ts = tile * kTile + warp * kSteps, len = plan.len;
     const long long state_at = (long long)at.b * t.D + ch;
     const unsigned resets = kCuts ? reset_bits(a.reset, ts, len, at.b, t.B) : 0u;
     const bool whole = ts + kSteps <= len, some = ts < len;
@@ -735,21 +789,28 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
     __syncthreads();
     if (warp == 1 && any) add_up(done);
     uint64_t first = 0ull;
-    if (warp == kWarps - 1 && at.order < t.group && a.dh_last) first = load_f32x2(a.dh_last + state_at, left);
+    if (warp == kWarps - 1 && at.order >> t.group_log2 == 0 && a.dh_last) first = load_f32x2(a.dh_last + state_at, left);
     const ulonglong2 run = exchange_runs<kCuts>(t, a.exchange, at, sm, sm.runs[turn], kWarps - 1, -1, first);
+    if (warp == 2) {
+      ahead_task = advance(t, ahead_task, step);
+      make_plan<T>(plans[now == 0 ? 2 : now - 1], t, a.io, a.lengths, ahead_task, true);
+    }
     for (int w = 0; w < warp; ++w) h = after<kCuts>(ahead[turn][w][lane], h);
     __syncthreads();
     uint64_t p = state_before<kCuts>(t, at, sm);
     if (warp == 0) {
       const uint64_t end = after<kCuts>(run, p);
       if (at.order == t.tiles - 1) store_f32x2(a.dh0 + state_at, left, end);
-      else if (at.order % t.group == t.group - 1)
-        publish(a.exchange.states + ((long long)(at.order / t.group) * t.slabs * t.B + at.b * t.slabs + at.slab) * 32 + lane, end);
+      else if (ends_group(t, at))
+        publish(a.exchange.states + ((long long)(at.order >> t.group_log2) * t.slabs * t.B + at.b * t.slabs + at.slab) * 32 + lane, end);
     }
     for (int w = kWarps - 1; w > warp; --w) p = after<kCuts>(sm.runs[turn][w][lane], p);
-    T* dx = static_cast<T*>(a.dx) + at.b * a.sdx.b + ch;
-    T* dr = static_cast<T*>(a.dr) + at.b * a.sdr.b + ch;
-    T* di = static_cast<T*>(a.di) + at.b * a.sdi.b + ch;
+    // the gradients' places at the warp's last timestep, from where the loops below go back
+    const long long sx = a.io.strides[4].t, sr_t = a.io.strides[5].t, si_t = a.io.strides[6].t;
+    const int last = warp * kSteps + kSteps - 1;
+    T* to_x = reinterpret_cast<T*>(plan.tensors[4]) + last * sx + 2 * lane;
+    T* to_r = reinterpret_cast<T*>(plan.tensors[5]) + last * sr_t + 2 * lane;
+    T* to_i = reinterpret_cast<T*>(plan.tensors[6]) + last * si_t + 2 * lane;
     uint64_t sum = 0ull;
     if (some) {
       // U becomes the state before each timestep
@@ -769,10 +830,6 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
           h = fma2(decay_of(low[s], k), h, u);
         }
       }
-      // from the warp's last timestep back
-      T* to_x = dx + (ts + kSteps - 1) * a.sdx.t;
-      T* to_r = dr + (ts + kSteps - 1) * a.sdr.t;
-      T* to_i = di + (ts + kSteps - 1) * a.sdi.t;
       if (whole && left > 0) {
 #pragma unroll
         for (int s = kSteps - 1; s >= 0; --s) {
@@ -782,9 +839,9 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
           store_both<T, kVec>(to_x, left, g.x);
           store_both<T, kVec>(to_r, left, g.r);
           store_both<T, kVec>(to_i, left, g.i);
-          to_x -= a.sdx.t;
-          to_r -= a.sdr.t;
-          to_i -= a.sdi.t;
+          to_x -= sx;
+          to_r -= sr_t;
+          to_i -= si_t;
         }
       } else {
 #pragma unroll
@@ -798,22 +855,23 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
             store_both<T, kVec>(to_r, left, g.r);
             store_both<T, kVec>(to_i, left, g.i);
           }
-          to_x -= a.sdx.t;
-          to_r -= a.sdr.t;
-          to_i -= a.sdi.t;
+          to_x -= sx;
+          to_r -= sr_t;
+          to_i -= si_t;
         }
       }
     } else if (left > 0) {
-      for (int n = ts; n < min(ts + kSteps, t.T); ++n) {
-        store_pair<T, kVec>(dx + n * a.sdx.t, left, 0.0f, 0.0f);
-        store_pair<T, kVec>(dr + n * a.sdr.t, left, 0.0f, 0.0f);
-        store_pair<T, kVec>(di + n * a.sdi.t, left, 0.0f, 0.0f);
+      for (int s = kSteps - 1; s >= 0; --s, to_x -= sx, to_r -= sr_t, to_i -= si_t) {
+        if (ts + s >= t.T) continue;
+        store_pair<T, kVec>(to_x, left, 0.0f, 0.0f);
+        store_pair<T, kVec>(to_r, left, 0.0f, 0.0f);
+        store_pair<T, kVec>(to_i, left, 0.0f, 0.0f);
       }
     }
     sums[warp][lane] = sum;
     done = at;
     any = true;
-    at = next;
+    now = now == 2 ? 0 : now + 1;
   }
   __syncthreads();
   if (warp == 1 && any) add_up(done);
@@ -873,8 +931,8 @@ __global__ void __launch_bounds__(256) gated_step_kernel(const StepArgs a) {
     uint64_t h = load_f32x2(st, left);
     if (a.reset && a.reset[b] != 0) h = 0ull;
     const Gates g = gates_of<true>(f32x2(r.x, r.y), f32x2(i.x, i.y), rate, k);
-    const uint64_t A = decay_of(g.low, k);
-    h = fma2(A, h, mul2(mul2(sqrt2(m2_of(g.low, A, k)), g.si), f32x2(x.x, x.y)));
+    const uint64_t A = decay_of(g.low, k), m2 = m2_of(g.low, A, k);
+    h = fma2(A, h, mul2(mul2(mul2(m2, rsqrt2(m2)), g.si), f32x2(x.x, x.y)));
     store_f32x2(st, left, h);
     float h0, h1;
     f32x2_split(h, h0, h1);
@@ -948,6 +1006,14 @@ size_t workspace_bytes_of(const Tasks& t) {
   return (exchange_bytes(t) + (size_t)t.tiles * t.B * t.slabs * kLanes * sizeof(float) + 15) / 16 * 16 + 16;
 }
 
+template <int N>
+void set_tensors(Tensors<N>& io, const void* const (&p)[N], const Strides* st) {
+  for (int n = 0; n < N; ++n) {
+    io.base[n] = static_cast<char*>(const_cast<void*>(p[n]));
+    io.strides[n] = st[n];
+  }
+}
+
 // Strides of n tensors: HOST [2n], or all contiguous [T][B][D].
 bool read_strides(const long long* strides, int n, int B, int D, Strides* out) {
   for (int k = 0; k < n; ++k) {
@@ -993,8 +1059,9 @@ extern "C" int lstm_approx_gated_scan(int dtype, const void* x, const void* r, c
   const Exchange exchange = exchange_of(workspace, tasks);
   cudaError_t e = launch_prepare(decay, c, tasks, exchange, s);
   if (int rc = op_launched(e, "scan preparation launch", msg, msg_len)) return rc;
-  ScanArgs a{x, r, i, y, st[0], st[1], st[2], st[3], h0, lengths, reset, tasks, exchange, h_last, states};
   const void* tensors[4] = {x, r, i, y};
+  ScanArgs a{{}, h0, lengths, reset, tasks, exchange, h_last, states};
+  set_tensors(a.io, tensors, st);
   const int copy = copy_bytes(D, es, tensors, st, 4);
   e = op_for_type(dtype, [&](auto* t) {
     using E = std::remove_pointer_t<decltype(t)>;
@@ -1042,10 +1109,11 @@ extern "C" int lstm_approx_gated_scan_backward(int dtype, const void* dy, const 
   if (B > 0) {
     cudaError_t e = launch_prepare(decay, c, tasks, exchange, s);
     if (int rc = op_launched(e, "scan preparation launch", msg, msg_len)) return rc;
-    ScanBackwardArgs a{dy,    x,       r,      i,       dx,    dr,    di,       st[0], st[1],  st[2], st[3], st[4],
-                       st[5], st[6],   dh_last, states, lengths, reset, tasks, exchange, dh0, partial};
-    const void* tensors[7] = {dy, x, r, i, dx, dr, di};
-    const int copy = copy_bytes(D, es, tensors, st, 7);
+    const void* tensors[7] = {x, r, i, dy, dx, dr, di};
+    const Strides order[7] = {st[1], st[2], st[3], st[0], st[4], st[5], st[6]};
+    ScanBackwardArgs a{{}, dh_last, states, lengths, reset, tasks, exchange, dh0, partial};
+    set_tensors(a.io, tensors, order);
+    const int copy = copy_bytes(D, es, tensors, order, 7);
     e = op_for_type(dtype, [&](auto* t) {
       using E = std::remove_pointer_t<decltype(t)>;
       auto go = [&](auto bytes) {
