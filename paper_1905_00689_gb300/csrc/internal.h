@@ -494,6 +494,10 @@ cudaError_t launch_tc_loop(const TcMap& V, const TcMap& U, const TcMap& Hm, cons
 bool tc_make_map_planes(TcMap* m, const void* base, uint64_t inner, uint64_t rows, uint64_t pitch_bytes,
                         uint64_t plane_bytes, uint32_t box_rows);
 
+// 3-D tensor [outer][mid][inner] of fp32 or 16-bit values, boxes of 64 inner elements x box_mid x box_outer, unswizzled.
+bool tc_make_map_steps(TcMap* m, const void* base, bool f32, uint64_t inner, uint64_t mid, uint64_t outer,
+                       uint64_t mid_bytes, uint64_t outer_bytes, uint32_t box_mid, uint32_t box_outer);
+
 // Compressed tau' (the recurrent part of the pruned v as (column, value)
 // entries per storage row g*Ks + k, entries off[row] .. off[row + 1]) on the
 // CUDA cores, for the tensor path; H <= tau_sparse_max_h().

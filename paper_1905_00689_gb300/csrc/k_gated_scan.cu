@@ -53,10 +53,14 @@ namespace {
 using namespace lstm_approx_dev;
 
 constexpr int kWarps = 8;
-constexpr int kSteps = 8;                 // timesteps of a warp in a tile
-constexpr int kTile = kWarps * kSteps;    // timesteps of a tile
-constexpr int kLanes = 64;                // channels of a block: two to a lane
-static_assert(kTile == LSTM_APPROX_SCAN_CHUNK, "one saved state per tile");
+constexpr int kLanes = 64;                    // channels of a block: two to a lane
+constexpr int kChunk = LSTM_APPROX_SCAN_CHUNK;  // timesteps from one saved state to the next
+// Timesteps of a warp in a tile, kWarps times that in the tile: 16 forward for
+// 16-bit values, 8 where the registers or shared memory do not hold so many.
+template <typename T>
+constexpr int kForwardSteps = sizeof(T) == 4 ? 8 : 16;
+constexpr int kBackwardSteps = 8;
+static_assert(kWarps * kBackwardSteps == kChunk, "the backward pass takes one saved state per tile");
 
 // softplus(d) = log(1 + e^d) and sigma(d) / softplus(d), both to fp32 accuracy
 // over the whole range (the ratio tends to 1 for d -> -inf).
@@ -185,75 +189,110 @@ struct Strides {
   long long t, b;
 };
 
-// How a tile comes into shared memory: by asynchronous copies of kCopy bytes
-// where every address is a multiple of it (16: everything aligned, D a multiple
-// of 8; 4: an even D, or 32-bit values), else value by value (2).
-//
-// A warp stages its own 8 timesteps of a tile, [kSteps][64] for each tensor,
-// and reads nothing else, so its copies need no barrier of the block.
-// Timesteps past `len` and channels past D come out as zeros, nothing of
-// theirs is read.
-template <typename T, int kCopy>
-struct Stage {
-  static constexpr int kPer = kCopy >= 4 ? kCopy / (int)sizeof(T) : 1;  // values of a copy
-  static constexpr int kRow = kLanes / kPer;                            // copies of a row
-  static constexpr int kRows = kRow >= 32 ? 1 : 32 / kRow;              // rows of one turn of the warp
-  static constexpr int kTurns = kRow >= 32 ? kRow / 32 : 1;             // turns of one row
-  static __device__ __forceinline__ int row0() { return kRow >= 32 ? 0 : (threadIdx.x & 31) / kRow; }
-  static __device__ __forceinline__ int col0() { return (threadIdx.x & 31) % kRow * kPer; }
+constexpr unsigned long long kWaitNs = 2000000000;  // the longest wait inside a kernel
+constexpr int kStages = 2;                          // a task's tile is used while the next one's arrives
 
-  // Byte offset of this lane's first copy from a tile's first value.
-  static __device__ __forceinline__ long long lane_offset(long long stride) {
-    return ((long long)((threadIdx.x >> 5) * kSteps + row0()) * stride + col0()) * (int)sizeof(T);
-  }
-  static __device__ __forceinline__ void copy(T* to, const char* from, bool in) {
-    if constexpr (kCopy == 16)
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(in ? 16 : 0)
-                   : "memory");
-    else if constexpr (kCopy == 4)
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(in ? 4 : 0)
-                   : "memory");
-    else
-      *to = in ? *reinterpret_cast<const T*>(from) : from_f32<T>(0.0f);
-  }
-  // dst: the warp's [kSteps][64]; tile: the tile's first value; rows, cols: how many of the warp's timesteps and the
-  // tile's channels exist.
-  static __device__ __forceinline__ void run(T* dst, const void* tile, long long offset, long long stride, int rows, int cols) {
-    const char* from = static_cast<const char*>(tile) + offset;
-    T* to = dst + row0() * kLanes + col0();
-    const long long step = kRows * stride * (int)sizeof(T);
-    if (rows >= kSteps && cols >= kLanes) {
-#pragma unroll
-      for (int s = 0; s < kSteps; s += kRows, from += step) {
-#pragma unroll
-        for (int q = 0; q < kTurns; ++q)
-          copy(to + s * kLanes + 32 * q * kPer, from + 32 * q * kPer * (int)sizeof(T), true);
-      }
-    } else {
-#pragma unroll 1
-      for (int s = 0; s < kSteps; s += kRows, from += step) {
-#pragma unroll
-        for (int q = 0; q < kTurns; ++q) {
-          const bool in = s + row0() < rows && col0() + 32 * q * kPer < cols;
-          copy(to + s * kLanes + 32 * q * kPer,
-               in ? from + 32 * q * kPer * (int)sizeof(T) : static_cast<const char*>(tile), in);
-        }
-      }
+// How a tile comes into shared memory, by the layout of all tensors (kCopy):
+//   16  tensor-map copies (TMA), one of a warp's timesteps by 64 channels for
+//       each tensor, counted by an mbarrier of the warp: rows at 16-byte steps
+//       whose strides nest (see map_of).  One lane issues them; by 16-byte copies
+//       of each lane staging took 6 of 50 instructions to a value.
+//   4   asynchronous copies of 4 bytes (an even D, or 32-bit values)
+//   2   value by value
+// A warp brings in its own timesteps of a tile, [kSteps][64] of each of the
+// first N tensors, and reads nothing else, so this needs no barrier of the
+// block.  What is staged for timesteps past the stream's end and channels past
+// D is used for nothing.
+template <typename T, int kCopy, int kSteps, int N>
+struct Loader {
+  static constexpr int kOne = kWarps * kSteps * kLanes;           // values of one staged tensor
+  static constexpr size_t kBytes = (size_t)N * kOne * sizeof(T);  // of a stage
+
+  unsigned char* staged;
+  uint64_t* bars;  // [kStages][kWarps]
+
+  // Called by all threads, before a barrier of the block.
+  __device__ __forceinline__ Loader(unsigned char* memory, uint64_t* barriers) : staged(memory), bars(barriers) {
+    if constexpr (kCopy == 16) {
+      if (threadIdx.x < kStages * kWarps) mbar_init(smem_u32(bars + threadIdx.x), 1);
+      if (threadIdx.x < 32) fence_mbarrier_init_cluster();
     }
   }
+  __device__ __forceinline__ T* part(int stage) const {  // this warp's timesteps of the first tensor
+    return reinterpret_cast<T*>(staged + stage * kBytes) + (threadIdx.x >> 5) * kSteps * kLanes;
+  }
+  // The warp's timesteps from ts on, `rows` of them the stream's (any number), channels ch0 .. of stream b.
+  template <typename Io>
+  __device__ __forceinline__ void fetch(int stage, char* const* tensors, const Io& io, int ts, int b, int ch0, int rows,
+                                        int cols) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    T* to = part(stage);
+    if constexpr (kCopy == 16) {
+      if (elect_one()) {
+        const uint32_t bar = smem_u32(bars + stage * kWarps + warp);
+        if (rows > 0) {
+          mbar_arrive_expect_tx(bar, N * kSteps * kLanes * (int)sizeof(T));
+#pragma unroll
+          for (int m = 0; m < N; ++m) {
+            const bool nested = io.stream_inner[m] != 0;
+            tma_load_3d(smem_u32(to + m * kOne), io.maps + m, bar, ch0, nested ? b : ts, nested ? ts : b);
+          }
+        } else {
+          mbar_arrive(bar);
+        }
+      }
+      __syncwarp();
+    } else {
+      constexpr int kPer = kCopy == 4 ? 4 / (int)sizeof(T) : 1;  // values of a copy
+      constexpr int kAcross = kLanes / kPer / 32;                // copies of a lane in a row
+      if (rows > 0) {
+#pragma unroll
+        for (int m = 0; m < N; ++m) {
+          const long long step = io.strides[m].t * (long long)sizeof(T);
+          const char* from = tensors[m] + warp * kSteps * step;
+          for (int s = 0; s < min(rows, kSteps); ++s, from += step) {
+#pragma unroll
+            for (int q = 0; q < kAcross; ++q) {
+              const int col = (lane + 32 * q) * kPer;
+              T* at = to + m * kOne + s * kLanes + col;
+              const T* src = reinterpret_cast<const T*>(from) + col;
+              if (col < cols) {
+                if constexpr (kCopy == 4)
+                  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(at)), "l"(src) : "memory");
+                else
+                  *at = *src;
+              }
+            }
+          }
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+  }
+  // Nothing more to fetch.
+  __device__ __forceinline__ void skip() {
+    if constexpr (kCopy != 16) asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  // Waits for the older of the two stages in flight; false if it does not come (then its values are not used).
+  __device__ __forceinline__ bool wait(int stage, unsigned parity) {
+    bool ok = true;
+    if constexpr (kCopy == 16) {
+      const int never = 0;
+      ok = mbar_wait_bounded<false>(smem_u32(bars + stage * kWarps + (threadIdx.x >> 5)), parity, kWaitNs, &never);
+    } else {
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
+    }
+    __syncwarp();
+    return ok;
+  }
 };
-__device__ __forceinline__ void stage_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void stage_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-  __syncwarp();
-}
 
 __device__ __forceinline__ int length_of(const int* lengths, int b, int T) {
   return lengths ? min(max(lengths[b], 0), T) : T;
 }
 
 // Bit s: reset at timestep ts + s of this warp (the same in all lanes).
+template <int kSteps>
 __device__ __forceinline__ unsigned reset_bits(const unsigned char* reset, int ts, int len, int b, int B) {
   const int lane = threadIdx.x & 31, t = ts + lane;
   const bool on = lane < kSteps && t < len && reset[(long long)t * B + b] != 0;
@@ -263,8 +302,8 @@ __device__ __forceinline__ unsigned reset_bits(const unsigned char* reset, int t
 // ---- tasks and the exchange between tiles -----------------------------------
 
 constexpr int kMaxGroup = 16;                       // tiles of a group
+constexpr float kNaN = __builtin_nanf("");
 constexpr unsigned kNotYet = 0xffffffffu;           // a word of the exchange before it is written
-constexpr unsigned long long kWaitNs = 2000000000;  // longest wait for one
 
 // One tile of 64 channels of one stream; `order` counts tiles in the direction of the scan.
 struct Task {
@@ -272,14 +311,16 @@ struct Task {
 };
 struct Tasks {
   int T, B, D;
+  int tile;          // timesteps of a tile
   int slabs, tiles;  // of a stream's channels, of the sequence (one at least)
   int group_log2;    // of the tiles of a group: a function of the shape
   long long count;   // slabs * B * tiles
 };
 // Shapes with few streams and channels have many tiles of one sequence in flight at once (about three blocks to an
 // SM share them); where there are more sequences than blocks a tile's predecessor is done long before.
-inline Tasks tasks_of(int T, int B, int D) {
-  Tasks t{T, B, D, (D + kLanes - 1) / kLanes, std::max(1, (T + kTile - 1) / kTile), 0, 0};
+inline Tasks tasks_of(int T, int B, int D, int steps) {
+  const int tile = kWarps * steps;
+  Tasks t{T, B, D, tile, (D + kLanes - 1) / kLanes, std::max(1, (T + tile - 1) / tile), 0, 0};
   const long long items = (long long)t.slabs * B;
   t.count = items * t.tiles;
   t.group_log2 = 0;
@@ -318,15 +359,17 @@ struct Plan {
   int len;              // of the stream
   char* tensors[7];     // the tile's first value in each tensor
 };
-// Tensors of a call as the kernels take them.
-template <int N>
+// Tensors of a call as the kernels take them: N, the first M of which are read through tensor maps where they can be.
+template <int N, int M>
 struct Tensors {
+  TcMap maps[M];
+  int stream_inner[M];  // the map's middle axis is the stream, else the timestep
   char* base[N];
   Strides strides[N];
 };
 // Called by one warp (all its lanes).
-template <typename T, int N>
-__device__ __forceinline__ void make_plan(Plan& plan, const Tasks& t, const Tensors<N>& tensors, const int* lengths,
+template <typename T, int N, int M>
+__device__ __forceinline__ void make_plan(Plan& plan, const Tasks& t, const Tensors<N, M>& tensors, const int* lengths,
                                           const Task& at, bool back) {
   const int lane = threadIdx.x & 31;
   if (at.order >= t.tiles) {
@@ -337,7 +380,7 @@ __device__ __forceinline__ void make_plan(Plan& plan, const Tasks& t, const Tens
   if (lane < N) {
     const Strides& st = tensors.strides[lane];
     plan.tensors[lane] =
-        tensors.base[lane] + (at.b * st.b + (long long)tile * kTile * st.t + at.slab * kLanes) * (long long)sizeof(T);
+        tensors.base[lane] + (at.b * st.b + (long long)tile * t.tile * st.t + at.slab * kLanes) * (long long)sizeof(T);
   } else if (lane == N) {
     plan.at = at;
     plan.len = length_of(lengths, at.b, t.T);
@@ -465,7 +508,7 @@ __device__ __forceinline__ uint64_t state_before(const Tasks& t, const Task& at,
 }
 
 struct ScanArgs {
-  Tensors<4> io;  // x, r, i, y
+  Tensors<4, 3> io;  // x, r, i, y
   const float* h0;
   const int* lengths;
   const unsigned char* reset;
@@ -474,12 +517,6 @@ struct ScanArgs {
   float* h_last;
   float* states;
 };
-
-// A task's tile is used while the next one's arrives: 16-bit values leave room
-// for three blocks to an SM forward and two backward, 32-bit ones two and one.
-constexpr int kStages = 2;
-template <typename T, int kTensors>
-constexpr size_t kStageBytes = (size_t)kTensors * kTile * kLanes * sizeof(T);
 
 __device__ __forceinline__ uint64_t load_f32x2(const float* p, int left) {
   return f32x2(left > 0 ? p[0] : 0.0f, left > 1 ? p[1] : 0.0f);
@@ -499,14 +536,15 @@ __device__ __forceinline__ void store_both(T* p, int left, uint64_t v) {
 }
 
 // a_t and m_t sigma(i_t) x_t of a warp's staged timesteps.
-template <typename T, bool kFar>
+template <typename T, bool kFar, int kSteps>
 __device__ __forceinline__ void form_runs(const T* here, uint64_t rate, const Constants& k, uint64_t (&A)[kSteps],
                                           uint64_t (&U)[kSteps]) {
+  constexpr int kOne = kWarps * kSteps * kLanes;  // values of one staged tensor
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
     const T* p = here + s * kLanes;
     const Gates g =
-        gates_of<kFar>(staged_pair<T>(p + kTile * kLanes), staged_pair<T>(p + 2 * kTile * kLanes), rate, k);
+        gates_of<kFar>(staged_pair<T>(p + kOne), staged_pair<T>(p + 2 * kOne), rate, k);
     A[s] = decay_of(g.low, k);
     const uint64_t m2 = m2_of(g.low, A[s], k);
     U[s] = mul2(mul2(mul2(m2, rsqrt2(m2)), g.si), staged_pair<T>(p));
@@ -514,7 +552,7 @@ __device__ __forceinline__ void form_runs(const T* here, uint64_t rate, const Co
 }
 
 // The run of a warp's timesteps (kCuts: with resets at the set bits, one at least).
-template <bool kCuts>
+template <bool kCuts, int kSteps>
 __device__ __forceinline__ ulonglong2 join_steps(const uint64_t (&A)[kSteps], const uint64_t (&U)[kSteps],
                                                  unsigned resets) {
   uint64_t PA = A[0], PU = U[0];
@@ -539,27 +577,19 @@ __device__ __forceinline__ bool any_far(uint64_t rate) {
 }
 
 template <typename T, int kCopy, bool kCuts>
-__global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 2 : 3) gated_scan_kernel(const ScanArgs a) {
-  extern __shared__ __align__(16) unsigned char staged[];
+__global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const __grid_constant__ ScanArgs a) {
+  extern __shared__ __align__(128) unsigned char staged[];
   __shared__ Join sm;
   __shared__ Plan plans[3];  // of this task and the next two
+  __shared__ __align__(8) uint64_t bars[kStages * kWarps];
   constexpr bool kVec = kCopy >= 2 * (int)sizeof(T);  // a lane's two channels of y in one store
-  constexpr int kOne = kTile * kLanes;                // values of one staged tensor
+  constexpr int kSteps = kForwardSteps<T>;
   const Tasks& t = a.tasks;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  using St = Stage<T, kCopy>;
-  long long offset[3];
-#pragma unroll
-  for (int n = 0; n < 3; ++n) offset[n] = St::lane_offset(a.io.strides[n].t);
-  // this warp's part of a task's tile into stage n
-  auto buffer = [&](int n) { return reinterpret_cast<T*>(staged + n * kStageBytes<T, 3>) + warp * kSteps * kLanes; };
+  Loader<T, kCopy, kSteps, 3> loader(staged, bars);
   auto fetch = [&](int n, const Plan& plan) {
-    const int rows = plan.len - plan.at.order * kTile - warp * kSteps, cols = t.D - plan.at.slab * kLanes;
-    if (rows > 0) {
-      T* to = buffer(n);
-#pragma unroll
-      for (int m = 0; m < 3; ++m) St::run(to + m * kOne, plan.tensors[m], offset[m], a.io.strides[m].t, rows, cols);
-    }
+    const int ts = plan.at.order * t.tile + warp * kSteps, ch0 = plan.at.slab * kLanes;
+    loader.fetch(n, plan.tensors, a.io, ts, plan.at.b, ch0, plan.len - ts, t.D - ch0);
   };
   const Task step = task_at(t, gridDim.x);
   Task ahead = advance(t, task_at(t, blockIdx.x), step);  // the furthest task with a plan
@@ -569,23 +599,24 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 2 : 3) gated_sca
   }
   __syncthreads();
   fetch(0, plans[0]);
-  stage_commit();
   const Constants k = constants();
   int turn = 0, now = 0;
+  unsigned parity = 0;  // of the stage in use
   for (; plans[now].at.order < t.tiles; turn ^= 1) {
     const Plan &plan = plans[now], &next = plans[now == 2 ? 0 : now + 1];
     const Task at = plan.at;
     const uint64_t rate = *reinterpret_cast<const uint64_t*>(a.exchange.rate + at.slab * kLanes + 2 * lane);
     __syncwarp();  // the lanes are done with the stage that the next tile goes to
     if (next.at.order < t.tiles) fetch(turn ^ 1, next);
-    stage_commit();
+    else loader.skip();
     const int ch = at.slab * kLanes + 2 * lane, left = t.D - ch;  // channels of this lane that exist: min(left, 2)
-    const int ts = at.order * kTile + warp * kSteps, len = plan.len;
+    const int ts = at.order * t.tile + warp * kSteps, len = plan.len;
     const long long state_at = (long long)at.b * t.D + ch;
-    const unsigned resets = kCuts ? reset_bits(a.reset, ts, len, at.b, t.B) : 0u;
+    const unsigned resets = kCuts ? reset_bits<kSteps>(a.reset, ts, len, at.b, t.B) : 0u;
     const bool whole = ts + kSteps <= len;
-    const T* here = buffer(turn) + 2 * lane;
-    stage_wait<1>();
+    const T* here = loader.part(turn) + 2 * lane;
+    const bool there = loader.wait(turn, parity);
+    parity ^= turn;
     uint64_t A[kSteps], U[kSteps];
     if (ts < len) {
       if (any_far(rate)) form_runs<T, true>(here, rate, k, A, U);
@@ -596,6 +627,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 2 : 3) gated_sca
       for (int s = 0; s < kSteps; ++s)
         if (ts + s >= len) A[s] = k.one, U[s] = 0ull;
     }
+    if (!there) U[0] = both(kNaN);
     sm.runs[turn][warp][lane] = kCuts && resets ? join_steps<true>(A, U, resets) : join_steps<false>(A, U, 0u);
     __syncthreads();
     uint64_t first = 0ull;
@@ -612,10 +644,14 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 2 : 3) gated_sca
       if (at.order == t.tiles - 1) store_f32x2(a.h_last + state_at, left, end);
       else if (ends_group(t, at))
         publish(a.exchange.states + ((long long)(at.order >> t.group_log2) * t.slabs * t.B + at.b * t.slabs + at.slab) * 32 + lane, end);
-      if (a.states && at.order * kTile < t.T)
-        store_f32x2(a.states + (long long)at.order * t.B * t.D + state_at, left, h);
     }
-    for (int w = 0; w < warp; ++w) h = after<kCuts>(sm.runs[turn][w][lane], h);
+#pragma unroll
+    for (int w = 0; w < kWarps - 1; ++w) {
+      const uint64_t to = after<kCuts>(sm.runs[turn][w][lane], h);
+      if (w < warp) h = to;
+    }
+    if (a.states && ts % kChunk == 0 && ts < t.T)
+      store_f32x2(a.states + (long long)(ts / kChunk) * t.B * t.D + state_at, left, h);
     if (kCuts && resets) {
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
@@ -643,7 +679,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 2 : 3) gated_sca
 }
 
 struct ScanBackwardArgs {
-  Tensors<7> io;  // x, r, i, dy, dx, dr, di
+  Tensors<7, 4> io;  // x, r, i, dy, dx, dr, di
   const float* dh_last;
   const float* states;
   const int* lengths;
@@ -655,14 +691,15 @@ struct ScanBackwardArgs {
 };
 
 // 1 - a_t, the gates and m_t sigma(i_t) x_t of a warp's staged timesteps.
-template <typename T, bool kFar>
+template <typename T, bool kFar, int kSteps>
 __device__ __forceinline__ void form_gates(const T* here, uint64_t rate, const Constants& k, uint64_t (&low)[kSteps],
                                            uint64_t (&sr)[kSteps], uint64_t (&si)[kSteps], uint64_t (&U)[kSteps]) {
+  constexpr int kOne = kWarps * kSteps * kLanes;
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
     const T* p = here + s * kLanes;
     const Gates g =
-        gates_of<kFar>(staged_pair<T>(p + kTile * kLanes), staged_pair<T>(p + 2 * kTile * kLanes), rate, k);
+        gates_of<kFar>(staged_pair<T>(p + kOne), staged_pair<T>(p + 2 * kOne), rate, k);
     low[s] = g.low;
     sr[s] = g.sr;
     si[s] = g.si;
@@ -672,8 +709,8 @@ __device__ __forceinline__ void form_gates(const T* here, uint64_t rate, const C
 }
 
 // The runs of a warp's timesteps, h -> A h + U forward and p -> A p + V back
-// (staged dy is zero past the stream's length; kCuts: one reset at least).
-template <typename T, bool kCuts>
+// (staged dy is zero past the stream's length; kCuts: with a reset, one at least).
+template <typename T, bool kCuts, int kSteps>
 __device__ __forceinline__ void join_both(const T* here, const uint64_t (&low)[kSteps], const uint64_t (&U)[kSteps],
                                           unsigned resets, const Constants& k, uint64_t& PA, uint64_t& PU, uint64_t& PV) {
 #pragma unroll
@@ -685,7 +722,7 @@ __device__ __forceinline__ void join_both(const T* here, const uint64_t (&low)[k
   }
 #pragma unroll
   for (int s = kSteps - 1; s >= 0; --s) {
-    PV = mul2(decay_of(low[s], k), add2(PV, staged_pair<T>(here + 3 * kTile * kLanes + s * kLanes)));
+    PV = mul2(decay_of(low[s], k), add2(PV, staged_pair<T>(here + 3 * kWarps * kSteps * kLanes + s * kLanes)));
     if (kCuts && (resets >> s & 1u)) PV = 0ull;
   }
   if (kCuts) PA = both(-1.0f);
@@ -700,7 +737,7 @@ template <typename T>
 __device__ __forceinline__ Gradients gradients_of(const T* here, uint64_t low, uint64_t sr, uint64_t si, uint64_t h,
                                                   uint64_t rate, const Constants& k, uint64_t& p) {
   const uint64_t A = decay_of(low, k), xs = staged_pair<T>(here);
-  const uint64_t g = add2(p, staged_pair<T>(here + 3 * kTile * kLanes));
+  const uint64_t g = add2(p, staged_pair<T>(here + 3 * kWarps * kBackwardSteps * kLanes));
   p = mul2(g, A);
   const uint64_t m2 = m2_of(low, A, k), inv_m = rsqrt2(m2);
   const uint64_t t = mul2(rate, sr);  // -log a
@@ -713,29 +750,22 @@ __device__ __forceinline__ Gradients gradients_of(const T* here, uint64_t low, u
 }
 
 template <typename T, int kCopy, bool kCuts>
-__global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_scan_backward_kernel(const ScanBackwardArgs a) {
-  extern __shared__ __align__(16) unsigned char staged[];
+__global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_scan_backward_kernel(const __grid_constant__ ScanBackwardArgs a) {
+  extern __shared__ __align__(128) unsigned char staged[];
   __shared__ Join sm;                             // p -> A p + V
   __shared__ ulonglong2 ahead[2][kWarps][32];     // h -> A h + U
   __shared__ uint64_t sums[kWarps][32];           // E over each warp's timesteps of the last task
   __shared__ Plan plans[3];
+  __shared__ __align__(8) uint64_t bars[kStages * kWarps];
   constexpr bool kVec = kCopy >= 2 * (int)sizeof(T);
-  constexpr int kOne = kTile * kLanes;
+  constexpr int kSteps = kBackwardSteps;
+  constexpr int kOne = kWarps * kSteps * kLanes;
   const Tasks& t = a.tasks;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  using St = Stage<T, kCopy>;
-  long long offset[4];
-#pragma unroll
-  for (int n = 0; n < 4; ++n) offset[n] = St::lane_offset(a.io.strides[n].t);
-  auto buffer = [&](int n) { return reinterpret_cast<T*>(staged + n * kStageBytes<T, 4>) + warp * kSteps * kLanes; };
+  Loader<T, kCopy, kSteps, 4> loader(staged, bars);
   auto fetch = [&](int n, const Plan& plan) {
-    const int rows = plan.len - (t.tiles - 1 - plan.at.order) * kTile - warp * kSteps;
-    const int cols = t.D - plan.at.slab * kLanes;
-    if (rows > 0) {
-      T* to = buffer(n);
-#pragma unroll
-      for (int m = 0; m < 4; ++m) St::run(to + m * kOne, plan.tensors[m], offset[m], a.io.strides[m].t, rows, cols);
-    }
+    const int ts = (t.tiles - 1 - plan.at.order) * t.tile + warp * kSteps, ch0 = plan.at.slab * kLanes;
+    loader.fetch(n, plan.tensors, a.io, ts, plan.at.b, ch0, plan.len - ts, t.D - ch0);
   };
   auto add_up = [&](const Task& at) {  // the sums of a finished task into its partial
     uint64_t v = sums[0][lane];
@@ -752,9 +782,9 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
   }
   __syncthreads();
   fetch(0, plans[0]);
-  stage_commit();
   const Constants k = constants();
   int turn = 0, now = 0;
+  unsigned parity = 0;
   bool any = false;
   for (; plans[now].at.order < t.tiles; turn ^= 1) {
     const Plan &plan = plans[now], &next = plans[now == 2 ? 0 : now + 1];
@@ -762,25 +792,32 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
     const uint64_t rate = *reinterpret_cast<const uint64_t*>(a.exchange.rate + at.slab * kLanes + 2 * lane);
     __syncwarp();
     if (next.at.order < t.tiles) fetch(turn ^ 1, next);
-    stage_commit();
+    else loader.skip();
     const int tile = t.tiles - 1 - at.order;
     const int ch = at.slab * kLanes + 2 * lane, left = t.D - ch;
-    const int ts = tile * kTile + warp * kSteps, len = plan.len;
+    const int ts = tile * t.tile + warp * kSteps, len = plan.len;
     const long long state_at = (long long)at.b * t.D + ch;
-    const unsigned resets = kCuts ? reset_bits(a.reset, ts, len, at.b, t.B) : 0u;
+    const unsigned resets = kCuts ? reset_bits<kSteps>(a.reset, ts, len, at.b, t.B) : 0u;
     const bool whole = ts + kSteps <= len, some = ts < len;
-    const T* here = buffer(turn) + 2 * lane;
+    T* here = loader.part(turn) + 2 * lane;
     uint64_t h = some ? load_f32x2(a.states + (long long)tile * t.B * t.D + state_at, left) : 0ull;
-    stage_wait<1>();
+    const bool there = loader.wait(turn, parity);
+    parity ^= turn;
     uint64_t low[kSteps], sr[kSteps], si[kSteps], U[kSteps], PA = k.one, PU = 0ull, PV = 0ull;
     if (some) {
       if (any_far(rate)) form_gates<T, true>(here, rate, k, low, sr, si, U);
       else form_gates<T, false>(here, rate, k, low, sr, si, U);
       if (!whole) {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s)
-          if (ts + s >= len) low[s] = U[s] = 0ull;
+        for (int s = 0; s < kSteps; ++s) {
+          if (ts + s >= len) {
+            low[s] = U[s] = 0ull;
+            here[3 * kOne + s * kLanes] = here[3 * kOne + s * kLanes + 1] = from_f32<T>(0.0f);  // dy
+          }
+        }
+        if (kCopy == 16) fence_proxy_async_shared();  // before a later bulk copy to the same place
       }
+      if (!there) low[0] = both(kNaN);
       if (kCuts && resets) join_both<T, true>(here, low, U, resets, k, PA, PU, PV);
       else join_both<T, false>(here, low, U, 0u, k, PA, PU, PV);
     }
@@ -795,7 +832,11 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
       ahead_task = advance(t, ahead_task, step);
       make_plan<T>(plans[now == 0 ? 2 : now - 1], t, a.io, a.lengths, ahead_task, true);
     }
-    for (int w = 0; w < warp; ++w) h = after<kCuts>(ahead[turn][w][lane], h);
+#pragma unroll
+    for (int w = 0; w < kWarps - 1; ++w) {
+      const uint64_t to = after<kCuts>(ahead[turn][w][lane], h);
+      if (w < warp) h = to;
+    }
     __syncthreads();
     uint64_t p = state_before<kCuts>(t, at, sm);
     if (warp == 0) {
@@ -804,7 +845,11 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
       else if (ends_group(t, at))
         publish(a.exchange.states + ((long long)(at.order >> t.group_log2) * t.slabs * t.B + at.b * t.slabs + at.slab) * 32 + lane, end);
     }
-    for (int w = kWarps - 1; w > warp; --w) p = after<kCuts>(sm.runs[turn][w][lane], p);
+#pragma unroll
+    for (int w = kWarps - 1; w > 0; --w) {
+      const uint64_t to = after<kCuts>(sm.runs[turn][w][lane], p);
+      if (w > warp) p = to;
+    }
     // the gradients' places at the warp's last timestep, from where the loops below go back
     const long long sx = a.io.strides[4].t, sr_t = a.io.strides[5].t, si_t = a.io.strides[6].t;
     const int last = warp * kSteps + kSteps - 1;
@@ -957,17 +1002,17 @@ int copy_bytes(int D, size_t es, const void* const* p, const Strides* s, int n) 
 int check_sizes(int dtype, int T, int B, int D, float c, char* msg, int msg_len) {
   if (!op_float_dtype(dtype)) return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "dtype %d", dtype);
   if (T < 0 || B < 0 || D < 1 || D > 0x7fffff00 || T > 0x7fffff00 ||
-      (double)B * ((D + kLanes - 1) / kLanes) * (T / kTile + 1) > 2147483647.0)
+      (double)B * ((D + kLanes - 1) / kLanes) * (T / kChunk + 1) > 2147483647.0)
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "need T, B >= 0, D >= 1 and fewer than 2^31 tiles of 64 x 64 values");
   if (!(c > 0.0f)) return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "c must be positive");
   return LSTM_APPROX_OK;
 }
 
-template <typename T, int kCopy, bool kCuts, int kTensors, typename A>
-cudaError_t launch_scan(void (*kern)(A), cudaStream_t s, const A& args) {
+template <typename T, int kCopy, bool kCuts, int kTensors, int kSteps, typename A>
+cudaError_t launch_scan(void (*kern)(const A), cudaStream_t s, const A& args) {
   static thread_local DeviceSet ready;  // of the one kernel that this instance launches
   static thread_local int resident[64];
-  constexpr size_t smem = kStages * kStageBytes<T, kTensors>;
+  constexpr size_t smem = kStages * Loader<T, kCopy, kSteps, kTensors>::kBytes;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess && dev >= 64) e = cudaErrorInvalidDevice;
@@ -1006,12 +1051,32 @@ size_t workspace_bytes_of(const Tasks& t) {
   return (exchange_bytes(t) + (size_t)t.tiles * t.B * t.slabs * kLanes * sizeof(float) + 15) / 16 * 16 + 16;
 }
 
-template <int N>
-void set_tensors(Tensors<N>& io, const void* const (&p)[N], const Strides* st) {
+// The tensor map of one tensor [T][B][D], its copies 64 channels by `steps` timesteps of one stream.  The axes go by
+// size of their strides, which have to be multiples of one another with no overlap (a size of 1 has any stride).
+bool map_of(TcMap* map, int* stream_inner, const void* p, int dtype, int T, int B, int D, const Strides& st, int steps) {
+  const long long es = (long long)op_dtype_bytes(dtype), row = (long long)D * es;
+  long long b = st.b * es, t = st.t * es;
+  *stream_inner = T == 1 || (B > 1 && b <= t);
+  if (B == 1) b = T == 1 ? row : t * T;
+  if (T == 1) t = b * B;
+  const long long in = *stream_inner ? b : t, out = *stream_inner ? t : b;
+  if (in < row || out % in != 0 || out < in * (*stream_inner ? B : T) || out >= 1ll << 40) return false;
+  return tc_make_map_steps(map, p, es == 4, D, *stream_inner ? B : T, *stream_inner ? T : B, in, out,
+                           *stream_inner ? 1 : steps, *stream_inner ? steps : 1);
+}
+
+// The tensors, and the kernels' kCopy for them.
+template <int N, int M>
+int set_tensors(Tensors<N, M>& io, const void* const (&p)[N], const Strides* st, int dtype, int T, int B, int D, int steps) {
+  const size_t es = op_dtype_bytes(dtype);
+  int copy = T > 0 ? copy_bytes(D, es, p, st, N) : 4;
   for (int n = 0; n < N; ++n) {
     io.base[n] = static_cast<char*>(const_cast<void*>(p[n]));
     io.strides[n] = st[n];
   }
+  for (int m = 0; m < M && copy == 16; ++m)
+    if (!map_of(&io.maps[m], &io.stream_inner[m], p[m], dtype, T, B, D, st[m], steps)) copy = 4;
+  return copy;
 }
 
 // Strides of n tensors: HOST [2n], or all contiguous [T][B][D].
@@ -1030,7 +1095,7 @@ using namespace lstm_approx_impl;
 
 extern "C" size_t lstm_approx_gated_scan_workspace_bytes(int T, int B, int D) {
   if (check_sizes(LSTM_APPROX_OP_FP32, T, B, D, 1.0f, nullptr, 0)) return 0;
-  return workspace_bytes_of(tasks_of(T, B, D));
+  return workspace_bytes_of(tasks_of(T, B, D, kBackwardSteps));  // (forward: as many tiles or half, no partial sums)
 }
 
 extern "C" int lstm_approx_gated_scan(int dtype, const void* x, const void* r, const void* i, const float* decay,
@@ -1049,8 +1114,8 @@ extern "C" int lstm_approx_gated_scan(int dtype, const void* x, const void* r, c
   Strides st[4];
   if (!read_strides(strides, 4, B, D, st))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "strides must not be negative");
-  const Tasks tasks = tasks_of(T, B, D);
-  const size_t need = workspace_bytes_of(tasks);
+  const Tasks tasks = tasks_of(T, B, D, dtype == LSTM_APPROX_OP_FP32 ? kForwardSteps<float> : kForwardSteps<__half>);
+  const size_t need = lstm_approx_gated_scan_workspace_bytes(T, B, D);
   if (B > 0 && (!op_aligned(workspace, 16) || workspace_bytes < need))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "needs a 16-byte aligned workspace of %zu bytes", need);
   if (int rc = op_check_device(msg, msg_len)) return rc;
@@ -1061,14 +1126,13 @@ extern "C" int lstm_approx_gated_scan(int dtype, const void* x, const void* r, c
   if (int rc = op_launched(e, "scan preparation launch", msg, msg_len)) return rc;
   const void* tensors[4] = {x, r, i, y};
   ScanArgs a{{}, h0, lengths, reset, tasks, exchange, h_last, states};
-  set_tensors(a.io, tensors, st);
-  const int copy = copy_bytes(D, es, tensors, st, 4);
+  const int copy = set_tensors(a.io, tensors, st, dtype, T, B, D, tasks.tile / kWarps);
   e = op_for_type(dtype, [&](auto* t) {
     using E = std::remove_pointer_t<decltype(t)>;
     auto go = [&](auto bytes) {
       constexpr int kCopy = decltype(bytes)::value;
-      return reset ? launch_scan<E, kCopy, true, 3>(gated_scan_kernel<E, kCopy, true>, s, a)
-                   : launch_scan<E, kCopy, false, 3>(gated_scan_kernel<E, kCopy, false>, s, a);
+      return reset ? launch_scan<E, kCopy, true, 3, kForwardSteps<E>>(gated_scan_kernel<E, kCopy, true>, s, a)
+                   : launch_scan<E, kCopy, false, 3, kForwardSteps<E>>(gated_scan_kernel<E, kCopy, false>, s, a);
     };
     if (copy == 16) return go(std::integral_constant<int, 16>());
     if (copy == 4) return go(std::integral_constant<int, 4>());
@@ -1098,8 +1162,8 @@ extern "C" int lstm_approx_gated_scan_backward(int dtype, const void* dy, const 
   Strides st[7];
   if (!read_strides(strides, 7, B, D, st))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "strides must not be negative");
-  const Tasks tasks = tasks_of(T, B, D);
-  const size_t need = workspace_bytes_of(tasks);
+  const Tasks tasks = tasks_of(T, B, D, kBackwardSteps);
+  const size_t need = lstm_approx_gated_scan_workspace_bytes(T, B, D);
   if (!op_aligned(workspace, 16) || workspace_bytes < need)
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "needs a 16-byte aligned workspace of %zu bytes", need);
   if (int rc = op_check_device(msg, msg_len)) return rc;
@@ -1112,14 +1176,13 @@ extern "C" int lstm_approx_gated_scan_backward(int dtype, const void* dy, const 
     const void* tensors[7] = {x, r, i, dy, dx, dr, di};
     const Strides order[7] = {st[1], st[2], st[3], st[0], st[4], st[5], st[6]};
     ScanBackwardArgs a{{}, dh_last, states, lengths, reset, tasks, exchange, dh0, partial};
-    set_tensors(a.io, tensors, order);
-    const int copy = copy_bytes(D, es, tensors, order, 7);
+    const int copy = set_tensors(a.io, tensors, order, dtype, T, B, D, tasks.tile / kWarps);
     e = op_for_type(dtype, [&](auto* t) {
       using E = std::remove_pointer_t<decltype(t)>;
       auto go = [&](auto bytes) {
         constexpr int kCopy = decltype(bytes)::value;
-        return reset ? launch_scan<E, kCopy, true, 4>(gated_scan_backward_kernel<E, kCopy, true>, s, a)
-                     : launch_scan<E, kCopy, false, 4>(gated_scan_backward_kernel<E, kCopy, false>, s, a);
+        return reset ? launch_scan<E, kCopy, true, 4, kBackwardSteps>(gated_scan_backward_kernel<E, kCopy, true>, s, a)
+                     : launch_scan<E, kCopy, false, 4, kBackwardSteps>(gated_scan_backward_kernel<E, kCopy, false>, s, a);
       };
       if (copy == 16) return go(std::integral_constant<int, 16>());
       if (copy == 4) return go(std::integral_constant<int, 4>());

@@ -1117,6 +1117,23 @@ bool tc_make_map_planes(TcMap* m, const void* base, uint64_t inner, uint64_t row
   return r == CUDA_SUCCESS;
 }
 
+bool tc_make_map_steps(TcMap* m, const void* base, bool f32, uint64_t inner, uint64_t mid, uint64_t outer,
+                       uint64_t mid_bytes, uint64_t outer_bytes, uint32_t box_mid, uint32_t box_outer) {
+  EncodeTiled enc = encoder();
+  if (!enc) return false;
+  std::memset(m->bytes, 0, sizeof(m->bytes));
+  const cuuint64_t dims[3] = {inner, mid, outer};
+  const cuuint64_t strides[2] = {mid_bytes, outer_bytes};
+  const cuuint32_t box[3] = {64u, box_mid, box_outer};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = enc(reinterpret_cast<CUtensorMap*>(m->bytes),
+                         f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 3,
+                         const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
+
 cudaError_t launch_tc_rows(const TcMap& A, const TcMap& Bm, const TcRowsArgs& a, int n_cols, int bn, cudaStream_t s) {
   switch (bn) {
     case 128:
