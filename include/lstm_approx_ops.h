@@ -200,6 +200,7 @@ int lstm_approx_gated_step(int dtype, const void *x, long long x_pitch, const vo
  *   q      [N][q_pitch] bytes: column k in the low (k even) or high (k odd)
  *          half of byte k / 2; 16-byte aligned, q_pitch a multiple of 16 and at
  *          least ceil(K / 2).  What lies beyond column K is read, not used.
+ *          1 <= K <= 32768.
  *   scale  [N][ceil(K / group)] scale_dtype (FP32, BF16 or FP16)
  *   zero   [N][ceil(K / group)] bytes, each 0..15 (only the low 4 bits are
  *          read), or NULL (8 throughout)
@@ -217,7 +218,7 @@ int lstm_approx_w4_quantize(int dtype, const void *w, long long w_pitch, int N, 
 
 /*
  * y[m][n] = sum_k x[m][k] W[n][k] (+ bias[n]) for a few rows m (the streams
- * that are served together; any number is right, the kernel is built for up
+ * that are served together; up to 65535 are right, the kernel is built for up
  * to some tens).
  *
  *   x_dtype   FP32, BF16, FP16, or E4M3 with scales
