@@ -23,8 +23,12 @@
 //       8-bit values as fp16, and 32-bit values as three columns of bf16 (the
 //       upper 8 bits of the mantissa, the next, the last; their sum is exactly x).
 //   sum Each group's sum, in fp32 (8 exact products to an addition), times its
-//       scale, is added to the row's; the warps of a block share its rows' K and
-//       add up through shared memory, always in the same order.
+//       scale, is added to the row's.
+//
+// The tiles of 16 or 32 rows are dealt out evenly over one block of threads per
+// SM, and a block's warps take equal stretches of its tiles' blocks in a line,
+// whatever the numbers; a tile that several warps have parts of is added up
+// through shared memory at the end, always in the same order.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -38,7 +42,6 @@ namespace {
 using namespace lstm_approx_dev;
 
 constexpr int kBlockK = 128;  // k of a block
-constexpr int kDepth = 4;     // blocks in flight or in use to a warp
 constexpr int kMaxWarps = 16;
 
 __device__ __forceinline__ float e4m3_to_f32(uint8_t v) {
@@ -62,7 +65,8 @@ struct W4Args {
   int y_dtype;
   bool x_vec;  // 8 values of x lie in aligned accesses
   int tokens;  // rows of x at a time
-  int tiles;   // of kMt * 16 rows
+  int depth;   // blocks in flight or in use to a warp: 4 or 8
+  int tiles_each, tiles_more;  // tiles of kMt * 16 rows to a block of threads, and how many blocks have one more
 };
 
 __device__ __forceinline__ float load_any(const void* p, long long at, int dtype) {
@@ -77,17 +81,40 @@ __device__ __forceinline__ void store_any(void* p, long long at, int dtype, floa
   else static_cast<__half*>(p)[at] = __float2half_rn(v);
 }
 
-// The four pairs of a word's nibbles as 16-bit numbers less `bias` (a pair of 128 + zero or 1024 + zero).
+// Two of a word's four pairs of nibbles, at bits 0..3 and 4..7 of its halves, as 16-bit numbers less the zero point.
+// zero: pair of 128 + z (bf16); of 1024 + z, and of -(64 + z) (fp16, whose ten bits of mantissa hold the nibble at bits
+// 4..7 as it lies: (1024 + 16 q) / 16 - (64 + z) in one operation, where bf16 has to shift it down first).
 template <bool kBf16>
-__device__ __forceinline__ uint32_t nibbles(uint32_t w, int shift, uint32_t bias) {
-  uint32_t v;  // (w >> shift & 0x000f000f) | magic
-  asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xea;" : "=r"(v) : "r"(w >> shift), "r"(kBf16 ? 0x43004300u : 0x64006400u));
+struct Zero {
+  uint32_t low, high;
+};
+template <bool kBf16>
+__device__ __forceinline__ Zero<kBf16> zero_of(unsigned z) {
+  if constexpr (kBf16) return {0x43004300u + z * 0x00010001u, 0u};
+  const __half2 h = __float2half2_rn(-64.0f - (float)z);
+  return {0x64006400u + z * 0x00010001u, *reinterpret_cast<const uint32_t*>(&h)};
+}
+__device__ __forceinline__ uint32_t masked(uint32_t w, uint32_t mask, uint32_t magic) {
+  uint32_t v;  // (w & mask) | magic
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(v) : "r"(w), "r"(mask), "r"(magic));
+  return v;
+}
+template <bool kBf16>
+__device__ __forceinline__ void nibbles(uint32_t w, const Zero<kBf16>& z, uint32_t& first, uint32_t& second) {
   if constexpr (kBf16) {
-    const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), *reinterpret_cast<const __nv_bfloat162*>(&bias));
-    return *reinterpret_cast<const uint32_t*>(&d);
+    const uint32_t v0 = masked(w, 0x000f000fu, 0x43004300u), v1 = masked(w >> 4, 0x000f000fu, 0x43004300u);
+    const __nv_bfloat162 zz = *reinterpret_cast<const __nv_bfloat162*>(&z.low);
+    const __nv_bfloat162 d0 = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v0), zz);
+    const __nv_bfloat162 d1 = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v1), zz);
+    first = *reinterpret_cast<const uint32_t*>(&d0);
+    second = *reinterpret_cast<const uint32_t*>(&d1);
   } else {
-    const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&bias));
-    return *reinterpret_cast<const uint32_t*>(&d);
+    const uint32_t v0 = masked(w, 0x000f000fu, 0x64006400u), v1 = masked(w, 0x00f000f0u, 0x64006400u);
+    const __half2 d0 = __hsub2(*reinterpret_cast<const __half2*>(&v0), *reinterpret_cast<const __half2*>(&z.low));
+    const __half2 d1 = __hfma2(*reinterpret_cast<const __half2*>(&v1), __float2half2_rn(1.0f / 16.0f),
+                               *reinterpret_cast<const __half2*>(&z.high));
+    first = *reinterpret_cast<const uint32_t*>(&d0);
+    second = *reinterpret_cast<const uint32_t*>(&d1);
   }
 }
 
@@ -148,6 +175,9 @@ __device__ __forceinline__ uint4 in_order(const uint32_t (&v)[8]) {  // 16-bit v
 template <int kX>
 constexpr int kParts = kX == LSTM_APPROX_OP_FP32 ? 3 : 1;
 
+// Where the w-th of equal stretches (or one longer) begins, each `each` long and the first `more` of them one longer.
+__device__ __forceinline__ int stretch(int w, int each, int more) { return w * each + min(w, more); }
+
 // kX: type of x.  A tile is kMt * 16 rows of W; kNt * 8 columns of x^T.  kSubs = group / 32.
 template <int kX, int kMt, int kNt, int kSubs>
 __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args a) {
@@ -155,131 +185,195 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
   constexpr bool kScaled = kX == LSTM_APPROX_OP_E4M3;
   constexpr int kP = kParts<kX>;
   constexpr int kRed = kNt * 8 + 1;         // pitch of the sums
+  constexpr int kSum = kMt * 16 * kRed;     // a tile's sums
   constexpr int kSets = 4 / kSubs;          // groups of a block
   extern __shared__ __align__(128) unsigned char memory[];
   const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int blocks = (a.K + kBlockK - 1) / kBlockK, mine = (blocks + warps - 1) / warps;  // of K, to a warp
+  const int blocks = (a.K + kBlockK - 1) / kBlockK;
   const int m0 = blockIdx.y * a.tokens, tokens = min(a.tokens, a.M - m0), cols = tokens * kP;
-  // ring [warps][kDepth][kMt][16][64 bytes], sums [2][warps][kMt * 16][kRed], x [blocks][4][cols][4] x 16 bytes, scales
-  // of x [blocks][kNt * 8]
-  unsigned char* ring = memory + warp * kDepth * kMt * 1024;
-  float* sums = reinterpret_cast<float*>(memory + warps * kDepth * kMt * 1024);
-  uint4* xs = reinterpret_cast<uint4*>(sums + 2 * warps * kMt * 16 * kRed);
+  // x [blocks][4][cols][4] x 16 bytes, scales of x [blocks][kNt * 8], ring [warps][depth][kMt][16][64 bytes], in whose
+  // place the sums [warps][2][kMt * 16][kRed] go at the end
+  uint4* xs = reinterpret_cast<uint4*>(memory);
   float* x_scales = reinterpret_cast<float*>(xs + blocks * 16 * cols);
+  unsigned char* rings = reinterpret_cast<unsigned char*>(x_scales + (kScaled ? blocks * kNt * 8 : 0));
+  unsigned char* ring = rings + warp * a.depth * kMt * 1024;
+  const int stage_bytes = kMt * 1024, ring_bytes = a.depth * stage_bytes;
 
-  // position (tile, j): block warp + warps * j of that tile; the copies run kDepth - 1 positions ahead
-  int to_tile = blockIdx.x, to_j = 0, to_stage = 0;
-  auto fetch = [&]() {
-    const int block = warp + warps * to_j;
-    if (to_tile < a.tiles && block < blocks) {
-#pragma unroll
-      for (int q = 0; q < 2 * kMt; ++q) {  // 8 rows of 64 bytes at a time
-        const int row = q * 8 + g, n = min(to_tile * kMt * 16 + row, a.N - 1);
-        const bool in = block * kBlockK + t * 32 < a.K;
-        const uint8_t* from = a.q + (long long)n * a.q_pitch + (in ? block * 64 + t * 16 : 0);
-        // sub-block t of row r at place t ^ (r / 2 % 4): no two lanes of a read below meet in a bank
-        const uint32_t at = smem_u32(ring + to_stage * kMt * 1024 + row * 64 + ((t ^ (row >> 1 & 3)) << 4));
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(from), "r"(in ? 16 : 0) : "memory");
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    to_stage = to_stage + 1 == kDepth ? 0 : to_stage + 1;
-    if (++to_j == mine) to_j = 0, to_tile += gridDim.x;
-  };
-  // scales and zero points: a lane takes one group's of the next kSubs positions, for rows g and g + 8 of each 16
-  struct Set {
-    float s[2 * kMt];
-    unsigned z[2 * kMt];
-  };
-  auto load_set = [&](int tile, int j) {
-    Set v;
-    const int block = warp + warps * (j + t / kSets), group = block * kSets + t % kSets;
-    const bool in = tile < a.tiles && j + t / kSets < mine && group < a.groups;
-#pragma unroll
-    for (int q = 0; q < 2 * kMt; ++q) {
-      const long long at = (long long)min(tile * kMt * 16 + q * 8 + g, a.N - 1) * a.groups + group;
-      v.s[q] = in ? load_any(a.scale, at, a.scale_dtype) : 0.0f;
-      v.z[q] = in && a.zero ? a.zero[at] & 15u : 8u;
-    }
-    return v;
-  };
-#pragma unroll
-  for (int d = 0; d < kDepth - 1; ++d) fetch();
-  Set now, next = load_set(blockIdx.x, 0);
+  // this block's tiles, at most one to a warp at a time (so that a warp's stretch meets two tiles at most)
+  const int last_tile = stretch(blockIdx.x + 1, a.tiles_each, a.tiles_more);
+  bool staged = false;
+  for (int tile0 = stretch(blockIdx.x, a.tiles_each, a.tiles_more); tile0 < last_tile; tile0 += warps) {
+    const int tiles = min(warps, last_tile - tile0), n = tiles * blocks;  // of this turn
+    const int each = n / warps, more = n - each * warps;
+    const int begin = stretch(warp, each, more), count = stretch(warp + 1, each, more) - begin;
 
-  for (int c = threadIdx.x; c < tokens * blocks * 16; c += blockDim.x) {
-    const int token = c / (blocks * 16), chunk = c % (blocks * 16), k = chunk * 8;
-    uint32_t v[8];
-    load_chunk<kX>(a, m0 + token, k, a.x_vec, v);
-    int slot, lane_t;
-    place<kSubs>(chunk >> 2 & 3, chunk & 3, slot, lane_t);
-    uint4* to = xs + (((chunk >> 4) * 4 + slot) * cols + token * kP) * 4 + lane_t;
-    if constexpr (kP == 3) {
-      // three times the upper 16 bits of what is left; not finite: all in the first
+    // the copies
+    const int begin_tile = begin / blocks, begin_block = begin - begin_tile * blocks;
+    int to_tile = tile0 + begin_tile, to_block = begin_block, to_left = count;
+    const uint8_t* from[2 * kMt];
+    auto rows_of = [&](int tile) {
 #pragma unroll
-      for (int part = 0; part < 3; ++part) {
-        uint32_t u[8];
+      for (int q = 0; q < 2 * kMt; ++q)
+        from[q] = a.q + (long long)min(tile * kMt * 16 + q * 8 + g, a.N - 1) * a.q_pitch + t * 16;
+    };
+    rows_of(to_tile);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          u[e] = v[e] >> 16;
-          const bool finite = (v[e] & 0x7f800000u) != 0x7f800000u;
-          if (!finite && (v[e] & 0x007f0000u) == 0u && (v[e] & 0x007fffffu) != 0u) u[e] |= 0x40u;  // a NaN stays one
-          v[e] = finite ? __float_as_uint(__uint_as_float(v[e]) - __uint_as_float(v[e] & 0xffff0000u)) : 0u;
+    for (int q = 0; q < 2 * kMt; ++q) from[q] += to_block * 64;
+    // sub-block t of row r at place t ^ (r / 2 % 4): no two lanes of a read below meet in a bank
+    const uint32_t to_first = smem_u32(ring) + g * 64 + ((t ^ (g >> 1)) << 4);
+    uint32_t to_stage = to_first;
+    auto fetch = [&]() {
+      if (to_left > 0) {
+        --to_left;
+        if (to_block * kBlockK + t * 32 < a.K) {  // (else the x to it is zero, and any word a finite number)
+#pragma unroll
+          for (int q = 0; q < 2 * kMt; ++q)  // 8 rows of 64 bytes at a time
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to_stage + q * 512), "l"(from[q]) : "memory");
         }
-        to[part * 4] = in_order(u);
+#pragma unroll
+        for (int q = 0; q < 2 * kMt; ++q) from[q] += 64;
+        if (++to_block == blocks) {
+          to_block = 0;
+          rows_of(++to_tile);
+        }
       }
-    } else {
-      to[0] = in_order(v);
-    }
-  }
-  if constexpr (kScaled) {
-    for (int c = threadIdx.x; c < blocks * kNt * 8; c += blockDim.x) {
-      const int token = c % (kNt * 8), block = c / (kNt * 8);
-      x_scales[c] = token < tokens ? a.x_scale[(long long)(m0 + token) * a.x_groups + (a.x_groups > 1 ? block : 0)] : 0.0f;
-    }
-  }
-  __syncthreads();
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      to_stage += stage_bytes;
+      if (to_stage == to_first + ring_bytes) to_stage = to_first;
+    };
+    for (int d = 0; d < a.depth - 1; ++d) fetch();
 
-  float acc[kMt][kNt][4] = {};
-  int stage = 0, j = 0, turn = 0;
-  for (int tile = blockIdx.x; tile < a.tiles;) {
-    if (j % kSubs == 0) {
-      now = next;
-      next = j + kSubs < mine ? load_set(tile, j + kSubs) : load_set(tile + gridDim.x, 0);
+    // scales and zero points: a lane takes one group's of the next kSubs blocks, for rows g and g + 8 of each 16
+    struct Set {
+      uint32_t s[2 * kMt];  // as stored
+      unsigned z[2 * kMt];
+    };
+    int set_tile = tile0 + begin_tile, set_group = begin_block * kSets + t;
+    long long set_at[2 * kMt];
+    auto begin_set = [&]() {
+#pragma unroll
+      for (int q = 0; q < 2 * kMt; ++q)
+        set_at[q] = (long long)min(set_tile * kMt * 16 + q * 8 + g, a.N - 1) * a.groups + set_group;
+    };
+    begin_set();
+    auto load_set = [&]() {
+      Set v;
+#pragma unroll
+      for (int q = 0; q < 2 * kMt; ++q) v.s[q] = 0u, v.z[q] = 8u;
+      if (set_group < a.groups) {
+        if (a.scale_dtype == LSTM_APPROX_OP_FP32) {
+#pragma unroll
+          for (int q = 0; q < 2 * kMt; ++q) v.s[q] = static_cast<const uint32_t*>(a.scale)[set_at[q]];
+        } else {
+#pragma unroll
+          for (int q = 0; q < 2 * kMt; ++q) v.s[q] = static_cast<const uint16_t*>(a.scale)[set_at[q]];
+        }
+        if (a.zero) {
+#pragma unroll
+          for (int q = 0; q < 2 * kMt; ++q) v.z[q] = a.zero[set_at[q]];
+        }
+      }
+      set_group += 4;
+#pragma unroll
+      for (int q = 0; q < 2 * kMt; ++q) set_at[q] += 4;
+      if (set_group - t >= blocks * kSets) {
+        set_group = t;
+        ++set_tile;
+        begin_set();
+      }
+      return v;
+    };
+    auto scale_of = [&](uint32_t v) {
+      if (a.scale_dtype == LSTM_APPROX_OP_FP16) return __half2float(__ushort_as_half((unsigned short)v));
+      return __uint_as_float(a.scale_dtype == LSTM_APPROX_OP_BF16 ? v << 16 : v);
+    };
+    Set next = load_set();
+
+    if (!staged) {
+      for (int token = 0; token < tokens; ++token) {
+        for (int chunk = threadIdx.x; chunk < blocks * 16; chunk += blockDim.x) {
+          uint32_t v[8];
+          load_chunk<kX>(a, m0 + token, chunk * 8, a.x_vec, v);
+          int slot, lane_t;
+          place<kSubs>(chunk >> 2 & 3, chunk & 3, slot, lane_t);
+          uint4* to = xs + (((chunk >> 4) * 4 + slot) * cols + token * kP) * 4 + lane_t;
+          if constexpr (kP == 3) {
+            // three times the upper 16 bits of what is left; not finite: all in the first
+#pragma unroll
+            for (int part = 0; part < 3; ++part) {
+              uint32_t u[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                u[e] = v[e] >> 16;
+                const bool finite = (v[e] & 0x7f800000u) != 0x7f800000u;
+                if (!finite && (v[e] & 0x007f0000u) == 0u && (v[e] & 0x007fffffu) != 0u) u[e] |= 0x40u;  // NaN stays NaN
+                v[e] = finite ? __float_as_uint(__uint_as_float(v[e]) - __uint_as_float(v[e] & 0xffff0000u)) : 0u;
+              }
+              to[part * 4] = in_order(u);
+            }
+          } else {
+            to[0] = in_order(v);
+          }
+        }
+      }
+      if constexpr (kScaled) {
+        for (int c = threadIdx.x; c < blocks * kNt * 8; c += blockDim.x) {
+          const int token = c % (kNt * 8), block = c / (kNt * 8);
+          x_scales[c] =
+              token < tokens ? a.x_scale[(long long)(m0 + token) * a.x_groups + (a.x_groups > 1 ? block : 0)] : 0.0f;
+        }
+      }
+      staged = true;
+      __syncthreads();
     }
-    asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 2) : "memory");
-    __syncwarp();
-    fetch();
-    const int block = warp + warps * j;
-    if (block < blocks) {
-      const unsigned char* here = ring + stage * kMt * 1024;
+
+    float acc[kMt][kNt][4] = {};
+    float kept[kMt][kNt][4];  // of the first of two tiles
+    float now_s[2 * kMt];
+    unsigned now_z[2 * kMt];
+    int block = begin_block, in_set = 0, here = 0;
+    bool second = false;
+    // a lane whose column of x^T does not exist takes the last one's values; what they lead to is not stored
+    const uint4* xs_here[kNt];
+#pragma unroll
+    for (int c = 0; c < kNt; ++c) xs_here[c] = xs + (block * 4 * cols + min(c * 8 + g, cols - 1)) * 4 + t;
+    for (int p = 0; p < count; ++p) {
+      if (in_set == 0) {
+#pragma unroll
+        for (int q = 0; q < 2 * kMt; ++q) {
+          now_s[q] = scale_of(next.s[q]);
+          now_z[q] = next.z[q] & 15u;
+        }
+        next = load_set();
+      }
+      if (a.depth == 4) asm volatile("cp.async.wait_group 2;" ::: "memory");
+      else asm volatile("cp.async.wait_group 6;" ::: "memory");
+      __syncwarp();
+      fetch();
       float xsc[kNt][2];
       if constexpr (kScaled) {
 #pragma unroll
-        for (int n = 0; n < kNt; ++n) {
-          const float2 v = *reinterpret_cast<const float2*>(x_scales + block * kNt * 8 + n * 8 + 2 * t);
-          xsc[n][0] = v.x;
-          xsc[n][1] = v.y;
+        for (int c = 0; c < kNt; ++c) {
+          const float2 v = *reinterpret_cast<const float2*>(x_scales + block * kNt * 8 + c * 8 + 2 * t);
+          xsc[c][0] = v.x;
+          xsc[c][1] = v.y;
         }
       }
 #pragma unroll
       for (int set = 0; set < kSets; ++set) {  // groups of the block
-        const int from = (lane & ~3) | ((j % kSubs) * kSets + set);
+        const int from_lane = (lane & ~3) | (in_set * kSets + set);
         float s[2 * kMt];
-        uint32_t z[2 * kMt];
+        Zero<kBf16> z[2 * kMt];
 #pragma unroll
         for (int q = 0; q < 2 * kMt; ++q) {
-          s[q] = __shfl_sync(0xffffffffu, now.s[q], from);
-          z[q] = (kBf16 ? 0x43004300u : 0x64006400u) + __shfl_sync(0xffffffffu, now.z[q], from) * 0x00010001u;
+          s[q] = __shfl_sync(0xffffffffu, now_s[q], from_lane);
+          z[q] = zero_of<kBf16>(__shfl_sync(0xffffffffu, now_z[q], from_lane));
         }
         uint4 b[kSubs][kNt];
 #pragma unroll
         for (int i = 0; i < kSubs; ++i) {
 #pragma unroll
-          for (int n = 0; n < kNt; ++n) {
-            b[i][n] = make_uint4(0u, 0u, 0u, 0u);
-            if (n * 8 + g < cols) b[i][n] = xs[((block * 4 + set * kSubs + i) * cols + n * 8 + g) * 4 + t];
-          }
+          for (int c = 0; c < kNt; ++c) b[i][c] = xs_here[c][(set * kSubs + i) * cols * 4];
         }
 #pragma unroll
         for (int m = 0; m < kMt; ++m) {
@@ -287,16 +381,16 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
           uint32_t w[2][kSubs];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int row = m * 16 + h * 8 + g, swz = row >> 1 & 3;
-            const unsigned char* p = here + row * 64;
+            const unsigned char* row = ring + here + (m * 16 + h * 8 + g) * 64;
+            const int swz = g >> 1;
             if constexpr (kSubs == 4) {
-              const uint4 v = *reinterpret_cast<const uint4*>(p + ((t ^ swz) << 4));
+              const uint4 v = *reinterpret_cast<const uint4*>(row + ((t ^ swz) << 4));
               w[h][0] = v.x, w[h][1] = v.y, w[h][2] = v.z, w[h][3] = v.w;
             } else if constexpr (kSubs == 2) {
-              const uint2 v = *reinterpret_cast<const uint2*>(p + (((2 * set + (t & 1)) ^ swz) << 4) + (t >> 1) * 8);
+              const uint2 v = *reinterpret_cast<const uint2*>(row + (((2 * set + (t & 1)) ^ swz) << 4) + (t >> 1) * 8);
               w[h][0] = v.x, w[h][1] = v.y;
             } else {
-              w[h][0] = *reinterpret_cast<const uint32_t*>(p + ((set ^ swz) << 4) + t * 4);
+              w[h][0] = *reinterpret_cast<const uint32_t*>(row + ((set ^ swz) << 4) + t * 4);
             }
           }
           float part[kNt][4] = {};
@@ -304,63 +398,91 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
           for (int i = 0; i < kSubs; ++i) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-              const uint32_t a0 = nibbles<kBf16>(w[0][i], 8 * half, z[2 * m]);
-              const uint32_t a1 = nibbles<kBf16>(w[1][i], 8 * half, z[2 * m + 1]);
-              const uint32_t a2 = nibbles<kBf16>(w[0][i], 8 * half + 4, z[2 * m]);
-              const uint32_t a3 = nibbles<kBf16>(w[1][i], 8 * half + 4, z[2 * m + 1]);
+              uint32_t a0, a1, a2, a3;
+              nibbles<kBf16>(w[0][i] >> (8 * half), z[2 * m], a0, a2);
+              nibbles<kBf16>(w[1][i] >> (8 * half), z[2 * m + 1], a1, a3);
 #pragma unroll
-              for (int n = 0; n < kNt; ++n) {
-                const uint32_t b0 = half ? b[i][n].z : b[i][n].x, b1 = half ? b[i][n].w : b[i][n].y;
-                if constexpr (kBf16) mma_16816_bf16<true>(part[n], a0, a1, a2, a3, b0, b1);
-                else mma_16816_f16<true>(part[n], a0, a1, a2, a3, b0, b1);
+              for (int c = 0; c < kNt; ++c) {
+                const uint32_t b0 = half ? b[i][c].z : b[i][c].x, b1 = half ? b[i][c].w : b[i][c].y;
+                if constexpr (kBf16) mma_16816_bf16<true>(part[c], a0, a1, a2, a3, b0, b1);
+                else mma_16816_f16<true>(part[c], a0, a1, a2, a3, b0, b1);
               }
             }
           }
 #pragma unroll
-          for (int n = 0; n < kNt; ++n) {
+          for (int c = 0; c < kNt; ++c) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float v = kScaled ? part[n][e] * xsc[n][e & 1] : part[n][e];
-              acc[m][n][e] = fmaf(v, s[2 * m + (e >> 1)], acc[m][n][e]);
+              const float v = kScaled ? part[c][e] * xsc[c][e & 1] : part[c][e];
+              acc[m][c][e] = fmaf(v, s[2 * m + (e >> 1)], acc[m][c][e]);
             }
           }
         }
       }
-    }
-    stage = stage + 1 == kDepth ? 0 : stage + 1;
-    if (++j < mine) continue;
-    // the tile's sums: the warps' parts, in their order
-    float* to = sums + (turn * warps + warp) * kMt * 16 * kRed;
+      here = here + stage_bytes == ring_bytes ? 0 : here + stage_bytes;
+      in_set = in_set + 1 == kSubs ? 0 : in_set + 1;
 #pragma unroll
-    for (int m = 0; m < kMt; ++m) {
+      for (int c = 0; c < kNt; ++c) xs_here[c] += 16 * cols;
+      if (++block == blocks) {
+        block = in_set = 0;
 #pragma unroll
-      for (int n = 0; n < kNt; ++n) {
+        for (int c = 0; c < kNt; ++c) xs_here[c] -= blocks * 16 * cols;
+        if (p + 1 < count) {
+          second = true;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          to[(m * 16 + (e >> 1) * 8 + g) * kRed + n * 8 + 2 * t + (e & 1)] = acc[m][n][e];
-          acc[m][n][e] = 0.0f;
+          for (int m = 0; m < kMt; ++m)
+#pragma unroll
+            for (int c = 0; c < kNt; ++c)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                kept[m][c][e] = acc[m][c][e];
+                acc[m][c][e] = 0.0f;
+              }
         }
       }
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();  // no ring is in use any more
+    float* sums = reinterpret_cast<float*>(rings);
+    auto owner = [&](int position) {  // the warp whose stretch has this block
+      const int longer = more * (each + 1);
+      return position < longer ? position / (each + 1) : more + (position - longer) / max(each, 1);
+    };
+    if (count > 0) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (h == 1 && !second) break;
+        float* to = sums + (2 * warp + h) * kSum;
+#pragma unroll
+        for (int m = 0; m < kMt; ++m)
+#pragma unroll
+          for (int c = 0; c < kNt; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              to[(m * 16 + (e >> 1) * 8 + g) * kRed + c * 8 + 2 * t + (e & 1)] =
+                  h == 0 && second ? kept[m][c][e] : acc[m][c][e];
+      }
+    }
     __syncthreads();
-    const float* from = sums + turn * warps * kMt * 16 * kRed;
-    for (int o = threadIdx.x; o < kMt * 16 * tokens; o += blockDim.x) {
-      const int row = o % (kMt * 16), token = o / (kMt * 16), n = tile * kMt * 16 + row;
-      if (n >= a.N) continue;
+    // half a warp takes 16 rows by one row of x; a tile's parts come from the warps whose stretches meet it: the first's
+    // last part and the others' first
+    for (int item = 2 * warp + (lane >> 4); item < tiles * kMt * tokens; item += 2 * warps) {
+      const int token = item % tokens, sixteen = item / tokens, tile = sixteen / kMt;
+      const int row = sixteen % kMt * 16 + (lane & 15), out = (tile0 + tile) * kMt * 16 + row;
+      if (out >= a.N) continue;
+      const int w0 = owner(tile * blocks), w1 = owner((tile + 1) * blocks - 1);
+      const float* part = sums + row * kRed + token * kP;
       float v = 0.0f;
-      for (int w = 0; w < warps; ++w) {
-        const float* p = from + (w * kMt * 16 + row) * kRed + token * kP;
+      for (int w = w0; w <= w1; ++w) {
+        const float* p = part + (2 * w + (w == w0 && stretch(w, each, more) < tile * blocks ? 1 : 0)) * kSum;
         if constexpr (kP == 3) v += p[0] + (p[1] + p[2]);
         else v += p[0];
       }
-      if (a.bias) v += a.bias[n];
-      store_any(a.y, (long long)(m0 + token) * a.N + n, a.y_dtype, v);
+      if (a.bias) v += a.bias[out];
+      store_any(a.y, (long long)(m0 + token) * a.N + out, a.y_dtype, v);
     }
-    turn ^= 1;  // the next tile's parts go beside these
-    j = 0;
-    tile += gridDim.x;
+    __syncthreads();  // the rings' place is theirs again
   }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
 struct W4QuantizeArgs {
@@ -428,29 +550,29 @@ __global__ void __launch_bounds__(256) w4_quantize_kernel(const W4QuantizeArgs a
   }
 }
 
-// What a launch of the kernel takes: rows of x at a time, warps of a block, shared memory.
+// What a launch of the kernel takes.
 struct W4Plan {
-  int tokens, warps;
+  int tokens;  // rows of x at a time
+  int warps;   // of a block of threads
+  int depth;   // blocks of W in flight or in use to a warp
   size_t smem;
 };
 constexpr size_t kMostShared = 227 * 1024;
 constexpr int kMaxK = 32768;  // one row of x in 32 bits then fits beside four warps' blocks
 
+// As many rows of x as leave room for four warps, then as many warps as fit; eight blocks to a warp where 16 warps have
+// room for them, else four.
 inline W4Plan plan_matvec(int M, int K, int parts, int mt, int nt, bool scaled) {
   const int blocks = (K + kBlockK - 1) / kBlockK;
-  const size_t per_warp = kDepth * mt * 1024 + 2 * mt * 16 * (nt * 8 + 1) * sizeof(float);
-  W4Plan p{std::min(M, nt * 8 / parts), 0, 0};
-  // as many rows of x as leave room for four warps, then as many warps as fit: 8 of them share a tile's K where
-  // several blocks of threads fit on an SM, up to 16 where one does
-  for (;; --p.tokens) {
+  const size_t sums = 2 * mt * 16 * (nt * 8 + 1) * sizeof(float);
+  auto per_warp = [&](int depth) { return std::max<size_t>(depth * mt * 1024, sums); };
+  for (W4Plan p{std::min(M, nt * 8 / parts), 0, 0, 0};; --p.tokens) {
     const size_t x = (size_t)blocks * (256 * p.tokens * parts + (scaled ? 32 * nt : 0));
-    const int most = x > 40 * 1024 ? kMaxWarps : 8;
-    const int fit = x < kMostShared ? (int)((kMostShared - x) / per_warp) : 0;
-    if (fit >= 4 || p.tokens == 1) {
-      p.warps = std::max(1, std::min({most, fit, blocks}));
-      p.smem = p.warps * per_warp + x;
-      return p;
-    }
+    const size_t left = x < kMostShared ? kMostShared - x : 0;
+    p.depth = left >= kMaxWarps * per_warp(8) ? 8 : 4;
+    p.warps = (int)std::min<size_t>(kMaxWarps, left / per_warp(p.depth));
+    p.smem = x + p.warps * per_warp(p.depth);
+    if (p.warps >= 4 || p.tokens == 1) return p;
   }
 }
 
@@ -462,11 +584,13 @@ cudaError_t launch_matvec(W4Args a, cudaStream_t s) {
       &ready, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostShared); });
   if (e != cudaSuccess) return e;
   const W4Plan p = plan_matvec(a.M, a.K, kParts<kX>, kMt, kNt, kX == LSTM_APPROX_OP_E4M3);
-  if (p.smem > kMostShared) return cudaErrorInvalidValue;
+  if (p.warps < 1) return cudaErrorInvalidValue;
   a.tokens = p.tokens;
-  a.tiles = (a.N + kMt * 16 - 1) / (kMt * 16);
-  const int per_sm = (int)std::max<size_t>(1, std::min<size_t>(228 * 1024 / (p.smem + 1024), 32 / p.warps));
-  const dim3 grid(std::min(a.tiles, 152 * per_sm), (a.M + p.tokens - 1) / p.tokens);
+  a.depth = p.depth;
+  const int tiles = (a.N + kMt * 16 - 1) / (kMt * 16), across = std::min(tiles, 152);
+  a.tiles_each = tiles / across;
+  a.tiles_more = tiles % across;
+  const dim3 grid(across, (a.M + p.tokens - 1) / p.tokens);
   return op_launch(kern, grid, dim3(p.warps * 32), p.smem, s, a);
 }
 
@@ -533,7 +657,7 @@ extern "C" int lstm_approx_w4_matvec(int x_dtype, const void* x, long long x_pit
   const size_t xs = op_dtype_bytes(x_dtype);
   W4Args a{x_dtype, x, x_pitch, x_scale, x_group >= K || !x8 ? 1 : (K + 127) / 128, q, q_pitch, scale, scale_dtype, zero,
            bias, M, N, K, (K + group - 1) / group, y, y_dtype,
-           op_aligned(x, std::min<size_t>(16, 8 * xs)) && x_pitch * xs % std::min<size_t>(16, 8 * xs) == 0, 0, 0};
+           op_aligned(x, std::min<size_t>(16, 8 * xs)) && x_pitch * xs % std::min<size_t>(16, 8 * xs) == 0, 0, 0, 0, 0};
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   auto of_type = [&](auto type) {
     constexpr int kX = decltype(type)::value;
