@@ -88,11 +88,10 @@ template <bool kBf16>
 struct Zero {
   uint32_t low, high;
 };
+// (low: the pair of 128 + z or 1024 + z; as bits, -(64 + z) is 0xd400 + 16 z)
 template <bool kBf16>
-__device__ __forceinline__ Zero<kBf16> zero_of(unsigned z) {
-  if constexpr (kBf16) return {0x43004300u + z * 0x00010001u, 0u};
-  const __half2 h = __float2half2_rn(-64.0f - (float)z);
-  return {0x64006400u + z * 0x00010001u, *reinterpret_cast<const uint32_t*>(&h)};
+__device__ __forceinline__ Zero<kBf16> zero_of(uint32_t low) {
+  return {low, kBf16 ? 0u : low * 16u + (0xd400d400u - 0x64006400u * 16u)};
 }
 __device__ __forceinline__ uint32_t masked(uint32_t w, uint32_t mask, uint32_t magic) {
   uint32_t v;  // (w & mask) | magic
@@ -134,41 +133,77 @@ __device__ __forceinline__ void place(int sub, int word, int& slot, int& t) {
   }
 }
 
-// 8 values of x from k on (zero from K on), as fp32 bits or 16-bit values.
+// 8 values of x from k on (zero from K on): as they lie in memory, and as 16-bit (or fp32) values each.
 template <int kX>
-__device__ __forceinline__ void load_chunk(const W4Args& a, long long row, int k, bool vec, uint32_t (&v)[8]) {
-  if (vec && k + 8 <= a.K) {
-    if constexpr (kX == LSTM_APPROX_OP_FP32) {
-      const uint4* p = reinterpret_cast<const uint4*>(static_cast<const float*>(a.x) + row * a.x_pitch + k);
-      const uint4 lo = p[0], hi = p[1];
-      v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
-    } else if constexpr (kX == LSTM_APPROX_OP_E4M3) {
-      const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.x) + row * a.x_pitch + k);
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        v[e] = __half_raw(__nv_cvt_fp8_to_halfraw((uint8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3))), __NV_E4M3)).x;
+struct Chunk {
+  static constexpr int kWords = kX == LSTM_APPROX_OP_FP32 ? 8 : (kX == LSTM_APPROX_OP_E4M3 ? 2 : 4);
+  uint32_t w[kWords];
+};
+template <int kX>
+__device__ __forceinline__ Chunk<kX> load_chunk(const W4Args& a, long long row, int k) {
+  Chunk<kX> v;
+  constexpr int kBytes = Chunk<kX>::kWords / 2;  // of a value
+  const uint8_t* p = static_cast<const uint8_t*>(a.x) + (row * a.x_pitch + k) * kBytes;
+  if (a.x_vec && k + 8 <= a.K) {
+    if constexpr (kX == LSTM_APPROX_OP_E4M3) {
+      const uint2 u = *reinterpret_cast<const uint2*>(p);
+      v.w[0] = u.x, v.w[1] = u.y;
     } else {
-      const uint4 w = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.x) + row * a.x_pitch + k);
-      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = u[e / 2] >> (16 * (e & 1)) & 0xffffu;
+      for (int q = 0; q < Chunk<kX>::kWords / 4; ++q) {
+        const uint4 u = reinterpret_cast<const uint4*>(p)[q];
+        v.w[4 * q] = u.x, v.w[4 * q + 1] = u.y, v.w[4 * q + 2] = u.z, v.w[4 * q + 3] = u.w;
+      }
     }
   } else {
 #pragma unroll
+    for (int q = 0; q < Chunk<kX>::kWords; ++q) v.w[q] = 0u;
+#pragma unroll
     for (int e = 0; e < 8; ++e) {
-      v[e] = 0u;
-      if (k + e < a.K) {
-        const long long at = row * a.x_pitch + k + e;
-        if constexpr (kX == LSTM_APPROX_OP_FP32) v[e] = static_cast<const uint32_t*>(a.x)[at];
-        else if constexpr (kX == LSTM_APPROX_OP_E4M3)
-          v[e] = __half_raw(__nv_cvt_fp8_to_halfraw(static_cast<const uint8_t*>(a.x)[at], __NV_E4M3)).x;
-        else v[e] = static_cast<const uint16_t*>(a.x)[at];
-      }
+      if (k + e >= a.K) continue;
+      if constexpr (kBytes == 4) v.w[e] = reinterpret_cast<const uint32_t*>(p)[e];
+      else if constexpr (kBytes == 2) v.w[e / 2] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[e] << 16 * (e & 1);
+      else v.w[e / 4] |= (uint32_t)p[e] << 8 * (e & 3);
     }
   }
+  return v;
 }
-__device__ __forceinline__ uint4 in_order(const uint32_t (&v)[8]) {  // 16-bit values as pairs (0, 4) (1, 5) (2, 6) (3, 7)
-  return make_uint4(v[0] | v[4] << 16, v[1] | v[5] << 16, v[2] | v[6] << 16, v[3] | v[7] << 16);
+// 16-bit values (0, 1) (2, 3) (4, 5) (6, 7) as pairs (0, 4) (1, 5) (2, 6) (3, 7)
+__device__ __forceinline__ uint4 in_order(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3) {
+  return make_uint4(__byte_perm(w0, w2, 0x5410), __byte_perm(w0, w2, 0x7632), __byte_perm(w1, w3, 0x5410),
+                    __byte_perm(w1, w3, 0x7632));
+}
+// A chunk into its place, `to` that of its first column and 4 places to the next.
+template <int kX>
+__device__ __forceinline__ void place_chunk(const Chunk<kX>& v, uint4* to) {
+  if constexpr (kX == LSTM_APPROX_OP_FP32) {
+    // three times the upper 16 bits of what is left; not finite: all in the first
+    uint32_t left[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) left[e] = v.w[e];
+#pragma unroll
+    for (int part = 0; part < 3; ++part) {
+      uint32_t u[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        u[e] = left[e] >> 16;
+        const bool finite = (left[e] & 0x7f800000u) != 0x7f800000u;
+        if (!finite && (left[e] & 0x007f0000u) == 0u && (left[e] & 0x007fffffu) != 0u) u[e] |= 0x40u;  // NaN stays NaN
+        left[e] = finite ? __float_as_uint(__uint_as_float(left[e]) - __uint_as_float(left[e] & 0xffff0000u)) : 0u;
+      }
+      to[part * 4] = make_uint4(u[0] | u[4] << 16, u[1] | u[5] << 16, u[2] | u[6] << 16, u[3] | u[7] << 16);
+    }
+  } else if constexpr (kX == LSTM_APPROX_OP_E4M3) {
+    uint32_t h[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(v.w[q / 2] >> 16 * (q & 1)), __NV_E4M3);
+      h[q] = r.x | (uint32_t)r.y << 16;
+    }
+    to[0] = in_order(h[0], h[1], h[2], h[3]);
+  } else {
+    to[0] = in_order(v.w[0], v.w[1], v.w[2], v.w[3]);
+  }
 }
 
 // Columns of x^T to a row of x: its three parts in 32 bits.
@@ -201,6 +236,26 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
 
   // this block's tiles, at most one to a warp at a time (so that a warp's stretch meets two tiles at most)
   const int last_tile = stretch(blockIdx.x + 1, a.tiles_each, a.tiles_more);
+  // x: items of 8 k of up to kAtOnce rows; a thread's first is asked for before the copies of W that would delay it
+  constexpr int kAtOnce = 16 / Chunk<kX>::kWords;
+  const int chunks = blocks * 16, items = chunks * ((tokens + kAtOnce - 1) / kAtOnce);
+  Chunk<kX> v[kAtOnce];
+  auto load_item = [&](int item, Chunk<kX>(&to)[kAtOnce]) {
+    const int token = item / chunks * kAtOnce, chunk = item % chunks;
+#pragma unroll
+    for (int e = 0; e < kAtOnce; ++e)
+      if (token + e < tokens) to[e] = load_chunk<kX>(a, m0 + token + e, chunk * 8);
+  };
+  auto place_item = [&](int item, const Chunk<kX>(&from)[kAtOnce]) {
+    const int token = item / chunks * kAtOnce, chunk = item % chunks;
+    int slot, lane_t;
+    place<kSubs>(chunk >> 2 & 3, chunk & 3, slot, lane_t);
+    uint4* to = xs + (((chunk >> 4) * 4 + slot) * cols + token * kP) * 4 + lane_t;
+#pragma unroll
+    for (int e = 0; e < kAtOnce; ++e)
+      if (token + e < tokens) place_chunk<kX>(from[e], to + e * kP * 4);
+  };
+  if ((int)threadIdx.x < items) load_item(threadIdx.x, v);
   bool staged = false;
   for (int tile0 = stretch(blockIdx.x, a.tiles_each, a.tiles_more); tile0 < last_tile; tile0 += warps) {
     const int tiles = min(warps, last_tile - tile0), n = tiles * blocks;  // of this turn
@@ -290,31 +345,12 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
     Set next = load_set();
 
     if (!staged) {
-      for (int token = 0; token < tokens; ++token) {
-        for (int chunk = threadIdx.x; chunk < blocks * 16; chunk += blockDim.x) {
-          uint32_t v[8];
-          load_chunk<kX>(a, m0 + token, chunk * 8, a.x_vec, v);
-          int slot, lane_t;
-          place<kSubs>(chunk >> 2 & 3, chunk & 3, slot, lane_t);
-          uint4* to = xs + (((chunk >> 4) * 4 + slot) * cols + token * kP) * 4 + lane_t;
-          if constexpr (kP == 3) {
-            // three times the upper 16 bits of what is left; not finite: all in the first
-#pragma unroll
-            for (int part = 0; part < 3; ++part) {
-              uint32_t u[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                u[e] = v[e] >> 16;
-                const bool finite = (v[e] & 0x7f800000u) != 0x7f800000u;
-                if (!finite && (v[e] & 0x007f0000u) == 0u && (v[e] & 0x007fffffu) != 0u) u[e] |= 0x40u;  // NaN stays NaN
-                v[e] = finite ? __float_as_uint(__uint_as_float(v[e]) - __uint_as_float(v[e] & 0xffff0000u)) : 0u;
-              }
-              to[part * 4] = in_order(u);
-            }
-          } else {
-            to[0] = in_order(v);
-          }
-        }
+      int item = threadIdx.x;
+      while (item < items) {
+        const int now = item;
+        item += blockDim.x;
+        place_item(now, v);
+        if (item < items) load_item(item, v);
       }
       if constexpr (kScaled) {
         for (int c = threadIdx.x; c < blocks * kNt * 8; c += blockDim.x) {
@@ -342,7 +378,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
 #pragma unroll
         for (int q = 0; q < 2 * kMt; ++q) {
           now_s[q] = scale_of(next.s[q]);
-          now_z[q] = next.z[q] & 15u;
+          now_z[q] = (kBf16 ? 0x43004300u : 0x64006400u) + (next.z[q] & 15u) * 0x00010001u;
         }
         next = load_set();
       }
@@ -393,7 +429,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
               w[h][0] = *reinterpret_cast<const uint32_t*>(row + ((set ^ swz) << 4) + t * 4);
             }
           }
-          float part[kNt][4] = {};
+          float part[kNt][4];
 #pragma unroll
           for (int i = 0; i < kSubs; ++i) {
 #pragma unroll
@@ -404,8 +440,13 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
 #pragma unroll
               for (int c = 0; c < kNt; ++c) {
                 const uint32_t b0 = half ? b[i][c].z : b[i][c].x, b1 = half ? b[i][c].w : b[i][c].y;
-                if constexpr (kBf16) mma_16816_bf16<true>(part[c], a0, a1, a2, a3, b0, b1);
-                else mma_16816_f16<true>(part[c], a0, a1, a2, a3, b0, b1);
+                if (i == 0 && half == 0) {
+                  if constexpr (kBf16) mma_16816_bf16<true, true>(part[c], a0, a1, a2, a3, b0, b1);
+                  else mma_16816_f16<true, true>(part[c], a0, a1, a2, a3, b0, b1);
+                } else {
+                  if constexpr (kBf16) mma_16816_bf16<true, false>(part[c], a0, a1, a2, a3, b0, b1);
+                  else mma_16816_f16<true, false>(part[c], a0, a1, a2, a3, b0, b1);
+                }
               }
             }
           }
@@ -464,22 +505,24 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
       }
     }
     __syncthreads();
-    // half a warp takes 16 rows by one row of x; a tile's parts come from the warps whose stretches meet it: the first's
-    // last part and the others' first
-    for (int item = 2 * warp + (lane >> 4); item < tiles * kMt * tokens; item += 2 * warps) {
-      const int token = item % tokens, sixteen = item / tokens, tile = sixteen / kMt;
-      const int row = sixteen % kMt * 16 + (lane & 15), out = (tile0 + tile) * kMt * 16 + row;
+    // a warp takes 16 rows, two rows of x at a time; a tile's parts come from the warps whose stretches meet it: the
+    // first's last part and the others' first
+    for (int sixteen = warp; sixteen < tiles * kMt; sixteen += warps) {
+      const int tile = sixteen / kMt, row = sixteen % kMt * 16 + (lane & 15), out = (tile0 + tile) * kMt * 16 + row;
       if (out >= a.N) continue;
       const int w0 = owner(tile * blocks), w1 = owner((tile + 1) * blocks - 1);
-      const float* part = sums + row * kRed + token * kP;
-      float v = 0.0f;
-      for (int w = w0; w <= w1; ++w) {
-        const float* p = part + (2 * w + (w == w0 && stretch(w, each, more) < tile * blocks ? 1 : 0)) * kSum;
-        if constexpr (kP == 3) v += p[0] + (p[1] + p[2]);
-        else v += p[0];
+      const float* part = sums + (2 * w0 + (stretch(w0, each, more) < tile * blocks ? 1 : 0)) * kSum + row * kRed;
+      const float* rest = sums + 2 * (w0 + 1) * kSum + row * kRed;
+      const float bias = a.bias ? a.bias[out] : 0.0f;
+      for (int token = lane >> 4; token < tokens; token += 2) {
+        auto sum_of = [&](const float* p) {
+          if constexpr (kP == 3) return p[0] + (p[1] + p[2]);
+          else return p[0];
+        };
+        float v = sum_of(part + token * kP);
+        for (int w = 0; w < w1 - w0; ++w) v += sum_of(rest + 2 * w * kSum + token * kP);
+        store_any(a.y, (long long)(m0 + token) * a.N + out, a.y_dtype, v + bias);
       }
-      if (a.bias) v += a.bias[out];
-      store_any(a.y, (long long)(m0 + token) * a.N + out, a.y_dtype, v);
     }
     __syncthreads();  // the rings' place is theirs again
   }

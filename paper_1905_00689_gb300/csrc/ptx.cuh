@@ -369,24 +369,26 @@ __device__ __forceinline__ void tma_prefetch_map(const void* tmap) {
 
 // ---- warp MMA (few columns: the operands come from registers) --------------
 
-// d += a b for a 16 x 16 (row g = lane / 4 and g + 8; columns 2 t, 2 t + 1 in a0 and a1, 8 more in a2 and a3, t =
-// lane % 4), b 16 x 8 (column g, rows likewise in b0, b1), d 16 x 8 fp32 (rows g and g + 8, columns 2 t, 2 t + 1).
-// kTogether: as for the tensor-memory loads.
-template <bool kTogether>
+// d = a b (kFirst) or d += a b for a 16 x 16 (row g = lane / 4 and g + 8; columns 2 t, 2 t + 1 in a0 and a1, 8 more in a2
+// and a3, t = lane % 4), b 16 x 8 (column g, rows likewise in b0, b1), d 16 x 8 fp32 (rows g and g + 8, columns 2 t,
+// 2 t + 1).  kTogether: as for the tensor-memory loads.
+template <bool kTogether, bool kFirst>
 __device__ __forceinline__ void mma_16816_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                                uint32_t b1) {
   if constexpr (!kTogether) __syncwarp();
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(kFirst ? 0.0f : d[0]), "f"(kFirst ? 0.0f : d[1]),
+                 "f"(kFirst ? 0.0f : d[2]), "f"(kFirst ? 0.0f : d[3]));
 }
-template <bool kTogether>
+template <bool kTogether, bool kFirst>
 __device__ __forceinline__ void mma_16816_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                               uint32_t b1) {
   if constexpr (!kTogether) __syncwarp();
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(kFirst ? 0.0f : d[0]), "f"(kFirst ? 0.0f : d[1]),
+                 "f"(kFirst ? 0.0f : d[2]), "f"(kFirst ? 0.0f : d[3]));
 }
 
 // ---- tcgen05: tensor memory and the 5th-generation MMA --------------------
