@@ -1,20 +1,25 @@
-"""Build the C-ABI library liblstm_approx.so in-tree with nvcc for sm_103a.
+"""Build the C-ABI library liblstm_approx.so in-tree with nvcc for sm_103a,
+and the module _torch_ops that passes torch tensors to its operators.
 
-Each CUDA translation unit is compiled in parallel, then linked into one
-shared library next to this file.  Objects go to ``_build/`` (git-ignored).
+Each translation unit is compiled in parallel, then linked into one shared
+library and one module next to this file.  Objects go to ``_build/``
+(git-ignored).
 """
 from __future__ import annotations
 
 import concurrent.futures
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "liblstm_approx.so")
+MODULE = os.path.join(HERE, "_torch_ops.so")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -38,10 +43,35 @@ def _deps():
 
 
 def up_to_date() -> bool:
-    if not os.path.exists(LIB):
+    if not (os.path.exists(LIB) and os.path.exists(MODULE)):
         return False
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(MODULE))
     return all(os.path.getmtime(p) <= t for p in _deps())
+
+
+def _run(cmd, what: str, verbose: bool = False):
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{what}:\n{r.stdout}\n{r.stderr}")
+    if verbose and (r.stdout or r.stderr):
+        sys.stderr.write(r.stdout + r.stderr)
+
+
+def _torch_dir() -> str:
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        raise RuntimeError("torch not found")
+    return spec.submodule_search_locations[0]
+
+
+def _compile_module() -> str:
+    torch, obj = _torch_dir(), os.path.join(BUILD, "torch_ops.o")
+    cuda = os.path.dirname(os.path.dirname(_nvcc()))
+    include = [INCLUDE, sysconfig.get_paths()["include"], os.path.join(torch, "include"),
+               os.path.join(torch, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")]
+    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", *("-I" + d for d in include), "-c",
+          os.path.join(CSRC, "torch_ops.cpp"), "-o", obj], "g++ failed for torch_ops.cpp")
+    return obj
 
 
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
@@ -55,21 +85,20 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
     def compile_one(src):
         obj = os.path.join(BUILD, os.path.basename(src)[:-3] + ".o")
         cmd = [nvcc, *NVCC_FLAGS, *extra_flags, "-c", src, "-o", obj]
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        if r.returncode != 0:
-            raise RuntimeError(f"nvcc failed for {src}:\n{r.stdout}\n{r.stderr}")
-        if verbose and (r.stdout or r.stderr):
-            sys.stderr.write(r.stdout + r.stderr)
+        _run(cmd, f"nvcc failed for {src}", verbose)
         return obj
 
-    with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
+    with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(srcs) + 1)) as ex:
+        module = ex.submit(_compile_module)
         objs = list(ex.map(compile_one, srcs))
+        module_obj = module.result()
     tmp = LIB + ".tmp"
-    cmd = [nvcc, *ARCH, "-shared", "-o", tmp, *objs]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
+    _run([nvcc, *ARCH, "-shared", "-o", tmp, *objs], "link failed")
     os.replace(tmp, LIB)
+    tmp = MODULE + ".tmp"
+    _run(["g++", "-shared", "-o", tmp, module_obj, "-L" + os.path.join(_torch_dir(), "lib"), "-ltorch", "-ltorch_python",
+          "-lc10", "-lc10_cuda", "-L" + HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"], "module link failed")
+    os.replace(tmp, MODULE)
     return LIB
 
 
