@@ -6,22 +6,147 @@
 //            columns: dw = sum over rows of dy s rstd
 //
 // Bound by memory: a row is read once, kept in registers as fp32 while its
-// sum is formed, and written once.  A thread holds VPT groups of 8
-// neighbouring columns (16-byte accesses where the addresses allow them),
-// `blockDim.x` threads share a row, and rows of at most 32 threads share a
-// block (no block-wide sum then).
+// sum is formed, and written once.  `blockDim.x` threads share a row, each
+// holds VPT times 8 neighbouring columns, and rows of at most 32 threads share
+// a block (no block-wide sum then).
+//
+// A warp moves its 256 columns in accesses of kUnit values: of 8 where every
+// address is a multiple of 16 bytes (a thread's own columns); else of 2 16-bit
+// values at even addresses or of single values, neighbouring lanes next to one
+// another, and the columns change hands through shared memory.  (With a
+// thread's columns fetched one by one, 5001 x 1531 in 32 bits took 48 us
+// forward, with this 27.)  The sums are the same bits in all three.
 #include <cuda_fp8.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "ops_common.cuh"
+#include "ptx.cuh"
 
 namespace lstm_approx_impl {
 namespace {
 
+using namespace lstm_approx_dev;
+
 constexpr int kMaxD = 32768;
 constexpr float kE4m3Max = 448.0f;
 constexpr float kMinScale = 1.17549435e-38f;  // 2^-126
+
+// Column of the thread's first in group j, and of its warp's first.
+__device__ __forceinline__ int column(int j) { return (j * (int)blockDim.x + (int)threadIdx.x) * 8; }
+__device__ __forceinline__ int warp_column(int j) { return (j * (int)blockDim.x + (int)(threadIdx.x & ~31u)) * 8; }
+
+// One warp's 256 columns on their way from lane to lane.
+struct Swap {
+  float4 v[64];
+};
+template <int kUnit>
+__device__ __forceinline__ Swap& swap_of_warp() {
+  __shared__ Swap swaps[kUnit == 8 ? 1 : 32];
+  return swaps[kUnit == 8 ? 0 : (threadIdx.y * blockDim.x + threadIdx.x) >> 5];
+}
+
+// A thread's part of group j as it lies in memory (zero past D), and its 8 columns as fp32.
+template <typename T, int kUnit>
+struct Raw8 {
+  uint32_t w[8 * sizeof(T) / 4];
+
+  __device__ __forceinline__ void load(const T* row, int j, int D) {
+    const int lane = threadIdx.x & 31;
+    if constexpr (kUnit == 8) {
+      const int col = column(j);
+#pragma unroll
+      for (int q = 0; q < (int)sizeof(T) / 2; ++q) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (col < D) v = reinterpret_cast<const uint4*>(row + col)[q];
+        w[4 * q] = v.x, w[4 * q + 1] = v.y, w[4 * q + 2] = v.z, w[4 * q + 3] = v.w;
+      }
+    } else if constexpr (kUnit * sizeof(T) == 4) {
+#pragma unroll
+      for (int q = 0; q < 8 / kUnit; ++q) {
+        const int col = warp_column(j) + (q * 32 + lane) * kUnit;
+        w[q] = col < D ? *reinterpret_cast<const uint32_t*>(row + col) : 0u;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int col = warp_column(j) + q * 32 + lane;
+        const uint32_t v = col < D ? *reinterpret_cast<const uint16_t*>(row + col) : 0u;
+        w[q / 2] = q & 1 ? w[q / 2] | v << 16 : v;
+      }
+    }
+  }
+  __device__ __forceinline__ float2 pair(int p) const {
+    if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * p]), __uint_as_float(w[2 * p + 1]));
+    else return Pair<T>::get(*reinterpret_cast<const typename Pair<T>::Raw*>(&w[p]));
+  }
+  // Called by whole warps.
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    if constexpr (kUnit == 8) {
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const float2 f = pair(p);
+        v[2 * p] = f.x;
+        v[2 * p + 1] = f.y;
+      }
+    } else {
+      const int lane = threadIdx.x & 31;
+      Swap& swap = swap_of_warp<kUnit>();
+      float* to = reinterpret_cast<float*>(swap.v);
+      __syncwarp();
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const float2 f = pair(p);
+        if constexpr (kUnit == 2) {
+          *reinterpret_cast<float2*>(to + (p * 32 + lane) * 2) = f;
+        } else {
+          to[2 * p * 32 + lane] = f.x;
+          to[(2 * p + 1) * 32 + lane] = f.y;
+        }
+      }
+      __syncwarp();
+      const float4 lo = swap.v[2 * lane], hi = swap.v[2 * lane + 1];
+      v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+    }
+  }
+};
+// Stores a thread's 8 columns of group j; called by whole warps.
+template <typename T, int kUnit>
+__device__ __forceinline__ void put8(T* row, int j, int D, const float (&v)[8]) {
+  if constexpr (kUnit == 8) {
+    const int col = column(j);
+    if (col < D) store8<T, true>(row + col, 8, v);
+  } else {
+    const int lane = threadIdx.x & 31;
+    Swap& swap = swap_of_warp<kUnit>();
+    const float* from = reinterpret_cast<const float*>(swap.v);
+    __syncwarp();
+    swap.v[2 * lane] = make_float4(v[0], v[1], v[2], v[3]);
+    swap.v[2 * lane + 1] = make_float4(v[4], v[5], v[6], v[7]);
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 8 / kUnit; ++q) {
+      const int at = (q * 32 + lane) * kUnit, col = warp_column(j) + at;
+      if (col >= D) continue;
+      if constexpr (kUnit == 2) {
+        const float2 f = *reinterpret_cast<const float2*>(from + at);
+        *reinterpret_cast<typename Pair<T>::Raw*>(row + col) = Pair<T>::put(f.x, f.y);
+      } else {
+        row[col] = from_f32<T>(from[at]);
+      }
+    }
+  }
+}
+__device__ __forceinline__ void weights8(const float* w, int j, int D, bool aligned, float (&v)[8]) {
+  const int col = column(j);
+  if (aligned && col + 8 <= D) {
+    load8<float, true>(w + col, 8, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = col + e < D ? w[col + e] : 0.0f;
+  }
+}
 
 struct NormArgs {
   const void* x;
@@ -37,6 +162,7 @@ struct NormArgs {
   int group, n_groups;  // columns per scale (0: no scales), scales per row
   void* sum_out;
   float* rstd;
+  bool weight_vec;  // weight is 16-byte aligned
 };
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -46,13 +172,17 @@ __device__ __forceinline__ float warp_sum(float v) {
 }
 
 // Sum over the threads of a row, the same bits in all of them.  `part`: one
-// slot per warp; every use of a `part` array has its own.
+// slot per warp of the row; every use of a `part` array has its own.  kMany:
+// rows share a block (threadIdx.y) and each meet in a barrier of their own (with
+// which a block takes all 16 of its barriers, and fewer blocks fit on an SM).
+template <bool kMany>
 __device__ __forceinline__ float row_sum(float v, float* part) {
   v = warp_sum(v);
   const int warps = blockDim.x >> 5;
   if (warps > 1) {
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
+    if (!kMany || blockDim.y == 1) __syncthreads();
+    else asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.y + 1), "r"(blockDim.x) : "memory");
     v = warp_sum((threadIdx.x & 31) < warps ? part[threadIdx.x & 31] : 0.0f);
   }
   return v;
@@ -73,12 +203,12 @@ __device__ __forceinline__ unsigned row_max(unsigned v, unsigned* part) {
 
 __device__ __forceinline__ float scale_of(unsigned amax_bits) {
   if (amax_bits == 0u) return 1.0f;
-  const float s = __uint_as_float(amax_bits) / kE4m3Max;
+  const float s = __uint_as_float(amax_bits) * (1.0f / kE4m3Max);
   return s < kMinScale ? kMinScale : s;  // NaN stays
 }
 
 __device__ __forceinline__ uint2 to_e4m3(const float (&y)[8], float scale) {
-  const float inv = 1.0f / scale;
+  const float inv = rcp_approx(scale);  // (a scale is at least 2^-126)
   unsigned w[2];
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
@@ -90,35 +220,35 @@ __device__ __forceinline__ uint2 to_e4m3(const float (&y)[8], float scale) {
   return make_uint2(w[0], w[1]);
 }
 
-template <typename T, int VPT, bool kVec, bool kQuant>
-__global__ void __launch_bounds__(1024) rms_norm_kernel(const NormArgs a) {
+template <typename T, int VPT, int kMost, int kUnit, bool kQuant>
+__global__ void __launch_bounds__(kMost) rms_norm_kernel(const NormArgs a) {
   __shared__ float part[32];
   __shared__ unsigned part_max[32];
   const long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
   if (row >= a.rows) return;  // a whole warp (rows share a block only where a row is one warp)
   const T* x = static_cast<const T*>(a.x) + row * a.x_pitch;
-  const T* res = a.residual ? static_cast<const T*>(a.residual) + row * a.residual_pitch : nullptr;
+  Raw8<T, kUnit> raw[VPT];
   float s[VPT][8];
-  float sum = 0.0f;
 #pragma unroll
-  for (int j = 0; j < VPT; ++j) {
-    const int col = 8 * (threadIdx.x + j * blockDim.x);
+  for (int j = 0; j < VPT; ++j) raw[j].load(x, j, a.D);
+  if (a.residual) {
+    const T* res = static_cast<const T*>(a.residual) + row * a.residual_pitch;
+    Raw8<T, kUnit> more[VPT];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[j][e] = 0.0f;
-    if (col < a.D) load8<T, kVec>(x + col, a.D - col, s[j]);
-  }
-  if (res) {
+    for (int j = 0; j < VPT; ++j) more[j].load(res, j, a.D);
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-      const int col = 8 * (threadIdx.x + j * blockDim.x);
-      if (col < a.D) {
-        float v[8];
-        load8<T, kVec>(res + col, a.D - col, v);
+      float v[8];
+      raw[j].get(s[j]);
+      more[j].get(v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[j][e] += v[e];
-      }
+      for (int e = 0; e < 8; ++e) s[j][e] += v[e];
     }
+  } else {
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) raw[j].get(s[j]);
   }
+  float sum = 0.0f;
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
 #pragma unroll
@@ -127,31 +257,22 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(const NormArgs a) {
   if (a.sum_out) {
     T* so = static_cast<T*>(a.sum_out) + row * a.D;
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-      const int col = 8 * (threadIdx.x + j * blockDim.x);
-      if (col < a.D) store8<T, kVec>(so + col, a.D - col, s[j]);
-    }
+    for (int j = 0; j < VPT; ++j) put8<T, kUnit>(so, j, a.D, s[j]);
   }
-  sum = row_sum(sum, part);
+  sum = row_sum<false>(sum, part);
   const float rstd = rsqrtf(sum / (float)a.D + a.eps);
   if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
-    const int col = 8 * (threadIdx.x + j * blockDim.x);
-    if (col < a.D) {
-      float w[8];
-      load8<float, kVec>(a.weight + col, a.D - col, w);
+    float w[8];
+    weights8(a.weight, j, a.D, a.weight_vec, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[j][e] = s[j][e] * rstd * w[e];
-    }
+    for (int e = 0; e < 8; ++e) s[j][e] = s[j][e] * rstd * w[e];
   }
   if constexpr (!kQuant) {
     T* out = static_cast<T*>(a.out) + row * a.D;
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-      const int col = 8 * (threadIdx.x + j * blockDim.x);
-      if (col < a.D) store8<T, kVec>(out + col, a.D - col, s[j]);
-    }
+    for (int j = 0; j < VPT; ++j) put8<T, kUnit>(out, j, a.D, s[j]);
   } else {
     // the largest |y| of each group: a group of 32 to 256 columns is 4 to 32
     // neighbouring lanes (blockDim.x is a multiple of 32), a longer one the row
@@ -162,7 +283,8 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(const NormArgs a) {
     for (int j = 0; j < VPT; ++j) {
       m[j] = 0u;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) m[j] = max(m[j], __float_as_uint(s[j][e]) & 0x7fffffffu);
+      for (int e = 0; e < 8; ++e)  // (a column past D: zero times an rstd that may not be finite)
+        if (column(j) + e < a.D) m[j] = max(m[j], __float_as_uint(s[j][e]) & 0x7fffffffu);
       all = max(all, m[j]);
     }
     if (whole) {
@@ -179,11 +301,11 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(const NormArgs a) {
     float* scales = a.scales + row * a.n_groups;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-      const int col = 8 * (threadIdx.x + j * blockDim.x);
+      const int col = column(j);
       if (col < a.D) {
         const float scale = scale_of(m[j]);
         const uint2 q = to_e4m3(s[j], scale);
-        if constexpr (kVec) {
+        if (kUnit == 8) {
           *reinterpret_cast<uint2*>(out + col) = q;
         } else {
 #pragma unroll
@@ -195,6 +317,8 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(const NormArgs a) {
     }
   }
 }
+
+constexpr int kMaxRows = 16;  // of a block
 
 struct NormBackwardArgs {
   const void* dy;
@@ -208,81 +332,97 @@ struct NormBackwardArgs {
   long long rows;
   int D;
   void* dx;
-  float* partial;  // [gridDim.x * blockDim.y][D]: sums of dy s rstd over the rows of each block row; or null
+  float* partial;  // [gridDim.x][pitch_of_partial(D)]: each block's sum of dy s rstd over its rows; or null
+  bool weight_vec;
 };
+__host__ __device__ constexpr int pitch_of_partial(int D) { return (D + 7) / 8 * 8; }
 
-template <typename T, int VPT, bool kVec>
-__global__ void __launch_bounds__(1024) rms_norm_backward_kernel(const NormBackwardArgs a) {
-  __shared__ float part[2][32];
+// A block's rows go on by all blocks' rows; the next one's values are on their way while this one's sum is formed.
+template <typename T, int VPT, int kMost, int kUnit>
+__global__ void __launch_bounds__(kMost) rms_norm_backward_kernel(const NormBackwardArgs a) {
+  __shared__ float part[2][kMaxRows][32];
+  extern __shared__ __align__(16) float merged[];  // [rows of the block][pitch] where there are several
   float w[VPT][8], dw[VPT][8];
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
-    const int col = 8 * (threadIdx.x + j * blockDim.x);
+    weights8(a.weight, j, a.D, a.weight_vec, w[j]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[j][e] = dw[j][e] = 0.0f;
-    if (col < a.D) load8<float, kVec>(a.weight + col, a.D - col, w[j]);
+    for (int e = 0; e < 8; ++e) dw[j][e] = 0.0f;
   }
   const long long step = (long long)gridDim.x * blockDim.y;
-  int turn = 0;
-  for (long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y; row < a.rows; row += step) {
+  long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+  Raw8<T, kUnit> raw_g[VPT], raw_s[VPT], raw_d[VPT];
+  float rstd = 0.0f;
+  auto load = [&](long long row) {
     const T* dy = static_cast<const T*>(a.dy) + row * a.dy_pitch;
     const T* s = static_cast<const T*>(a.s) + row * a.s_pitch;
-    const T* ds = a.dsum ? static_cast<const T*>(a.dsum) + row * a.dsum_pitch : nullptr;
-    const float rstd = a.rstd[row];
-    float g[VPT][8], v[VPT][8];
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) raw_g[j].load(dy, j, a.D), raw_s[j].load(s, j, a.D);
+    if (a.dsum) {
+      const T* ds = static_cast<const T*>(a.dsum) + row * a.dsum_pitch;
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) raw_d[j].load(ds, j, a.D);
+    }
+    rstd = a.rstd[row];
+  };
+  if (row < a.rows) load(row);
+  int turn = 0;
+  for (; row < a.rows; row += step) {
+    float g[VPT][8], v[VPT][8], r[VPT][8];
     float sum = 0.0f;
+    const float scale = rstd;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-      const int col = 8 * (threadIdx.x + j * blockDim.x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) g[j][e] = v[j][e] = 0.0f;
-      if (col < a.D) {
-        load8<T, kVec>(dy + col, a.D - col, g[j]);
-        load8<T, kVec>(s + col, a.D - col, v[j]);
-      }
+      raw_g[j].get(g[j]);
+      raw_s[j].get(v[j]);
+      if (a.dsum) raw_d[j].get(r[j]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        v[j][e] *= rstd;
+        if (!a.dsum) r[j][e] = 0.0f;
+        v[j][e] *= scale;
         dw[j][e] = fmaf(g[j][e], v[j][e], dw[j][e]);
         g[j][e] *= w[j][e];
         sum = fmaf(g[j][e], v[j][e], sum);
       }
     }
-    sum = row_sum(sum, part[turn]);
+    if (row + step < a.rows) load(row + step);
+    sum = row_sum<true>(sum, part[turn][threadIdx.y]);
     turn ^= 1;  // the next row's sums may be written while slow threads still read this row's
     const float mean = sum / (float)a.D;
     T* dx = static_cast<T*>(a.dx) + row * a.D;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-      const int col = 8 * (threadIdx.x + j * blockDim.x);
-      if (col < a.D) {
-        float r[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = 0.0f;
-        if (ds) load8<T, kVec>(ds + col, a.D - col, r);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = fmaf(rstd, g[j][e] - v[j][e] * mean, r[e]);
-        store8<T, kVec>(dx + col, a.D - col, r);
-      }
+      for (int e = 0; e < 8; ++e) r[j][e] = fmaf(scale, g[j][e] - v[j][e] * mean, r[j][e]);
+      put8<T, kUnit>(dx, j, a.D, r[j]);
     }
   }
   if (a.partial) {
-    float* p = a.partial + ((long long)blockIdx.x * blockDim.y + threadIdx.y) * a.D;
+    const int pitch = pitch_of_partial(a.D);
+    float* p = a.partial + (long long)blockIdx.x * pitch;
+    float* to = blockDim.y == 1 ? p : merged + threadIdx.y * pitch;
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-      const int col = 8 * (threadIdx.x + j * blockDim.x);
-      if (col < a.D) store8<float, kVec>(p + col, a.D - col, dw[j]);
+    for (int j = 0; j < VPT; ++j)
+      if (column(j) < a.D) store8<float, true>(to + column(j), 8, dw[j]);
+    if (blockDim.y > 1) {  // the block's rows, in their order
+      __syncthreads();
+      for (int col = threadIdx.y * blockDim.x + threadIdx.x; col < a.D; col += blockDim.x * blockDim.y) {
+        float v = 0.0f;
+        for (int y = 0; y < (int)blockDim.y; ++y) v += merged[y * pitch + col];
+        p[col] = v;
+      }
     }
   }
 }
 
-// Column sums of partial [n][D], in a fixed order.
+// Column sums of partial [n][pitch_of_partial(D)], in a fixed order.
 __global__ void __launch_bounds__(1024) column_sum_kernel(const float* partial, int n, int D, float* out) {
   __shared__ float acc[32][33];
   const int col = blockIdx.x * 32 + threadIdx.x;
   float v = 0.0f;
   if (col < D)
-    for (int k = threadIdx.y; k < n; k += 32) v += partial[(long long)k * D + col];
+#pragma unroll 4
+    for (int k = threadIdx.y; k < n; k += 32) v += partial[(long long)k * pitch_of_partial(D) + col];
   acc[threadIdx.y][threadIdx.x] = v;
   __syncthreads();
   v = warp_sum(acc[threadIdx.x][threadIdx.y]);
@@ -294,19 +434,54 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const float* partial, 
 struct RowShape {
   int threads, vpt, rows_per_block;
 };
-RowShape row_shape(int D) {
+// 16-bit values in 16-byte accesses: two groups to a thread from 1024 columns on and four from 4096 (at 8192 x 4096, 512
+// threads with one group took 50 us, 256 with two 44); else two only where one would take more than 512 threads.
+RowShape row_shape(int D, bool wide) {
   const int n = (D + 7) / 8;
   RowShape r;
-  r.vpt = n > 2048 ? 4 : (n > 512 ? 2 : 1);
+  r.vpt = n > 2048 ? 4 : (n > 512 ? (wide && n <= 1024 ? 4 : 2) : (wide && n >= 128 ? 2 : 1));
   r.threads = ((n + r.vpt - 1) / r.vpt + 31) / 32 * 32;
   r.rows_per_block = r.threads == 32 ? 4 : 1;
   return r;
 }
 
+// The same backward, where a thread holds three tensors' columns: two groups from 1024 columns on.  Short rows share a
+// block of up to 512 threads, so that there are at most 304 blocks' sums to add up.
+RowShape backward_shape(int D, bool wide) {
+  RowShape r;
+  const int n = (D + 7) / 8;
+  r.vpt = n > 2048 ? 4 : (n > 512 || (wide && n >= 128) ? 2 : 1);
+  r.threads = ((n + r.vpt - 1) / r.vpt + 31) / 32 * 32;
+  r.rows_per_block = r.threads == 32 ? kMaxRows : std::max(1, std::min(8, 512 / r.threads));
+  return r;
+}
 int backward_blocks(long long rows, const RowShape& r) {
-  const int per = std::max(1, 1024 / (r.threads * r.rows_per_block));
-  const long long need = (rows + r.rows_per_block - 1) / r.rows_per_block;
-  return (int)std::min<long long>(need, 152ll * per);
+  return (int)std::min<long long>((rows + r.rows_per_block - 1) / r.rows_per_block, 2 * 152);
+}
+
+// Values of an access (see the top): every pointer a multiple of it and every pitch.
+struct Access {
+  const void* p;
+  long long pitch;
+};
+int unit_of(int D, size_t es, std::initializer_list<Access> all) {
+  auto fits = [&](size_t bytes) {
+    for (const Access& a : all)
+      if (a.p && (!op_aligned(a.p, bytes) || a.pitch * es % bytes != 0)) return false;
+    return D * es % bytes == 0;
+  };
+  return D % 8 == 0 && fits(16) ? 8 : (es == 2 && fits(4) ? 2 : 1);
+}
+
+// f(groups of 8 columns to a thread, most threads of the kernel) for a row's shape.
+template <typename F>
+cudaError_t with_shape(const RowShape& r, F f) {
+  using std::integral_constant;
+  if (r.vpt == 1) return f(integral_constant<int, 1>(), integral_constant<int, 512>());
+  if (r.vpt == 2 && r.threads <= 512) return f(integral_constant<int, 2>(), integral_constant<int, 512>());
+  if (r.vpt == 2) return f(integral_constant<int, 2>(), integral_constant<int, 1024>());
+  if (r.threads <= 256) return f(integral_constant<int, 4>(), integral_constant<int, 256>());
+  return f(integral_constant<int, 4>(), integral_constant<int, 1024>());
 }
 
 }  // namespace
@@ -334,33 +509,37 @@ extern "C" int lstm_approx_rms_norm(int dtype, int group, const void* x, long lo
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "a negative pitch, or a pointer not aligned to its type");
   if (int rc = op_check_device(msg, msg_len)) return rc;
   if (rows == 0) return LSTM_APPROX_OK;
-  NormArgs a{x, x_pitch, residual, residual_pitch, weight, eps, rows, D, out, scales, group, 0, sum_out, rstd};
+  NormArgs a{x, x_pitch, residual, residual_pitch, weight, eps, rows, D, out, scales, group, 0, sum_out, rstd, false};
   a.n_groups = group > 0 ? (group >= D ? 1 : (D + group - 1) / group) : 0;
-  const bool vec = D % 8 == 0 && op_aligned(x, 16) && op_aligned(residual, 16) && op_aligned(weight, 16) &&
-                   op_aligned(sum_out, 16) && op_aligned(out, group > 0 ? 8 : 16) && x_pitch * es % 16 == 0 &&
-                   (!residual || residual_pitch * es % 16 == 0);
-  const RowShape r = row_shape(D);
+  int unit = unit_of(D, es, {{x, x_pitch}, {residual, residual_pitch}, {sum_out, D}, {group > 0 ? nullptr : out, D}});
+  if (unit == 8 && group > 0 && !op_aligned(out, 8)) unit = 1;
+  a.weight_vec = op_aligned(weight, 16);
+  const RowShape r = row_shape(D, unit == 8 && es == 2);
   const dim3 grid((unsigned)((rows + r.rows_per_block - 1) / r.rows_per_block)), block(r.threads, r.rows_per_block);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = op_for_type(dtype, [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
-    auto at = [&](auto vpt) {
-      constexpr int V = decltype(vpt)::value;
-      auto k = vec ? (group > 0 ? rms_norm_kernel<T, V, true, true> : rms_norm_kernel<T, V, true, false>)
-                   : (group > 0 ? rms_norm_kernel<T, V, false, true> : rms_norm_kernel<T, V, false, false>);
-      return op_launch(k, grid, block, 0, s, a);
-    };
-    if (r.vpt == 1) return at(std::integral_constant<int, 1>());
-    if (r.vpt == 2) return at(std::integral_constant<int, 2>());
-    return at(std::integral_constant<int, 4>());
+    return with_shape(r, [&](auto vpt, auto most) {
+      constexpr int V = decltype(vpt)::value, M = decltype(most)::value;
+      if constexpr (sizeof(T) == 2)
+        if (unit == 2)
+          return op_launch(group > 0 ? rms_norm_kernel<T, V, M, 2, true> : rms_norm_kernel<T, V, M, 2, false>, grid, block,
+                           0, s, a);
+      if (unit == 8)
+        return op_launch(group > 0 ? rms_norm_kernel<T, V, M, 8, true> : rms_norm_kernel<T, V, M, 8, false>, grid, block, 0,
+                         s, a);
+      return op_launch(group > 0 ? rms_norm_kernel<T, V, M, 1, true> : rms_norm_kernel<T, V, M, 1, false>, grid, block, 0, s,
+                       a);
+    });
   });
   return op_launched(e, "norm launch", msg, msg_len);
 }
 
 extern "C" size_t lstm_approx_rms_norm_workspace_bytes(long long rows, int D) {
   if (rows < 0 || rows > 0x7fffffffll || D < 1 || D > kMaxD) return 0;
-  const RowShape r = row_shape(D);
-  return ((size_t)backward_blocks(rows, r) * r.rows_per_block * D * sizeof(float) + 15) / 16 * 16 + 16;
+  size_t parts = 0;  // of either shape
+  for (const bool wide : {false, true}) parts = std::max(parts, (size_t)backward_blocks(rows, backward_shape(D, wide)));
+  return parts * pitch_of_partial(D) * sizeof(float) + 16;
 }
 
 extern "C" int lstm_approx_rms_norm_backward(int dtype, const void* dy, long long dy_pitch, const void* s,
@@ -383,30 +562,29 @@ extern "C" int lstm_approx_rms_norm_backward(int dtype, const void* dy, long lon
   if (dweight && (!workspace || !op_aligned(workspace, 16) || workspace_bytes < need))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "dweight needs a 16-byte aligned workspace of %zu bytes", need);
   if (int rc = op_check_device(msg, msg_len)) return rc;
-  const RowShape r = row_shape(D);
+  const int unit = unit_of(D, es, {{dy, dy_pitch}, {s, s_pitch}, {dsum, dsum_pitch}, {dx, D}});
+  const RowShape r = backward_shape(D, unit == 8 && es == 2);
   const int blocks = backward_blocks(rows, r);
+  const size_t smem = r.rows_per_block > 1 ? (size_t)r.rows_per_block * pitch_of_partial(D) * sizeof(float) : 0;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (rows > 0) {
     NormBackwardArgs a{dy, dy_pitch, s, s_pitch, weight, rstd, dsum, dsum_pitch, rows, D, dx,
-                       dweight ? static_cast<float*>(workspace) : nullptr};
-    const bool vec = D % 8 == 0 && op_aligned(dy, 16) && op_aligned(s, 16) && op_aligned(dsum, 16) &&
-                     op_aligned(dx, 16) && op_aligned(weight, 16) && dy_pitch * es % 16 == 0 &&
-                     s_pitch * es % 16 == 0 && (!dsum || dsum_pitch * es % 16 == 0);
+                       dweight ? static_cast<float*>(workspace) : nullptr, op_aligned(weight, 16)};
     const cudaError_t e = op_for_type(dtype, [&](auto* t) {
       using T = std::remove_pointer_t<decltype(t)>;
-      auto at = [&](auto vpt) {
-        constexpr int V = decltype(vpt)::value;
-        return op_launch(vec ? rms_norm_backward_kernel<T, V, true> : rms_norm_backward_kernel<T, V, false>,
-                         dim3(blocks), dim3(r.threads, r.rows_per_block), 0, st, a);
-      };
-      if (r.vpt == 1) return at(std::integral_constant<int, 1>());
-      if (r.vpt == 2) return at(std::integral_constant<int, 2>());
-      return at(std::integral_constant<int, 4>());
+      return with_shape(r, [&](auto vpt, auto most) {
+        constexpr int V = decltype(vpt)::value, M = decltype(most)::value;
+        const dim3 block(r.threads, r.rows_per_block);
+        if constexpr (sizeof(T) == 2)
+          if (unit == 2) return op_launch(rms_norm_backward_kernel<T, V, M, 2>, dim3(blocks), block, smem, st, a);
+        return op_launch(unit == 8 ? rms_norm_backward_kernel<T, V, M, 8> : rms_norm_backward_kernel<T, V, M, 1>, dim3(blocks),
+                         block, smem, st, a);
+      });
     });
     if (int rc = op_launched(e, "norm backward launch", msg, msg_len)) return rc;
   }
   if (!dweight) return LSTM_APPROX_OK;
   const cudaError_t e = op_launch(column_sum_kernel, dim3((D + 31) / 32), dim3(32, 32), 0, st,
-                                  static_cast<const float*>(workspace), blocks * r.rows_per_block, D, dweight);
+                                  static_cast<const float*>(workspace), blocks, D, dweight);
   return op_launched(e, "weight gradient launch", msg, msg_len);
 }
