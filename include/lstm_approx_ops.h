@@ -227,13 +227,18 @@ int lstm_approx_w4_quantize(int dtype, const void *w, long long w_pitch, int N, 
  *             outputs of lstm_approx_rms_norm); else NULL (x_group is ignored)
  *   bias      [N] fp32, or NULL
  *   y         [M][N] y_dtype (FP32, BF16 or FP16), contiguous
- * Products are exact where x has 16 or 8 bits; sums are held in 32 bits.
+ *   workspace at least lstm_approx_w4_workspace_bytes(x_dtype, M, K) bytes,
+ *             16-byte aligned, not shared by calls in flight; NULL where that
+ *             is 0
+ * Products are exact; sums are held in 32 bits.
  */
 int lstm_approx_w4_matvec(int x_dtype, const void *x, long long x_pitch, const float *x_scale,
                           int x_group, const unsigned char *q, long long q_pitch, const void *scale,
                           int scale_dtype, const unsigned char *zero, const float *bias, int M, int N,
-                          int K, int group, void *y, int y_dtype, void *cuda_stream, char *msg,
-                          int msg_len);
+                          int K, int group, void *y, int y_dtype, void *workspace,
+                          size_t workspace_bytes, void *cuda_stream, char *msg, int msg_len);
+/* Workspace bytes of the call above (0: none, or invalid sizes). */
+size_t lstm_approx_w4_workspace_bytes(int x_dtype, int M, int K);
 
 #ifdef __cplusplus
 }

@@ -42,7 +42,7 @@ EXPORTS = (
     "lstm_approx_dense_set_launch_order", "lstm_approx_rms_norm", "lstm_approx_rms_norm_backward",
     "lstm_approx_rms_norm_workspace_bytes", "lstm_approx_gated_scan", "lstm_approx_gated_scan_backward",
     "lstm_approx_gated_scan_workspace_bytes", "lstm_approx_gated_step", "lstm_approx_w4_quantize",
-    "lstm_approx_w4_matvec",
+    "lstm_approx_w4_matvec", "lstm_approx_w4_workspace_bytes",
 )
 
 _lib = None
@@ -97,7 +97,8 @@ def load(path: str = LIB_PATH):
     lib.lstm_approx_gated_scan_workspace_bytes.argtypes = [I, I, I]
     lib.lstm_approx_gated_step.argtypes = [I, P, LL, P, LL, P, LL, P, F, P, I, P, P, I, I, P] + end
     lib.lstm_approx_w4_quantize.argtypes = [I, P, LL, I, I, I, P, LL, P, I, P] + end
-    lib.lstm_approx_w4_matvec.argtypes = [I, P, LL, P, I, P, LL, P, I, P, P, I, I, I, I, P, I] + end
+    lib.lstm_approx_w4_matvec.argtypes = [I, P, LL, P, I, P, LL, P, I, P, P, I, I, I, I, P, I, P, Z] + end
+    lib.lstm_approx_w4_workspace_bytes.argtypes = [I, I, I]
     for name in EXPORTS:
         if name.endswith("_workspace_bytes"):
             getattr(lib, name).restype = ctypes.c_size_t

@@ -170,7 +170,7 @@ def w4_quantize(w, group: int = 128, *, scale_dtype=torch.float16, stream=None) 
     return run(w) if stream is None else _on(stream, run, w)
 
 
-def w4_matvec(x, w: W4Weight, *, x_scale=None, bias=None, out=None, out_dtype=None, stream=None):
+def w4_matvec(x, w: W4Weight, *, x_scale=None, bias=None, out=None, out_dtype=None, workspace=None, stream=None):
     """y = x W^T (+ bias) for x [..., K] (a few rows) and a 4-bit matrix W [N, K].
 
     x: fp32, bf16, fp16, or float8_e4m3fn with x_scale [..., ceil(K / 128)] or
@@ -179,5 +179,5 @@ def w4_matvec(x, w: W4Weight, *, x_scale=None, bias=None, out=None, out_dtype=No
     """
     code = -1 if out_dtype is None else _CODES.get(out_dtype, -2)
     _need(code > -2, "out_dtype must be float32, bfloat16 or float16")
-    args = (x, w.q, w.scale, w.zero, w.K, w.group, w.pitch, x_scale, bias, out, code)
+    args = (x, w.q, w.scale, w.zero, w.K, w.group, w.pitch, x_scale, bias, out, code, workspace)
     return _ops.w4_matvec(*args) if stream is None else _on(stream, _ops.w4_matvec, *args)

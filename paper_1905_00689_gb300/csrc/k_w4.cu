@@ -10,8 +10,8 @@
 // shared memory or tensor memory, to which 4-bit weights would first have to be
 // expanded, four bytes written for each byte read.
 //
-//   W   A block of 16 rows by 128 k (1 KB, 64 bytes to a row) comes into shared
-//       memory by asynchronous copies, kDepth blocks in flight to a warp.  Four
+//   W   A block of 16 rows by 128 k (64 bytes to a row) comes into shared memory
+//       by asynchronous copies.  Four
 //       lanes share a row; a lane's 32-bit word holds 8 k as 4 pairs of 16-bit
 //       integers after one AND-OR each, (0, 4) (1, 5) (2, 6) (3, 7): or-ed into
 //       the mantissa of 128 (bf16) or 1024 (fp16), from which 128 + zero or 1024
@@ -26,9 +26,10 @@
 //       scale, is added to the row's.
 //
 // The tiles of 16 or 32 rows are dealt out evenly over one block of threads per
-// SM, and a block's warps take equal stretches of its tiles' blocks in a line,
-// whatever the numbers; a tile that several warps have parts of is added up
-// through shared memory at the end, always in the same order.
+// SM; a block has one warp at least to each of its tiles, and as many more as
+// divide evenly, which share the tile's K and add up through shared memory at
+// the end, always in the same order.  A warp goes on by sets of 4 groups
+// (unrolled), whose weights are copied and whose scales are asked for ahead.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -63,9 +64,11 @@ struct W4Args {
   int M, N, K, groups;
   void* y;
   int y_dtype;
-  bool x_vec;  // 8 values of x lie in aligned accesses
+  bool x_vec;    // 8 values of x lie in aligned accesses
+  bool set_vec;  // so do the scales (of 16 bits) and zero points of 4 groups
   int tokens;  // rows of x at a time
-  int depth;   // blocks in flight or in use to a warp: 4 or 8
+  int depth;   // sets in flight or in use to a warp: 2 to 4
+  const unsigned char* x_laid;  // x laid out by the kernel before, or null
   int tiles_each, tiles_more;  // tiles of kMt * 16 rows to a block of threads, and how many blocks have one more
 };
 
@@ -210,6 +213,22 @@ __device__ __forceinline__ void place_chunk(const Chunk<kX>& v, uint4* to) {
 template <int kX>
 constexpr int kParts = kX == LSTM_APPROX_OP_FP32 ? 3 : 1;
 
+// x in the order of the product's shared memory, `tokens` rows at a time one after another: [rows / tokens][blocks][4]
+// [columns][4] x 16 bytes.  A thread takes 8 k of one row.
+template <int kX, int kSubs>
+__global__ void __launch_bounds__(256) w4_lay_out_kernel(const W4Args a, uint4* to) {
+  griddep_launch_dependents();
+  const int blocks = (a.K + kBlockK - 1) / kBlockK, chunks = blocks * 16;
+  const long long item = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  if (item >= (long long)a.M * chunks) return;
+  const int row = (int)(item / chunks), chunk = (int)(item % chunks);
+  const int m0 = row / a.tokens * a.tokens, cols = min(a.tokens, a.M - m0) * kParts<kX>;
+  int slot, lane_t;
+  place<kSubs>(chunk >> 2 & 3, chunk & 3, slot, lane_t);
+  uint4* at = to + (long long)m0 * kParts<kX> * blocks * 16 + (((chunk >> 4) * 4 + slot) * cols + (row - m0) * kParts<kX>) * 4 + lane_t;
+  place_chunk<kX>(load_chunk<kX>(a, row, chunk * 8), at);
+}
+
 // Where the w-th of equal stretches (or one longer) begins, each `each` long and the first `more` of them one longer.
 __device__ __forceinline__ int stretch(int w, int each, int more) { return w * each + min(w, more); }
 
@@ -221,21 +240,21 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
   constexpr int kP = kParts<kX>;
   constexpr int kRed = kNt * 8 + 1;         // pitch of the sums
   constexpr int kSum = kMt * 16 * kRed;     // a tile's sums
-  constexpr int kSets = 4 / kSubs;          // groups of a block
+  constexpr int kSets = 4 / kSubs;          // groups of a block; a set is kSubs blocks
+  constexpr int kRow = kSubs * 64;          // bytes of a row of a set
+  constexpr int kStage = kMt * 16 * kRow;   // of a set
   extern __shared__ __align__(128) unsigned char memory[];
   const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int blocks = (a.K + kBlockK - 1) / kBlockK;
+  const int blocks = (a.K + kBlockK - 1) / kBlockK, sets = (blocks + kSubs - 1) / kSubs;
   const int m0 = blockIdx.y * a.tokens, tokens = min(a.tokens, a.M - m0), cols = tokens * kP;
-  // x [blocks][4][cols][4] x 16 bytes, scales of x [blocks][kNt * 8], ring [warps][depth][kMt][16][64 bytes], in whose
-  // place the sums [warps][2][kMt * 16][kRed] go at the end
+  // x [blocks][4][cols][4] x 16 bytes, scales of x [blocks][kNt * 8], ring [warps][depth][kMt * 16][kRow], in whose
+  // place the sums [warps][kMt * 16][kRed] go at the end
   uint4* xs = reinterpret_cast<uint4*>(memory);
   float* x_scales = reinterpret_cast<float*>(xs + blocks * 16 * cols);
   unsigned char* rings = reinterpret_cast<unsigned char*>(x_scales + (kScaled ? blocks * kNt * 8 : 0));
-  unsigned char* ring = rings + warp * a.depth * kMt * 1024;
-  const int stage_bytes = kMt * 1024, ring_bytes = a.depth * stage_bytes;
+  const int ring_bytes = a.depth * kStage;
+  unsigned char* ring = rings + warp * ring_bytes;
 
-  // this block's tiles, at most one to a warp at a time (so that a warp's stretch meets two tiles at most)
-  const int last_tile = stretch(blockIdx.x + 1, a.tiles_each, a.tiles_more);
   // x: items of 8 k of up to kAtOnce rows; a thread's first is asked for before the copies of W that would delay it
   constexpr int kAtOnce = 16 / Chunk<kX>::kWords;
   const int chunks = blocks * 16, items = chunks * ((tokens + kAtOnce - 1) / kAtOnce);
@@ -255,102 +274,114 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
     for (int e = 0; e < kAtOnce; ++e)
       if (token + e < tokens) place_chunk<kX>(from[e], to + e * kP * 4);
   };
-  if ((int)threadIdx.x < items) load_item(threadIdx.x, v);
-  bool staged = false;
+  if (!a.x_laid && (int)threadIdx.x < items) load_item(threadIdx.x, v);
+  __shared__ __align__(8) uint64_t x_bar;
+  if (a.x_laid && threadIdx.x == 0) {
+    mbar_init(smem_u32(&x_bar), 1);
+    fence_mbarrier_init_cluster();
+  }
+
+  // this block's tiles, at most one to a warp at a time
+  const int last_tile = stretch(blockIdx.x + 1, a.tiles_each, a.tiles_more);
+  bool staged = false, x_there = true;
   for (int tile0 = stretch(blockIdx.x, a.tiles_each, a.tiles_more); tile0 < last_tile; tile0 += warps) {
-    const int tiles = min(warps, last_tile - tile0), n = tiles * blocks;  // of this turn
-    const int each = n / warps, more = n - each * warps;
-    const int begin = stretch(warp, each, more), count = stretch(warp + 1, each, more) - begin;
+    const int tiles = min(warps, last_tile - tile0), share = warps / tiles;  // warps to a tile
+    const int my_tile = warp / share, part_k = warp - my_tile * share;
+    const int begin = part_k * sets / share, end = my_tile < tiles ? (part_k + 1) * sets / share : 0;  // my sets
 
     // the copies
-    const int begin_tile = begin / blocks, begin_block = begin - begin_tile * blocks;
-    int to_tile = tile0 + begin_tile, to_block = begin_block, to_left = count;
+    int to_set = begin;
     const uint8_t* from[2 * kMt];
-    auto rows_of = [&](int tile) {
+    long long set_at[2 * kMt];  // of the scales and zero points of the set that is asked for next
 #pragma unroll
-      for (int q = 0; q < 2 * kMt; ++q)
-        from[q] = a.q + (long long)min(tile * kMt * 16 + q * 8 + g, a.N - 1) * a.q_pitch + t * 16;
-    };
-    rows_of(to_tile);
-#pragma unroll
-    for (int q = 0; q < 2 * kMt; ++q) from[q] += to_block * 64;
-    // sub-block t of row r at place t ^ (r / 2 % 4): no two lanes of a read below meet in a bank
-    const uint32_t to_first = smem_u32(ring) + g * 64 + ((t ^ (g >> 1)) << 4);
+    for (int q = 0; q < 2 * kMt; ++q) {
+      const int n = min((tile0 + my_tile) * kMt * 16 + q * 8 + g, a.N - 1);
+      from[q] = a.q + n * a.q_pitch + begin * kRow + t * 16;
+      set_at[q] = (long long)n * a.groups + begin * 4;
+    }
+    // 16-byte piece c of row r goes to place c ^ swizzle(r): no two lanes of a read below meet in a bank
+    const int swizzle = kSubs == 4 ? (g & 1) << 2 : (kSubs == 2 ? (g & 3) << 1 : g >> 1);
+    const uint32_t to_first = smem_u32(ring) + g * kRow;
     uint32_t to_stage = to_first;
     auto fetch = [&]() {
-      if (to_left > 0) {
-        --to_left;
-        if (to_block * kBlockK + t * 32 < a.K) {  // (else the x to it is zero, and any word a finite number)
+      if (to_set < end) {
+        const bool whole = (to_set + 1) * kSubs * kBlockK <= a.K;
 #pragma unroll
-          for (int q = 0; q < 2 * kMt; ++q)  // 8 rows of 64 bytes at a time
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to_stage + q * 512), "l"(from[q]) : "memory");
+        for (int i = 0; i < kSubs; ++i) {
+          // (where x is zero any word will do, a finite number)
+          if (whole || (to_set * kSubs + i) * kBlockK + t * 32 < a.K) {
+#pragma unroll
+            for (int q = 0; q < 2 * kMt; ++q)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to_stage + q * 8 * kRow +
+                                                                             (((i * 4 + t) ^ swizzle) << 4)),
+                           "l"(from[q] + i * 64)
+                           : "memory");
+          }
         }
 #pragma unroll
-        for (int q = 0; q < 2 * kMt; ++q) from[q] += 64;
-        if (++to_block == blocks) {
-          to_block = 0;
-          rows_of(++to_tile);
-        }
+        for (int q = 0; q < 2 * kMt; ++q) from[q] += kRow;
+        ++to_set;
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
-      to_stage += stage_bytes;
+      to_stage += kStage;
       if (to_stage == to_first + ring_bytes) to_stage = to_first;
     };
     for (int d = 0; d < a.depth - 1; ++d) fetch();
 
-    // scales and zero points: a lane takes one group's of the next kSubs blocks, for rows g and g + 8 of each 16
+    // Scales (16 bits) and zero points of a set, for rows g and g + 8 of each 16; 32-bit scales are read where they are
+    // used.
     struct Set {
-      uint32_t s[2 * kMt];  // as stored
-      unsigned z[2 * kMt];
+      uint32_t s[2 * kMt][2], z[2 * kMt];
     };
-    int set_tile = tile0 + begin_tile, set_group = begin_block * kSets + t;
-    long long set_at[2 * kMt];
-    auto begin_set = [&]() {
-#pragma unroll
-      for (int q = 0; q < 2 * kMt; ++q)
-        set_at[q] = (long long)min(set_tile * kMt * 16 + q * 8 + g, a.N - 1) * a.groups + set_group;
-    };
-    begin_set();
+    const bool wide = a.scale_dtype == LSTM_APPROX_OP_FP32;
+    int set_group = begin * 4;
     auto load_set = [&]() {
-      Set v;
+      Set r;
 #pragma unroll
-      for (int q = 0; q < 2 * kMt; ++q) v.s[q] = 0u, v.z[q] = 8u;
-      if (set_group < a.groups) {
-        if (a.scale_dtype == LSTM_APPROX_OP_FP32) {
-#pragma unroll
-          for (int q = 0; q < 2 * kMt; ++q) v.s[q] = static_cast<const uint32_t*>(a.scale)[set_at[q]];
+      for (int q = 0; q < 2 * kMt; ++q) {
+        r.s[q][0] = r.s[q][1] = 0u;
+        r.z[q] = 0x08080808u;
+        if (a.set_vec) {
+          if (set_group < a.groups) {
+            const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.scale) + set_at[q]);
+            r.s[q][0] = w.x;
+            r.s[q][1] = w.y;
+            if (a.zero) r.z[q] = *reinterpret_cast<const uint32_t*>(a.zero + set_at[q]);
+          }
         } else {
+          if (a.zero) r.z[q] = 0u;
 #pragma unroll
-          for (int q = 0; q < 2 * kMt; ++q) v.s[q] = static_cast<const uint16_t*>(a.scale)[set_at[q]];
+          for (int e = 0; e < 4; ++e) {
+            if (set_group + e >= a.groups) continue;
+            if (!wide) r.s[q][e / 2] |= (uint32_t) static_cast<const uint16_t*>(a.scale)[set_at[q] + e] << 16 * (e & 1);
+            if (a.zero) r.z[q] |= (uint32_t)a.zero[set_at[q] + e] << 8 * e;
+          }
         }
-        if (a.zero) {
-#pragma unroll
-          for (int q = 0; q < 2 * kMt; ++q) v.z[q] = a.zero[set_at[q]];
-        }
+        set_at[q] += 4;
       }
       set_group += 4;
-#pragma unroll
-      for (int q = 0; q < 2 * kMt; ++q) set_at[q] += 4;
-      if (set_group - t >= blocks * kSets) {
-        set_group = t;
-        ++set_tile;
-        begin_set();
-      }
-      return v;
-    };
-    auto scale_of = [&](uint32_t v) {
-      if (a.scale_dtype == LSTM_APPROX_OP_FP16) return __half2float(__ushort_as_half((unsigned short)v));
-      return __uint_as_float(a.scale_dtype == LSTM_APPROX_OP_BF16 ? v << 16 : v);
+      return r;
     };
     Set next = load_set();
 
     if (!staged) {
-      int item = threadIdx.x;
-      while (item < items) {
-        const int now = item;
-        item += blockDim.x;
-        place_item(now, v);
-        if (item < items) load_item(item, v);
+      if (a.x_laid) {
+        // the kernel before has laid it out (and what came before that one has been complete since it started)
+        griddep_wait();
+        if (threadIdx.x == 0) {
+          const uint32_t bytes = (uint32_t)blocks * 256 * cols, bar = smem_u32(&x_bar);
+          const unsigned char* from_x = a.x_laid + (long long)m0 * kP * blocks * 256;
+          mbar_arrive_expect_tx(bar, bytes);
+          for (uint32_t at = 0; at < bytes; at += 32768) bulk_copy_g2s(smem_u32(xs) + at, from_x + at, min(32768u, bytes - at), bar);
+        }
+      } else {
+        int item = threadIdx.x;
+        while (item < items) {
+          const int now = item;
+          item += blockDim.x;
+          place_item(now, v);
+          if (item < items) load_item(item, v);
+        }
       }
       if constexpr (kScaled) {
         for (int c = threadIdx.x; c < blocks * kNt * 8; c += blockDim.x) {
@@ -361,167 +392,155 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
       }
       staged = true;
       __syncthreads();
+      if (a.x_laid) {
+        const int never = 0;
+        x_there = mbar_wait_bounded<false>(smem_u32(&x_bar), 0, 2000000000ull, &never);
+      }
     }
 
     float acc[kMt][kNt][4] = {};
-    float kept[kMt][kNt][4];  // of the first of two tiles
-    float now_s[2 * kMt];
-    unsigned now_z[2 * kMt];
-    int block = begin_block, in_set = 0, here = 0;
-    bool second = false;
+    const unsigned char* here = ring + g * kRow;
+    const unsigned char* const ring_end = here + ring_bytes;
     // a lane whose column of x^T does not exist takes the last one's values; what they lead to is not stored
     const uint4* xs_here[kNt];
 #pragma unroll
-    for (int c = 0; c < kNt; ++c) xs_here[c] = xs + (block * 4 * cols + min(c * 8 + g, cols - 1)) * 4 + t;
-    for (int p = 0; p < count; ++p) {
-      if (in_set == 0) {
-#pragma unroll
-        for (int q = 0; q < 2 * kMt; ++q) {
-          now_s[q] = scale_of(next.s[q]);
-          now_z[q] = (kBf16 ? 0x43004300u : 0x64006400u) + (next.z[q] & 15u) * 0x00010001u;
-        }
-        next = load_set();
-      }
-      if (a.depth == 4) asm volatile("cp.async.wait_group 2;" ::: "memory");
-      else asm volatile("cp.async.wait_group 6;" ::: "memory");
+    for (int c = 0; c < kNt; ++c) xs_here[c] = xs + (begin * kSubs * 4 * cols + min(c * 8 + g, cols - 1)) * 4 + t;
+    const int xs_step = cols * 4;
+    for (int set = begin; set < end; ++set) {
+      const Set held = next;
+      if (a.depth == 2) asm volatile("cp.async.wait_group 0;" ::: "memory");
+      else if (a.depth == 3) asm volatile("cp.async.wait_group 1;" ::: "memory");
+      else asm volatile("cp.async.wait_group 2;" ::: "memory");
       __syncwarp();
       fetch();
-      float xsc[kNt][2];
-      if constexpr (kScaled) {
+      next = load_set();
 #pragma unroll
-        for (int c = 0; c < kNt; ++c) {
-          const float2 v = *reinterpret_cast<const float2*>(x_scales + block * kNt * 8 + c * 8 + 2 * t);
-          xsc[c][0] = v.x;
-          xsc[c][1] = v.y;
-        }
-      }
+      for (int i = 0; i < kSubs; ++i) {  // blocks of the set
+        const int block = set * kSubs + i;
+        if (i > 0 && block >= blocks) break;
+        float xsc[kNt][2];
+        float sum[kMt][kNt][4];  // of the block, where x has a scale for each
+        if constexpr (kScaled) {
 #pragma unroll
-      for (int set = 0; set < kSets; ++set) {  // groups of the block
-        const int from_lane = (lane & ~3) | (in_set * kSets + set);
-        float s[2 * kMt];
-        Zero<kBf16> z[2 * kMt];
-#pragma unroll
-        for (int q = 0; q < 2 * kMt; ++q) {
-          s[q] = __shfl_sync(0xffffffffu, now_s[q], from_lane);
-          z[q] = zero_of<kBf16>(__shfl_sync(0xffffffffu, now_z[q], from_lane));
-        }
-        uint4 b[kSubs][kNt];
-#pragma unroll
-        for (int i = 0; i < kSubs; ++i) {
-#pragma unroll
-          for (int c = 0; c < kNt; ++c) b[i][c] = xs_here[c][(set * kSubs + i) * cols * 4];
+          for (int c = 0; c < kNt; ++c) {
+            const float2 f = *reinterpret_cast<const float2*>(x_scales + block * kNt * 8 + c * 8 + 2 * t);
+            xsc[c][0] = f.x;
+            xsc[c][1] = f.y;
+          }
         }
 #pragma unroll
-        for (int m = 0; m < kMt; ++m) {
-          // the lane's kSubs words of rows g and g + 8
-          uint32_t w[2][kSubs];
+        for (int h = 0; h < kSets; ++h) {  // groups of the block
+          const int e = i * kSets + h;
+          uint4 b[kSubs][kNt];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const unsigned char* row = ring + here + (m * 16 + h * 8 + g) * 64;
-            const int swz = g >> 1;
-            if constexpr (kSubs == 4) {
-              const uint4 v = *reinterpret_cast<const uint4*>(row + ((t ^ swz) << 4));
-              w[h][0] = v.x, w[h][1] = v.y, w[h][2] = v.z, w[h][3] = v.w;
-            } else if constexpr (kSubs == 2) {
-              const uint2 v = *reinterpret_cast<const uint2*>(row + (((2 * set + (t & 1)) ^ swz) << 4) + (t >> 1) * 8);
-              w[h][0] = v.x, w[h][1] = v.y;
-            } else {
-              w[h][0] = *reinterpret_cast<const uint32_t*>(row + ((set ^ swz) << 4) + t * 4);
+          for (int k = 0; k < kSubs; ++k) {
+#pragma unroll
+            for (int c = 0; c < kNt; ++c) {
+              b[k][c] = *xs_here[c];
+              xs_here[c] += xs_step;
             }
           }
-          float part[kNt][4];
+          float s[2 * kMt];
+          Zero<kBf16> z[2 * kMt];
+          uint32_t w[2 * kMt][kSubs];  // the lane's words of rows g and g + 8 of each 16
 #pragma unroll
-          for (int i = 0; i < kSubs; ++i) {
+          for (int q = 0; q < 2 * kMt; ++q) {
+            const uint32_t bits = held.s[q][e / 2] >> 16 * (e & 1);
+            if (wide) s[q] = set * 4 + e < a.groups ? static_cast<const float*>(a.scale)[set_at[q] - 8 + e] : 0.0f;
+            else s[q] = a.scale_dtype == LSTM_APPROX_OP_BF16 ? __uint_as_float(bits << 16)
+                                                             : __half2float(__ushort_as_half((unsigned short)bits));
+            z[q] = zero_of<kBf16>((kBf16 ? 0x43004300u : 0x64006400u) + (held.z[q] >> 8 * e & 15u) * 0x00010001u);
+            const unsigned char* row = here + q * 8 * kRow;
+            if constexpr (kSubs == 4) {
+              const uint4 u = *reinterpret_cast<const uint4*>(row + (((i * 4 + t) ^ swizzle) << 4));
+              w[q][0] = u.x, w[q][1] = u.y, w[q][2] = u.z, w[q][3] = u.w;
+            } else if constexpr (kSubs == 2) {
+              const uint2 u =
+                  *reinterpret_cast<const uint2*>(row + (((i * 4 + 2 * h + (t & 1)) ^ swizzle) << 4) + (t >> 1) * 8);
+              w[q][0] = u.x, w[q][1] = u.y;
+            } else {
+              w[q][0] = *reinterpret_cast<const uint32_t*>(row + ((h ^ swizzle) << 4) + t * 4);
+            }
+          }
+          float part[kMt][kNt][4];  // (the MMAs of one step belong to different sums)
+#pragma unroll
+          for (int k = 0; k < kSubs; ++k) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-              uint32_t a0, a1, a2, a3;
-              nibbles<kBf16>(w[0][i] >> (8 * half), z[2 * m], a0, a2);
-              nibbles<kBf16>(w[1][i] >> (8 * half), z[2 * m + 1], a1, a3);
 #pragma unroll
-              for (int c = 0; c < kNt; ++c) {
-                const uint32_t b0 = half ? b[i][c].z : b[i][c].x, b1 = half ? b[i][c].w : b[i][c].y;
-                if (i == 0 && half == 0) {
-                  if constexpr (kBf16) mma_16816_bf16<true, true>(part[c], a0, a1, a2, a3, b0, b1);
-                  else mma_16816_f16<true, true>(part[c], a0, a1, a2, a3, b0, b1);
-                } else {
-                  if constexpr (kBf16) mma_16816_bf16<true, false>(part[c], a0, a1, a2, a3, b0, b1);
-                  else mma_16816_f16<true, false>(part[c], a0, a1, a2, a3, b0, b1);
+              for (int m = 0; m < kMt; ++m) {
+                uint32_t a0, a1, a2, a3;
+                nibbles<kBf16>(w[2 * m][k] >> (8 * half), z[2 * m], a0, a2);
+                nibbles<kBf16>(w[2 * m + 1][k] >> (8 * half), z[2 * m + 1], a1, a3);
+#pragma unroll
+                for (int c = 0; c < kNt; ++c) {
+                  const uint32_t b0 = half ? b[k][c].z : b[k][c].x, b1 = half ? b[k][c].w : b[k][c].y;
+                  if (k == 0 && half == 0) {
+                    if constexpr (kBf16) mma_16816_bf16<true, true>(part[m][c], a0, a1, a2, a3, b0, b1);
+                    else mma_16816_f16<true, true>(part[m][c], a0, a1, a2, a3, b0, b1);
+                  } else {
+                    if constexpr (kBf16) mma_16816_bf16<true, false>(part[m][c], a0, a1, a2, a3, b0, b1);
+                    else mma_16816_f16<true, false>(part[m][c], a0, a1, a2, a3, b0, b1);
+                  }
                 }
               }
             }
           }
 #pragma unroll
-          for (int c = 0; c < kNt; ++c) {
+          for (int m = 0; m < kMt; ++m) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float v = kScaled ? part[c][e] * xsc[c][e & 1] : part[c][e];
-              acc[m][c][e] = fmaf(v, s[2 * m + (e >> 1)], acc[m][c][e]);
+            for (int c = 0; c < kNt; ++c) {
+#pragma unroll
+              for (int n = 0; n < 4; ++n) {
+                const float scale = s[2 * m + (n >> 1)];
+                if constexpr (kScaled)
+                  sum[m][c][n] = h == 0 ? part[m][c][n] * scale : fmaf(part[m][c][n], scale, sum[m][c][n]);
+                else
+                  acc[m][c][n] = fmaf(part[m][c][n], scale, acc[m][c][n]);
+              }
             }
           }
         }
-      }
-      here = here + stage_bytes == ring_bytes ? 0 : here + stage_bytes;
-      in_set = in_set + 1 == kSubs ? 0 : in_set + 1;
-#pragma unroll
-      for (int c = 0; c < kNt; ++c) xs_here[c] += 16 * cols;
-      if (++block == blocks) {
-        block = in_set = 0;
-#pragma unroll
-        for (int c = 0; c < kNt; ++c) xs_here[c] -= blocks * 16 * cols;
-        if (p + 1 < count) {
-          second = true;
+        if constexpr (kScaled) {
 #pragma unroll
           for (int m = 0; m < kMt; ++m)
 #pragma unroll
             for (int c = 0; c < kNt; ++c)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                kept[m][c][e] = acc[m][c][e];
-                acc[m][c][e] = 0.0f;
-              }
+              for (int n = 0; n < 4; ++n) acc[m][c][n] = fmaf(sum[m][c][n], xsc[c][n & 1], acc[m][c][n]);
         }
       }
+      here += kStage;
+      if (here == ring_end) here -= ring_bytes;
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();  // no ring is in use any more
     float* sums = reinterpret_cast<float*>(rings);
-    auto owner = [&](int position) {  // the warp whose stretch has this block
-      const int longer = more * (each + 1);
-      return position < longer ? position / (each + 1) : more + (position - longer) / max(each, 1);
-    };
-    if (count > 0) {
+    if (my_tile < tiles) {
+      float* to = sums + warp * kSum;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (h == 1 && !second) break;
-        float* to = sums + (2 * warp + h) * kSum;
+      for (int m = 0; m < kMt; ++m)
 #pragma unroll
-        for (int m = 0; m < kMt; ++m)
+        for (int c = 0; c < kNt; ++c)
 #pragma unroll
-          for (int c = 0; c < kNt; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              to[(m * 16 + (e >> 1) * 8 + g) * kRed + c * 8 + 2 * t + (e & 1)] =
-                  h == 0 && second ? kept[m][c][e] : acc[m][c][e];
-      }
+          for (int n = 0; n < 4; ++n) to[(m * 16 + (n >> 1) * 8 + g) * kRed + c * 8 + 2 * t + (n & 1)] = acc[m][c][n];
     }
     __syncthreads();
-    // a warp takes 16 rows, two rows of x at a time; a tile's parts come from the warps whose stretches meet it: the
-    // first's last part and the others' first
+    // a warp takes 16 rows, two rows of x at a time
     for (int sixteen = warp; sixteen < tiles * kMt; sixteen += warps) {
       const int tile = sixteen / kMt, row = sixteen % kMt * 16 + (lane & 15), out = (tile0 + tile) * kMt * 16 + row;
       if (out >= a.N) continue;
-      const int w0 = owner(tile * blocks), w1 = owner((tile + 1) * blocks - 1);
-      const float* part = sums + (2 * w0 + (stretch(w0, each, more) < tile * blocks ? 1 : 0)) * kSum + row * kRed;
-      const float* rest = sums + 2 * (w0 + 1) * kSum + row * kRed;
+      const float* first = sums + tile * share * kSum + row * kRed;
       const float bias = a.bias ? a.bias[out] : 0.0f;
       for (int token = lane >> 4; token < tokens; token += 2) {
-        auto sum_of = [&](const float* p) {
-          if constexpr (kP == 3) return p[0] + (p[1] + p[2]);
-          else return p[0];
-        };
-        float v = sum_of(part + token * kP);
-        for (int w = 0; w < w1 - w0; ++w) v += sum_of(rest + 2 * w * kSum + token * kP);
-        store_any(a.y, (long long)(m0 + token) * a.N + out, a.y_dtype, v + bias);
+        float total = 0.0f;
+        const float* p = first + token * kP;
+        for (int w = 0; w < share; ++w, p += kSum) {
+          if constexpr (kP == 3) total += p[0] + (p[1] + p[2]);
+          else total += p[0];
+        }
+        if (!x_there) total = __builtin_nanf("");
+        store_any(a.y, (long long)(m0 + token) * a.N + out, a.y_dtype, total + bias);
       }
     }
     __syncthreads();  // the rings' place is theirs again
@@ -597,44 +616,67 @@ __global__ void __launch_bounds__(256) w4_quantize_kernel(const W4QuantizeArgs a
 struct W4Plan {
   int tokens;  // rows of x at a time
   int warps;   // of a block of threads
-  int depth;   // blocks of W in flight or in use to a warp
+  int depth;   // sets of W in flight or in use to a warp
   size_t smem;
 };
-constexpr size_t kMostShared = 227 * 1024;
-constexpr int kMaxK = 32768;  // one row of x in 32 bits then fits beside four warps' blocks
+constexpr size_t kMostShared = 227 * 1024 - 1024;  // (and a barrier besides)
+constexpr int kMaxK = 32768;  // one row of x in 32 bits then fits beside four warps' sets
 
-// As many rows of x as leave room for four warps, then as many warps as fit; eight blocks to a warp where 16 warps have
-// room for them, else four.
-inline W4Plan plan_matvec(int M, int K, int parts, int mt, int nt, bool scaled) {
+// As many rows of x as leave room for four warps with two sets each, then as many warps as fit, then as many sets.
+inline W4Plan plan_matvec(int M, int K, int parts, int mt, int nt, int subs, bool scaled) {
   const int blocks = (K + kBlockK - 1) / kBlockK;
-  const size_t sums = 2 * mt * 16 * (nt * 8 + 1) * sizeof(float);
-  auto per_warp = [&](int depth) { return std::max<size_t>(depth * mt * 1024, sums); };
+  const size_t sums = mt * 16 * (nt * 8 + 1) * sizeof(float), stage = mt * 1024 * subs;
   for (W4Plan p{std::min(M, nt * 8 / parts), 0, 0, 0};; --p.tokens) {
     const size_t x = (size_t)blocks * (256 * p.tokens * parts + (scaled ? 32 * nt : 0));
     const size_t left = x < kMostShared ? kMostShared - x : 0;
-    p.depth = left >= kMaxWarps * per_warp(8) ? 8 : 4;
-    p.warps = (int)std::min<size_t>(kMaxWarps, left / per_warp(p.depth));
-    p.smem = x + p.warps * per_warp(p.depth);
-    if (p.warps >= 4 || p.tokens == 1) return p;
+    p.warps = (int)std::min<size_t>(kMaxWarps, left / std::max(2 * stage, sums));
+    if (p.warps < 4 && p.tokens > 1) continue;
+    p.depth = (int)std::min<size_t>(4, left / (std::max(1, p.warps) * stage));
+    p.smem = x + p.warps * std::max(p.depth * stage, sums);
+    return p;
   }
 }
 
+// Bytes of x laid out, where a kernel does it before the product: from 24 KB on, for which each block of threads on its own
+// would need several turns through its caches (16 x 4096 8-bit values: 13 of 38 us); below that the second launch costs
+// more.
+inline size_t laid_out_bytes(int x_dtype, int M, int K) {
+  const size_t bytes = (size_t)M * ((K + kBlockK - 1) / kBlockK) * 256 * (x_dtype == LSTM_APPROX_OP_FP32 ? 3 : 1);
+  return bytes >= 24 * 1024 ? bytes : 0;
+}
+
 template <int kX, int kMt, int kNt, int kSubs>
-cudaError_t launch_matvec(W4Args a, cudaStream_t s) {
+cudaError_t launch_matvec(W4Args a, unsigned char* workspace, cudaStream_t s) {
   static thread_local DeviceSet ready;  // of the one kernel that this instance launches
   auto kern = w4_matvec_kernel<kX, kMt, kNt, kSubs>;
-  const cudaError_t e = once_per_device(
+  cudaError_t e = once_per_device(
       &ready, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostShared); });
   if (e != cudaSuccess) return e;
-  const W4Plan p = plan_matvec(a.M, a.K, kParts<kX>, kMt, kNt, kX == LSTM_APPROX_OP_E4M3);
+  const W4Plan p = plan_matvec(a.M, a.K, kParts<kX>, kMt, kNt, kSubs, kX == LSTM_APPROX_OP_E4M3);
   if (p.warps < 1) return cudaErrorInvalidValue;
   a.tokens = p.tokens;
   a.depth = p.depth;
   const int tiles = (a.N + kMt * 16 - 1) / (kMt * 16), across = std::min(tiles, 152);
   a.tiles_each = tiles / across;
   a.tiles_more = tiles % across;
-  const dim3 grid(across, (a.M + p.tokens - 1) / p.tokens);
-  return op_launch(kern, grid, dim3(p.warps * 32), p.smem, s, a);
+  if (laid_out_bytes(kX, a.M, a.K) > 0) {
+    a.x_laid = workspace;
+    const long long items = (long long)a.M * ((a.K + kBlockK - 1) / kBlockK) * 16;
+    e = op_launch(w4_lay_out_kernel<kX, kSubs>, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, s, a,
+                  reinterpret_cast<uint4*>(workspace));
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(across, (a.M + p.tokens - 1) / p.tokens);
+  cfg.blockDim = dim3(p.warps * 32);
+  cfg.dynamicSmemBytes = p.smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // W is on its way while x is laid out
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.x_laid ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
 int check_matrix(int N, int K, int group, const void* q, long long q_pitch, const void* scale, int scale_dtype,
@@ -678,10 +720,15 @@ extern "C" int lstm_approx_w4_quantize(int dtype, const void* w, long long w_pit
                      "quantiser launch", msg, msg_len);
 }
 
+extern "C" size_t lstm_approx_w4_workspace_bytes(int x_dtype, int M, int K) {
+  return M < 0 || M > 65535 || K < 1 || K > kMaxK ? 0 : laid_out_bytes(x_dtype, M, K);
+}
+
 extern "C" int lstm_approx_w4_matvec(int x_dtype, const void* x, long long x_pitch, const float* x_scale, int x_group,
                                      const unsigned char* q, long long q_pitch, const void* scale, int scale_dtype,
                                      const unsigned char* zero, const float* bias, int M, int N, int K, int group,
-                                     void* y, int y_dtype, void* cuda_stream, char* msg, int msg_len) {
+                                     void* y, int y_dtype, void* workspace, size_t workspace_bytes, void* cuda_stream,
+                                     char* msg, int msg_len) {
   if (msg && msg_len > 0) msg[0] = '\0';
   const bool x8 = x_dtype == LSTM_APPROX_OP_E4M3;
   if ((!op_float_dtype(x_dtype) && !x8) || !op_float_dtype(y_dtype))
@@ -695,21 +742,27 @@ extern "C" int lstm_approx_w4_matvec(int x_dtype, const void* x, long long x_pit
   if (x_pitch < 0 || !op_aligned(x, op_dtype_bytes(x_dtype)) || !op_aligned(x_scale, 4) || !op_aligned(bias, 4) ||
       !op_aligned(y, op_dtype_bytes(y_dtype)))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "a negative pitch, or a pointer not aligned to its type");
+  const size_t need = lstm_approx_w4_workspace_bytes(x_dtype, M, K);
+  if (need > 0 && N > 0 && (!workspace || !op_aligned(workspace, 16) || workspace_bytes < need))
+    return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "needs a 16-byte aligned workspace of %zu bytes", need);
   if (int rc = op_check_device(msg, msg_len)) return rc;
   if (M == 0 || N == 0) return LSTM_APPROX_OK;
   const size_t xs = op_dtype_bytes(x_dtype);
   W4Args a{x_dtype, x, x_pitch, x_scale, x_group >= K || !x8 ? 1 : (K + 127) / 128, q, q_pitch, scale, scale_dtype, zero,
            bias, M, N, K, (K + group - 1) / group, y, y_dtype,
-           op_aligned(x, std::min<size_t>(16, 8 * xs)) && x_pitch * xs % std::min<size_t>(16, 8 * xs) == 0, 0, 0, 0, 0};
+           op_aligned(x, std::min<size_t>(16, 8 * xs)) && x_pitch * xs % std::min<size_t>(16, 8 * xs) == 0,
+           scale_dtype != LSTM_APPROX_OP_FP32 && (K + group - 1) / group % 4 == 0 && op_aligned(scale, 8) && op_aligned(zero, 4),
+           0, 0, nullptr, 0, 0};
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
   auto of_type = [&](auto type) {
     constexpr int kX = decltype(type)::value;
     const int cols = std::min(M, 32) * kParts<kX>;
     auto of_group = [&](auto subs) {
       constexpr int kSubs = decltype(subs)::value;
-      if (cols <= 8) return launch_matvec<kX, 1, 1, kSubs>(a, s);
-      if (cols <= 16) return launch_matvec<kX, 2, 2, kSubs>(a, s);
-      return launch_matvec<kX, 2, 4, kSubs>(a, s);
+      if (cols <= 8) return launch_matvec<kX, 1, 1, kSubs>(a, ws, s);
+      if (cols <= 16) return launch_matvec<kX, 2, 2, kSubs>(a, ws, s);
+      return launch_matvec<kX, 2, 4, kSubs>(a, ws, s);
     };
     if (group == 128) return of_group(std::integral_constant<int, 4>());
     if (group == 64) return of_group(std::integral_constant<int, 2>());

@@ -371,7 +371,7 @@ PyObject* w4_quantize(PyObject*, PyObject* const* a, Py_ssize_t) {
   });
 }
 
-// w4_matvec(x, q, scale, zero, K, group, pitch, x_scale, bias, out, out_dtype) -> out  (out_dtype: an operator code or -1;
+// w4_matvec(x, q, scale, zero, K, group, pitch, x_scale, bias, out, out_dtype, workspace) -> out  (out_dtype: an operator code or -1;
 // q, scale and zero have been checked against one another)
 PyObject* w4_matvec(PyObject*, PyObject* const* a, Py_ssize_t) {
   return guarded([&]() -> PyObject* {
@@ -412,11 +412,14 @@ PyObject* w4_matvec(PyObject*, PyObject* const* a, Py_ssize_t) {
     const int out_code = float_code(out_type);
     need(out_code >= 0, "out must be float32, bfloat16 or float16");
     Tensor out = call.out(a[9], "out", out_type, sizes);
+    std::optional<Tensor> ws;
+    const size_t bytes = lstm_approx_w4_workspace_bytes(code, (int)M, (int)K);
+    if (bytes > 0) ws = call.workspace(a[11], bytes);
     call.done(lstm_approx_w4_matvec(code, px, pitch_of(x, "x"), x_scale, x_group, q.data_ptr<uint8_t>(), integer(a[6]),
                                     scale.data_ptr(), float_code(scale, "scale"),
                                     a[3] == Py_None ? nullptr : tensor(a[3], "zero").data_ptr<uint8_t>(), bias, (int)M,
-                                    (int)N, (int)K, (int)integer(a[5]), out.data_ptr(), out_code, call.stream, call.msg,
-                                    sizeof(call.msg)));
+                                    (int)N, (int)K, (int)integer(a[5]), out.data_ptr(), out_code, ws ? ws->data_ptr() : nullptr,
+                                    ws ? ws->nbytes() : 0, call.stream, call.msg, sizeof(call.msg)));
     return wrap(out);
   });
 }
@@ -439,7 +442,7 @@ PyMethodDef g_methods[] = {
     entry<rms_norm, 9>("rms_norm"),           entry<rms_norm_backward, 8>("rms_norm_backward"),
     entry<gated_scan, 12>("gated_scan"),      entry<gated_scan_backward, 16>("gated_scan_backward"),
     entry<gated_step, 9>("gated_step"),       entry<w4_quantize, 5>("w4_quantize"),
-    entry<w4_matvec, 11>("w4_matvec"),        {nullptr, nullptr, 0, nullptr},
+    entry<w4_matvec, 12>("w4_matvec"),        {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_torch_ops", "The operators on torch tensors (see _operators).", -1,
                         g_methods};

@@ -174,13 +174,13 @@ def test_matvec_other_stream(cuda_device):
 
 
 MATVEC = dict(xd=1, x=64, xp=64, xs=None, xg=0, q=64, qp=32, scale=64, sd=2, zero=64, bias=None, M=2, N=4, K=64, group=32,
-              y=64, yd=1)
+              y=64, yd=1, ws=None, nbytes=0)
 QUANTIZE = dict(d=0, w=64, wp=64, N=4, K=64, group=32, q=64, qp=32, scale=64, sd=2, zero=64)
 BAD = ([(MATVEC, "w4_matvec", b) for b in (
             dict(xd=4), dict(yd=3), dict(xd=-1), dict(x=None), dict(y=None), dict(q=None), dict(scale=None), dict(q=72),
             dict(qp=40), dict(qp=16), dict(group=48), dict(group=256), dict(sd=3), dict(M=-1), dict(N=-1), dict(K=0),
             dict(xs=64), dict(xd=3), dict(xd=3, xs=64, xg=32), dict(x=65), dict(xp=-1), dict(scale=65), dict(bias=66),
-            dict(y=65))]
+            dict(y=65), dict(M=400), dict(M=400, ws=72, nbytes=1 << 30), dict(M=400, ws=64, nbytes=64))]
        + [(QUANTIZE, "w4_quantize", b) for b in (
             dict(d=3), dict(w=None), dict(zero=None), dict(q=None), dict(scale=None), dict(q=68), dict(qp=30),
             dict(qp=16), dict(group=16), dict(sd=-1), dict(K=0), dict(N=-1), dict(w=66), dict(wp=-1))])
