@@ -761,8 +761,8 @@ extern "C" int lstm_approx_w4_matvec(int x_dtype, const void* x, long long x_pit
     auto of_group = [&](auto subs) {
       constexpr int kSubs = decltype(subs)::value;
       if (cols <= 8) return launch_matvec<kX, 1, 1, kSubs>(a, ws, s);
-      if (cols <= 16) return launch_matvec<kX, 2, 2, kSubs>(a, ws, s);
-      return launch_matvec<kX, 2, 4, kSubs>(a, ws, s);
+      if (cols <= 16) return launch_matvec<kX, 1, 2, kSubs>(a, ws, s);
+      return launch_matvec<kX, 1, 4, kSubs>(a, ws, s);
     };
     if (group == 128) return of_group(std::integral_constant<int, 4>());
     if (group == 64) return of_group(std::integral_constant<int, 2>());
