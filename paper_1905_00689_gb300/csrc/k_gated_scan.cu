@@ -519,9 +519,14 @@ struct ScanArgs {
 };
 
 __device__ __forceinline__ uint64_t load_f32x2(const float* p, int left) {
+  if (left > 1 && (reinterpret_cast<uintptr_t>(p) & 7u) == 0) return *reinterpret_cast<const uint64_t*>(p);
   return f32x2(left > 0 ? p[0] : 0.0f, left > 1 ? p[1] : 0.0f);
 }
 __device__ __forceinline__ void store_f32x2(float* p, int left, uint64_t v) {
+  if (left > 1 && (reinterpret_cast<uintptr_t>(p) & 7u) == 0) {
+    *reinterpret_cast<uint64_t*>(p) = v;
+    return;
+  }
   float a, b;
   f32x2_split(v, a, b);
   if (left > 0) p[0] = a;
@@ -954,34 +959,49 @@ struct StepArgs {
   void* y;
 };
 
-// One timestep: a thread per pair of channels of one stream.  A few
-// thousand values at most take longer to launch than to compute.
-template <typename T, bool kVec>
+// One timestep: a thread takes a pair of channels of kRows streams, all of whose values it asks for before it forms the
+// decays' rates, which cost more than a stream's timestep.  (One stream to a thread: 1000 x 2048 in 10.3 us, bound by
+// the rates.)
+template <typename T, bool kVec, int kRows>
 __global__ void __launch_bounds__(256) gated_step_kernel(const StepArgs a) {
   const int ch = 2 * (blockIdx.x * blockDim.x + threadIdx.x), left = a.D - ch;
   if (left <= 0) return;
-  const uint64_t rate = rate_of(a.decay + ch, left, a.c);
-  const Constants k = constants();
-  for (int b = blockIdx.y; b < a.B; b += gridDim.y) {
-    T* y = static_cast<T*>(a.y) + (long long)b * a.D + ch;
-    const int slot = a.slots ? a.slots[b] : b;
-    if (slot < 0 || slot >= a.n_slots) {
-      store_pair<T, kVec>(y, left, 0.0f, 0.0f);
-      continue;
+  for (int b0 = blockIdx.y * kRows; b0 < a.B; b0 += gridDim.y * kRows) {
+    float2 x[kRows], r[kRows], i[kRows];
+    uint64_t h[kRows];
+    int slot[kRows];
+#pragma unroll
+    for (int n = 0; n < kRows; ++n) {
+      const int b = b0 + n;
+      slot[n] = b >= a.B ? -1 : (a.slots ? a.slots[b] : b);
     }
-    const float2 x = load_pair<T, kVec>(static_cast<const T*>(a.x) + b * a.x_pitch + ch, left);
-    const float2 r = load_pair<T, kVec>(static_cast<const T*>(a.r) + b * a.r_pitch + ch, left);
-    const float2 i = load_pair<T, kVec>(static_cast<const T*>(a.i) + b * a.i_pitch + ch, left);
-    float* st = a.state + (long long)slot * a.D + ch;
-    uint64_t h = load_f32x2(st, left);
-    if (a.reset && a.reset[b] != 0) h = 0ull;
-    const Gates g = gates_of<true>(f32x2(r.x, r.y), f32x2(i.x, i.y), rate, k);
-    const uint64_t A = decay_of(g.low, k), m2 = m2_of(g.low, A, k);
-    h = fma2(A, h, mul2(mul2(mul2(m2, rsqrt2(m2)), g.si), f32x2(x.x, x.y)));
-    store_f32x2(st, left, h);
-    float h0, h1;
-    f32x2_split(h, h0, h1);
-    store_pair<T, kVec>(y, left, h0, h1);
+#pragma unroll
+    for (int n = 0; n < kRows; ++n) {
+      const long long b = b0 + n;
+      if (slot[n] < 0 || slot[n] >= a.n_slots) continue;
+      x[n] = load_pair<T, kVec>(static_cast<const T*>(a.x) + b * a.x_pitch + ch, left);
+      r[n] = load_pair<T, kVec>(static_cast<const T*>(a.r) + b * a.r_pitch + ch, left);
+      i[n] = load_pair<T, kVec>(static_cast<const T*>(a.i) + b * a.i_pitch + ch, left);
+      h[n] = load_f32x2(a.state + (long long)slot[n] * a.D + ch, left);
+      if (a.reset && a.reset[b] != 0) h[n] = 0ull;
+    }
+    const uint64_t rate = rate_of(a.decay + ch, left, a.c);
+    const Constants k = constants();
+#pragma unroll
+    for (int n = 0; n < kRows; ++n) {
+      const int b = b0 + n;
+      if (b >= a.B) continue;
+      T* y = static_cast<T*>(a.y) + (long long)b * a.D + ch;
+      if (slot[n] < 0 || slot[n] >= a.n_slots) {
+        store_pair<T, kVec>(y, left, 0.0f, 0.0f);
+        continue;
+      }
+      const Gates g = gates_of<true>(f32x2(r[n].x, r[n].y), f32x2(i[n].x, i[n].y), rate, k);
+      const uint64_t A = decay_of(g.low, k), m2 = m2_of(g.low, A, k);
+      const uint64_t after = fma2(A, h[n], mul2(mul2(mul2(m2, rsqrt2(m2)), g.si), f32x2(x[n].x, x[n].y)));
+      store_f32x2(a.state + (long long)slot[n] * a.D + ch, left, after);
+      store_both<T, kVec>(y, left, after);
+    }
   }
 }
 
@@ -1215,12 +1235,15 @@ extern "C" int lstm_approx_gated_step(int dtype, const void* x, long long x_pitc
   StepArgs a{x, r, i, x_pitch, r_pitch, i_pitch, decay, c, state, n_slots, slots, reset, B, D, y};
   const bool vec = D % 2 == 0 && aligned_to(2 * es, x, es, {0, x_pitch}) && aligned_to(2 * es, r, es, {0, r_pitch}) &&
                    aligned_to(2 * es, i, es, {0, i_pitch}) && op_aligned(y, 2 * es);
-  const int threads = D >= 512 ? 256 : 64;
-  const dim3 grid((D + 2 * threads - 1) / (2 * threads), std::min(B, 65535));
+  const int threads = D >= 512 ? 256 : 64, across = (D + 2 * threads - 1) / (2 * threads);
+  // one stream to a thread while that leaves no SM with more than 8 blocks
+  const bool many = (long long)across * B > 8 * 152;
+  const dim3 grid(across, std::min(many ? (B + 3) / 4 : B, 65535));
   const cudaError_t e = op_for_type(dtype, [&](auto* t) {
     using E = std::remove_pointer_t<decltype(t)>;
-    return op_launch(vec ? gated_step_kernel<E, true> : gated_step_kernel<E, false>, grid, dim3(threads), 0,
-                     static_cast<cudaStream_t>(cuda_stream), a);
+    auto kern = vec ? (many ? gated_step_kernel<E, true, 4> : gated_step_kernel<E, true, 1>)
+                    : (many ? gated_step_kernel<E, false, 4> : gated_step_kernel<E, false, 1>);
+    return op_launch(kern, grid, dim3(threads), 0, static_cast<cudaStream_t>(cuda_stream), a);
   });
   return op_launched(e, "step launch", msg, msg_len);
 }
