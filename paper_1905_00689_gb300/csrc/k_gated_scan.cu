@@ -411,6 +411,7 @@ inline size_t exchange_bytes(const Tasks& t) { return ((size_t)t.slabs * kLanes 
 // Fills the exchange and forms the rates, once per call.
 __global__ void __launch_bounds__(256) scan_prepare_kernel(const float* decay, float c, int D, int rates, float* rate,
                                                            uint4* fill, long long n) {
+  begin_op();
   const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   if (i < rates) rate[i] = i < D ? c * softplus_f(decay[i]) : 0.0f;
   for (long long k = i; k < n; k += (long long)gridDim.x * blockDim.x)
@@ -604,6 +605,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const __grid
   }
   __syncthreads();
   fetch(0, plans[0]);
+  begin_op();
   const Constants k = constants();
   int turn = 0, now = 0;
   unsigned parity = 0;  // of the stage in use
@@ -787,6 +789,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
   }
   __syncthreads();
   fetch(0, plans[0]);
+  begin_op();
   const Constants k = constants();
   int turn = 0, now = 0;
   unsigned parity = 0;
@@ -930,6 +933,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
 // ddecay from partial [n][pitch], summed in a fixed order.
 __global__ void __launch_bounds__(1024) decay_gradient_kernel(const float* partial, int n, int pitch, int D,
                                                               const float* decay, float* ddecay) {
+  begin_op();
   __shared__ float acc[32][33];
   const int col = blockIdx.x * 32 + threadIdx.x;
   float v = 0.0f;
@@ -964,6 +968,7 @@ struct StepArgs {
 // the rates.)
 template <typename T, bool kVec, int kRows>
 __global__ void __launch_bounds__(256) gated_step_kernel(const StepArgs a) {
+  begin_op();
   const int ch = 2 * (blockIdx.x * blockDim.x + threadIdx.x), left = a.D - ch;
   if (left <= 0) return;
   for (int b0 = blockIdx.y * kRows; b0 < a.B; b0 += gridDim.y * kRows) {
@@ -1051,11 +1056,13 @@ cudaError_t launch_scan(void (*kern)(const A), cudaStream_t s, const A& args) {
   cfg.blockDim = dim3(kWarps * 32);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeCooperative;  // all blocks at once: they wait for one another's tiles
-  attr[0].val.cooperative = 1;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // the first tiles are on their way meanwhile
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeCooperative;  // all blocks at once: they wait for one another's tiles
+  attr[1].val.cooperative = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = args.tasks.tiles > 1 ? 1 : 0;  // (a single tile waits for none)
+  cfg.numAttrs = args.tasks.tiles > 1 ? 2 : 1;  // (a single tile waits for none)
   return cudaLaunchKernelEx(&cfg, kern, args);
 }
 

@@ -222,6 +222,7 @@ __device__ __forceinline__ uint2 to_e4m3(const float (&y)[8], float scale) {
 
 template <typename T, int VPT, int kMost, int kUnit, bool kQuant>
 __global__ void __launch_bounds__(kMost) rms_norm_kernel(const NormArgs a) {
+  begin_op();
   __shared__ float part[32];
   __shared__ unsigned part_max[32];
   const long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
@@ -340,6 +341,7 @@ __host__ __device__ constexpr int pitch_of_partial(int D) { return (D + 7) / 8 *
 // A block's rows go on by all blocks' rows; the next one's values are on their way while this one's sum is formed.
 template <typename T, int VPT, int kMost, int kUnit>
 __global__ void __launch_bounds__(kMost) rms_norm_backward_kernel(const NormBackwardArgs a) {
+  begin_op();
   __shared__ float part[2][kMaxRows][32];
   extern __shared__ __align__(16) float merged[];  // [rows of the block][pitch] where there are several
   float w[VPT][8], dw[VPT][8];
@@ -417,6 +419,7 @@ __global__ void __launch_bounds__(kMost) rms_norm_backward_kernel(const NormBack
 
 // Column sums of partial [n][pitch_of_partial(D)], in a fixed order.
 __global__ void __launch_bounds__(1024) column_sum_kernel(const float* partial, int n, int D, float* out) {
+  begin_op();
   __shared__ float acc[32][33];
   const int col = blockIdx.x * 32 + threadIdx.x;
   float v = 0.0f;
@@ -434,12 +437,12 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const float* partial, 
 struct RowShape {
   int threads, vpt, rows_per_block;
 };
-// 16-bit values in 16-byte accesses: two groups to a thread from 1024 columns on and four from 4096 (at 8192 x 4096, 512
+// 16-bit values in 16-byte accesses: two groups to a thread above 256 columns and four above 4096 (at 8192 x 4096, 512
 // threads with one group took 50 us, 256 with two 44); else two only where one would take more than 512 threads.
 RowShape row_shape(int D, bool wide) {
   const int n = (D + 7) / 8;
   RowShape r;
-  r.vpt = n > 2048 ? 4 : (n > 512 ? (wide && n <= 1024 ? 4 : 2) : (wide && n >= 128 ? 2 : 1));
+  r.vpt = n > 2048 ? 4 : (n > 512 ? (wide && n <= 1024 ? 4 : 2) : (wide && n > 32 ? 2 : 1));
   r.threads = ((n + r.vpt - 1) / r.vpt + 31) / 32 * 32;
   r.rows_per_block = r.threads == 32 ? 4 : 1;
   return r;

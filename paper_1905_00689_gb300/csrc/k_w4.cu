@@ -217,7 +217,7 @@ constexpr int kParts = kX == LSTM_APPROX_OP_FP32 ? 3 : 1;
 // [columns][4] x 16 bytes.  A thread takes 8 k of one row.
 template <int kX, int kSubs>
 __global__ void __launch_bounds__(256) w4_lay_out_kernel(const W4Args a, uint4* to) {
-  griddep_launch_dependents();
+  begin_op();
   const int blocks = (a.K + kBlockK - 1) / kBlockK, chunks = blocks * 16;
   const long long item = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   if (item >= (long long)a.M * chunks) return;
@@ -235,6 +235,9 @@ __device__ __forceinline__ int stretch(int w, int each, int more) { return w * e
 // kX: type of x.  A tile is kMt * 16 rows of W; kNt * 8 columns of x^T.  kSubs = group / 32.
 template <int kX, int kMt, int kNt, int kSubs>
 __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args a) {
+  // where x is laid out by the kernel before, W, which that kernel does not write and which was complete before it
+  // began, is on its way meanwhile
+  if (!a.x_laid) begin_op();
   constexpr bool kBf16 = kX == LSTM_APPROX_OP_BF16 || kX == LSTM_APPROX_OP_FP32;
   constexpr bool kScaled = kX == LSTM_APPROX_OP_E4M3;
   constexpr int kP = kParts<kX>;
@@ -366,8 +369,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
 
     if (!staged) {
       if (a.x_laid) {
-        // the kernel before has laid it out (and what came before that one has been complete since it started)
-        griddep_wait();
+        begin_op();
         if (threadIdx.x == 0) {
           const uint32_t bytes = (uint32_t)blocks * 256 * cols, bar = smem_u32(&x_bar);
           const unsigned char* from_x = a.x_laid + (long long)m0 * kP * blocks * 256;
@@ -568,6 +570,7 @@ __device__ __forceinline__ float round_to(float v, int dtype) {
 // A warp per group of columns of one row; lane l packs columns 4 l .. 4 l + 3
 // of the group (two bytes).  The last group's warp also clears the row's rest.
 __global__ void __launch_bounds__(256) w4_quantize_kernel(const W4QuantizeArgs a) {
+  begin_op();
   const long long item = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (item >= (long long)a.N * a.groups) return;
   const int lane = threadIdx.x & 31;
@@ -666,17 +669,7 @@ cudaError_t launch_matvec(W4Args a, unsigned char* workspace, cudaStream_t s) {
                   reinterpret_cast<uint4*>(workspace));
     if (e != cudaSuccess) return e;
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(across, (a.M + p.tokens - 1) / p.tokens);
-  cfg.blockDim = dim3(p.warps * 32);
-  cfg.dynamicSmemBytes = p.smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // W is on its way while x is laid out
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = a.x_laid ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kern, a);
+  return op_launch(kern, dim3(across, (a.M + p.tokens - 1) / p.tokens), dim3(p.warps * 32), p.smem, s, a);
 }
 
 int check_matrix(int N, int K, int group, const void* q, long long q_pitch, const void* scale, int scale_dtype,
