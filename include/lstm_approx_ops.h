@@ -75,11 +75,14 @@ enum lstm_approx_op_dtype {
  *   scales    [rows][ceil(D / group)] fp32 when group > 0, else NULL
  *   sum_out   [rows][D] contiguous, or NULL; may be x or residual itself where
  *             that is contiguous (the residual stream updated in place)
+ *   sum_low   [rows][D] contiguous, or NULL; 16-bit types without 8-bit output
+ *             only: what sum_out's rounding took off s, for the backward pass (without it dweight is
+ *             off by that rounding)
  *   rstd      [rows] fp32, or NULL: kept for the backward pass
  */
 int lstm_approx_rms_norm(int dtype, int group, const void *x, long long x_pitch, const void *residual,
                          long long residual_pitch, const float *weight, float eps, long long rows,
-                         int D, void *out, float *scales, void *sum_out, float *rstd,
+                         int D, void *out, float *scales, void *sum_out, short *sum_low, float *rstd,
                          void *cuda_stream, char *msg, int msg_len);
 
 /*
@@ -91,6 +94,7 @@ int lstm_approx_rms_norm(int dtype, int group, const void *x, long long x_pitch,
  *   dy        [rows][D], pitch dy_pitch: gradient of out
  *   s         [rows][D], pitch s_pitch: sum_out of the forward call (x itself
  *             where there was no residual);  rstd [rows] of that call
+ *   s_low     [rows][D] contiguous: sum_low of that call, or NULL
  *   dsum      [rows][D], pitch dsum_pitch: gradient that reaches sum_out by
  *             another way (the residual stream), or NULL
  *   dx        [rows][D] contiguous: ds, the gradient of x and of residual
@@ -101,7 +105,7 @@ int lstm_approx_rms_norm(int dtype, int group, const void *x, long long x_pitch,
  *             dweight is NULL
  */
 int lstm_approx_rms_norm_backward(int dtype, const void *dy, long long dy_pitch, const void *s,
-                                  long long s_pitch, const float *weight, const float *rstd,
+                                  long long s_pitch, const short *s_low, const float *weight, const float *rstd,
                                   const void *dsum, long long dsum_pitch, long long rows, int D,
                                   void *dx, float *dweight, void *workspace, size_t workspace_bytes,
                                   void *cuda_stream, char *msg, int msg_len);

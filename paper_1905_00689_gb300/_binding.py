@@ -88,8 +88,8 @@ def load(path: str = LIB_PATH):
     lib.lstm_approx_dense_set_launch_order.argtypes = [I]
     # the operators of include/lstm_approx_ops.h; each ends in (stream, msg, msg_len)
     F, Z, end = ctypes.c_float, ctypes.c_size_t, [P, ctypes.c_char_p, I]
-    lib.lstm_approx_rms_norm.argtypes = [I, I, P, LL, P, LL, P, F, LL, I, P, P, P, P] + end
-    lib.lstm_approx_rms_norm_backward.argtypes = [I, P, LL, P, LL, P, P, P, LL, LL, I, P, P, P, Z] + end
+    lib.lstm_approx_rms_norm.argtypes = [I, I, P, LL, P, LL, P, F, LL, I, P, P, P, P, P] + end
+    lib.lstm_approx_rms_norm_backward.argtypes = [I, P, LL, P, LL, P, P, P, P, LL, LL, I, P, P, P, Z] + end
     lib.lstm_approx_rms_norm_workspace_bytes.argtypes = [LL, I]
     lib.lstm_approx_gated_scan.argtypes = [I, P, P, P, P, F, P, P, P, I, I, I, P, P, P, P, P, Z] + end
     lib.lstm_approx_gated_scan_backward.argtypes = ([I, P, P, P, P, P, P, F, P, P, P, I, I, I, P, P, P, P, P, P, P, Z]

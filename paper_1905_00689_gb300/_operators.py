@@ -55,7 +55,9 @@ def rms_norm(x, weight, residual=None, *, eps: float = 1e-6, out=None, residual_
     x, residual [..., D] fp32, bf16 or fp16; weight [D] fp32.  Returns (out,
     s): s in x's type, None without a residual (and without residual_out).
     ``residual_out`` may be ``residual`` itself; ``rstd`` [...] fp32 receives
-    1 / sqrt(mean(s^2) + eps) for :func:`rms_norm_backward`.
+    1 / sqrt(mean(s^2) + eps) for :func:`rms_norm_backward`.  With ``rstd`` and a
+    residual in 16 bits, s has what its rounding took off as its attribute
+    ``sum_low`` (int16, for the backward pass).
     """
     args = (x, weight, residual, eps, 0, out, None, residual_out, rstd)
     out, _, total = _ops.rms_norm(*args) if stream is None else _on(stream, _ops.rms_norm, *args)
@@ -79,6 +81,9 @@ def rms_norm_backward(dy, s, weight, rstd, dsum=None, *, dx=None, dweight=None, 
     s is the forward call's sum (x itself without a residual), rstd what it
     wrote there, dsum the gradient that reaches s by another way.  dx is the
     gradient of x and of the residual alike; it may be dy or dsum itself.
+    Where s has a ``sum_low`` and has not been changed since, the gradients are
+    those of the sum before its rounding to 16 bits; else (a copy, say) dweight
+    is off by that rounding.
     """
     args = (dy, s, weight, rstd, dsum, dx, dweight, workspace)
     return _ops.rms_norm_backward(*args) if stream is None else _on(stream, _ops.rms_norm_backward, *args)

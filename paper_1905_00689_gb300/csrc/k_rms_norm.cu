@@ -148,6 +148,24 @@ __device__ __forceinline__ void weights8(const float* w, int j, int D, bool alig
   }
 }
 
+// What a 16-bit type T takes off a 32-bit sum: the distance of their bit patterns (both as fp32, magnitudes), at most half
+// a unit of T in its last place.  So 16 + 16 bits give the sum back (a tie's half unit of bf16, and what rounds to a
+// subnormal of fp16, up to the bound), and whatever the low part holds, the result is within its bound of the high part.
+template <typename T>
+constexpr int kMostLow = std::is_same_v<T, __half> ? 1 << 12 : (1 << 15) - 1;
+template <typename T>
+__device__ __forceinline__ float low_part(float s) {  // an integer, as the bits of a float
+  const unsigned high = __float_as_uint(to_f32(from_f32<T>(s))) & 0x7fffffffu;
+  const int d = (int)(__float_as_uint(s) & 0x7fffffffu) - (int)high;
+  return __int_as_float(high < 0x7f800000u ? min(max(d, -kMostLow<T>), kMostLow<T>) : 0);
+}
+template <typename T>
+__device__ __forceinline__ float with_low_part(float high, float low) {
+  const unsigned bits = __float_as_uint(high), m = bits & 0x7fffffffu;
+  const int d = min(max(__float_as_int(low), -kMostLow<T>), kMostLow<T>);
+  return m < 0x7f800000u ? __uint_as_float((bits & 0x80000000u) | (unsigned)max((int)m + d, 0)) : high;
+}
+
 struct NormArgs {
   const void* x;
   long long x_pitch;
@@ -161,6 +179,7 @@ struct NormArgs {
   float* scales;
   int group, n_groups;  // columns per scale (0: no scales), scales per row
   void* sum_out;
+  int16_t* sum_low;
   float* rstd;
   bool weight_vec;  // weight is 16-byte aligned
 };
@@ -260,6 +279,17 @@ __global__ void __launch_bounds__(kMost) rms_norm_kernel(const NormArgs a) {
 #pragma unroll
     for (int j = 0; j < VPT; ++j) put8<T, kUnit>(so, j, a.D, s[j]);
   }
+  if constexpr (sizeof(T) == 2 && !kQuant) {
+    if (a.sum_low) {
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        float low[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) low[e] = low_part<T>(s[j][e]);
+        put8<int16_t, kUnit>(a.sum_low + row * a.D, j, a.D, low);
+      }
+    }
+  }
   sum = row_sum<false>(sum, part);
   const float rstd = rsqrtf(sum / (float)a.D + a.eps);
   if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
@@ -326,6 +356,7 @@ struct NormBackwardArgs {
   long long dy_pitch;
   const void* s;
   long long s_pitch;
+  const int16_t* s_low;
   const float* weight;
   const float* rstd;
   const void* dsum;
@@ -339,8 +370,9 @@ struct NormBackwardArgs {
 __host__ __device__ constexpr int pitch_of_partial(int D) { return (D + 7) / 8 * 8; }
 
 // A block's rows go on by all blocks' rows; the next one's values are on their way while this one's sum is formed.
-template <typename T, int VPT, int kMost, int kUnit>
-__global__ void __launch_bounds__(kMost) rms_norm_backward_kernel(const NormBackwardArgs a) {
+// kLow: s comes with the low parts of sum_out.
+template <typename T, int VPT, int kMost, int kUnit, bool kLow>
+__global__ void __launch_bounds__(kMost, 1) rms_norm_backward_kernel(const NormBackwardArgs a) {
   begin_op();
   __shared__ float part[2][kMaxRows][32];
   extern __shared__ __align__(16) float merged[];  // [rows of the block][pitch] where there are several
@@ -354,12 +386,17 @@ __global__ void __launch_bounds__(kMost) rms_norm_backward_kernel(const NormBack
   const long long step = (long long)gridDim.x * blockDim.y;
   long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
   Raw8<T, kUnit> raw_g[VPT], raw_s[VPT], raw_d[VPT];
+  Raw8<int16_t, kUnit> raw_low[kLow ? VPT : 1];
   float rstd = 0.0f;
   auto load = [&](long long row) {
     const T* dy = static_cast<const T*>(a.dy) + row * a.dy_pitch;
     const T* s = static_cast<const T*>(a.s) + row * a.s_pitch;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) raw_g[j].load(dy, j, a.D), raw_s[j].load(s, j, a.D);
+    if constexpr (kLow) {
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) raw_low[j].load(a.s_low + row * a.D, j, a.D);
+    }
     if (a.dsum) {
       const T* ds = static_cast<const T*>(a.dsum) + row * a.dsum_pitch;
 #pragma unroll
@@ -377,6 +414,12 @@ __global__ void __launch_bounds__(kMost) rms_norm_backward_kernel(const NormBack
     for (int j = 0; j < VPT; ++j) {
       raw_g[j].get(g[j]);
       raw_s[j].get(v[j]);
+      if constexpr (kLow) {
+        float low[8];
+        raw_low[j].get(low);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[j][e] = with_low_part<T>(v[j][e], low[e]);
+      }
       if (a.dsum) raw_d[j].get(r[j]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -494,8 +537,8 @@ using namespace lstm_approx_impl;
 
 extern "C" int lstm_approx_rms_norm(int dtype, int group, const void* x, long long x_pitch, const void* residual,
                                     long long residual_pitch, const float* weight, float eps, long long rows, int D,
-                                    void* out, float* scales, void* sum_out, float* rstd, void* cuda_stream, char* msg,
-                                    int msg_len) {
+                                    void* out, float* scales, void* sum_out, short* sum_low, float* rstd,
+                                    void* cuda_stream, char* msg, int msg_len) {
   if (msg && msg_len > 0) msg[0] = '\0';
   if (!op_float_dtype(dtype)) return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "dtype %d", dtype);
   if (rows < 0 || rows > 0x7fffffffll || D < 1 || D > kMaxD)
@@ -503,18 +546,23 @@ extern "C" int lstm_approx_rms_norm(int dtype, int group, const void* x, long lo
   if (group < 0 || (group > 0 && group < D && group != 32 && group != 64 && group != 128 && group != 256))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "group must be 0, 32, 64, 128, 256 or >= D, not %d", group);
   if (!(eps >= 0.0f)) return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "eps must not be negative");
+  if (sum_low && (dtype == LSTM_APPROX_OP_FP32 || group > 0))
+    return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "sum_low is for 16-bit types, and not for 8-bit output");
   if (rows > 0 && (!x || !weight || !out || (group > 0) != (scales != nullptr)))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL,
                      "x, weight and out must not be NULL; scales are given for 8-bit output only");
   const size_t es = op_dtype_bytes(dtype);
   if (x_pitch < 0 || residual_pitch < 0 || !op_aligned(x, es) || !op_aligned(residual, es) || !op_aligned(sum_out, es) ||
-      !op_aligned(weight, 4) || !op_aligned(scales, 4) || !op_aligned(rstd, 4) || (group == 0 && !op_aligned(out, es)))
+      !op_aligned(weight, 4) || !op_aligned(scales, 4) || !op_aligned(sum_low, 2) || !op_aligned(rstd, 4) ||
+      (group == 0 && !op_aligned(out, es)))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "a negative pitch, or a pointer not aligned to its type");
   if (int rc = op_check_device(msg, msg_len)) return rc;
   if (rows == 0) return LSTM_APPROX_OK;
-  NormArgs a{x, x_pitch, residual, residual_pitch, weight, eps, rows, D, out, scales, group, 0, sum_out, rstd, false};
+  NormArgs a{x, x_pitch, residual, residual_pitch, weight, eps, rows, D, out, scales, group, 0, sum_out, sum_low, rstd,
+             false};
   a.n_groups = group > 0 ? (group >= D ? 1 : (D + group - 1) / group) : 0;
-  int unit = unit_of(D, es, {{x, x_pitch}, {residual, residual_pitch}, {sum_out, D}, {group > 0 ? nullptr : out, D}});
+  int unit = unit_of(D, es, {{x, x_pitch}, {residual, residual_pitch}, {sum_out, D}, {sum_low, D},
+                        {group > 0 ? nullptr : out, D}});
   if (unit == 8 && group > 0 && !op_aligned(out, 8)) unit = 1;
   a.weight_vec = op_aligned(weight, 16);
   const RowShape r = row_shape(D, unit == 8 && es == 2);
@@ -546,42 +594,50 @@ extern "C" size_t lstm_approx_rms_norm_workspace_bytes(long long rows, int D) {
 }
 
 extern "C" int lstm_approx_rms_norm_backward(int dtype, const void* dy, long long dy_pitch, const void* s,
-                                             long long s_pitch, const float* weight, const float* rstd,
+                                             long long s_pitch, const short* s_low, const float* weight, const float* rstd,
                                              const void* dsum, long long dsum_pitch, long long rows, int D, void* dx,
                                              float* dweight, void* workspace, size_t workspace_bytes,
                                              void* cuda_stream, char* msg, int msg_len) {
   if (msg && msg_len > 0) msg[0] = '\0';
   if (!op_float_dtype(dtype)) return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "dtype %d", dtype);
+  if (s_low && dtype == LSTM_APPROX_OP_FP32)
+    return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "s_low is for 16-bit types");
   if (rows < 0 || rows > 0x7fffffffll || D < 1 || D > kMaxD)
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "need 0 <= rows < 2^31 and 1 <= D <= %d", kMaxD);
   if (rows > 0 && (!dy || !s || !weight || !rstd || !dx))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "dy, s, weight, rstd and dx must not be NULL");
   const size_t es = op_dtype_bytes(dtype);
   if (dy_pitch < 0 || s_pitch < 0 || dsum_pitch < 0 || !op_aligned(dy, es) || !op_aligned(s, es) ||
-      !op_aligned(dsum, es) || !op_aligned(dx, es) || !op_aligned(weight, 4) || !op_aligned(rstd, 4) ||
+      !op_aligned(s_low, 2) || !op_aligned(dsum, es) || !op_aligned(dx, es) || !op_aligned(weight, 4) || !op_aligned(rstd, 4) ||
       !op_aligned(dweight, 4))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "a negative pitch, or a pointer not aligned to its type");
   const size_t need = lstm_approx_rms_norm_workspace_bytes(rows, D);
   if (dweight && (!workspace || !op_aligned(workspace, 16) || workspace_bytes < need))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "dweight needs a 16-byte aligned workspace of %zu bytes", need);
   if (int rc = op_check_device(msg, msg_len)) return rc;
-  const int unit = unit_of(D, es, {{dy, dy_pitch}, {s, s_pitch}, {dsum, dsum_pitch}, {dx, D}});
+  const int unit = unit_of(D, es, {{dy, dy_pitch}, {s, s_pitch}, {s_low, D}, {dsum, dsum_pitch}, {dx, D}});
   const RowShape r = backward_shape(D, unit == 8 && es == 2);
   const int blocks = backward_blocks(rows, r);
   const size_t smem = r.rows_per_block > 1 ? (size_t)r.rows_per_block * pitch_of_partial(D) * sizeof(float) : 0;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (rows > 0) {
-    NormBackwardArgs a{dy, dy_pitch, s, s_pitch, weight, rstd, dsum, dsum_pitch, rows, D, dx,
+    NormBackwardArgs a{dy, dy_pitch, s, s_pitch, s_low, weight, rstd, dsum, dsum_pitch, rows, D, dx,
                        dweight ? static_cast<float*>(workspace) : nullptr, op_aligned(weight, 16)};
     const cudaError_t e = op_for_type(dtype, [&](auto* t) {
       using T = std::remove_pointer_t<decltype(t)>;
       return with_shape(r, [&](auto vpt, auto most) {
         constexpr int V = decltype(vpt)::value, M = decltype(most)::value;
         const dim3 block(r.threads, r.rows_per_block);
+        auto run = [&](auto low) {
+          constexpr bool kLow = decltype(low)::value;
+          auto kern = unit == 8 ? rms_norm_backward_kernel<T, V, M, 8, kLow> : rms_norm_backward_kernel<T, V, M, 1, kLow>;
+          if constexpr (sizeof(T) == 2)
+            if (unit == 2) kern = rms_norm_backward_kernel<T, V, M, 2, kLow>;
+          return op_launch(kern, dim3(blocks), block, smem, st, a);
+        };
         if constexpr (sizeof(T) == 2)
-          if (unit == 2) return op_launch(rms_norm_backward_kernel<T, V, M, 2>, dim3(blocks), block, smem, st, a);
-        return op_launch(unit == 8 ? rms_norm_backward_kernel<T, V, M, 8> : rms_norm_backward_kernel<T, V, M, 1>, dim3(blocks),
-                         block, smem, st, a);
+          if (s_low) return run(std::true_type());
+        return run(std::false_type());
       });
     });
     if (int rc = op_launched(e, "norm backward launch", msg, msg_len)) return rc;

@@ -42,6 +42,12 @@ __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { retu
 template <>
 __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 
+// Integers, carried as the bits of a float.
+template <>
+__device__ __forceinline__ float to_f32<int16_t>(int16_t v) { return __int_as_float(v); }
+template <>
+__device__ __forceinline__ int16_t from_f32<int16_t>(float v) { return (int16_t)__float_as_int(v); }
+
 // Two neighbouring elements in one access.
 template <typename T>
 struct Pair;
@@ -62,6 +68,12 @@ struct Pair<__half> {
   using Raw = __half2;
   static __device__ __forceinline__ float2 get(Raw v) { return __half22float2(v); }
   static __device__ __forceinline__ Raw put(float a, float b) { return __floats2half2_rn(a, b); }
+};
+template <>
+struct Pair<int16_t> {
+  using Raw = short2;
+  static __device__ __forceinline__ float2 get(Raw v) { return make_float2(to_f32(v.x), to_f32(v.y)); }
+  static __device__ __forceinline__ Raw put(float a, float b) { return make_short2(from_f32<int16_t>(a), from_f32<int16_t>(b)); }
 };
 
 // Eight neighbouring elements: in 16-byte accesses (kVec: the address is

@@ -120,11 +120,16 @@ struct Call {
   void* dense(PyObject* o, const char* name, at::ScalarType type, at::IntArrayRef shape) const {
     return o == Py_None ? nullptr : dense(tensor(o, name), name, type, shape);
   }
+  // A tensor of the caller that the call writes to: torch counts its changes.
+  static void written(const Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+  }
   // The caller's tensor, or a new one.
   Tensor out(PyObject* o, const char* name, at::ScalarType type, at::IntArrayRef shape) const {
     if (o == Py_None) return at::empty(shape, at::TensorOptions().dtype(type).device(device));
     const Tensor& t = tensor(o, name);
     dense(t, name, type, shape);
+    written(t);
     return t;
   }
   // The caller's workspace (its bytes are checked by the library), or a new one.
@@ -170,6 +175,36 @@ PyObject* wrap_all(const Ts&... ts) {
   return nullptr;
 }
 
+// A 16-bit sum of rms_norm that a backward pass will read carries what its rounding took off as its attribute `sum_low`,
+// with the version that the sum had then.  After a change of the sum in place, by torch or by an operator here, it no
+// longer counts.  (A change that torch does not see does little: a low part moves a value by half a unit in the last
+// place of the 16-bit type at most.)
+PyObject *g_sum_low = nullptr, *g_sum_low_version = nullptr;
+
+bool set_sum_low(PyObject* sum, const Tensor& t, const std::optional<Tensor>& low) {
+  if (!low) return !PyObject_HasAttr(sum, g_sum_low) || PyObject_DelAttr(sum, g_sum_low) == 0;  // an earlier call's
+  PyObject *v = wrap(*low), *n = v ? PyLong_FromLongLong(t._version()) : nullptr;
+  const bool ok = n && PyObject_SetAttr(sum, g_sum_low, v) == 0 && PyObject_SetAttr(sum, g_sum_low_version, n) == 0;
+  Py_XDECREF(v);
+  Py_XDECREF(n);
+  return ok;
+}
+std::optional<Tensor> get_sum_low(PyObject* sum, const Tensor& t) {
+  std::optional<Tensor> found;
+  if (t.is_inference() || !PyObject_HasAttr(sum, g_sum_low)) return found;
+  PyObject *v = PyObject_GetAttr(sum, g_sum_low), *n = PyObject_GetAttr(sum, g_sum_low_version);
+  if (v && n && THPVariable_Check(v) && PyLong_Check(n) && PyLong_AsLongLong(n) == (long long)t._version()) {
+    const Tensor& low = THPVariable_Unpack(v);
+    if (low.scalar_type() == at::kShort && low.sizes() == t.sizes() && low.device() == t.device() &&
+        low.is_contiguous() && t.is_contiguous())
+      found = low;
+  }
+  Py_XDECREF(v);
+  Py_XDECREF(n);
+  PyErr_Clear();
+  return found;
+}
+
 // rms_norm(x, weight, residual, eps, group, out, scales, residual_out, rstd) -> (out, scales, residual_out)
 PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t) {
   return guarded([&]() -> PyObject* {
@@ -193,6 +228,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t) {
       res_pitch = pitch_of(r, "residual");
     }
     float* rstd = static_cast<float*>(call.dense(a[8], "rstd", at::kFloat, lead));
+    if (rstd) Call::written(tensor(a[8], "rstd"));
     need(D <= 0x7fffffff && group <= 0x7fffffff && group >= 0, "D and group must be 32-bit numbers");
     if (pr || a[7] != Py_None) total = call.out(a[7], "residual_out", type, shape);
     if (group > 0) {
@@ -201,10 +237,15 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t) {
       scales = call.out(a[6], "scales", at::kFloat, sizes);
     }
     Tensor out = call.out(a[5], "out", group > 0 ? at::kFloat8_e4m3fn : type, shape);
+    std::optional<Tensor> low;  // where a backward pass will follow (rstd is asked for) and s has more than 16 bits
+    if (pr && rstd && group == 0 && type != at::kFloat && !total->is_inference()) low = call.out(Py_None, "", at::kShort, shape);
     call.done(lstm_approx_rms_norm(code, (int)group, px, pitch, pr, res_pitch, static_cast<const float*>(pw), real(a[3]),
                                    rows, (int)D, out.data_ptr(), scales ? scales->data_ptr<float>() : nullptr,
-                                   total ? total->data_ptr() : nullptr, rstd, call.stream, call.msg, sizeof(call.msg)));
-    return wrap_all(out, scales, total);
+                                   total ? total->data_ptr() : nullptr, low ? low->data_ptr<int16_t>() : nullptr, rstd,
+                                   call.stream, call.msg, sizeof(call.msg)));
+    PyObject* result = wrap_all(out, scales, total);
+    if (result && total && !set_sum_low(PyTuple_GET_ITEM(result, 2), *total, low)) Py_CLEAR(result);
+    return result;
   });
 }
 
@@ -221,6 +262,8 @@ PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t) {
     need(D <= 0x7fffffff, "D must be a 32-bit number");
     const Tensor& s = tensor(a[1], "s");
     void *pdy = call.rows(dy, "dy", type, shape), *ps = call.rows(s, "s", type, shape), *pd = nullptr;
+    const std::optional<Tensor> low = type != at::kFloat ? get_sum_low(a[1], s) : std::nullopt;
+    if (low) low->record_stream(c10::Stream(c10::cuda::getCurrentCUDAStream(call.device.index())));
     long long d_pitch = 0;
     if (a[4] != Py_None) {
       const Tensor& d = tensor(a[4], "dsum");
@@ -231,8 +274,9 @@ PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t) {
     const float* rstd = static_cast<const float*>(call.dense(tensor(a[3], "rstd"), "rstd", at::kFloat, lead));
     Tensor dx = call.out(a[5], "dx", type, shape), dw = call.out(a[6], "dweight", at::kFloat, {D});
     Tensor ws = call.workspace(a[7], lstm_approx_rms_norm_workspace_bytes(rows, (int)D));
-    call.done(lstm_approx_rms_norm_backward(code, pdy, pitch_of(dy, "dy"), ps, pitch_of(s, "s"), w, rstd, pd, d_pitch,
-                                            rows, (int)D, dx.data_ptr(), dw.data_ptr<float>(), ws.data_ptr(), ws.nbytes(),
+    call.done(lstm_approx_rms_norm_backward(code, pdy, pitch_of(dy, "dy"), ps, pitch_of(s, "s"),
+                                            low ? low->data_ptr<int16_t>() : nullptr, w, rstd, pd, d_pitch, rows, (int)D,
+                                            dx.data_ptr(), dw.data_ptr<float>(), ws.data_ptr(), ws.nbytes(),
                                             call.stream, call.msg, sizeof(call.msg)));
     return wrap_all(dx, dw);
   });
@@ -273,7 +317,9 @@ struct Sequence {
   }
 };
 Tensor sequence_out(const Call& call, const Sequence& q, PyObject* o, const char* name) {
-  return o == Py_None ? call.out(o, name, q.type, q.shape) : tensor(o, name);
+  if (o == Py_None) return call.out(o, name, q.type, q.shape);
+  Call::written(tensor(o, name));
+  return tensor(o, name);
 }
 
 // gated_scan(x, r, i, decay, h0, c, lengths, reset, y, h_last, states, workspace) -> (y, h_last)
@@ -290,6 +336,7 @@ PyObject* gated_scan(PyObject*, PyObject* const* a, Py_ssize_t) {
     const float* decay = static_cast<const float*>(call.dense(tensor(a[3], "decay"), "decay", at::kFloat, {q.D}));
     const float* h0 = static_cast<const float*>(call.dense(a[4], "h0", at::kFloat, {q.B, q.D}));
     float* states = static_cast<float*>(call.dense(a[10], "states", at::kFloat, {q.chunks, q.B, q.D}));
+    if (states) Call::written(tensor(a[10], "states"));
     Tensor y = sequence_out(call, q, a[8], "y"), last = call.out(a[9], "h_last", at::kFloat, {q.B, q.D});
     void* py = q.add(call, y, "y", strides, n);
     Tensor ws = call.workspace(a[11], lstm_approx_gated_scan_workspace_bytes((int)q.T, (int)q.B, (int)q.D));
@@ -346,6 +393,7 @@ PyObject* gated_step(PyObject*, PyObject* const* a, Py_ssize_t) {
     void *px = call.rows(x, "x", type, shape), *pr = call.rows(r, "r", type, shape), *pi = call.rows(i, "i", type, shape);
     const float* decay = static_cast<const float*>(call.dense(tensor(a[3], "decay"), "decay", at::kFloat, {D}));
     float* ps = static_cast<float*>(call.dense(state, "state", at::kFloat, {slots, D}));
+    Call::written(state);
     const int32_t* at_slots = static_cast<const int32_t*>(call.dense(a[6], "slots", at::kInt, {B}));
     const unsigned char* reset = Sequence::resets(call, a[7], {B});
     Tensor y = call.out(a[8], "y", type, shape);
@@ -454,5 +502,7 @@ PyMODINIT_FUNC PyInit__torch_ops() {
   if (!binding) return nullptr;
   g_error = PyObject_GetAttrString(binding, "LSTMApproxError");
   Py_DECREF(binding);
-  return g_error ? PyModule_Create(&g_module) : nullptr;
+  g_sum_low = PyUnicode_InternFromString("sum_low");
+  g_sum_low_version = PyUnicode_InternFromString("sum_low_version");
+  return g_error && g_sum_low && g_sum_low_version ? PyModule_Create(&g_module) : nullptr;
 }

@@ -174,6 +174,42 @@ def test_norm_backward(cuda_device, rows, D, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,D", [(40, 64), (300, 1000), (65, 333), (20, 30)])
+def test_norm_backward_of_a_16_bit_sum(cuda_device, rows, D, dtype):
+    """The sum of a 16-bit forward pass brings along what its rounding took off: the gradients are those of x + residual, not
+    of its rounding; a changed or copied sum falls back to what it holds."""
+    import torch
+    from paper_1905_00689_gb300 import rms_norm, rms_norm_backward
+    x, res, dy, w = (make(rows, D, dtype, 61), make(rows, D, dtype, 62, std=3.0), make(rows, D, dtype, 63), weight(D))
+    rstd = torch.empty(rows, device="cuda")
+    _, total = rms_norm(x, w, res, eps=1e-5, rstd=rstd)
+    s = ref.f64(x) + ref.f64(res)
+    assert total.sum_low.dtype == torch.int16 and total.sum_low.shape == total.shape
+
+    def compare(got, s):
+        want, want_dw = ref.norm_backward(ref.f64(dy), s, ref.f64(w), None, 1e-5)
+        r = 1 / np.sqrt((s ** 2).mean(1, keepdims=True) + 1e-5)
+        wdy, xhat = np.abs(ref.f64(dy) * ref.f64(w)), np.abs(s) * r
+        ref.check(got[0], want, r * (wdy + xhat * (wdy * xhat).mean(1, keepdims=True)), 2 * TOL, dtype, "dx")
+        ref.check(got[1], want_dw, (np.abs(ref.f64(dy)) * xhat).sum(0), 2 * TOL, what="dw")
+    compare(rms_norm_backward(dy, total, w, rstd), s)
+    copy = total.clone()
+    rounded = torch.empty(rows, device="cuda")
+    rms_norm(copy, w, eps=1e-5, rstd=rounded)
+    compare(rms_norm_backward(dy, copy, w, rounded), ref.f64(copy))
+    total.mul_(2.0)  # sum_low no longer belongs to it
+    rms_norm(total, w, eps=1e-5, rstd=rounded)
+    compare(rms_norm_backward(dy, total, w, rounded), ref.f64(total))
+    assert not hasattr(rms_norm(x, w, res)[1], "sum_low")
+    held = res.clone()
+    rms_norm(x, w, held, residual_out=held, rstd=rstd)
+    assert hasattr(held, "sum_low")
+    rms_norm(x, w, held, residual_out=held)  # a later call on the same tensor takes it away
+    assert not hasattr(held, "sum_low")
+
+
+@pytest.mark.gpu
 def test_norm_gradients_against_differences(cuda_device):
     import torch
     from paper_1905_00689_gb300 import rms_norm, rms_norm_backward
@@ -212,17 +248,18 @@ def test_norm_no_rows_and_other_stream(cuda_device):
 
 def _args(**kw):
     a = dict(dtype=0, group=0, x=64, xp=8, res=None, rp=0, w=64, eps=1e-6, rows=2, D=8, out=64, scales=None, total=None,
-             rstd=None)
+             low=None, rstd=None)
     a.update(kw)
     return [a[k] for k in ("dtype", "group", "x", "xp", "res", "rp", "w", "eps", "rows", "D", "out", "scales", "total",
-                           "rstd")]
+                           "low", "rstd")]
 
 
 @pytest.mark.parametrize("bad", [dict(dtype=3), dict(dtype=-1), dict(group=48), dict(group=-1), dict(x=None),
                                  dict(w=None), dict(out=None), dict(rows=-1), dict(D=0), dict(D=32769),
                                  dict(eps=-1.0), dict(eps=float("nan")), dict(scales=64), dict(group=8, scales=None),
                                  dict(x=66), dict(dtype=1, x=65), dict(w=66), dict(res=66), dict(xp=-1),
-                                 dict(total=66), dict(rstd=2), dict(rows=1 << 31), dict(out=65)])
+                                 dict(total=66), dict(low=64), dict(dtype=1, low=63),
+                                 dict(dtype=1, group=128, scales=64, low=64), dict(rstd=2), dict(rows=1 << 31), dict(out=65)])
 def test_norm_refusals(bad):
     """Refused before any device work (the pointers are never read)."""
     from paper_1905_00689_gb300 import load
@@ -232,10 +269,10 @@ def test_norm_refusals(bad):
 
 @pytest.mark.parametrize("bad", [dict(dtype=3), dict(dy=None), dict(s=None), dict(w=None), dict(rstd=None),
                                  dict(dx=None), dict(rows=-1), dict(D=0), dict(ws=None), dict(ws=72), dict(nbytes=8),
-                                 dict(dy=66), dict(dsum=65), dict(sp=-4)])
+                                 dict(dy=66), dict(dsum=65), dict(sp=-4), dict(low=64), dict(dtype=1, low=63)])
 def test_norm_backward_refusals(bad):
     from paper_1905_00689_gb300 import load
-    a = dict(dtype=0, dy=64, dyp=8, s=64, sp=8, w=64, rstd=64, dsum=None, dsp=0, rows=2, D=8, dx=64, dw=64, ws=64,
+    a = dict(dtype=0, dy=64, dyp=8, s=64, sp=8, low=None, w=64, rstd=64, dsum=None, dsp=0, rows=2, D=8, dx=64, dw=64, ws=64,
              nbytes=1 << 20)
     a.update(bad)
     msg = ctypes.create_string_buffer(200)
