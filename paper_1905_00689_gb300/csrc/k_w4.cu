@@ -5,7 +5,7 @@
 //   y[m][n] = sum_g scale[n][g] sum_{k in g} (q[n][k] - zero[n][g]) x[m][k]
 //
 // Bound by memory: the 4-bit matrix, which is read once for up to 32 columns
-// (below) at a time.  The products are warp MMAs of 16 rows of W by 16 k by 8
+// of x^T (below) at a time.  The products are warp MMAs of 16 rows of W by 16 k by 8
 // columns of x^T, their operands in registers: tcgen05 takes both operands from
 // shared memory or tensor memory, to which 4-bit weights would first have to be
 // expanded, four bytes written for each byte read.
@@ -25,7 +25,7 @@
 //   sum Each group's sum, in fp32 (8 exact products to an addition), times its
 //       scale, is added to the row's.
 //
-// The tiles of 16 or 32 rows are dealt out evenly over one block of threads per
+// The tiles of 16 rows are dealt out evenly over one block of threads per
 // SM; a block has one warp at least to each of its tiles, and as many more as
 // divide evenly, which share the tile's K and add up through shared memory at
 // the end, always in the same order.  A warp goes on by sets of 4 groups
@@ -69,7 +69,7 @@ struct W4Args {
   int tokens;  // rows of x at a time
   int depth;   // sets in flight or in use to a warp: 2 to 4
   const unsigned char* x_laid;  // x laid out by the kernel before, or null
-  int tiles_each, tiles_more;  // tiles of kMt * 16 rows to a block of threads, and how many blocks have one more
+  int tiles_each, tiles_more;  // tiles of 16 rows to a block of threads, and how many blocks have one more
 };
 
 __device__ __forceinline__ float load_any(const void* p, long long at, int dtype) {
@@ -232,8 +232,9 @@ __global__ void __launch_bounds__(256) w4_lay_out_kernel(const W4Args a, uint4* 
 // Where the w-th of equal stretches (or one longer) begins, each `each` long and the first `more` of them one longer.
 __device__ __forceinline__ int stretch(int w, int each, int more) { return w * each + min(w, more); }
 
-// kX: type of x.  A tile is kMt * 16 rows of W; kNt * 8 columns of x^T.  kSubs = group / 32.
-template <int kX, int kMt, int kNt, int kSubs>
+// kX: type of x.  A tile is 16 rows of W (two to a thread's part: g and g + 8); kNt * 8 columns of x^T.
+// kSubs = group / 32.
+template <int kX, int kNt, int kSubs>
 __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args a) {
   // where x is laid out by the kernel before, W, which that kernel does not write and which was complete before it
   // began, is on its way meanwhile
@@ -242,16 +243,16 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
   constexpr bool kScaled = kX == LSTM_APPROX_OP_E4M3;
   constexpr int kP = kParts<kX>;
   constexpr int kRed = kNt * 8 + 1;         // pitch of the sums
-  constexpr int kSum = kMt * 16 * kRed;     // a tile's sums
+  constexpr int kSum = 16 * kRed;     // a tile's sums
   constexpr int kSets = 4 / kSubs;          // groups of a block; a set is kSubs blocks
   constexpr int kRow = kSubs * 64;          // bytes of a row of a set
-  constexpr int kStage = kMt * 16 * kRow;   // of a set
+  constexpr int kStage = 16 * kRow;   // of a set
   extern __shared__ __align__(128) unsigned char memory[];
   const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int blocks = (a.K + kBlockK - 1) / kBlockK, sets = (blocks + kSubs - 1) / kSubs;
   const int m0 = blockIdx.y * a.tokens, tokens = min(a.tokens, a.M - m0), cols = tokens * kP;
-  // x [blocks][4][cols][4] x 16 bytes, scales of x [blocks][kNt * 8], ring [warps][depth][kMt * 16][kRow], in whose
-  // place the sums [warps][kMt * 16][kRed] go at the end
+  // x [blocks][4][cols][4] x 16 bytes, scales of x [blocks][kNt * 8], ring [warps][depth][16][kRow], in whose
+  // place the sums [warps][16][kRed] go at the end
   uint4* xs = reinterpret_cast<uint4*>(memory);
   float* x_scales = reinterpret_cast<float*>(xs + blocks * 16 * cols);
   unsigned char* rings = reinterpret_cast<unsigned char*>(x_scales + (kScaled ? blocks * kNt * 8 : 0));
@@ -294,11 +295,11 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
 
     // the copies
     int to_set = begin;
-    const uint8_t* from[2 * kMt];
-    long long set_at[2 * kMt];  // of the scales and zero points of the set that is asked for next
+    const uint8_t* from[2];
+    long long set_at[2];  // of the scales and zero points of the set that is asked for next
 #pragma unroll
-    for (int q = 0; q < 2 * kMt; ++q) {
-      const int n = min((tile0 + my_tile) * kMt * 16 + q * 8 + g, a.N - 1);
+    for (int q = 0; q < 2; ++q) {
+      const int n = min((tile0 + my_tile) * 16 + q * 8 + g, a.N - 1);
       from[q] = a.q + n * a.q_pitch + begin * kRow + t * 16;
       set_at[q] = (long long)n * a.groups + begin * 4;
     }
@@ -314,7 +315,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
           // (where x is zero any word will do, a finite number)
           if (whole || (to_set * kSubs + i) * kBlockK + t * 32 < a.K) {
 #pragma unroll
-            for (int q = 0; q < 2 * kMt; ++q)
+            for (int q = 0; q < 2; ++q)
               asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to_stage + q * 8 * kRow +
                                                                              (((i * 4 + t) ^ swizzle) << 4)),
                            "l"(from[q] + i * 64)
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
           }
         }
 #pragma unroll
-        for (int q = 0; q < 2 * kMt; ++q) from[q] += kRow;
+        for (int q = 0; q < 2; ++q) from[q] += kRow;
         ++to_set;
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
@@ -331,17 +332,16 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
     };
     for (int d = 0; d < a.depth - 1; ++d) fetch();
 
-    // Scales (16 bits) and zero points of a set, for rows g and g + 8 of each 16; 32-bit scales are read where they are
-    // used.
+    // Scales (16 bits) and zero points of a set, for rows g and g + 8; 32-bit scales are read where they are used.
     struct Set {
-      uint32_t s[2 * kMt][2], z[2 * kMt];
+      uint32_t s[2][2], z[2];
     };
     const bool wide = a.scale_dtype == LSTM_APPROX_OP_FP32;
     int set_group = begin * 4;
     auto load_set = [&]() {
       Set r;
 #pragma unroll
-      for (int q = 0; q < 2 * kMt; ++q) {
+      for (int q = 0; q < 2; ++q) {
         r.s[q][0] = r.s[q][1] = 0u;
         r.z[q] = 0x08080808u;
         if (a.set_vec) {
@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
       }
     }
 
-    float acc[kMt][kNt][4] = {};
+    float acc[kNt][4] = {};
     const unsigned char* here = ring + g * kRow;
     const unsigned char* const ring_end = here + ring_bytes;
     // a lane whose column of x^T does not exist takes the last one's values; what they lead to is not stored
@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
         const int block = set * kSubs + i;
         if (i > 0 && block >= blocks) break;
         float xsc[kNt][2];
-        float sum[kMt][kNt][4];  // of the block, where x has a scale for each
+        float sum[kNt][4];  // of the block, where x has a scale for each
         if constexpr (kScaled) {
 #pragma unroll
           for (int c = 0; c < kNt; ++c) {
@@ -442,11 +442,11 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
               xs_here[c] += xs_step;
             }
           }
-          float s[2 * kMt];
-          Zero<kBf16> z[2 * kMt];
-          uint32_t w[2 * kMt][kSubs];  // the lane's words of rows g and g + 8 of each 16
+          float s[2];
+          Zero<kBf16> z[2];
+          uint32_t w[2][kSubs];  // the lane's words of rows g and g + 8
 #pragma unroll
-          for (int q = 0; q < 2 * kMt; ++q) {
+          for (int q = 0; q < 2; ++q) {
             const uint32_t bits = held.s[q][e / 2] >> 16 * (e & 1);
             if (wide) s[q] = set * 4 + e < a.groups ? static_cast<const float*>(a.scale)[set_at[q] - 8 + e] : 0.0f;
             else s[q] = a.scale_dtype == LSTM_APPROX_OP_BF16 ? __uint_as_float(bits << 16)
@@ -464,52 +464,42 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
               w[q][0] = *reinterpret_cast<const uint32_t*>(row + ((h ^ swizzle) << 4) + t * 4);
             }
           }
-          float part[kMt][kNt][4];  // (the MMAs of one step belong to different sums)
+          float part[kNt][4];  // (the MMAs of one step belong to different sums)
 #pragma unroll
           for (int k = 0; k < kSubs; ++k) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
+              uint32_t a0, a1, a2, a3;
+              nibbles<kBf16>(w[0][k] >> (8 * half), z[0], a0, a2);
+              nibbles<kBf16>(w[1][k] >> (8 * half), z[1], a1, a3);
 #pragma unroll
-              for (int m = 0; m < kMt; ++m) {
-                uint32_t a0, a1, a2, a3;
-                nibbles<kBf16>(w[2 * m][k] >> (8 * half), z[2 * m], a0, a2);
-                nibbles<kBf16>(w[2 * m + 1][k] >> (8 * half), z[2 * m + 1], a1, a3);
-#pragma unroll
-                for (int c = 0; c < kNt; ++c) {
-                  const uint32_t b0 = half ? b[k][c].z : b[k][c].x, b1 = half ? b[k][c].w : b[k][c].y;
-                  if (k == 0 && half == 0) {
-                    if constexpr (kBf16) mma_16816_bf16<true, true>(part[m][c], a0, a1, a2, a3, b0, b1);
-                    else mma_16816_f16<true, true>(part[m][c], a0, a1, a2, a3, b0, b1);
-                  } else {
-                    if constexpr (kBf16) mma_16816_bf16<true, false>(part[m][c], a0, a1, a2, a3, b0, b1);
-                    else mma_16816_f16<true, false>(part[m][c], a0, a1, a2, a3, b0, b1);
-                  }
+              for (int c = 0; c < kNt; ++c) {
+                const uint32_t b0 = half ? b[k][c].z : b[k][c].x, b1 = half ? b[k][c].w : b[k][c].y;
+                if (k == 0 && half == 0) {
+                  if constexpr (kBf16) mma_16816_bf16<true, true>(part[c], a0, a1, a2, a3, b0, b1);
+                  else mma_16816_f16<true, true>(part[c], a0, a1, a2, a3, b0, b1);
+                } else {
+                  if constexpr (kBf16) mma_16816_bf16<true, false>(part[c], a0, a1, a2, a3, b0, b1);
+                  else mma_16816_f16<true, false>(part[c], a0, a1, a2, a3, b0, b1);
                 }
               }
             }
           }
 #pragma unroll
-          for (int m = 0; m < kMt; ++m) {
+          for (int c = 0; c < kNt; ++c) {
 #pragma unroll
-            for (int c = 0; c < kNt; ++c) {
-#pragma unroll
-              for (int n = 0; n < 4; ++n) {
-                const float scale = s[2 * m + (n >> 1)];
-                if constexpr (kScaled)
-                  sum[m][c][n] = h == 0 ? part[m][c][n] * scale : fmaf(part[m][c][n], scale, sum[m][c][n]);
-                else
-                  acc[m][c][n] = fmaf(part[m][c][n], scale, acc[m][c][n]);
-              }
+            for (int n = 0; n < 4; ++n) {
+              const float scale = s[n >> 1];
+              if constexpr (kScaled) sum[c][n] = h == 0 ? part[c][n] * scale : fmaf(part[c][n], scale, sum[c][n]);
+              else acc[c][n] = fmaf(part[c][n], scale, acc[c][n]);
             }
           }
         }
         if constexpr (kScaled) {
 #pragma unroll
-          for (int m = 0; m < kMt; ++m)
+          for (int c = 0; c < kNt; ++c)
 #pragma unroll
-            for (int c = 0; c < kNt; ++c)
-#pragma unroll
-              for (int n = 0; n < 4; ++n) acc[m][c][n] = fmaf(sum[m][c][n], xsc[c][n & 1], acc[m][c][n]);
+            for (int n = 0; n < 4; ++n) acc[c][n] = fmaf(sum[c][n], xsc[c][n & 1], acc[c][n]);
         }
       }
       here += kStage;
@@ -521,16 +511,14 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
     if (my_tile < tiles) {
       float* to = sums + warp * kSum;
 #pragma unroll
-      for (int m = 0; m < kMt; ++m)
+      for (int c = 0; c < kNt; ++c)
 #pragma unroll
-        for (int c = 0; c < kNt; ++c)
-#pragma unroll
-          for (int n = 0; n < 4; ++n) to[(m * 16 + (n >> 1) * 8 + g) * kRed + c * 8 + 2 * t + (n & 1)] = acc[m][c][n];
+        for (int n = 0; n < 4; ++n) to[((n >> 1) * 8 + g) * kRed + c * 8 + 2 * t + (n & 1)] = acc[c][n];
     }
     __syncthreads();
-    // a warp takes 16 rows, two rows of x at a time
-    for (int sixteen = warp; sixteen < tiles * kMt; sixteen += warps) {
-      const int tile = sixteen / kMt, row = sixteen % kMt * 16 + (lane & 15), out = (tile0 + tile) * kMt * 16 + row;
+    // a warp takes a tile, two rows of x at a time
+    for (int tile = warp; tile < tiles; tile += warps) {
+      const int row = lane & 15, out = (tile0 + tile) * 16 + row;
       if (out >= a.N) continue;
       const float* first = sums + tile * share * kSum + row * kRed;
       const float bias = a.bias ? a.bias[out] : 0.0f;
@@ -626,9 +614,9 @@ constexpr size_t kMostShared = 227 * 1024 - 1024;  // (and a barrier besides)
 constexpr int kMaxK = 32768;  // one row of x in 32 bits then fits beside four warps' sets
 
 // As many rows of x as leave room for four warps with two sets each, then as many warps as fit, then as many sets.
-inline W4Plan plan_matvec(int M, int K, int parts, int mt, int nt, int subs, bool scaled) {
+inline W4Plan plan_matvec(int M, int K, int parts, int nt, int subs, bool scaled) {
   const int blocks = (K + kBlockK - 1) / kBlockK;
-  const size_t sums = mt * 16 * (nt * 8 + 1) * sizeof(float), stage = mt * 1024 * subs;
+  const size_t sums = 16 * (nt * 8 + 1) * sizeof(float), stage = 1024 * subs;
   for (W4Plan p{std::min(M, nt * 8 / parts), 0, 0, 0};; --p.tokens) {
     const size_t x = (size_t)blocks * (256 * p.tokens * parts + (scaled ? 32 * nt : 0));
     const size_t left = x < kMostShared ? kMostShared - x : 0;
@@ -648,18 +636,18 @@ inline size_t laid_out_bytes(int x_dtype, int M, int K) {
   return bytes >= 24 * 1024 ? bytes : 0;
 }
 
-template <int kX, int kMt, int kNt, int kSubs>
+template <int kX, int kNt, int kSubs>
 cudaError_t launch_matvec(W4Args a, unsigned char* workspace, cudaStream_t s) {
   static thread_local DeviceSet ready;  // of the one kernel that this instance launches
-  auto kern = w4_matvec_kernel<kX, kMt, kNt, kSubs>;
+  auto kern = w4_matvec_kernel<kX, kNt, kSubs>;
   cudaError_t e = once_per_device(
       &ready, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostShared); });
   if (e != cudaSuccess) return e;
-  const W4Plan p = plan_matvec(a.M, a.K, kParts<kX>, kMt, kNt, kSubs, kX == LSTM_APPROX_OP_E4M3);
+  const W4Plan p = plan_matvec(a.M, a.K, kParts<kX>, kNt, kSubs, kX == LSTM_APPROX_OP_E4M3);
   if (p.warps < 1) return cudaErrorInvalidValue;
   a.tokens = p.tokens;
   a.depth = p.depth;
-  const int tiles = (a.N + kMt * 16 - 1) / (kMt * 16), across = std::min(tiles, 152);
+  const int tiles = (a.N + 15) / 16, across = std::min(tiles, 152);
   a.tiles_each = tiles / across;
   a.tiles_more = tiles % across;
   if (laid_out_bytes(kX, a.M, a.K) > 0) {
@@ -753,9 +741,9 @@ extern "C" int lstm_approx_w4_matvec(int x_dtype, const void* x, long long x_pit
     const int cols = std::min(M, 32) * kParts<kX>;
     auto of_group = [&](auto subs) {
       constexpr int kSubs = decltype(subs)::value;
-      if (cols <= 8) return launch_matvec<kX, 1, 1, kSubs>(a, ws, s);
-      if (cols <= 16) return launch_matvec<kX, 1, 2, kSubs>(a, ws, s);
-      return launch_matvec<kX, 1, 4, kSubs>(a, ws, s);
+      if (cols <= 8) return launch_matvec<kX, 1, kSubs>(a, ws, s);
+      if (cols <= 16) return launch_matvec<kX, 2, kSubs>(a, ws, s);
+      return launch_matvec<kX, 4, kSubs>(a, ws, s);
     };
     if (group == 128) return of_group(std::integral_constant<int, 4>());
     if (group == 64) return of_group(std::integral_constant<int, 2>());

@@ -15,8 +15,12 @@
 
 namespace lstm_approx_impl {
 
-// The first statement of every kernel that op_launch launches: nothing in memory
-// is read or written before.  The next kernel may be set up from here on.
+// Every kernel is launched before the one ahead of it in the stream has ended
+// (op_launch) and begins with this: it waits for that end and lets the next
+// kernel be set up.  Two kinds of kernel fetch inputs before it, which is sound
+// where another kernel of the same call goes ahead: that one has waited for
+// everything older, and does not write them.  (Small kernels back to back:
+// 4.2 us each launched one after the other's end, so 1.7 to 2.6.)
 __device__ __forceinline__ void begin_op() {
   lstm_approx_dev::griddep_wait();
   lstm_approx_dev::griddep_launch_dependents();
