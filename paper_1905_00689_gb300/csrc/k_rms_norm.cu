@@ -349,7 +349,7 @@ __global__ void __launch_bounds__(kMost) rms_norm_kernel(const NormArgs a) {
   }
 }
 
-constexpr int kMaxRows = 16;  // of a block
+constexpr int kMaxRows = 8;  // of a block
 
 struct NormBackwardArgs {
   const void* dy;
@@ -369,10 +369,14 @@ struct NormBackwardArgs {
 };
 __host__ __device__ constexpr int pitch_of_partial(int D) { return (D + 7) / 8 * 8; }
 
+// Blocks of the backward kernel to an SM.
+template <int VPT, int kMost>
+constexpr int kPerSm = kMost > 256 ? 1 : (VPT == 1 ? 3 : 2);
+
 // A block's rows go on by all blocks' rows; the next one's values are on their way while this one's sum is formed.
 // kLow: s comes with the low parts of sum_out.
 template <typename T, int VPT, int kMost, int kUnit, bool kLow>
-__global__ void __launch_bounds__(kMost, 1) rms_norm_backward_kernel(const NormBackwardArgs a) {
+__global__ void __launch_bounds__(kMost, kPerSm<VPT, kMost>) rms_norm_backward_kernel(const NormBackwardArgs a) {
   begin_op();
   __shared__ float part[2][kMaxRows][32];
   extern __shared__ __align__(16) float merged[];  // [rows of the block][pitch] where there are several
@@ -491,18 +495,19 @@ RowShape row_shape(int D, bool wide) {
   return r;
 }
 
-// The same backward, where a thread holds three tensors' columns: two groups from 1024 columns on.  Short rows share a
-// block of up to 512 threads, so that there are at most 304 blocks' sums to add up.
+// The same backward, where a thread holds three tensors' columns: two groups from 1024 columns on.  Blocks of up to 256
+// threads, of as many rows as fit, and as many blocks as are on the GPU at once (`per_sm`).
 RowShape backward_shape(int D, bool wide) {
   RowShape r;
   const int n = (D + 7) / 8;
-  r.vpt = n > 2048 ? 4 : (n > 512 || (wide && n >= 128) ? 2 : 1);
+  r.vpt = n > 2048 ? 4 : (n > 256 || (wide && n >= 128) ? 2 : 1);
   r.threads = ((n + r.vpt - 1) / r.vpt + 31) / 32 * 32;
-  r.rows_per_block = r.threads == 32 ? kMaxRows : std::max(1, std::min(8, 512 / r.threads));
+  r.rows_per_block = std::max(1, 256 / r.threads);
   return r;
 }
 int backward_blocks(long long rows, const RowShape& r) {
-  return (int)std::min<long long>((rows + r.rows_per_block - 1) / r.rows_per_block, 2 * 152);
+  const int per_sm = r.threads > 256 ? 1 : (r.vpt == 1 ? 768 : 512) / (r.threads * r.rows_per_block);
+  return (int)std::min<long long>((rows + r.rows_per_block - 1) / r.rows_per_block, per_sm * 152);
 }
 
 // Values of an access (see the top): every pointer a multiple of it and every pitch.
@@ -527,6 +532,17 @@ cudaError_t with_shape(const RowShape& r, F f) {
   if (r.vpt == 2 && r.threads <= 512) return f(integral_constant<int, 2>(), integral_constant<int, 512>());
   if (r.vpt == 2) return f(integral_constant<int, 2>(), integral_constant<int, 1024>());
   if (r.threads <= 256) return f(integral_constant<int, 4>(), integral_constant<int, 256>());
+  return f(integral_constant<int, 4>(), integral_constant<int, 1024>());
+}
+
+// The same for the backward kernel's shapes.
+template <typename F>
+cudaError_t with_backward_shape(const RowShape& r, F f) {
+  using std::integral_constant;
+  if (r.vpt == 1) return f(integral_constant<int, 1>(), integral_constant<int, 256>());
+  if (r.vpt == 2 && r.threads <= 256) return f(integral_constant<int, 2>(), integral_constant<int, 256>());
+  if (r.vpt == 2 && r.threads <= 512) return f(integral_constant<int, 2>(), integral_constant<int, 512>());
+  if (r.vpt == 2) return f(integral_constant<int, 2>(), integral_constant<int, 1024>());
   return f(integral_constant<int, 4>(), integral_constant<int, 1024>());
 }
 
@@ -625,7 +641,7 @@ extern "C" int lstm_approx_rms_norm_backward(int dtype, const void* dy, long lon
                        dweight ? static_cast<float*>(workspace) : nullptr, op_aligned(weight, 16)};
     const cudaError_t e = op_for_type(dtype, [&](auto* t) {
       using T = std::remove_pointer_t<decltype(t)>;
-      return with_shape(r, [&](auto vpt, auto most) {
+      return with_backward_shape(r, [&](auto vpt, auto most) {
         constexpr int V = decltype(vpt)::value, M = decltype(most)::value;
         const dim3 block(r.threads, r.rows_per_block);
         auto run = [&](auto low) {
