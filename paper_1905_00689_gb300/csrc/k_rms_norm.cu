@@ -37,9 +37,15 @@ constexpr float kMinScale = 1.17549435e-38f;  // 2^-126
 __device__ __forceinline__ int column(int j) { return (j * (int)blockDim.x + (int)threadIdx.x) * 8; }
 __device__ __forceinline__ int warp_column(int j) { return (j * (int)blockDim.x + (int)(threadIdx.x & ~31u)) * 8; }
 
-// One warp's 256 columns on their way from lane to lane.
+// One warp's 256 columns on their way from lane to lane.  Every second 32 words have the halves of their 8 words
+// exchanged: no two lanes meet in a bank, neither by single words nor when a lane takes 8 words (as 2 x 16 bytes).
 struct Swap {
   float4 v[64];
+
+  __device__ __forceinline__ static int place(int word) { return word ^ (word >> 3 & 4); }
+  __device__ __forceinline__ float& word(int w) { return reinterpret_cast<float*>(v)[place(w)]; }
+  __device__ __forceinline__ float2& pair(int w) { return *reinterpret_cast<float2*>(&word(w)); }
+  __device__ __forceinline__ float4& four(int w) { return *reinterpret_cast<float4*>(&word(w)); }
 };
 template <int kUnit>
 __device__ __forceinline__ Swap& swap_of_warp() {
@@ -93,20 +99,19 @@ struct Raw8 {
     } else {
       const int lane = threadIdx.x & 31;
       Swap& swap = swap_of_warp<kUnit>();
-      float* to = reinterpret_cast<float*>(swap.v);
       __syncwarp();
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
         const float2 f = pair(p);
         if constexpr (kUnit == 2) {
-          *reinterpret_cast<float2*>(to + (p * 32 + lane) * 2) = f;
+          swap.pair((p * 32 + lane) * 2) = f;
         } else {
-          to[2 * p * 32 + lane] = f.x;
-          to[(2 * p + 1) * 32 + lane] = f.y;
+          swap.word(2 * p * 32 + lane) = f.x;
+          swap.word((2 * p + 1) * 32 + lane) = f.y;
         }
       }
       __syncwarp();
-      const float4 lo = swap.v[2 * lane], hi = swap.v[2 * lane + 1];
+      const float4 lo = swap.four(8 * lane), hi = swap.four(8 * lane + 4);
       v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
     }
   }
@@ -120,20 +125,19 @@ __device__ __forceinline__ void put8(T* row, int j, int D, const float (&v)[8]) 
   } else {
     const int lane = threadIdx.x & 31;
     Swap& swap = swap_of_warp<kUnit>();
-    const float* from = reinterpret_cast<const float*>(swap.v);
     __syncwarp();
-    swap.v[2 * lane] = make_float4(v[0], v[1], v[2], v[3]);
-    swap.v[2 * lane + 1] = make_float4(v[4], v[5], v[6], v[7]);
+    swap.four(8 * lane) = make_float4(v[0], v[1], v[2], v[3]);
+    swap.four(8 * lane + 4) = make_float4(v[4], v[5], v[6], v[7]);
     __syncwarp();
 #pragma unroll
     for (int q = 0; q < 8 / kUnit; ++q) {
       const int at = (q * 32 + lane) * kUnit, col = warp_column(j) + at;
       if (col >= D) continue;
       if constexpr (kUnit == 2) {
-        const float2 f = *reinterpret_cast<const float2*>(from + at);
+        const float2 f = swap.pair(at);
         *reinterpret_cast<typename Pair<T>::Raw*>(row + col) = Pair<T>::put(f.x, f.y);
       } else {
-        row[col] = from_f32<T>(from[at]);
+        row[col] = from_f32<T>(swap.word(at));
       }
     }
   }
