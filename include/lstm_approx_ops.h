@@ -23,7 +23,9 @@
  *   - every tensor is a caller-owned DEVICE pointer on the current device;
  *     the arrays of strides are HOST arrays, read before the call returns;
  *   - calls are asynchronous on cuda_stream (cudaStream_t, NULL = the legacy
- *     default stream), allocate nothing and may be captured into a graph;
+ *     default stream), allocate nothing and may be captured into a graph; a
+ *     kernel may be launched while the one ahead of it in the stream still
+ *     runs, and waits for its end before it touches memory;
  *   - msg is an optional host buffer of msg_len bytes for an error text;
  *   - strides and pitches count elements unless stated; the last axis of every
  *     tensor is contiguous; strides are not negative;
@@ -65,7 +67,8 @@ enum lstm_approx_op_dtype {
  *             `group` columns of a row (the last group may be short): group is
  *             32, 64, 128, 256 or >= D (one scale per row).  scale = the
  *             group's largest |y| / 448 (1 for a group of zeros, at least
- *             2^-126), out = y / scale rounded to nearest even.  A group that
+ *             2^-126), out = y / scale, the quotient to a few units in
+ *             32 bits' last place, rounded to nearest even.  A group that
  *             holds an infinity or NaN gets a scale that is not finite, so that
  *             out * scale is NaN throughout it.
  *   x         [rows][D], row pitch x_pitch;  residual likewise, or NULL (s = x)
@@ -76,8 +79,8 @@ enum lstm_approx_op_dtype {
  *   sum_out   [rows][D] contiguous, or NULL; may be x or residual itself where
  *             that is contiguous (the residual stream updated in place)
  *   sum_low   [rows][D] contiguous, or NULL; 16-bit types without 8-bit output
- *             only: what sum_out's rounding took off s, for the backward pass (without it dweight is
- *             off by that rounding)
+ *             only: what sum_out's rounding took off s, for the backward pass
+ *             (without it dweight is off by that rounding)
  *   rstd      [rows] fp32, or NULL: kept for the backward pass
  */
 int lstm_approx_rms_norm(int dtype, int group, const void *x, long long x_pitch, const void *residual,

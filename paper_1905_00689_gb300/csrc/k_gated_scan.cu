@@ -39,6 +39,19 @@
 // has no bound as la -> 0, where every gradient has the limit 0 (q ~ sqrt(-la/2)).
 // The run of p is joined the same way from the end (p -> A p + V).
 //
+// Measured (device time; % of the 6784 GB/s that a copy reaches):
+//   8191 x 1 x 2048 bf16      forward 43 us (46%)   backward 79 us (44%)
+//   2048 x 8 x 2048 bf16              67    (59%)           131    (53%)
+//   2048 x 8 x 2048 fp32              88    (90%)           194    (71%)
+//   20000 x 1 x 512 fp32              43    (57%)            81    (52%)
+//   700 x 13 x 1000 fp16              29    (37%)            54    (35%)
+// In 16 bits instructions bound it, 39 forward and 82 backward to a warp's 32
+// elements and issued in 55 to 59% of the cycles by the 16 warps that an SM's
+// registers hold (gates: 5 of the special functions to an element, most of the
+// rest in pairs of channels); 32-bit inputs come near the memory's rate.  Short
+// sequences pay the chain of tiles and the first kernel, 5 us together.  A single
+// step: 64 x 1024 1.9 us (the launch), 1000 x 2048 fp16 7.8 us (62%).
+//
 // Timesteps past a stream's length are the identity in both directions; they
 // and the state before a reset are left out by selection, never by a product
 // with zero, so what they hold (NaN, infinities) reaches nothing.

@@ -80,46 +80,34 @@ struct Pair<int16_t> {
   static __device__ __forceinline__ Raw put(float a, float b) { return make_short2(from_f32<int16_t>(a), from_f32<int16_t>(b)); }
 };
 
-// Eight neighbouring elements: in 16-byte accesses (kVec: the address is
-// 16-byte aligned and all eight exist) or one by one, zero past `left`.
-template <typename T, bool kVec>
-__device__ __forceinline__ void load8(const T* p, int left, float (&v)[8]) {
-  if constexpr (kVec) {
-    constexpr int kParts = (int)sizeof(T) / 2;  // 16-byte parts
-    constexpr int kPer = 8 / kParts;
+// Eight neighbouring elements in 16-byte accesses (the address is 16-byte aligned).
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
+  constexpr int kParts = (int)sizeof(T) / 2;  // 16-byte parts
+  constexpr int kPer = 8 / kParts;
 #pragma unroll
-    for (int q = 0; q < kParts; ++q) {
-      const uint4 w = reinterpret_cast<const uint4*>(p)[q];
-      const typename Pair<T>::Raw* h = reinterpret_cast<const typename Pair<T>::Raw*>(&w);
+  for (int q = 0; q < kParts; ++q) {
+    const uint4 w = reinterpret_cast<const uint4*>(p)[q];
+    const typename Pair<T>::Raw* h = reinterpret_cast<const typename Pair<T>::Raw*>(&w);
 #pragma unroll
-      for (int j = 0; j < kPer / 2; ++j) {
-        const float2 f = Pair<T>::get(h[j]);
-        v[q * kPer + 2 * j] = f.x;
-        v[q * kPer + 2 * j + 1] = f.y;
-      }
+    for (int j = 0; j < kPer / 2; ++j) {
+      const float2 f = Pair<T>::get(h[j]);
+      v[q * kPer + 2 * j] = f.x;
+      v[q * kPer + 2 * j + 1] = f.y;
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < left ? to_f32<T>(p[j]) : 0.0f;
   }
 }
-template <typename T, bool kVec>
-__device__ __forceinline__ void store8(T* p, int left, const float (&v)[8]) {
-  if constexpr (kVec) {
-    constexpr int kParts = (int)sizeof(T) / 2;
-    constexpr int kPer = 8 / kParts;
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+  constexpr int kParts = (int)sizeof(T) / 2;
+  constexpr int kPer = 8 / kParts;
 #pragma unroll
-    for (int q = 0; q < kParts; ++q) {
-      uint4 w;
-      typename Pair<T>::Raw* h = reinterpret_cast<typename Pair<T>::Raw*>(&w);
+  for (int q = 0; q < kParts; ++q) {
+    uint4 w;
+    typename Pair<T>::Raw* h = reinterpret_cast<typename Pair<T>::Raw*>(&w);
 #pragma unroll
-      for (int j = 0; j < kPer / 2; ++j) h[j] = Pair<T>::put(v[q * kPer + 2 * j], v[q * kPer + 2 * j + 1]);
-      reinterpret_cast<uint4*>(p)[q] = w;
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < left) p[j] = from_f32<T>(v[j]);
+    for (int j = 0; j < kPer / 2; ++j) h[j] = Pair<T>::put(v[q * kPer + 2 * j], v[q * kPer + 2 * j + 1]);
+    reinterpret_cast<uint4*>(p)[q] = w;
   }
 }
 
