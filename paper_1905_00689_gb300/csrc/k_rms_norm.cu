@@ -21,11 +21,13 @@
 // launch and one pass of latencies.
 //
 // A warp moves its 256 columns in accesses of kUnit values: of 8 where every
-// address is a multiple of 16 bytes (a thread's own columns); else of 2 16-bit
-// values at even addresses or of single values, neighbouring lanes next to one
-// another, and the columns change hands through shared memory.  (With a
-// thread's columns fetched one by one, 5001 x 1531 in 32 bits took 48 us
-// forward, with this 25.)  The sums are the same bits in all three.
+// address is a multiple of 16 bytes, 8 neighbouring columns to a thread; else of
+// 2 16-bit values at even addresses or of single values, a thread's columns 64
+// or 32 apart, so that the lanes' lie next to one another.  For the forward
+// pass's sum, and for groups of 8-bit outputs, these change hands through shared
+// memory: the sum has the same bits in all three.  (With 8 neighbouring columns
+// fetched one by one, 5001 x 1531 in 32 bits took 48 us forward; with all four
+// tensors changing hands 25 forward and 32 backward.)
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -43,9 +45,15 @@ constexpr int kMaxD = 32768;
 constexpr float kE4m3Max = 448.0f;
 constexpr float kMinScale = 1.17549435e-38f;  // 2^-126
 
-// Column of the thread's first in group j, and of its warp's first.
+// Column of the thread's first of 8 neighbours in group j, and of its warp's first.
 __device__ __forceinline__ int column(int j) { return (j * (int)blockDim.x + (int)threadIdx.x) * 8; }
 __device__ __forceinline__ int warp_column(int j) { return (j * (int)blockDim.x + (int)(threadIdx.x & ~31u)) * 8; }
+
+// Column of a thread's e-th value in group j.
+template <int kUnit>
+__device__ __forceinline__ int column_of(int j, int e) {
+  return kUnit == 8 ? column(j) + e : warp_column(j) + (e / kUnit * 32 + (int)(threadIdx.x & 31)) * kUnit + e % kUnit;
+}
 
 // One warp's 256 columns on their way from lane to lane.  Every second 32 words have the halves of their 8 words
 // exchanged: no two lanes meet in a bank, neither by single words nor when a lane takes 8 words (as 2 x 16 bytes).
@@ -57,13 +65,31 @@ struct Swap {
   __device__ __forceinline__ float2& pair(int w) { return *reinterpret_cast<float2*>(&word(w)); }
   __device__ __forceinline__ float4& four(int w) { return *reinterpret_cast<float4*>(&word(w)); }
 };
-template <int kUnit>
 __device__ __forceinline__ Swap& swap_of_warp() {
-  __shared__ Swap swaps[kUnit == 8 ? 1 : 32];
-  return swaps[kUnit == 8 ? 0 : (threadIdx.y * blockDim.x + threadIdx.x) >> 5];
+  __shared__ Swap swaps[32];
+  return swaps[(threadIdx.y * blockDim.x + threadIdx.x) >> 5];
 }
 
-// A thread's part of group j as it lies in memory (zero past D), and its 8 columns as fp32.
+// A thread's 8 values in the order of kUnit become those of 8 neighbouring columns; called by whole warps.
+template <int kUnit>
+__device__ __forceinline__ void to_neighbours(float (&v)[8]) {
+  if constexpr (kUnit != 8) {
+    const int lane = threadIdx.x & 31;
+    Swap& swap = swap_of_warp();
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < 8; e += kUnit) {
+      const int at = (e / kUnit * 32 + lane) * kUnit;
+      if constexpr (kUnit == 2) swap.pair(at) = make_float2(v[e], v[e + 1]);
+      else swap.word(at) = v[e];
+    }
+    __syncwarp();
+    const float4 lo = swap.four(8 * lane), hi = swap.four(8 * lane + 4);
+    v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+  }
+}
+
+// A thread's part of group j as it lies in memory (zero past D), and as fp32.
 template <typename T, int kUnit>
 struct Raw8 {
   uint32_t w[8 * sizeof(T) / 4];
@@ -97,68 +123,38 @@ struct Raw8 {
     if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * p]), __uint_as_float(w[2 * p + 1]));
     else return Pair<T>::get(*reinterpret_cast<const typename Pair<T>::Raw*>(&w[p]));
   }
-  // Called by whole warps.
   __device__ __forceinline__ void get(float (&v)[8]) const {
-    if constexpr (kUnit == 8) {
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const float2 f = pair(p);
-        v[2 * p] = f.x;
-        v[2 * p + 1] = f.y;
-      }
-    } else {
-      const int lane = threadIdx.x & 31;
-      Swap& swap = swap_of_warp<kUnit>();
-      __syncwarp();
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const float2 f = pair(p);
-        if constexpr (kUnit == 2) {
-          swap.pair((p * 32 + lane) * 2) = f;
-        } else {
-          swap.word(2 * p * 32 + lane) = f.x;
-          swap.word((2 * p + 1) * 32 + lane) = f.y;
-        }
-      }
-      __syncwarp();
-      const float4 lo = swap.four(8 * lane), hi = swap.four(8 * lane + 4);
-      v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+    for (int p = 0; p < 4; ++p) {
+      const float2 f = pair(p);
+      v[2 * p] = f.x;
+      v[2 * p + 1] = f.y;
     }
   }
 };
-// Stores a thread's 8 columns of group j; called by whole warps.
+// Stores a thread's part of group j.
 template <typename T, int kUnit>
 __device__ __forceinline__ void put8(T* row, int j, int D, const float (&v)[8]) {
   if constexpr (kUnit == 8) {
     const int col = column(j);
     if (col < D) store8(row + col, v);
   } else {
-    const int lane = threadIdx.x & 31;
-    Swap& swap = swap_of_warp<kUnit>();
-    __syncwarp();
-    swap.four(8 * lane) = make_float4(v[0], v[1], v[2], v[3]);
-    swap.four(8 * lane + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    __syncwarp();
 #pragma unroll
-    for (int q = 0; q < 8 / kUnit; ++q) {
-      const int at = (q * 32 + lane) * kUnit, col = warp_column(j) + at;
+    for (int e = 0; e < 8; e += kUnit) {
+      const int col = column_of<kUnit>(j, e);
       if (col >= D) continue;
-      if constexpr (kUnit == 2) {
-        const float2 f = swap.pair(at);
-        *reinterpret_cast<typename Pair<T>::Raw*>(row + col) = Pair<T>::put(f.x, f.y);
-      } else {
-        row[col] = from_f32<T>(swap.word(at));
-      }
+      if constexpr (kUnit == 2) *reinterpret_cast<typename Pair<T>::Raw*>(row + col) = Pair<T>::put(v[e], v[e + 1]);
+      else row[col] = from_f32<T>(v[e]);
     }
   }
 }
+template <int kUnit>
 __device__ __forceinline__ void weights8(const float* w, int j, int D, bool aligned, float (&v)[8]) {
-  const int col = column(j);
-  if (aligned && col + 8 <= D) {
-    load8(w + col, v);
+  if (kUnit == 8 && aligned && column(j) < D) {
+    load8(w + column(j), v);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = col + e < D ? w[col + e] : 0.0f;
+    for (int e = 0; e < 8; ++e) v[e] = column_of<kUnit>(j, e) < D ? w[column_of<kUnit>(j, e)] : 0.0f;
   }
 }
 
@@ -254,7 +250,7 @@ __device__ __forceinline__ uint2 to_e4m3(const float (&y)[8], float scale) {
 }
 
 template <typename T, int VPT, int kMost, int kUnit, bool kQuant>
-__global__ void __launch_bounds__(kMost) rms_norm_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kMost, kMost == 512 && kUnit == 8 ? 3 : 1) rms_norm_kernel(const NormArgs a) {
   begin_op();
   __shared__ float part[32];
   __shared__ unsigned part_max[32];
@@ -285,8 +281,12 @@ __global__ void __launch_bounds__(kMost) rms_norm_kernel(const NormArgs a) {
   float sum = 0.0f;
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
+    float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum = fmaf(s[j][e], s[j][e], sum);
+    for (int e = 0; e < 8; ++e) v[e] = s[j][e];
+    to_neighbours<kUnit>(v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf(v[e], v[e], sum);
   }
   if (a.sum_out) {
     T* so = static_cast<T*>(a.sum_out) + row * a.D;
@@ -310,9 +310,10 @@ __global__ void __launch_bounds__(kMost) rms_norm_kernel(const NormArgs a) {
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
     float w[8];
-    weights8(a.weight, j, a.D, a.weight_vec, w);
+    weights8<kUnit>(a.weight, j, a.D, a.weight_vec, w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[j][e] = s[j][e] * rstd * w[e];
+    if (kQuant) to_neighbours<kUnit>(s[j]);
   }
   if constexpr (!kQuant) {
     T* out = static_cast<T*>(a.out) + row * a.D;
@@ -383,21 +384,17 @@ struct NormBackwardArgs {
 };
 __host__ __device__ constexpr int pitch_of_partial(int D) { return (D + 7) / 8 * 8; }
 
-// Blocks of the backward kernel to an SM.
-template <int VPT, int kMost>
-constexpr int kPerSm = kMost > 256 ? 1 : (VPT == 1 ? 3 : 2);
-
 // A block's rows go on by all blocks' rows; the next one's values are on their way while this one's sum is formed.
 // kLow: s comes with the low parts of sum_out.
 template <typename T, int VPT, int kMost, int kUnit, bool kLow>
-__global__ void __launch_bounds__(kMost, kPerSm<VPT, kMost>) rms_norm_backward_kernel(const NormBackwardArgs a) {
+__global__ void __launch_bounds__(kMost, 1) rms_norm_backward_kernel(const NormBackwardArgs a) {
   begin_op();
   __shared__ float part[2][kMaxRows][32];
   extern __shared__ __align__(16) float merged[];  // [rows of the block][pitch] where there are several
   float w[VPT][8], dw[VPT][8];
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
-    weights8(a.weight, j, a.D, a.weight_vec, w[j]);
+    weights8<kUnit>(a.weight, j, a.D, a.weight_vec, w[j]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[j][e] = 0.0f;
   }
@@ -465,8 +462,7 @@ __global__ void __launch_bounds__(kMost, kPerSm<VPT, kMost>) rms_norm_backward_k
     float* p = a.partial + (long long)blockIdx.x * pitch;
     float* to = blockDim.y == 1 ? p : merged + threadIdx.y * pitch;
 #pragma unroll
-    for (int j = 0; j < VPT; ++j)
-      if (column(j) < a.D) store8(to + column(j), dw[j]);
+    for (int j = 0; j < VPT; ++j) put8<float, kUnit>(to, j, pitch, dw[j]);
     if (blockDim.y > 1) {  // the block's rows, in their order
       __syncthreads();
       for (int col = threadIdx.y * blockDim.x + threadIdx.x; col < a.D; col += blockDim.x * blockDim.y) {
@@ -509,18 +505,20 @@ RowShape row_shape(int D, bool wide) {
   return r;
 }
 
-// The same backward, where a thread holds three tensors' columns: two groups from 1024 columns on.  Blocks of up to 256
-// threads, of as many rows as fit, and as many blocks as are on the GPU at once (`per_sm`).
-RowShape backward_shape(int D, bool wide) {
+// The same backward, where a thread holds three tensors' columns and those of the next row: two groups above 256 of them
+// (16-byte accesses: from 128 on), in 32 bits above 768 (with two groups of 32-bit values, which do not fit in a thread's
+// registers, 3000 x 5001 took 157 us).  Blocks of up to 256 threads, of as many rows as fit, and as many blocks as are on
+// the GPU at once.
+RowShape backward_shape(int D, size_t es, bool wide) {
   RowShape r;
   const int n = (D + 7) / 8;
-  r.vpt = n > 2048 ? 4 : (n > 256 || (wide && n >= 128) ? 2 : 1);
+  r.vpt = n > 2048 ? 4 : (n > (es == 4 ? 768 : 256) || (wide && n >= 128) ? 2 : 1);
   r.threads = ((n + r.vpt - 1) / r.vpt + 31) / 32 * 32;
   r.rows_per_block = std::max(1, 256 / r.threads);
   return r;
 }
 int backward_blocks(long long rows, const RowShape& r) {
-  const int per_sm = r.threads > 256 ? 1 : (r.vpt == 1 ? 768 : 512) / (r.threads * r.rows_per_block);
+  const int per_sm = std::max(1, (r.vpt == 1 ? 768 : 512) / (r.threads * r.rows_per_block));
   return (int)std::min<long long>((rows + r.rows_per_block - 1) / r.rows_per_block, per_sm * 152);
 }
 
@@ -553,8 +551,7 @@ cudaError_t with_shape(const RowShape& r, F f) {
 template <typename F>
 cudaError_t with_backward_shape(const RowShape& r, F f) {
   using std::integral_constant;
-  if (r.vpt == 1) return f(integral_constant<int, 1>(), integral_constant<int, 256>());
-  if (r.vpt == 2 && r.threads <= 256) return f(integral_constant<int, 2>(), integral_constant<int, 256>());
+  if (r.vpt == 1) return f(integral_constant<int, 1>(), integral_constant<int, 768>());
   if (r.vpt == 2 && r.threads <= 512) return f(integral_constant<int, 2>(), integral_constant<int, 512>());
   if (r.vpt == 2) return f(integral_constant<int, 2>(), integral_constant<int, 1024>());
   return f(integral_constant<int, 4>(), integral_constant<int, 1024>());
@@ -618,8 +615,9 @@ extern "C" int lstm_approx_rms_norm(int dtype, int group, const void* x, long lo
 
 extern "C" size_t lstm_approx_rms_norm_workspace_bytes(long long rows, int D) {
   if (rows < 0 || rows > 0x7fffffffll || D < 1 || D > kMaxD) return 0;
-  size_t parts = 0;  // of either shape
-  for (const bool wide : {false, true}) parts = std::max(parts, (size_t)backward_blocks(rows, backward_shape(D, wide)));
+  size_t parts = 0;  // of any of the shapes
+  for (const RowShape& r : {backward_shape(D, 4, false), backward_shape(D, 2, false), backward_shape(D, 2, true)})
+    parts = std::max(parts, (size_t)backward_blocks(rows, r));
   return parts * pitch_of_partial(D) * sizeof(float) + 16;
 }
 
@@ -646,7 +644,7 @@ extern "C" int lstm_approx_rms_norm_backward(int dtype, const void* dy, long lon
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "dweight needs a 16-byte aligned workspace of %zu bytes", need);
   if (int rc = op_check_device(msg, msg_len)) return rc;
   const int unit = unit_of(D, es, {{dy, dy_pitch}, {s, s_pitch}, {s_low, D}, {dsum, dsum_pitch}, {dx, D}});
-  const RowShape r = backward_shape(D, unit == 8 && es == 2);
+  const RowShape r = backward_shape(D, es, unit == 8 && es == 2);
   const int blocks = backward_blocks(rows, r);
   const size_t smem = r.rows_per_block > 1 ? (size_t)r.rows_per_block * pitch_of_partial(D) * sizeof(float) : 0;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
