@@ -12,12 +12,12 @@
 //
 // Measured (device time, of the 6784 GB/s that a copy reaches): forward with
 // residual, sum and output, 8192 x 4096 bf16 42 us (94%), 4000 x 7168 fp32 70 us
-// (96%), 5001 x 1531 fp32 25 us (72%: unaligned rows, bound by the L1 that the
-// exchange between lanes goes through); with 8-bit output 8192 x 4096 46 us
+// (96%), 5001 x 1531 fp32 24 us (76%: unaligned rows in single values); with 8-bit output 8192 x 4096 46 us
 // (75%: the conversions).  With the sum's low parts kept for the backward
 // pass, 8192 x 4096 bf16 52 us (95%).  Backward, 8192 x 4096 bf16 49 us (80%), 20000 x
-// 512 20 us (61%), 5001 x 1531 fp32 32 us (56%): every row's sum is a barrier, behind which only the next row's loads
-// are under way, and the column sums take 2 to 3 us more.  One token: 2.8 us, the
+// 512 20 us (61%), 5001 x 1531 fp32 27 us (67%), 3000 x 7001 fp32 75 us (67%): every
+// row's sum is a barrier, behind which only the next row's loads are under way,
+// and the column sums take 2 to 3 us more.  One token: 2.8 us, the
 // launch and one pass of latencies.
 //
 // A warp moves its 256 columns in accesses of kUnit values: of 8 where every
@@ -384,11 +384,13 @@ struct NormBackwardArgs {
 };
 __host__ __device__ constexpr int pitch_of_partial(int D) { return (D + 7) / 8 * 8; }
 
-// A block's rows go on by all blocks' rows; the next one's values are on their way while this one's sum is formed.
+// A block's rows go on by all blocks' rows; the next one's values are on their way while this one's sum is formed,
+// except of the widest rows, of which one alone keeps an SM's loads busy.
 // kLow: s comes with the low parts of sum_out.
 template <typename T, int VPT, int kMost, int kUnit, bool kLow>
 __global__ void __launch_bounds__(kMost, 1) rms_norm_backward_kernel(const NormBackwardArgs a) {
   begin_op();
+  constexpr bool kAhead = VPT * sizeof(T) < 8;  // else a thread's registers do not hold the next row's values too
   __shared__ float part[2][kMaxRows][32];
   extern __shared__ __align__(16) float merged[];  // [rows of the block][pitch] where there are several
   float w[VPT][8], dw[VPT][8];
@@ -419,11 +421,12 @@ __global__ void __launch_bounds__(kMost, 1) rms_norm_backward_kernel(const NormB
     }
     rstd = a.rstd[row];
   };
-  if (row < a.rows) load(row);
+  if (kAhead && row < a.rows) load(row);
   int turn = 0;
   for (; row < a.rows; row += step) {
     float g[VPT][8], v[VPT][8], r[VPT][8];
     float sum = 0.0f;
+    if (!kAhead) load(row);
     const float scale = rstd;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
@@ -445,7 +448,7 @@ __global__ void __launch_bounds__(kMost, 1) rms_norm_backward_kernel(const NormB
         sum = fmaf(g[j][e], v[j][e], sum);
       }
     }
-    if (row + step < a.rows) load(row + step);
+    if (kAhead && row + step < a.rows) load(row + step);
     sum = row_sum<true>(sum, part[turn][threadIdx.y]);
     turn ^= 1;  // the next row's sums may be written while slow threads still read this row's
     const float mean = sum / (float)a.D;
@@ -506,8 +509,7 @@ RowShape row_shape(int D, bool wide) {
 }
 
 // The same backward, where a thread holds three tensors' columns and those of the next row: two groups above 256 of them
-// (16-byte accesses: from 128 on), in 32 bits above 768 (with two groups of 32-bit values, which do not fit in a thread's
-// registers, 3000 x 5001 took 157 us).  Blocks of up to 256 threads, of as many rows as fit, and as many blocks as are on
+// (16-byte accesses: from 128 on), in 32 bits above 768 (with two groups of 32-bit values 3000 x 5001 took 54 us, with one 47).  Blocks of up to 256 threads, of as many rows as fit, and as many blocks as are on
 // the GPU at once.
 RowShape backward_shape(int D, size_t es, bool wide) {
   RowShape r;
