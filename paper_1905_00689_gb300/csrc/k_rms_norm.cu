@@ -15,7 +15,7 @@
 // (96%), 5001 x 1531 fp32 24 us (76%: unaligned rows in single values); with 8-bit output 8192 x 4096 46 us
 // (75%: the conversions).  With the sum's low parts kept for the backward
 // pass, 8192 x 4096 bf16 52 us (95%).  Backward, 8192 x 4096 bf16 49 us (80%), 20000 x
-// 512 20 us (61%), 5001 x 1531 fp32 27 us (67%), 3000 x 7001 fp32 75 us (67%): every
+// 512 20 us (61%), 5001 x 1531 fp32 26.5 us (68%), 3000 x 7001 fp32 75 us (67%): every
 // row's sum is a barrier, behind which only the next row's loads are under way,
 // and the column sums take 2 to 3 us more.  One token: 2.8 us, the
 // launch and one pass of latencies.
@@ -477,20 +477,28 @@ __global__ void __launch_bounds__(kMost, 1) rms_norm_backward_kernel(const NormB
   }
 }
 
-// Column sums of partial [n][pitch_of_partial(D)], in a fixed order.
+// Column sums of partial [n][pitch_of_partial(D)], in a fixed order: kColumns columns to a block, 1024 / kColumns rows at a
+// time.  8 columns up to 2048 of them, so that the few blocks have few loads one behind the other, else 32 (backward pass
+// of 20000 x 512 bf16 19.1 us with 8, 20.0 with 32; of 3000 x 8192 bf16 41.9 and 38.0).
+template <int kColumns>
 __global__ void __launch_bounds__(1024) column_sum_kernel(const float* partial, int n, int D, float* out) {
   begin_op();
-  __shared__ float acc[32][33];
-  const int col = blockIdx.x * 32 + threadIdx.x;
+  constexpr int kRows = 1024 / kColumns;
+  __shared__ float acc[kRows][kColumns + 1];
+  const int col = blockIdx.x * kColumns + threadIdx.x;
   float v = 0.0f;
   if (col < D)
-#pragma unroll 4
-    for (int k = threadIdx.y; k < n; k += 32) v += partial[(long long)k * pitch_of_partial(D) + col];
+#pragma unroll 8
+    for (int k = threadIdx.y; k < n; k += kRows) v += partial[(long long)k * pitch_of_partial(D) + col];
   acc[threadIdx.y][threadIdx.x] = v;
   __syncthreads();
-  v = warp_sum(acc[threadIdx.x][threadIdx.y]);
-  const int c = blockIdx.x * 32 + threadIdx.y;
-  if (threadIdx.x == 0 && c < D) out[c] = v;
+  const int t = threadIdx.y * kColumns + threadIdx.x, c = t >> 5, lane = t & 31;  // a warp to a column
+  if (c >= kColumns) return;
+  v = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kRows; k += 32) v += acc[k + lane][c];
+  v = warp_sum(v);
+  if (lane == 0 && blockIdx.x * kColumns + c < D) out[blockIdx.x * kColumns + c] = v;
 }
 
 // Threads of a row and the groups of 8 columns of each.
@@ -673,7 +681,8 @@ extern "C" int lstm_approx_rms_norm_backward(int dtype, const void* dy, long lon
     if (int rc = op_launched(e, "norm backward launch", msg, msg_len)) return rc;
   }
   if (!dweight) return LSTM_APPROX_OK;
-  const cudaError_t e = op_launch(column_sum_kernel, dim3((D + 31) / 32), dim3(32, 32), 0, st,
-                                  static_cast<const float*>(workspace), blocks, D, dweight);
+  const int columns = D <= 2048 ? 8 : 32;
+  const cudaError_t e = op_launch(columns == 8 ? column_sum_kernel<8> : column_sum_kernel<32>, dim3((D + columns - 1) / columns),
+                                  dim3(columns, 1024 / columns), 0, st, static_cast<const float*>(workspace), blocks, D, dweight);
   return op_launched(e, "weight gradient launch", msg, msg_len);
 }

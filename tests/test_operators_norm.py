@@ -174,6 +174,27 @@ def test_norm_backward(cuda_device, rows, D, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,at", [("fp32", 0), ("fp32", 1), ("bf16", 0), ("bf16", 1), ("fp16", 2)])
+@pytest.mark.parametrize("rows,D", [(400, 2056), (330, 4104), (310, 6144), (310, 6160), (200, 8200), (160, 16392)])
+def test_norm_backward_of_wide_rows(cuda_device, rows, D, dtype, at):
+    """Widths on both sides of those where the columns are dealt out otherwise, several rows to a block of threads,
+    out of wider tensors at every alignment; the gradients are those of contiguous copies to a few roundoffs."""
+    import torch
+    from paper_1905_00689_gb300 import rms_norm, rms_norm_backward
+    w = weight(D)
+    dy, s, dsum = (make(rows, D + 8, dtype, 71 + k)[:, at:at + D] for k in range(3))
+    rstd = torch.empty(rows, device="cuda")
+    rms_norm(s, w, eps=1e-5, rstd=rstd)
+    dx, dw = rms_norm_backward(dy, s, w, rstd, dsum)
+    want, want_dw = ref.norm_backward(ref.f64(dy), ref.f64(s), ref.f64(w), ref.f64(dsum), 1e-5)
+    r = 1 / np.sqrt((ref.f64(s) ** 2).mean(1, keepdims=True) + 1e-5)
+    wdy, xhat = np.abs(ref.f64(dy) * ref.f64(w)), np.abs(ref.f64(s)) * r
+    mag = r * (wdy + xhat * (wdy * xhat).mean(1, keepdims=True)) + np.abs(ref.f64(dsum))
+    ref.check(dx, want, mag, 2 * TOL, dtype, "dx")
+    ref.check(dw, want_dw, (np.abs(ref.f64(dy)) * xhat).sum(0), 2 * TOL, what="dw")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("rows,D", [(40, 64), (300, 1000), (65, 333), (20, 30)])
 def test_norm_backward_of_a_16_bit_sum(cuda_device, rows, D, dtype):
