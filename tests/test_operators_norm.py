@@ -312,3 +312,40 @@ def test_norm_wrapper_refusals(cuda_device):
                  lambda: rms_norm_quant(x, w, group=0)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.gpu
+def test_sum_low_is_not_stale(cuda_device):
+    """A sum that an operator, a view or a copy overwrites no longer counts as the one its sum_low belongs to; what torch
+    does not see moves the gradients by no more than the sum's rounding; a sum_low of another shape is left alone."""
+    import torch
+    from paper_1905_00689_gb300 import rms_norm, rms_norm_backward
+    rows, D = 64, 256
+    x, res, dy, w = (make(rows, D, "bf16", 81), make(rows, D, "bf16", 82), make(rows, D, "bf16", 83), weight(D))
+    rstd, rstd2 = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+
+    def sum_of():
+        return rms_norm(x, w, res, rstd=rstd)[1]
+
+    def overwritten(total):
+        clean = total.clone()
+        rms_norm(clean, w, rstd=rstd2)
+        return all(torch.equal(a, b) for a, b in zip(rms_norm_backward(dy, total, w, rstd2),
+                                                     rms_norm_backward(dy, clean, w, rstd2)))
+    for change in (lambda t: rms_norm(x, w, out=t), lambda t: t[3:5].zero_(), lambda t: t.view(-1).copy_(x.view(-1)),
+                   lambda t: rms_norm_backward(dy, x, w, rstd, dx=t)):
+        total = sum_of()
+        change(total)
+        assert overwritten(total)
+    total = sum_of()
+    assert not overwritten(total)
+    other = sum_of()
+    other.sum_low = other.sum_low[:32]
+    assert overwritten(other)
+    # behind torch's back: within half a unit in the last place of every value
+    total = sum_of()
+    total.data.copy_(x)
+    rms_norm(x, w, rstd=rstd2)
+    got, want = rms_norm_backward(dy, total, w, rstd2)[1].double(), rms_norm_backward(dy, x, w, rstd2)[1].double()
+    bound = (dy.double().abs() * x.double().abs() * rstd2.double()[:, None]).sum(0) * 2.0 ** -8
+    assert bool(((got - want).abs() <= 1.01 * bound).all())

@@ -405,3 +405,38 @@ def test_scan_wrapper_refusals(cuda_device):
                  lambda: gated_step(x[0], r[0], i[0], decay, h0.t().contiguous().t())):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("axis", ["t", "b"])
+def test_offsets_past_32_bits(cuda_device, axis):
+    """Timesteps or streams 2^31 elements apart, forward and backward, and a state pool of more than 2^31 values."""
+    import torch
+    from paper_1905_00689_gb300 import gated_scan, gated_scan_backward, gated_scan_states, gated_step
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    T, B, D = (2, 3, 64) if axis == "t" else (70, 2, 64)
+    strides = (1 << 31, D, 1) if axis == "t" else (D, 1 << 31, 1)
+    decay = torch.rand(D, generator=gen, device="cuda") - 5.0
+    z = torch.randn(4, T, B, D, generator=gen, device="cuda").to(torch.bfloat16)
+    far = [torch.empty((1 << 31) + 16 * T * B * D, dtype=torch.bfloat16, device="cuda").as_strided((T, B, D), strides, k)
+           for k in (0, 0, 2, 1)]  # (three of the kinds of alignment)
+    for to, values in zip(far, z):
+        to.copy_(values)
+    x, r, i, dy = far
+    states = [gated_scan_states(T, B, D) for _ in range(2)]
+    y = gated_scan(x, r, i, decay, states=states[0])
+    want = gated_scan(z[0], z[1], z[2], decay, states=states[1])
+    assert torch.equal(y[0], want[0]) and torch.equal(y[1], want[1]) and torch.equal(*states)
+    out = torch.empty((1 << 31) + 16 * T * B * D, dtype=torch.bfloat16, device="cuda").as_strided((T, B, D), strides)
+    got = gated_scan_backward(dy, x, r, i, decay, states[0], dx=out)
+    want = gated_scan_backward(z[3], z[0], z[1], z[2], decay, states[1])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    del far, x, r, i, dy, out, to, got
+    n = (1 << 31) // D + 3
+    state = torch.zeros(n, D, device="cuda")
+    slots = torch.tensor([n - 1, 0], device="cuda", dtype=torch.int32)
+    h = torch.randn(2, D, generator=gen, device="cuda")
+    state[slots.long()] = h
+    y = gated_step(z[0, 0, :2], z[1, 0, :2], z[2, 0, :2], decay, state, slots=slots)
+    assert torch.equal(y, gated_step(z[0, 0, :2], z[1, 0, :2], z[2, 0, :2], decay, h))
+    assert torch.equal(state[slots.long()], h)

@@ -212,3 +212,15 @@ def test_w4_wrapper_refusals(cuda_device):
                  lambda: w4_quantize(x[0]), lambda: w4_quantize(x, scale_dtype=torch.float64)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.gpu
+def test_rows_past_32_bits(cuda_device):
+    """Rows of W 2^27 bytes apart, 20 of them: offsets past 2^31."""
+    import torch
+    from paper_1905_00689_gb300 import W4Weight, w4_matvec
+    near = matrix(20, 100, 32, 8)
+    q = torch.empty((20 << 27), dtype=torch.uint8, device="cuda").as_strided((20, near.q.shape[1]), (1 << 27, 1))
+    q.copy_(near.q)
+    x = rows(2, 100, "bf16", 9)
+    assert torch.equal(w4_matvec(x, W4Weight(q, near.scale, near.zero, 100, 32)), w4_matvec(x, near))
