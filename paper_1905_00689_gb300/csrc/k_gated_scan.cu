@@ -492,8 +492,10 @@ struct Join {                             // shared memory of a block
 };
 
 // Brings what a task needs from other tiles into shared memory, one run to a warp, and this tile's run out to them;
-// `mine`: the warps' runs of this tile, in the direction of the scan from warp `w0` in steps of `dw`.  Returns this
-// tile's run in warp 0.  The block meets in a barrier before and after.
+// `mine`: the warps' runs of this tile, in the direction of the scan from warp `w0` in steps of `dw`.  `first`: the
+// state before the sequence, in warp 0 of its first tile, whose run it goes into: no other tile reads it, and what
+// the sequence ends in follows from that run, so that the state may be overwritten by the sequence's last.  Returns
+// this tile's run (without `first`) in warp 0.  The block meets in a barrier before and after.
 template <bool kCuts>
 __device__ __forceinline__ ulonglong2 exchange_runs(const Tasks& t, const Exchange& e, const Task& at, Join& sm,
                                                     const ulonglong2 (&mine)[kWarps][32], int w0, int dw, uint64_t first) {
@@ -505,9 +507,12 @@ __device__ __forceinline__ ulonglong2 exchange_runs(const Tasks& t, const Exchan
     all = mine[w0][lane];
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) all = join<kCuts>(all, mine[w0 + dw * w][lane]);
-    if (!ends_group(t, at) && at.order != t.tiles - 1) publish(e.runs + (at.order * items + item) * 32 + lane, all);
+    if (!ends_group(t, at) && at.order != t.tiles - 1)
+      publish(e.runs + (at.order * items + item) * 32 + lane,
+              at.order == 0 ? make_ulonglong2(all.x, after<kCuts>(all, first)) : all);
+    if (group == 0) sm.start[lane] = first;
   }
-  if (warp == kWarps - 1) sm.start[lane] = group == 0 ? first : receive(e.states + ((group - 1) * items + item) * 32 + lane);
+  if (warp == kWarps - 1 && group > 0) sm.start[lane] = receive(e.states + ((group - 1) * items + item) * 32 + lane);
   for (int q = warp; q < place; q += kWarps)
     sm.before[q][lane] = receive(e.runs + ((long long)(at.order - place + q) * items + item) * 32 + lane);
   return all;
@@ -634,6 +639,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const __grid
     const long long state_at = (long long)at.b * t.D + ch;
     const unsigned resets = kCuts ? reset_bits<kSteps>(a.reset, ts, len, at.b, t.B) : 0u;
     const bool whole = ts + kSteps <= len;
+    uint64_t first = 0ull;
+    if (warp == 0 && at.order == 0 && a.h0) first = load_f32x2(a.h0 + state_at, left);
     const T* here = loader.part(turn) + 2 * lane;
     const bool there = loader.wait(turn, parity);
     parity ^= turn;
@@ -650,8 +657,6 @@ __global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const __grid
     if (!there) U[0] = both(kNaN);
     sm.runs[turn][warp][lane] = kCuts && resets ? join_steps<true>(A, U, resets) : join_steps<false>(A, U, 0u);
     __syncthreads();
-    uint64_t first = 0ull;
-    if (warp == kWarps - 1 && at.order >> t.group_log2 == 0 && a.h0) first = load_f32x2(a.h0 + state_at, left);
     const ulonglong2 tile = exchange_runs<kCuts>(t, a.exchange, at, sm, sm.runs[turn], 0, 1, first);
     if (warp == 2) {
       ahead = advance(t, ahead, step);
@@ -821,6 +826,8 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
     const unsigned resets = kCuts ? reset_bits<kSteps>(a.reset, ts, len, at.b, t.B) : 0u;
     const bool whole = ts + kSteps <= len, some = ts < len;
     T* here = loader.part(turn) + 2 * lane;
+    uint64_t first = 0ull;
+    if (warp == 0 && at.order == 0 && a.dh_last) first = load_f32x2(a.dh_last + state_at, left);
     uint64_t h = some ? load_f32x2(a.states + (long long)tile * t.B * t.D + state_at, left) : 0ull;
     const bool there = loader.wait(turn, parity);
     parity ^= turn;
@@ -846,8 +853,6 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
     sm.runs[turn][warp][lane] = make_ulonglong2(PA, PV);
     __syncthreads();
     if (warp == 1 && any) add_up(done);
-    uint64_t first = 0ull;
-    if (warp == kWarps - 1 && at.order >> t.group_log2 == 0 && a.dh_last) first = load_f32x2(a.dh_last + state_at, left);
     const ulonglong2 run = exchange_runs<kCuts>(t, a.exchange, at, sm, sm.runs[turn], kWarps - 1, -1, first);
     if (warp == 2) {
       ahead_task = advance(t, ahead_task, step);
