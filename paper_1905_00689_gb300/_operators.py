@@ -81,9 +81,10 @@ def rms_norm_backward(dy, s, weight, rstd, dsum=None, *, dx=None, dweight=None, 
     s is the forward call's sum (x itself without a residual), rstd what it
     wrote there, dsum the gradient that reaches s by another way.  dx is the
     gradient of x and of the residual alike; it may be dy or dsum itself.
-    Where s has a ``sum_low`` and has not been changed since, the gradients are
-    those of the sum before its rounding to 16 bits; else (a copy, say) dweight
-    is off by that rounding.
+    Where s has a ``sum_low`` and s and rstd are what that call left, neither of
+    them changed or copied since, the gradients are those of the sum before its
+    rounding to 16 bits; else (a copy, say) dweight is off by that rounding.  A
+    further norm of s itself has an rstd of its own: its gradients are at s.
     """
     args = (dy, s, weight, rstd, dsum, dx, dweight, workspace)
     return _ops.rms_norm_backward(*args) if stream is None else _on(stream, _ops.rms_norm_backward, *args)

@@ -175,32 +175,48 @@ PyObject* wrap_all(const Ts&... ts) {
   return nullptr;
 }
 
-// A 16-bit sum of rms_norm that a backward pass will read carries what its rounding took off as its attribute `sum_low`,
-// with the version that the sum had then.  After a change of the sum in place, by torch or by an operator here, it no
-// longer counts.  (A change that torch does not see does little: a low part moves a value by half a unit in the last
-// place of the 16-bit type at most.)
-PyObject *g_sum_low = nullptr, *g_sum_low_version = nullptr;
+// A 16-bit sum of rms_norm that a backward pass will read carries what its rounding took off as its attribute `sum_low`.
+// It belongs to that one call: beside it stand the version that the sum had then and the call's rstd with its version
+// (a tuple).  It counts for the backward pass of that rstd only: another norm of the same sum, without a residual, read
+// the rounded values.  After a change of either in place, by torch or by an operator here, it no longer counts.  (A
+// change that torch does not see does little: a low part moves a value by half a unit in the last place of the 16-bit
+// type at most.)
+PyObject *g_sum_low = nullptr, *g_sum_low_call = nullptr;
 
-bool set_sum_low(PyObject* sum, const Tensor& t, const std::optional<Tensor>& low) {
-  if (!low) return !PyObject_HasAttr(sum, g_sum_low) || PyObject_DelAttr(sum, g_sum_low) == 0;  // an earlier call's
-  PyObject *v = wrap(*low), *n = v ? PyLong_FromLongLong(t._version()) : nullptr;
-  const bool ok = n && PyObject_SetAttr(sum, g_sum_low, v) == 0 && PyObject_SetAttr(sum, g_sum_low_version, n) == 0;
+bool set_sum_low(PyObject* sum, const Tensor& t, const std::optional<Tensor>& low, PyObject* rstd) {
+  if (!low) {  // an earlier call's
+    for (PyObject* name : {g_sum_low, g_sum_low_call})
+      if (PyObject_HasAttr(sum, name) && PyObject_DelAttr(sum, name) != 0) return false;
+    return true;
+  }
+  PyObject* v = wrap(*low);
+  PyObject* call = v ? Py_BuildValue("LOL", (long long)t._version(), rstd, (long long)tensor(rstd, "rstd")._version()) : nullptr;
+  const bool ok = call && PyObject_SetAttr(sum, g_sum_low, v) == 0 && PyObject_SetAttr(sum, g_sum_low_call, call) == 0;
   Py_XDECREF(v);
-  Py_XDECREF(n);
+  Py_XDECREF(call);
   return ok;
 }
-std::optional<Tensor> get_sum_low(PyObject* sum, const Tensor& t) {
+// Whether the call noted beside the low part left the sum t and this rstd, both unchanged since.
+bool is_sum_low_call(PyObject* call, const Tensor& t, const Tensor& rstd) {
+  if (!call || !PyTuple_Check(call) || PyTuple_GET_SIZE(call) != 3) return false;
+  PyObject *version = PyTuple_GET_ITEM(call, 0), *of = PyTuple_GET_ITEM(call, 1), *of_version = PyTuple_GET_ITEM(call, 2);
+  if (!PyLong_Check(version) || !THPVariable_Check(of) || !PyLong_Check(of_version)) return false;
+  const Tensor& r = THPVariable_Unpack(of);
+  return PyLong_AsLongLong(version) == (long long)t._version() && !r.is_inference() &&
+         PyLong_AsLongLong(of_version) == (long long)r._version() && rstd.is_alias_of(r) && rstd.data_ptr() == r.data_ptr();
+}
+std::optional<Tensor> get_sum_low(PyObject* sum, const Tensor& t, const Tensor& rstd) {
   std::optional<Tensor> found;
   if (t.is_inference() || !PyObject_HasAttr(sum, g_sum_low)) return found;
-  PyObject *v = PyObject_GetAttr(sum, g_sum_low), *n = PyObject_GetAttr(sum, g_sum_low_version);
-  if (v && n && THPVariable_Check(v) && PyLong_Check(n) && PyLong_AsLongLong(n) == (long long)t._version()) {
+  PyObject *v = PyObject_GetAttr(sum, g_sum_low), *call = PyObject_GetAttr(sum, g_sum_low_call);
+  if (v && THPVariable_Check(v) && is_sum_low_call(call, t, rstd)) {
     const Tensor& low = THPVariable_Unpack(v);
     if (low.scalar_type() == at::kShort && low.sizes() == t.sizes() && low.device() == t.device() &&
         low.is_contiguous() && t.is_contiguous())
       found = low;
   }
   Py_XDECREF(v);
-  Py_XDECREF(n);
+  Py_XDECREF(call);
   PyErr_Clear();
   return found;
 }
@@ -238,13 +254,14 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t) {
     }
     Tensor out = call.out(a[5], "out", group > 0 ? at::kFloat8_e4m3fn : type, shape);
     std::optional<Tensor> low;  // where a backward pass will follow (rstd is asked for) and s has more than 16 bits
-    if (pr && rstd && group == 0 && type != at::kFloat && !total->is_inference()) low = call.out(Py_None, "", at::kShort, shape);
+    if (pr && rstd && group == 0 && type != at::kFloat && !total->is_inference() && !tensor(a[8], "rstd").is_inference())
+      low = call.out(Py_None, "", at::kShort, shape);
     call.done(lstm_approx_rms_norm(code, (int)group, px, pitch, pr, res_pitch, static_cast<const float*>(pw), real(a[3]),
                                    rows, (int)D, out.data_ptr(), scales ? scales->data_ptr<float>() : nullptr,
                                    total ? total->data_ptr() : nullptr, low ? low->data_ptr<int16_t>() : nullptr, rstd,
                                    call.stream, call.msg, sizeof(call.msg)));
     PyObject* result = wrap_all(out, scales, total);
-    if (result && total && !set_sum_low(PyTuple_GET_ITEM(result, 2), *total, low)) Py_CLEAR(result);
+    if (result && total && !set_sum_low(PyTuple_GET_ITEM(result, 2), *total, low, a[8])) Py_CLEAR(result);
     return result;
   });
 }
@@ -262,7 +279,8 @@ PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t) {
     need(D <= 0x7fffffff, "D must be a 32-bit number");
     const Tensor& s = tensor(a[1], "s");
     void *pdy = call.rows(dy, "dy", type, shape), *ps = call.rows(s, "s", type, shape), *pd = nullptr;
-    const std::optional<Tensor> low = type != at::kFloat ? get_sum_low(a[1], s) : std::nullopt;
+    const Tensor& rs = tensor(a[3], "rstd");
+    const std::optional<Tensor> low = type != at::kFloat ? get_sum_low(a[1], s, rs) : std::nullopt;
     if (low) low->record_stream(c10::Stream(c10::cuda::getCurrentCUDAStream(call.device.index())));
     long long d_pitch = 0;
     if (a[4] != Py_None) {
@@ -271,7 +289,7 @@ PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t) {
       d_pitch = pitch_of(d, "dsum");
     }
     const float* w = static_cast<const float*>(call.dense(tensor(a[2], "weight"), "weight", at::kFloat, {D}));
-    const float* rstd = static_cast<const float*>(call.dense(tensor(a[3], "rstd"), "rstd", at::kFloat, lead));
+    const float* rstd = static_cast<const float*>(call.dense(rs, "rstd", at::kFloat, lead));
     Tensor dx = call.out(a[5], "dx", type, shape), dw = call.out(a[6], "dweight", at::kFloat, {D});
     Tensor ws = call.workspace(a[7], lstm_approx_rms_norm_workspace_bytes(rows, (int)D));
     call.done(lstm_approx_rms_norm_backward(code, pdy, pitch_of(dy, "dy"), ps, pitch_of(s, "s"),
@@ -503,6 +521,6 @@ PyMODINIT_FUNC PyInit__torch_ops() {
   g_error = PyObject_GetAttrString(binding, "LSTMApproxError");
   Py_DECREF(binding);
   g_sum_low = PyUnicode_InternFromString("sum_low");
-  g_sum_low_version = PyUnicode_InternFromString("sum_low_version");
-  return g_error && g_sum_low && g_sum_low_version ? PyModule_Create(&g_module) : nullptr;
+  g_sum_low_call = PyUnicode_InternFromString("_sum_low_call");
+  return g_error && g_sum_low && g_sum_low_call ? PyModule_Create(&g_module) : nullptr;
 }
