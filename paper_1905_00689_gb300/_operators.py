@@ -48,18 +48,24 @@ def _on(stream, function, *args):
 # ---------------------------------------------------------------------------
 # norm
 
-def rms_norm(x, weight, residual=None, *, eps: float = 1e-6, out=None, residual_out=None, rstd=None, stream=None):
+def rms_norm(x, weight, residual=None, *, eps: float = 1e-6, out=None, residual_out=None, rstd=None, sum_low=None,
+             stream=None):
     """Root-mean-square norm over the last axis of s = x (+ residual):
     s / sqrt(mean(s^2) + eps) * weight.
 
     x, residual [..., D] fp32, bf16 or fp16; weight [D] fp32.  Returns (out,
     s): s in x's type, None without a residual (and without residual_out).
     ``residual_out`` may be ``residual`` itself; ``rstd`` [...] fp32 receives
-    1 / sqrt(mean(s^2) + eps) for :func:`rms_norm_backward`.  With ``rstd`` and a
-    residual in 16 bits, s has what its rounding took off as its attribute
-    ``sum_low`` (int16, for the backward pass).
+    1 / sqrt(mean(s^2) + eps) for :func:`rms_norm_backward`.
+
+    ``sum_low``: with ``rstd`` and a residual in 16 bits, s has what its rounding
+    took off as its attribute ``sum_low`` (int16 [..., D], for the backward pass:
+    2 bytes a value written and kept).  False: it is not made.  A tensor: it
+    is written there, for callers that keep it themselves, since an attribute
+    stays with this one tensor object (``save_for_backward`` of an output loses
+    it).
     """
-    args = (x, weight, residual, eps, 0, out, None, residual_out, rstd)
+    args = (x, weight, residual, eps, 0, out, None, residual_out, rstd, sum_low)
     out, _, total = _ops.rms_norm(*args) if stream is None else _on(stream, _ops.rms_norm, *args)
     return out, total
 
@@ -71,11 +77,12 @@ def rms_norm_quant(x, weight, residual=None, *, eps: float = 1e-6, group: int = 
     q * scale ~ the norm's output.  group: 32, 64, 128, 256 or >= D.
     """
     _need(group > 0, "group must be positive")
-    args = (x, weight, residual, eps, group, out, scales, residual_out, rstd)
+    args = (x, weight, residual, eps, group, out, scales, residual_out, rstd, False)
     return _ops.rms_norm(*args) if stream is None else _on(stream, _ops.rms_norm, *args)
 
 
-def rms_norm_backward(dy, s, weight, rstd, dsum=None, *, dx=None, dweight=None, workspace=None, stream=None):
+def rms_norm_backward(dy, s, weight, rstd, dsum=None, *, sum_low=None, dx=None, dweight=None, workspace=None,
+                      stream=None):
     """Gradients of :func:`rms_norm`: (dx, dweight).
 
     s is the forward call's sum (x itself without a residual), rstd what it
@@ -85,8 +92,9 @@ def rms_norm_backward(dy, s, weight, rstd, dsum=None, *, dx=None, dweight=None, 
     them changed or copied since, the gradients are those of the sum before its
     rounding to 16 bits; else (a copy, say) dweight is off by that rounding.  A
     further norm of s itself has an rstd of its own: its gradients are at s.
+    ``sum_low``: the forward call's, where the caller kept it; False: none.
     """
-    args = (dy, s, weight, rstd, dsum, dx, dweight, workspace)
+    args = (dy, s, weight, rstd, dsum, dx, dweight, workspace, sum_low)
     return _ops.rms_norm_backward(*args) if stream is None else _on(stream, _ops.rms_norm_backward, *args)
 
 

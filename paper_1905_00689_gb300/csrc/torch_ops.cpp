@@ -221,7 +221,8 @@ std::optional<Tensor> get_sum_low(PyObject* sum, const Tensor& t, const Tensor& 
   return found;
 }
 
-// rms_norm(x, weight, residual, eps, group, out, scales, residual_out, rstd) -> (out, scales, residual_out)
+// rms_norm(x, weight, residual, eps, group, out, scales, residual_out, rstd, sum_low) -> (out, scales, residual_out)
+// (sum_low: None where it is made as needed, False, or the tensor for it)
 PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t) {
   return guarded([&]() -> PyObject* {
     const Tensor& x = tensor(a[0], "x");
@@ -253,20 +254,28 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t) {
       scales = call.out(a[6], "scales", at::kFloat, sizes);
     }
     Tensor out = call.out(a[5], "out", group > 0 ? at::kFloat8_e4m3fn : type, shape);
-    std::optional<Tensor> low;  // where a backward pass will follow (rstd is asked for) and s has more than 16 bits
-    if (pr && rstd && group == 0 && type != at::kFloat && !total->is_inference() && !tensor(a[8], "rstd").is_inference())
-      low = call.out(Py_None, "", at::kShort, shape);
+    std::optional<Tensor> low;
+    if (a[9] == Py_None) {  // where a backward pass will follow (rstd is asked for) and s has more than 16 bits
+      if (pr && rstd && group == 0 && type != at::kFloat && !total->is_inference() && !tensor(a[8], "rstd").is_inference())
+        low = call.out(Py_None, "", at::kShort, shape);
+    } else if (a[9] != Py_False) {
+      need(total && type != at::kFloat && group == 0, "sum_low is for the 16-bit sum of x and a residual");
+      low = call.out(a[9], "sum_low", at::kShort, shape);
+    }
     call.done(lstm_approx_rms_norm(code, (int)group, px, pitch, pr, res_pitch, static_cast<const float*>(pw), real(a[3]),
                                    rows, (int)D, out.data_ptr(), scales ? scales->data_ptr<float>() : nullptr,
                                    total ? total->data_ptr() : nullptr, low ? low->data_ptr<int16_t>() : nullptr, rstd,
                                    call.stream, call.msg, sizeof(call.msg)));
     PyObject* result = wrap_all(out, scales, total);
+    // one that the caller handed over without an rstd is the caller's alone
+    if (low && (!rstd || total->is_inference() || tensor(a[8], "rstd").is_inference())) low.reset();
     if (result && total && !set_sum_low(PyTuple_GET_ITEM(result, 2), *total, low, a[8])) Py_CLEAR(result);
     return result;
   });
 }
 
-// rms_norm_backward(dy, s, weight, rstd, dsum, dx, dweight, workspace) -> (dx, dweight)
+// rms_norm_backward(dy, s, weight, rstd, dsum, dx, dweight, workspace, sum_low) -> (dx, dweight)
+// (sum_low: None where s brings its own along, False, or that of the forward call)
 PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t) {
   return guarded([&]() -> PyObject* {
     const Tensor& dy = tensor(a[0], "dy");
@@ -280,7 +289,14 @@ PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t) {
     const Tensor& s = tensor(a[1], "s");
     void *pdy = call.rows(dy, "dy", type, shape), *ps = call.rows(s, "s", type, shape), *pd = nullptr;
     const Tensor& rs = tensor(a[3], "rstd");
-    const std::optional<Tensor> low = type != at::kFloat ? get_sum_low(a[1], s, rs) : std::nullopt;
+    std::optional<Tensor> low;
+    if (a[8] == Py_None) {
+      if (type != at::kFloat) low = get_sum_low(a[1], s, rs);
+    } else if (a[8] != Py_False) {
+      need(type != at::kFloat, "sum_low is for 16-bit sums");
+      low = tensor(a[8], "sum_low");
+      call.dense(*low, "sum_low", at::kShort, shape);
+    }
     if (low) low->record_stream(c10::Stream(c10::cuda::getCurrentCUDAStream(call.device.index())));
     long long d_pitch = 0;
     if (a[4] != Py_None) {
@@ -505,7 +521,7 @@ PyMethodDef entry(const char* name) {
 }
 
 PyMethodDef g_methods[] = {
-    entry<rms_norm, 9>("rms_norm"),           entry<rms_norm_backward, 8>("rms_norm_backward"),
+    entry<rms_norm, 10>("rms_norm"),          entry<rms_norm_backward, 9>("rms_norm_backward"),
     entry<gated_scan, 12>("gated_scan"),      entry<gated_scan_backward, 16>("gated_scan_backward"),
     entry<gated_step, 9>("gated_step"),       entry<w4_quantize, 5>("w4_quantize"),
     entry<w4_matvec, 12>("w4_matvec"),        {nullptr, nullptr, 0, nullptr},

@@ -84,3 +84,56 @@ def test_low_part_of_another_shape_or_behind_a_change(cuda_device):
     got, want = rms_norm_backward(dy, total, w, rstd)[1].double(), rms_norm_backward(dy, x, w, rstd)[1].double()
     bound = (dy.double().abs() * x.double().abs() * rstd.double()[:, None]).sum(0) * 2.0 ** -8
     assert not torch.equal(got, want) and bool(((got - want).abs() <= 1.01 * bound).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_low_part_kept_by_the_caller(cuda_device, dtype):
+    """Through save_for_backward the sum comes back as another object, without its attribute: the low part handed over
+    by itself gives the same gradients.  It can be declined, and refused tensors are refused."""
+    import torch
+    from paper_1905_00689_gb300 import rms_norm, rms_norm_backward, rms_norm_quant
+    x, res, dy, w = make(ROWS, D, dtype, 91), make(ROWS, D, dtype, 92, std=3.0), make(ROWS, D, dtype, 93), weight(D)
+
+    class Norm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, res, w):
+            rstd, low = torch.empty(x.shape[:-1], device="cuda"), torch.empty_like(x, dtype=torch.int16)
+            y, total = rms_norm(x, w, res, eps=1e-5, rstd=rstd, sum_low=low)
+            ctx.save_for_backward(total, w, rstd, low)
+            return y, total
+
+        @staticmethod
+        def backward(ctx, dy, dtotal):
+            total, w, rstd, low = ctx.saved_tensors
+            dx, dw = rms_norm_backward(dy, total, w, rstd, dtotal, sum_low=low)
+            return dx, dx, dw
+    for t in (x, res, w):
+        t.requires_grad_()
+    y, total = Norm.apply(x, res, w)
+    y.backward(dy)
+    s = ref.f64(x) + ref.f64(res)
+    compare((x.grad, w.grad), dy, s, w, dtype)
+    assert torch.equal(x.grad, res.grad)
+    x, res, w = x.detach(), res.detach(), w.detach()
+    rstd, low = torch.empty(ROWS, device="cuda"), torch.full((ROWS, D), 77, dtype=torch.int16, device="cuda")
+    _, total = rms_norm(x, w, res, eps=1e-5, rstd=rstd, sum_low=low)
+    assert total.sum_low is low
+    want = rms_norm_backward(dy, total, w, rstd)
+    plain = rms_norm_backward(dy, total.clone(), w, rstd)
+    same = lambda a, b: all(torch.equal(u, v) for u, v in zip(a, b))  # noqa: E731
+    assert not same(want, plain)
+    assert same(rms_norm_backward(dy, total.clone(), w, rstd, sum_low=low), want)
+    assert same(rms_norm_backward(dy, total, w, rstd, sum_low=False), plain)
+    _, bare = rms_norm(x, w, res, eps=1e-5, rstd=rstd, sum_low=False)
+    assert not hasattr(bare, "sum_low") and torch.equal(bare, total)
+    _, bare = rms_norm(x, w, res, eps=1e-5, sum_low=low.zero_())  # no rstd: the caller's alone
+    assert not hasattr(bare, "sum_low") and same(rms_norm_backward(dy, bare, w, rstd, sum_low=low), want)
+    for call in (lambda: rms_norm(x, w, res, rstd=rstd, sum_low=low.int()), lambda: rms_norm(x, w, res, rstd=rstd, sum_low=low[:3]),
+                 lambda: rms_norm(x, w, sum_low=low), lambda: rms_norm(x.float(), w, res.float(), rstd=rstd, sum_low=low),
+                 lambda: rms_norm(x, w, res, rstd=rstd, sum_low=True),
+                 lambda: rms_norm_backward(dy, total, w, rstd, sum_low=low.t()),
+                 lambda: rms_norm_backward(dy.float(), total.float(), w, rstd, sum_low=low)):
+        with pytest.raises(ValueError):
+            call()
+    assert not hasattr(rms_norm_quant(x, w, res, rstd=rstd)[2], "sum_low")
