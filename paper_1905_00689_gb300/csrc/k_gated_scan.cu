@@ -118,26 +118,31 @@ __device__ __forceinline__ uint64_t sigmoid2(uint64_t z, const Constants& k) {
 }
 
 // The gates of a lane's two channels (pairs of fp32, two per instruction where
-// there is one for two): sigma(r), sigma(i) and 1 - a, from which a and m
-// follow.  rate = c softplus(decay), the largest -log a; far: it is above 1/8.
+// there is one for two): sigma(r), sigma(i), a and 1 - a, from which m
+// follows.  rate = c softplus(decay), the largest t = -log a of a channel.
 //
 // 1 - a = 1 - e^-t by its Taylor series: no cancellation, a = 1 - (1 - a)
 // comes out correctly rounded, which matters where a state decays over hundreds
 // of timesteps, and 1 - a^2 = (1 - a)(1 + a) keeps its digits.  Up to t = 1/8
 // (decays down to 0.88 where the gate is open) five terms do (the sixth is
 // below 4.3e-8 of the first); beyond, eight up to t = 0.35 (the ninth is below
-// 7e-10), and the exponential itself above that.
+// 7e-10).  Above that a is the exponential itself, within 2^-22 + t 2^-23 of its
+// size, and 1 - a follows from it: a small a is a factor of all that goes back
+// through the timestep, and 1 - (1 - a) would leave it to a multiple of 2^-24.
+// What a warp has to do goes by the largest rate of its channels:
+enum Reach { kNear, kMiddle, kFar };  // up to 1/8, up to 0.35, above
+constexpr float kNearRate = 0.125f, kMiddleRate = 0.35f;
+//
+// Sigma is formed from the hardware's exponential and reciprocal: within 2^-21
+// + |z| 2^-24 of its size (2e-6 at |z| = 20).
 struct Gates {
-  uint64_t sr, si, low;
+  uint64_t sr, si, a, low;  // low: 1 - a
 };
-template <bool kFar>
-__device__ __forceinline__ Gates gates_of(uint64_t r, uint64_t i, uint64_t rate, const Constants& k) {
-  Gates g;
-  g.sr = sigmoid2(r, k);
-  g.si = sigmoid2(i, k);
-  const uint64_t t = mul2(rate, g.sr);
+// The series.
+template <Reach kReach>
+__device__ __forceinline__ uint64_t low_series(uint64_t t, const Constants& k) {
   uint64_t p = k.c4;
-  if constexpr (kFar) {
+  if constexpr (kReach != kNear) {
     p = both(-1.0f / 40320.0f);
     p = fma2(p, t, both(1.0f / 5040.0f));
     p = fma2(p, t, both(-1.0f / 720.0f));
@@ -147,18 +152,45 @@ __device__ __forceinline__ Gates gates_of(uint64_t r, uint64_t i, uint64_t rate,
   p = fma2(p, t, k.c2);
   p = fma2(p, t, k.c1);
   p = fma2(p, t, k.one);
-  g.low = mul2(t, p);
-  if constexpr (kFar) {
-    float t0, t1, l0, l1;
+  return mul2(t, p);
+}
+template <Reach kReach>
+__device__ __forceinline__ Gates gates_of(uint64_t r, uint64_t i, uint64_t rate, const Constants& k) {
+  Gates g;
+  g.sr = sigmoid2(r, k);
+  g.si = sigmoid2(i, k);
+  const uint64_t t = mul2(rate, g.sr);
+  g.low = low_series<kReach>(t, k);
+  g.a = sub2(k.one, g.low);
+  if constexpr (kReach == kFar) {
+    float t0, t1, a0, a1, l0, l1;
     f32x2_split(t, t0, t1);
+    f32x2_split(g.a, a0, a1);
     f32x2_split(g.low, l0, l1);
-    if (t0 > 0.35f) l0 = 1.0f - ex2_approx(-t0 * kLog2E);
-    if (t1 > 0.35f) l1 = 1.0f - ex2_approx(-t1 * kLog2E);
+    if (t0 > kMiddleRate) a0 = ex2_approx(-t0 * kLog2E), l0 = 1.0f - a0;
+    if (t1 > kMiddleRate) a1 = ex2_approx(-t1 * kLog2E), l1 = 1.0f - a1;
+    g.a = f32x2(a0, a1);
     g.low = f32x2(l0, l1);
   }
   return g;
 }
-__device__ __forceinline__ uint64_t decay_of(uint64_t low, const Constants& k) { return sub2(k.one, low); }
+// What the backward pass keeps of a timestep's decay: 1 - a, from which a follows, but a itself where it may be small
+// (kFar), and then 1 - a is formed again from t.
+template <Reach kReach>
+__device__ __forceinline__ uint64_t held_decay(const Gates& g) { return kReach == kFar ? g.a : g.low; }
+template <Reach kReach>
+__device__ __forceinline__ uint64_t decay_of(uint64_t held, const Constants& k) {
+  return kReach == kFar ? held : sub2(k.one, held);
+}
+template <Reach kReach>
+__device__ __forceinline__ uint64_t low_of(uint64_t held, uint64_t t, const Constants& k) {
+  if constexpr (kReach != kFar) return held;
+  float t0, t1, a0, a1, l0, l1;
+  f32x2_split(t, t0, t1);
+  f32x2_split(held, a0, a1);
+  f32x2_split(low_series<kReach>(t, k), l0, l1);
+  return f32x2(t0 > kMiddleRate ? 1.0f - a0 : l0, t1 > kMiddleRate ? 1.0f - a1 : l1);
+}
 // 1 - a^2
 __device__ __forceinline__ uint64_t m2_of(uint64_t low, uint64_t a, const Constants& k) {
   return mul2(low, add2(a, k.one));
@@ -560,7 +592,7 @@ __device__ __forceinline__ void store_both(T* p, int left, uint64_t v) {
 }
 
 // a_t and m_t sigma(i_t) x_t of a warp's staged timesteps.
-template <typename T, bool kFar, int kSteps>
+template <typename T, Reach kReach, int kSteps>
 __device__ __forceinline__ void form_runs(const T* here, uint64_t rate, const Constants& k, uint64_t (&A)[kSteps],
                                           uint64_t (&U)[kSteps]) {
   constexpr int kOne = kWarps * kSteps * kLanes;  // values of one staged tensor
@@ -568,9 +600,9 @@ __device__ __forceinline__ void form_runs(const T* here, uint64_t rate, const Co
   for (int s = 0; s < kSteps; ++s) {
     const T* p = here + s * kLanes;
     const Gates g =
-        gates_of<kFar>(staged_pair<T>(p + kOne), staged_pair<T>(p + 2 * kOne), rate, k);
-    A[s] = decay_of(g.low, k);
-    const uint64_t m2 = m2_of(g.low, A[s], k);
+        gates_of<kReach>(staged_pair<T>(p + kOne), staged_pair<T>(p + 2 * kOne), rate, k);
+    A[s] = g.a;
+    const uint64_t m2 = m2_of(g.low, g.a, k);
     U[s] = mul2(mul2(mul2(m2, rsqrt2(m2)), g.si), staged_pair<T>(p));
   }
 }
@@ -593,11 +625,19 @@ __device__ __forceinline__ ulonglong2 join_steps(const uint64_t (&A)[kSteps], co
 __device__ __forceinline__ uint64_t rate_of(const float* decay, int left, float c) {
   return f32x2(left > 0 ? c * softplus_f(decay[0]) : 0.0f, left > 1 ? c * softplus_f(decay[1]) : 0.0f);
 }
-// Whether -log a of some lane may be above 1/8.
-__device__ __forceinline__ bool any_far(uint64_t rate) {
+// How far -log a may be from zero in some lane, the same in all of them (kFar also for a NaN).
+__device__ __forceinline__ Reach reach_of(uint64_t rate) {
   float r0, r1;
   f32x2_split(rate, r0, r1);
-  return __any_sync(0xffffffffu, !(r0 <= 0.125f && r1 <= 0.125f));
+  if (!__any_sync(0xffffffffu, !(r0 <= kNearRate && r1 <= kNearRate))) return kNear;
+  return __any_sync(0xffffffffu, !(r0 <= kMiddleRate && r1 <= kMiddleRate)) ? kFar : kMiddle;
+}
+// f(the reach as a constant)
+template <typename F>
+__device__ __forceinline__ void with_reach(Reach reach, F f) {
+  if (reach == kNear) f(std::integral_constant<Reach, kNear>());
+  else if (reach == kMiddle) f(std::integral_constant<Reach, kMiddle>());
+  else f(std::integral_constant<Reach, kFar>());
 }
 
 template <typename T, int kCopy, bool kCuts>
@@ -646,8 +686,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) gated_scan_kernel(const __grid
     parity ^= turn;
     uint64_t A[kSteps], U[kSteps];
     if (ts < len) {
-      if (any_far(rate)) form_runs<T, true>(here, rate, k, A, U);
-      else form_runs<T, false>(here, rate, k, A, U);
+      with_reach(reach_of(rate), [&](auto reach) { form_runs<T, decltype(reach)::value>(here, rate, k, A, U); });
     }
     if (!whole) {
 #pragma unroll
@@ -715,39 +754,39 @@ struct ScanBackwardArgs {
   float* partial;  // [tiles][B][slabs * 64]: each tile's sum of E
 };
 
-// 1 - a_t, the gates and m_t sigma(i_t) x_t of a warp's staged timesteps.
-template <typename T, bool kFar, int kSteps>
-__device__ __forceinline__ void form_gates(const T* here, uint64_t rate, const Constants& k, uint64_t (&low)[kSteps],
+// a_t (see held_decay), the gates and m_t sigma(i_t) x_t of a warp's staged timesteps.
+template <typename T, Reach kReach, int kSteps>
+__device__ __forceinline__ void form_gates(const T* here, uint64_t rate, const Constants& k, uint64_t (&held)[kSteps],
                                            uint64_t (&sr)[kSteps], uint64_t (&si)[kSteps], uint64_t (&U)[kSteps]) {
   constexpr int kOne = kWarps * kSteps * kLanes;
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
     const T* p = here + s * kLanes;
     const Gates g =
-        gates_of<kFar>(staged_pair<T>(p + kOne), staged_pair<T>(p + 2 * kOne), rate, k);
-    low[s] = g.low;
+        gates_of<kReach>(staged_pair<T>(p + kOne), staged_pair<T>(p + 2 * kOne), rate, k);
+    held[s] = held_decay<kReach>(g);
     sr[s] = g.sr;
     si[s] = g.si;
-    const uint64_t m2 = m2_of(g.low, decay_of(g.low, k), k);
+    const uint64_t m2 = m2_of(g.low, g.a, k);
     U[s] = mul2(mul2(mul2(m2, rsqrt2(m2)), g.si), staged_pair<T>(p));
   }
 }
 
 // The runs of a warp's timesteps, h -> A h + U forward and p -> A p + V back
 // (staged dy is zero past the stream's length; kCuts: with a reset, one at least).
-template <typename T, bool kCuts, int kSteps>
-__device__ __forceinline__ void join_both(const T* here, const uint64_t (&low)[kSteps], const uint64_t (&U)[kSteps],
+template <typename T, Reach kReach, bool kCuts, int kSteps>
+__device__ __forceinline__ void join_both(const T* here, const uint64_t (&held)[kSteps], const uint64_t (&U)[kSteps],
                                           unsigned resets, const Constants& k, uint64_t& PA, uint64_t& PU, uint64_t& PV) {
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
-    const uint64_t A = decay_of(low[s], k);
+    const uint64_t A = decay_of<kReach>(held[s], k);
     if (kCuts && (resets >> s & 1u)) PU = 0ull;
     PU = fma2(A, PU, U[s]);
     PA = mul2(PA, A);
   }
 #pragma unroll
   for (int s = kSteps - 1; s >= 0; --s) {
-    PV = mul2(decay_of(low[s], k), add2(PV, staged_pair<T>(here + 3 * kWarps * kSteps * kLanes + s * kLanes)));
+    PV = mul2(decay_of<kReach>(held[s], k), add2(PV, staged_pair<T>(here + 3 * kWarps * kSteps * kLanes + s * kLanes)));
     if (kCuts && (resets >> s & 1u)) PV = 0ull;
   }
   if (kCuts) PA = both(-1.0f);
@@ -758,14 +797,14 @@ struct Gradients {
 };
 // The gradients of the staged timestep at `here`, from p after it, which
 // becomes p before it; h: the state before it.
-template <typename T>
-__device__ __forceinline__ Gradients gradients_of(const T* here, uint64_t low, uint64_t sr, uint64_t si, uint64_t h,
+template <typename T, Reach kReach>
+__device__ __forceinline__ Gradients gradients_of(const T* here, uint64_t held, uint64_t sr, uint64_t si, uint64_t h,
                                                   uint64_t rate, const Constants& k, uint64_t& p) {
-  const uint64_t A = decay_of(low, k), xs = staged_pair<T>(here);
+  const uint64_t A = decay_of<kReach>(held, k), xs = staged_pair<T>(here);
   const uint64_t g = add2(p, staged_pair<T>(here + 3 * kWarps * kBackwardSteps * kLanes));
   p = mul2(g, A);
-  const uint64_t m2 = m2_of(low, A, k), inv_m = rsqrt2(m2);
   const uint64_t t = mul2(rate, sr);  // -log a
+  const uint64_t m2 = m2_of(low_of<kReach>(held, t, k), A, k), inv_m = rsqrt2(m2);
   Gradients d;
   d.E = mul2(mul2(p, t), sub2(mul2(mul2(mul2(si, xs), A), inv_m), h));  // g a t (si x a / m - h)
   d.x = mul2(g, mul2(mul2(m2, inv_m), si));
@@ -831,23 +870,29 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
     uint64_t h = some ? load_f32x2(a.states + (long long)tile * t.B * t.D + state_at, left) : 0ull;
     const bool there = loader.wait(turn, parity);
     parity ^= turn;
-    uint64_t low[kSteps], sr[kSteps], si[kSteps], U[kSteps], PA = k.one, PU = 0ull, PV = 0ull;
+    const Reach reach = reach_of(rate);
+    uint64_t held[kSteps], sr[kSteps], si[kSteps], U[kSteps], PA = k.one, PU = 0ull, PV = 0ull;
     if (some) {
-      if (any_far(rate)) form_gates<T, true>(here, rate, k, low, sr, si, U);
-      else form_gates<T, false>(here, rate, k, low, sr, si, U);
+      with_reach(reach, [&](auto at_most) { form_gates<T, decltype(at_most)::value>(here, rate, k, held, sr, si, U); });
       if (!whole) {
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
           if (ts + s >= len) {
-            low[s] = U[s] = 0ull;
+            held[s] = reach == kFar ? k.one : 0ull;  // a = 1
+            U[s] = 0ull;
             here[3 * kOne + s * kLanes] = here[3 * kOne + s * kLanes + 1] = from_f32<T>(0.0f);  // dy
           }
         }
         if (kCopy == 16) fence_proxy_async_shared();  // before a later bulk copy to the same place
       }
-      if (!there) low[0] = both(kNaN);
-      if (kCuts && resets) join_both<T, true>(here, low, U, resets, k, PA, PU, PV);
-      else join_both<T, false>(here, low, U, 0u, k, PA, PU, PV);
+      if (!there) held[0] = both(kNaN);
+      auto join = [&](auto at_most) {
+        constexpr Reach kReach = decltype(at_most)::value;
+        if (kCuts && resets) join_both<T, kReach, true>(here, held, U, resets, k, PA, PU, PV);
+        else join_both<T, kReach, false>(here, held, U, 0u, k, PA, PU, PV);
+      };
+      if (reach == kFar) join(std::integral_constant<Reach, kFar>());
+      else join(std::integral_constant<Reach, kMiddle>());
     }
     ahead[turn][warp][lane] = make_ulonglong2(PA, PU);
     sm.runs[turn][warp][lane] = make_ulonglong2(PA, PV);
@@ -883,7 +928,8 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
     T* to_r = reinterpret_cast<T*>(plan.tensors[5]) + last * sr_t + 2 * lane;
     T* to_i = reinterpret_cast<T*>(plan.tensors[6]) + last * si_t + 2 * lane;
     uint64_t sum = 0ull;
-    if (some) {
+    auto gradients = [&](auto at_most) {
+      constexpr Reach kReach = decltype(at_most)::value;
       // U becomes the state before each timestep
       if (kCuts && resets) {
 #pragma unroll
@@ -891,20 +937,20 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
           if (resets >> s & 1u) h = 0ull;
           const uint64_t u = U[s];
           U[s] = h;
-          h = fma2(decay_of(low[s], k), h, u);
+          h = fma2(decay_of<kReach>(held[s], k), h, u);
         }
       } else {
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
           const uint64_t u = U[s];
           U[s] = h;
-          h = fma2(decay_of(low[s], k), h, u);
+          h = fma2(decay_of<kReach>(held[s], k), h, u);
         }
       }
       if (whole && left > 0) {
 #pragma unroll
         for (int s = kSteps - 1; s >= 0; --s) {
-          const Gradients g = gradients_of<T>(here + s * kLanes, low[s], sr[s], si[s], U[s], rate, k, p);
+          const Gradients g = gradients_of<T, kReach>(here + s * kLanes, held[s], sr[s], si[s], U[s], rate, k, p);
           if (kCuts && (resets >> s & 1u)) p = 0ull;
           sum = add2(sum, g.E);
           store_both<T, kVec>(to_x, left, g.x);
@@ -918,7 +964,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
 #pragma unroll
         for (int s = kSteps - 1; s >= 0; --s) {
           Gradients g = {0ull, 0ull, 0ull, 0ull};
-          if (ts + s < len) g = gradients_of<T>(here + s * kLanes, low[s], sr[s], si[s], U[s], rate, k, p);
+          if (ts + s < len) g = gradients_of<T, kReach>(here + s * kLanes, held[s], sr[s], si[s], U[s], rate, k, p);
           if (kCuts && (resets >> s & 1u)) p = 0ull;
           sum = add2(sum, g.E);
           if (left > 0 && ts + s < t.T) {
@@ -931,6 +977,10 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 4 ? 1 : 2) gated_sca
           to_i -= si_t;
         }
       }
+    };
+    if (some) {
+      if (reach == kFar) gradients(std::integral_constant<Reach, kFar>());
+      else gradients(std::integral_constant<Reach, kMiddle>());
     } else if (left > 0) {
       for (int s = kSteps - 1; s >= 0; --s, to_x -= sx, to_r -= sr_t, to_i -= si_t) {
         if (ts + s >= t.T) continue;
@@ -1019,9 +1069,9 @@ __global__ void __launch_bounds__(256) gated_step_kernel(const StepArgs a) {
         store_pair<T, kVec>(y, left, 0.0f, 0.0f);
         continue;
       }
-      const Gates g = gates_of<true>(f32x2(r[n].x, r[n].y), f32x2(i[n].x, i[n].y), rate, k);
-      const uint64_t A = decay_of(g.low, k), m2 = m2_of(g.low, A, k);
-      const uint64_t after = fma2(A, h[n], mul2(mul2(mul2(m2, rsqrt2(m2)), g.si), f32x2(x[n].x, x[n].y)));
+      const Gates g = gates_of<kFar>(f32x2(r[n].x, r[n].y), f32x2(i[n].x, i[n].y), rate, k);
+      const uint64_t m2 = m2_of(g.low, g.a, k);
+      const uint64_t after = fma2(g.a, h[n], mul2(mul2(mul2(m2, rsqrt2(m2)), g.si), f32x2(x[n].x, x[n].y)));
       store_f32x2(a.state + (long long)slot[n] * a.D + ch, left, after);
       store_both<T, kVec>(y, left, after);
     }
