@@ -20,6 +20,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "liblstm_approx.so")
 MODULE = os.path.join(HERE, "_torch_ops.so")
+MODULE_FOR = os.path.join(BUILD, "torch_ops.torch")  # what the module was compiled for, see _torch_abi
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -45,6 +46,8 @@ def _deps():
 def up_to_date() -> bool:
     if not (os.path.exists(LIB) and os.path.exists(MODULE)):
         return False
+    if not os.path.exists(MODULE_FOR) or open(MODULE_FOR).read() != _torch_abi():
+        return False
     t = min(os.path.getmtime(LIB), os.path.getmtime(MODULE))
     return all(os.path.getmtime(p) <= t for p in _deps())
 
@@ -62,6 +65,12 @@ def _torch_dir() -> str:
     if spec is None:
         raise RuntimeError("torch not found")
     return spec.submodule_search_locations[0]
+
+
+def _torch_abi() -> str:
+    """The torch and the Python that the module is for: with another one of either it may not load."""
+    with open(os.path.join(_torch_dir(), "version.py")) as f:
+        return f"{f.read()}\n{sysconfig.get_config_var('SOABI')}\n"
 
 
 def _compile_module() -> str:
@@ -99,6 +108,8 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
     _run(["g++", "-shared", "-o", tmp, module_obj, "-L" + os.path.join(_torch_dir(), "lib"), "-ltorch", "-ltorch_python",
           "-lc10", "-lc10_cuda", "-L" + HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"], "module link failed")
     os.replace(tmp, MODULE)
+    with open(MODULE_FOR, "w") as f:
+        f.write(_torch_abi())
     return LIB
 
 
