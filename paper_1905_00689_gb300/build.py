@@ -44,11 +44,13 @@ def _deps():
 
 
 def up_to_date() -> bool:
-    if not (os.path.exists(LIB) and os.path.exists(MODULE)):
+    """Whether the library, and where there is a torch the module, are newer than every source (and for that torch)."""
+    made = [LIB] + ([MODULE] if _torch_dir() else [])
+    if not all(os.path.exists(p) for p in made):
         return False
-    if not os.path.exists(MODULE_FOR) or open(MODULE_FOR).read() != _torch_abi():
+    if _torch_dir() and not (os.path.exists(MODULE_FOR) and open(MODULE_FOR).read() == _torch_abi()):
         return False
-    t = min(os.path.getmtime(LIB), os.path.getmtime(MODULE))
+    t = min(os.path.getmtime(p) for p in made)
     return all(os.path.getmtime(p) <= t for p in _deps())
 
 
@@ -60,11 +62,10 @@ def _run(cmd, what: str, verbose: bool = False):
         sys.stderr.write(r.stdout + r.stderr)
 
 
-def _torch_dir() -> str:
+def _torch_dir():
+    """Where torch is; None without one (the library needs none, the module is for it alone)."""
     spec = importlib.util.find_spec("torch")
-    if spec is None:
-        raise RuntimeError("torch not found")
-    return spec.submodule_search_locations[0]
+    return spec.submodule_search_locations[0] if spec else None
 
 
 def _torch_abi() -> str:
@@ -84,7 +85,8 @@ def _compile_module() -> str:
 
 
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
-    """Compile every .cu under csrc/ and link liblstm_approx.so; returns its path."""
+    """Compile every .cu under csrc/, link liblstm_approx.so and, where there is a torch, the operators' module;
+    returns the library's path."""
     if not force and up_to_date():
         return LIB
     nvcc = _nvcc()
@@ -98,14 +100,15 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         return obj
 
     with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(srcs) + 1)) as ex:
-        module = ex.submit(_compile_module)
+        module = ex.submit(_compile_module) if _torch_dir() else None
         objs = list(ex.map(compile_one, srcs))
-        module_obj = module.result()
     tmp = LIB + ".tmp"
     _run([nvcc, *ARCH, "-shared", "-o", tmp, *objs], "link failed")
     os.replace(tmp, LIB)
+    if module is None:
+        return LIB
     tmp = MODULE + ".tmp"
-    _run(["g++", "-shared", "-o", tmp, module_obj, "-L" + os.path.join(_torch_dir(), "lib"), "-ltorch", "-ltorch_python",
+    _run(["g++", "-shared", "-o", tmp, module.result(), "-L" + os.path.join(_torch_dir(), "lib"), "-ltorch", "-ltorch_python",
           "-lc10", "-lc10_cuda", "-L" + HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"], "module link failed")
     os.replace(tmp, MODULE)
     with open(MODULE_FOR, "w") as f:

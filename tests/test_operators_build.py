@@ -15,6 +15,7 @@ def build(tmp_path, monkeypatch):
         if hasattr(b, name):
             monkeypatch.setattr(b, name, str(tmp_path / "_build" / os.path.basename(getattr(b, name))))
     monkeypatch.setattr(b, "BUILD", str(tmp_path / "_build"))
+    b.found_torch_dir = b._torch_dir
     monkeypatch.setattr(b, "_torch_dir", lambda: str(torch))
     runs = []
 
@@ -25,7 +26,7 @@ def build(tmp_path, monkeypatch):
     monkeypatch.setattr(b, "_nvcc", lambda: "/usr/local/cuda/bin/nvcc")
     b.runs, b.torch = runs, torch
     yield b
-    del b.runs, b.torch
+    del b.runs, b.torch, b.found_torch_dir
 
 
 def test_built_once(build):
@@ -46,3 +47,30 @@ def test_another_torch_needs_another_module(build):
     assert not build.up_to_date()
     build.build()
     assert any("torch_ops.cpp" in " ".join(c) for c in build.runs) and build.up_to_date()
+
+
+def test_the_library_needs_no_torch(build, monkeypatch):
+    """Without a torch the library is built as ever; the module, which only torch's users load, is left out until there
+    is one."""
+    monkeypatch.setattr(build.importlib.util, "find_spec", lambda name: None)
+    monkeypatch.setattr(build, "_torch_dir", build.found_torch_dir)
+    build.build()
+    assert os.path.exists(build.LIB) and not os.path.exists(build.MODULE) and build.up_to_date()
+    assert not any("g++" in c[0] for c in build.runs)
+    monkeypatch.setattr(build, "_torch_dir", lambda: str(build.torch))
+    assert not build.up_to_date()
+    build.build()
+    assert os.path.exists(build.MODULE) and build.up_to_date()
+
+
+def test_the_library_is_there_where_the_module_fails(build, monkeypatch):
+    plain = build._run
+
+    def run(cmd, what, verbose=False):
+        if "torch_ops.cpp" in " ".join(cmd):
+            raise RuntimeError(what)
+        plain(cmd, what, verbose)
+    monkeypatch.setattr(build, "_run", run)
+    with pytest.raises(RuntimeError, match="torch_ops.cpp"):
+        build.build()
+    assert os.path.exists(build.LIB) and not os.path.exists(build.MODULE) and not build.up_to_date()
