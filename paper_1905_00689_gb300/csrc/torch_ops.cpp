@@ -145,8 +145,9 @@ struct Call {
   }
 };
 
-// The element pitch of the rows of t [..., D], which lie at one pitch.
+// The element pitch of the rows of t [..., D], which lie at one pitch (no rows: at any).
 long long pitch_of(const Tensor& t, const char* name) {
+  if (t.numel() == 0) return t.size(-1);
   long long pitch = -1, span = 0;
   for (int64_t k = t.dim() - 2; k >= 0; --k) {
     if (t.size(k) == 1) continue;
