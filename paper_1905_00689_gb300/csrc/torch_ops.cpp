@@ -248,7 +248,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t) {
     float* rstd = static_cast<float*>(call.dense(a[8], "rstd", at::kFloat, lead));
     if (rstd) Call::written(tensor(a[8], "rstd"));
     need(D <= 0x7fffffff && group <= 0x7fffffff && group >= 0, "D and group must be 32-bit numbers");
-    if (pr || a[7] != Py_None) total = call.out(a[7], "residual_out", type, shape);
+    if (a[2] != Py_None || a[7] != Py_None) total = call.out(a[7], "residual_out", type, shape);
     if (group > 0) {
       auto sizes = lead.vec();
       sizes.push_back(group >= D ? 1 : (D + group - 1) / group);
@@ -257,7 +257,8 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t) {
     Tensor out = call.out(a[5], "out", group > 0 ? at::kFloat8_e4m3fn : type, shape);
     std::optional<Tensor> low;
     if (a[9] == Py_None) {  // where a backward pass will follow (rstd is asked for) and s has more than 16 bits
-      if (pr && rstd && group == 0 && type != at::kFloat && !total->is_inference() && !tensor(a[8], "rstd").is_inference())
+      if (a[2] != Py_None && a[8] != Py_None && group == 0 && type != at::kFloat && !total->is_inference() &&
+          !tensor(a[8], "rstd").is_inference())
         low = call.out(Py_None, "", at::kShort, shape);
     } else if (a[9] != Py_False) {
       need(total && type != at::kFloat && group == 0, "sum_low is for the 16-bit sum of x and a residual");
@@ -269,7 +270,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t) {
                                    call.stream, call.msg, sizeof(call.msg)));
     PyObject* result = wrap_all(out, scales, total);
     // one that the caller handed over without an rstd is the caller's alone
-    if (low && (!rstd || total->is_inference() || tensor(a[8], "rstd").is_inference())) low.reset();
+    if (low && (a[8] == Py_None || total->is_inference() || tensor(a[8], "rstd").is_inference())) low.reset();
     if (result && total && !set_sum_low(PyTuple_GET_ITEM(result, 2), *total, low, a[8])) Py_CLEAR(result);
     return result;
   });

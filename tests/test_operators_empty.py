@@ -20,3 +20,19 @@ def test_no_rows(cuda_device, lead):
         assert w4_matvec(x, W, bias=torch.ones(5, device="cuda")).shape == (*lead, 5)
         wide = torch.empty(*lead, 200, device="cuda", dtype=dtype)[..., 7:71]
         assert rms_norm(wide, w)[0].shape == x.shape
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lead", [(0,), (3, 0)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_sum_of_no_rows(cuda_device, lead, dtype):
+    """A residual without rows has a sum without rows, not none."""
+    import torch
+    from paper_1905_00689_gb300 import rms_norm, rms_norm_backward, rms_norm_quant
+    w = torch.ones(64, device="cuda")
+    x, rstd = torch.empty(*lead, 64, device="cuda", dtype=getattr(torch, dtype)), torch.empty(*lead, device="cuda")
+    y, total = rms_norm(x, w, x.clone(), rstd=rstd)
+    assert y.shape == total.shape == x.shape and total.dtype == x.dtype
+    dx, dw = rms_norm_backward(x, total, w, rstd, x)
+    assert dx.shape == x.shape and bool((dw == 0).all())
+    assert rms_norm_quant(x, w, x.clone())[2].shape == x.shape
