@@ -1039,14 +1039,15 @@ __global__ void __launch_bounds__(256) gated_step_kernel(const StepArgs a) {
   begin_op();
   const int ch = 2 * (blockIdx.x * blockDim.x + threadIdx.x), left = a.D - ch;
   if (left <= 0) return;
-  for (int b0 = blockIdx.y * kRows; b0 < a.B; b0 += gridDim.y * kRows) {
+  // (unsigned: the last of 2^31 - 1 streams and a turn of all blocks further on)
+  for (unsigned b0 = blockIdx.y * kRows; b0 < (unsigned)a.B; b0 += gridDim.y * kRows) {
     float2 x[kRows], r[kRows], i[kRows];
     uint64_t h[kRows];
     int slot[kRows];
 #pragma unroll
     for (int n = 0; n < kRows; ++n) {
-      const int b = b0 + n;
-      slot[n] = b >= a.B ? -1 : (a.slots ? a.slots[b] : b);
+      const unsigned b = b0 + n;
+      slot[n] = b >= (unsigned)a.B ? -1 : (a.slots ? a.slots[b] : (int)b);
     }
 #pragma unroll
     for (int n = 0; n < kRows; ++n) {
@@ -1062,8 +1063,8 @@ __global__ void __launch_bounds__(256) gated_step_kernel(const StepArgs a) {
     const Constants k = constants();
 #pragma unroll
     for (int n = 0; n < kRows; ++n) {
-      const int b = b0 + n;
-      if (b >= a.B) continue;
+      const unsigned b = b0 + n;
+      if (b >= (unsigned)a.B) continue;
       T* y = static_cast<T*>(a.y) + (long long)b * a.D + ch;
       if (slot[n] < 0 || slot[n] >= a.n_slots) {
         store_pair<T, kVec>(y, left, 0.0f, 0.0f);
@@ -1310,10 +1311,10 @@ extern "C" int lstm_approx_gated_step(int dtype, const void* x, long long x_pitc
   StepArgs a{x, r, i, x_pitch, r_pitch, i_pitch, decay, c, state, n_slots, slots, reset, B, D, y};
   const bool vec = D % 2 == 0 && aligned_to(2 * es, x, es, {0, x_pitch}) && aligned_to(2 * es, r, es, {0, r_pitch}) &&
                    aligned_to(2 * es, i, es, {0, i_pitch}) && op_aligned(y, 2 * es);
-  const int threads = D >= 512 ? 256 : 64, across = (D + 2 * threads - 1) / (2 * threads);
+  const int threads = D >= 512 ? 256 : 64, across = (D - 1) / (2 * threads) + 1;
   // one stream to a thread while that leaves no SM with more than 8 blocks
   const bool many = (long long)across * B > 8 * 152;
-  const dim3 grid(across, std::min(many ? (B + 3) / 4 : B, 65535));
+  const dim3 grid(across, std::min(many ? (B - 1) / 4 + 1 : B, 65535));
   const cudaError_t e = op_for_type(dtype, [&](auto* t) {
     using E = std::remove_pointer_t<decltype(t)>;
     auto kern = vec ? (many ? gated_step_kernel<E, true, 4> : gated_step_kernel<E, true, 1>)
