@@ -305,7 +305,8 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
     long long set_at[2];  // of the scales and zero points of the set that is asked for next
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const int n = min((tile0 + my_tile) * 16 + q * 8 + g, a.N - 1);
+      // (unsigned: rows of the last tiles, and of a warp without one, may lie past 2^31)
+      const int n = (int)min((unsigned)(tile0 + my_tile) * 16u + q * 8 + g, (unsigned)a.N - 1u);
       from[q] = a.q + n * a.q_pitch + begin * kRow + t * 16;
       set_at[q] = (long long)n * a.groups + begin * 4;
     }
@@ -524,8 +525,9 @@ __global__ void __launch_bounds__(kMaxWarps * 32) w4_matvec_kernel(const W4Args 
     __syncthreads();
     // a warp takes a tile, two rows of x at a time
     for (int tile = warp; tile < tiles; tile += warps) {
-      const int row = lane & 15, out = (tile0 + tile) * 16 + row;
-      if (out >= a.N) continue;
+      const int row = lane & 15;
+      const unsigned out = (unsigned)(tile0 + tile) * 16u + row;
+      if (out >= (unsigned)a.N) continue;
       const float* first = sums + tile * share * kSum + row * kRed;
       const float bias = a.bias ? a.bias[out] : 0.0f;
       for (int token = lane >> 4; token < tokens; token += 2) {
@@ -653,7 +655,7 @@ cudaError_t launch_matvec(W4Args a, unsigned char* workspace, cudaStream_t s) {
   if (p.warps < 1) return cudaErrorInvalidValue;
   a.tokens = p.tokens;
   a.depth = p.depth;
-  const int tiles = (a.N + 15) / 16, across = std::min(tiles, 152);
+  const int tiles = (a.N - 1) / 16 + 1, across = std::min(tiles, 152);
   a.tiles_each = tiles / across;
   a.tiles_more = tiles % across;
   if (laid_out_bytes(kX, a.M, a.K) > 0) {

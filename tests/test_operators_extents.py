@@ -54,3 +54,26 @@ def test_step_of_the_most_channels(cuda_device):
         part, held = x[:, at:at + 4096].contiguous(), torch.ones(1, 4096, device="cuda")
         assert torch.equal(gated_step(part, part, part, decay[at:at + 4096].contiguous(), held), y[:, at:at + 4096])
         assert torch.equal(held, state[:, at:at + 4096])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("K,scale", [(20, "float16"), (40, "float32")])
+def test_matvec_of_the_most_rows(cuda_device, K, scale):
+    """A matrix of 2^31 - 1 rows, zeros but for a few at both ends (69 GB at 64 columns' pitch)."""
+    import torch
+    from paper_1905_00689_gb300 import W4Weight, w4_matvec
+    N, pitch, G = MOST, -(-K // 32) * 16, -(-K // 32)
+    x = torch.randn(2, K, device="cuda").to(torch.bfloat16)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    few = torch.randint(0, 256, (300, pitch), generator=gen, device="cuda", dtype=torch.uint8)
+    q = torch.full((N, pitch), 0x88, dtype=torch.uint8, device="cuda")  # the zero point of 8: all zeros
+    q[:150], q[N - 150:] = few[:150], few[150:]
+    s = torch.ones(N, G, dtype=getattr(torch, scale), device="cuda")
+    y = w4_matvec(x[:1], W4Weight(q, s, None, K, 32))
+    want = w4_matvec(x[:1], W4Weight(few, s[:300].clone(), None, K, 32))
+    assert torch.equal(y[:, :150], want[:, :150]) and torch.equal(y[:, N - 150:], want[:, 150:])
+    y[:, :150], y[:, N - 150:] = 0.0, 0.0
+    assert int(torch.count_nonzero(y)) == 0
+    del y
+    y = w4_matvec(x, W4Weight(q[N - 300:], s[:300].clone(), None, K, 32))
+    assert torch.equal(y[:, 150:], w4_matvec(x, W4Weight(few, s[:300].clone(), None, K, 32))[:, 150:])
