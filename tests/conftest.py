@@ -12,6 +12,13 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a CUDA device (sm_103a) and the built library")
 
 
+def pytest_collection_modifyitems(items):
+    """One test asks for a value that is wrong and fails: the gradients of a norm of rounded values, taken at the sum
+    before its rounding (test_operators_low_parts.py holds the right ones against 64 bits).  It goes last, so that a run
+    that stops at the first failure has run all others."""
+    items.sort(key=lambda i: i.nodeid.endswith("test_operators_norm.py::test_sum_low_is_not_stale"))
+
+
 def pytest_runtest_setup(item):
     import parity_util
     parity_util.CURRENT_TEST[0] = item.nodeid
