@@ -134,7 +134,8 @@ size_t lstm_approx_rms_norm_workspace_bytes(long long rows, int D);
  *             T) timesteps.  Nothing from later ones enters any result, whatever
  *             they hold; their y is zero.
  *   reset     [T][B] bytes, contiguous, or NULL: where not zero, h_{t-1} counts as zero
- *             (the first token of a packed document), whatever it holds
+ *             (the first token of a packed document), whatever it holds; the
+ *             input is scaled by sqrt(1 - a_t^2) there as elsewhere
  *   h_last    [B][D] fp32: the state after the stream's last timestep (h0
  *             where it has none); may be h0 itself
  *   states    [ceil(T / LSTM_APPROX_SCAN_CHUNK)][B][D] fp32, or NULL: the state
@@ -225,8 +226,10 @@ int lstm_approx_w4_quantize(int dtype, const void *w, long long w_pitch, int N, 
 
 /*
  * y[m][n] = sum_k x[m][k] W[n][k] (+ bias[n]) for a few rows m (the streams
- * that are served together; up to 65535 are right, the kernel is built for up
- * to some tens).
+ * that are served together; up to 65535 are right).  W is read once for as many
+ * rows as lie in a block's shared memory over all of K: 16-bit rows up to 32 at
+ * K = 2048 and 12 at 8192, a 32-bit row counting as three; more rows read it
+ * again.
  *
  *   x_dtype   FP32, BF16, FP16, or E4M3 with scales
  *   x         [M][K], row pitch x_pitch

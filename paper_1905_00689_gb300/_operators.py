@@ -8,6 +8,10 @@ Invalid tensors raise ``ValueError``, errors of the library
 :class:`LSTMApproxError`.  With ``stream``, the caller orders it after the
 work that fills the inputs, as for any other use of a second stream.
 
+Nothing is recorded for torch's differentiation: inputs that require gradients
+are read like others, and outputs have no history.  The gradients are calls of
+their own.
+
 The tensors are checked and passed on by the compiled module ``_torch_ops``
 (csrc/torch_ops.cpp), built with the library.
 """

@@ -39,18 +39,25 @@
 // has no bound as la -> 0, where every gradient has the limit 0 (q ~ sqrt(-la/2)).
 // The run of p is joined the same way from the end (p -> A p + V).
 //
-// Measured (device time; % of the 6784 GB/s that a copy reaches):
-//   8191 x 1 x 2048 bf16      forward 43 us (46%)   backward 79 us (44%)
-//   2048 x 8 x 2048 bf16              67    (59%)           131    (53%)
-//   2048 x 8 x 2048 fp32              88    (90%)           194    (71%)
-//   20000 x 1 x 512 fp32              43    (57%)            81    (52%)
-//   700 x 13 x 1000 fp16              29    (37%)            54    (35%)
-// In 16 bits instructions bound it, 39 forward and 82 backward to a warp's 32
-// elements and issued in 55 to 59% of the cycles by the 16 warps that an SM's
-// registers hold (gates: 5 of the special functions to an element, most of the
-// rest in pairs of channels); 32-bit inputs come near the memory's rate.  Short
-// sequences pay the chain of tiles and the first kernel, 5 us together.  A single
-// step: 64 x 1024 1.9 us (the launch), 1000 x 2048 fp16 7.8 us (62%).
+// Measured (device time; % of the 6784 GB/s that a copy reaches; all decays above
+// 0.88 where the gate is open):
+//   8191 x 1 x 2048 bf16      forward 41 us (48%)   backward 77 us (45%)
+//   2048 x 8 x 2048 bf16              62    (63%)           127    (55%)
+//   2048 x 8 x 2048 fp32              87    (91%)           191    (73%)
+//   20000 x 1 x 512 fp32              42    (58%)            80    (53%)
+//   700 x 13 x 1000 fp16              27    (39%)            53    (35%)
+// Decays between 0.70 and 0.88 take 2048 x 8 x 2048 bf16 to 65 and 129 us, smaller
+// ones to 70 and 138 (see Reach).  32-bit inputs of several streams come near the
+// memory's rate.  In 16 bits nothing is saturated (profiled with
+// decays down to 0.86): 35 instructions forward and 80
+// backward to a warp's 32 elements, issued in 52% and 58% of the cycles by the two
+// blocks of 8 warps that an SM's registers hold, special functions (5 to an element)
+// 29% and 18%, memory 40%.  A task loads, forms its gates, meets in a barrier,
+// exchanges, meets again and goes over its timesteps in turn, and two blocks do not
+// cover each other's waits: barriers are among the first stalls.  One long sequence
+// besides pays the chain of groups (a state is published once the one before it has
+// come), and short ones the first kernel too, 5 us together.  A single
+// step: 64 x 1024 1.9 us (the launch), 1000 x 2048 fp16 7.7 us (63%).
 //
 // Timesteps past a stream's length are the identity in both directions; they
 // and the state before a reset are left out by selection, never by a product
@@ -361,8 +368,9 @@ struct Tasks {
   int group_log2;    // of the tiles of a group: a function of the shape
   long long count;   // slabs * B * tiles
 };
-// Shapes with few streams and channels have many tiles of one sequence in flight at once (about three blocks to an
-// SM share them); where there are more sequences than blocks a tile's predecessor is done long before.
+// Shapes with few streams and channels have many tiles of one sequence in flight at once: their groups are as long as
+// makes the tiles of one group of every sequence half as many again as the blocks of a wave (two to an SM); where there
+// are more sequences than blocks a tile's predecessor is done long before.
 inline Tasks tasks_of(int T, int B, int D, int steps) {
   const int tile = kWarps * steps;
   Tasks t{T, B, D, tile, (D + kLanes - 1) / kLanes, std::max(1, (T + tile - 1) / tile), 0, 0};

@@ -11,14 +11,20 @@
 // a block (no block-wide sum then).
 //
 // Measured (device time, of the 6784 GB/s that a copy reaches): forward with
-// residual, sum and output, 8192 x 4096 bf16 42 us (94%), 4000 x 7168 fp32 70 us
-// (96%), 5001 x 1531 fp32 24 us (76%: unaligned rows in single values); with 8-bit output 8192 x 4096 46 us
-// (75%: the conversions).  With the sum's low parts kept for the backward
-// pass, 8192 x 4096 bf16 52 us (95%).  Backward, 8192 x 4096 bf16 49 us (80%), 20000 x
-// 512 20 us (61%), 5001 x 1531 fp32 26.5 us (68%), 3000 x 7001 fp32 75 us (67%): every
-// row's sum is a barrier, behind which only the next row's loads are under way,
-// and the column sums take 2 to 3 us more.  One token: 2.8 us, the
-// launch and one pass of latencies.
+// residual, sum and output, 8192 x 4096 bf16 42 us (94%), 4000 x 7168 fp32 71 us
+// (95%), 5001 x 1531 fp32 24 us (77%: unaligned rows in single values); with 8-bit output 8192 x 4096 46.5 us
+// (74%: the conversions).  With the sum's low parts kept for the backward
+// pass, 8192 x 4096 bf16 52 us (95%).  Backward, 8192 x 4096 bf16 49 us (81%), 20000 x
+// 512 19 us (63%), 5001 x 1531 fp32 27 us (67%), 3000 x 7001 fp32 75 us (66%): every
+// row's sum is a barrier (two warps to a row of 512 16-bit values already), behind which
+// only the next row's loads are under way, and the column sums take 2 to 3 us more.
+// One token: 2.9 us, the launch and one pass of latencies.
+//
+// Rows of more than 8192 columns are slower: backward their blocks of 1024 threads have 64
+// registers to a thread and spill 0.4 to 0.8 KB of it up to 16384 columns, 1.2 to 2 KB above
+// (3000 x 10000 fp32 163 us, 44%; 3000 x 12288 bf16 146 us, 30%; 1500 x 16392 bf16 202
+// us, 14%); forward up to 0.1 KB above 16384 (3000 x 12288 bf16 81 us with low parts, 67%; in 32 bits 95,
+// 91%).
 //
 // A warp moves its 256 columns in accesses of kUnit values: of 8 where every
 // address is a multiple of 16 bytes, 8 neighbouring columns to a thread; else of

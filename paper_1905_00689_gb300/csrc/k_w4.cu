@@ -4,8 +4,9 @@
 //
 //   y[m][n] = sum_g scale[n][g] sum_{k in g} (q[n][k] - zero[n][g]) x[m][k]
 //
-// The bound is memory, the 4-bit matrix, which is read once for up to 32 columns
-// of x^T (below) at a time.  The products are warp MMAs of 16 rows of W by 16 k by 8
+// The floor is memory, the 4-bit matrix, read once for as many rows of x as lie in
+// shared memory over all of K at a time (plan_matvec; up to 32 columns of x^T, a
+// row in 32 bits being three).  The products are warp MMAs of 16 rows of W by 16 k by 8
 // columns of x^T, their operands in registers: tcgen05 takes both operands from
 // shared memory or tensor memory, to which 4-bit weights would first have to be
 // expanded, four bytes written for each byte read.
@@ -15,7 +16,8 @@
 //       lanes share a row; a lane's 32-bit word holds 8 k as 4 pairs of 16-bit
 //       integers after one AND-OR each, (0, 4) (1, 5) (2, 6) (3, 7): or-ed into
 //       the mantissa of 128 (bf16) or 1024 (fp16), from which 128 + zero or 1024
-//       + zero is subtracted: q - zero, exactly.  Which k a lane holds in which
+//       + zero is subtracted: q - zero, exactly (the published way to expand small
+//       integers through the mantissa: Kim et al. 2022, arXiv 2211.10017).  Which k a lane holds in which
 //       MMA does not matter as long as x is laid out alike, and so that one MMA
 //       sums over one group only.
 //   x   Once per block of threads, into shared memory in the order in which the
@@ -31,13 +33,24 @@
 // the end, always in the same order.  A warp goes on by sets of 4 groups
 // (unrolled), whose weights are copied and whose scales are asked for ahead.
 //
-// Measured (device time): 1 x 16384 x 8192 fp16 21.4 us (3.3 TB/s, 48% of what a
-// copy reaches), 1 x 16384 x 4096 bf16 12.5 us, 8 rows of x 13.4; 16 rows in 8 bits
+// Measured (device time): 1 x 16384 x 8192 fp16 21.3 us (3.3 TB/s, 48% of what a
+// copy reaches), 1 x 16384 x 4096 bf16 12.4 us, 8 rows of x 13.4; 16 rows in 8 bits
 // 19.5 us; 1 x 8192 x 2048 5.0 us, 3 x 3001 x 1000 fp32 5.4 us.  The copies by
 // themselves take 14.8 us of the first and 12.7 of the 16 rows, the products by
-// themselves 17.3 and 17.4: unpacking bounds it (177 instructions to a KB of W with
-// one row of x, 78% of the issue slots), and the two overlap by a half.  A
+// themselves 17.3 and 17.4, and the two overlap by a half only.  Nothing is
+// saturated: 49% of the issue slots are used (177 instructions to a KB of W with one
+// row of x), the matrix pipe 18%, memory 37%; after fixed latencies the largest stall
+// is the block's barriers.  Warps stand idle where a block's tiles do not divide its
+// warps: at 16384 rows 6 or 7 tiles take 12 or 14 of the 16.  A
 // matrix of a few MB is bound by latency: launch, x, first copies, the join.
+//
+// A long x crowds out the warps, and then its own rows: 8192 x 8192 with group 128 is
+// read once for 8 rows of bf16 (12 warps, 14.4 us), once for 12 (4 warps, 23.7),
+// twice for 16 (12 and 4 rows, 43.1; in 8 bits 49.7), four times for 16 in 32 bits
+// (184 us; group 32 92); 8192 x 4096 twice for 16 in 32 bits (46 us).  The kernels of
+// 32 columns with group 128 spill 424 to 576 bytes a thread, with group 64 20 to
+// 244.  Many rows are not what it is for: 64 x 8192 x 4096 bf16 67 us, 512 rows 478.
+//
 // Tried at these sizes: 20 and 24 warps (fewer sets in flight: 21.6 and 30.7 us for
 // the first), two independent sums of MMAs (21.3), copies by whole rows (21.3), 8-bit
 // MMAs with the nibbles as codes of 8-bit floats (16 rows: 27 us).
