@@ -14,8 +14,11 @@
  *   lstm_approx_gated_scan         the recurrence over a sequence
  *   lstm_approx_gated_scan_backward  its gradients
  *   lstm_approx_gated_step         one timestep of it on a pool of states
+ *   lstm_approx_delta_step         one timestep of a recurrence with a matrix
+ *                                  state (the gated delta rule) on a pool of them
  *   lstm_approx_w4_quantize        a matrix to 4 bits per value
  *   lstm_approx_w4_matvec          matrix-vector products with such a matrix
+ *   lstm_approx_adamw_step         an AdamW update of many tensors at once
  *
  * Conventions for every entry point, beside those of lstm_approx.h (an
  * lstm_approx_status is returned; nothing aborts, throws or prints; arguments
@@ -249,6 +252,80 @@ int lstm_approx_w4_matvec(int x_dtype, const void *x, long long x_pitch, const f
                           size_t workspace_bytes, void *cuda_stream, char *msg, int msg_len);
 /* Workspace bytes of the call above (0: none, or invalid sizes). */
 size_t lstm_approx_w4_workspace_bytes(int x_dtype, int M, int K);
+
+/*
+ * The gated delta rule, a recurrence whose state is a matrix S [Dk][Dv] for
+ * every stream and value head:
+ *
+ *     u_t = beta_t (v_t - e^{g_t} S_{t-1}^T k_t)
+ *     S_t = e^{g_t} S_{t-1} + k_t u_t^T;   o_t = scale S_t^T q_t
+ *
+ * Heads: v, o, g, beta and the states have H of them, q and k have Hk, a
+ * divisor of H; value head h goes with query and key head h / (H / Hk).  g is the
+ * logarithm of the decay (at most 0; below -200 it counts as -200, a decay of
+ * zero), beta the step towards v, 0 to 1 as a rule.  k is used as it is: with
+ * |k| = 1 and beta <= 2 no state grows by itself.
+ *
+ * One timestep for B streams, states updated in place:
+ *
+ *   dtype     FP32, BF16 or FP16: q, k, v, o
+ *   q, k      [B][Hk][Dk], v, o [B][H][Dv];  1 <= Dk <= 128
+ *   g, beta   [B][H] fp32
+ *   strides   HOST [10]: the b and head strides of q, k, v and o, the b strides
+ *             of g and beta, in this order; NULL: all contiguous
+ *   state     [n_slots][H][Dk][Dv] fp32, contiguous
+ *   slots     [B] int32, or NULL (stream b owns row b; then B <= n_slots): the
+ *             row of state that holds stream b.  A stream whose slot lies
+ *             outside [0, n_slots) is idle: no state changes, its o is zero.
+ *             Slots in range are distinct.
+ *   reset     [B] bytes, or NULL: where not zero the state counts as zero,
+ *             whatever it holds
+ */
+int lstm_approx_delta_step(int dtype, const void *q, const void *k, const void *v, const float *g,
+                           const float *beta, float scale, float *state, int n_slots,
+                           const int32_t *slots, const unsigned char *reset, int B, int H, int Hk,
+                           int Dk, int Dv, void *o, const long long *strides, void *cuda_stream,
+                           char *msg, int msg_len);
+
+/*
+ * An AdamW update of many tensors at once.  For every value, t the step:
+ *
+ *     g' = grad_scale g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
+ *     p = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+ *
+ * in 32 bits, p rounded to its type.  `tensors` is a HOST array, read before
+ * the call returns.  Of each:
+ *
+ *   p, g      n values, contiguous, FP32, BF16 or FP16 each.  g NULL: the
+ *             tensor is left as it is.
+ *   m, v      bits 32: the two averages, fp32.  bits 8: m and sqrt(v) as E4M3
+ *             with scales m_scale, v_scale [ceil(n / 256)] fp32, one for each 256
+ *             values: largest magnitude / 448, at least 2^-126.  They are
+ *             rounded to either neighbour with the chances that keep the mean, by a
+ *             hash of seed, step and the value's position among all tensors'; a
+ *             sqrt(v) above zero does not become zero.
+ *   copy      n values of copy_dtype that receive p, or NULL
+ * No two of the tensors overlap.
+ *
+ *   step      t >= 1, or step_at: a DEVICE int32 that holds it (for captured
+ *             graphs; it is read, not changed);  lr, or lr_at: a DEVICE float
+ *   beta1, beta2  in [0, 1);  eps >= 0
+ *   grad_scale  DEVICE float that multiplies every gradient, or NULL
+ *   skip      DEVICE byte, or NULL: where not zero nothing changes
+ * Several hundred tensors go into one launch.
+ */
+typedef struct lstm_approx_adamw_tensor {
+  void *p, *m, *v, *copy;
+  const void *g;
+  float *m_scale, *v_scale;
+  long long n;
+  int p_dtype, g_dtype, copy_dtype;
+} lstm_approx_adamw_tensor;
+int lstm_approx_adamw_step(int count, const lstm_approx_adamw_tensor *tensors, int bits, int step,
+                           const int32_t *step_at, double lr, const float *lr_at, double beta1,
+                           double beta2, double eps, double weight_decay, const float *grad_scale,
+                           const unsigned char *skip, unsigned seed, void *cuda_stream, char *msg,
+                           int msg_len);
 
 #ifdef __cplusplus
 }

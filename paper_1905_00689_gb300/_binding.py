@@ -43,6 +43,7 @@ EXPORTS = (
     "lstm_approx_rms_norm_workspace_bytes", "lstm_approx_gated_scan", "lstm_approx_gated_scan_backward",
     "lstm_approx_gated_scan_workspace_bytes", "lstm_approx_gated_step", "lstm_approx_w4_quantize",
     "lstm_approx_w4_matvec", "lstm_approx_w4_workspace_bytes",
+    "lstm_approx_delta_step", "lstm_approx_adamw_step",
 )
 
 _lib = None
@@ -87,7 +88,7 @@ def load(path: str = LIB_PATH):
     lib.lstm_approx_dense_workspace_bytes.argtypes = [I, I, I]
     lib.lstm_approx_dense_set_launch_order.argtypes = [I]
     # the operators of include/lstm_approx_ops.h; each ends in (stream, msg, msg_len)
-    F, Z, end = ctypes.c_float, ctypes.c_size_t, [P, ctypes.c_char_p, I]
+    D, F, Z, end = ctypes.c_double, ctypes.c_float, ctypes.c_size_t, [P, ctypes.c_char_p, I]
     lib.lstm_approx_rms_norm.argtypes = [I, I, P, LL, P, LL, P, F, LL, I, P, P, P, P, P] + end
     lib.lstm_approx_rms_norm_backward.argtypes = [I, P, LL, P, LL, P, P, P, P, LL, LL, I, P, P, P, Z] + end
     lib.lstm_approx_rms_norm_workspace_bytes.argtypes = [LL, I]
@@ -99,6 +100,8 @@ def load(path: str = LIB_PATH):
     lib.lstm_approx_w4_quantize.argtypes = [I, P, LL, I, I, I, P, LL, P, I, P] + end
     lib.lstm_approx_w4_matvec.argtypes = [I, P, LL, P, I, P, LL, P, I, P, P, I, I, I, I, P, I, P, Z] + end
     lib.lstm_approx_w4_workspace_bytes.argtypes = [I, I, I]
+    lib.lstm_approx_delta_step.argtypes = [I, P, P, P, P, P, F, P, I, P, P, I, I, I, I, I, P, P] + end
+    lib.lstm_approx_adamw_step.argtypes = [I, P, I, I, P, D, P, D, D, D, D, P, P, ctypes.c_uint] + end
     for name in EXPORTS:
         if name.endswith("_workspace_bytes"):
             getattr(lib, name).restype = ctypes.c_size_t

@@ -146,6 +146,26 @@ def gated_step(x, r, i, decay, state, *, c: float = 8.0, slots=None, reset=None,
 
 
 # ---------------------------------------------------------------------------
+# recurrence with a matrix state
+
+def delta_step(q, k, v, g, beta, state, *, scale=None, slots=None, reset=None, o=None, stream=None):
+    """One timestep of the gated delta rule: with S the state of a stream and value head,
+
+        u = beta (v - e^g S^T k);  S = e^g S + k u^T;  o = scale S^T q
+
+    q, k [B, Hk, Dk] and v [B, H, Dv] (fp32, bf16 or fp16, any b and head
+    strides; H a multiple of Hk: value head h goes with query and key head
+    h // (H // Hk); Dk <= 128), g (the decay's logarithm, at most 0) and beta
+    [B, H] fp32.  Returns o [B, H, Dv] and updates state [n_slots, H, Dk, Dv]
+    fp32 in place.  scale: None for Dk ** -0.5.  slots [B] int32: the row of
+    state of each stream (None: row b); one outside [0, n_slots) marks an idle
+    stream, whose o is zero.  reset [B]: where true the state counts as zero.
+    """
+    args = (q, k, v, g, beta, state, scale, slots, reset, o)
+    return _ops.delta_step(*args) if stream is None else _on(stream, _ops.delta_step, *args)
+
+
+# ---------------------------------------------------------------------------
 # 4-bit matrices
 
 class W4Weight:
@@ -199,3 +219,71 @@ def w4_matvec(x, w: W4Weight, *, x_scale=None, bias=None, out=None, out_dtype=No
     _need(code > -2, "out_dtype must be float32, bfloat16 or float16")
     args = (x, w.q, w.scale, w.zero, w.K, w.group, w.pitch, x_scale, bias, out, code, workspace)
     return _ops.w4_matvec(*args) if stream is None else _on(stream, _ops.w4_matvec, *args)
+
+
+# ---------------------------------------------------------------------------
+# updates
+
+class AdamWState:
+    """The moving averages that :func:`adamw_step` keeps for a list of tensors:
+    exp_avg and exp_avg_sq, lists of tensors of the parameters' shapes.  In
+    32 bits both are fp32.  In 8 bits they are float8_e4m3fn with lists of scales,
+    [ceil(n / 256)] fp32 for a tensor of n values, one for each 256 of them:
+    exp_avg * scale is the average, (exp_avg_sq * scale) ** 2 that of the
+    squares.  Holds the tensors; nothing is copied.
+    """
+
+    def __init__(self, exp_avg, exp_avg_sq, exp_avg_scale=None, exp_avg_sq_scale=None):
+        _need((exp_avg_scale is None) == (exp_avg_sq_scale is None), "both averages have scales, or none")
+        lists = [list(x) for x in (exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale) if x is not None]
+        _need(len({len(x) for x in lists}) == 1, "the lists must be of one length")
+        kind = torch.float32 if exp_avg_scale is None else torch.float8_e4m3fn
+        _need(all(t.dtype == kind for x in lists[:2] for t in x),
+              f"averages must be {kind}" + (" (8-bit ones need scales)" if exp_avg_scale is None else ""))
+        self.exp_avg, self.exp_avg_sq = lists[:2]
+        self.exp_avg_scale, self.exp_avg_sq_scale = lists[2:] if len(lists) == 4 else (None, None)
+
+    @classmethod
+    def zeros(cls, params, bits: int = 32):
+        """Averages of zero for `params`, in 32 or 8 bits."""
+        _need(bits in (8, 32), "averages have 8 or 32 bits")
+        params = list(params)
+        if bits == 32:
+            return cls(*([torch.zeros(p.shape, dtype=torch.float32, device=p.device) for p in params] for _ in range(2)))
+        return cls(*([torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn) for p in params]
+                     for _ in range(2)),
+                   *([torch.ones(-(-p.numel() // 256), dtype=torch.float32, device=p.device) for p in params]
+                     for _ in range(2)))
+
+
+def adamw_step(params, grads, state: AdamWState, step, *, lr, betas=(0.9, 0.999), eps: float = 1e-8,
+               weight_decay: float = 0.01, copies=None, grad_scale=None, skip=None, seed: int = 0, stream=None) -> None:
+    """One AdamW update of many tensors, in place.  For each, with t the step:
+
+        g' = grad_scale g;  m = b1 m + (1 - b1) g';  v = b2 v + (1 - b2) g'^2
+        p = p (1 - lr weight_decay) - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
+
+    params, grads: lists of contiguous CUDA tensors of one device, fp32, bf16 or
+    fp16 each (a parameter in 16 bits is rounded to the nearest, so steps below
+    half a unit of it are lost); a gradient of None leaves its tensor as it is.
+    state: :class:`AdamWState`; 8-bit averages are rounded at random (`seed`, step and
+    position choose), so that they move on average by what they should.  copies: a
+    list of tensors (or None) that receive the parameters in a type of their own, as
+    the next forward pass reads them.
+
+    step: the number of this update, from 1; or a CUDA int32 tensor of one value that
+    holds it, for captured graphs (read, not changed: count it up before the call, in
+    the graph).  lr may likewise be a CUDA fp32 tensor.  grad_scale: a CUDA fp32
+    tensor of one value (a clipping factor, the reciprocal of a loss scale); skip: a
+    CUDA bool of one value, where true nothing changes.
+    """
+    _need(len(betas) == 2, "betas must be two numbers")
+    params, grads, copies = (x if x is None or isinstance(x, (list, tuple)) else list(x) for x in (params, grads, copies))
+    args = (params, grads, state.exp_avg, state.exp_avg_sq, state.exp_avg_scale, state.exp_avg_sq_scale, copies, step, lr,
+            betas[0], betas[1], eps, weight_decay, grad_scale, skip, seed)
+    if stream is None:
+        _ops.adamw_step(*args)
+        return
+    _on(stream, _ops.adamw_step, *args)
+    for t in (t for x in args[:7] if x is not None for t in x if isinstance(t, torch.Tensor)):
+        t.record_stream(stream)

@@ -172,6 +172,16 @@ cudaError_t op_launch(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem
   return cudaLaunchKernelEx(&cfg, kern, KArgs(args)...);
 }
 
+// The sizes of the gated delta rule's calls.
+constexpr int kDeltaMostDk = 128;
+inline int delta_check_sizes(int T, int B, int H, int Hk, int Dk, int Dv, char* msg, int msg_len) {
+  if (T < 0 || B < 0) return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "negative sizes");
+  if (H < 1 || Hk < 1 || H % Hk) return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "H (%d) must be a multiple of Hk (%d)", H, Hk);
+  if (Dk < 1 || Dk > kDeltaMostDk || Dv < 1)
+    return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "need 1 <= Dk <= %d and 1 <= Dv, not %d and %d", kDeltaMostDk, Dk, Dv);
+  return LSTM_APPROX_OK;
+}
+
 // Calls f with a null pointer of the element type of `dtype` (FP32, BF16, FP16).
 template <typename F>
 cudaError_t op_for_type(int dtype, F f) {

@@ -12,9 +12,13 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <cmath>
 #include <optional>
 #include <stdexcept>
 #include <string>
+#include <utility>
+#include <vector>
 
 #include "../../include/lstm_approx_ops.h"
 
@@ -508,6 +512,195 @@ PyObject* w4_matvec(PyObject*, PyObject* const* a, Py_ssize_t) {
   });
 }
 
+// q, k, v, g and beta of the delta rule's calls; `lead`: the axes before the heads (T and B, or B).
+struct Heads {
+  int code;
+  at::ScalarType type;
+  std::vector<int64_t> lead;
+  int64_t H, Hk, Dk, Dv;
+
+  Heads(const Call& call, const Tensor& q, const Tensor& v, int64_t axes)
+      : code(float_code(q, "q")), type(q.scalar_type()) {
+    need(q.dim() == axes + 2 && v.dim() == axes + 2,
+         axes == 2 ? "q must be [T, B, Hk, Dk] and v [T, B, H, Dv]" : "q must be [B, Hk, Dk] and v [B, H, Dv]");
+    lead = q.sizes().slice(0, axes).vec();
+    Hk = q.size(axes), Dk = q.size(axes + 1), H = v.size(axes), Dv = v.size(axes + 1);
+    for (int64_t n : lead) need(n <= 0x7fffffff, "sizes must be 32-bit numbers");
+    need(Hk <= 0x7fffffff && Dk <= 0x7fffffff && H <= 0x7fffffff && Dv <= 0x7fffffff, "sizes must be 32-bit numbers");
+    need(Hk >= 1 && H >= 1 && H % Hk == 0, "v's heads must be a multiple of q's");
+    need(Dk >= 1 && Dv >= 1, "Dk and Dv must not be zero");
+  }
+  std::vector<int64_t> shape(bool keys) const {
+    std::vector<int64_t> s = lead;
+    s.push_back(keys ? Hk : H);
+    s.push_back(keys ? Dk : Dv);
+    return s;
+  }
+  std::vector<int64_t> per_head() const {
+    std::vector<int64_t> s = lead;
+    s.push_back(H);
+    return s;
+  }
+  // A tensor of q's or v's shape (any strides but the last axis's): its address, its strides appended.
+  void* add(const Call& call, const Tensor& t, const char* name, bool keys, long long* strides, int& n) const {
+    void* p = call.rows(t, name, type, shape(keys));
+    for (size_t k = 0; k <= lead.size(); ++k) strides[n++] = t.stride(k);
+    return p;
+  }
+  // One of g's shape.
+  float* add_gate(const Call& call, const Tensor& t, const char* name, long long* strides, int& n) const {
+    void* p = call.rows(t, name, at::kFloat, per_head());
+    for (size_t k = 0; k < lead.size(); ++k) strides[n++] = t.stride(k);
+    return static_cast<float*>(p);
+  }
+  Tensor out(const Call& call, PyObject* o, const char* name, bool keys) const {
+    if (o == Py_None) return call.out(o, name, type, shape(keys));
+    Call::written(tensor(o, name));
+    return tensor(o, name);
+  }
+  float scale(PyObject* o) const { return o == Py_None ? (float)(1.0 / std::sqrt((double)Dk)) : real(o); }
+};
+
+// delta_step(q, k, v, g, beta, state, scale, slots, reset, o) -> o
+PyObject* delta_step(PyObject*, PyObject* const* a, Py_ssize_t) {
+  return guarded([&]() -> PyObject* {
+    const Tensor &q = tensor(a[0], "q"), &v = tensor(a[2], "v"), &state = tensor(a[5], "state");
+    Call call(q, "q");
+    const Heads heads(call, q, v, 1);
+    const int64_t B = heads.lead[0], slots = state.dim() > 0 ? state.size(0) : 0;
+    need(slots <= 0x7fffffff, "sizes must be 32-bit numbers");
+    long long strides[10];
+    int n = 0;
+    void* pq = heads.add(call, q, "q", true, strides, n);
+    void* pk = heads.add(call, tensor(a[1], "k"), "k", true, strides, n);
+    void* pv = heads.add(call, v, "v", false, strides, n);
+    const int at_o = n;
+    n += 2;
+    const float* g = heads.add_gate(call, tensor(a[3], "g"), "g", strides, n);
+    const float* beta = heads.add_gate(call, tensor(a[4], "beta"), "beta", strides, n);
+    float* ps = static_cast<float*>(call.dense(state, "state", at::kFloat, {slots, heads.H, heads.Dk, heads.Dv}));
+    const int32_t* at_slots = static_cast<const int32_t*>(call.dense(a[7], "slots", at::kInt, {B}));
+    const unsigned char* reset = Sequence::resets(call, a[8], {B});
+    const float scale = heads.scale(a[6]);
+    Tensor o = heads.out(call, a[9], "o", false);
+    n = at_o;
+    void* po = heads.add(call, o, "o", false, strides, n);
+    Call::written(state);
+    call.done(lstm_approx_delta_step(heads.code, pq, pk, pv, g, beta, scale, ps, (int)slots, at_slots, reset, (int)B,
+                                     (int)heads.H, (int)heads.Hk, (int)heads.Dk, (int)heads.Dv, po, strides, call.stream,
+                                     call.msg, sizeof(call.msg)));
+    return wrap(o);
+  });
+}
+
+// The items of a sequence of tensors.
+struct Items {
+  PyObject* fast;
+  Items(PyObject* o, const char* name) : fast(PySequence_Fast(o, "")) {
+    if (!fast) {
+      PyErr_Clear();
+      invalid(std::string(name) + " must be a sequence of tensors");
+    }
+  }
+  Items(const Items&) = delete;
+  ~Items() { Py_DECREF(fast); }
+  Py_ssize_t size() const { return PySequence_Fast_GET_SIZE(fast); }
+  PyObject* operator[](Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(fast, i); }
+};
+
+// adamw_step(params, grads, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale, copies, step, lr, beta1, beta2, eps,
+// weight_decay, grad_scale, skip, seed): the averages have 8 bits where there are scales
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t) {
+  return guarded([&]() -> PyObject* {
+    const Items params(a[0], "params"), grads(a[1], "grads"), m(a[2], "exp_avg"), v(a[3], "exp_avg_sq");
+    const Py_ssize_t count = params.size();
+    need(count <= 0x7fffffff, "too many tensors");
+    need(grads.size() == count && m.size() == count && v.size() == count, "params, grads and the averages must be as many");
+    if (count == 0) Py_RETURN_NONE;
+    const bool few_bits = a[4] != Py_None, copied = a[6] != Py_None;
+    std::optional<Items> ms, vs, copies;
+    if (few_bits) ms.emplace(a[4], "exp_avg_scale"), vs.emplace(a[5], "exp_avg_sq_scale");
+    if (copied) copies.emplace(a[6], "copies");
+    need(!few_bits || (ms->size() == count && vs->size() == count), "params and the scales must be as many");
+    need(!copied || copies->size() == count, "params and copies must be as many");
+    Call call(tensor(params[0], "params"), "params");
+    const at::ScalarType kind = few_bits ? at::kFloat8_e4m3fn : at::kFloat;
+    std::vector<lstm_approx_adamw_tensor> table((size_t)count);
+    std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+    spans.reserve((size_t)count);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+      const Tensor& p = tensor(params[i], "params");
+      lstm_approx_adamw_tensor& t = table[(size_t)i];
+      t = {};
+      const auto shape = p.sizes();
+      t.n = p.numel();
+      t.p_dtype = t.g_dtype = float_code(p, "params");
+      t.p = call.dense(p, "params", p.scalar_type(), shape);
+      t.m = call.dense(tensor(m[i], "exp_avg"), "exp_avg", kind, shape);
+      t.v = call.dense(tensor(v[i], "exp_avg_sq"), "exp_avg_sq", kind, shape);
+      if (few_bits) {
+        const int64_t blocks = (t.n + 255) / 256;
+        t.m_scale = static_cast<float*>(call.dense(tensor((*ms)[i], "exp_avg_scale"), "exp_avg_scale", at::kFloat, {blocks}));
+        t.v_scale = static_cast<float*>(call.dense(tensor((*vs)[i], "exp_avg_sq_scale"), "exp_avg_sq_scale", at::kFloat, {blocks}));
+      }
+      if (copied && (*copies)[i] != Py_None) {
+        const Tensor& c = tensor((*copies)[i], "copies");
+        t.copy_dtype = float_code(c, "copies");
+        t.copy = call.dense(c, "copies", c.scalar_type(), shape);
+      }
+      if (grads[i] != Py_None) {
+        const Tensor& g = tensor(grads[i], "grads");
+        t.g_dtype = float_code(g, "grads");
+        t.g = call.dense(g, "grads", g.scalar_type(), shape);
+      }
+      if (t.n > 0) {
+        const auto at = reinterpret_cast<uintptr_t>(t.p);
+        spans.emplace_back(at, at + p.nbytes());
+      }
+    }
+    std::sort(spans.begin(), spans.end());
+    for (size_t i = 1; i < spans.size(); ++i) need(spans[i].first >= spans[i - 1].second, "two of params overlap");
+    auto device_value = [&](PyObject* o, const char* name, at::ScalarType type) -> const void* {
+      const Tensor& t = tensor(o, name);
+      need(t.numel() == 1, "step, lr, grad_scale and skip must have one value");
+      return call.dense(t, name, type, t.sizes());
+    };
+    const int32_t* step_at = nullptr;
+    const float *lr_at = nullptr, *clip = nullptr;
+    const unsigned char* skip = nullptr;
+    long long step = 0;
+    double lr = 0.0;
+    if (THPVariable_Check(a[7])) step_at = static_cast<const int32_t*>(device_value(a[7], "step", at::kInt));
+    else step = integer(a[7]);
+    need(step_at || (step >= 1 && step <= 0x7fffffff), "step must be 1 or more");
+    auto number = [](PyObject* o) {
+      const double x = PyFloat_AsDouble(o);
+      if (x == -1.0 && PyErr_Occurred()) {
+        PyErr_Clear();
+        invalid("a number was expected");
+      }
+      return x;
+    };
+    if (THPVariable_Check(a[8])) lr_at = static_cast<const float*>(device_value(a[8], "lr", at::kFloat));
+    else lr = number(a[8]);
+    if (a[13] != Py_None) clip = static_cast<const float*>(device_value(a[13], "grad_scale", at::kFloat));
+    if (a[14] != Py_None)
+      skip = static_cast<const unsigned char*>(device_value(
+          a[14], "skip", tensor(a[14], "skip").scalar_type() == at::kByte ? at::kByte : at::kBool));
+    const double beta1 = number(a[9]), beta2 = number(a[10]), eps = number(a[11]), decay = number(a[12]);
+    const unsigned seed = (unsigned)(unsigned long long)integer(a[15]);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+      if (grads[i] == Py_None) continue;
+      for (const Items* list : {&params, &m, &v}) Call::written(tensor((*list)[i], ""));
+      if (few_bits) Call::written(tensor((*ms)[i], "")), Call::written(tensor((*vs)[i], ""));
+      if (table[(size_t)i].copy) Call::written(tensor((*copies)[i], ""));
+    }
+    call.done(lstm_approx_adamw_step((int)count, table.data(), few_bits ? 8 : 32, (int)step, step_at, lr, lr_at, beta1, beta2,
+                                     eps, decay, clip, skip, seed, call.stream, call.msg, sizeof(call.msg)));
+    Py_RETURN_NONE;
+  });
+}
+
 // Each entry takes exactly the arguments that _operators.py gives it.
 template <PyObject* (*kF)(PyObject*, PyObject* const*, Py_ssize_t), Py_ssize_t kN>
 PyObject* counted(PyObject* self, PyObject* const* a, Py_ssize_t n) {
@@ -526,7 +719,8 @@ PyMethodDef g_methods[] = {
     entry<rms_norm, 10>("rms_norm"),          entry<rms_norm_backward, 9>("rms_norm_backward"),
     entry<gated_scan, 12>("gated_scan"),      entry<gated_scan_backward, 16>("gated_scan_backward"),
     entry<gated_step, 9>("gated_step"),       entry<w4_quantize, 5>("w4_quantize"),
-    entry<w4_matvec, 12>("w4_matvec"),        {nullptr, nullptr, 0, nullptr},
+    entry<w4_matvec, 12>("w4_matvec"),        entry<delta_step, 10>("delta_step"),
+    entry<adamw_step, 16>("adamw_step"),      {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_torch_ops", "The operators on torch tensors (see _operators).", -1,
                         g_methods};
