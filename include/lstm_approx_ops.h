@@ -14,8 +14,10 @@
  *   lstm_approx_gated_scan         the recurrence over a sequence
  *   lstm_approx_gated_scan_backward  its gradients
  *   lstm_approx_gated_step         one timestep of it on a pool of states
- *   lstm_approx_delta_step         one timestep of a recurrence with a matrix
- *                                  state (the gated delta rule) on a pool of them
+ *   lstm_approx_delta_scan         a recurrence with a matrix for its state (the
+ *                                  gated delta rule) over a sequence
+ *   lstm_approx_delta_scan_backward  its gradients
+ *   lstm_approx_delta_step         one timestep of it on a pool of states
  *   lstm_approx_w4_quantize        a matrix to 4 bits per value
  *   lstm_approx_w4_matvec          matrix-vector products with such a matrix
  *   lstm_approx_adamw_step         an AdamW update of many tensors at once
@@ -266,6 +268,69 @@ size_t lstm_approx_w4_workspace_bytes(int x_dtype, int M, int K);
  * zero), beta the step towards v, 0 to 1 as a rule.  k is used as it is: with
  * |k| = 1 and beta <= 2 no state grows by itself.
  *
+ * Over a sequence:
+ *
+ *   dtype     FP32, BF16 or FP16: q, k, v, o
+ *   q, k      [T][B][Hk][Dk], v, o [T][B][H][Dv];  1 <= Dk <= 128
+ *   g, beta   [T][B][H] fp32
+ *   strides   HOST [16]: the t, b and head strides of q, k, v and o, the t and b
+ *             strides of g and beta, in this order; NULL: all contiguous
+ *   h0        [B][H][Dk][Dv] fp32, or NULL (zeros)
+ *   lengths   [B] int32, or NULL (all T): stream b has min(max(lengths[b], 0),
+ *             T) timesteps.  Nothing from later ones enters any result, whatever
+ *             they hold; their o is zero.
+ *   reset     [T][B] bytes, contiguous, or NULL: where not zero, S_{t-1} counts as
+ *             zero (the first token of a packed document), whatever it holds
+ *   h_last    [B][H][Dk][Dv] fp32: the state after the stream's last timestep
+ *             (h0 where it has none); may be h0 itself
+ *   states    [ceil(T / LSTM_APPROX_DELTA_CHUNK)][B][H][Dk][Dv] fp32, or NULL:
+ *             the state before every chunk's first timestep (of chunks that the
+ *             stream reaches), kept for the backward pass
+ *   workspace at least lstm_approx_delta_scan_workspace_bytes(T, B, H, Hk, Dk,
+ *             Dv, 0) bytes, 16-byte aligned, not shared by calls in flight
+ *
+ * Values that are not finite stay in their stream, head and (from the next
+ * reset on) document, but reach earlier timesteps of their chunk.
+ */
+#define LSTM_APPROX_DELTA_CHUNK 64
+int lstm_approx_delta_scan(int dtype, const void *q, const void *k, const void *v, const float *g,
+                           const float *beta, float scale, const float *h0, const int32_t *lengths,
+                           const unsigned char *reset, int T, int B, int H, int Hk, int Dk, int Dv,
+                           void *o, const long long *strides, float *h_last, float *states,
+                           void *workspace, size_t workspace_bytes, void *cuda_stream, char *msg,
+                           int msg_len);
+/* Workspace bytes of the call above, or (backward not 0) of the next; 0 for invalid sizes. */
+size_t lstm_approx_delta_scan_workspace_bytes(int T, int B, int H, int Hk, int Dk, int Dv,
+                                              int backward);
+
+/*
+ * Its gradients:
+ *
+ *   d_o       [T][B][H][Dv] dtype;  dh_last [B][H][Dk][Dv] fp32 or NULL (zeros)
+ *   q, k, v, g, beta, scale, lengths, reset: as in the forward call; states its
+ *             output
+ *   dq, dk    [T][B][Hk][Dk] dtype, summed over the value heads that share
+ *             them;  dv [T][B][H][Dv] dtype;  dg, dbeta [T][B][H] fp32
+ *             (all zero past a stream's length);  dh0 [B][H][Dk][Dv] fp32
+ *   strides   HOST [29]: the t, b and head strides of d_o, q, k, v, dq, dk and dv,
+ *             the t and b strides of g, beta, dg and dbeta, in this order; NULL:
+ *             all contiguous
+ *   workspace at least lstm_approx_delta_scan_workspace_bytes(T, B, H, Hk, Dk,
+ *             Dv, 1) bytes, 16-byte aligned, not shared by calls in flight
+ *
+ * dg is zero at a reset and where g is below -200.
+ */
+int lstm_approx_delta_scan_backward(int dtype, const void *d_o, const float *dh_last, const void *q,
+                                    const void *k, const void *v, const float *g,
+                                    const float *beta, float scale, const float *states,
+                                    const int32_t *lengths, const unsigned char *reset, int T,
+                                    int B, int H, int Hk, int Dk, int Dv, void *dq, void *dk,
+                                    void *dv, float *dg, float *dbeta, float *dh0,
+                                    const long long *strides, void *workspace,
+                                    size_t workspace_bytes, void *cuda_stream, char *msg,
+                                    int msg_len);
+
+/*
  * One timestep for B streams, states updated in place:
  *
  *   dtype     FP32, BF16 or FP16: q, k, v, o

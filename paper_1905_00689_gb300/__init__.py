@@ -20,8 +20,8 @@ from ._binding import (  # noqa: F401
 
 # The operators work on torch tensors and are imported (with torch) when first used.
 _OPERATORS = (
-    "AdamWState", "OP_BF16", "OP_E4M3", "OP_FP16", "OP_FP32", "SCAN_CHUNK", "W4Weight", "adamw_step", "delta_step",
-    "gated_scan", "gated_scan_backward", "gated_scan_states", "gated_step", "rms_norm", "rms_norm_backward",
+    "AdamWState", "DELTA_CHUNK", "OP_BF16", "OP_E4M3", "OP_FP16", "OP_FP32", "SCAN_CHUNK", "W4Weight", "adamw_step",
+    "delta_scan", "delta_scan_backward", "delta_scan_states", "delta_step", "gated_scan", "gated_scan_backward", "gated_scan_states", "gated_step", "rms_norm", "rms_norm_backward",
     "rms_norm_quant", "w4_matvec", "w4_quantize",
 )
 

@@ -43,7 +43,8 @@ EXPORTS = (
     "lstm_approx_rms_norm_workspace_bytes", "lstm_approx_gated_scan", "lstm_approx_gated_scan_backward",
     "lstm_approx_gated_scan_workspace_bytes", "lstm_approx_gated_step", "lstm_approx_w4_quantize",
     "lstm_approx_w4_matvec", "lstm_approx_w4_workspace_bytes",
-    "lstm_approx_delta_step", "lstm_approx_adamw_step",
+    "lstm_approx_delta_scan", "lstm_approx_delta_scan_backward",
+    "lstm_approx_delta_scan_workspace_bytes", "lstm_approx_delta_step", "lstm_approx_adamw_step",
 )
 
 _lib = None
@@ -100,6 +101,9 @@ def load(path: str = LIB_PATH):
     lib.lstm_approx_w4_quantize.argtypes = [I, P, LL, I, I, I, P, LL, P, I, P] + end
     lib.lstm_approx_w4_matvec.argtypes = [I, P, LL, P, I, P, LL, P, I, P, P, I, I, I, I, P, I, P, Z] + end
     lib.lstm_approx_w4_workspace_bytes.argtypes = [I, I, I]
+    lib.lstm_approx_delta_scan.argtypes = [I, P, P, P, P, P, F, P, P, P, I, I, I, I, I, I, P, P, P, P, P, Z] + end
+    lib.lstm_approx_delta_scan_backward.argtypes = ([I, P, P, P, P, P, P, P, F, P, P, P, I, I, I, I, I, I] + [P] * 8 + [Z] + end)
+    lib.lstm_approx_delta_scan_workspace_bytes.argtypes = [I, I, I, I, I, I, I]
     lib.lstm_approx_delta_step.argtypes = [I, P, P, P, P, P, F, P, I, P, P, I, I, I, I, I, P, P] + end
     lib.lstm_approx_adamw_step.argtypes = [I, P, I, I, P, D, P, D, D, D, D, P, P, ctypes.c_uint] + end
     for name in EXPORTS:

@@ -29,7 +29,7 @@ except ImportError as e:
                        "__graft_entry__.build() or python -m paper_1905_00689_gb300.build") from e
 
 OP_FP32, OP_BF16, OP_FP16, OP_E4M3 = range(4)
-SCAN_CHUNK = 64
+SCAN_CHUNK = DELTA_CHUNK = 64
 _CODES = {torch.float32: OP_FP32, torch.bfloat16: OP_BF16, torch.float16: OP_FP16}
 
 
@@ -148,16 +148,50 @@ def gated_step(x, r, i, decay, state, *, c: float = 8.0, slots=None, reset=None,
 # ---------------------------------------------------------------------------
 # recurrence with a matrix state
 
-def delta_step(q, k, v, g, beta, state, *, scale=None, slots=None, reset=None, o=None, stream=None):
-    """One timestep of the gated delta rule: with S the state of a stream and value head,
+def delta_scan_states(q, v):
+    """An empty ``states`` for :func:`delta_scan` of q [T, B, Hk, Dk] and v [T, B, H, Dv]: [ceil(T / DELTA_CHUNK), B, H,
+    Dk, Dv] fp32."""
+    _need(q.dim() == 4 and v.dim() == 4, "q must be [T, B, Hk, Dk] and v [T, B, H, Dv]")
+    return torch.empty(-(-q.shape[0] // DELTA_CHUNK), *v.shape[1:3], q.shape[3], v.shape[3], dtype=torch.float32,
+                       device=q.device)
 
-        u = beta (v - e^g S^T k);  S = e^g S + k u^T;  o = scale S^T q
 
-    q, k [B, Hk, Dk] and v [B, H, Dv] (fp32, bf16 or fp16, any b and head
-    strides; H a multiple of Hk: value head h goes with query and key head
+def delta_scan(q, k, v, g, beta, h0=None, *, scale=None, lengths=None, reset=None, o=None, h_last=None, states=None,
+               workspace=None, stream=None):
+    """The gated delta rule over a sequence: for every stream and value head, with S_t [Dk, Dv] in 32 bits,
+
+        u_t = beta_t (v_t - e^{g_t} S_{t-1}^T k_t);  S_t = e^{g_t} S_{t-1} + k_t u_t^T;  o_t = scale S_t^T q_t
+
+    q, k [T, B, Hk, Dk] and v [T, B, H, Dv] (fp32, bf16 or fp16, any t, b and
+    head strides; H a multiple of Hk: value head h goes with query and key head
     h // (H // Hk); Dk <= 128), g (the decay's logarithm, at most 0) and beta
-    [B, H] fp32.  Returns o [B, H, Dv] and updates state [n_slots, H, Dk, Dv]
-    fp32 in place.  scale: None for Dk ** -0.5.  slots [B] int32: the row of
+    [T, B, H] fp32.  k is used as it is: models give it length 1.  Returns (o,
+    h_last): o [T, B, H, Dv] in v's type, h_last [B, H, Dk, Dv] fp32.
+
+    scale: None for Dk ** -0.5.  h0 [B, H, Dk, Dv] fp32 or None; lengths [B]
+    int32: the timesteps of each stream; reset [T, B] bool or uint8: where true, the
+    state before counts as zero.  ``states`` (:func:`delta_scan_states`) receives
+    what :func:`delta_scan_backward` needs.
+    """
+    args = (q, k, v, g, beta, h0, scale, lengths, reset, o, h_last, states, workspace)
+    return _ops.delta_scan(*args) if stream is None else _on(stream, _ops.delta_scan, *args)
+
+
+def delta_scan_backward(do, q, k, v, g, beta, states, dh_last=None, *, scale=None, lengths=None, reset=None, dq=None,
+                        dk=None, dv=None, dg=None, dbeta=None, dh0=None, workspace=None, stream=None):
+    """Gradients of :func:`delta_scan` (same q, k, v, g, beta, scale, lengths and
+    reset; the states it wrote): (dq, dk, dv, dg, dbeta, dh0), those of q and k
+    summed over the value heads that share them.  dq, dk and dv may be given with
+    any t, b and head strides, as slices of one projection's gradient.
+    """
+    args = (do, q, k, v, g, beta, states, dh_last, scale, lengths, reset, dq, dk, dv, dg, dbeta, dh0, workspace)
+    return _ops.delta_scan_backward(*args) if stream is None else _on(stream, _ops.delta_scan_backward, *args)
+
+
+def delta_step(q, k, v, g, beta, state, *, scale=None, slots=None, reset=None, o=None, stream=None):
+    """One timestep of :func:`delta_scan` for q, k [B, Hk, Dk], v [B, H, Dv], g and
+    beta [B, H]: returns o [B, H, Dv] and updates state [n_slots, H, Dk, Dv]
+    fp32 in place.  slots [B] int32: the row of
     state of each stream (None: row b); one outside [0, n_slots) marks an idle
     stream, whose o is zero.  reset [B]: where true the state counts as zero.
     """

@@ -561,6 +561,88 @@ struct Heads {
   float scale(PyObject* o) const { return o == Py_None ? (float)(1.0 / std::sqrt((double)Dk)) : real(o); }
 };
 
+// delta_scan(q, k, v, g, beta, h0, scale, lengths, reset, o, h_last, states, workspace) -> (o, h_last)
+PyObject* delta_scan(PyObject*, PyObject* const* a, Py_ssize_t) {
+  return guarded([&]() -> PyObject* {
+    const Tensor &q = tensor(a[0], "q"), &v = tensor(a[2], "v");
+    Call call(q, "q");
+    const Heads heads(call, q, v, 2);
+    const int64_t T = heads.lead[0], B = heads.lead[1], H = heads.H, Dk = heads.Dk, Dv = heads.Dv;
+    long long strides[16];
+    int n = 0;
+    void* pq = heads.add(call, q, "q", true, strides, n);
+    void* pk = heads.add(call, tensor(a[1], "k"), "k", true, strides, n);
+    void* pv = heads.add(call, v, "v", false, strides, n);
+    n += 3;
+    const float* g = heads.add_gate(call, tensor(a[3], "g"), "g", strides, n);
+    const float* beta = heads.add_gate(call, tensor(a[4], "beta"), "beta", strides, n);
+    const float* h0 = static_cast<const float*>(call.dense(a[5], "h0", at::kFloat, {B, H, Dk, Dv}));
+    const int32_t* lengths = static_cast<const int32_t*>(call.dense(a[7], "lengths", at::kInt, {B}));
+    const unsigned char* reset = Sequence::resets(call, a[8], {T, B});
+    float* states = static_cast<float*>(call.dense(
+        a[11], "states", at::kFloat, {(T + LSTM_APPROX_DELTA_CHUNK - 1) / LSTM_APPROX_DELTA_CHUNK, B, H, Dk, Dv}));
+    const float scale = heads.scale(a[6]);
+    Tensor o = heads.out(call, a[9], "o", false);
+    n = 9;
+    void* po = heads.add(call, o, "o", false, strides, n);
+    Tensor last = call.out(a[10], "h_last", at::kFloat, {B, H, Dk, Dv});
+    if (states) Call::written(tensor(a[11], "states"));
+    Tensor ws = call.workspace(a[12], lstm_approx_delta_scan_workspace_bytes((int)T, (int)B, (int)H, (int)heads.Hk, (int)Dk, (int)Dv, 0));
+    call.done(lstm_approx_delta_scan(heads.code, pq, pk, pv, g, beta, scale, h0, lengths, reset, (int)T, (int)B, (int)H,
+                                     (int)heads.Hk, (int)Dk, (int)Dv, po, strides, last.data_ptr<float>(), states,
+                                     ws.data_ptr(), ws.nbytes(), call.stream, call.msg, sizeof(call.msg)));
+    return wrap_all(o, last);
+  });
+}
+
+// delta_scan_backward(do, q, k, v, g, beta, states, dh_last, scale, lengths, reset, dq, dk, dv, dg, dbeta, dh0, workspace)
+//   -> (dq, dk, dv, dg, dbeta, dh0)
+PyObject* delta_scan_backward(PyObject*, PyObject* const* a, Py_ssize_t) {
+  return guarded([&]() -> PyObject* {
+    const Tensor &q = tensor(a[1], "q"), &v = tensor(a[3], "v");
+    Call call(q, "q");
+    const Heads heads(call, q, v, 2);
+    const int64_t T = heads.lead[0], B = heads.lead[1], H = heads.H, Dk = heads.Dk, Dv = heads.Dv;
+    long long strides[29];
+    int n = 0;
+    void* pdo = heads.add(call, tensor(a[0], "do"), "do", false, strides, n);
+    void* pq = heads.add(call, q, "q", true, strides, n);
+    void* pk = heads.add(call, tensor(a[2], "k"), "k", true, strides, n);
+    void* pv = heads.add(call, v, "v", false, strides, n);
+    n = 21;
+    const float* g = heads.add_gate(call, tensor(a[4], "g"), "g", strides, n);
+    const float* beta = heads.add_gate(call, tensor(a[5], "beta"), "beta", strides, n);
+    const float* states = static_cast<const float*>(
+        call.dense(tensor(a[6], "states"), "states", at::kFloat,
+                   {(T + LSTM_APPROX_DELTA_CHUNK - 1) / LSTM_APPROX_DELTA_CHUNK, B, H, Dk, Dv}));
+    const float* dl = static_cast<const float*>(call.dense(a[7], "dh_last", at::kFloat, {B, H, Dk, Dv}));
+    const int32_t* lengths = static_cast<const int32_t*>(call.dense(a[9], "lengths", at::kInt, {B}));
+    const unsigned char* reset = Sequence::resets(call, a[10], {T, B});
+    const float scale = heads.scale(a[8]);
+    Tensor dq = heads.out(call, a[11], "dq", true), dk = heads.out(call, a[12], "dk", true), dv = heads.out(call, a[13], "dv", false);
+    auto gate_out = [&](PyObject* o, const char* name) {
+      if (o == Py_None) return call.out(o, name, at::kFloat, heads.per_head());
+      Call::written(tensor(o, name));
+      return tensor(o, name);
+    };
+    Tensor dg = gate_out(a[14], "dg"), dbeta = gate_out(a[15], "dbeta");
+    n = 12;
+    void* pdq = heads.add(call, dq, "dq", true, strides, n);
+    void* pdk = heads.add(call, dk, "dk", true, strides, n);
+    void* pdv = heads.add(call, dv, "dv", false, strides, n);
+    n = 25;
+    float* pdg = heads.add_gate(call, dg, "dg", strides, n);
+    float* pdbeta = heads.add_gate(call, dbeta, "dbeta", strides, n);
+    Tensor dh0 = call.out(a[16], "dh0", at::kFloat, {B, H, Dk, Dv});
+    Tensor ws = call.workspace(a[17], lstm_approx_delta_scan_workspace_bytes((int)T, (int)B, (int)H, (int)heads.Hk, (int)Dk, (int)Dv, 1));
+    call.done(lstm_approx_delta_scan_backward(heads.code, pdo, dl, pq, pk, pv, g, beta, scale, states, lengths, reset, (int)T,
+                                              (int)B, (int)H, (int)heads.Hk, (int)Dk, (int)Dv, pdq, pdk, pdv, pdg, pdbeta,
+                                              dh0.data_ptr<float>(), strides, ws.data_ptr(), ws.nbytes(), call.stream, call.msg,
+                                              sizeof(call.msg)));
+    return wrap_all(dq, dk, dv, dg, dbeta, dh0);
+  });
+}
+
 // delta_step(q, k, v, g, beta, state, scale, slots, reset, o) -> o
 PyObject* delta_step(PyObject*, PyObject* const* a, Py_ssize_t) {
   return guarded([&]() -> PyObject* {
@@ -720,6 +802,7 @@ PyMethodDef g_methods[] = {
     entry<gated_scan, 12>("gated_scan"),      entry<gated_scan_backward, 16>("gated_scan_backward"),
     entry<gated_step, 9>("gated_step"),       entry<w4_quantize, 5>("w4_quantize"),
     entry<w4_matvec, 12>("w4_matvec"),        entry<delta_step, 10>("delta_step"),
+    entry<delta_scan, 13>("delta_scan"),      entry<delta_scan_backward, 18>("delta_scan_backward"),
     entry<adamw_step, 16>("adamw_step"),      {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_torch_ops", "The operators on torch tensors (see _operators).", -1,
