@@ -286,8 +286,8 @@ size_t lstm_approx_w4_workspace_bytes(int x_dtype, int M, int K);
  *   states    [ceil(T / LSTM_APPROX_DELTA_CHUNK)][B][H][Dk][Dv] fp32, or NULL:
  *             the state before every chunk's first timestep (of chunks that the
  *             stream reaches), kept for the backward pass
- *   workspace at least lstm_approx_delta_scan_workspace_bytes(T, B, H, Hk, Dk,
- *             Dv, 0) bytes, 16-byte aligned, not shared by calls in flight
+ *   workspace at least lstm_approx_delta_scan_workspace_bytes(dtype, T, B, H,
+ *             Hk, Dk, Dv, 0) bytes, 16-byte aligned, not shared by calls in flight
  *
  * Values that are not finite stay in their stream, head and (from the next
  * reset on) document, but reach earlier timesteps of their chunk.
@@ -300,8 +300,8 @@ int lstm_approx_delta_scan(int dtype, const void *q, const void *k, const void *
                            void *workspace, size_t workspace_bytes, void *cuda_stream, char *msg,
                            int msg_len);
 /* Workspace bytes of the call above, or (backward not 0) of the next; 0 for invalid sizes. */
-size_t lstm_approx_delta_scan_workspace_bytes(int T, int B, int H, int Hk, int Dk, int Dv,
-                                              int backward);
+size_t lstm_approx_delta_scan_workspace_bytes(int dtype, int T, int B, int H, int Hk, int Dk,
+                                              int Dv, int backward);
 
 /*
  * Its gradients:
@@ -315,8 +315,8 @@ size_t lstm_approx_delta_scan_workspace_bytes(int T, int B, int H, int Hk, int D
  *   strides   HOST [29]: the t, b and head strides of d_o, q, k, v, dq, dk and dv,
  *             the t and b strides of g, beta, dg and dbeta, in this order; NULL:
  *             all contiguous
- *   workspace at least lstm_approx_delta_scan_workspace_bytes(T, B, H, Hk, Dk,
- *             Dv, 1) bytes, 16-byte aligned, not shared by calls in flight
+ *   workspace at least lstm_approx_delta_scan_workspace_bytes(dtype, T, B, H,
+ *             Hk, Dk, Dv, 1) bytes, 16-byte aligned, not shared by calls in flight
  *
  * dg is zero at a reset and where g is below -200.
  */

@@ -103,7 +103,7 @@ def load(path: str = LIB_PATH):
     lib.lstm_approx_w4_workspace_bytes.argtypes = [I, I, I]
     lib.lstm_approx_delta_scan.argtypes = [I, P, P, P, P, P, F, P, P, P, I, I, I, I, I, I, P, P, P, P, P, Z] + end
     lib.lstm_approx_delta_scan_backward.argtypes = ([I, P, P, P, P, P, P, P, F, P, P, P, I, I, I, I, I, I] + [P] * 8 + [Z] + end)
-    lib.lstm_approx_delta_scan_workspace_bytes.argtypes = [I, I, I, I, I, I, I]
+    lib.lstm_approx_delta_scan_workspace_bytes.argtypes = [I] * 8
     lib.lstm_approx_delta_step.argtypes = [I, P, P, P, P, P, F, P, I, P, P, I, I, I, I, I, P, P] + end
     lib.lstm_approx_adamw_step.argtypes = [I, P, I, I, P, D, P, D, D, D, D, P, P, ctypes.c_uint] + end
     for name in EXPORTS:

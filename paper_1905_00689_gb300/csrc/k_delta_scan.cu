@@ -5,35 +5,45 @@
 //
 //   u_t = beta_t (v_t - e^{g_t} S_{t-1}^T k_t);  S_t = e^{g_t} S_{t-1} + k_t u_t^T;  o_t = scale S_t^T q_t
 //
-// By chunks of 64 timesteps (i, j: rows of a chunk; S0: the state before it; G: the sum of g up to and with a row):
+// By chunks of 64 timesteps (i, j: rows of a chunk; S0: the state before it; G: the sum of g up to and with a row; B:
+// diag(beta)):
 //
 //   D_ij = e^{G_i - G_j} (i >= j);  gam_i = e^{G_i};  dec_j = e^{G_63 - G_j}
-//   A_ij = beta_i D_ij k_i . k_j (i > j);  Tm = (I + A)^-1;  M_ij = D_ij q_i . k_j
-//   U = Tm diag(beta) (V - diag(gam) K S0);  O = scale (diag(gam) Q S0 + M U);  S = gam_63 S0 + K^T diag(dec) U
+//   A_ij = D_ij k_i . k_j (i > j);  N = (I + A B)^-1 A;  M_ij = D_ij q_i . k_j
+//   X = V - diag(gam) K S0;  Y = X - N B X;  U = B Y
+//   O = scale (diag(gam) Q S0 + M U);  S = gam_63 S0 + K^T diag(dec) U
 //
-// and for the gradients (dS that of S, R = Tm^T dU):
+// and for the gradients (dS that of S):
 //
-//   dU = scale M^T dO + diag(dec) K dS;  dV = diag(beta) R
-//   dS0 = gam_63 dS + Q^T diag(scale gam) dO - K^T diag(beta gam) R
-//   P_ij = scale D_ij dO_i . u_j (i >= j);  E_ij = D_ij R_i . u_j (i > j);  w = diag(gam) R S0^T + E K
-//   dQ = P K + diag(scale gam) dO S0^T;  t = P^T Q - E^T diag(beta) K + diag(dec) U dS^T;  dK = t - diag(beta) w
-//   dbeta_i = R_i . v_i - k_i . w_i;  dG_i = q_i . dq_i - k_i . (beta_i w_i + t_i)
-//   dG_63 += gam_63 <dS, S0> + sum_j dec_j k_j . (dS u_j);  dg_t = sum of dG_i over i >= t
+//   dU = scale M^T dO + diag(dec) K dS;  R = dU - N^T B dU;  dV = B R
+//   dS0 = gam_63 dS + Q^T diag(scale gam) dO - K^T diag(gam) dV;  dbeta_i = R_i . Y_i
+//   P_ij = scale D_ij dO_i . u_j (i >= j);  E_ij = beta_i D_ij R_i . u_j (i > j)
+//   dQ = P K + diag(scale gam) dO S0^T
+//   dK = P^T Q + diag(dec) U dS^T - E^T K - E K - diag(gam) dV S0^T
 //
-// Kernels: one per chunk and head makes Tm and M; one per head and 16 or 32
-// columns of S (which do not see one another) runs along the chunks, forward or
-// backward; one per chunk makes the gradients of q, k, g and beta.
+// Scaling g_t scales what is there of S_t, of which everything behind is linear:
 //
-// Products run on the warp MMAs of 32-bit floats cut to 11 bits (m16n8k8): an
-// operand that came in 16 bits is exact there, any other is taken in two parts,
-// value = high + low, and two or three products are summed in 32 bits, which
-// leaves 2^-21 of a factor at most.  A state carries thousands of timesteps, so
-// these are not rounded to 16 bits.
+//   dg_t = <dS0, S0> - the sum of q_i . dq_i - v_i . dv_i over rows i < t
+//
+// Kernels: one per chunk and key head makes N and M, and copies of q and k whose
+// rows have 64 or 128 columns; one per value head and 16 or 32 columns of S (which
+// do not see one another) runs along the chunks, forward or backward; one per
+// chunk and key head makes the gradients of q, k, g and beta.
+//
+// Products run on warp MMAs of bf16 with 32-bit sums.  An operand of 32 bits is
+// taken in three parts of 8 bits each (x = high + middle + low), one in fp16 in
+// two, and the products of parts down to 2^-16 of the largest are summed: 2^-24
+// of a factor is left out.  What only goes into a 16-bit output has two parts and
+// products down to 2^-8 (2^-16 left out).  A state carries thousands of
+// timesteps, so it is never rounded to 16 bits.  An operand is split once, where
+// it is made, and lies in shared memory as the MMA wants it.  (Split where it is
+// used, in two parts of 11 bits on MMAs of 32-bit floats, these kernels executed
+// 4 times the instructions: a chunk of 64 x 128 x 16 took 5.1 us.)
 //
 // At a reset the state before counts as zero, and so does everything before it
 // in its chunk: a chunk with resets is taken piece by piece, and rows of other
 // pieces are left out, not multiplied by zero.
-#include <algorithm>
+#include <type_traits>
 
 #include "ops_common.cuh"
 
@@ -47,177 +57,136 @@ static_assert(C == 64, "rows of a chunk");
 constexpr int kThreads = 256;
 constexpr float kLeastG = -200.0f;
 
+using bf16 = __nv_bfloat16;
+
+// Parts of a value of T; of an operand of the sums that only a T is made of, and how far their products go (see `mma`).
+template <typename T>
+constexpr int kParts = sizeof(T) == 4 ? 3 : std::is_same_v<T, bf16> ? 1 : 2;
+template <typename T>
+constexpr int kOutParts = sizeof(T) == 4 ? 3 : 2;
+template <typename T>
+constexpr int kOutDepth = sizeof(T) == 4 ? 2 : 1;
+
 // ---- matrices in shared memory and the products of warps ---------------------
 
-// [64][W] values of T.  Every row's 16-byte pieces (16 bits) or 8-word groups (32 bits) are exchanged by a rule on the row, so
-// that eight rows of a column, or a row's neighbours, lie in different banks.
-template <typename T, int W>
-struct Tile {
-  T* p;
+// [kRows][W] values, kP parts of each, one matrix behind the other.  16-byte pieces of a row are exchanged by a rule on the row:
+// the same piece of eight neighbouring rows lies in different banks.
+template <int kRows, int W, int kP>
+struct Mat {
+  bf16* p;
+  static constexpr int kSize = kRows * W, kBytes = kSize * kP * 2;
   __device__ __forceinline__ static int at(int row, int col) {
-    if constexpr (sizeof(T) == 2) return row * W + (col ^ (row & 7) << 3);
-    else return row * W + (col ^ ((row ^ row >> 2) & 3) << 3);
+    constexpr int kPieces = W / 8;
+    const int turn = kPieces >= 8 ? row & 7 : row / (8 / kPieces) & (kPieces - 1);
+    return row * W + (col ^ turn << 3);
+  }
+  // Columns col and col + 1 (col even).
+  __device__ __forceinline__ void put(int row, int col, float x, float y) const {
+    const int i = at(row, col);
+#pragma unroll
+    for (int q = 0; q < kP; ++q) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+      *reinterpret_cast<__nv_bfloat162*>(p + q * kSize + i) = h;
+      if (q + 1 < kP) {
+        const float2 f = __bfloat1622float2(h);
+        x -= f.x;
+        y -= f.y;
+      }
+    }
   }
   __device__ __forceinline__ float2 pair(int row, int col) const {
-    return Pair<T>::get(*reinterpret_cast<const typename Pair<T>::Raw*>(p + at(row, col)));
+    const int i = at(row, col);
+    float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int q = kP - 1; q >= 0; --q) {
+      const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(p + q * kSize + i));
+      s.x += f.x;
+      s.y += f.y;
+    }
+    return s;
   }
-  __device__ __forceinline__ float one(int row, int col) const { return to_f32(p[at(row, col)]); }
-};
-// 32-bit values, rows LD apart.
-template <int LD>
-struct Padded {
-  float* p;
-  __device__ __forceinline__ float2 pair(int row, int col) const { return *reinterpret_cast<const float2*>(p + row * LD + col); }
-  __device__ __forceinline__ float one(int row, int col) const { return p[row * LD + col]; }
-  __device__ __forceinline__ float& to(int row, int col) { return p[row * LD + col]; }
 };
 
-// The products below are reached by whole warps: a barrier lies before each, and between that and the last of its loads and
-// MMAs only branches that a warp's lanes take alike.
-//
-// Parts of the m16n8k8 MMA's operands: lane = 4 g + t holds rows g, g + 8 of A (columns 2 t, then 2 t + 1: the order of k is
-// free as long as both agree) and column g of B.
-struct FragA {
-  float x[4];  // (g, 2t), (g + 8, 2t), (g, 2t + 1), (g + 8, 2t + 1)
-};
-struct FragB {
-  float x[2];  // (2t, g), (2t + 1, g)
-};
-
+// The loads and MMAs below are reached by whole warps: a barrier lies before each, and between that and the last of them only
+// branches that a warp's lanes take alike.  Lane = 4 g + t of an MMA has rows g and g + 8 and columns 2 t and 2 t + 1 of its
+// result.
 __device__ __forceinline__ int lane_g() { return (threadIdx.x & 31) >> 2; }
 __device__ __forceinline__ int lane_t() { return threadIdx.x & 3; }
 
-template <typename T>
-__device__ __forceinline__ float2 unpack(uint32_t v) {
-  return Pair<T>::get(*reinterpret_cast<const typename Pair<T>::Raw*>(&v));
+// A, 16 rows and 16 columns (k): kP parts of it, from rows that are A's; from rows that are A's columns.
+template <int kP, int kRows, int W, int kHas>
+__device__ __forceinline__ void load_a(const Mat<kRows, W, kHas>& m, int m0, int k0, uint32_t (&a)[kP][4]) {
+  static_assert(kP <= kHas, "parts");
+  const int l = threadIdx.x & 31;
+  const uint32_t addr = smem_u32(m.p + m.at(m0 + (l & 15), k0 + (l >> 4) * 8));
+#pragma unroll
+  for (int q = 0; q < kP; ++q) ldmatrix4<true>(addr + q * m.kSize * 2, a[q]);
+}
+template <int kP, int kRows, int W, int kHas>
+__device__ __forceinline__ void load_at(const Mat<kRows, W, kHas>& m, int m0, int k0, uint32_t (&a)[kP][4]) {
+  static_assert(kP <= kHas, "parts");
+  const int l = threadIdx.x & 31;
+  const uint32_t addr = smem_u32(m.p + m.at(k0 + (l & 7) + (l >> 4) * 8, m0 + (l >> 3 & 1) * 8));
+#pragma unroll
+  for (int q = 0; q < kP; ++q) ldmatrix4_trans<true>(addr + q * m.kSize * 2, a[q]);
+}
+// B, 16 rows (k) and 16 columns, [part][column / 8][k / 8]: from rows that are B's columns; from rows that are B's.
+template <int kP, int kRows, int W, int kHas>
+__device__ __forceinline__ void load_b(const Mat<kRows, W, kHas>& m, int n0, int k0, uint32_t (&b)[kP][2][2]) {
+  static_assert(kP <= kHas, "parts");
+  const int l = threadIdx.x & 31;
+  const uint32_t addr = smem_u32(m.p + m.at(n0 + (l & 7) + (l >> 4) * 8, k0 + (l >> 3 & 1) * 8));
+#pragma unroll
+  for (int q = 0; q < kP; ++q) {
+    uint32_t r[4];
+    ldmatrix4<true>(addr + q * m.kSize * 2, r);
+    b[q][0][0] = r[0], b[q][0][1] = r[1], b[q][1][0] = r[2], b[q][1][1] = r[3];
+  }
+}
+template <int kP, int kRows, int W, int kHas>
+__device__ __forceinline__ void load_bt(const Mat<kRows, W, kHas>& m, int n0, int k0, uint32_t (&b)[kP][2][2]) {
+  static_assert(kP <= kHas, "parts");
+  const int l = threadIdx.x & 31;
+  const uint32_t addr = smem_u32(m.p + m.at(k0 + (l & 15), n0 + (l >> 4) * 8));
+#pragma unroll
+  for (int q = 0; q < kP; ++q) {
+    uint32_t r[4];
+    ldmatrix4_trans<true>(addr + q * m.kSize * 2, r);
+    b[q][0][0] = r[0], b[q][0][1] = r[1], b[q][1][0] = r[2], b[q][1][1] = r[3];
+  }
+}
+// The same of 32 rows of k and 8 columns: [part][k / 16][k / 8 % 2].
+template <int kP, int kRows, int W, int kHas>
+__device__ __forceinline__ void load_bt_tall(const Mat<kRows, W, kHas>& m, int n0, int k0, uint32_t (&b)[kP][2][2]) {
+  static_assert(kP <= kHas, "parts");
+  const uint32_t addr = smem_u32(m.p + m.at(k0 + (threadIdx.x & 31), n0));
+#pragma unroll
+  for (int q = 0; q < kP; ++q) {
+    uint32_t r[4];
+    ldmatrix4_trans<true>(addr + q * m.kSize * 2, r);
+    b[q][0][0] = r[0], b[q][0][1] = r[1], b[q][1][0] = r[2], b[q][1][1] = r[3];
+  }
 }
 
-// A of 16 rows and 16 columns of k from a tile whose rows are A's.
-template <typename T, int W>
-__device__ __forceinline__ void load_a(const Tile<T, W>& tile, int m0, int k0, FragA (&f)[2]) {
-  if constexpr (sizeof(T) == 2) {
-    const int l = threadIdx.x & 31;
-    uint32_t r[4];
-    ldmatrix4<true>(smem_u32(tile.p + tile.at(m0 + (l & 15), k0 + (l >> 4) * 8)), r);
+// d + e += a b: part i of a with part j of b where i + j <= kDepth, the first ones' product to d, the others to e.
+template <int kDepth, int kPA, int kPB>
+__device__ __forceinline__ void mma(float (&d)[4], float (&e)[4], const uint32_t (&a)[kPA][4], const uint32_t (&b0)[kPB],
+                                    const uint32_t (&b1)[kPB]) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const float2 a = unpack<T>(r[2 * s]), b = unpack<T>(r[2 * s + 1]);
-      f[s] = {{a.x, b.x, a.y, b.y}};
-    }
-  } else {
+  for (int s = kDepth; s >= 0; --s)
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const float2 a = tile.pair(m0 + lane_g(), k0 + 8 * s + 2 * lane_t()), b = tile.pair(m0 + 8 + lane_g(), k0 + 8 * s + 2 * lane_t());
-      f[s] = {{a.x, b.x, a.y, b.y}};
-    }
-  }
+    for (int i = 0; i < kPA; ++i)
+      if (s - i >= 0 && s - i < kPB)
+        mma_16816_bf16<true, false>(s ? e : d, a[i][0], a[i][1], a[i][2], a[i][3], b0[s - i], b1[s - i]);
 }
-template <int LD>
-__device__ __forceinline__ void load_a(const Padded<LD>& m, int m0, int k0, FragA (&f)[2]) {
+template <int kDepth, int kPA, int kPB>
+__device__ __forceinline__ void mma(float (&d)[4], float (&e)[4], const uint32_t (&a)[kPA][4], const uint32_t (&b)[kPB][2][2], int x) {
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const float2 a = m.pair(m0 + lane_g(), k0 + 8 * s + 2 * lane_t()), b = m.pair(m0 + 8 + lane_g(), k0 + 8 * s + 2 * lane_t());
-    f[s] = {{a.x, b.x, a.y, b.y}};
-  }
-}
-// The same from a tile whose columns are A's rows.
-template <typename Mat>
-__device__ __forceinline__ void load_at_words(const Mat& m, int m0, int k0, FragA (&f)[2]) {
+  for (int s = kDepth; s >= 0; --s)
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const int k = k0 + 8 * s + 2 * lane_t(), r = m0 + lane_g();
-    f[s] = {{m.one(k, r), m.one(k, r + 8), m.one(k + 1, r), m.one(k + 1, r + 8)}};
-  }
-}
-template <typename T, int W>
-__device__ __forceinline__ void load_at(const Tile<T, W>& tile, int m0, int k0, FragA (&f)[2]) {
-  if constexpr (sizeof(T) == 2) {
-    const int l = threadIdx.x & 31;
-    uint32_t r[4];
-    ldmatrix4_trans<true>(smem_u32(tile.p + tile.at(k0 + (l & 7) + (l >> 4) * 8, m0 + (l >> 3 & 1) * 8)), r);
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const float2 a = unpack<T>(r[2 * s]), b = unpack<T>(r[2 * s + 1]);
-      f[s] = {{a.x, b.x, a.y, b.y}};
-    }
-  } else {
-    load_at_words(tile, m0, k0, f);
-  }
-}
-template <int LD>
-__device__ __forceinline__ void load_at(const Padded<LD>& m, int m0, int k0, FragA (&f)[2]) {
-  load_at_words(m, m0, k0, f);
-}
-
-// B of 16 rows of k and 16 columns (f[column / 8][k / 8]) from a tile whose rows are B's columns.
-template <typename T, int W>
-__device__ __forceinline__ void load_b16(const Tile<T, W>& tile, int n0, int k0, FragB (&f)[2][2]) {
-  if constexpr (sizeof(T) == 2) {
-    const int l = threadIdx.x & 31;
-    uint32_t r[4];
-    ldmatrix4<true>(smem_u32(tile.p + tile.at(n0 + (l & 15), k0 + (l >> 4) * 8)), r);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float2 v = unpack<T>(r[q]);
-      f[q & 1][q >> 1] = {{v.x, v.y}};
-    }
-  } else {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float2 v = tile.pair(n0 + 8 * (q & 1) + lane_g(), k0 + 8 * (q >> 1) + 2 * lane_t());
-      f[q & 1][q >> 1] = {{v.x, v.y}};
-    }
-  }
-}
-// From a tile whose rows are B's.
-template <typename T, int W>
-__device__ __forceinline__ void load_bt16(const Tile<T, W>& tile, int n0, int k0, FragB (&f)[2][2]) {
-  if constexpr (sizeof(T) == 2) {
-    const int l = threadIdx.x & 31;
-    uint32_t r[4];
-    ldmatrix4_trans<true>(smem_u32(tile.p + tile.at(k0 + (l & 15), n0 + (l >> 4) * 8)), r);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float2 v = unpack<T>(r[q]);
-      f[q >> 1][q & 1] = {{v.x, v.y}};
-    }
-  } else {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int n = n0 + 8 * (q >> 1) + lane_g(), k = k0 + 8 * (q & 1) + 2 * lane_t();
-      f[q >> 1][q & 1] = {{tile.one(k, n), tile.one(k + 1, n)}};
-    }
-  }
-}
-// 8 columns and 8 rows of k from 32-bit rows that are B's columns; that are B's rows.
-template <int LD>
-__device__ __forceinline__ FragB load_b(const Padded<LD>& m, int n0, int k0) {
-  const float2 v = m.pair(n0 + lane_g(), k0 + 2 * lane_t());
-  return {{v.x, v.y}};
-}
-template <int LD>
-__device__ __forceinline__ FragB load_bt(const Padded<LD>& m, int n0, int k0) {
-  return {{m.one(k0 + 2 * lane_t(), n0 + lane_g()), m.one(k0 + 2 * lane_t() + 1, n0 + lane_g())}};
-}
-
-// x = high + low: the MMA reads a sign, 8 bits of exponent and 10 of fraction.  high: x to the nearest of those (its further
-// bits are not read); low: what is left, of either sign (cut off instead, x would lose 2^-22 of itself on average, and a long
-// sequence of that shows: 9e-7 of o, so 4e-7).  Not finite values stay so in one of the two.
-__device__ __forceinline__ float high(float x) { return __uint_as_float(__float_as_uint(x) + 0x1000u); }
-__device__ __forceinline__ float low(float x) { return x - __uint_as_float((__float_as_uint(x) + 0x1000u) & 0xffffe000u); }
-
-// d + e += a b: the high parts' product to d, the others to e (two chains of sums; d and e may be the same).
-// kOneA, kOneB: the operand is exact in 11 bits.
-template <bool kOneA, bool kOneB>
-__device__ __forceinline__ void mma(float (&d)[4], float (&e)[4], const FragA& a, const FragB& b) {
-  float ah[4], bh[2];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) ah[i] = kOneA ? a.x[i] : high(a.x[i]);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) bh[i] = kOneB ? b.x[i] : high(b.x[i]);
-  if constexpr (!kOneB) mma_1688_tf32<true>(e, ah[0], ah[1], ah[2], ah[3], low(b.x[0]), low(b.x[1]));
-  if constexpr (!kOneA) mma_1688_tf32<true>(e, low(a.x[0]), low(a.x[1]), low(a.x[2]), low(a.x[3]), bh[0], bh[1]);
-  mma_1688_tf32<true>(d, ah[0], ah[1], ah[2], ah[3], bh[0], bh[1]);
+    for (int i = 0; i < kPA; ++i)
+      if (s - i >= 0 && s - i < kPB)
+        mma_16816_bf16<true, false>(s ? e : d, a[i][0], a[i][1], a[i][2], a[i][3], b[s - i][x][0], b[s - i][x][1]);
 }
 
 // ---- what the kernels share ----------------------------------------------------
@@ -244,57 +213,59 @@ struct DeltaArgs {
   const int32_t* lengths;
   const unsigned char* reset;
   int T, B, H, share, Dk, Dv, tiles;
-  bool wide;   // q and k in 16-byte pieces
+  bool wide;   // q, k, dq and dk in 16-byte pieces
   bool pairs;  // v, o, dO and dV two at a time
+  bool even;   // states two at a time
   void* o;
   float *h_last, *states;
-  // workspace: per chunk, stream and head
-  float *Tm, *M;
-  Gates* gates;
+  // workspace: per chunk, stream and key head the parts of k and q; per value head those of N and M, and the gates
+  unsigned char *keys, *heads;
   // backward
   const float* dh_last;
-  float *dS, *R, *sum_q, *sum_k;
+  float *dS, *R, *dots, *sum_q, *sum_k;
   void *dq, *dk, *dv;
   float *dg, *dbeta, *dh0;
   long long dgt, dgb, dbt, dbb;
 };
 
+// The workspace's parts.  M has three parts where a backward pass reads it.
+template <typename T, int KD>
+using KeyMat = Mat<C, KD, kParts<T>>;
+using SquareMat = Mat<C, C, 3>;
+template <typename T, int KD>
+constexpr size_t kKeysBytes = 2 * KeyMat<T, KD>::kBytes;
+constexpr size_t kHeadBytes = 2 * SquareMat::kBytes + sizeof(Gates);
+
 __device__ __forceinline__ int length_of(const DeltaArgs& a, int b) {
   return a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
 }
 
-__device__ __forceinline__ void copy16(void* to, const void* from, int bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(bytes) : "memory");
+__device__ __forceinline__ void copy16(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kLeft>
 __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
 }
-
-// Rows [lo, hi) of a chunk of q or k; zeros elsewhere and past Dk.  p: the chunk's first row.
-template <typename T, int W>
-__device__ __forceinline__ void fetch_tile(Tile<T, W> to, const T* p, long long t_stride, int lo, int hi, int Dk, bool wide) {
-  constexpr int kPer = 16 / (int)sizeof(T);
-  for (int i = threadIdx.x; i < C * (W / kPer); i += kThreads) {
-    const int row = i / (W / kPer), col = i % (W / kPer) * kPer;
-    T* dst = to.p + to.at(row, col);
-    const bool in = row >= lo && row < hi;
-    if (wide) {
-      const bool some = in && col < Dk;
-      copy16(dst, some ? p + row * t_stride + col : p, some ? 16 : 0);
-    } else {
-      T x[kPer];
+template <int kBytes>
+__device__ __forceinline__ void fetch(void* to, const void* from) {
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) x[e] = in && col + e < Dk ? p[row * t_stride + col + e] : from_f32<T>(0.0f);
-      *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(x);
-    }
-  }
+  for (int i = 0; i < kBytes; i += kThreads * 16)
+    if (i + kThreads * 16 <= kBytes || i + (int)threadIdx.x * 16 < kBytes)
+      copy16(static_cast<char*>(to) + i + threadIdx.x * 16, static_cast<const char*>(from) + i + threadIdx.x * 16);
 }
-template <typename P>
-__device__ __forceinline__ void fetch_plain(P* to, const P* from, int bytes) {
-  for (int i = threadIdx.x; i < bytes / 16; i += kThreads)
-    copy16(reinterpret_cast<char*>(to) + i * 16, reinterpret_cast<const char*>(from) + i * 16, 16);
+// The same of kP parts of a square matrix without its blocks above the diagonal.
+template <int kP>
+__device__ __forceinline__ void fetch_lower(bf16* to, const bf16* from) {
+  static_assert(C * C / 8 == 2 * kThreads, "two rounds to a part");
+#pragma unroll
+  for (int q = 0; q < kP; ++q)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int i = (half * kThreads + (int)threadIdx.x) * 8, row = i / C, col = (i % C) ^ (row & 7) << 3;
+      if (col / 16 <= row / 16) copy16(to + q * C * C + i, from + q * C * C + i);
+    }
 }
 
 // Two neighbouring values of a row (the second only if it lies in the row).
@@ -320,180 +291,274 @@ __device__ __forceinline__ int piece_end(unsigned long long cuts, int lo) {
 }
 // Whether a reset lies at or before the row.
 __device__ __forceinline__ bool cut_before(unsigned long long cuts, int row) { return (cuts << (63 - row)) != 0ull; }
-
 // Whether one lies behind row j and not behind row i >= j.
 __device__ __forceinline__ bool cut_between(unsigned long long cuts, int j, int i) {
   return i > j && cuts >> (j + 1) << (64 - (i - j)) != 0ull;
 }
 
-// ---- per chunk and head: gates, Tm and M ----------------------------------------
+// ---- per chunk and key head: copies of q and k, gates, N and M --------------------
 
 template <typename T, int KD>
+struct PrepareShared {
+  KeyMat<T, KD> K, Q;
+  float *A, *N, *H;  // [C][kPitch]
+  Gates* gates;
+  static constexpr int kPitch = C + 4;
+  static constexpr size_t kBytes = kKeysBytes<T, KD> + (2 * C + C / 2) * kPitch * 4 + sizeof(Gates);
+  __device__ __forceinline__ explicit PrepareShared(unsigned char* p)
+      : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * kParts<T>}, A(reinterpret_cast<float*>(Q.p + Q.kSize * kParts<T>)),
+        N(A + C * kPitch), H(N + C * kPitch), gates(reinterpret_cast<Gates*>(H + C / 2 * kPitch)) {}
+};
+
+// Rows of q or k as the MMAs read them: in parts, zeros past the stream's length and past Dk.
+template <typename T, int KD>
+__device__ __forceinline__ void fill_keys(const KeyMat<T, KD>& to, const T* p, long long t_stride, int rows, int Dk, bool wide) {
+  constexpr int kPer = 16 / (int)sizeof(T);
+#pragma unroll 4
+  for (int i = threadIdx.x; i < C * (KD / kPer); i += kThreads) {
+    const int row = i / (KD / kPer), col = i % (KD / kPer) * kPer;
+    uint4 raw = make_uint4(0u, 0u, 0u, 0u);
+    if (row < rows) {
+      if (wide) {
+        if (col < Dk) raw = *reinterpret_cast<const uint4*>(p + row * t_stride + col);
+      } else {
+        T x[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) x[e] = col + e < Dk ? p[row * t_stride + col + e] : from_f32<T>(0.0f);
+        raw = *reinterpret_cast<const uint4*>(x);
+      }
+    }
+    if constexpr (std::is_same_v<T, bf16>) {
+      *reinterpret_cast<uint4*>(to.p + to.at(row, col)) = raw;
+    } else {
+      const typename Pair<T>::Raw* h = reinterpret_cast<const typename Pair<T>::Raw*>(&raw);
+#pragma unroll
+      for (int e = 0; e < kPer / 2; ++e) {
+        const float2 f = Pair<T>::get(h[e]);
+        to.put(row, col + 2 * e, f.x, f.y);
+      }
+    }
+  }
+}
+
+// One warp: a chunk's sums of g, the decays that follow, beta (rows lane and lane + 32).  The sums are of 64 bits, so that
+// differences of far ones keep their digits, and begin anew at a reset, whose own g counts as zero.
+__device__ __forceinline__ void make_gates(const DeltaArgs& a, int t0, int rows, int b, int h, Gates& gates) {
+  const int lane = threadIdx.x & 31;
+  double G[2];
+  unsigned cut[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const int row = lane + 32 * s;
+    const long long t = t0 + row;
+    float g = 0.0f, beta = 0.0f;
+    bool reset = false;
+    if (row < rows) {
+      g = a.g[t * a.gt + b * a.gb + h];
+      g = g < kLeastG ? kLeastG : g;
+      beta = a.beta[t * a.bt + b * a.bb + h];
+      reset = a.reset && a.reset[t * a.B + b];
+    }
+    gates.beta[row] = beta;
+    cut[s] = __ballot_sync(0xffffffffu, reset);
+    const unsigned before = cut[s] & (2u << lane) - 1u;
+    const int start = before ? 31 - __clz((int)before) : 0;
+    double x = reset ? 0.0 : (double)g;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const double y = __shfl_up_sync(0xffffffffu, x, d);
+      if (lane - d >= start) x += y;
+    }
+    G[s] = x;
+  }
+  const double first = __shfl_sync(0xffffffffu, G[0], 31);
+  if (!(cut[1] & (2u << lane) - 1u)) G[1] += first;
+  const double last = __shfl_sync(0xffffffffu, G[1], 31);
+  const unsigned long long cuts = cut[0] | (unsigned long long)cut[1] << 32;
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const int row = lane + 32 * s;
+    const float high = (float)G[s], rest = (float)(G[s] - (double)high), e = expf(high);
+    gates.g_high[row] = high;
+    gates.g_low[row] = rest;
+    gates.gam[row] = cut_before(cuts, row) ? 0.0f : fmaf(e, rest, e);
+    gates.dec[row] = row < 63 && cuts >> (row + 1) ? 0.0f : expf((float)(last - G[s]));
+  }
+  if (lane == 0) gates.cuts = cuts, gates.pad = 0ull;
+}
+
+template <typename T, int KD, bool kBackward>
 __global__ void __launch_bounds__(kThreads) delta_prepare_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
-  Tile<T, KD> K{reinterpret_cast<T*>(smem)}, Q{K.p + C * KD};
-  Padded<C + 4> A{reinterpret_cast<float*>(Q.p + C * KD)}, Ti{A.p + C * (C + 4)};
-  Gates& gates = *reinterpret_cast<Gates*>(Ti.p + C * (C + 4));
+  using Sh = PrepareShared<T, KD>;
+  constexpr int kPitch = Sh::kPitch;
+  const Sh sh(smem);
+  Gates& gates = *sh.gates;
   begin_op();
-  const long long chunk = blockIdx.x;  // (n B + b) H + h
-  const int h = (int)(chunk % a.H), b = (int)(chunk / a.H % a.B), n = (int)(chunk / a.H / a.B);
+  const int Hk = a.H / a.share, hk = (int)(blockIdx.x % Hk), b = (int)(blockIdx.x / Hk % a.B), n = (int)(blockIdx.x / Hk / a.B);
   const int t0 = n * C, rows = min(length_of(a, b) - t0, C);
   if (rows <= 0) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const T* k = static_cast<const T*>(a.k) + t0 * a.ks.t + b * a.ks.b + (h / a.share) * a.ks.h;
-  const T* q = static_cast<const T*>(a.q) + t0 * a.qs.t + b * a.qs.b + (h / a.share) * a.qs.h;
-  fetch_tile(K, k, a.ks.t, 0, rows, a.Dk, a.wide);
-  fetch_tile(Q, q, a.qs.t, 0, rows, a.Dk, a.wide);
-  copies_commit();
-  if (warp == 0) {  // rows lane and lane + 32; the sums in 64 bits: differences of far sums keep their digits
-    double G[2];
-    unsigned cut[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int row = lane + 32 * s, t = t0 + row;
-      float g = 0.0f, beta = 0.0f;
-      bool reset = false;
-      if (row < rows) {
-        g = a.g[t * a.gt + b * a.gb + h];
-        g = g < kLeastG ? kLeastG : g;
-        beta = a.beta[t * a.bt + b * a.bb + h];
-        reset = a.reset && a.reset[(long long)t * a.B + b];
-      }
-      gates.beta[row] = beta;
-      cut[s] = __ballot_sync(0xffffffffu, reset);
-      // from the last reset on; the row of the reset counts as zero (its state before does not pass)
-      const unsigned before = cut[s] & (2u << lane) - 1u;
-      const int start = before ? 31 - __clz((int)before) : 0;
-      double x = reset ? 0.0 : (double)g;
-#pragma unroll
-      for (int d = 1; d < 32; d *= 2) {
-        const double y = __shfl_up_sync(0xffffffffu, x, d);
-        if (lane - d >= start) x += y;
-      }
-      G[s] = x;
-    }
-    const double first = __shfl_sync(0xffffffffu, G[0], 31);
-    if (!(cut[1] & (2u << lane) - 1u)) G[1] += first;
-    const double last = __shfl_sync(0xffffffffu, G[1], 31);
-    const unsigned long long cuts = cut[0] | (unsigned long long)cut[1] << 32;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int row = lane + 32 * s;
-      const float high = (float)G[s], rest = (float)(G[s] - (double)high), e = expf(high);
-      gates.g_high[row] = high;
-      gates.g_low[row] = rest;
-      gates.gam[row] = cut_before(cuts, row) ? 0.0f : fmaf(e, rest, e);
-      gates.dec[row] = row < 63 && cuts >> (row + 1) ? 0.0f : expf((float)(last - G[s]));
-    }
-    if (lane == 0) gates.cuts = cuts;
-  }
-  copies_wait<0>();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane_g(), t = lane_t();
+  if (warp == 7) make_gates(a, t0, rows, b, hk * a.share, gates);
+  fill_keys<T, KD>(sh.K, static_cast<const T*>(a.k) + t0 * a.ks.t + b * a.ks.b + hk * a.ks.h, a.ks.t, rows, a.Dk, a.wide);
+  fill_keys<T, KD>(sh.Q, static_cast<const T*>(a.q) + t0 * a.qs.t + b * a.qs.b + hk * a.qs.h, a.qs.t, rows, a.Dk, a.wide);
   __syncthreads();
+  uint4* keys = reinterpret_cast<uint4*>(a.keys + (size_t)blockIdx.x * kKeysBytes<T, KD>);
+#pragma unroll 4
+  for (int i = threadIdx.x; i < (int)(kKeysBytes<T, KD> / 16); i += kThreads) keys[i] = reinterpret_cast<const uint4*>(smem)[i];
 
-  // K K^T and Q K^T where j <= i: ten blocks of 16 x 16 each
-  const unsigned long long cuts = gates.cuts;
-  float* M = a.M + chunk * C * C;
-  for (int task = warp; task < 20; task += 8) {
-    const int block = task % 10;
-    const int bi = block < 1 ? 0 : block < 3 ? 1 : block < 6 ? 2 : 3, bj = block - bi * (bi + 1) / 2;
-    const bool keys = task < 10;
-    float d[2][4] = {}, e[2][4] = {};
-    constexpr bool kOne = sizeof(T) == 2;
+  // K K^T and Q K^T where j <= i: 20 tiles of 16 x 8, the warps' in turn
+  constexpr int kMost = 3;
+  float kk[kMost][4] = {}, qk[kMost][4] = {};
+  auto tile_at = [&](int x, int& i0, int& j0) {
+    const int tile = warp + 8 * x;
+    const int bi = tile < 2 ? 0 : tile < 6 ? 1 : tile < 12 ? 2 : 3;
+    i0 = bi * 16, j0 = (tile - bi * (bi + 1)) * 8;
+    return tile < 20;
+  };
+  __syncwarp();
+#pragma unroll
+  for (int x = 0; x < kMost; ++x) {
+    int i0, j0;
+    if (!tile_at(x, i0, j0)) continue;
+    float ke[4] = {}, qe[4] = {};
 #pragma unroll
     for (int k0 = 0; k0 < KD; k0 += 16) {
-      FragA fa[2];
-      FragB fb[2][2];
-      load_a(keys ? K : Q, bi * 16, k0, fa);
-      load_b16(K, bj * 16, k0, fb);
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) mma<kOne, kOne>(d[x], kOne ? d[x] : e[x], fa[s], fb[x][s]);
-    }
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = bi * 16 + lane_g() + 8 * (r >> 1), j = bj * 16 + x * 8 + 2 * lane_t() + (r & 1);
-        const float dist = (gates.g_high[i] - gates.g_high[j]) + (gates.g_low[i] - gates.g_low[j]);
-        const bool same = i >= j && !cut_between(cuts, j, i);
-        const float v = same ? expf(dist) * (d[x][r] + e[x][r]) : 0.0f;
-        if (keys) A.to(i, j) = i > j ? gates.beta[i] * v : 0.0f;
-        else M[Tile<float, C>::at(i, j)] = v;
+      uint32_t fk[kParts<T>][4], fq[kParts<T>][4], fb[kParts<T>][2][2];
+      load_a<kParts<T>>(sh.K, i0, k0, fk);
+      load_a<kParts<T>>(sh.Q, i0, k0, fq);
+      load_b<kParts<T>>(sh.K, j0 & ~8, k0, fb);
+      if (j0 & 8) {
+        mma<2>(kk[x], ke, fk, fb, 1);
+        mma<2>(qk[x], qe, fq, fb, 1);
+      } else {
+        mma<2>(kk[x], ke, fk, fb, 0);
+        mma<2>(qk[x], qe, fq, fb, 0);
       }
-  }
-  __syncthreads();
-
-  // (I + A)^-1: the 16 x 16 blocks on the diagonal column by column, then [L 0; X R]^-1 = [L^-1 0; -R^-1 X L^-1 R^-1]
-  if (warp < 4 && lane < 16) {
-    const int o = warp * 16;
-    float x[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float s = i == lane ? 1.0f : 0.0f;
-#pragma unroll
-      for (int j = 0; j < i; ++j) s = fmaf(-A.one(o + i, o + j), x[j], s);
-      x[i] = i < lane ? 0.0f : s;  // (whatever the rows of another document hold)
-      Ti.to(o + i, o + lane) = x[i];
     }
-  }
-  __syncthreads();
 #pragma unroll
-  for (int half = 16; half < C; half *= 2) {
-    const int per = half * half, count = C / (2 * half) * per;  // outputs of all blocks of this size
-    // X L^-1 goes where A's block above the diagonal lies (never read)
-    for (int i = threadIdx.x; i < count; i += kThreads) {
-      const int o = i / per * 2 * half, r = i % per / half, c = i % half;
-      float s = 0.0f;
-      for (int j = c; j < half; ++j) s = fmaf(A.one(o + half + r, o + j), Ti.one(o + j, o + c), s);
-      A.to(o + r, o + half + c) = s;
+    for (int r = 0; r < 4; ++r) kk[x][r] += ke[r], qk[x][r] += qe[r];
+  }
+
+  for (int h = hk * a.share; h < (hk + 1) * a.share; ++h) {
+    if (h > hk * a.share) {
+      __syncthreads();
+      if (warp == 7) make_gates(a, t0, rows, b, h, gates);
+      __syncthreads();
+    }
+    const unsigned long long cuts = gates.cuts;
+    unsigned char* head = a.heads + ((size_t)((long long)n * a.B + b) * a.H + h) * kHeadBytes;
+    const SquareMat N{reinterpret_cast<bf16*>(head)}, M{N.p + 3 * N.kSize};
+#pragma unroll
+    for (int x = 0; x < kMost; ++x) {
+      int i0, j0;
+      if (!tile_at(x, i0, j0)) continue;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int i = i0 + g + 8 * r, j = j0 + 2 * t;
+        float m[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const float dist = (gates.g_high[i] - gates.g_high[j + y]) + (gates.g_low[i] - gates.g_low[j + y]);
+          const bool same = i >= j + y && !cut_between(cuts, j + y, i);
+          const float D = same ? expf(dist) : 0.0f;
+          m[y] = same ? D * qk[x][2 * r + y] : 0.0f;
+          sh.A[i * kPitch + j + y] = same && i > j + y ? D * kk[x][2 * r + y] : 0.0f;
+        }
+        if constexpr (kBackward || sizeof(T) == 4) M.put(i, j, m[0], m[1]);
+        else Mat<C, C, 2>{M.p}.put(i, j, m[0], m[1]);
+      }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < count; i += kThreads) {
-      const int o = i / per * 2 * half, r = i % per / half, c = i % half;
-      float s = 0.0f;
-      for (int j = 0; j <= r; ++j) s = fmaf(Ti.one(o + half + r, o + half + j), A.one(o + j, o + half + c), s);
-      Ti.to(o + half + r, o + c) = -s;
+
+    // N = A - A B N: 16 x 16 blocks on the diagonal column by column (rows above a column's own stay zero, whatever rows of
+    // another document hold), then for [L 0; X R]: N_X = (I - N_R B) X (I - B N_L)
+    if (warp < 4 && lane < 16) {
+      const int o = warp * 16;
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float row[16];
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+          const float4 v = *reinterpret_cast<const float4*>(sh.A + (o + i) * kPitch + o + j);
+          row[j] = v.x, row[j + 1] = v.y, row[j + 2] = v.z, row[j + 3] = v.w;
+        }
+        float s = sh.A[(o + i) * kPitch + o + lane];
+#pragma unroll
+        for (int j = 0; j < i; ++j) s = fmaf(-row[j], x[j], s);
+        s = i <= lane ? 0.0f : s;
+        sh.N[(o + i) * kPitch + o + lane] = s;
+        x[i] = i <= lane ? 0.0f : gates.beta[o + i] * s;
+      }
     }
     __syncthreads();
+#pragma unroll
+    for (int half = 16; half < C; half *= 2) {
+      const int groups = half / 4, count = C / (2 * half) * half * groups;  // four columns to a thread
+      const int o = (int)threadIdx.x / (half * groups) * 2 * half, r = (int)threadIdx.x / groups % half, c = (int)threadIdx.x % groups * 4;
+      const bool mine = (int)threadIdx.x < count;
+      float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (mine) {
+        const float* X = sh.A + (o + half + r) * kPitch + o;
+        s = *reinterpret_cast<const float4*>(X + c);
+        for (int j = c; j < half; ++j) {
+          const float w = X[j] != 0.0f ? -X[j] * gates.beta[o + j] : 0.0f;  // (beta of another document: anything)
+          const float4 v = *reinterpret_cast<const float4*>(sh.N + (o + j) * kPitch + o + c);
+          s.x = fmaf(w, v.x, s.x), s.y = fmaf(w, v.y, s.y), s.z = fmaf(w, v.z, s.z), s.w = fmaf(w, v.w, s.w);
+        }
+        *reinterpret_cast<float4*>(sh.H + (o / 2 + r) * kPitch + c) = s;
+      }
+      __syncthreads();
+      if (mine) {
+        const float* NR = sh.N + (o + half + r) * kPitch + o + half;
+        for (int j = 0; j < r; ++j) {
+          const float w = NR[j] != 0.0f ? -NR[j] * gates.beta[o + half + j] : 0.0f;
+          const float4 v = *reinterpret_cast<const float4*>(sh.H + (o / 2 + j) * kPitch + c);
+          s.x = fmaf(w, v.x, s.x), s.y = fmaf(w, v.y, s.y), s.z = fmaf(w, v.z, s.z), s.w = fmaf(w, v.w, s.w);
+        }
+        *reinterpret_cast<float4*>(sh.N + (o + half + r) * kPitch + o + c) = s;
+      }
+      __syncthreads();
+    }
+#pragma unroll 4
+    for (int x = threadIdx.x; x < C * C / 2; x += kThreads) {
+      const int i = x / (C / 2), j = x % (C / 2) * 2;
+      if (j / 16 > i / 16) continue;
+      const float2 v = *reinterpret_cast<const float2*>(sh.N + i * kPitch + j);
+      N.put(i, j, i > j && !cut_between(cuts, j, i) ? v.x : 0.0f, i > j + 1 && !cut_between(cuts, j + 1, i) ? v.y : 0.0f);
+    }
+    if (threadIdx.x < sizeof(Gates) / 16)
+      reinterpret_cast<uint4*>(M.p + 3 * M.kSize)[threadIdx.x] = reinterpret_cast<const uint4*>(&gates)[threadIdx.x];
   }
-  float* Tm = a.Tm + chunk * C * C;
-  for (int x = threadIdx.x; x < C * C; x += kThreads) {
-    const int i = x / C, j = x % C;
-    const bool same = i >= j && !cut_between(cuts, j, i);
-    Tm[Tile<float, C>::at(i, j)] = same ? Ti.one(i, j) : 0.0f;
-  }
-  for (int i = threadIdx.x; i < (int)sizeof(Gates) / 4; i += kThreads)
-    reinterpret_cast<unsigned*>(a.gates + chunk)[i] = reinterpret_cast<const unsigned*>(&gates)[i];
 }
 
-template <typename T, int KD>
-constexpr size_t prepare_smem() {
-  return 2 * C * KD * sizeof(T) + 2 * C * (C + 4) * 4 + sizeof(Gates);
-}
+// ---- along the chunks -------------------------------------------------------------
 
-// ---- along the chunks, forward ---------------------------------------------------
-
-// What a chunk brings along for a run over the chunks.
-template <typename T, int KD>
+// What a chunk brings along.
+template <typename T, int KD, int kMParts>
 struct Stage {
-  Tile<T, KD> K, Q;
-  Tile<float, C> Tm, M;
+  KeyMat<T, KD> K, Q;
+  SquareMat N;
+  Mat<C, C, kMParts> M;
   Gates* gates;
-  static constexpr size_t kBytes = 2 * C * KD * sizeof(T) + 2 * C * C * 4 + sizeof(Gates);
+  static constexpr size_t kBytes = kKeysBytes<T, KD> + SquareMat::kBytes + Mat<C, C, kMParts>::kBytes + sizeof(Gates);
   __device__ __forceinline__ explicit Stage(unsigned char* p)
-      : K{reinterpret_cast<T*>(p)}, Q{K.p + C * KD}, Tm{reinterpret_cast<float*>(Q.p + C * KD)}, M{Tm.p + C * C},
-        gates(reinterpret_cast<Gates*>(M.p + C * C)) {}
-  __device__ __forceinline__ void fetch(const DeltaArgs& a, int n, int b, int h, int len) const {
-    const int t0 = n * C, rows = min(len - t0, C);
-    const long long chunk = ((long long)n * a.B + b) * a.H + h;
-    fetch_tile(K, static_cast<const T*>(a.k) + t0 * a.ks.t + b * a.ks.b + (h / a.share) * a.ks.h, a.ks.t, 0, rows, a.Dk, a.wide);
-    fetch_tile(Q, static_cast<const T*>(a.q) + t0 * a.qs.t + b * a.qs.b + (h / a.share) * a.qs.h, a.qs.t, 0, rows, a.Dk, a.wide);
-    fetch_plain(Tm.p, a.Tm + chunk * C * C, C * C * 4);
-    fetch_plain(M.p, a.M + chunk * C * C, C * C * 4);
-    fetch_plain(gates, a.gates + chunk, (int)sizeof(Gates));
+      : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * kParts<T>}, N{Q.p + Q.kSize * kParts<T>}, M{N.p + N.kSize * 3},
+        gates(reinterpret_cast<Gates*>(M.p + M.kSize * kMParts)) {}
+  __device__ __forceinline__ void load(const DeltaArgs& a, int n, int b, int h) const {
+    const size_t at = (size_t)n * a.B + b;
+    fetch<(int)kKeysBytes<T, KD>>(K.p, a.keys + (at * (a.H / a.share) + h / a.share) * kKeysBytes<T, KD>);
+    const unsigned char* head = a.heads + (at * a.H + h) * kHeadBytes;
+    const bf16* from = reinterpret_cast<const bf16*>(head);
+    fetch_lower<3>(N.p, from);
+    fetch_lower<kMParts>(M.p, from + SquareMat::kSize * 3);
+    fetch<(int)sizeof(Gates)>(gates, head + 2 * SquareMat::kBytes);
   }
 };
+// Chunks in shared memory at a time: two, or one where the parts of wide keys fill it.
+template <typename T, int KD>
+constexpr int kStages = kParts<T> > 1 && KD == 128 ? 1 : 2;
 
 // A block's part of the state: 16 rows of S (a warp's) and kTiles times 8 columns in the MMA's result layout.
 template <int KD, int NV>
@@ -503,44 +568,141 @@ struct StatePart {
   __device__ __forceinline__ static int row0() { return (threadIdx.x >> 5) % (KD / 16) * 16; }
   __device__ __forceinline__ static int col0() { return (threadIdx.x >> 5) / (KD / 16) * (NV / kGroups); }
   template <typename F>
-  __device__ __forceinline__ void each(F f) {  // f(row, column, value)
+  __device__ __forceinline__ void each(F f) {  // f(row, column, its value, the next column's)
 #pragma unroll
     for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) f(row0() + lane_g() + 8 * (r >> 1), col0() + n * 8 + 2 * lane_t() + (r & 1), x[n][r]);
+      for (int r = 0; r < 2; ++r) f(row0() + lane_g() + 8 * r, col0() + n * 8 + 2 * lane_t(), x[n][2 * r], x[n][2 * r + 1]);
   }
-  __device__ __forceinline__ void load(const float* p, int Dk, int Dv, int v0) {
-    each([&](int r, int c, float& v) { v = p && r < Dk && v0 + c < Dv ? p[(long long)r * Dv + v0 + c] : 0.0f; });
-  }
-  __device__ __forceinline__ void store(float* p, int Dk, int Dv, int v0) {
-    each([&](int r, int c, float& v) {
-      if (r < Dk && v0 + c < Dv) p[(long long)r * Dv + v0 + c] = v;
+  __device__ __forceinline__ void load(const float* p, const DeltaArgs& a, int v0) {
+    each([&](int r, int c, float& x, float& y) {
+      const float2 v = p && r < a.Dk ? get2(p + (long long)r * a.Dv, v0 + c, a.Dv, a.even) : make_float2(0.0f, 0.0f);
+      x = v.x, y = v.y;
     });
   }
+  __device__ __forceinline__ void store(float* p, const DeltaArgs& a, int v0) {
+    each([&](int r, int c, float& x, float& y) {
+      if (r < a.Dk) put2(p + (long long)r * a.Dv, v0 + c, a.Dv, a.even, x, y);
+    });
+  }
+  __device__ __forceinline__ void split(const Mat<KD, NV, 3>& to) {
+    each([&](int r, int c, float& x, float& y) { to.put(r, c, x, y); });
+  }
+  // += keys^T rows (kP parts of keys)
+  template <int kP, int kHas>
+  __device__ __forceinline__ void add(float (&e)[kTiles][4], const Mat<C, KD, kHas>& keys, const Mat<C, NV, 3>& rows) {
+#pragma unroll
+    for (int k0 = 0; k0 < C; k0 += 16) {
+      uint32_t fa[kP][4];
+      load_at<kP>(keys, row0(), k0, fa);
+      if constexpr (kTiles == 1) {
+        uint32_t fb[3][2][2];
+        load_bt<3>(rows, col0() & ~8, k0, fb);
+        if (col0() & 8) mma<2>(x[0], e[0], fa, fb, 1);
+        else mma<2>(x[0], e[0], fa, fb, 0);
+      } else {
+#pragma unroll
+        for (int n = 0; n < kTiles; n += 2) {
+          uint32_t fb[3][2][2];
+          load_bt<3>(rows, col0() + n * 8, k0, fb);
+          mma<2>(x[n], e[n], fa, fb, 0);
+          mma<2>(x[n + 1], e[n + 1], fa, fb, 1);
+        }
+      }
+    }
+  }
+};
+
+// d + e += rows m0 of A (kLength columns from k0 on) times columns n0.. of B: kTiles times 8 columns, PA and PB parts.
+template <int kDepth, int PA, int PB, int kTiles, int kLength, bool kTransA, typename MatA, typename MatB>
+__device__ __forceinline__ void product(float (&d)[kTiles][4], float (&e)[kTiles][4], const MatA& A, int m0, const MatB& B, int n0, int k0) {
+  if constexpr (kTiles == 1) {
+#pragma unroll
+    for (int k = 0; k < kLength; k += 32) {
+      uint32_t fb[PB][2][2];
+      load_bt_tall<PB>(B, n0, k0 + k, fb);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        uint32_t fa[PA][4];
+        if constexpr (kTransA) load_at<PA>(A, m0, k0 + k + 16 * s, fa);
+        else load_a<PA>(A, m0, k0 + k + 16 * s, fa);
+        mma<kDepth>(d[0], e[0], fa, fb, s);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kLength; k += 16) {
+      uint32_t fa[PA][4];
+      if constexpr (kTransA) load_at<PA>(A, m0, k0 + k, fa);
+      else load_a<PA>(A, m0, k0 + k, fa);
+#pragma unroll
+      for (int n = 0; n < kTiles; n += 2) {
+        uint32_t fb[PB][2][2];
+        load_bt<PB>(B, n0 + n * 8, k0 + k, fb);
+        mma<kDepth>(d[n], e[n], fa, fb, 0);
+        mma<kDepth>(d[n + 1], e[n + 1], fa, fb, 1);
+      }
+    }
+  }
+}
+// The same for a square matrix of which only columns [k0, k1) are not zero (multiples of 16).
+template <int kDepth, int PA, int PB, int kTiles, bool kTransA, typename MatA, typename MatB>
+__device__ __forceinline__ void product_part(float (&d)[kTiles][4], float (&e)[kTiles][4], const MatA& A, int m0, const MatB& B, int n0,
+                                             int k0, int k1) {
+#pragma unroll
+  for (int k = 0; k < C; k += 16) {
+    if (k < k0 || k >= k1) continue;
+    uint32_t fa[PA][4];
+    if constexpr (kTransA) load_at<PA>(A, m0, k, fa);
+    else load_a<PA>(A, m0, k, fa);
+#pragma unroll
+    for (int n = 0; n < kTiles; n += 2) {
+      uint32_t fb[PB][2][2];
+      load_bt<PB>(B, kTiles == 1 ? n0 & ~8 : n0 + n * 8, k, fb);
+      if constexpr (kTiles == 1) {
+        if (n0 & 8) mma<kDepth>(d[0], e[0], fa, fb, 1);
+        else mma<kDepth>(d[0], e[0], fa, fb, 0);
+      } else {
+        mma<kDepth>(d[n], e[n], fa, fb, 0);
+        mma<kDepth>(d[n + 1], e[n + 1], fa, fb, 1);
+      }
+    }
+  }
+}
+
+template <typename T, int KD, int NV>
+struct ForwardShared {
+  static constexpr int kOut = kOutParts<T>;
+  using St = Stage<T, KD, kOut>;
+  Mat<KD, NV, 3> S;
+  Mat<C, NV, 3> X, Ud;
+  Mat<C, NV, kOut> U;
+  static constexpr size_t kBytes = kStages<T, KD> * St::kBytes + decltype(S)::kBytes + 2 * decltype(X)::kBytes + decltype(U)::kBytes;
+  __device__ __forceinline__ explicit ForwardShared(unsigned char* p)
+      : S{reinterpret_cast<bf16*>(p + kStages<T, KD> * St::kBytes)}, X{S.p + S.kSize * 3}, Ud{X.p + X.kSize * 3}, U{Ud.p + Ud.kSize * 3} {}
 };
 
 template <typename T, int KD, int NV>
 __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
-  constexpr int kTiles = NV / 16;  // column tiles of a warp's 16 rows of the chunk: half of the columns
-  constexpr bool kOne = sizeof(T) == 2;
-  using St = Stage<T, KD>;
-  // [column][row]: the state before the chunk, and the next
-  const Padded<KD + 8> S{reinterpret_cast<float*>(smem + 2 * St::kBytes)};
-  Padded<C + 8> X{S.p + 2 * NV * (KD + 8)}, U{X.p + NV * (C + 8)}, Ud{U.p + NV * (C + 8)};  // [column][timestep]
+  constexpr int kTiles = NV / 16;  // a warp's 16 rows of the chunk and half of the columns
+  constexpr int P = kParts<T>, kOut = kOutParts<T>, kDepth = kOutDepth<T>, kTwo = kStages<T, KD> - 1;
+  using Sh = ForwardShared<T, KD, NV>;
+  using St = typename Sh::St;
+  const Sh sh(smem);
   begin_op();
   const int v0 = (int)(blockIdx.x % a.tiles) * NV, bh = blockIdx.x / a.tiles, h = bh % a.H, b = bh / a.H;
   const int len = length_of(a, b), chunks = (len + C - 1) / C;
   const int warp = threadIdx.x >> 5, g = lane_g(), t = lane_t();
-  const int rb = (warp & 3) * 16, rb2 = (warp < 4 ? warp : 7 - warp) * 16;  // the second balances triangles over the SM's parts
+  const int rb = (warp < 4 ? warp : 7 - warp) * 16;  // warps w and w + 4 share a part of the SM: of triangles, a short and a long row
   const int cb = (warp >> 2) * (NV / 2);
   const long long DD = (long long)a.Dk * a.Dv;
   const T* v = static_cast<const T*>(a.v) + b * a.vs.b + h * a.vs.h;
   T* o = static_cast<T*>(a.o) + b * a.os.b + h * a.os.h;
 
   StatePart<KD, NV> s;
-  s.load(a.h0 ? a.h0 + (long long)bh * DD : nullptr, a.Dk, a.Dv, v0);
-  s.each([&](int r, int c, float& x) { S.p[c * (KD + 8) + r] = x; });
+  s.load(a.h0 ? a.h0 + (long long)bh * DD : nullptr, a, v0);
+  s.split(sh.S);
   float2 vx[kTiles][2];
   auto fetch_v = [&](int n) {
 #pragma unroll
@@ -552,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const DeltaA
       }
   };
   if (chunks > 0) {
-    St(smem).fetch(a, 0, b, h, len);
+    St(smem).load(a, 0, b, h);
     fetch_v(0);
   }
   copies_commit();
@@ -560,135 +722,108 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const DeltaA
   for (int n = 0; n < chunks; ++n) {
     copies_wait<0>();
     __syncthreads();
-    const St now(smem + (n & 1) * St::kBytes);
-    const Padded<KD + 8> S0{S.p + (n & 1) * NV * (KD + 8)};
-    Padded<KD + 8> S1{S.p + (~n & 1) * NV * (KD + 8)};
+    const St now(smem + (n & kTwo) * St::kBytes);
     const Gates& gate = *now.gates;
     float2 vn[kTiles][2];
 #pragma unroll
     for (int x = 0; x < kTiles; ++x) vn[x][0] = vx[x][0], vn[x][1] = vx[x][1];
     if (n + 1 < chunks) {
-      St(smem + (~n & 1) * St::kBytes).fetch(a, n + 1, b, h, len);
+      if constexpr (kTwo) St(smem + (~n & 1) * St::kBytes).load(a, n + 1, b, h);
       fetch_v(n + 1);
     }
     copies_commit();
-    if (a.states) s.store(a.states + (((long long)n * a.B + b) * a.H + h) * DD, a.Dk, a.Dv, v0);
+    if (a.states) s.store(a.states + (((long long)n * a.B + b) * a.H + h) * DD, a, v0);
     const unsigned long long cuts = gate.cuts;
 
     for (int lo = 0; lo < C;) {
       const int hi = piece_end(cuts, lo);
+      const bool fresh = cut_before(cuts, lo);
+      float x[kTiles][4];      // B X, then U
+      float oq[kTiles][4] = {};  // gam Q S0
       __syncwarp();
-      {  // X = beta (V - gam K S0)
+      {
         float d[kTiles][4] = {}, e[kTiles][4] = {};
-        if (!cut_before(cuts, lo)) {
-#pragma unroll
-          for (int k0 = 0; k0 < KD; k0 += 16) {
-            FragA fa[2];
-            load_a(now.K, rb, k0, fa);
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-              for (int x = 0; x < kTiles; ++x) mma<kOne, false>(d[x], e[x], fa[q], load_b(S0, cb + x * 8, k0 + 8 * q));
-          }
-        }
+        if (!fresh) product<2, P, 3, kTiles, KD, false>(d, e, now.K, rb, sh.S, cb, 0);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int i = rb + g + 8 * r;
           const float gam = gate.gam[i], beta = gate.beta[i];
           const bool in = i >= lo && i < hi;
 #pragma unroll
-          for (int x = 0; x < kTiles; ++x) {
-            const float p = vn[x][r].x - gam * (d[x][2 * r] + e[x][2 * r]), q = vn[x][r].y - gam * (d[x][2 * r + 1] + e[x][2 * r + 1]);
-            const int c = cb + x * 8 + 2 * t;
-            X.to(c, i) = in ? beta * p : 0.0f;
-            X.to(c + 1, i) = in ? beta * q : 0.0f;
+          for (int c = 0; c < kTiles; ++c) {
+            x[c][2 * r] = in ? beta * (vn[c][r].x - gam * (d[c][2 * r] + e[c][2 * r])) : 0.0f;
+            x[c][2 * r + 1] = in ? beta * (vn[c][r].y - gam * (d[c][2 * r + 1] + e[c][2 * r + 1])) : 0.0f;
+            sh.X.put(i, cb + c * 8 + 2 * t, x[c][2 * r], x[c][2 * r + 1]);
           }
         }
-      }
-      __syncthreads();
-      {  // U = Tm X
-        float d[kTiles][4] = {}, e[kTiles][4] = {};
-        for (int k0 = 0; k0 <= rb2; k0 += 16) {
-          FragA fa[2];
-          load_a(now.Tm, rb2, k0, fa);
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int x = 0; x < kTiles; ++x) mma<false, false>(d[x], e[x], fa[q], load_b(X, cb + x * 8, k0 + 8 * q));
-        }
-#pragma unroll
-        for (int x = 0; x < kTiles; ++x)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int i = rb2 + g + 8 * (r >> 1), c = cb + x * 8 + 2 * t + (r & 1);
-            const float u = i >= lo && i < hi ? d[x][r] + e[x][r] : 0.0f;
-            U.to(c, i) = u;
-            Ud.to(c, i) = gate.dec[i] * u;
-          }
-      }
-      if (hi == C && lo > 0)  // the last piece's keys alone reach the next chunk
-        for (int i = threadIdx.x; i < lo * KD; i += kThreads) now.K.p[i] = from_f32<T>(0.0f);
-      __syncthreads();
-      if (hi == C) {  // S = gam_63 S0 + K^T dec U
-        float e[StatePart<KD, NV>::kTiles][4] = {};
-        const float keep = gate.gam[C - 1];
-        s.each([&](int, int, float& x) { x = cuts ? 0.0f : keep * x; });
-#pragma unroll
-        for (int k0 = 0; k0 < C; k0 += 16) {
-          FragA fa[2];
-          load_at(now.K, s.row0(), k0, fa);
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int x = 0; x < s.kTiles; ++x) mma<kOne, false>(s.x[x], e[x], fa[q], load_b(Ud, s.col0() + x * 8, k0 + 8 * q));
-        }
-#pragma unroll
-        for (int x = 0; x < s.kTiles; ++x)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) s.x[x][r] += e[x][r];
-        s.each([&](int r, int c, float& x) { S1.to(c, r) = x; });
       }
       __syncwarp();
-      {  // O = scale (gam Q S0 + M U)
+      if (!fresh) {
         float d[kTiles][4] = {}, e[kTiles][4] = {};
-        if (!cut_before(cuts, lo)) {
+        product<kDepth, P, kOut, kTiles, KD, false>(d, e, now.Q, rb, sh.S, cb, 0);
 #pragma unroll
-          for (int k0 = 0; k0 < KD; k0 += 16) {
-            FragA fa[2];
-            load_a(now.Q, rb2, k0, fa);
+        for (int c = 0; c < kTiles; ++c)
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-              for (int x = 0; x < kTiles; ++x) mma<kOne, false>(d[x], e[x], fa[q], load_b(S0, cb + x * 8, k0 + 8 * q));
-          }
-#pragma unroll
-          for (int x = 0; x < kTiles; ++x)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) d[x][r] = gate.gam[rb2 + g + 8 * (r >> 1)] * (d[x][r] + e[x][r]), e[x][r] = 0.0f;
-        }
-        for (int k0 = 0; k0 <= rb2; k0 += 16) {
-          FragA fa[2];
-          load_a(now.M, rb2, k0, fa);
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int x = 0; x < kTiles; ++x) mma<false, false>(d[x], e[x], fa[q], load_b(U, cb + x * 8, k0 + 8 * q));
-        }
+          for (int r = 0; r < 4; ++r) oq[c][r] = gate.gam[rb + g + 8 * (r >> 1)] * (d[c][r] + e[c][r]);
+      }
+      __syncthreads();
+      {
+        float d[kTiles][4] = {}, e[kTiles][4] = {};
+        product_part<2, 3, 3, kTiles, false>(d, e, now.N, rb, sh.X, cb, 0, rb + 16);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const int i = rb2 + g + 8 * r, time = n * C + i;
+          const int i = rb + g + 8 * r;
+          const bool in = i >= lo && i < hi;
+          const float beta = gate.beta[i], dec = gate.dec[i];
+#pragma unroll
+          for (int c = 0; c < kTiles; ++c) {
+            const float p = in ? x[c][2 * r] - beta * (d[c][2 * r] + e[c][2 * r]) : 0.0f;
+            const float q = in ? x[c][2 * r + 1] - beta * (d[c][2 * r + 1] + e[c][2 * r + 1]) : 0.0f;
+            sh.U.put(i, cb + c * 8 + 2 * t, p, q);
+            sh.Ud.put(i, cb + c * 8 + 2 * t, in ? dec * p : 0.0f, in ? dec * q : 0.0f);
+          }
+        }
+      }
+      if (hi == C && lo > 0)  // the last piece's keys alone reach the next chunk
+        for (int i = threadIdx.x; i < lo * KD; i += kThreads)
+#pragma unroll
+          for (int q = 0; q < P; ++q) now.K.p[q * now.K.kSize + i] = from_f32<bf16>(0.0f);
+      __syncthreads();
+      if (hi == C) {
+        float e[s.kTiles][4] = {};
+        const float keep = gate.gam[C - 1];
+        s.each([&](int, int, float& p, float& q) { p = cuts ? 0.0f : keep * p, q = cuts ? 0.0f : keep * q; });
+        s.template add<P>(e, now.K, sh.Ud);
+#pragma unroll
+        for (int c = 0; c < s.kTiles; ++c)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s.x[c][r] += e[c][r];
+        s.split(sh.S);
+      }
+      __syncwarp();
+      {
+        float e[kTiles][4] = {};
+        product_part<kDepth, kOut, kOut, kTiles, false>(oq, e, now.M, rb, sh.U, cb, 0, rb + 16);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int i = rb + g + 8 * r, time = n * C + i;
           if (i < lo || i >= hi || time >= len) continue;
 #pragma unroll
-          for (int x = 0; x < kTiles; ++x)
-            put2(o + time * a.os.t, v0 + cb + x * 8 + 2 * t, a.Dv, a.pairs, a.scale * (d[x][2 * r] + e[x][2 * r]),
-                 a.scale * (d[x][2 * r + 1] + e[x][2 * r + 1]));
+          for (int c = 0; c < kTiles; ++c)
+            put2(o + time * a.os.t, v0 + cb + c * 8 + 2 * t, a.Dv, a.pairs, a.scale * (oq[c][2 * r] + e[c][2 * r]),
+                 a.scale * (oq[c][2 * r + 1] + e[c][2 * r + 1]));
         }
       }
       lo = hi;
       if (lo < C) __syncthreads();
     }
+    if constexpr (!kTwo) {
+      __syncthreads();
+      if (n + 1 < chunks) St(smem).load(a, n + 1, b, h);
+      copies_commit();
+    }
   }
-  s.store(a.h_last + (long long)bh * DD, a.Dk, a.Dv, v0);
+  s.store(a.h_last + (long long)bh * DD, a, v0);
   for (long long i = (long long)len * NV + threadIdx.x; i < (long long)a.T * NV; i += kThreads) {
     const int c = v0 + (int)(i % NV);
     if (c < a.Dv) o[i / NV * a.os.t + c] = from_f32<T>(0.0f);
@@ -696,34 +831,38 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const DeltaA
 }
 
 template <typename T, int KD, int NV>
-constexpr size_t forward_smem() {
-  return 2 * Stage<T, KD>::kBytes + (2 * NV * (KD + 8) + 3 * NV * (C + 8)) * 4;
-}
+struct BackwardShared {
+  using St = Stage<T, KD, 3>;
+  Mat<KD, NV, 3> S;                // dS
+  Mat<C, NV, 3> Od, Z;             // scale gam dO; B dU, then - gam B R
+  Mat<C, NV, kParts<T>> O;         // dO
+  float* sums;                     // [8]
+  static constexpr size_t kBytes = kStages<T, KD> * St::kBytes + decltype(S)::kBytes + 2 * decltype(Z)::kBytes + decltype(O)::kBytes + 32;
+  __device__ __forceinline__ explicit BackwardShared(unsigned char* p)
+      : S{reinterpret_cast<bf16*>(p + kStages<T, KD> * St::kBytes)}, Od{S.p + S.kSize * 3}, Z{Od.p + Od.kSize * 3}, O{Z.p + Z.kSize * 3},
+        sums(reinterpret_cast<float*>(O.p + O.kSize * kParts<T>)) {}
+};
 
-// ---- along the chunks, backward ------------------------------------------------
-
-// dS before a chunk from dS behind it; keeps the latter and R for the gradients of the rest, and writes dV.
+// dS before a chunk from dS behind it; keeps the latter, R and <dS0, S0> for the gradients of the rest, and writes dV.
 template <typename T, int KD, int NV>
 __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
-  constexpr int kTiles = NV / 16;
-  constexpr bool kOne = sizeof(T) == 2;
-  using St = Stage<T, KD>;
-  const Padded<KD + 8> S{reinterpret_cast<float*>(smem + 2 * St::kBytes)};                      // dS, [column][row]
-  Padded<C + 8> X{S.p + 2 * NV * (KD + 8)}, Y{X.p + NV * (C + 8)}, Z{Y.p + NV * (C + 8)};  // [column][timestep]
+  constexpr int kTiles = NV / 16, P = kParts<T>, kTwo = kStages<T, KD> - 1;
+  using Sh = BackwardShared<T, KD, NV>;
+  using St = typename Sh::St;
+  const Sh sh(smem);
   begin_op();
   const int v0 = (int)(blockIdx.x % a.tiles) * NV, bh = blockIdx.x / a.tiles, h = bh % a.H, b = bh / a.H;
   const int len = length_of(a, b), chunks = (len + C - 1) / C;
   const int warp = threadIdx.x >> 5, g = lane_g(), t = lane_t();
-  const int rb = (warp & 3) * 16, rb2 = (warp < 4 ? warp : 7 - warp) * 16;
-  const int cb = (warp >> 2) * (NV / 2);
+  const int rb = (warp < 4 ? warp : 7 - warp) * 16, cb = (warp >> 2) * (NV / 2);
   const long long DD = (long long)a.Dk * a.Dv;
   const T* d_o = static_cast<const T*>(a.d_o) + b * a.dos.b + h * a.dos.h;
   T* dv = static_cast<T*>(a.dv) + b * a.dvs.b + h * a.dvs.h;
 
-  StatePart<KD, NV> s;
-  s.load(a.dh_last ? a.dh_last + (long long)bh * DD : nullptr, a.Dk, a.Dv, v0);
-  s.each([&](int r, int c, float& x) { S.p[c * (KD + 8) + r] = x; });
+  StatePart<KD, NV> s, before;
+  s.load(a.dh_last ? a.dh_last + (long long)bh * DD : nullptr, a, v0);
+  s.split(sh.S);
   float2 ox[kTiles][2];
   auto fetch_o = [&](int n) {
 #pragma unroll
@@ -735,29 +874,27 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const Delta
       }
   };
   if (chunks > 0) {
-    St(smem + ((chunks - 1) & 1) * St::kBytes).fetch(a, chunks - 1, b, h, len);
+    St(smem + ((chunks - 1) & kTwo) * St::kBytes).load(a, chunks - 1, b, h);
     fetch_o(chunks - 1);
   }
   copies_commit();
 
   for (int n = chunks - 1; n >= 0; --n) {
-    const int turn = (chunks - 1 - n) & 1;
     copies_wait<0>();
     __syncthreads();
-    const St now(smem + (n & 1) * St::kBytes);
-    const Padded<KD + 8> S1{S.p + turn * NV * (KD + 8)};
-    Padded<KD + 8> S0{S.p + (turn ^ 1) * NV * (KD + 8)};
+    const St now(smem + (n & kTwo) * St::kBytes);
     const Gates& gate = *now.gates;
     const long long chunk = ((long long)n * a.B + b) * a.H + h;
     float2 on[kTiles][2];
 #pragma unroll
     for (int x = 0; x < kTiles; ++x) on[x][0] = ox[x][0], on[x][1] = ox[x][1];
     if (n > 0) {
-      St(smem + (~n & 1) * St::kBytes).fetch(a, n - 1, b, h, len);
+      if constexpr (kTwo) St(smem + (~n & 1) * St::kBytes).load(a, n - 1, b, h);
       fetch_o(n - 1);
     }
     copies_commit();
-    s.store(a.dS + chunk * DD, a.Dk, a.Dv, v0);
+    s.store(a.dS + chunk * DD, a, v0);
+    before.load(a.states + chunk * DD, a, v0);
     const unsigned long long cuts = gate.cuts;
     float* R = a.R + chunk * C * a.Dv;
 
@@ -768,116 +905,106 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const Delta
       for (int r = 0; r < 2; ++r) {
         const int i = rb + g + 8 * r;
         const bool in = i >= lo && i < hi;
-        const float gam = a.scale * gate.gam[i];
+        const float gam = in ? a.scale * gate.gam[i] : 0.0f;
 #pragma unroll
-        for (int x = 0; x < kTiles; ++x) {
-          const int c = cb + x * 8 + 2 * t;
-          const float p = in ? on[x][r].x : 0.0f, q = in ? on[x][r].y : 0.0f;
-          X.to(c, i) = p, X.to(c + 1, i) = q;
-          Y.to(c, i) = gam * p, Y.to(c + 1, i) = gam * q;
+        for (int c = 0; c < kTiles; ++c) {
+          const float p = in ? on[c][r].x : 0.0f, q = in ? on[c][r].y : 0.0f;
+          sh.O.put(i, cb + c * 8 + 2 * t, p, q);
+          sh.Od.put(i, cb + c * 8 + 2 * t, gam * p, gam * q);
         }
       }
       __syncthreads();
+      float du[kTiles][4];
       {  // dU = scale M^T dO + dec K dS
         float d[kTiles][4] = {}, e[kTiles][4] = {};
-        if (hi == C) {
+        if (hi == C) product<2, P, 3, kTiles, KD, false>(d, e, now.K, rb, sh.S, cb, 0);
 #pragma unroll
-          for (int k0 = 0; k0 < KD; k0 += 16) {
-            FragA fa[2];
-            load_a(now.K, rb2, k0, fa);
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-              for (int x = 0; x < kTiles; ++x) mma<kOne, false>(d[x], e[x], fa[q], load_b(S1, cb + x * 8, k0 + 8 * q));
-          }
-        }
-        float du[kTiles][4];
-#pragma unroll
-        for (int x = 0; x < kTiles; ++x)
+        for (int c = 0; c < kTiles; ++c)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            du[x][r] = hi == C ? gate.dec[rb2 + g + 8 * (r >> 1)] * (d[x][r] + e[x][r]) : 0.0f;
-            d[x][r] = e[x][r] = 0.0f;
+            du[c][r] = hi == C ? gate.dec[rb + g + 8 * (r >> 1)] * (d[c][r] + e[c][r]) : 0.0f;
+            d[c][r] = e[c][r] = 0.0f;
           }
-        for (int k0 = rb2; k0 < C; k0 += 16) {
-          FragA fa[2];
-          load_at(now.M, rb2, k0, fa);
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int x = 0; x < kTiles; ++x) mma<false, kOne>(d[x], e[x], fa[q], load_b(X, cb + x * 8, k0 + 8 * q));
-        }
-#pragma unroll
-        for (int x = 0; x < kTiles; ++x)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int i = rb2 + g + 8 * (r >> 1);
-            Z.to(cb + x * 8 + 2 * t + (r & 1), i) = i >= lo && i < hi ? fmaf(a.scale, d[x][r] + e[x][r], du[x][r]) : 0.0f;
-          }
-      }
-      __syncthreads();
-      {  // R = Tm^T dU, dV = beta R; - beta gam R goes where dO was
-        float d[kTiles][4] = {}, e[kTiles][4] = {};
-        for (int k0 = rb2; k0 < C; k0 += 16) {
-          FragA fa[2];
-          load_at(now.Tm, rb2, k0, fa);
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int x = 0; x < kTiles; ++x) mma<false, false>(d[x], e[x], fa[q], load_b(Z, cb + x * 8, k0 + 8 * q));
-        }
+        product_part<2, 3, P, kTiles, true>(d, e, now.M, rb, sh.O, cb, rb, C);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const int i = rb2 + g + 8 * r, time = n * C + i;
+          const int i = rb + g + 8 * r;
           const bool in = i >= lo && i < hi;
-          const float beta = gate.beta[i], back = in ? -beta * gate.gam[i] : 0.0f;
+          const float beta = gate.beta[i];
 #pragma unroll
-          for (int x = 0; x < kTiles; ++x) {
-            const int c = cb + x * 8 + 2 * t;
-            const float p = in ? d[x][2 * r] + e[x][2 * r] : 0.0f, q = in ? d[x][2 * r + 1] + e[x][2 * r + 1] : 0.0f;
-            X.to(c, i) = back * p, X.to(c + 1, i) = back * q;
+          for (int c = 0; c < kTiles; ++c) {
+#pragma unroll
+            for (int y = 2 * r; y < 2 * r + 2; ++y) du[c][y] = in ? fmaf(a.scale, d[c][y] + e[c][y], du[c][y]) : 0.0f;
+            sh.Z.put(i, cb + c * 8 + 2 * t, in ? beta * du[c][2 * r] : 0.0f, in ? beta * du[c][2 * r + 1] : 0.0f);
+          }
+        }
+      }
+      __syncthreads();
+      {  // R = dU - N^T B dU, dV = B R
+        float d[kTiles][4] = {}, e[kTiles][4] = {};
+        product_part<2, 3, 3, kTiles, true>(d, e, now.N, rb, sh.Z, cb, rb, C);
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int i = rb + g + 8 * r, time = n * C + i;
+          const bool in = i >= lo && i < hi;
+          const float beta = gate.beta[i], back = -gate.gam[i];
+#pragma unroll
+          for (int c = 0; c < kTiles; ++c) {
+            const int col = cb + c * 8 + 2 * t;
+            const float p = in ? du[c][2 * r] - (d[c][2 * r] + e[c][2 * r]) : 0.0f;
+            const float q = in ? du[c][2 * r + 1] - (d[c][2 * r + 1] + e[c][2 * r + 1]) : 0.0f;
+            const float bp = in ? beta * p : 0.0f, bq = in ? beta * q : 0.0f;
+            sh.Z.put(i, col, in ? back * bp : 0.0f, in ? back * bq : 0.0f);
             if (!in) continue;
-            if (v0 + c < a.Dv) R[(long long)i * a.Dv + v0 + c] = p;
-            if (v0 + c + 1 < a.Dv) R[(long long)i * a.Dv + v0 + c + 1] = q;
-            if (time < len) put2(dv + time * a.dvs.t, v0 + c, a.Dv, a.pairs, beta * p, beta * q);
+            put2(R + (long long)i * a.Dv, v0 + col, a.Dv, a.even, p, q);
+            if (time < len) put2(dv + time * a.dvs.t, v0 + col, a.Dv, a.pairs, bp, bq);
           }
         }
       }
       if (lo == 0 && cuts)  // rows behind the first reset do not reach the state before
-        for (int i = threadIdx.x + hi * KD; i < C * KD; i += kThreads) now.K.p[i] = now.Q.p[i] = from_f32<T>(0.0f);
+        for (int i = threadIdx.x + hi * KD; i < C * KD; i += kThreads)
+#pragma unroll
+          for (int q = 0; q < P; ++q) now.K.p[q * now.K.kSize + i] = now.Q.p[q * now.Q.kSize + i] = from_f32<bf16>(0.0f);
       __syncthreads();
-      if (lo == 0) {  // dS = gam_63 dS + Q^T scale gam dO - K^T beta gam R
-        float e[StatePart<KD, NV>::kTiles][4] = {};
-        const bool fresh = cuts & 1ull;
+      if (lo == 0) {  // dS = gam_63 dS + Q^T scale gam dO - K^T gam dV
+        float e[s.kTiles][4] = {};
         const float keep = gate.gam[C - 1];
-        s.each([&](int, int, float& x) { x = cuts ? 0.0f : keep * x; });
-        if (!fresh) {
-#pragma unroll
-          for (int k0 = 0; k0 < C; k0 += 16) {
-            FragA fa[2];
-            load_at(now.Q, s.row0(), k0, fa);
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-              for (int x = 0; x < s.kTiles; ++x) mma<kOne, false>(s.x[x], e[x], fa[q], load_b(Y, s.col0() + x * 8, k0 + 8 * q));
-            load_at(now.K, s.row0(), k0, fa);
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-              for (int x = 0; x < s.kTiles; ++x) mma<kOne, false>(s.x[x], e[x], fa[q], load_b(X, s.col0() + x * 8, k0 + 8 * q));
-          }
+        s.each([&](int, int, float& p, float& q) { p = cuts ? 0.0f : keep * p, q = cuts ? 0.0f : keep * q; });
+        if (!(cuts & 1ull)) {
+          s.template add<P>(e, now.Q, sh.Od);
+          s.template add<P>(e, now.K, sh.Z);
         }
 #pragma unroll
-        for (int x = 0; x < s.kTiles; ++x)
+        for (int c = 0; c < s.kTiles; ++c)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) s.x[x][r] += e[x][r];
-        s.each([&](int r, int c, float& x) { S0.to(c, r) = x; });
+          for (int r = 0; r < 4; ++r) s.x[c][r] += e[c][r];
+        s.split(sh.S);
+        float dot = 0.0f;
+#pragma unroll
+        for (int c = 0; c < s.kTiles; ++c)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) dot = cuts & 1ull ? 0.0f : fmaf(s.x[c][r], before.x[c][r], dot);
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, d);
+        if ((threadIdx.x & 31) == 0) sh.sums[warp] = dot;
       }
       hi = lo;
       if (hi > 0) __syncthreads();
     }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      float dot = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) dot += sh.sums[w];
+      a.dots[chunk * a.tiles + blockIdx.x % a.tiles] = dot;
+    }
+    if constexpr (!kTwo) {
+      if (n > 0) St(smem).load(a, n - 1, b, h);
+      copies_commit();
+    }
   }
-  s.store(a.dh0 + (long long)bh * DD, a.Dk, a.Dv, v0);
+  s.store(a.dh0 + (long long)bh * DD, a, v0);
   for (long long i = (long long)len * NV + threadIdx.x; i < (long long)a.T * NV; i += kThreads) {
     const int c = v0 + (int)(i % NV);
     if (c < a.Dv) dv[i / NV * a.dvs.t + c] = from_f32<T>(0.0f);
@@ -886,39 +1013,71 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const Delta
 
 // ---- per chunk and key head: the gradients of q, k, g and beta ---------------------
 
-// Rows of a tile whose pitch is 40 words: 32 columns of S, dS, dO, R and U.
-constexpr int kSlice = 32, kPitch = kSlice + 8;
+// Columns of S to a round: fewer where the parts of 32-bit keys fill the shared memory.
+template <typename T, int KD>
+constexpr int kSlice = sizeof(T) == 4 && KD == 128 ? 16 : 32;
 
 template <typename T, int KD>
 struct GradShared {
-  Tile<T, KD> K, Q;
-  Tile<float, C> Tm;
-  Padded<kPitch> S, dS, dO, R, U;
-  Padded<C + 8> X, P, E;  // X: [column][timestep]; P, E: [i][j]
+  static constexpr int W = kSlice<T, KD>, P = kParts<T>, kOut = kOutParts<T>;
+  KeyMat<T, KD> K, Q;
+  SquareMat N;
   Gates* gates;
-  float* sums;  // [5][2][C], [8]
-  static constexpr size_t kBytes = 2 * C * KD * sizeof(T) + C * C * 4 + (2 * KD + 3 * C) * kPitch * 4 + (kSlice + 2 * C) * (C + 8) * 4 +
-                                   sizeof(Gates) + (10 * C + 8) * 4;
+  float* sums;  // [3][2][C]
+  // one round's: S0, dS, dO, R, B X, U; after the last, P and E
+  Mat<KD, W, 3> S;
+  Mat<KD, W, kOut> dS;
+  Mat<C, W, P> dO;
+  Mat<C, W, kOut> R;
+  Mat<C, W, 3> X, U;
+  SquareMat Pm;
+  Mat<C, C, kOut> E;
+  static constexpr size_t kFixed = kKeysBytes<T, KD> + SquareMat::kBytes + sizeof(Gates) + 6 * C * 4;
+  static constexpr size_t kRound = decltype(S)::kBytes + decltype(dS)::kBytes + decltype(dO)::kBytes + decltype(R)::kBytes + 2 * decltype(X)::kBytes;
+  static constexpr size_t kAfter = decltype(Pm)::kBytes + decltype(E)::kBytes;
+  static constexpr size_t kBytes = kFixed + (kRound > kAfter ? kRound : kAfter);
   __device__ __forceinline__ explicit GradShared(unsigned char* p)
-      : K{reinterpret_cast<T*>(p)}, Q{K.p + C * KD}, Tm{reinterpret_cast<float*>(Q.p + C * KD)}, S{Tm.p + C * C},
-        dS{S.p + KD * kPitch}, dO{dS.p + KD * kPitch}, R{dO.p + C * kPitch}, U{R.p + C * kPitch}, X{U.p + C * kPitch},
-        P{X.p + kSlice * (C + 8)}, E{P.p + C * (C + 8)}, gates(reinterpret_cast<Gates*>(E.p + C * (C + 8))),
-        sums(reinterpret_cast<float*>(gates + 1)) {}
+      : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * P}, N{Q.p + Q.kSize * P}, gates(reinterpret_cast<Gates*>(N.p + N.kSize * 3)),
+        sums(reinterpret_cast<float*>(gates + 1)), S{reinterpret_cast<bf16*>(sums + 6 * C)}, dS{S.p + S.kSize * 3},
+        dO{dS.p + dS.kSize * kOut}, R{dO.p + dO.kSize * P}, X{R.p + R.kSize * kOut}, U{X.p + X.kSize * 3}, Pm{S.p}, E{Pm.p + Pm.kSize * 3} {}
 };
+
+// acc += rows m0 of A (parts PA) times the transposed rows n0.. of B, over kLength columns; two tiles of 8 rows of B at a time,
+// summed apart first (an MMA's sum is cut, not rounded, to 24 bits).
+template <int kDepth, int PB, int kTiles, int kLength, int PA, typename MatB>
+__device__ __forceinline__ void add_rows(float (&acc)[kTiles][4], const uint32_t (&fa)[kLength / 16][PA][4], const MatB& B, int n0, int first) {
+#pragma unroll
+  for (int n = 0; n < kTiles; n += 2) {
+    if (n0 + n * 8 >= first) continue;
+    float d[2][4] = {}, e[2][4] = {};
+#pragma unroll
+    for (int k = 0; k < kLength / 16; ++k) {
+      uint32_t fb[PB][2][2];
+      load_b<PB>(B, n0 + n * 8, k * 16, fb);
+      mma<kDepth>(d[0], e[0], fa[k], fb, 0);
+      mma<kDepth>(d[1], e[1], fa[k], fb, 1);
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[n + x][r] += d[x][r] + e[x][r];
+  }
+}
 
 template <typename T, int KD>
 __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
-  constexpr bool kOne = sizeof(T) == 2;
+  constexpr int W = kSlice<T, KD>, P = kParts<T>, kOut = kOutParts<T>, kDepth = kOutDepth<T>;
   constexpr int kHalf = KD / 2, kTiles = kHalf / 8;  // a warp has 16 rows and half of the columns
-  GradShared<T, KD> sh(smem);
-  Gates& gate = *sh.gates;
+  constexpr int kXTiles = W / 16;
+  const GradShared<T, KD> sh(smem);
+  const Gates& gate = *sh.gates;
   begin_op();
   const int Hk = a.H / a.share;
   const int hk = (int)(blockIdx.x % Hk), b = (int)(blockIdx.x / Hk % a.B), n = (int)(blockIdx.x / Hk / a.B);
   const int len = length_of(a, b), t0 = n * C, rows = min(len - t0, C), all = min(a.T - t0, C);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane_g(), t = lane_t();
-  const int rb = (warp & 3) * 16, side = warp >> 2, rb2 = (warp < 4 ? warp : 7 - warp) * 16;
+  const int rb = (warp < 4 ? warp : 7 - warp) * 16, side = warp >> 2;
   T* dq = static_cast<T*>(a.dq) + t0 * a.dqs.t + b * a.dqs.b + hk * a.dqs.h;
   T* dk = static_cast<T*>(a.dk) + t0 * a.dks.t + b * a.dks.b + hk * a.dks.h;
   for (int i = threadIdx.x + max(rows, 0) * a.Dk; i < all * a.Dk; i += kThreads) {  // past the stream's length
@@ -926,22 +1085,24 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
     dk[i / a.Dk * a.dks.t + i % a.Dk] = from_f32<T>(0.0f);
   }
   for (int i = threadIdx.x + max(rows, 0) * a.share; i < all * a.share; i += kThreads) {
-    const int row = t0 + i / a.share, h = hk * a.share + i % a.share;
+    const long long row = t0 + i / a.share;
+    const int h = hk * a.share + i % a.share;
     a.dg[row * a.dgt + b * a.dgb + h] = 0.0f;
     a.dbeta[row * a.dbt + b * a.dbb + h] = 0.0f;
   }
   if (rows <= 0) return;
-  const T* k = static_cast<const T*>(a.k) + t0 * a.ks.t + b * a.ks.b + hk * a.ks.h;
-  const T* q = static_cast<const T*>(a.q) + t0 * a.qs.t + b * a.qs.b + hk * a.qs.h;
   const long long DD = (long long)a.Dk * a.Dv;
+  const size_t where = ((size_t)n * a.B + b) * Hk + hk;
 
   for (int h = hk * a.share; h < (hk + 1) * a.share; ++h) {
     const long long chunk = ((long long)n * a.B + b) * a.H + h;
     const T* v = static_cast<const T*>(a.v) + t0 * a.vs.t + b * a.vs.b + h * a.vs.h;
     const T* d_o = static_cast<const T*>(a.d_o) + t0 * a.dos.t + b * a.dos.b + h * a.dos.h;
+    const float *S = a.states + chunk * DD, *dS = a.dS + chunk * DD, *R = a.R + chunk * C * a.Dv;
+    const unsigned char* head = a.heads + (size_t)chunk * kHeadBytes;
     __syncthreads();
-    fetch_plain(sh.Tm.p, a.Tm + chunk * C * C, C * C * 4);
-    fetch_plain(sh.gates, a.gates + chunk, (int)sizeof(Gates));
+    fetch_lower<3>(sh.N.p, reinterpret_cast<const bf16*>(head));
+    fetch<(int)sizeof(Gates)>(sh.gates, head + 2 * SquareMat::kBytes);
     copies_commit();
     copies_wait<0>();
     __syncthreads();
@@ -951,204 +1112,204 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
       const int hi = min(piece_end(cuts, lo), rows);
       const bool fresh = cut_before(cuts, lo), last = hi == rows;  // the state before counts as zero; the one behind goes on
       __syncthreads();
-      fetch_tile(sh.K, k, a.ks.t, lo, hi, a.Dk, a.wide);
-      fetch_tile(sh.Q, q, a.qs.t, lo, hi, a.Dk, a.wide);
-      copies_commit();
+      if (h == hk * a.share || cuts) {
+        fetch<(int)kKeysBytes<T, KD>>(sh.K.p, a.keys + where * kKeysBytes<T, KD>);
+        copies_commit();
+        copies_wait<0>();
+        if (cuts) {
+          __syncthreads();
+          for (int i = threadIdx.x; i < C * KD; i += kThreads)
+            if (i / KD < lo || i / KD >= hi)
+#pragma unroll
+              for (int q = 0; q < P; ++q) sh.K.p[q * sh.K.kSize + i] = sh.Q.p[q * sh.Q.kSize + i] = from_f32<bf16>(0.0f);
+        }
+      }
       float acc_q[kTiles][4] = {}, acc_w[kTiles][4] = {}, acc_t[kTiles][4] = {};  // dO S0^T, R S0^T, U dS^T
       float acc_p[4][4] = {}, acc_e[4][4] = {};                                  // dO U^T, R U^T
-      float rv[2] = {}, dots = 0.0f;                                             // R . V, <dS, S0>
+      float rv[2] = {}, ry[2] = {};                                              // R . V, R . Y
 
-      for (int v0 = 0; v0 < a.Dv; v0 += kSlice) {
+      for (int v0 = 0; v0 < a.Dv; v0 += W) {
         __syncthreads();
-        const float* S = a.states + chunk * DD;
-        const float* dS = a.dS + chunk * DD;
-        for (int i = threadIdx.x; i < KD * kSlice; i += kThreads) {
-          const int r = i / kSlice, c = i % kSlice;
-          const bool in = r < a.Dk && v0 + c < a.Dv;
-          const float x = in && !fresh ? S[(long long)r * a.Dv + v0 + c] : 0.0f, y = in && last ? dS[(long long)r * a.Dv + v0 + c] : 0.0f;
-          sh.S.to(r, c) = x;
-          sh.dS.to(r, c) = y;
-          dots = fmaf(x, y, dots);
+        for (int i = threadIdx.x; i < KD * W / 2; i += kThreads) {
+          const int r = i / (W / 2), c = i % (W / 2) * 2;
+          const float2 zero = make_float2(0.0f, 0.0f);
+          const float2 x = r < a.Dk && !fresh ? get2(S + (long long)r * a.Dv, v0 + c, a.Dv, a.even) : zero;
+          const float2 y = r < a.Dk && last ? get2(dS + (long long)r * a.Dv, v0 + c, a.Dv, a.even) : zero;
+          sh.S.put(r, c, x.x, x.y);
+          sh.dS.put(r, c, y.x, y.y);
         }
-        for (int i = threadIdx.x; i < C * kSlice; i += kThreads) {
-          const int r = i / kSlice, c = i % kSlice;
-          const bool in = r >= lo && r < hi && v0 + c < a.Dv;
-          sh.dO.to(r, c) = in ? to_f32(d_o[r * a.dos.t + v0 + c]) : 0.0f;
-          sh.R.to(r, c) = in ? a.R[(chunk * C + r) * a.Dv + v0 + c] : 0.0f;
-        }
-        copies_wait<0>();
-        __syncthreads();
-        {  // X = beta (V - gam K S0), and R . V
-          float d[2][4] = {}, e[2][4] = {};
-          if (!fresh) {
+        float2 vx[kXTiles][2], rx[kXTiles][2];
 #pragma unroll
-            for (int k0 = 0; k0 < KD; k0 += 16) {
-              FragA fa[2];
-              load_a(sh.K, rb, k0, fa);
+        for (int r = 0; r < 2; ++r) {
+          const int i = rb + g + 8 * r;
+          const bool in = i >= lo && i < hi;
 #pragma unroll
-              for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int x = 0; x < 2; ++x) mma<kOne, false>(d[x], e[x], fa[s], load_bt(sh.S, side * 16 + x * 8, k0 + 8 * s));
-            }
+          for (int c = 0; c < kXTiles; ++c) {
+            const int col = side * (W / 2) + c * 8 + 2 * t;
+            const float2 zero = make_float2(0.0f, 0.0f);
+            vx[c][r] = in ? get2(v + i * a.vs.t, v0 + col, a.Dv, a.pairs) : zero;
+            rx[c][r] = in ? get2(R + (long long)i * a.Dv, v0 + col, a.Dv, a.even) : zero;
+            const float2 ox = in ? get2(d_o + i * a.dos.t, v0 + col, a.Dv, a.pairs) : zero;
+            sh.R.put(i, col, rx[c][r].x, rx[c][r].y);
+            sh.dO.put(i, col, ox.x, ox.y);
           }
+        }
+        __syncthreads();
+        float x[kXTiles][4];  // X
+        {
+          float d[kXTiles][4] = {}, e[kXTiles][4] = {};
+          if (!fresh) product<2, P, 3, kXTiles, KD, false>(d, e, sh.K, rb, sh.S, side * (W / 2), 0);
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
             const int i = rb + g + 8 * r;
             const bool in = i >= lo && i < hi;
             const float gam = gate.gam[i], beta = gate.beta[i];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const int c = side * 16 + x * 8 + 2 * t;
-              const float2 w = in ? get2(v + i * a.vs.t, v0 + c, a.Dv, a.pairs) : make_float2(0.0f, 0.0f);
-              const float2 y = sh.R.pair(i, c);
-              rv[r] = fmaf(y.x, w.x, fmaf(y.y, w.y, rv[r]));
-              sh.X.to(c, i) = in ? beta * (w.x - gam * (d[x][2 * r] + e[x][2 * r])) : 0.0f;
-              sh.X.to(c + 1, i) = in ? beta * (w.y - gam * (d[x][2 * r + 1] + e[x][2 * r + 1])) : 0.0f;
+            for (int c = 0; c < kXTiles; ++c) {
+              x[c][2 * r] = in ? vx[c][r].x - gam * (d[c][2 * r] + e[c][2 * r]) : 0.0f;
+              x[c][2 * r + 1] = in ? vx[c][r].y - gam * (d[c][2 * r + 1] + e[c][2 * r + 1]) : 0.0f;
+              sh.X.put(i, side * (W / 2) + c * 8 + 2 * t, in ? beta * x[c][2 * r] : 0.0f, in ? beta * x[c][2 * r + 1] : 0.0f);
             }
           }
         }
         __syncthreads();
-        {  // U = Tm X
-          float d[2][4] = {}, e[2][4] = {};
-          for (int k0 = 0; k0 <= rb2; k0 += 16) {
-            FragA fa[2];
-            load_a(sh.Tm, rb2, k0, fa);
+        {
+          float d[kXTiles][4] = {}, e[kXTiles][4] = {};
+          product_part<2, 3, 3, kXTiles, false>(d, e, sh.N, rb, sh.X, side * (W / 2), 0, rb + 16);
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
+          for (int r = 0; r < 2; ++r) {
+            const int i = rb + g + 8 * r;
+            const bool in = i >= lo && i < hi;
+            const float beta = gate.beta[i];
 #pragma unroll
-              for (int x = 0; x < 2; ++x) mma<false, false>(d[x], e[x], fa[s], load_b(sh.X, side * 16 + x * 8, k0 + 8 * s));
-          }
-#pragma unroll
-          for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int i = rb2 + g + 8 * (r >> 1);
-              sh.U.to(i, side * 16 + x * 8 + 2 * t + (r & 1)) = i >= lo && i < hi ? d[x][r] + e[x][r] : 0.0f;
+            for (int c = 0; c < kXTiles; ++c) {
+              const float y = in ? x[c][2 * r] - (d[c][2 * r] + e[c][2 * r]) : 0.0f;
+              const float z = in ? x[c][2 * r + 1] - (d[c][2 * r + 1] + e[c][2 * r + 1]) : 0.0f;
+              rv[r] = fmaf(rx[c][r].x, vx[c][r].x, fmaf(rx[c][r].y, vx[c][r].y, rv[r]));
+              ry[r] = fmaf(rx[c][r].x, y, fmaf(rx[c][r].y, z, ry[r]));
+              sh.U.put(i, side * (W / 2) + c * 8 + 2 * t, in ? beta * y : 0.0f, in ? beta * z : 0.0f);
             }
+          }
         }
         __syncthreads();
+        const int below = rb + 16;  // columns j of P and E that are not zero everywhere
+        {
+          uint32_t fa[W / 16][P][4];
 #pragma unroll
-        for (int k0 = 0; k0 < kSlice; k0 += 16) {
-          FragA fo[2], fr[2], fu[2];
-          load_a(sh.dO, rb, k0, fo);
-          load_a(sh.R, rb, k0, fr);
-          load_a(sh.U, rb, k0, fu);
+          for (int k = 0; k < W / 16; ++k) load_a<P>(sh.dO, rb, k * 16, fa[k]);
+          add_rows<2, 3, 4, W>(acc_p, fa, sh.U, side * 32, below);
+          if (!fresh) add_rows<2, 3, kTiles, W>(acc_q, fa, sh.S, side * kHalf, KD);
+        }
+        {
+          uint32_t fa[W / 16][kOut][4];
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
+          for (int k = 0; k < W / 16; ++k) load_a<kOut>(sh.R, rb, k * 16, fa[k]);
+          add_rows<kDepth, kOut, 4, W>(acc_e, fa, sh.U, side * 32, below);
+          if (!fresh) add_rows<kDepth, kOut, kTiles, W>(acc_w, fa, sh.S, side * kHalf, KD);
+        }
+        if (last) {
+          uint32_t fa[W / 16][kOut][4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              if (side * 32 + x * 8 > rb + 15) continue;
-              const FragB fb = load_b(sh.U, side * 32 + x * 8, k0 + 8 * s);
-              mma<kOne, false>(acc_p[x], acc_p[x], fo[s], fb);
-              mma<false, false>(acc_e[x], acc_e[x], fr[s], fb);
-            }
-            if (!fresh) {
-#pragma unroll
-              for (int x = 0; x < kTiles; ++x) {
-                const FragB fb = load_b(sh.S, side * kHalf + x * 8, k0 + 8 * s);
-                mma<kOne, false>(acc_q[x], acc_q[x], fo[s], fb);
-                mma<false, false>(acc_w[x], acc_w[x], fr[s], fb);
-              }
-            }
-            if (last) {
-#pragma unroll
-              for (int x = 0; x < kTiles; ++x)
-                mma<false, false>(acc_t[x], acc_t[x], fu[s], load_b(sh.dS, side * kHalf + x * 8, k0 + 8 * s));
-            }
-          }
+          for (int k = 0; k < W / 16; ++k) load_a<kOut>(sh.U, rb, k * 16, fa[k]);
+          add_rows<kDepth, kOut, kTiles, W>(acc_t, fa, sh.dS, side * kHalf, KD);
         }
       }
-
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int i = rb + g + 8 * (r >> 1), j = side * 32 + x * 8 + 2 * t + (r & 1);
-          const float dist = (gate.g_high[i] - gate.g_high[j]) + (gate.g_low[i] - gate.g_low[j]);
-          const float D = i >= j && j >= lo && i < hi ? expf(dist) : 0.0f;
-          sh.P.to(i, j) = D != 0.0f ? a.scale * D * acc_p[x][r] : 0.0f;
-          sh.E.to(i, j) = D != 0.0f && i > j ? D * acc_e[x][r] : 0.0f;
-        }
       __syncthreads();
 
-      float far[2] = {}, dot_q[2] = {}, dot_w[2] = {}, dot_t[2] = {};  // row sums with K or Q
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int i = rb + g + 8 * r;
-        const float gam = gate.gam[i], dec = gate.dec[i];
-#pragma unroll
-        for (int x = 0; x < kTiles; ++x) {
-          const float2 kx = sh.K.pair(i, side * kHalf + x * 8 + 2 * t);
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            acc_q[x][2 * r + c] = fresh ? 0.0f : a.scale * gam * acc_q[x][2 * r + c];
-            acc_w[x][2 * r + c] = fresh ? 0.0f : gam * acc_w[x][2 * r + c];
-            acc_t[x][2 * r + c] = last ? dec * acc_t[x][2 * r + c] : 0.0f;
-            far[r] = fmaf(c ? kx.y : kx.x, acc_t[x][2 * r + c], far[r]);
-          }
-        }
-      }
-      for (int k0 = 0; k0 <= rb; k0 += 16) {  // P K, E K
-        FragA fp[2], fe[2];
-        load_a(sh.P, rb, k0, fp);
-        load_a(sh.E, rb, k0, fe);
-#pragma unroll
-        for (int x = 0; x < kTiles; x += 2) {
-          FragB fb[2][2];
-          load_bt16(sh.K, side * kHalf + x * 8, k0, fb);
-#pragma unroll
-          for (int y = 0; y < 2; ++y)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              mma<false, kOne>(acc_q[x + y], acc_q[x + y], fp[s], fb[y][s]);
-              mma<false, kOne>(acc_w[x + y], acc_w[x + y], fe[s], fb[y][s]);
-            }
-        }
-      }
-      for (int k0 = rb; k0 < C; k0 += 16) {  // P^T Q, - E^T beta K
-        FragA fp[2], fe[2];
-        load_at(sh.P, rb, k0, fp);
-        load_at(sh.E, rb, k0, fe);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const int i = k0 + 8 * s + 2 * t;
-          const float b0 = i >= lo && i < hi ? -gate.beta[i] : 0.0f, b1 = i + 1 >= lo && i + 1 < hi ? -gate.beta[i + 1] : 0.0f;
-          fe[s].x[0] *= b0, fe[s].x[1] *= b0, fe[s].x[2] *= b1, fe[s].x[3] *= b1;
-        }
-#pragma unroll
-        for (int x = 0; x < kTiles; x += 2) {
-          FragB fq[2][2], fk[2][2];
-          load_bt16(sh.Q, side * kHalf + x * 8, k0, fq);
-          load_bt16(sh.K, side * kHalf + x * 8, k0, fk);
-#pragma unroll
-          for (int y = 0; y < 2; ++y)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              mma<false, kOne>(acc_t[x + y], acc_t[x + y], fp[s], fq[y][s]);
-              mma<false, kOne>(acc_t[x + y], acc_t[x + y], fe[s], fk[y][s]);
-            }
-        }
-      }
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int i = rb + g + 8 * r;
         const bool in = i >= lo && i < hi;
         const float beta = gate.beta[i];
-        float* sum_q = a.sum_q + (((long long)n * a.B + b) * Hk + hk) * C * KD + i * KD;
-        float* sum_k = a.sum_k + (((long long)n * a.B + b) * Hk + hk) * C * KD + i * KD;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int j = side * 32 + x * 8 + 2 * t;
+          float p[2], e[2];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const float dist = (gate.g_high[i] - gate.g_high[j + y]) + (gate.g_low[i] - gate.g_low[j + y]);
+            const bool both = in && i >= j + y && j + y >= lo;
+            const float D = both ? expf(dist) : 0.0f;
+            p[y] = both ? a.scale * D * acc_p[x][2 * r + y] : 0.0f;
+            e[y] = both && i > j + y ? beta * D * acc_e[x][2 * r + y] : 0.0f;
+          }
+          sh.Pm.put(i, j, p[0], p[1]);
+          sh.E.put(i, j, e[0], e[1]);
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int i = rb + g + 8 * r;
+        const float gam = gate.gam[i], dec = gate.dec[i], back = -gate.beta[i] * gam;
+#pragma unroll
+        for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+          for (int y = 2 * r; y < 2 * r + 2; ++y) {
+            acc_q[x][y] = fresh ? 0.0f : a.scale * gam * acc_q[x][y];
+            acc_t[x][y] = (last ? dec * acc_t[x][y] : 0.0f) + (fresh ? 0.0f : back * acc_w[x][y]);
+          }
+      }
+      // P K to acc_q; P^T Q - E^T K - E K to acc_t (E's sign turned where it is subtracted: acc_w)
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) acc_w[x][y] = 0.0f;
+#pragma unroll
+      for (int k0 = 0; k0 < C; k0 += 16) {
+        if (k0 > rb) continue;
+        uint32_t fp[3][4], fe[kOut][4];
+        load_a<3>(sh.Pm, rb, k0, fp);
+        load_a<kOut>(sh.E, rb, k0, fe);
+#pragma unroll
+        for (int x = 0; x < kTiles; x += 2) {
+          uint32_t fb[P][2][2];
+          load_bt<P>(sh.K, side * kHalf + x * 8, k0, fb);
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            float d[4] = {}, e[4] = {};
+            mma<2>(d, e, fp, fb, y);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc_q[x + y][r] += d[r] + e[r];
+            mma<kDepth>(acc_w[x + y], acc_w[x + y], fe, fb, y);
+          }
+        }
+      }
+#pragma unroll
+      for (int k0 = 0; k0 < C; k0 += 16) {
+        if (k0 < rb) continue;
+        uint32_t fp[kOut][4], fe[kOut][4];
+        load_at<kOut>(sh.Pm, rb, k0, fp);
+        load_at<kOut>(sh.E, rb, k0, fe);
+#pragma unroll
+        for (int x = 0; x < kTiles; x += 2) {
+          uint32_t fk[P][2][2], fq[P][2][2];
+          load_bt<P>(sh.K, side * kHalf + x * 8, k0, fk);
+          load_bt<P>(sh.Q, side * kHalf + x * 8, k0, fq);
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            mma<kDepth>(acc_t[x + y], acc_t[x + y], fp, fq, y);
+            mma<kDepth>(acc_w[x + y], acc_w[x + y], fe, fk, y);
+          }
+        }
+      }
+      float dot_q[2] = {};
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int i = rb + g + 8 * r;
+        const bool in = i >= lo && i < hi;
+        float* sum_q = a.sum_q + (where * C + i) * KD;
+        float* sum_k = a.sum_k + (where * C + i) * KD;
 #pragma unroll
         for (int x = 0; x < kTiles; ++x) {
           const int c = side * kHalf + x * 8 + 2 * t;
-          const float2 kx = sh.K.pair(i, c), qx = sh.Q.pair(i, c);
+          const float2 qx = sh.Q.pair(i, c);
           float gq[2], gk[2];
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            const float aq = acc_q[x][2 * r + y], aw = acc_w[x][2 * r + y], at = acc_t[x][2 * r + y];
-            dot_q[r] = fmaf(y ? qx.y : qx.x, aq, dot_q[r]);
-            dot_w[r] = fmaf(y ? kx.y : kx.x, aw, dot_w[r]);
-            dot_t[r] = fmaf(y ? kx.y : kx.x, at, dot_t[r]);
-            gq[y] = aq;
-            gk[y] = fmaf(-beta, aw, at);
+            gq[y] = acc_q[x][2 * r + y];
+            gk[y] = acc_t[x][2 * r + y] - acc_w[x][2 * r + y];
+            dot_q[r] = fmaf(y ? qx.y : qx.x, gq[y], dot_q[r]);
           }
           if (!in) continue;
           if (a.share > 1) {  // over the value heads of a key head: each thread goes on with what it wrote itself
@@ -1165,7 +1326,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
           }
         }
       }
-      // sums over a row's columns: four lanes and two warps; over the block for <dS, S0>
+      // sums over a row's columns: four lanes and two warps
       auto row_sum = [&](int which, float (&x)[2]) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -1176,51 +1337,37 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
         }
       };
       row_sum(0, rv);
-      row_sum(1, far);
+      row_sum(1, ry);
       row_sum(2, dot_q);
-      row_sum(3, dot_w);
-      row_sum(4, dot_t);
-#pragma unroll
-      for (int d = 16; d > 0; d /= 2) dots += __shfl_xor_sync(0xffffffffu, dots, d);
-      if (lane == 0) sh.sums[10 * C + warp] = dots;
       __syncthreads();
-      if (warp == 0) {  // dbeta, and dg as sums from the piece's end (rows lane and lane + 32)
+      if (warp == 0) {  // dbeta, and dg: what the state before gives, less the rows before (rows lane and lane + 32)
         auto sum_of = [&](int which, int row) { return sh.sums[which * 2 * C + row] + sh.sums[(which * 2 + 1) * C + row]; };
-        float G[2], far_all = 0.0f;
+        float start = 0.0f;
+        if (!fresh)
+          for (int i = 0; i < a.tiles; ++i) start += a.dots[chunk * a.tiles + i];
+        float G[2], own[2];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           const int row = lane + 32 * s;
           const bool in = row >= lo && row < hi;
-          G[s] = in ? sum_of(2, row) - fmaf(gate.beta[row], sum_of(3, row), sum_of(4, row)) : 0.0f;
-          far_all += in ? sum_of(1, row) : 0.0f;
-          if (in) a.dbeta[(t0 + row) * a.dbt + b * a.dbb + h] = sum_of(0, row) - sum_of(3, row);
-        }
-#pragma unroll
-        for (int d = 16; d > 0; d /= 2) far_all += __shfl_xor_sync(0xffffffffu, far_all, d);
-        float all_dots = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) all_dots += sh.sums[10 * C + w];
-        const float end = last ? (cuts ? far_all : fmaf(gate.gam[C - 1], all_dots, far_all)) : 0.0f;
-#pragma unroll
-        for (int s = 1; s >= 0; --s) {
-          if (lane + 32 * s == hi - 1) G[s] += end;
+          own[s] = in ? sum_of(2, row) - gate.beta[row] * sum_of(0, row) : 0.0f;
+          if (in) a.dbeta[(long long)(t0 + row) * a.dbt + b * a.dbb + h] = sum_of(1, row);
+          float x = own[s];
 #pragma unroll
           for (int d = 1; d < 32; d *= 2) {
-            const float y = __shfl_down_sync(0xffffffffu, G[s], d);
-            if (lane + d < 32) G[s] += y;
+            const float y = __shfl_up_sync(0xffffffffu, x, d);
+            if (lane >= d) x += y;
           }
-          if (s == 1) {
-            const float behind = __shfl_sync(0xffffffffu, G[1], 0);
-            if (lane == 31) G[0] += behind;
-          }
+          G[s] = x;
         }
+        G[1] += __shfl_sync(0xffffffffu, G[0], 31);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           const int row = lane + 32 * s;
           if (row < lo || row >= hi) continue;
-          const float g_in = a.g[(t0 + row) * a.gt + b * a.gb + h];
+          const float g_in = a.g[(long long)(t0 + row) * a.gt + b * a.gb + h];
           const bool none = (cuts >> row & 1ull) || g_in < kLeastG;  // a decay that nothing passes through
-          a.dg[(t0 + row) * a.dgt + b * a.dgb + h] = none ? 0.0f : G[s];
+          a.dg[(long long)(t0 + row) * a.dgt + b * a.dgb + h] = none ? 0.0f : start - (G[s] - own[s]);
         }
       }
       lo = hi;
@@ -1231,10 +1378,10 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
 // ---- host ----------------------------------------------------------------------
 
 struct Workspace {
-  size_t Tm, M, gates, dS, R, sum_q, sum_k, bytes;
+  size_t keys, heads, dS, R, dots, sum_q, sum_k, bytes;
 };
-Workspace workspace_of(long long T, long long B, long long H, long long Hk, long long Dk, long long Dv, bool backward) {
-  const size_t chunks = (size_t)((T + C - 1) / C) * B * H, KD = Dk <= 64 ? 64 : 128;
+Workspace workspace_of(size_t es, bool exact, long long T, long long B, long long H, long long Hk, long long Dk, long long Dv, bool backward) {
+  const size_t chunks = (size_t)((T + C - 1) / C) * B, KD = Dk <= 64 ? 64 : 128;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t from = at;
@@ -1242,25 +1389,24 @@ Workspace workspace_of(long long T, long long B, long long H, long long Hk, long
     return from;
   };
   Workspace w{};
-  w.Tm = take(chunks * C * C * 4);
-  w.M = take(chunks * C * C * 4);
-  w.gates = take(chunks * sizeof(Gates));
+  w.keys = take(chunks * Hk * 2 * C * KD * 2 * (es == 4 ? 3 : exact ? 1 : 2));
+  w.heads = take(chunks * H * kHeadBytes);
   if (backward) {
-    w.dS = take(chunks * Dk * Dv * 4);
-    w.R = take(chunks * C * Dv * 4);
+    w.dS = take(chunks * H * Dk * Dv * 4);
+    w.R = take(chunks * H * C * Dv * 4);
+    w.dots = take(chunks * H * ((Dv + 15) / 16) * 4);
     if (H > Hk) {
-      w.sum_q = take(chunks / H * Hk * C * KD * 4);
-      w.sum_k = take(chunks / H * Hk * C * KD * 4);
+      w.sum_q = take(chunks * Hk * C * KD * 4);
+      w.sum_k = take(chunks * Hk * C * KD * 4);
     }
   }
   w.bytes = at + 256;
   return w;
 }
 
-// Columns of S to a block: 16 while that fits the device in one wave, and where two chunks of 32-bit keys fill the
-// shared memory.
-int columns_of(long long heads, int Dk, int Dv, size_t es) {
-  return heads * ((Dv + 15) / 16) <= 152 || (es == 4 && Dk > 64) ? 16 : 32;
+// Columns of S to a block: 16 while that fits the device in one wave, and for 32-bit keys, whose parts fill the shared memory.
+int columns_of(long long heads, int Dv, size_t es) {
+  return heads * ((Dv + 15) / 16) <= 152 || es == 4 ? 16 : 32;
 }
 
 template <auto kKern>
@@ -1279,13 +1425,15 @@ cudaError_t for_shape(int dtype, int Dk, F f) {
   });
 }
 
-cudaError_t prepare(int dtype, const DeltaArgs& a, cudaStream_t s) {
-  const long long blocks = (long long)((a.T + C - 1) / C) * a.B * a.H;
+cudaError_t prepare(int dtype, const DeltaArgs& a, bool backward, cudaStream_t s) {
+  const long long blocks = (long long)((a.T + C - 1) / C) * a.B * (a.H / a.share);
   if (blocks == 0) return cudaSuccess;
   return for_shape(dtype, a.Dk, [&](auto* t, auto kd) {
     using T = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
-    return launch_big<delta_prepare_kernel<T, KD>>(dim3((unsigned)blocks), prepare_smem<T, KD>(), s, a);
+    constexpr size_t bytes = PrepareShared<T, KD>::kBytes;
+    if (backward) return launch_big<delta_prepare_kernel<T, KD, true>>(dim3((unsigned)blocks), bytes, s, a);
+    return launch_big<delta_prepare_kernel<T, KD, false>>(dim3((unsigned)blocks), bytes, s, a);
   });
 }
 
@@ -1319,11 +1467,11 @@ int check(int dtype, const void* q, const void* k, const void* v, const float* g
 
 using namespace lstm_approx_impl;
 
-extern "C" size_t lstm_approx_delta_scan_workspace_bytes(int T, int B, int H, int Hk, int Dk, int Dv, int backward) {
-  if (check(LSTM_APPROX_OP_FP32, nullptr, nullptr, nullptr, nullptr, nullptr, 0, B, H, Hk, Dk, Dv, nullptr, 0, nullptr, 0) || T < 0 ||
+extern "C" size_t lstm_approx_delta_scan_workspace_bytes(int dtype, int T, int B, int H, int Hk, int Dk, int Dv, int backward) {
+  if (check(dtype, nullptr, nullptr, nullptr, nullptr, nullptr, 0, B, H, Hk, Dk, Dv, nullptr, 0, nullptr, 0) || T < 0 ||
       (long long)((T + 63ll) / 64) * B > 0x7fffffffll / H)
     return 0;
-  return workspace_of(T, B, H, Hk, Dk, Dv, backward != 0).bytes;
+  return workspace_of(op_dtype_bytes(dtype), dtype == LSTM_APPROX_OP_BF16, T, B, H, Hk, Dk, Dv, backward != 0).bytes;
 }
 
 extern "C" int lstm_approx_delta_scan(int dtype, const void* q, const void* k, const void* v, const float* g, const float* beta,
@@ -1338,7 +1486,7 @@ extern "C" int lstm_approx_delta_scan(int dtype, const void* q, const void* k, c
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "o and h_last must not be NULL");
   if (!op_aligned(o, es) || !op_aligned(h0, 4) || !op_aligned(h_last, 4) || !op_aligned(states, 4) || !op_aligned(lengths, 4))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "a pointer not aligned to its type");
-  const Workspace w = workspace_of(T, B, H, Hk, Dk, Dv, false);
+  const Workspace w = workspace_of(es, dtype == LSTM_APPROX_OP_BF16, T, B, H, Hk, Dk, Dv, false);
   if (!workspace || !op_aligned(workspace, 16) || workspace_bytes < w.bytes)
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "needs a 16-byte aligned workspace of %zu bytes", w.bytes);
   if (int rc = op_check_device(msg, msg_len)) return rc;
@@ -1354,21 +1502,21 @@ extern "C" int lstm_approx_delta_scan(int dtype, const void* q, const void* k, c
   a.T = T, a.B = B, a.H = H, a.share = H / Hk, a.Dk = Dk, a.Dv = Dv;
   a.wide = wide_rows(q, a.qs, Dk, es) && wide_rows(k, a.ks, Dk, es);
   a.pairs = pair_rows(v, a.vs, Dv, es) && pair_rows(o, a.os, Dv, es);
+  a.even = Dv % 2 == 0 && op_aligned(h0, 8) && op_aligned(h_last, 8) && op_aligned(states, 8);
   a.h_last = h_last, a.states = states;
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) / 256 * 256);
-  a.Tm = reinterpret_cast<float*>(ws + w.Tm), a.M = reinterpret_cast<float*>(ws + w.M);
-  a.gates = reinterpret_cast<Gates*>(ws + w.gates);
+  a.keys = reinterpret_cast<unsigned char*>(ws + w.keys), a.heads = reinterpret_cast<unsigned char*>(ws + w.heads);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  if (int rc = op_launched(prepare(dtype, a, s), "delta scan launch", msg, msg_len)) return rc;
-  const int NV = columns_of((long long)B * H, Dk, Dv, es);
+  if (int rc = op_launched(prepare(dtype, a, false, s), "delta scan launch", msg, msg_len)) return rc;
+  const int NV = columns_of((long long)B * H, Dv, es);
   a.tiles = (Dv + NV - 1) / NV;
   const dim3 grid((unsigned)(B * H * a.tiles));
   const cudaError_t e = for_shape(dtype, Dk, [&](auto* t, auto kd) {
     using Ty = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
-    if constexpr (sizeof(Ty) == 2 || KD == 64)
-      if (NV == 32) return launch_big<delta_forward_kernel<Ty, KD, 32>>(grid, forward_smem<Ty, KD, 32>(), s, a);
-    return launch_big<delta_forward_kernel<Ty, KD, 16>>(grid, forward_smem<Ty, KD, 16>(), s, a);
+    if constexpr (sizeof(Ty) == 2)
+      if (NV == 32) return launch_big<delta_forward_kernel<Ty, KD, 32>>(grid, ForwardShared<Ty, KD, 32>::kBytes, s, a);
+    return launch_big<delta_forward_kernel<Ty, KD, 16>>(grid, ForwardShared<Ty, KD, 16>::kBytes, s, a);
   });
   return op_launched(e, "delta scan launch", msg, msg_len);
 }
@@ -1387,7 +1535,7 @@ extern "C" int lstm_approx_delta_scan_backward(int dtype, const void* d_o, const
   if (!op_aligned(d_o, es) || !op_aligned(dq, es) || !op_aligned(dk, es) || !op_aligned(dv, es) || !op_aligned(dh_last, 4) ||
       !op_aligned(states, 4) || !op_aligned(lengths, 4) || !op_aligned(dg, 4) || !op_aligned(dbeta, 4) || !op_aligned(dh0, 4))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "a pointer not aligned to its type");
-  const Workspace w = workspace_of(T, B, H, Hk, Dk, Dv, true);
+  const Workspace w = workspace_of(es, dtype == LSTM_APPROX_OP_BF16, T, B, H, Hk, Dk, Dv, true);
   if (!workspace || !op_aligned(workspace, 16) || workspace_bytes < w.bytes)
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "needs a 16-byte aligned workspace of %zu bytes", w.bytes);
   if (int rc = op_check_device(msg, msg_len)) return rc;
@@ -1405,24 +1553,25 @@ extern "C" int lstm_approx_delta_scan_backward(int dtype, const void* d_o, const
   a.T = T, a.B = B, a.H = H, a.share = H / Hk, a.Dk = Dk, a.Dv = Dv;
   a.wide = wide_rows(q, a.qs, Dk, es) && wide_rows(k, a.ks, Dk, es) && wide_rows(dq, a.dqs, Dk, es) && wide_rows(dk, a.dks, Dk, es);
   a.pairs = pair_rows(v, a.vs, Dv, es) && pair_rows(d_o, a.dos, Dv, es) && pair_rows(dv, a.dvs, Dv, es);
+  a.even = Dv % 2 == 0 && op_aligned(states, 8) && op_aligned(dh_last, 8) && op_aligned(dh0, 8);
   a.states = const_cast<float*>(states), a.dh_last = dh_last;
   a.dq = dq, a.dk = dk, a.dv = dv, a.dg = dg, a.dbeta = dbeta, a.dh0 = dh0;
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) / 256 * 256);
-  a.Tm = reinterpret_cast<float*>(ws + w.Tm), a.M = reinterpret_cast<float*>(ws + w.M);
-  a.gates = reinterpret_cast<Gates*>(ws + w.gates);
+  a.keys = reinterpret_cast<unsigned char*>(ws + w.keys), a.heads = reinterpret_cast<unsigned char*>(ws + w.heads);
   a.dS = reinterpret_cast<float*>(ws + w.dS), a.R = reinterpret_cast<float*>(ws + w.R);
+  a.dots = reinterpret_cast<float*>(ws + w.dots);
   a.sum_q = reinterpret_cast<float*>(ws + w.sum_q), a.sum_k = reinterpret_cast<float*>(ws + w.sum_k);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  if (int rc = op_launched(prepare(dtype, a, s), "delta scan launch", msg, msg_len)) return rc;
-  const int NV = columns_of((long long)B * H, Dk, Dv, es);
+  if (int rc = op_launched(prepare(dtype, a, true, s), "delta scan launch", msg, msg_len)) return rc;
+  const int NV = columns_of((long long)B * H, Dv, es);
   a.tiles = (Dv + NV - 1) / NV;
   const dim3 grid((unsigned)(B * H * a.tiles));
   cudaError_t e = for_shape(dtype, Dk, [&](auto* t, auto kd) {
     using Ty = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
-    if constexpr (sizeof(Ty) == 2 || KD == 64)
-      if (NV == 32) return launch_big<delta_backward_kernel<Ty, KD, 32>>(grid, forward_smem<Ty, KD, 32>(), s, a);
-    return launch_big<delta_backward_kernel<Ty, KD, 16>>(grid, forward_smem<Ty, KD, 16>(), s, a);
+    if constexpr (sizeof(Ty) == 2)
+      if (NV == 32) return launch_big<delta_backward_kernel<Ty, KD, 32>>(grid, BackwardShared<Ty, KD, 32>::kBytes, s, a);
+    return launch_big<delta_backward_kernel<Ty, KD, 16>>(grid, BackwardShared<Ty, KD, 16>::kBytes, s, a);
   });
   if (int rc = op_launched(e, "delta scan backward launch", msg, msg_len)) return rc;
   if (T == 0) return LSTM_APPROX_OK;

@@ -587,7 +587,7 @@ PyObject* delta_scan(PyObject*, PyObject* const* a, Py_ssize_t) {
     void* po = heads.add(call, o, "o", false, strides, n);
     Tensor last = call.out(a[10], "h_last", at::kFloat, {B, H, Dk, Dv});
     if (states) Call::written(tensor(a[11], "states"));
-    Tensor ws = call.workspace(a[12], lstm_approx_delta_scan_workspace_bytes((int)T, (int)B, (int)H, (int)heads.Hk, (int)Dk, (int)Dv, 0));
+    Tensor ws = call.workspace(a[12], lstm_approx_delta_scan_workspace_bytes(heads.code, (int)T, (int)B, (int)H, (int)heads.Hk, (int)Dk, (int)Dv, 0));
     call.done(lstm_approx_delta_scan(heads.code, pq, pk, pv, g, beta, scale, h0, lengths, reset, (int)T, (int)B, (int)H,
                                      (int)heads.Hk, (int)Dk, (int)Dv, po, strides, last.data_ptr<float>(), states,
                                      ws.data_ptr(), ws.nbytes(), call.stream, call.msg, sizeof(call.msg)));
@@ -634,7 +634,7 @@ PyObject* delta_scan_backward(PyObject*, PyObject* const* a, Py_ssize_t) {
     float* pdg = heads.add_gate(call, dg, "dg", strides, n);
     float* pdbeta = heads.add_gate(call, dbeta, "dbeta", strides, n);
     Tensor dh0 = call.out(a[16], "dh0", at::kFloat, {B, H, Dk, Dv});
-    Tensor ws = call.workspace(a[17], lstm_approx_delta_scan_workspace_bytes((int)T, (int)B, (int)H, (int)heads.Hk, (int)Dk, (int)Dv, 1));
+    Tensor ws = call.workspace(a[17], lstm_approx_delta_scan_workspace_bytes(heads.code, (int)T, (int)B, (int)H, (int)heads.Hk, (int)Dk, (int)Dv, 1));
     call.done(lstm_approx_delta_scan_backward(heads.code, pdo, dl, pq, pk, pv, g, beta, scale, states, lengths, reset, (int)T,
                                               (int)B, (int)H, (int)heads.Hk, (int)Dk, (int)Dv, pdq, pdk, pdv, pdg, pdbeta,
                                               dh0.data_ptr<float>(), strides, ws.data_ptr(), ws.nbytes(), call.stream, call.msg,

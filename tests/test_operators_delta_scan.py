@@ -368,7 +368,7 @@ def test_many_heads_and_wide_values(cuda_device):
 def test_refusals(lib):
     P, msg = ctypes.c_void_p, ctypes.create_string_buffer(256)
     sizes = dict(T=8, B=2, H=4, Hk=2, Dk=64, Dv=64)
-    need = {back: lib.lstm_approx_delta_scan_workspace_bytes(*sizes.values(), back) for back in (0, 1)}
+    need = {back: lib.lstm_approx_delta_scan_workspace_bytes(1, *sizes.values(), back) for back in (0, 1)}
     assert 0 < need[0] < need[1]
     forward = dict(dtype=1, q=P(256), k=P(256), v=P(256), g=P(256), beta=P(256), scale=1.0, h0=None, lengths=None, reset=None,
                    **sizes, o=P(256), strides=None, h_last=P(256), states=None, workspace=P(256), bytes=need[0])
@@ -387,7 +387,8 @@ def test_refusals(lib):
             assert call(*args.values(), None, msg, 256) == EINVAL, change
             assert msg.value
     for bad in (dict(T=-1), dict(H=3), dict(Dk=129), dict(B=2 ** 31 - 1, T=2 ** 31 - 1)):
-        assert lib.lstm_approx_delta_scan_workspace_bytes(*{**sizes, **bad}.values(), 1) == 0
+        assert lib.lstm_approx_delta_scan_workspace_bytes(1, *{**sizes, **bad}.values(), 1) == 0
+    assert lib.lstm_approx_delta_scan_workspace_bytes(3, *sizes.values(), 1) == 0
 
 
 @pytest.mark.gpu
