@@ -168,25 +168,20 @@ __device__ __forceinline__ void load_bt_tall(const Mat<kRows, W, kHas>& m, int n
   }
 }
 
-// d + e += a b: part i of a with part j of b where i + j <= kDepth, the first ones' product to d, the others to e.
+// d + e (+ f) += a b, column tile x of b: part i of a with part j of b where i + j <= kDepth, to d, e and f by i + j.
 template <int kDepth, int kPA, int kPB>
-__device__ __forceinline__ void mma(float (&d)[4], float (&e)[4], const uint32_t (&a)[kPA][4], const uint32_t (&b0)[kPB],
-                                    const uint32_t (&b1)[kPB]) {
+__device__ __forceinline__ void mma(float (&d)[4], float (&e)[4], float (&f)[4], const uint32_t (&a)[kPA][4], const uint32_t (&b)[kPB][2][2],
+                                    int x) {
 #pragma unroll
-  for (int s = kDepth; s >= 0; --s)
+  for (int i = 0; i < kPA; ++i)
 #pragma unroll
-    for (int i = 0; i < kPA; ++i)
+    for (int s = kDepth; s >= 0; --s)
       if (s - i >= 0 && s - i < kPB)
-        mma_16816_bf16<true, false>(s ? e : d, a[i][0], a[i][1], a[i][2], a[i][3], b0[s - i], b1[s - i]);
+        mma_16816_bf16<true, false>(s == 0 ? d : s == 1 ? e : f, a[i][0], a[i][1], a[i][2], a[i][3], b[s - i][x][0], b[s - i][x][1]);
 }
 template <int kDepth, int kPA, int kPB>
 __device__ __forceinline__ void mma(float (&d)[4], float (&e)[4], const uint32_t (&a)[kPA][4], const uint32_t (&b)[kPB][2][2], int x) {
-#pragma unroll
-  for (int s = kDepth; s >= 0; --s)
-#pragma unroll
-    for (int i = 0; i < kPA; ++i)
-      if (s - i >= 0 && s - i < kPB)
-        mma_16816_bf16<true, false>(s ? e : d, a[i][0], a[i][1], a[i][2], a[i][3], b[s - i][x][0], b[s - i][x][1]);
+  mma<kDepth>(d, e, e, a, b, x);
 }
 
 // ---- what the kernels share ----------------------------------------------------
@@ -212,10 +207,11 @@ struct DeltaArgs {
   const float* h0;
   const int32_t* lengths;
   const unsigned char* reset;
-  int T, B, H, share, Dk, Dv, tiles;
+  int T, B, H, share, Dk, Dv, tiles, cluster;
   bool wide;   // q, k, dq and dk in 16-byte pieces
   bool pairs;  // v, o, dO and dV two at a time
   bool even;   // states two at a time
+  bool quads;  // states four at a time
   void* o;
   float *h_last, *states;
   // workspace: per chunk, stream and key head the parts of k and q; per value head those of N and M, and the gates
@@ -240,39 +236,49 @@ __device__ __forceinline__ int length_of(const DeltaArgs& a, int b) {
   return a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
 }
 
-__device__ __forceinline__ void copy16(void* to, const void* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+// Copies that this thread waits for (of `bytes`; zeros for the rest of 16, 4).
+__device__ __forceinline__ void copy16(void* to, const void* from, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy4(void* to, const void* from, int bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kLeft>
 __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
 }
-template <int kBytes>
+template <int kBytes, int kBy>
 __device__ __forceinline__ void fetch(void* to, const void* from) {
 #pragma unroll
-  for (int i = 0; i < kBytes; i += kThreads * 16)
-    if (i + kThreads * 16 <= kBytes || i + (int)threadIdx.x * 16 < kBytes)
-      copy16(static_cast<char*>(to) + i + threadIdx.x * 16, static_cast<const char*>(from) + i + threadIdx.x * 16);
+  for (int i = 0; i < kBytes; i += kBy * 16)
+    if (i + kBy * 16 <= kBytes || i + (int)threadIdx.x * 16 < kBytes)
+      copy16(static_cast<char*>(to) + i + threadIdx.x * 16, static_cast<const char*>(from) + i + threadIdx.x * 16, 16);
 }
-// The same of kP parts of a square matrix without its blocks above the diagonal.
-template <int kP>
-__device__ __forceinline__ void fetch_lower(bf16* to, const bf16* from) {
-  static_assert(C * C / 8 == 2 * kThreads, "two rounds to a part");
-#pragma unroll
-  for (int q = 0; q < kP; ++q)
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int i = (half * kThreads + (int)threadIdx.x) * 8, row = i / C, col = (i % C) ^ (row & 7) << 3;
-      if (col / 16 <= row / 16) copy16(to + q * C * C + i, from + q * C * C + i);
-    }
-}
+
+// A wait for a copy that a working device always completes; on one that does not the results are NaN.
+constexpr uint64_t kWaitNs = 2000000000ull;
+__device__ const int g_never = 0;
 
 // Two neighbouring values of a row (the second only if it lies in the row).
 template <typename T>
 __device__ __forceinline__ float2 get2(const T* row, int col, int D, bool pairs) {
   if (pairs) return col < D ? Pair<T>::get(*reinterpret_cast<const typename Pair<T>::Raw*>(row + col)) : make_float2(0.0f, 0.0f);
   return make_float2(col < D ? to_f32(row[col]) : 0.0f, col + 1 < D ? to_f32(row[col + 1]) : 0.0f);
+}
+// The same as they lie in memory: converted where they are used, so that nothing waits for them before.
+template <typename T>
+using Raw2 = typename Pair<T>::Raw;
+template <typename T>
+__device__ __forceinline__ Raw2<T> raw2(const T* row, int col, int D, bool pairs, bool in) {
+  Raw2<T> v = Pair<T>::put(0.0f, 0.0f);
+  if (pairs) {
+    if (in && col < D) v = *reinterpret_cast<const Raw2<T>*>(row + col);
+  } else {
+    if (in && col < D) v.x = row[col];
+    if (in && col + 1 < D) v.y = row[col + 1];
+  }
+  return v;
 }
 template <typename T>
 __device__ __forceinline__ void put2(T* row, int col, int D, bool pairs, float x, float y) {
@@ -283,6 +289,9 @@ __device__ __forceinline__ void put2(T* row, int col, int D, bool pairs, float x
     if (col + 1 < D) row[col + 1] = from_f32<T>(y);
   }
 }
+
+// e^x for x <= 0 from the hardware's 2^z: off by 2^-22 + |x| 2^-24 of it, which is under 2^-23 of 1.
+__device__ __forceinline__ float decay_of(float x) { return ex2_approx(x * kLog2E); }
 
 // The piece of a chunk that begins at row lo ends before this row.
 __device__ __forceinline__ int piece_end(unsigned long long cuts, int lo) {
@@ -298,40 +307,52 @@ __device__ __forceinline__ bool cut_between(unsigned long long cuts, int j, int 
 
 // ---- per chunk and key head: copies of q and k, gates, N and M --------------------
 
-template <typename T, int KD>
+template <typename T, int KD, int kMParts>
 struct PrepareShared {
-  KeyMat<T, KD> K, Q;
-  float *A, *N, *H;  // [C][kPitch]
-  Gates* gates;
+  static constexpr size_t kFirst = kKeysBytes<T, KD> > SquareMat::kBytes ? kKeysBytes<T, KD> : SquareMat::kBytes;
   static constexpr int kPitch = C + 4;
-  static constexpr size_t kBytes = kKeysBytes<T, KD> + (2 * C + C / 2) * kPitch * 4 + sizeof(Gates);
+  KeyMat<T, KD> K, Q;
+  SquareMat N;  // where K and Q were
+  Gates* gates;
+  Mat<C, C, kMParts> M;  // behind the gates, as in the workspace
+  SquareMat AB;          // A B
+  Mat<C / 2, C / 2, 3> BH;
+  float* A;  // [C][kPitch]; then N's blocks on the diagonal
+  static constexpr uint32_t kTail = sizeof(Gates) + Mat<C, C, kMParts>::kBytes;
+  static constexpr size_t kBytes = kFirst + kTail + SquareMat::kBytes + decltype(BH)::kBytes + C * kPitch * 4;
   __device__ __forceinline__ explicit PrepareShared(unsigned char* p)
-      : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * kParts<T>}, A(reinterpret_cast<float*>(Q.p + Q.kSize * kParts<T>)),
-        N(A + C * kPitch), H(N + C * kPitch), gates(reinterpret_cast<Gates*>(H + C / 2 * kPitch)) {}
+      : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * kParts<T>}, N{K.p}, gates(reinterpret_cast<Gates*>(p + kFirst)),
+        M{reinterpret_cast<bf16*>(gates + 1)}, AB{M.p + M.kSize * kMParts}, BH{AB.p + AB.kSize * 3},
+        A(reinterpret_cast<float*>(BH.p + BH.kSize * 3)) {}
 };
 
 // Rows of q or k as the MMAs read them: in parts, zeros past the stream's length and past Dk.
 template <typename T, int KD>
 __device__ __forceinline__ void fill_keys(const KeyMat<T, KD>& to, const T* p, long long t_stride, int rows, int Dk, bool wide) {
-  constexpr int kPer = 16 / (int)sizeof(T);
-#pragma unroll 4
-  for (int i = threadIdx.x; i < C * (KD / kPer); i += kThreads) {
-    const int row = i / (KD / kPer), col = i % (KD / kPer) * kPer;
-    uint4 raw = make_uint4(0u, 0u, 0u, 0u);
-    if (row < rows) {
-      if (wide) {
-        if (col < Dk) raw = *reinterpret_cast<const uint4*>(p + row * t_stride + col);
-      } else {
-        T x[kPer];
+  constexpr int kPer = 16 / (int)sizeof(T), kRounds = C * (KD / kPer) / kThreads;
+  uint4 raw[kRounds];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) x[e] = col + e < Dk ? p[row * t_stride + col + e] : from_f32<T>(0.0f);
-        raw = *reinterpret_cast<const uint4*>(x);
+  for (int x = 0; x < kRounds; ++x) {
+    const int i = threadIdx.x + x * kThreads, row = i / (KD / kPer), col = i % (KD / kPer) * kPer;
+    raw[x] = make_uint4(0u, 0u, 0u, 0u);
+    if (row < rows && col < Dk) {
+      if (wide) {
+        raw[x] = *reinterpret_cast<const uint4*>(p + row * t_stride + col);
+      } else {
+        T v[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) v[e] = col + e < Dk ? p[row * t_stride + col + e] : from_f32<T>(0.0f);
+        raw[x] = *reinterpret_cast<const uint4*>(v);
       }
     }
+  }
+#pragma unroll
+  for (int x = 0; x < kRounds; ++x) {
+    const int i = threadIdx.x + x * kThreads, row = i / (KD / kPer), col = i % (KD / kPer) * kPer;
     if constexpr (std::is_same_v<T, bf16>) {
-      *reinterpret_cast<uint4*>(to.p + to.at(row, col)) = raw;
+      *reinterpret_cast<uint4*>(to.p + to.at(row, col)) = raw[x];
     } else {
-      const typename Pair<T>::Raw* h = reinterpret_cast<const typename Pair<T>::Raw*>(&raw);
+      const typename Pair<T>::Raw* h = reinterpret_cast<const typename Pair<T>::Raw*>(&raw[x]);
 #pragma unroll
       for (int e = 0; e < kPer / 2; ++e) {
         const float2 f = Pair<T>::get(h[e]);
@@ -343,23 +364,31 @@ __device__ __forceinline__ void fill_keys(const KeyMat<T, KD>& to, const T* p, l
 
 // One warp: a chunk's sums of g, the decays that follow, beta (rows lane and lane + 32).  The sums are of 64 bits, so that
 // differences of far ones keep their digits, and begin anew at a reset, whose own g counts as zero.
-__device__ __forceinline__ void make_gates(const DeltaArgs& a, int t0, int rows, int b, int h, Gates& gates) {
+struct RawGates {
+  float g[2], beta[2];
+  unsigned char reset[2];
+  __device__ __forceinline__ void load(const DeltaArgs& a, int t0, int rows, int b, int h) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int row = (threadIdx.x & 31) + 32 * s;
+      const long long t = t0 + row;
+      const bool in = row < rows;
+      g[s] = in ? a.g[t * a.gt + b * a.gb + h] : 0.0f;
+      beta[s] = in ? a.beta[t * a.bt + b * a.bb + h] : 0.0f;
+      reset[s] = in && a.reset ? a.reset[t * a.B + b] : 0;
+    }
+  }
+};
+__device__ __forceinline__ void make_gates(const RawGates& raw, Gates& gates) {
   const int lane = threadIdx.x & 31;
   double G[2];
   unsigned cut[2];
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     const int row = lane + 32 * s;
-    const long long t = t0 + row;
-    float g = 0.0f, beta = 0.0f;
-    bool reset = false;
-    if (row < rows) {
-      g = a.g[t * a.gt + b * a.gb + h];
-      g = g < kLeastG ? kLeastG : g;
-      beta = a.beta[t * a.bt + b * a.bb + h];
-      reset = a.reset && a.reset[t * a.B + b];
-    }
-    gates.beta[row] = beta;
+    const float g = raw.g[s] < kLeastG ? kLeastG : raw.g[s];
+    const bool reset = raw.reset[s] != 0;
+    gates.beta[row] = raw.beta[s];
     cut[s] = __ballot_sync(0xffffffffu, reset);
     const unsigned before = cut[s] & (2u << lane) - 1u;
     const int start = before ? 31 - __clz((int)before) : 0;
@@ -388,9 +417,10 @@ __device__ __forceinline__ void make_gates(const DeltaArgs& a, int t0, int rows,
 }
 
 template <typename T, int KD, bool kBackward>
-__global__ void __launch_bounds__(kThreads) delta_prepare_kernel(const DeltaArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
-  using Sh = PrepareShared<T, KD>;
+  constexpr int P = kParts<T>;
+  using Sh = PrepareShared<T, KD, kBackward ? 3 : kOutParts<T>>;
   constexpr int kPitch = Sh::kPitch;
   const Sh sh(smem);
   Gates& gates = *sh.gates;
@@ -399,161 +429,191 @@ __global__ void __launch_bounds__(kThreads) delta_prepare_kernel(const DeltaArgs
   const int t0 = n * C, rows = min(length_of(a, b) - t0, C);
   if (rows <= 0) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane_g(), t = lane_t();
-  if (warp == 7) make_gates(a, t0, rows, b, hk * a.share, gates);
+  const int i0 = (warp & 3) * 16, side = (warp >> 2) * 32;  // a warp's 16 rows and 32 columns
+  RawGates raw;
+  if (warp == 7) raw.load(a, t0, rows, b, hk * a.share);
   fill_keys<T, KD>(sh.K, static_cast<const T*>(a.k) + t0 * a.ks.t + b * a.ks.b + hk * a.ks.h, a.ks.t, rows, a.Dk, a.wide);
   fill_keys<T, KD>(sh.Q, static_cast<const T*>(a.q) + t0 * a.qs.t + b * a.qs.b + hk * a.qs.h, a.qs.t, rows, a.Dk, a.wide);
+  if (warp == 7) make_gates(raw, gates);
+  fence_proxy_async_shared();
   __syncthreads();
-  uint4* keys = reinterpret_cast<uint4*>(a.keys + (size_t)blockIdx.x * kKeysBytes<T, KD>);
-#pragma unroll 4
-  for (int i = threadIdx.x; i < (int)(kKeysBytes<T, KD> / 16); i += kThreads) keys[i] = reinterpret_cast<const uint4*>(smem)[i];
-
-  // K K^T and Q K^T where j <= i: 20 tiles of 16 x 8, the warps' in turn
-  constexpr int kMost = 3;
-  float kk[kMost][4] = {}, qk[kMost][4] = {};
-  auto tile_at = [&](int x, int& i0, int& j0) {
-    const int tile = warp + 8 * x;
-    const int bi = tile < 2 ? 0 : tile < 6 ? 1 : tile < 12 ? 2 : 3;
-    i0 = bi * 16, j0 = (tile - bi * (bi + 1)) * 8;
-    return tile < 20;
-  };
+  if (threadIdx.x == 0)
+    bulk_copy_s2g(a.keys + (size_t)blockIdx.x * kKeysBytes<T, KD>, smem_u32(smem), (uint32_t)kKeysBytes<T, KD>);
   __syncwarp();
-#pragma unroll
-  for (int x = 0; x < kMost; ++x) {
-    int i0, j0;
-    if (!tile_at(x, i0, j0)) continue;
-    float ke[4] = {}, qe[4] = {};
+
+  float kk[4][4] = {}, qk[4][4] = {};  // K K^T and Q K^T
+  if (side < i0 + 16) {
+    float ke[4][4] = {}, qe[4][4] = {};
 #pragma unroll
     for (int k0 = 0; k0 < KD; k0 += 16) {
-      uint32_t fk[kParts<T>][4], fq[kParts<T>][4], fb[kParts<T>][2][2];
-      load_a<kParts<T>>(sh.K, i0, k0, fk);
-      load_a<kParts<T>>(sh.Q, i0, k0, fq);
-      load_b<kParts<T>>(sh.K, j0 & ~8, k0, fb);
-      if (j0 & 8) {
-        mma<2>(kk[x], ke, fk, fb, 1);
-        mma<2>(qk[x], qe, fq, fb, 1);
-      } else {
-        mma<2>(kk[x], ke, fk, fb, 0);
-        mma<2>(qk[x], qe, fq, fb, 0);
+      uint32_t fk[P][4], fq[P][4], fb[2][P][2][2];
+      load_a<P>(sh.K, i0, k0, fk);
+      load_a<P>(sh.Q, i0, k0, fq);
+      load_b<P>(sh.K, side, k0, fb[0]);
+      load_b<P>(sh.K, side + 16, k0, fb[1]);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        mma<2>(kk[x], ke[x], fk, fb[x >> 1], x & 1);
+        mma<2>(qk[x], qe[x], fq, fb[x >> 1], x & 1);
       }
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) kk[x][r] += ke[r], qk[x][r] += qe[r];
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) kk[x][r] += ke[x][r], qk[x][r] += qe[x][r];
   }
 
   for (int h = hk * a.share; h < (hk + 1) * a.share; ++h) {
+    if (threadIdx.x == 0) bulk_wait_read();  // of K and Q, or of the head before
+    __syncthreads();
     if (h > hk * a.share) {
-      __syncthreads();
-      if (warp == 7) make_gates(a, t0, rows, b, h, gates);
+      if (warp == 7) {
+        raw.load(a, t0, rows, b, h);
+        make_gates(raw, gates);
+      }
       __syncthreads();
     }
     const unsigned long long cuts = gates.cuts;
-    unsigned char* head = a.heads + ((size_t)((long long)n * a.B + b) * a.H + h) * kHeadBytes;
-    const SquareMat N{reinterpret_cast<bf16*>(head)}, M{N.p + 3 * N.kSize};
 #pragma unroll
-    for (int x = 0; x < kMost; ++x) {
-      int i0, j0;
-      if (!tile_at(x, i0, j0)) continue;
+    for (int x = 0; x < 4; ++x)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const int i = i0 + g + 8 * r, j = j0 + 2 * t;
-        float m[2];
+        const int i = i0 + g + 8 * r, j = side + x * 8 + 2 * t;
+        float m[2], v[2], w[2];
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           const float dist = (gates.g_high[i] - gates.g_high[j + y]) + (gates.g_low[i] - gates.g_low[j + y]);
-          const bool same = i >= j + y && !cut_between(cuts, j + y, i);
-          const float D = same ? expf(dist) : 0.0f;
+          const bool same = i >= j + y && !(cuts && cut_between(cuts, j + y, i));
+          const float D = same ? decay_of(dist) : 0.0f;
           m[y] = same ? D * qk[x][2 * r + y] : 0.0f;
-          sh.A[i * kPitch + j + y] = same && i > j + y ? D * kk[x][2 * r + y] : 0.0f;
+          v[y] = same && i > j + y ? D * kk[x][2 * r + y] : 0.0f;
+          w[y] = v[y] != 0.0f ? v[y] * gates.beta[j + y] : 0.0f;  // (beta of another document: anything)
         }
-        if constexpr (kBackward || sizeof(T) == 4) M.put(i, j, m[0], m[1]);
-        else Mat<C, C, 2>{M.p}.put(i, j, m[0], m[1]);
+        sh.M.put(i, j, m[0], m[1]);
+        sh.AB.put(i, j, w[0], w[1]);
+        *reinterpret_cast<float2*>(sh.A + i * kPitch + j) = make_float2(v[0], v[1]);
+        if (side + x * 8 >= i0 + 16) sh.N.put(i, j, 0.0f, 0.0f);
       }
-    }
     __syncthreads();
 
-    // N = A - A B N: 16 x 16 blocks on the diagonal column by column (rows above a column's own stay zero, whatever rows of
-    // another document hold), then for [L 0; X R]: N_X = (I - N_R B) X (I - B N_L)
+    // N = A - A B N.  16 x 16 blocks on the diagonal: a lane has a column, whose rows follow one another
     if (warp < 4 && lane < 16) {
       const int o = warp * 16;
+      float* D = sh.A + o * kPitch + o;
       float x[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float row[16];
+      for (int i = 0; i < 16; ++i) x[i] = i > lane ? D[i * kPitch + lane] : 0.0f;
 #pragma unroll
-        for (int j = 0; j < 16; j += 4) {
-          const float4 v = *reinterpret_cast<const float4*>(sh.A + (o + i) * kPitch + o + j);
-          row[j] = v.x, row[j + 1] = v.y, row[j + 2] = v.z, row[j + 3] = v.w;
-        }
-        float s = sh.A[(o + i) * kPitch + o + lane];
+      for (int j = 0; j < 15; ++j) {
+        const float bx = j > lane ? gates.beta[o + j] * x[j] : 0.0f;
 #pragma unroll
-        for (int j = 0; j < i; ++j) s = fmaf(-row[j], x[j], s);
-        s = i <= lane ? 0.0f : s;
-        sh.N[(o + i) * kPitch + o + lane] = s;
-        x[i] = i <= lane ? 0.0f : gates.beta[o + i] * s;
+        for (int i = j + 1; i < 16; ++i) x[i] = fmaf(-D[i * kPitch + j], bx, x[i]);
       }
+      __syncwarp(0xffffu);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) D[i * kPitch + lane] = i > lane ? x[i] : 0.0f;
     }
     __syncthreads();
+    auto put_n = [&](int i, int j, float x, float y) {
+      if (cuts) x = cut_between(cuts, j, i) ? 0.0f : x, y = cut_between(cuts, j + 1, i) ? 0.0f : y;
+      sh.N.put(i, j, x, y);
+    };
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int p = threadIdx.x + x * kThreads, o = p / 128 * 16, i = o + p % 128 / 8, j = o + p % 8 * 2;
+      const float2 v = *reinterpret_cast<const float2*>(sh.A + i * kPitch + j);
+      put_n(i, j, v.x, v.y);
+    }
+    __syncthreads();
+    // for [L 0; X R]: N_X = H - N_R B H with H = X - X B N_L; tiles of 16 x 8
 #pragma unroll
     for (int half = 16; half < C; half *= 2) {
-      const int groups = half / 4, count = C / (2 * half) * half * groups;  // four columns to a thread
-      const int o = (int)threadIdx.x / (half * groups) * 2 * half, r = (int)threadIdx.x / groups % half, c = (int)threadIdx.x % groups * 4;
-      const bool mine = (int)threadIdx.x < count;
-      float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      const bool mine = half == 32 || warp < 4;
+      const int o = half == 16 ? (warp >> 1 & 1) * 32 : 0;               // the block's first row
+      const int r0 = half == 16 ? 0 : (warp & 1) * 16;                   // the tile in X
+      const int c0 = half == 16 ? (warp & 1) * 8 : (warp >> 1) * 8;
+      const int h0 = half == 16 ? (warp >> 1 & 1) * 16 : 0;              // H's first row in BH
+      float H[4];
       if (mine) {
-        const float* X = sh.A + (o + half + r) * kPitch + o;
-        s = *reinterpret_cast<const float4*>(X + c);
-        for (int j = c; j < half; ++j) {
-          const float w = X[j] != 0.0f ? -X[j] * gates.beta[o + j] : 0.0f;  // (beta of another document: anything)
-          const float4 v = *reinterpret_cast<const float4*>(sh.N + (o + j) * kPitch + o + c);
-          s.x = fmaf(w, v.x, s.x), s.y = fmaf(w, v.y, s.y), s.z = fmaf(w, v.z, s.z), s.w = fmaf(w, v.w, s.w);
+        float d[4] = {}, e[4] = {}, e2[4] = {};
+#pragma unroll
+        for (int k0 = 0; k0 < half; k0 += 16) {
+          uint32_t fa[3][4], fb[3][2][2];
+          load_a<3>(sh.AB, o + half + r0, o + k0, fa);
+          load_bt<3>(sh.N, o + (c0 & ~8), o + k0, fb);
+          if (c0 & 8) mma<2>(d, e, e2, fa, fb, 1);
+          else mma<2>(d, e, e2, fa, fb, 0);
         }
-        *reinterpret_cast<float4*>(sh.H + (o / 2 + r) * kPitch + c) = s;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int i = o + half + r0 + g + 8 * r, j = o + c0 + 2 * t;
+          float bh[2];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const float v = sh.A[i * kPitch + j + y] - (d[2 * r + y] + (e[2 * r + y] + e2[2 * r + y]));
+            H[2 * r + y] = cuts && cut_between(cuts, j + y, i) ? 0.0f : v;
+            bh[y] = H[2 * r + y] != 0.0f ? gates.beta[i] * H[2 * r + y] : 0.0f;
+          }
+          sh.BH.put(h0 + r0 + g + 8 * r, c0 + 2 * t, bh[0], bh[1]);
+        }
       }
       __syncthreads();
       if (mine) {
-        const float* NR = sh.N + (o + half + r) * kPitch + o + half;
-        for (int j = 0; j < r; ++j) {
-          const float w = NR[j] != 0.0f ? -NR[j] * gates.beta[o + half + j] : 0.0f;
-          const float4 v = *reinterpret_cast<const float4*>(sh.H + (o / 2 + j) * kPitch + c);
-          s.x = fmaf(w, v.x, s.x), s.y = fmaf(w, v.y, s.y), s.z = fmaf(w, v.z, s.z), s.w = fmaf(w, v.w, s.w);
+        float d[4] = {}, e[4] = {}, e2[4] = {};
+#pragma unroll
+        for (int k0 = 0; k0 < half; k0 += 16) {
+          uint32_t fa[3][4], fb[3][2][2];
+          load_a<3>(sh.N, o + half + r0, o + half + k0, fa);
+          load_bt<3>(sh.BH, c0 & ~8, h0 + k0, fb);
+          if (c0 & 8) mma<2>(d, e, e2, fa, fb, 1);
+          else mma<2>(d, e, e2, fa, fb, 0);
         }
-        *reinterpret_cast<float4*>(sh.N + (o + half + r) * kPitch + o + c) = s;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+          put_n(o + half + r0 + g + 8 * r, o + c0 + 2 * t, H[2 * r] - (d[2 * r] + (e[2 * r] + e2[2 * r])),
+                H[2 * r + 1] - (d[2 * r + 1] + (e[2 * r + 1] + e2[2 * r + 1])));
       }
       __syncthreads();
     }
-#pragma unroll 4
-    for (int x = threadIdx.x; x < C * C / 2; x += kThreads) {
-      const int i = x / (C / 2), j = x % (C / 2) * 2;
-      if (j / 16 > i / 16) continue;
-      const float2 v = *reinterpret_cast<const float2*>(sh.N + i * kPitch + j);
-      N.put(i, j, i > j && !cut_between(cuts, j, i) ? v.x : 0.0f, i > j + 1 && !cut_between(cuts, j + 1, i) ? v.y : 0.0f);
+    fence_proxy_async_shared();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      unsigned char* head = a.heads + ((size_t)((long long)n * a.B + b) * a.H + h) * kHeadBytes;
+      bulk_copy_s2g(head, smem_u32(sh.N.p), SquareMat::kBytes);
+      bulk_copy_s2g(head + SquareMat::kBytes, smem_u32(sh.gates), Sh::kTail);
     }
-    if (threadIdx.x < sizeof(Gates) / 16)
-      reinterpret_cast<uint4*>(M.p + 3 * M.kSize)[threadIdx.x] = reinterpret_cast<const uint4*>(&gates)[threadIdx.x];
   }
+  if (threadIdx.x == 0) bulk_wait_all();
 }
 
 // ---- along the chunks -------------------------------------------------------------
 
-// What a chunk brings along.
+// What a chunk brings along: parts of K and Q, N, gates, M.  The blocks of a cluster have the same head: each asks for its share
+// and sends it to all (from L2, 16 heads of 8 blocks would otherwise take 73 KB to a block and chunk: 3400 cycles).
 template <typename T, int KD, int kMParts>
 struct Stage {
   KeyMat<T, KD> K, Q;
   SquareMat N;
-  Mat<C, C, kMParts> M;
   Gates* gates;
-  static constexpr size_t kBytes = kKeysBytes<T, KD> + SquareMat::kBytes + Mat<C, C, kMParts>::kBytes + sizeof(Gates);
+  Mat<C, C, kMParts> M;
+  static constexpr uint32_t kKeys = (uint32_t)kKeysBytes<T, KD>, kHead = SquareMat::kBytes + sizeof(Gates) + Mat<C, C, kMParts>::kBytes;
+  static constexpr size_t kBytes = kKeys + kHead;
   __device__ __forceinline__ explicit Stage(unsigned char* p)
-      : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * kParts<T>}, N{Q.p + Q.kSize * kParts<T>}, M{N.p + N.kSize * 3},
-        gates(reinterpret_cast<Gates*>(M.p + M.kSize * kMParts)) {}
-  __device__ __forceinline__ void load(const DeltaArgs& a, int n, int b, int h) const {
+      : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * kParts<T>}, N{Q.p + Q.kSize * kParts<T>},
+        gates(reinterpret_cast<Gates*>(N.p + N.kSize * 3)), M{reinterpret_cast<bf16*>(gates + 1)} {}
+  __device__ __forceinline__ static void share(uint32_t to, const unsigned char* from, uint32_t bytes, int cluster, uint32_t rank, uint32_t bar) {
+    const uint32_t per = (bytes / 16 + cluster - 1) / cluster * 16, at = rank * per;
+    if (at >= bytes) return;
+    const uint32_t mine = min(per, bytes - at);
+    if (cluster == 1) bulk_copy_g2s(to + at, from + at, mine, bar);
+    else bulk_copy_g2cluster(to + at, from + at, mine, bar, (uint16_t)((1u << cluster) - 1u));
+  }
+  // One thread of every block of the cluster; no block reads its stage any more.
+  __device__ __forceinline__ void load(const DeltaArgs& a, int n, int b, int h, uint32_t rank, uint32_t bar) const {
     const size_t at = (size_t)n * a.B + b;
-    fetch<(int)kKeysBytes<T, KD>>(K.p, a.keys + (at * (a.H / a.share) + h / a.share) * kKeysBytes<T, KD>);
-    const unsigned char* head = a.heads + (at * a.H + h) * kHeadBytes;
-    const bf16* from = reinterpret_cast<const bf16*>(head);
-    fetch_lower<3>(N.p, from);
-    fetch_lower<kMParts>(M.p, from + SquareMat::kSize * 3);
-    fetch<(int)sizeof(Gates)>(gates, head + 2 * SquareMat::kBytes);
+    mbar_arrive_expect_tx(bar, kKeys + kHead);
+    share(smem_u32(K.p), a.keys + (at * (a.H / a.share) + h / a.share) * kKeysBytes<T, KD>, kKeys, a.cluster, rank, bar);
+    share(smem_u32(N.p), a.heads + (at * a.H + h) * kHeadBytes, kHead, a.cluster, rank, bar);
   }
 };
 // Chunks in shared memory at a time: two, or one where the parts of wide keys fill it.
@@ -588,86 +648,70 @@ struct StatePart {
   __device__ __forceinline__ void split(const Mat<KD, NV, 3>& to) {
     each([&](int r, int c, float& x, float& y) { to.put(r, c, x, y); });
   }
-  // += keys^T rows (kP parts of keys)
-  template <int kP, int kHas>
-  __device__ __forceinline__ void add(float (&e)[kTiles][4], const Mat<C, KD, kHas>& keys, const Mat<C, NV, 3>& rows) {
+};
+
+// d + e += rows m0 of A (kLength columns from k0 on) times columns n0.. of B: kTiles times 8 columns, PA and PB parts.  The
+// operands of a step are asked for before the MMAs of the one before.
+template <int PA, int PB, int kTiles, bool kTransA>
+struct Operands {
+  static constexpr int kDepthOf = kTiles == 1 ? 32 : 16;  // rows of k to a step
+  uint32_t a[kDepthOf / 16][PA][4], b[kTiles == 1 ? 1 : kTiles / 2][PB][2][2];
+  template <typename MatA, typename MatB>
+  __device__ __forceinline__ void load(const MatA& A, int m0, const MatB& B, int n0, int k0) {
 #pragma unroll
-    for (int k0 = 0; k0 < C; k0 += 16) {
-      uint32_t fa[kP][4];
-      load_at<kP>(keys, row0(), k0, fa);
-      if constexpr (kTiles == 1) {
-        uint32_t fb[3][2][2];
-        load_bt<3>(rows, col0() & ~8, k0, fb);
-        if (col0() & 8) mma<2>(x[0], e[0], fa, fb, 1);
-        else mma<2>(x[0], e[0], fa, fb, 0);
-      } else {
+    for (int s = 0; s < kDepthOf / 16; ++s) {
+      if constexpr (kTransA) load_at<PA>(A, m0, k0 + 16 * s, a[s]);
+      else load_a<PA>(A, m0, k0 + 16 * s, a[s]);
+    }
+    if constexpr (kTiles == 1) {
+      load_bt_tall<PB>(B, n0, k0, b[0]);
+    } else {
 #pragma unroll
-        for (int n = 0; n < kTiles; n += 2) {
-          uint32_t fb[3][2][2];
-          load_bt<3>(rows, col0() + n * 8, k0, fb);
-          mma<2>(x[n], e[n], fa, fb, 0);
-          mma<2>(x[n + 1], e[n + 1], fa, fb, 1);
-        }
-      }
+      for (int n = 0; n < kTiles / 2; ++n) load_bt<PB>(B, n0 + 16 * n, k0, b[n]);
+    }
+  }
+  template <int kDepth>
+  __device__ __forceinline__ void multiply(float (&d)[kTiles][4], float (&e)[kTiles][4], float (&f)[4]) {
+    if constexpr (kTiles == 1) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) mma<kDepth>(d[0], e[0], f, a[s], b[0], s);
+    } else {
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n) mma<kDepth>(d[n], e[n], a[0], b[n / 2], n & 1);
     }
   }
 };
-
-// d + e += rows m0 of A (kLength columns from k0 on) times columns n0.. of B: kTiles times 8 columns, PA and PB parts.
 template <int kDepth, int PA, int PB, int kTiles, int kLength, bool kTransA, typename MatA, typename MatB>
 __device__ __forceinline__ void product(float (&d)[kTiles][4], float (&e)[kTiles][4], const MatA& A, int m0, const MatB& B, int n0, int k0) {
-  if constexpr (kTiles == 1) {
+  using Ops = Operands<PA, PB, kTiles, kTransA>;
+  constexpr int kSteps = kLength / Ops::kDepthOf;
+  Ops ops[2];
+  float f[4] = {};  // (a third chain of sums where there is one tile)
+  ops[0].load(A, m0, B, n0, k0);
 #pragma unroll
-    for (int k = 0; k < kLength; k += 32) {
-      uint32_t fb[PB][2][2];
-      load_bt_tall<PB>(B, n0, k0 + k, fb);
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        uint32_t fa[PA][4];
-        if constexpr (kTransA) load_at<PA>(A, m0, k0 + k + 16 * s, fa);
-        else load_a<PA>(A, m0, k0 + k + 16 * s, fa);
-        mma<kDepth>(d[0], e[0], fa, fb, s);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < kLength; k += 16) {
-      uint32_t fa[PA][4];
-      if constexpr (kTransA) load_at<PA>(A, m0, k0 + k, fa);
-      else load_a<PA>(A, m0, k0 + k, fa);
-#pragma unroll
-      for (int n = 0; n < kTiles; n += 2) {
-        uint32_t fb[PB][2][2];
-        load_bt<PB>(B, n0 + n * 8, k0 + k, fb);
-        mma<kDepth>(d[n], e[n], fa, fb, 0);
-        mma<kDepth>(d[n + 1], e[n + 1], fa, fb, 1);
-      }
-    }
+  for (int k = 0; k < kSteps; ++k) {
+    if (k + 1 < kSteps) ops[(k + 1) & 1].load(A, m0, B, n0, k0 + (k + 1) * Ops::kDepthOf);
+    ops[k & 1].template multiply<kDepth>(d, e, f);
   }
+  if constexpr (kTiles == 1)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) e[0][r] += f[r];
 }
-// The same for a square matrix of which only columns [k0, k1) are not zero (multiples of 16).
+// S += keys^T rows (P parts of the keys).
+template <int P, int KD, int NV, int kHas>
+__device__ __forceinline__ void add_keys(StatePart<KD, NV>& s, const Mat<C, KD, kHas>& keys, const Mat<C, NV, 3>& rows) {
+  float e[StatePart<KD, NV>::kTiles][4] = {};
+  product<2, P, 3, StatePart<KD, NV>::kTiles, C, true>(s.x, e, keys, s.row0(), rows, s.col0(), 0);
+#pragma unroll
+  for (int c = 0; c < s.kTiles; ++c)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s.x[c][r] += e[c][r];
+}
+// The same for a matrix [64][64] that is zero above the diagonal.
 template <int kDepth, int PA, int PB, int kTiles, bool kTransA, typename MatA, typename MatB>
-__device__ __forceinline__ void product_part(float (&d)[kTiles][4], float (&e)[kTiles][4], const MatA& A, int m0, const MatB& B, int n0,
-                                             int k0, int k1) {
-#pragma unroll
-  for (int k = 0; k < C; k += 16) {
-    if (k < k0 || k >= k1) continue;
-    uint32_t fa[PA][4];
-    if constexpr (kTransA) load_at<PA>(A, m0, k, fa);
-    else load_a<PA>(A, m0, k, fa);
-#pragma unroll
-    for (int n = 0; n < kTiles; n += 2) {
-      uint32_t fb[PB][2][2];
-      load_bt<PB>(B, kTiles == 1 ? n0 & ~8 : n0 + n * 8, k, fb);
-      if constexpr (kTiles == 1) {
-        if (n0 & 8) mma<kDepth>(d[0], e[0], fa, fb, 1);
-        else mma<kDepth>(d[0], e[0], fa, fb, 0);
-      } else {
-        mma<kDepth>(d[n], e[n], fa, fb, 0);
-        mma<kDepth>(d[n + 1], e[n + 1], fa, fb, 1);
-      }
-    }
-  }
+__device__ __forceinline__ void product_lower(float (&d)[kTiles][4], float (&e)[kTiles][4], const MatA& A, int m0, const MatB& B, int n0) {
+  if (kTransA ? m0 >= C / 2 : m0 < C / 2) product<kDepth, PA, PB, kTiles, C / 2, kTransA>(d, e, A, m0, B, n0, kTransA ? C / 2 : 0);
+  else product<kDepth, PA, PB, kTiles, C, kTransA>(d, e, A, m0, B, n0, 0);
 }
 
 template <typename T, int KD, int NV>
@@ -677,9 +721,11 @@ struct ForwardShared {
   Mat<KD, NV, 3> S;
   Mat<C, NV, 3> X, Ud;
   Mat<C, NV, kOut> U;
-  static constexpr size_t kBytes = kStages<T, KD> * St::kBytes + decltype(S)::kBytes + 2 * decltype(X)::kBytes + decltype(U)::kBytes;
+  uint64_t* bars;  // [2]
+  static constexpr size_t kBytes = kStages<T, KD> * St::kBytes + decltype(S)::kBytes + 2 * decltype(X)::kBytes + decltype(U)::kBytes + 16;
   __device__ __forceinline__ explicit ForwardShared(unsigned char* p)
-      : S{reinterpret_cast<bf16*>(p + kStages<T, KD> * St::kBytes)}, X{S.p + S.kSize * 3}, Ud{X.p + X.kSize * 3}, U{Ud.p + Ud.kSize * 3} {}
+      : S{reinterpret_cast<bf16*>(p + kStages<T, KD> * St::kBytes)}, X{S.p + S.kSize * 3}, Ud{X.p + X.kSize * 3}, U{Ud.p + Ud.kSize * 3},
+        bars(reinterpret_cast<uint64_t*>(U.p + U.kSize * kOut)) {}
 };
 
 template <typename T, int KD, int NV>
@@ -703,35 +749,43 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const DeltaA
   StatePart<KD, NV> s;
   s.load(a.h0 ? a.h0 + (long long)bh * DD : nullptr, a, v0);
   s.split(sh.S);
-  float2 vx[kTiles][2];
+  Raw2<T> vx[kTiles][2];
   auto fetch_v = [&](int n) {
 #pragma unroll
     for (int x = 0; x < kTiles; ++x)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int time = n * C + rb + g + 8 * r;
-        vx[x][r] = time < len ? get2(v + time * a.vs.t, v0 + cb + x * 8 + 2 * t, a.Dv, a.pairs) : make_float2(0.0f, 0.0f);
+        vx[x][r] = raw2(v + time * a.vs.t, v0 + cb + x * 8 + 2 * t, a.Dv, a.pairs, time < len);
       }
   };
-  if (chunks > 0) {
-    St(smem).load(a, 0, b, h);
-    fetch_v(0);
+  const uint32_t rank = cluster_ctarank(), bar = smem_u32(sh.bars);
+  const bool asks = threadIdx.x == 7 * 32;
+  if (asks) {
+    mbar_init(bar, 1);
+    mbar_init(bar + 8, 1);
+    fence_mbarrier_init_cluster();
   }
-  copies_commit();
+  if (chunks > 0) fetch_v(0);
+  cluster_sync_all();  // barriers and buffers of all blocks are ready
+  if (asks && chunks > 0) St(smem).load(a, 0, b, h, rank, bar);
 
   for (int n = 0; n < chunks; ++n) {
-    copies_wait<0>();
+    const bool came = mbar_wait_bounded<true>(bar + (n & kTwo) * 8, (uint32_t)(n >> kTwo) & 1u, kWaitNs, &g_never);
     __syncthreads();
     const St now(smem + (n & kTwo) * St::kBytes);
     const Gates& gate = *now.gates;
     float2 vn[kTiles][2];
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x) vn[x][0] = vx[x][0], vn[x][1] = vx[x][1];
+    for (int x = 0; x < kTiles; ++x) vn[x][0] = Pair<T>::get(vx[x][0]), vn[x][1] = Pair<T>::get(vx[x][1]);
+    if (!came) vn[0][0].x = __int_as_float(0x7fffffff);
     if (n + 1 < chunks) {
-      if constexpr (kTwo) St(smem + (~n & 1) * St::kBytes).load(a, n + 1, b, h);
+      if (kTwo && warp == 7) {  // (the others wait for the cluster at the chunk's end, where nothing is left to wait for)
+        if (n > 0) cluster_wait();
+        if (asks) St(smem + (~n & 1) * St::kBytes).load(a, n + 1, b, h, rank, bar + (~n & 1) * 8);
+      }
       fetch_v(n + 1);
     }
-    copies_commit();
     if (a.states) s.store(a.states + (((long long)n * a.B + b) * a.H + h) * DD, a, v0);
     const unsigned long long cuts = gate.cuts;
 
@@ -769,7 +823,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const DeltaA
       __syncthreads();
       {
         float d[kTiles][4] = {}, e[kTiles][4] = {};
-        product_part<2, 3, 3, kTiles, false>(d, e, now.N, rb, sh.X, cb, 0, rb + 16);
+        product_lower<2, 3, 3, kTiles, false>(d, e, now.N, rb, sh.X, cb);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int i = rb + g + 8 * r;
@@ -790,20 +844,15 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const DeltaA
           for (int q = 0; q < P; ++q) now.K.p[q * now.K.kSize + i] = from_f32<bf16>(0.0f);
       __syncthreads();
       if (hi == C) {
-        float e[s.kTiles][4] = {};
         const float keep = gate.gam[C - 1];
         s.each([&](int, int, float& p, float& q) { p = cuts ? 0.0f : keep * p, q = cuts ? 0.0f : keep * q; });
-        s.template add<P>(e, now.K, sh.Ud);
-#pragma unroll
-        for (int c = 0; c < s.kTiles; ++c)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) s.x[c][r] += e[c][r];
+        add_keys<P>(s, now.K, sh.Ud);
         s.split(sh.S);
       }
       __syncwarp();
       {
         float e[kTiles][4] = {};
-        product_part<kDepth, kOut, kOut, kTiles, false>(oq, e, now.M, rb, sh.U, cb, 0, rb + 16);
+        product_lower<kDepth, kOut, kOut, kTiles, false>(oq, e, now.M, rb, sh.U, cb);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int i = rb + g + 8 * r, time = n * C + i;
@@ -817,12 +866,17 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const DeltaA
       lo = hi;
       if (lo < C) __syncthreads();
     }
-    if constexpr (!kTwo) {
-      __syncthreads();
-      if (n + 1 < chunks) St(smem).load(a, n + 1, b, h);
-      copies_commit();
+    if (cuts) fence_proxy_async_shared();  // rows zeroed above, before a copy overwrites them
+    if constexpr (kTwo) {
+      if (n > 0 && (warp != 7 || n + 1 == chunks)) cluster_wait();
+      cluster_arrive();
+    } else {
+      cluster_sync_all();
+      if (asks && n + 1 < chunks) St(smem).load(a, n + 1, b, h, rank, bar);
     }
   }
+  if (kTwo && chunks > 0) cluster_wait();
+  if (v0 >= a.Dv) return;
   s.store(a.h_last + (long long)bh * DD, a, v0);
   for (long long i = (long long)len * NV + threadIdx.x; i < (long long)a.T * NV; i += kThreads) {
     const int c = v0 + (int)(i % NV);
@@ -836,11 +890,12 @@ struct BackwardShared {
   Mat<KD, NV, 3> S;                // dS
   Mat<C, NV, 3> Od, Z;             // scale gam dO; B dU, then - gam B R
   Mat<C, NV, kParts<T>> O;         // dO
+  uint64_t* bars;                  // [2]
   float* sums;                     // [8]
-  static constexpr size_t kBytes = kStages<T, KD> * St::kBytes + decltype(S)::kBytes + 2 * decltype(Z)::kBytes + decltype(O)::kBytes + 32;
+  static constexpr size_t kBytes = kStages<T, KD> * St::kBytes + decltype(S)::kBytes + 2 * decltype(Z)::kBytes + decltype(O)::kBytes + 48;
   __device__ __forceinline__ explicit BackwardShared(unsigned char* p)
       : S{reinterpret_cast<bf16*>(p + kStages<T, KD> * St::kBytes)}, Od{S.p + S.kSize * 3}, Z{Od.p + Od.kSize * 3}, O{Z.p + Z.kSize * 3},
-        sums(reinterpret_cast<float*>(O.p + O.kSize * kParts<T>)) {}
+        bars(reinterpret_cast<uint64_t*>(O.p + O.kSize * kParts<T>)), sums(reinterpret_cast<float*>(bars + 2)) {}
 };
 
 // dS before a chunk from dS behind it; keeps the latter, R and <dS0, S0> for the gradients of the rest, and writes dV.
@@ -863,36 +918,45 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const Delta
   StatePart<KD, NV> s, before;
   s.load(a.dh_last ? a.dh_last + (long long)bh * DD : nullptr, a, v0);
   s.split(sh.S);
-  float2 ox[kTiles][2];
+  Raw2<T> ox[kTiles][2];
   auto fetch_o = [&](int n) {
 #pragma unroll
     for (int x = 0; x < kTiles; ++x)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int time = n * C + rb + g + 8 * r;
-        ox[x][r] = time < len ? get2(d_o + time * a.dos.t, v0 + cb + x * 8 + 2 * t, a.Dv, a.pairs) : make_float2(0.0f, 0.0f);
+        ox[x][r] = raw2(d_o + time * a.dos.t, v0 + cb + x * 8 + 2 * t, a.Dv, a.pairs, time < len);
       }
   };
-  if (chunks > 0) {
-    St(smem + ((chunks - 1) & kTwo) * St::kBytes).load(a, chunks - 1, b, h);
-    fetch_o(chunks - 1);
+  const uint32_t rank = cluster_ctarank(), bar = smem_u32(sh.bars);
+  const bool asks = threadIdx.x == 7 * 32;
+  if (asks) {
+    mbar_init(bar, 1);
+    mbar_init(bar + 8, 1);
+    fence_mbarrier_init_cluster();
   }
-  copies_commit();
+  if (chunks > 0) fetch_o(chunks - 1);
+  cluster_sync_all();
+  if (asks && chunks > 0) St(smem).load(a, chunks - 1, b, h, rank, bar);
 
   for (int n = chunks - 1; n >= 0; --n) {
-    copies_wait<0>();
+    const int turn = chunks - 1 - n;
+    const bool came = mbar_wait_bounded<true>(bar + (turn & kTwo) * 8, (uint32_t)(turn >> kTwo) & 1u, kWaitNs, &g_never);
     __syncthreads();
-    const St now(smem + (n & kTwo) * St::kBytes);
+    const St now(smem + (turn & kTwo) * St::kBytes);
     const Gates& gate = *now.gates;
     const long long chunk = ((long long)n * a.B + b) * a.H + h;
     float2 on[kTiles][2];
 #pragma unroll
-    for (int x = 0; x < kTiles; ++x) on[x][0] = ox[x][0], on[x][1] = ox[x][1];
+    for (int x = 0; x < kTiles; ++x) on[x][0] = Pair<T>::get(ox[x][0]), on[x][1] = Pair<T>::get(ox[x][1]);
+    if (!came) on[0][0].x = __int_as_float(0x7fffffff);
     if (n > 0) {
-      if constexpr (kTwo) St(smem + (~n & 1) * St::kBytes).load(a, n - 1, b, h);
+      if (kTwo && warp == 7) {
+        if (turn > 0) cluster_wait();
+        if (asks) St(smem + (~turn & 1) * St::kBytes).load(a, n - 1, b, h, rank, bar + (~turn & 1) * 8);
+      }
       fetch_o(n - 1);
     }
-    copies_commit();
     s.store(a.dS + chunk * DD, a, v0);
     before.load(a.states + chunk * DD, a, v0);
     const unsigned long long cuts = gate.cuts;
@@ -925,7 +989,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const Delta
             du[c][r] = hi == C ? gate.dec[rb + g + 8 * (r >> 1)] * (d[c][r] + e[c][r]) : 0.0f;
             d[c][r] = e[c][r] = 0.0f;
           }
-        product_part<2, 3, P, kTiles, true>(d, e, now.M, rb, sh.O, cb, rb, C);
+        product_lower<2, 3, P, kTiles, true>(d, e, now.M, rb, sh.O, cb);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int i = rb + g + 8 * r;
@@ -942,7 +1006,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const Delta
       __syncthreads();
       {  // R = dU - N^T B dU, dV = B R
         float d[kTiles][4] = {}, e[kTiles][4] = {};
-        product_part<2, 3, 3, kTiles, true>(d, e, now.N, rb, sh.Z, cb, rb, C);
+        product_lower<2, 3, 3, kTiles, true>(d, e, now.N, rb, sh.Z, cb);
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -968,17 +1032,12 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const Delta
           for (int q = 0; q < P; ++q) now.K.p[q * now.K.kSize + i] = now.Q.p[q * now.Q.kSize + i] = from_f32<bf16>(0.0f);
       __syncthreads();
       if (lo == 0) {  // dS = gam_63 dS + Q^T scale gam dO - K^T gam dV
-        float e[s.kTiles][4] = {};
         const float keep = gate.gam[C - 1];
         s.each([&](int, int, float& p, float& q) { p = cuts ? 0.0f : keep * p, q = cuts ? 0.0f : keep * q; });
         if (!(cuts & 1ull)) {
-          s.template add<P>(e, now.Q, sh.Od);
-          s.template add<P>(e, now.K, sh.Z);
+          add_keys<P>(s, now.Q, sh.Od);
+          add_keys<P>(s, now.K, sh.Z);
         }
-#pragma unroll
-        for (int c = 0; c < s.kTiles; ++c)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) s.x[c][r] += e[c][r];
         s.split(sh.S);
         float dot = 0.0f;
 #pragma unroll
@@ -999,11 +1058,17 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const Delta
       for (int w = 0; w < 8; ++w) dot += sh.sums[w];
       a.dots[chunk * a.tiles + blockIdx.x % a.tiles] = dot;
     }
-    if constexpr (!kTwo) {
-      if (n > 0) St(smem).load(a, n - 1, b, h);
-      copies_commit();
+    if (cuts) fence_proxy_async_shared();
+    if constexpr (kTwo) {
+      if (turn > 0 && (warp != 7 || n == 0)) cluster_wait();
+      cluster_arrive();
+    } else {
+      cluster_sync_all();
+      if (asks && n > 0) St(smem).load(a, n - 1, b, h, rank, bar);
     }
   }
+  if (kTwo && chunks > 0) cluster_wait();
+  if (v0 >= a.Dv) return;
   s.store(a.dh0 + (long long)bh * DD, a, v0);
   for (long long i = (long long)len * NV + threadIdx.x; i < (long long)a.T * NV; i += kThreads) {
     const int c = v0 + (int)(i % NV);
@@ -1016,6 +1081,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const Delta
 // Columns of S to a round: fewer where the parts of 32-bit keys fill the shared memory.
 template <typename T, int KD>
 constexpr int kSlice = sizeof(T) == 4 && KD == 128 ? 16 : 32;
+constexpr int kGradThreads = 512;
 
 template <typename T, int KD>
 struct GradShared {
@@ -1023,7 +1089,8 @@ struct GradShared {
   KeyMat<T, KD> K, Q;
   SquareMat N;
   Gates* gates;
-  float* sums;  // [3][2][C]
+  float* sums;  // [3][4][C]
+  float *next_S, *next_dS;  // the next round's, as they come
   // one round's: S0, dS, dO, R, B X, U; after the last, P and E
   Mat<KD, W, 3> S;
   Mat<KD, W, kOut> dS;
@@ -1032,23 +1099,43 @@ struct GradShared {
   Mat<C, W, 3> X, U;
   SquareMat Pm;
   Mat<C, C, kOut> E;
-  static constexpr size_t kFixed = kKeysBytes<T, KD> + SquareMat::kBytes + sizeof(Gates) + 6 * C * 4;
+  static constexpr size_t kFixed = kKeysBytes<T, KD> + SquareMat::kBytes + sizeof(Gates) + 12 * C * 4 + 2 * KD * W * 4;
   static constexpr size_t kRound = decltype(S)::kBytes + decltype(dS)::kBytes + decltype(dO)::kBytes + decltype(R)::kBytes + 2 * decltype(X)::kBytes;
   static constexpr size_t kAfter = decltype(Pm)::kBytes + decltype(E)::kBytes;
   static constexpr size_t kBytes = kFixed + (kRound > kAfter ? kRound : kAfter);
   __device__ __forceinline__ explicit GradShared(unsigned char* p)
       : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * P}, N{Q.p + Q.kSize * P}, gates(reinterpret_cast<Gates*>(N.p + N.kSize * 3)),
-        sums(reinterpret_cast<float*>(gates + 1)), S{reinterpret_cast<bf16*>(sums + 6 * C)}, dS{S.p + S.kSize * 3},
-        dO{dS.p + dS.kSize * kOut}, R{dO.p + dO.kSize * P}, X{R.p + R.kSize * kOut}, U{X.p + X.kSize * 3}, Pm{S.p}, E{Pm.p + Pm.kSize * 3} {}
+        sums(reinterpret_cast<float*>(gates + 1)), next_S(sums + 12 * C), next_dS(next_S + KD * W),
+        S{reinterpret_cast<bf16*>(next_dS + KD * W)}, dS{S.p + S.kSize * 3}, dO{dS.p + dS.kSize * kOut}, R{dO.p + dO.kSize * P},
+        X{R.p + R.kSize * kOut}, U{X.p + X.kSize * 3}, Pm{S.p}, E{Pm.p + Pm.kSize * 3} {}
 };
+
+// [rows][W] values of a matrix [Dk][Dv] from column v0 on, as they come (zeros past its ends); `quads`: in 16-byte pieces.
+template <int KD, int W>
+__device__ __forceinline__ void fetch_slice(float* to, const float* from, int v0, int Dk, int Dv, bool quads) {
+  if (quads) {
+#pragma unroll
+    for (int i = threadIdx.x; i < KD * W / 4; i += kGradThreads) {
+      const int r = i / (W / 4), c = i % (W / 4) * 4;
+      const bool in = r < Dk && v0 + c < Dv;
+      copy16(to + i * 4, in ? from + (long long)r * Dv + v0 + c : from, in ? 16 : 0);
+    }
+  } else {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < KD * W; i += kGradThreads) {
+      const int r = i / W, c = i % W;
+      const bool in = r < Dk && v0 + c < Dv;
+      copy4(to + i, in ? from + (long long)r * Dv + v0 + c : from, in ? 4 : 0);
+    }
+  }
+}
 
 // acc += rows m0 of A (parts PA) times the transposed rows n0.. of B, over kLength columns; two tiles of 8 rows of B at a time,
 // summed apart first (an MMA's sum is cut, not rounded, to 24 bits).
 template <int kDepth, int PB, int kTiles, int kLength, int PA, typename MatB>
-__device__ __forceinline__ void add_rows(float (&acc)[kTiles][4], const uint32_t (&fa)[kLength / 16][PA][4], const MatB& B, int n0, int first) {
+__device__ __forceinline__ void add_rows(float (&acc)[kTiles][4], const uint32_t (&fa)[kLength / 16][PA][4], const MatB& B, int n0) {
 #pragma unroll
   for (int n = 0; n < kTiles; n += 2) {
-    if (n0 + n * 8 >= first) continue;
     float d[2][4] = {}, e[2][4] = {};
 #pragma unroll
     for (int k = 0; k < kLength / 16; ++k) {
@@ -1065,11 +1152,10 @@ __device__ __forceinline__ void add_rows(float (&acc)[kTiles][4], const uint32_t
 }
 
 template <typename T, int KD>
-__global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const DeltaArgs a) {
+__global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr int W = kSlice<T, KD>, P = kParts<T>, kOut = kOutParts<T>, kDepth = kOutDepth<T>;
-  constexpr int kHalf = KD / 2, kTiles = kHalf / 8;  // a warp has 16 rows and half of the columns
-  constexpr int kXTiles = W / 16;
+  constexpr int kPart = KD / 4, kTiles = kPart / 8;  // a warp has 16 rows and a quarter of the columns
   const GradShared<T, KD> sh(smem);
   const Gates& gate = *sh.gates;
   begin_op();
@@ -1077,14 +1163,14 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
   const int hk = (int)(blockIdx.x % Hk), b = (int)(blockIdx.x / Hk % a.B), n = (int)(blockIdx.x / Hk / a.B);
   const int len = length_of(a, b), t0 = n * C, rows = min(len - t0, C), all = min(a.T - t0, C);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane_g(), t = lane_t();
-  const int rb = (warp < 4 ? warp : 7 - warp) * 16, side = warp >> 2;
+  const int side = warp >> 2, rb = (side & 1 ? 3 - (warp & 3) : warp & 3) * 16;  // (long rows of triangles beside short ones)
   T* dq = static_cast<T*>(a.dq) + t0 * a.dqs.t + b * a.dqs.b + hk * a.dqs.h;
   T* dk = static_cast<T*>(a.dk) + t0 * a.dks.t + b * a.dks.b + hk * a.dks.h;
-  for (int i = threadIdx.x + max(rows, 0) * a.Dk; i < all * a.Dk; i += kThreads) {  // past the stream's length
+  for (int i = threadIdx.x + max(rows, 0) * a.Dk; i < all * a.Dk; i += kGradThreads) {  // past the stream's length
     dq[i / a.Dk * a.dqs.t + i % a.Dk] = from_f32<T>(0.0f);
     dk[i / a.Dk * a.dks.t + i % a.Dk] = from_f32<T>(0.0f);
   }
-  for (int i = threadIdx.x + max(rows, 0) * a.share; i < all * a.share; i += kThreads) {
+  for (int i = threadIdx.x + max(rows, 0) * a.share; i < all * a.share; i += kGradThreads) {
     const long long row = t0 + i / a.share;
     const int h = hk * a.share + i % a.share;
     a.dg[row * a.dgt + b * a.dgb + h] = 0.0f;
@@ -1093,6 +1179,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
   if (rows <= 0) return;
   const long long DD = (long long)a.Dk * a.Dv;
   const size_t where = ((size_t)n * a.B + b) * Hk + hk;
+  const float2 zero = make_float2(0.0f, 0.0f);
 
   for (int h = hk * a.share; h < (hk + 1) * a.share; ++h) {
     const long long chunk = ((long long)n * a.B + b) * a.H + h;
@@ -1101,8 +1188,10 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
     const float *S = a.states + chunk * DD, *dS = a.dS + chunk * DD, *R = a.R + chunk * C * a.Dv;
     const unsigned char* head = a.heads + (size_t)chunk * kHeadBytes;
     __syncthreads();
-    fetch_lower<3>(sh.N.p, reinterpret_cast<const bf16*>(head));
-    fetch<(int)sizeof(Gates)>(sh.gates, head + 2 * SquareMat::kBytes);
+    fetch<(int)(SquareMat::kBytes + sizeof(Gates)), kGradThreads>(sh.N.p, head);
+    if (h == hk * a.share) fetch<(int)kKeysBytes<T, KD>, kGradThreads>(sh.K.p, a.keys + where * kKeysBytes<T, KD>);
+    fetch_slice<KD, W>(sh.next_S, S, 0, a.Dk, a.Dv, a.quads);
+    fetch_slice<KD, W>(sh.next_dS, dS, 0, a.Dk, a.Dv, a.quads);
     copies_commit();
     copies_wait<0>();
     __syncthreads();
@@ -1111,107 +1200,115 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
     for (int lo = 0; lo < rows;) {
       const int hi = min(piece_end(cuts, lo), rows);
       const bool fresh = cut_before(cuts, lo), last = hi == rows;  // the state before counts as zero; the one behind goes on
-      __syncthreads();
-      if (h == hk * a.share || cuts) {
-        fetch<(int)kKeysBytes<T, KD>>(sh.K.p, a.keys + where * kKeysBytes<T, KD>);
+      if (cuts) {  // this piece's keys and the first slices anew
+        __syncthreads();
+        fetch<(int)kKeysBytes<T, KD>, kGradThreads>(sh.K.p, a.keys + where * kKeysBytes<T, KD>);
+        fetch_slice<KD, W>(sh.next_S, S, 0, a.Dk, a.Dv, a.quads);
+        fetch_slice<KD, W>(sh.next_dS, dS, 0, a.Dk, a.Dv, a.quads);
         copies_commit();
         copies_wait<0>();
-        if (cuts) {
-          __syncthreads();
-          for (int i = threadIdx.x; i < C * KD; i += kThreads)
-            if (i / KD < lo || i / KD >= hi)
+        __syncthreads();
+        for (int i = threadIdx.x; i < C * KD; i += kGradThreads)
+          if (i / KD < lo || i / KD >= hi)
 #pragma unroll
-              for (int q = 0; q < P; ++q) sh.K.p[q * sh.K.kSize + i] = sh.Q.p[q * sh.Q.kSize + i] = from_f32<bf16>(0.0f);
-        }
+            for (int q = 0; q < P; ++q) sh.K.p[q * sh.K.kSize + i] = sh.Q.p[q * sh.Q.kSize + i] = from_f32<bf16>(0.0f);
       }
       float acc_q[kTiles][4] = {}, acc_w[kTiles][4] = {}, acc_t[kTiles][4] = {};  // dO S0^T, R S0^T, U dS^T
-      float acc_p[4][4] = {}, acc_e[4][4] = {};                                  // dO U^T, R U^T
+      float acc_p[2][4] = {}, acc_e[2][4] = {};                                  // dO U^T, R U^T
       float rv[2] = {}, ry[2] = {};                                              // R . V, R . Y
-
-      for (int v0 = 0; v0 < a.Dv; v0 += W) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < KD * W / 2; i += kThreads) {
-          const int r = i / (W / 2), c = i % (W / 2) * 2;
-          const float2 zero = make_float2(0.0f, 0.0f);
-          const float2 x = r < a.Dk && !fresh ? get2(S + (long long)r * a.Dv, v0 + c, a.Dv, a.even) : zero;
-          const float2 y = r < a.Dk && last ? get2(dS + (long long)r * a.Dv, v0 + c, a.Dv, a.even) : zero;
-          sh.S.put(r, c, x.x, x.y);
-          sh.dS.put(r, c, y.x, y.y);
-        }
-        float2 vx[kXTiles][2], rx[kXTiles][2];
+      const bool mine = side < W / 8;  // this warp's 8 columns of a round's 16 or 32
+      const int col = side * 8 + 2 * t;
+      Raw2<T> vx[2], ox[2];
+      float2 rx[2];
+      auto fetch_rows = [&](int v0) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int i = rb + g + 8 * r;
-          const bool in = i >= lo && i < hi;
+          const bool in = mine && i >= lo && i < hi;
+          vx[r] = raw2(v + i * a.vs.t, v0 + col, a.Dv, a.pairs, in);
+          rx[r] = raw2(R + (long long)i * a.Dv, v0 + col, a.Dv, a.even, in);
+          ox[r] = raw2(d_o + i * a.dos.t, v0 + col, a.Dv, a.pairs, in);
+        }
+      };
+      fetch_rows(0);
+
+      for (int v0 = 0; v0 < a.Dv; v0 += W) {
+        copies_wait<0>();
+        __syncthreads();  // the slices are there, and nobody reads the round before
 #pragma unroll
-          for (int c = 0; c < kXTiles; ++c) {
-            const int col = side * (W / 2) + c * 8 + 2 * t;
-            const float2 zero = make_float2(0.0f, 0.0f);
-            vx[c][r] = in ? get2(v + i * a.vs.t, v0 + col, a.Dv, a.pairs) : zero;
-            rx[c][r] = in ? get2(R + (long long)i * a.Dv, v0 + col, a.Dv, a.even) : zero;
-            const float2 ox = in ? get2(d_o + i * a.dos.t, v0 + col, a.Dv, a.pairs) : zero;
-            sh.R.put(i, col, rx[c][r].x, rx[c][r].y);
-            sh.dO.put(i, col, ox.x, ox.y);
-          }
+        for (int i = threadIdx.x; i < KD * W / 2; i += kGradThreads) {
+          const int r = i / (W / 2), c = i % (W / 2) * 2;
+          const float2 x = fresh ? zero : reinterpret_cast<const float2*>(sh.next_S)[i];
+          const float2 y = last ? reinterpret_cast<const float2*>(sh.next_dS)[i] : zero;
+          sh.S.put(r, c, x.x, x.y);
+          sh.dS.put(r, c, y.x, y.y);
+        }
+        float2 vn[2], rn[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          vn[r] = Pair<T>::get(vx[r]), rn[r] = rx[r];
+          const float2 on = Pair<T>::get(ox[r]);
+          if (mine) sh.R.put(rb + g + 8 * r, col, rx[r].x, rx[r].y), sh.dO.put(rb + g + 8 * r, col, on.x, on.y);
         }
         __syncthreads();
-        float x[kXTiles][4];  // X
-        {
-          float d[kXTiles][4] = {}, e[kXTiles][4] = {};
-          if (!fresh) product<2, P, 3, kXTiles, KD, false>(d, e, sh.K, rb, sh.S, side * (W / 2), 0);
+        if (v0 + W < a.Dv) {
+          fetch_slice<KD, W>(sh.next_S, S, v0 + W, a.Dk, a.Dv, a.quads);
+          fetch_slice<KD, W>(sh.next_dS, dS, v0 + W, a.Dk, a.Dv, a.quads);
+          fetch_rows(v0 + W);
+        }
+        copies_commit();
+        float x[4];  // X
+        __syncwarp();
+        if (mine) {
+          float d[1][4] = {}, e[1][4] = {};
+          if (!fresh) product<2, P, 3, 1, KD, false>(d, e, sh.K, rb, sh.S, side * 8, 0);
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
             const int i = rb + g + 8 * r;
             const bool in = i >= lo && i < hi;
             const float gam = gate.gam[i], beta = gate.beta[i];
-#pragma unroll
-            for (int c = 0; c < kXTiles; ++c) {
-              x[c][2 * r] = in ? vx[c][r].x - gam * (d[c][2 * r] + e[c][2 * r]) : 0.0f;
-              x[c][2 * r + 1] = in ? vx[c][r].y - gam * (d[c][2 * r + 1] + e[c][2 * r + 1]) : 0.0f;
-              sh.X.put(i, side * (W / 2) + c * 8 + 2 * t, in ? beta * x[c][2 * r] : 0.0f, in ? beta * x[c][2 * r + 1] : 0.0f);
-            }
+            x[2 * r] = in ? vn[r].x - gam * (d[0][2 * r] + e[0][2 * r]) : 0.0f;
+            x[2 * r + 1] = in ? vn[r].y - gam * (d[0][2 * r + 1] + e[0][2 * r + 1]) : 0.0f;
+            sh.X.put(i, col, in ? beta * x[2 * r] : 0.0f, in ? beta * x[2 * r + 1] : 0.0f);
           }
         }
         __syncthreads();
-        {
-          float d[kXTiles][4] = {}, e[kXTiles][4] = {};
-          product_part<2, 3, 3, kXTiles, false>(d, e, sh.N, rb, sh.X, side * (W / 2), 0, rb + 16);
+        if (mine) {
+          float d[1][4] = {}, e[1][4] = {};
+          product_lower<2, 3, 3, 1, false>(d, e, sh.N, rb, sh.X, side * 8);
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
             const int i = rb + g + 8 * r;
             const bool in = i >= lo && i < hi;
             const float beta = gate.beta[i];
-#pragma unroll
-            for (int c = 0; c < kXTiles; ++c) {
-              const float y = in ? x[c][2 * r] - (d[c][2 * r] + e[c][2 * r]) : 0.0f;
-              const float z = in ? x[c][2 * r + 1] - (d[c][2 * r + 1] + e[c][2 * r + 1]) : 0.0f;
-              rv[r] = fmaf(rx[c][r].x, vx[c][r].x, fmaf(rx[c][r].y, vx[c][r].y, rv[r]));
-              ry[r] = fmaf(rx[c][r].x, y, fmaf(rx[c][r].y, z, ry[r]));
-              sh.U.put(i, side * (W / 2) + c * 8 + 2 * t, in ? beta * y : 0.0f, in ? beta * z : 0.0f);
-            }
+            const float y = in ? x[2 * r] - (d[0][2 * r] + e[0][2 * r]) : 0.0f;
+            const float z = in ? x[2 * r + 1] - (d[0][2 * r + 1] + e[0][2 * r + 1]) : 0.0f;
+            rv[r] = fmaf(rn[r].x, vn[r].x, fmaf(rn[r].y, vn[r].y, rv[r]));
+            ry[r] = fmaf(rn[r].x, y, fmaf(rn[r].y, z, ry[r]));
+            sh.U.put(i, col, in ? beta * y : 0.0f, in ? beta * z : 0.0f);
           }
         }
         __syncthreads();
-        const int below = rb + 16;  // columns j of P and E that are not zero everywhere
+        const bool below = side * 16 <= rb;  // else the warp's part of P and E lies above the diagonal
         {
           uint32_t fa[W / 16][P][4];
 #pragma unroll
           for (int k = 0; k < W / 16; ++k) load_a<P>(sh.dO, rb, k * 16, fa[k]);
-          add_rows<2, 3, 4, W>(acc_p, fa, sh.U, side * 32, below);
-          if (!fresh) add_rows<2, 3, kTiles, W>(acc_q, fa, sh.S, side * kHalf, KD);
+          if (below) add_rows<2, 3, 2, W>(acc_p, fa, sh.U, side * 16);
+          if (!fresh) add_rows<2, 3, kTiles, W>(acc_q, fa, sh.S, side * kPart);
         }
         {
           uint32_t fa[W / 16][kOut][4];
 #pragma unroll
           for (int k = 0; k < W / 16; ++k) load_a<kOut>(sh.R, rb, k * 16, fa[k]);
-          add_rows<kDepth, kOut, 4, W>(acc_e, fa, sh.U, side * 32, below);
-          if (!fresh) add_rows<kDepth, kOut, kTiles, W>(acc_w, fa, sh.S, side * kHalf, KD);
+          if (below) add_rows<kDepth, kOut, 2, W>(acc_e, fa, sh.U, side * 16);
+          if (!fresh) add_rows<kDepth, kOut, kTiles, W>(acc_w, fa, sh.S, side * kPart);
         }
         if (last) {
           uint32_t fa[W / 16][kOut][4];
 #pragma unroll
           for (int k = 0; k < W / 16; ++k) load_a<kOut>(sh.U, rb, k * 16, fa[k]);
-          add_rows<kDepth, kOut, kTiles, W>(acc_t, fa, sh.dS, side * kHalf, KD);
+          add_rows<kDepth, kOut, kTiles, W>(acc_t, fa, sh.dS, side * kPart);
         }
       }
       __syncthreads();
@@ -1222,14 +1319,14 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
         const bool in = i >= lo && i < hi;
         const float beta = gate.beta[i];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int j = side * 32 + x * 8 + 2 * t;
+        for (int x = 0; x < 2; ++x) {
+          const int j = side * 16 + x * 8 + 2 * t;
           float p[2], e[2];
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             const float dist = (gate.g_high[i] - gate.g_high[j + y]) + (gate.g_low[i] - gate.g_low[j + y]);
             const bool both = in && i >= j + y && j + y >= lo;
-            const float D = both ? expf(dist) : 0.0f;
+            const float D = both ? decay_of(dist) : 0.0f;
             p[y] = both ? a.scale * D * acc_p[x][2 * r + y] : 0.0f;
             e[y] = both && i > j + y ? beta * D * acc_e[x][2 * r + y] : 0.0f;
           }
@@ -1238,6 +1335,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
         }
       }
       __syncthreads();
+      // acc_q: diag(scale gam) dO S0^T + P K; acc_t: diag(dec) U dS^T - diag(gam) dV S0^T + P^T Q; acc_w: E K + E^T K
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int i = rb + g + 8 * r;
@@ -1248,13 +1346,9 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
           for (int y = 2 * r; y < 2 * r + 2; ++y) {
             acc_q[x][y] = fresh ? 0.0f : a.scale * gam * acc_q[x][y];
             acc_t[x][y] = (last ? dec * acc_t[x][y] : 0.0f) + (fresh ? 0.0f : back * acc_w[x][y]);
+            acc_w[x][y] = 0.0f;
           }
       }
-      // P K to acc_q; P^T Q - E^T K - E K to acc_t (E's sign turned where it is subtracted: acc_w)
-#pragma unroll
-      for (int x = 0; x < kTiles; ++x)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) acc_w[x][y] = 0.0f;
 #pragma unroll
       for (int k0 = 0; k0 < C; k0 += 16) {
         if (k0 > rb) continue;
@@ -1264,7 +1358,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
 #pragma unroll
         for (int x = 0; x < kTiles; x += 2) {
           uint32_t fb[P][2][2];
-          load_bt<P>(sh.K, side * kHalf + x * 8, k0, fb);
+          load_bt<P>(sh.K, side * kPart + x * 8, k0, fb);
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             float d[4] = {}, e[4] = {};
@@ -1284,8 +1378,8 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
 #pragma unroll
         for (int x = 0; x < kTiles; x += 2) {
           uint32_t fk[P][2][2], fq[P][2][2];
-          load_bt<P>(sh.K, side * kHalf + x * 8, k0, fk);
-          load_bt<P>(sh.Q, side * kHalf + x * 8, k0, fq);
+          load_bt<P>(sh.K, side * kPart + x * 8, k0, fk);
+          load_bt<P>(sh.Q, side * kPart + x * 8, k0, fq);
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             mma<kDepth>(acc_t[x + y], acc_t[x + y], fp, fq, y);
@@ -1302,7 +1396,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
         float* sum_k = a.sum_k + (where * C + i) * KD;
 #pragma unroll
         for (int x = 0; x < kTiles; ++x) {
-          const int c = side * kHalf + x * 8 + 2 * t;
+          const int c = side * kPart + x * 8 + 2 * t;
           const float2 qx = sh.Q.pair(i, c);
           float gq[2], gk[2];
 #pragma unroll
@@ -1326,14 +1420,14 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
           }
         }
       }
-      // sums over a row's columns: four lanes and two warps
+      // sums over a row's columns: four lanes and four warps
       auto row_sum = [&](int which, float (&x)[2]) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           float y = x[r];
           y += __shfl_xor_sync(0xffffffffu, y, 1);
           y += __shfl_xor_sync(0xffffffffu, y, 2);
-          if (t == 0) sh.sums[(which * 2 + side) * C + rb + g + 8 * r] = y;
+          if (t == 0) sh.sums[(which * 4 + side) * C + rb + g + 8 * r] = y;
         }
       };
       row_sum(0, rv);
@@ -1341,7 +1435,10 @@ __global__ void __launch_bounds__(kThreads, 1) delta_gradients_kernel(const Delt
       row_sum(2, dot_q);
       __syncthreads();
       if (warp == 0) {  // dbeta, and dg: what the state before gives, less the rows before (rows lane and lane + 32)
-        auto sum_of = [&](int which, int row) { return sh.sums[which * 2 * C + row] + sh.sums[(which * 2 + 1) * C + row]; };
+        auto sum_of = [&](int which, int row) {
+          const float* x = sh.sums + which * 4 * C + row;
+          return (x[0] + x[C]) + (x[2 * C] + x[3 * C]);
+        };
         float start = 0.0f;
         if (!fresh)
           for (int i = 0; i < a.tiles; ++i) start += a.dots[chunk * a.tiles + i];
@@ -1394,7 +1491,7 @@ Workspace workspace_of(size_t es, bool exact, long long T, long long B, long lon
   if (backward) {
     w.dS = take(chunks * H * Dk * Dv * 4);
     w.R = take(chunks * H * C * Dv * 4);
-    w.dots = take(chunks * H * ((Dv + 15) / 16) * 4);
+    w.dots = take(chunks * H * ((Dv + 15) / 16 + 8) * 4);
     if (H > Hk) {
       w.sum_q = take(chunks * Hk * C * KD * 4);
       w.sum_k = take(chunks * Hk * C * KD * 4);
@@ -1409,12 +1506,25 @@ int columns_of(long long heads, int Dv, size_t es) {
   return heads * ((Dv + 15) / 16) <= 152 || es == 4 ? 16 : 32;
 }
 
+// Blocks of a head (tiles of columns, with some that have none) and of a cluster: as large as few idle blocks allow, any number
+// of them while the device has room.
+void clusters_of(long long heads, DeltaArgs& a, int NV) {
+  const int tiles = (a.Dv + NV - 1) / NV;
+  for (int c = 4;; c /= 2) {
+    const int padded = (tiles + c - 1) / c * c;
+    if (c == 1 || (c < 2 * tiles && (heads * padded <= 152 || 4 * padded <= 5 * tiles))) {
+      a.cluster = c, a.tiles = padded;
+      return;
+    }
+  }
+}
+
 template <auto kKern>
-cudaError_t launch_big(dim3 grid, size_t smem, cudaStream_t s, const DeltaArgs& a) {
+cudaError_t launch_big(dim3 grid, size_t smem, cudaStream_t s, const DeltaArgs& a, int cluster = 1, int threads = kThreads) {
   static thread_local DeviceSet ready;  // of this kernel
   const cudaError_t e =
       once_per_device(&ready, [&] { return cudaFuncSetAttribute(kKern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
-  return e != cudaSuccess ? e : op_launch(kKern, grid, dim3(kThreads), smem, s, a);
+  return e != cudaSuccess ? e : op_launch_clusters(cluster, kKern, grid, dim3(threads), smem, s, a);
 }
 
 template <typename F>
@@ -1431,9 +1541,9 @@ cudaError_t prepare(int dtype, const DeltaArgs& a, bool backward, cudaStream_t s
   return for_shape(dtype, a.Dk, [&](auto* t, auto kd) {
     using T = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
-    constexpr size_t bytes = PrepareShared<T, KD>::kBytes;
-    if (backward) return launch_big<delta_prepare_kernel<T, KD, true>>(dim3((unsigned)blocks), bytes, s, a);
-    return launch_big<delta_prepare_kernel<T, KD, false>>(dim3((unsigned)blocks), bytes, s, a);
+    const dim3 grid((unsigned)blocks);
+    if (backward) return launch_big<delta_prepare_kernel<T, KD, true>>(grid, PrepareShared<T, KD, 3>::kBytes, s, a);
+    return launch_big<delta_prepare_kernel<T, KD, false>>(grid, PrepareShared<T, KD, kOutParts<T>>::kBytes, s, a);
   });
 }
 
@@ -1450,7 +1560,7 @@ int check(int dtype, const void* q, const void* k, const void* v, const float* g
   if (!op_float_dtype(dtype)) return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "dtype %d", dtype);
   if (int rc = delta_check_sizes(T, B, H, Hk, Dk, Dv, msg, msg_len)) return rc;
   const long long tiles = (Dv + 15) / 16;
-  if ((long long)B * H > 0x7fffffffll / tiles || (long long)((T + 63ll) / 64) * B > 0x7fffffffll / H)
+  if ((long long)B * H > 0x7fffffffll / (tiles + 8) || (long long)((T + 63ll) / 64) * B > 0x7fffffffll / H)
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "B H ceil(Dv / 16) and ceil(T / 64) B H must be below 2^31");
   const size_t es = op_dtype_bytes(dtype);
   if (T > 0 && B > 0 && (!q || !k || !v || !g || !beta))
@@ -1509,14 +1619,14 @@ extern "C" int lstm_approx_delta_scan(int dtype, const void* q, const void* k, c
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   if (int rc = op_launched(prepare(dtype, a, false, s), "delta scan launch", msg, msg_len)) return rc;
   const int NV = columns_of((long long)B * H, Dv, es);
-  a.tiles = (Dv + NV - 1) / NV;
+  clusters_of((long long)B * H, a, NV);
   const dim3 grid((unsigned)(B * H * a.tiles));
   const cudaError_t e = for_shape(dtype, Dk, [&](auto* t, auto kd) {
     using Ty = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
     if constexpr (sizeof(Ty) == 2)
-      if (NV == 32) return launch_big<delta_forward_kernel<Ty, KD, 32>>(grid, ForwardShared<Ty, KD, 32>::kBytes, s, a);
-    return launch_big<delta_forward_kernel<Ty, KD, 16>>(grid, ForwardShared<Ty, KD, 16>::kBytes, s, a);
+      if (NV == 32) return launch_big<delta_forward_kernel<Ty, KD, 32>>(grid, ForwardShared<Ty, KD, 32>::kBytes, s, a, a.cluster);
+    return launch_big<delta_forward_kernel<Ty, KD, 16>>(grid, ForwardShared<Ty, KD, 16>::kBytes, s, a, a.cluster);
   });
   return op_launched(e, "delta scan launch", msg, msg_len);
 }
@@ -1554,6 +1664,7 @@ extern "C" int lstm_approx_delta_scan_backward(int dtype, const void* d_o, const
   a.wide = wide_rows(q, a.qs, Dk, es) && wide_rows(k, a.ks, Dk, es) && wide_rows(dq, a.dqs, Dk, es) && wide_rows(dk, a.dks, Dk, es);
   a.pairs = pair_rows(v, a.vs, Dv, es) && pair_rows(d_o, a.dos, Dv, es) && pair_rows(dv, a.dvs, Dv, es);
   a.even = Dv % 2 == 0 && op_aligned(states, 8) && op_aligned(dh_last, 8) && op_aligned(dh0, 8);
+  a.quads = Dv % 4 == 0 && op_aligned(states, 16);
   a.states = const_cast<float*>(states), a.dh_last = dh_last;
   a.dq = dq, a.dk = dk, a.dv = dv, a.dg = dg, a.dbeta = dbeta, a.dh0 = dh0;
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) / 256 * 256);
@@ -1564,14 +1675,14 @@ extern "C" int lstm_approx_delta_scan_backward(int dtype, const void* d_o, const
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   if (int rc = op_launched(prepare(dtype, a, true, s), "delta scan launch", msg, msg_len)) return rc;
   const int NV = columns_of((long long)B * H, Dv, es);
-  a.tiles = (Dv + NV - 1) / NV;
+  clusters_of((long long)B * H, a, NV);
   const dim3 grid((unsigned)(B * H * a.tiles));
   cudaError_t e = for_shape(dtype, Dk, [&](auto* t, auto kd) {
     using Ty = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
     if constexpr (sizeof(Ty) == 2)
-      if (NV == 32) return launch_big<delta_backward_kernel<Ty, KD, 32>>(grid, BackwardShared<Ty, KD, 32>::kBytes, s, a);
-    return launch_big<delta_backward_kernel<Ty, KD, 16>>(grid, BackwardShared<Ty, KD, 16>::kBytes, s, a);
+      if (NV == 32) return launch_big<delta_backward_kernel<Ty, KD, 32>>(grid, BackwardShared<Ty, KD, 32>::kBytes, s, a, a.cluster);
+    return launch_big<delta_backward_kernel<Ty, KD, 16>>(grid, BackwardShared<Ty, KD, 16>::kBytes, s, a, a.cluster);
   });
   if (int rc = op_launched(e, "delta scan backward launch", msg, msg_len)) return rc;
   if (T == 0) return LSTM_APPROX_OK;
@@ -1579,7 +1690,7 @@ extern "C" int lstm_approx_delta_scan_backward(int dtype, const void* d_o, const
   e = for_shape(dtype, Dk, [&](auto* t, auto kd) {
     using Ty = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
-    return launch_big<delta_gradients_kernel<Ty, KD>>(blocks, GradShared<Ty, KD>::kBytes, s, a);
+    return launch_big<delta_gradients_kernel<Ty, KD>>(blocks, GradShared<Ty, KD>::kBytes, s, a, 1, kGradThreads);
   });
   return op_launched(e, "delta gradients launch", msg, msg_len);
 }
