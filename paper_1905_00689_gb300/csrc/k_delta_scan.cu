@@ -186,6 +186,10 @@ __device__ __forceinline__ void mma(float (&d)[4], float (&e)[4], const uint32_t
 
 // ---- what the kernels share ----------------------------------------------------
 
+// A wait for a copy that a working device always completes; on one that does not the results are NaN.
+constexpr uint64_t kWaitNs = 2000000000ull;
+__device__ const int g_never = 0;
+
 struct Gates {  // of a chunk and head
   float gam[C], dec[C], beta[C], g_high[C], g_low[C];
   unsigned long long cuts;  // bit i: a reset at row i
@@ -256,30 +260,36 @@ __device__ __forceinline__ void fetch(void* to, const void* from) {
       copy16(static_cast<char*>(to) + i + threadIdx.x * 16, static_cast<const char*>(from) + i + threadIdx.x * 16, 16);
 }
 
-// A wait for a copy that a working device always completes; on one that does not the results are NaN.
-constexpr uint64_t kWaitNs = 2000000000ull;
-__device__ const int g_never = 0;
-
 // Two neighbouring values of a row (the second only if it lies in the row).
 template <typename T>
 __device__ __forceinline__ float2 get2(const T* row, int col, int D, bool pairs) {
   if (pairs) return col < D ? Pair<T>::get(*reinterpret_cast<const typename Pair<T>::Raw*>(row + col)) : make_float2(0.0f, 0.0f);
   return make_float2(col < D ? to_f32(row[col]) : 0.0f, col + 1 < D ? to_f32(row[col + 1]) : 0.0f);
 }
-// The same as they lie in memory: converted where they are used, so that nothing waits for them before.
+// The same as they lie in memory, to be converted where they are used: nothing waits for them before.  (Without the empty
+// statement the compiler converts them where they are loaded, and a chunk forward took 0.6 us more.)
 template <typename T>
-using Raw2 = typename Pair<T>::Raw;
-template <typename T>
-__device__ __forceinline__ Raw2<T> raw2(const T* row, int col, int D, bool pairs, bool in) {
-  Raw2<T> v = Pair<T>::put(0.0f, 0.0f);
-  if (pairs) {
-    if (in && col < D) v = *reinterpret_cast<const Raw2<T>*>(row + col);
-  } else {
-    if (in && col < D) v.x = row[col];
-    if (in && col + 1 < D) v.y = row[col + 1];
+struct Raw2 {
+  typename Pair<T>::Raw v;
+  __device__ __forceinline__ void load(const T* row, int col, int D, bool pairs, bool in) {
+    v = Pair<T>::put(0.0f, 0.0f);
+    if (pairs) {
+      if (in && col < D) v = *reinterpret_cast<const typename Pair<T>::Raw*>(row + col);
+    } else {
+      if (in && col < D) v.x = row[col];
+      if (in && col + 1 < D) v.y = row[col + 1];
+    }
   }
-  return v;
-}
+  __device__ __forceinline__ float2 get() {
+    if constexpr (sizeof(T) == 4) {
+      asm volatile("" : "+f"(v.x), "+f"(v.y));
+    } else {
+      uint32_t& bits = reinterpret_cast<uint32_t&>(v);
+      asm volatile("" : "+r"(bits));
+    }
+    return Pair<T>::get(v);
+  }
+};
 template <typename T>
 __device__ __forceinline__ void put2(T* row, int col, int D, bool pairs, float x, float y) {
   if (pairs) {
@@ -620,6 +630,38 @@ struct Stage {
 template <typename T, int KD>
 constexpr int kStages = kParts<T> > 1 && KD == 128 ? 1 : 2;
 
+// The kernels along the chunks have 8 warps for what leads from one state to the next, 4 that work beside them and one that asks
+// for the chunks.  Barriers among them:
+constexpr int kChainThreads = 256, kSideThreads = 128, kBothThreads = kChainThreads + kSideThreads, kAllThreads = kBothThreads + 32;
+constexpr uint32_t kChain = 1, kSide = 2, kToSide = 3, kToChain = 4, kStateToSide = 5;
+
+// Two rings of barriers of a block: a stage's chunk has come; all warps of the cluster have read it.
+template <int kN>
+struct Ring {
+  uint32_t full, empty;  // addresses
+  int cluster;
+  bool ok;
+  __device__ __forceinline__ Ring(uint64_t* bars, int cluster_) : full(smem_u32(bars)), empty(smem_u32(bars + kN)), cluster(cluster_), ok(true) {}
+  __device__ __forceinline__ void init() const {  // one thread
+#pragma unroll
+    for (int i = 0; i < kN; ++i) mbar_init(full + 8 * i, 1), mbar_init(empty + 8 * i, (kBothThreads / 32) * cluster);
+    fence_mbarrier_init_cluster();
+  }
+  // The k-th chunk (once a wait has run out, no further one is waited for).
+  __device__ __forceinline__ bool wait_full(int k) {
+    ok = ok && mbar_wait_bounded<true>(full + k % kN * 8, (uint32_t)(k / kN) & 1u, kWaitNs, &g_never);
+    return ok;
+  }
+  __device__ __forceinline__ bool wait_empty(int k) {
+    ok = ok && (k < kN || mbar_wait_bounded<true>(empty + k % kN * 8, (uint32_t)(k / kN - 1) & 1u, kWaitNs, &g_never));
+    return ok;
+  }
+  __device__ __forceinline__ void release(int k) const {  // a whole warp
+    __syncwarp();
+    if ((int)(threadIdx.x & 31) < cluster) mbar_arrive_cluster(mapa_shared(empty + k % kN * 8, threadIdx.x & 31));
+  }
+};
+
 // A block's part of the state: 16 rows of S (a warp's) and kTiles times 8 columns in the MMA's result layout.
 template <int KD, int NV>
 struct StatePart {
@@ -716,364 +758,403 @@ __device__ __forceinline__ void product_lower(float (&d)[kTiles][4], float (&e)[
 
 template <typename T, int KD, int NV>
 struct ForwardShared {
-  static constexpr int kOut = kOutParts<T>;
+  static constexpr int kOut = kOutParts<T>, kN = kStages<T, KD>;
   using St = Stage<T, KD, kOut>;
-  Mat<KD, NV, 3> S;
+  using SMat = Mat<KD, NV, 3>;
+  SMat S;  // before the chunk; the next one's behind it
   Mat<C, NV, 3> X, Ud;
   Mat<C, NV, kOut> U;
-  uint64_t* bars;  // [2]
-  static constexpr size_t kBytes = kStages<T, KD> * St::kBytes + decltype(S)::kBytes + 2 * decltype(X)::kBytes + decltype(U)::kBytes + 16;
+  uint64_t* bars;  // [2 kN]
+  static constexpr size_t kBytes = kN * St::kBytes + 2 * SMat::kBytes + 2 * decltype(X)::kBytes + decltype(U)::kBytes + 16 * kN;
   __device__ __forceinline__ explicit ForwardShared(unsigned char* p)
-      : S{reinterpret_cast<bf16*>(p + kStages<T, KD> * St::kBytes)}, X{S.p + S.kSize * 3}, Ud{X.p + X.kSize * 3}, U{Ud.p + Ud.kSize * 3},
+      : S{reinterpret_cast<bf16*>(p + kN * St::kBytes)}, X{S.p + 2 * S.kSize * 3}, Ud{X.p + X.kSize * 3}, U{Ud.p + Ud.kSize * 3},
         bars(reinterpret_cast<uint64_t*>(U.p + U.kSize * kOut)) {}
+  __device__ __forceinline__ SMat state(int n) const { return SMat{S.p + (n & 1) * S.kSize * 3}; }
 };
 
+// Warps 0 to 7: X, Y and the next state.  Warps 8 to 11: O, from the state and U.  (All of it by 8 warps: 0.6 us of 2.8 us to a
+// chunk of 64 x 128 x 16.)
 template <typename T, int KD, int NV>
-__global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const DeltaArgs a) {
+__global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
-  constexpr int kTiles = NV / 16;  // a warp's 16 rows of the chunk and half of the columns
-  constexpr int P = kParts<T>, kOut = kOutParts<T>, kDepth = kOutDepth<T>, kTwo = kStages<T, KD> - 1;
+  constexpr int P = kParts<T>, kOut = kOutParts<T>, kDepth = kOutDepth<T>;
   using Sh = ForwardShared<T, KD, NV>;
   using St = typename Sh::St;
+  constexpr int kN = Sh::kN;
   const Sh sh(smem);
   begin_op();
   const int v0 = (int)(blockIdx.x % a.tiles) * NV, bh = blockIdx.x / a.tiles, h = bh % a.H, b = bh / a.H;
   const int len = length_of(a, b), chunks = (len + C - 1) / C;
   const int warp = threadIdx.x >> 5, g = lane_g(), t = lane_t();
-  const int rb = (warp < 4 ? warp : 7 - warp) * 16;  // warps w and w + 4 share a part of the SM: of triangles, a short and a long row
-  const int cb = (warp >> 2) * (NV / 2);
   const long long DD = (long long)a.Dk * a.Dv;
-  const T* v = static_cast<const T*>(a.v) + b * a.vs.b + h * a.vs.h;
   T* o = static_cast<T*>(a.o) + b * a.os.b + h * a.os.h;
-
+  Ring<kN> ring(sh.bars, a.cluster);
   StatePart<KD, NV> s;
-  s.load(a.h0 ? a.h0 + (long long)bh * DD : nullptr, a, v0);
-  s.split(sh.S);
-  Raw2<T> vx[kTiles][2];
-  auto fetch_v = [&](int n) {
-#pragma unroll
-    for (int x = 0; x < kTiles; ++x)
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int time = n * C + rb + g + 8 * r;
-        vx[x][r] = raw2(v + time * a.vs.t, v0 + cb + x * 8 + 2 * t, a.Dv, a.pairs, time < len);
-      }
-  };
-  const uint32_t rank = cluster_ctarank(), bar = smem_u32(sh.bars);
-  const bool asks = threadIdx.x == 7 * 32;
-  if (asks) {
-    mbar_init(bar, 1);
-    mbar_init(bar + 8, 1);
-    fence_mbarrier_init_cluster();
+  if (warp < 8) {
+    s.load(a.h0 ? a.h0 + (long long)bh * DD : nullptr, a, v0);
+    s.split(sh.S);
   }
-  if (chunks > 0) fetch_v(0);
+  if (threadIdx.x == kBothThreads) ring.init();
+  __syncthreads();
   cluster_sync_all();  // barriers and buffers of all blocks are ready
-  if (asks && chunks > 0) St(smem).load(a, 0, b, h, rank, bar);
 
-  for (int n = 0; n < chunks; ++n) {
-    const bool came = mbar_wait_bounded<true>(bar + (n & kTwo) * 8, (uint32_t)(n >> kTwo) & 1u, kWaitNs, &g_never);
-    __syncthreads();
-    const St now(smem + (n & kTwo) * St::kBytes);
-    const Gates& gate = *now.gates;
-    float2 vn[kTiles][2];
-#pragma unroll
-    for (int x = 0; x < kTiles; ++x) vn[x][0] = Pair<T>::get(vx[x][0]), vn[x][1] = Pair<T>::get(vx[x][1]);
-    if (!came) vn[0][0].x = __int_as_float(0x7fffffff);
-    if (n + 1 < chunks) {
-      if (kTwo && warp == 7) {  // (the others wait for the cluster at the chunk's end, where nothing is left to wait for)
-        if (n > 0) cluster_wait();
-        if (asks) St(smem + (~n & 1) * St::kBytes).load(a, n + 1, b, h, rank, bar + (~n & 1) * 8);
-      }
-      fetch_v(n + 1);
+  if (warp == kBothThreads / 32) {
+    if (threadIdx.x == kBothThreads) {
+      const uint32_t rank = cluster_ctarank();
+      for (int n = 0; n < chunks && ring.wait_empty(n); ++n) St(smem + n % kN * St::kBytes).load(a, n, b, h, rank, ring.full + n % kN * 8);
     }
-    if (a.states) s.store(a.states + (((long long)n * a.B + b) * a.H + h) * DD, a, v0);
-    const unsigned long long cuts = gate.cuts;
+  } else if (warp < 8) {
+    constexpr int kTiles = NV / 16;  // a warp's 16 rows of the chunk and half of the columns
+    const int rb = (warp < 4 ? warp : 7 - warp) * 16;  // warps w and w + 4 share a part of the SM: of triangles, a short and a long row
+    const int cb = (warp >> 2) * (NV / 2);
+    const T* v = static_cast<const T*>(a.v) + b * a.vs.b + h * a.vs.h;
+    Raw2<T> vx[kTiles][2];
+    auto fetch_v = [&](int n) {
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int time = n * C + rb + g + 8 * r;
+          vx[x][r].load(v + time * a.vs.t, v0 + cb + x * 8 + 2 * t, a.Dv, a.pairs, time < len);
+        }
+    };
+    fetch_v(0);
+    for (int n = 0; n < chunks; ++n) {
+      const bool came = ring.wait_full(n);
+      __syncwarp();
+      const St now(smem + n % kN * St::kBytes);
+      const auto S0 = sh.state(n);
+      const Gates& gate = *now.gates;
+      float2 vn[kTiles][2];
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x) vn[x][0] = vx[x][0].get(), vn[x][1] = vx[x][1].get();
+      if (!came) vn[0][0].x = __int_as_float(0x7fffffff);
+      fetch_v(n + 1);
+      if (a.states) s.store(a.states + (((long long)n * a.B + b) * a.H + h) * DD, a, v0);
+      const unsigned long long cuts = gate.cuts;
 
-    for (int lo = 0; lo < C;) {
-      const int hi = piece_end(cuts, lo);
-      const bool fresh = cut_before(cuts, lo);
-      float x[kTiles][4];      // B X, then U
-      float oq[kTiles][4] = {};  // gam Q S0
-      __syncwarp();
-      {
-        float d[kTiles][4] = {}, e[kTiles][4] = {};
-        if (!fresh) product<2, P, 3, kTiles, KD, false>(d, e, now.K, rb, sh.S, cb, 0);
+      for (int lo = 0; lo < C;) {
+        const int hi = piece_end(cuts, lo);
+        float x[kTiles][4];  // B X
+        __syncwarp();
+        {
+          float d[kTiles][4] = {}, e[kTiles][4] = {};
+          if (!cut_before(cuts, lo)) product<2, P, 3, kTiles, KD, false>(d, e, now.K, rb, S0, cb, 0);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int i = rb + g + 8 * r;
-          const float gam = gate.gam[i], beta = gate.beta[i];
-          const bool in = i >= lo && i < hi;
+          for (int r = 0; r < 2; ++r) {
+            const int i = rb + g + 8 * r;
+            const float gam = gate.gam[i], beta = gate.beta[i];
+            const bool in = i >= lo && i < hi;
 #pragma unroll
-          for (int c = 0; c < kTiles; ++c) {
-            x[c][2 * r] = in ? beta * (vn[c][r].x - gam * (d[c][2 * r] + e[c][2 * r])) : 0.0f;
-            x[c][2 * r + 1] = in ? beta * (vn[c][r].y - gam * (d[c][2 * r + 1] + e[c][2 * r + 1])) : 0.0f;
-            sh.X.put(i, cb + c * 8 + 2 * t, x[c][2 * r], x[c][2 * r + 1]);
+            for (int c = 0; c < kTiles; ++c) {
+              x[c][2 * r] = in ? beta * (vn[c][r].x - gam * (d[c][2 * r] + e[c][2 * r])) : 0.0f;
+              x[c][2 * r + 1] = in ? beta * (vn[c][r].y - gam * (d[c][2 * r + 1] + e[c][2 * r + 1])) : 0.0f;
+              sh.X.put(i, cb + c * 8 + 2 * t, x[c][2 * r], x[c][2 * r + 1]);
+            }
           }
         }
-      }
-      __syncwarp();
-      if (!fresh) {
-        float d[kTiles][4] = {}, e[kTiles][4] = {};
-        product<kDepth, P, kOut, kTiles, KD, false>(d, e, now.Q, rb, sh.S, cb, 0);
+        named_sync(kChain, kChainThreads);
+        {
+          float d[kTiles][4] = {}, e[kTiles][4] = {};
+          product_lower<2, 3, 3, kTiles, false>(d, e, now.N, rb, sh.X, cb);
+          named_sync(kToChain, kBothThreads);  // the U before has been read
 #pragma unroll
-        for (int c = 0; c < kTiles; ++c)
+          for (int r = 0; r < 2; ++r) {
+            const int i = rb + g + 8 * r;
+            const bool in = i >= lo && i < hi;
+            const float beta = gate.beta[i], dec = gate.dec[i];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) oq[c][r] = gate.gam[rb + g + 8 * (r >> 1)] * (d[c][r] + e[c][r]);
-      }
-      __syncthreads();
-      {
-        float d[kTiles][4] = {}, e[kTiles][4] = {};
-        product_lower<2, 3, 3, kTiles, false>(d, e, now.N, rb, sh.X, cb);
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int i = rb + g + 8 * r;
-          const bool in = i >= lo && i < hi;
-          const float beta = gate.beta[i], dec = gate.dec[i];
-#pragma unroll
-          for (int c = 0; c < kTiles; ++c) {
-            const float p = in ? x[c][2 * r] - beta * (d[c][2 * r] + e[c][2 * r]) : 0.0f;
-            const float q = in ? x[c][2 * r + 1] - beta * (d[c][2 * r + 1] + e[c][2 * r + 1]) : 0.0f;
-            sh.U.put(i, cb + c * 8 + 2 * t, p, q);
-            sh.Ud.put(i, cb + c * 8 + 2 * t, in ? dec * p : 0.0f, in ? dec * q : 0.0f);
+            for (int c = 0; c < kTiles; ++c) {
+              const float p = in ? x[c][2 * r] - beta * (d[c][2 * r] + e[c][2 * r]) : 0.0f;
+              const float q = in ? x[c][2 * r + 1] - beta * (d[c][2 * r + 1] + e[c][2 * r + 1]) : 0.0f;
+              sh.U.put(i, cb + c * 8 + 2 * t, p, q);
+              if (hi == C) sh.Ud.put(i, cb + c * 8 + 2 * t, in ? dec * p : 0.0f, in ? dec * q : 0.0f);
+            }
           }
         }
-      }
-      if (hi == C && lo > 0)  // the last piece's keys alone reach the next chunk
-        for (int i = threadIdx.x; i < lo * KD; i += kThreads)
+        if (hi == C && lo > 0) {  // the last piece's keys alone reach the next chunk
+          for (int i = threadIdx.x; i < lo * KD; i += kChainThreads)
 #pragma unroll
-          for (int q = 0; q < P; ++q) now.K.p[q * now.K.kSize + i] = from_f32<bf16>(0.0f);
-      __syncthreads();
-      if (hi == C) {
-        const float keep = gate.gam[C - 1];
-        s.each([&](int, int, float& p, float& q) { p = cuts ? 0.0f : keep * p, q = cuts ? 0.0f : keep * q; });
-        add_keys<P>(s, now.K, sh.Ud);
-        s.split(sh.S);
+            for (int q = 0; q < P; ++q) now.K.p[q * now.K.kSize + i] = from_f32<bf16>(0.0f);
+          fence_proxy_async_shared();  // (before a copy overwrites them)
+        }
+        named_arrive(kToSide, kBothThreads);
+        named_sync(kChain, kChainThreads);
+        lo = hi;
       }
-      __syncwarp();
-      {
-        float e[kTiles][4] = {};
-        product_lower<kDepth, kOut, kOut, kTiles, false>(oq, e, now.M, rb, sh.U, cb);
+      const float keep = gate.gam[C - 1];
+      s.each([&](int, int, float& p, float& q) { p = cuts ? 0.0f : keep * p, q = cuts ? 0.0f : keep * q; });
+      add_keys<P>(s, now.K, sh.Ud);
+      ring.release(n);
+      s.split(sh.state(n + 1));
+      if (n + 1 < chunks) named_arrive(kStateToSide, kBothThreads);
+      named_sync(kChain, kChainThreads);
+    }
+    s.store(a.h_last + (long long)bh * DD, a, v0);
+  } else {
+    constexpr int kTiles = NV / 8;
+    const int rb = (warp - 8) * 16;
+    for (int n = 0; n < chunks; ++n) {
+      const bool came = ring.wait_full(n);
+      if (n > 0) named_sync(kStateToSide, kBothThreads);
+      const St now(smem + n % kN * St::kBytes);
+      const Gates& gate = *now.gates;
+      const unsigned long long cuts = gate.cuts;
+      for (int lo = 0; lo < C;) {
+        const int hi = piece_end(cuts, lo);
+        float d[kTiles][4] = {}, e[kTiles][4] = {};
+        __syncwarp();
+        if (!cut_before(cuts, lo)) {
+          product<kDepth, P, kOut, kTiles, KD, false>(d, e, now.Q, rb, sh.state(n), 0, 0);
+#pragma unroll
+          for (int c = 0; c < kTiles; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) d[c][r] = gate.gam[rb + g + 8 * (r >> 1)] * (d[c][r] + e[c][r]), e[c][r] = 0.0f;
+        }
+        named_arrive(kToChain, kBothThreads);
+        named_sync(kToSide, kBothThreads);
+        product_lower<kDepth, kOut, kOut, kTiles, false>(d, e, now.M, rb, sh.U, 0);
+        if (hi == C) ring.release(n);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int i = rb + g + 8 * r, time = n * C + i;
           if (i < lo || i >= hi || time >= len) continue;
 #pragma unroll
-          for (int c = 0; c < kTiles; ++c)
-            put2(o + time * a.os.t, v0 + cb + c * 8 + 2 * t, a.Dv, a.pairs, a.scale * (oq[c][2 * r] + e[c][2 * r]),
-                 a.scale * (oq[c][2 * r + 1] + e[c][2 * r + 1]));
+          for (int c = 0; c < kTiles; ++c) {
+            const float p = came ? a.scale * (d[c][2 * r] + e[c][2 * r]) : __int_as_float(0x7fffffff);
+            put2(o + time * a.os.t, v0 + c * 8 + 2 * t, a.Dv, a.pairs, p, a.scale * (d[c][2 * r + 1] + e[c][2 * r + 1]));
+          }
         }
+        lo = hi;
       }
-      lo = hi;
-      if (lo < C) __syncthreads();
     }
-    if (cuts) fence_proxy_async_shared();  // rows zeroed above, before a copy overwrites them
-    if constexpr (kTwo) {
-      if (n > 0 && (warp != 7 || n + 1 == chunks)) cluster_wait();
-      cluster_arrive();
-    } else {
-      cluster_sync_all();
-      if (asks && n + 1 < chunks) St(smem).load(a, n + 1, b, h, rank, bar);
+    for (long long i = (long long)len * NV + (threadIdx.x - kChainThreads); i < (long long)a.T * NV; i += kSideThreads) {
+      const int c = v0 + (int)(i % NV);
+      if (c < a.Dv) o[i / NV * a.os.t + c] = from_f32<T>(0.0f);
     }
   }
-  if (kTwo && chunks > 0) cluster_wait();
-  if (v0 >= a.Dv) return;
-  s.store(a.h_last + (long long)bh * DD, a, v0);
-  for (long long i = (long long)len * NV + threadIdx.x; i < (long long)a.T * NV; i += kThreads) {
-    const int c = v0 + (int)(i % NV);
-    if (c < a.Dv) o[i / NV * a.os.t + c] = from_f32<T>(0.0f);
-  }
+  cluster_sync_all();  // nothing is sent to a block that has ended
 }
 
 template <typename T, int KD, int NV>
 struct BackwardShared {
+  static constexpr int kN = kStages<T, KD>, kLPitch = NV + 4;
   using St = Stage<T, KD, 3>;
   Mat<KD, NV, 3> S;                // dS
   Mat<C, NV, 3> Od, Z;             // scale gam dO; B dU, then - gam B R
   Mat<C, NV, kParts<T>> O;         // dO
-  uint64_t* bars;                  // [2]
+  float* L;                        // scale M^T dO, [C][kLPitch]
+  uint64_t* bars;                  // [2 kN]
   float* sums;                     // [8]
-  static constexpr size_t kBytes = kStages<T, KD> * St::kBytes + decltype(S)::kBytes + 2 * decltype(Z)::kBytes + decltype(O)::kBytes + 48;
+  static constexpr size_t kBytes = kN * St::kBytes + decltype(S)::kBytes + 2 * decltype(Z)::kBytes + decltype(O)::kBytes + C * kLPitch * 4 + 16 * kN + 32;
   __device__ __forceinline__ explicit BackwardShared(unsigned char* p)
-      : S{reinterpret_cast<bf16*>(p + kStages<T, KD> * St::kBytes)}, Od{S.p + S.kSize * 3}, Z{Od.p + Od.kSize * 3}, O{Z.p + Z.kSize * 3},
-        bars(reinterpret_cast<uint64_t*>(O.p + O.kSize * kParts<T>)), sums(reinterpret_cast<float*>(bars + 2)) {}
+      : S{reinterpret_cast<bf16*>(p + kN * St::kBytes)}, Od{S.p + S.kSize * 3}, Z{Od.p + Od.kSize * 3}, O{Z.p + Z.kSize * 3},
+        L(reinterpret_cast<float*>(O.p + O.kSize * kParts<T>)), bars(reinterpret_cast<uint64_t*>(L + C * kLPitch)),
+        sums(reinterpret_cast<float*>(bars + 2 * kN)) {}
 };
 
-// dS before a chunk from dS behind it; keeps the latter, R and <dS0, S0> for the gradients of the rest, and writes dV.
+// dS before a chunk from dS behind it; keeps the latter, R and <dS0, S0> for the gradients of the rest, and writes dV.  Warps 8 to
+// 11 go ahead with what dO alone gives.
 template <typename T, int KD, int NV>
-__global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const DeltaArgs a) {
+__global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
-  constexpr int kTiles = NV / 16, P = kParts<T>, kTwo = kStages<T, KD> - 1;
+  constexpr int P = kParts<T>;
   using Sh = BackwardShared<T, KD, NV>;
   using St = typename Sh::St;
+  constexpr int kN = Sh::kN;
   const Sh sh(smem);
   begin_op();
   const int v0 = (int)(blockIdx.x % a.tiles) * NV, bh = blockIdx.x / a.tiles, h = bh % a.H, b = bh / a.H;
   const int len = length_of(a, b), chunks = (len + C - 1) / C;
   const int warp = threadIdx.x >> 5, g = lane_g(), t = lane_t();
-  const int rb = (warp < 4 ? warp : 7 - warp) * 16, cb = (warp >> 2) * (NV / 2);
   const long long DD = (long long)a.Dk * a.Dv;
-  const T* d_o = static_cast<const T*>(a.d_o) + b * a.dos.b + h * a.dos.h;
-  T* dv = static_cast<T*>(a.dv) + b * a.dvs.b + h * a.dvs.h;
-
-  StatePart<KD, NV> s, before;
-  s.load(a.dh_last ? a.dh_last + (long long)bh * DD : nullptr, a, v0);
-  s.split(sh.S);
-  Raw2<T> ox[kTiles][2];
-  auto fetch_o = [&](int n) {
-#pragma unroll
-    for (int x = 0; x < kTiles; ++x)
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int time = n * C + rb + g + 8 * r;
-        ox[x][r] = raw2(d_o + time * a.dos.t, v0 + cb + x * 8 + 2 * t, a.Dv, a.pairs, time < len);
-      }
-  };
-  const uint32_t rank = cluster_ctarank(), bar = smem_u32(sh.bars);
-  const bool asks = threadIdx.x == 7 * 32;
-  if (asks) {
-    mbar_init(bar, 1);
-    mbar_init(bar + 8, 1);
-    fence_mbarrier_init_cluster();
+  Ring<kN> ring(sh.bars, a.cluster);
+  StatePart<KD, NV> s;
+  if (warp < 8) {
+    s.load(a.dh_last ? a.dh_last + (long long)bh * DD : nullptr, a, v0);
+    s.split(sh.S);
   }
-  if (chunks > 0) fetch_o(chunks - 1);
+  if (threadIdx.x == kBothThreads) ring.init();
+  __syncthreads();
   cluster_sync_all();
-  if (asks && chunks > 0) St(smem).load(a, chunks - 1, b, h, rank, bar);
 
-  for (int n = chunks - 1; n >= 0; --n) {
-    const int turn = chunks - 1 - n;
-    const bool came = mbar_wait_bounded<true>(bar + (turn & kTwo) * 8, (uint32_t)(turn >> kTwo) & 1u, kWaitNs, &g_never);
-    __syncthreads();
-    const St now(smem + (turn & kTwo) * St::kBytes);
-    const Gates& gate = *now.gates;
-    const long long chunk = ((long long)n * a.B + b) * a.H + h;
-    float2 on[kTiles][2];
-#pragma unroll
-    for (int x = 0; x < kTiles; ++x) on[x][0] = Pair<T>::get(ox[x][0]), on[x][1] = Pair<T>::get(ox[x][1]);
-    if (!came) on[0][0].x = __int_as_float(0x7fffffff);
-    if (n > 0) {
-      if (kTwo && warp == 7) {
-        if (turn > 0) cluster_wait();
-        if (asks) St(smem + (~turn & 1) * St::kBytes).load(a, n - 1, b, h, rank, bar + (~turn & 1) * 8);
-      }
-      fetch_o(n - 1);
+  if (warp == kBothThreads / 32) {
+    if (threadIdx.x == kBothThreads) {
+      const uint32_t rank = cluster_ctarank();
+      for (int k = 0; k < chunks && ring.wait_empty(k); ++k)
+        St(smem + k % kN * St::kBytes).load(a, chunks - 1 - k, b, h, rank, ring.full + k % kN * 8);
     }
-    s.store(a.dS + chunk * DD, a, v0);
-    before.load(a.states + chunk * DD, a, v0);
-    const unsigned long long cuts = gate.cuts;
-    float* R = a.R + chunk * C * a.Dv;
+  } else if (warp < 8) {
+    constexpr int kTiles = NV / 16;
+    const int rb = (warp < 4 ? warp : 7 - warp) * 16, cb = (warp >> 2) * (NV / 2);
+    T* dv = static_cast<T*>(a.dv) + b * a.dvs.b + h * a.dvs.h;
+    for (int k = 0; k < chunks; ++k) {
+      const int n = chunks - 1 - k;
+      const bool came = ring.wait_full(k);
+      __syncwarp();
+      const St now(smem + k % kN * St::kBytes);
+      const Gates& gate = *now.gates;
+      const long long chunk = ((long long)n * a.B + b) * a.H + h;
+      s.store(a.dS + chunk * DD, a, v0);
+      StatePart<KD, NV> before;
+      before.load(a.states + chunk * DD, a, v0);
+      const unsigned long long cuts = gate.cuts;
+      float* R = a.R + chunk * C * a.Dv;
 
-    for (int hi = C; hi > 0;) {  // pieces, the last first
-      int lo = 0;
-      for (int next = piece_end(cuts, lo); next < hi; next = piece_end(cuts, lo)) lo = next;
+      for (int hi = C; hi > 0;) {  // pieces, the last first
+        int lo = 0;
+        for (int next = piece_end(cuts, lo); next < hi; next = piece_end(cuts, lo)) lo = next;
+        float du[kTiles][4];
+        __syncwarp();
+        {  // dU = scale M^T dO + dec K dS
+          float d[kTiles][4] = {}, e[kTiles][4] = {};
+          if (hi == C) product<2, P, 3, kTiles, KD, false>(d, e, now.K, rb, sh.S, cb, 0);
+          named_sync(kToChain, kBothThreads);  // this piece's L and Od
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int i = rb + g + 8 * r;
-        const bool in = i >= lo && i < hi;
-        const float gam = in ? a.scale * gate.gam[i] : 0.0f;
+          for (int r = 0; r < 2; ++r) {
+            const int i = rb + g + 8 * r;
+            const bool in = i >= lo && i < hi;
+            const float beta = gate.beta[i], dec = gate.dec[i];
 #pragma unroll
-        for (int c = 0; c < kTiles; ++c) {
-          const float p = in ? on[c][r].x : 0.0f, q = in ? on[c][r].y : 0.0f;
-          sh.O.put(i, cb + c * 8 + 2 * t, p, q);
-          sh.Od.put(i, cb + c * 8 + 2 * t, gam * p, gam * q);
+            for (int c = 0; c < kTiles; ++c) {
+              const int col = cb + c * 8 + 2 * t;
+              const float2 l = *reinterpret_cast<const float2*>(sh.L + i * Sh::kLPitch + col);
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                const float far = hi == C ? dec * (d[c][2 * r + y] + e[c][2 * r + y]) : 0.0f;
+                du[c][2 * r + y] = in ? (y ? l.y : l.x) + far : 0.0f;
+              }
+              if (!came) du[c][0] = __int_as_float(0x7fffffff);
+              sh.Z.put(i, col, in ? beta * du[c][2 * r] : 0.0f, in ? beta * du[c][2 * r + 1] : 0.0f);
+            }
+          }
         }
+        named_sync(kChain, kChainThreads);
+        {  // R = dU - N^T B dU, dV = B R
+          float d[kTiles][4] = {}, e[kTiles][4] = {};
+          product_lower<2, 3, 3, kTiles, true>(d, e, now.N, rb, sh.Z, cb);
+          named_sync(kChain, kChainThreads);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const int i = rb + g + 8 * r, time = n * C + i;
+            const bool in = i >= lo && i < hi;
+            const float beta = gate.beta[i], back = -gate.gam[i];
+#pragma unroll
+            for (int c = 0; c < kTiles; ++c) {
+              const int col = cb + c * 8 + 2 * t;
+              const float p = in ? du[c][2 * r] - (d[c][2 * r] + e[c][2 * r]) : 0.0f;
+              const float q = in ? du[c][2 * r + 1] - (d[c][2 * r + 1] + e[c][2 * r + 1]) : 0.0f;
+              const float bp = in ? beta * p : 0.0f, bq = in ? beta * q : 0.0f;
+              if (lo == 0) sh.Z.put(i, col, in ? back * bp : 0.0f, in ? back * bq : 0.0f);
+              if (!in) continue;
+              put2(R + (long long)i * a.Dv, v0 + col, a.Dv, a.even, p, q);
+              if (time < len) put2(dv + time * a.dvs.t, v0 + col, a.Dv, a.pairs, bp, bq);
+            }
+          }
+        }
+        if (lo == 0 && cuts) {  // rows behind the first reset do not reach the state before
+          for (int i = threadIdx.x + hi * KD; i < C * KD; i += kChainThreads)
+#pragma unroll
+            for (int q = 0; q < P; ++q) now.K.p[q * now.K.kSize + i] = now.Q.p[q * now.Q.kSize + i] = from_f32<bf16>(0.0f);
+          fence_proxy_async_shared();
+        }
+        named_sync(kChain, kChainThreads);
+        if (lo > 0) named_arrive(kToSide, kBothThreads);  // L and Od have been read
+        hi = lo;
       }
-      __syncthreads();
-      float du[kTiles][4];
-      {  // dU = scale M^T dO + dec K dS
-        float d[kTiles][4] = {}, e[kTiles][4] = {};
-        if (hi == C) product<2, P, 3, kTiles, KD, false>(d, e, now.K, rb, sh.S, cb, 0);
+      // dS = gam_63 dS + Q^T scale gam dO - K^T gam dV
+      const float keep = gate.gam[C - 1];
+      s.each([&](int, int, float& p, float& q) { p = cuts ? 0.0f : keep * p, q = cuts ? 0.0f : keep * q; });
+      if (!(cuts & 1ull)) {
+        add_keys<P>(s, now.Q, sh.Od);
+        add_keys<P>(s, now.K, sh.Z);
+      }
+      ring.release(k);
+      s.split(sh.S);
+      float dot = 0.0f;
+#pragma unroll
+      for (int c = 0; c < s.kTiles; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) dot = cuts & 1ull ? 0.0f : fmaf(s.x[c][r], before.x[c][r], dot);
+#pragma unroll
+      for (int d = 16; d > 0; d /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, d);
+      if ((threadIdx.x & 31) == 0) sh.sums[warp] = dot;
+      if (k + 1 < chunks) named_arrive(kToSide, kBothThreads);
+      named_sync(kChain, kChainThreads);
+      if (threadIdx.x == 0) {
+        dot = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) dot += sh.sums[w];
+        a.dots[chunk * a.tiles + blockIdx.x % a.tiles] = dot;
+      }
+    }
+    s.store(a.dh0 + (long long)bh * DD, a, v0);
+    for (long long i = (long long)len * NV + threadIdx.x; i < (long long)a.T * NV; i += kChainThreads) {
+      const int c = v0 + (int)(i % NV);
+      if (c < a.Dv) dv[i / NV * a.dvs.t + c] = from_f32<T>(0.0f);
+    }
+  } else {
+    constexpr int kTiles = NV / 8;
+    const int rb = (warp - 8) * 16;
+    const T* d_o = static_cast<const T*>(a.d_o) + b * a.dos.b + h * a.dos.h;
+    Raw2<T> ox[kTiles][2];
+    auto fetch_o = [&](int n) {
+#pragma unroll
+      for (int c = 0; c < kTiles; ++c)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int time = n * C + rb + g + 8 * r;
+          ox[c][r].load(d_o + time * a.dos.t, v0 + c * 8 + 2 * t, a.Dv, a.pairs, n >= 0 && time < len);
+        }
+    };
+    fetch_o(chunks - 1);
+    for (int k = 0; k < chunks; ++k) {
+      const int n = chunks - 1 - k;
+      ring.wait_full(k);
+      __syncwarp();
+      const St now(smem + k % kN * St::kBytes);
+      const Gates& gate = *now.gates;
+      const unsigned long long cuts = gate.cuts;
+      float2 on[kTiles][2];
+#pragma unroll
+      for (int c = 0; c < kTiles; ++c) on[c][0] = ox[c][0].get(), on[c][1] = ox[c][1].get();
+      fetch_o(n - 1);
+      for (int hi = C; hi > 0;) {
+        int lo = 0;
+        for (int next = piece_end(cuts, lo); next < hi; next = piece_end(cuts, lo)) lo = next;
 #pragma unroll
         for (int c = 0; c < kTiles; ++c)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            du[c][r] = hi == C ? gate.dec[rb + g + 8 * (r >> 1)] * (d[c][r] + e[c][r]) : 0.0f;
-            d[c][r] = e[c][r] = 0.0f;
+          for (int r = 0; r < 2; ++r) {
+            const int i = rb + g + 8 * r;
+            const bool in = i >= lo && i < hi;
+            sh.O.put(i, c * 8 + 2 * t, in ? on[c][r].x : 0.0f, in ? on[c][r].y : 0.0f);
           }
-        product_lower<2, 3, P, kTiles, true>(d, e, now.M, rb, sh.O, cb);
+        named_sync(kSide, kSideThreads);
+        float d[kTiles][4] = {}, e[kTiles][4] = {};
+        product_lower<2, 3, P, kTiles, true>(d, e, now.M, rb, sh.O, 0);
+        if (lo == 0) ring.release(k);  // (the gates below are read before the chain is done with the chunk)
+        if (k > 0 || hi < C) named_sync(kToSide, kBothThreads);  // the L and Od before have been read
+        else named_sync(kSide, kSideThreads);                    // (O has been read by all, as behind the other barrier)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int i = rb + g + 8 * r;
           const bool in = i >= lo && i < hi;
-          const float beta = gate.beta[i];
+          const float gam = in ? a.scale * gate.gam[i] : 0.0f;
 #pragma unroll
           for (int c = 0; c < kTiles; ++c) {
-#pragma unroll
-            for (int y = 2 * r; y < 2 * r + 2; ++y) du[c][y] = in ? fmaf(a.scale, d[c][y] + e[c][y], du[c][y]) : 0.0f;
-            sh.Z.put(i, cb + c * 8 + 2 * t, in ? beta * du[c][2 * r] : 0.0f, in ? beta * du[c][2 * r + 1] : 0.0f);
+            const int col = c * 8 + 2 * t;
+            *reinterpret_cast<float2*>(sh.L + i * Sh::kLPitch + col) =
+                make_float2(a.scale * (d[c][2 * r] + e[c][2 * r]), a.scale * (d[c][2 * r + 1] + e[c][2 * r + 1]));
+            if (lo == 0) sh.Od.put(i, col, in ? gam * on[c][r].x : 0.0f, in ? gam * on[c][r].y : 0.0f);
           }
         }
+        named_arrive(kToChain, kBothThreads);
+        hi = lo;
       }
-      __syncthreads();
-      {  // R = dU - N^T B dU, dV = B R
-        float d[kTiles][4] = {}, e[kTiles][4] = {};
-        product_lower<2, 3, 3, kTiles, true>(d, e, now.N, rb, sh.Z, cb);
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int i = rb + g + 8 * r, time = n * C + i;
-          const bool in = i >= lo && i < hi;
-          const float beta = gate.beta[i], back = -gate.gam[i];
-#pragma unroll
-          for (int c = 0; c < kTiles; ++c) {
-            const int col = cb + c * 8 + 2 * t;
-            const float p = in ? du[c][2 * r] - (d[c][2 * r] + e[c][2 * r]) : 0.0f;
-            const float q = in ? du[c][2 * r + 1] - (d[c][2 * r + 1] + e[c][2 * r + 1]) : 0.0f;
-            const float bp = in ? beta * p : 0.0f, bq = in ? beta * q : 0.0f;
-            sh.Z.put(i, col, in ? back * bp : 0.0f, in ? back * bq : 0.0f);
-            if (!in) continue;
-            put2(R + (long long)i * a.Dv, v0 + col, a.Dv, a.even, p, q);
-            if (time < len) put2(dv + time * a.dvs.t, v0 + col, a.Dv, a.pairs, bp, bq);
-          }
-        }
-      }
-      if (lo == 0 && cuts)  // rows behind the first reset do not reach the state before
-        for (int i = threadIdx.x + hi * KD; i < C * KD; i += kThreads)
-#pragma unroll
-          for (int q = 0; q < P; ++q) now.K.p[q * now.K.kSize + i] = now.Q.p[q * now.Q.kSize + i] = from_f32<bf16>(0.0f);
-      __syncthreads();
-      if (lo == 0) {  // dS = gam_63 dS + Q^T scale gam dO - K^T gam dV
-        const float keep = gate.gam[C - 1];
-        s.each([&](int, int, float& p, float& q) { p = cuts ? 0.0f : keep * p, q = cuts ? 0.0f : keep * q; });
-        if (!(cuts & 1ull)) {
-          add_keys<P>(s, now.Q, sh.Od);
-          add_keys<P>(s, now.K, sh.Z);
-        }
-        s.split(sh.S);
-        float dot = 0.0f;
-#pragma unroll
-        for (int c = 0; c < s.kTiles; ++c)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) dot = cuts & 1ull ? 0.0f : fmaf(s.x[c][r], before.x[c][r], dot);
-#pragma unroll
-        for (int d = 16; d > 0; d /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, d);
-        if ((threadIdx.x & 31) == 0) sh.sums[warp] = dot;
-      }
-      hi = lo;
-      if (hi > 0) __syncthreads();
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      float dot = 0.0f;
-#pragma unroll
-      for (int w = 0; w < 8; ++w) dot += sh.sums[w];
-      a.dots[chunk * a.tiles + blockIdx.x % a.tiles] = dot;
-    }
-    if (cuts) fence_proxy_async_shared();
-    if constexpr (kTwo) {
-      if (turn > 0 && (warp != 7 || n == 0)) cluster_wait();
-      cluster_arrive();
-    } else {
-      cluster_sync_all();
-      if (asks && n > 0) St(smem).load(a, n - 1, b, h, rank, bar);
     }
   }
-  if (kTwo && chunks > 0) cluster_wait();
-  if (v0 >= a.Dv) return;
-  s.store(a.dh0 + (long long)bh * DD, a, v0);
-  for (long long i = (long long)len * NV + threadIdx.x; i < (long long)a.T * NV; i += kThreads) {
-    const int c = v0 + (int)(i % NV);
-    if (c < a.Dv) dv[i / NV * a.dvs.t + c] = from_f32<T>(0.0f);
-  }
+  cluster_sync_all();
 }
 
 // ---- per chunk and key head: the gradients of q, k, g and beta ---------------------
@@ -1219,15 +1300,15 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
       const bool mine = side < W / 8;  // this warp's 8 columns of a round's 16 or 32
       const int col = side * 8 + 2 * t;
       Raw2<T> vx[2], ox[2];
-      float2 rx[2];
+      Raw2<float> rx[2];
       auto fetch_rows = [&](int v0) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int i = rb + g + 8 * r;
           const bool in = mine && i >= lo && i < hi;
-          vx[r] = raw2(v + i * a.vs.t, v0 + col, a.Dv, a.pairs, in);
-          rx[r] = raw2(R + (long long)i * a.Dv, v0 + col, a.Dv, a.even, in);
-          ox[r] = raw2(d_o + i * a.dos.t, v0 + col, a.Dv, a.pairs, in);
+          vx[r].load(v + i * a.vs.t, v0 + col, a.Dv, a.pairs, in);
+          rx[r].load(R + (long long)i * a.Dv, v0 + col, a.Dv, a.even, in);
+          ox[r].load(d_o + i * a.dos.t, v0 + col, a.Dv, a.pairs, in);
         }
       };
       fetch_rows(0);
@@ -1246,9 +1327,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
         float2 vn[2], rn[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          vn[r] = Pair<T>::get(vx[r]), rn[r] = rx[r];
-          const float2 on = Pair<T>::get(ox[r]);
-          if (mine) sh.R.put(rb + g + 8 * r, col, rx[r].x, rx[r].y), sh.dO.put(rb + g + 8 * r, col, on.x, on.y);
+          vn[r] = vx[r].get(), rn[r] = rx[r].get();
+          const float2 on = ox[r].get();
+          if (mine) sh.R.put(rb + g + 8 * r, col, rn[r].x, rn[r].y), sh.dO.put(rb + g + 8 * r, col, on.x, on.y);
         }
         __syncthreads();
         if (v0 + W < a.Dv) {
@@ -1625,8 +1706,8 @@ extern "C" int lstm_approx_delta_scan(int dtype, const void* q, const void* k, c
     using Ty = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
     if constexpr (sizeof(Ty) == 2)
-      if (NV == 32) return launch_big<delta_forward_kernel<Ty, KD, 32>>(grid, ForwardShared<Ty, KD, 32>::kBytes, s, a, a.cluster);
-    return launch_big<delta_forward_kernel<Ty, KD, 16>>(grid, ForwardShared<Ty, KD, 16>::kBytes, s, a, a.cluster);
+      if (NV == 32) return launch_big<delta_forward_kernel<Ty, KD, 32>>(grid, ForwardShared<Ty, KD, 32>::kBytes, s, a, a.cluster, kAllThreads);
+    return launch_big<delta_forward_kernel<Ty, KD, 16>>(grid, ForwardShared<Ty, KD, 16>::kBytes, s, a, a.cluster, kAllThreads);
   });
   return op_launched(e, "delta scan launch", msg, msg_len);
 }
@@ -1681,8 +1762,8 @@ extern "C" int lstm_approx_delta_scan_backward(int dtype, const void* d_o, const
     using Ty = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
     if constexpr (sizeof(Ty) == 2)
-      if (NV == 32) return launch_big<delta_backward_kernel<Ty, KD, 32>>(grid, BackwardShared<Ty, KD, 32>::kBytes, s, a, a.cluster);
-    return launch_big<delta_backward_kernel<Ty, KD, 16>>(grid, BackwardShared<Ty, KD, 16>::kBytes, s, a, a.cluster);
+      if (NV == 32) return launch_big<delta_backward_kernel<Ty, KD, 32>>(grid, BackwardShared<Ty, KD, 32>::kBytes, s, a, a.cluster, kAllThreads);
+    return launch_big<delta_backward_kernel<Ty, KD, 16>>(grid, BackwardShared<Ty, KD, 16>::kBytes, s, a, a.cluster, kAllThreads);
   });
   if (int rc = op_launched(e, "delta scan backward launch", msg, msg_len)) return rc;
   if (T == 0) return LSTM_APPROX_OK;

@@ -81,6 +81,21 @@ __device__ __forceinline__ void mbar_arrive(uint32_t mb) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(mb) : "memory");
 }
 
+// At the barrier that a CTA of the cluster has at the same place (its address from mapa).
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t mb_cluster) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mb_cluster) : "memory");
+}
+
+// Barriers among some warps of a CTA (`threads` of them in all; 0 is __syncthreads'): with those that arrive, without waiting.
+__device__ __forceinline__ void named_sync(uint32_t id, uint32_t threads) {
+  __syncwarp();
+  asm volatile("barrier.cta.sync.aligned %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+__device__ __forceinline__ void named_arrive(uint32_t id, uint32_t threads) {
+  __syncwarp();
+  asm volatile("barrier.cta.arrive.aligned %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
 // One poll of an mbarrier phase (acquire at cluster scope, so data written
 // by st.async from other CTAs of the cluster is visible once it returns 1).
 // The suspend-time hint (ns) lets a waiting warp sleep in hardware instead
