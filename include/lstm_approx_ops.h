@@ -283,9 +283,10 @@ size_t lstm_approx_w4_workspace_bytes(int x_dtype, int M, int K);
  *             zero (the first token of a packed document), whatever it holds
  *   h_last    [B][H][Dk][Dv] fp32: the state after the stream's last timestep
  *             (h0 where it has none); may be h0 itself
- *   states    [ceil(T / LSTM_APPROX_DELTA_CHUNK)][B][H][Dk][Dv] fp32, or NULL:
- *             the state before every chunk's first timestep (of chunks that the
- *             stream reaches), kept for the backward pass
+ *   states    [ceil(T / LSTM_APPROX_DELTA_CHUNK)][B][H][Dk +
+ *             LSTM_APPROX_DELTA_CHUNK][Dv] fp32, or NULL: of every chunk that the
+ *             stream reaches the state before its first timestep, then u_t / beta_t
+ *             of its timesteps, kept for the backward pass
  *   workspace at least lstm_approx_delta_scan_workspace_bytes(dtype, T, B, H,
  *             Hk, Dk, Dv, 0) bytes, 16-byte aligned, not shared by calls in flight
  *

@@ -150,9 +150,9 @@ def gated_step(x, r, i, decay, state, *, c: float = 8.0, slots=None, reset=None,
 
 def delta_scan_states(q, v):
     """An empty ``states`` for :func:`delta_scan` of q [T, B, Hk, Dk] and v [T, B, H, Dv]: [ceil(T / DELTA_CHUNK), B, H,
-    Dk, Dv] fp32."""
+    Dk + DELTA_CHUNK, Dv] fp32."""
     _need(q.dim() == 4 and v.dim() == 4, "q must be [T, B, Hk, Dk] and v [T, B, H, Dv]")
-    return torch.empty(-(-q.shape[0] // DELTA_CHUNK), *v.shape[1:3], q.shape[3], v.shape[3], dtype=torch.float32,
+    return torch.empty(-(-q.shape[0] // DELTA_CHUNK), *v.shape[1:3], q.shape[3] + DELTA_CHUNK, v.shape[3], dtype=torch.float32,
                        device=q.device)
 
 

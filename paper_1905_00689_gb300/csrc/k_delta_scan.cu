@@ -372,7 +372,18 @@ __device__ __forceinline__ void fill_keys(const KeyMat<T, KD>& to, const T* p, l
   }
 }
 
-// One warp: a chunk's sums of g, the decays that follow, beta (rows lane and lane + 32).  The sums are of 64 bits, so that
+// high + low, low at most half a unit of high in its last place.  (A sum's rounding: what the terms lack of their own part of it.)
+struct TwoFloats {
+  float high, low;
+  __device__ __forceinline__ TwoFloats operator+(const TwoFloats& o) const {
+    const float s = __fadd_rn(high, o.high), mine = __fsub_rn(s, o.high);
+    const float rest = __fadd_rn(__fadd_rn(__fsub_rn(high, mine), __fsub_rn(o.high, __fsub_rn(s, mine))), __fadd_rn(low, o.low));
+    const float t = __fadd_rn(s, rest);
+    return {t, __fsub_rn(rest, __fsub_rn(t, s))};
+  }
+};
+
+// One warp: a chunk's sums of g, the decays that follow, beta (rows lane and lane + 32).  The sums are of two parts, so that
 // differences of far ones keep their digits, and begin anew at a reset, whose own g counts as zero.
 struct RawGates {
   float g[2], beta[2];
@@ -391,7 +402,7 @@ struct RawGates {
 };
 __device__ __forceinline__ void make_gates(const RawGates& raw, Gates& gates) {
   const int lane = threadIdx.x & 31;
-  double G[2];
+  TwoFloats G[2];
   unsigned cut[2];
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
@@ -402,26 +413,26 @@ __device__ __forceinline__ void make_gates(const RawGates& raw, Gates& gates) {
     cut[s] = __ballot_sync(0xffffffffu, reset);
     const unsigned before = cut[s] & (2u << lane) - 1u;
     const int start = before ? 31 - __clz((int)before) : 0;
-    double x = reset ? 0.0 : (double)g;
+    TwoFloats x{reset ? 0.0f : g, 0.0f};
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-      const double y = __shfl_up_sync(0xffffffffu, x, d);
-      if (lane - d >= start) x += y;
+      const TwoFloats y{__shfl_up_sync(0xffffffffu, x.high, d), __shfl_up_sync(0xffffffffu, x.low, d)};
+      if (lane - d >= start) x = y + x;
     }
     G[s] = x;
   }
-  const double first = __shfl_sync(0xffffffffu, G[0], 31);
-  if (!(cut[1] & (2u << lane) - 1u)) G[1] += first;
-  const double last = __shfl_sync(0xffffffffu, G[1], 31);
+  const TwoFloats first{__shfl_sync(0xffffffffu, G[0].high, 31), __shfl_sync(0xffffffffu, G[0].low, 31)};
+  if (!(cut[1] & (2u << lane) - 1u)) G[1] = first + G[1];
+  const TwoFloats last{__shfl_sync(0xffffffffu, G[1].high, 31), __shfl_sync(0xffffffffu, G[1].low, 31)};
   const unsigned long long cuts = cut[0] | (unsigned long long)cut[1] << 32;
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     const int row = lane + 32 * s;
-    const float high = (float)G[s], rest = (float)(G[s] - (double)high), e = expf(high);
-    gates.g_high[row] = high;
-    gates.g_low[row] = rest;
-    gates.gam[row] = cut_before(cuts, row) ? 0.0f : fmaf(e, rest, e);
-    gates.dec[row] = row < 63 && cuts >> (row + 1) ? 0.0f : expf((float)(last - G[s]));
+    const float e = expf(G[s].high);
+    gates.g_high[row] = G[s].high;
+    gates.g_low[row] = G[s].low;
+    gates.gam[row] = cut_before(cuts, row) ? 0.0f : fmaf(e, G[s].low, e);
+    gates.dec[row] = row < 63 && cuts >> (row + 1) ? 0.0f : expf((last.high - G[s].high) + (last.low - G[s].low));
   }
   if (lane == 0) gates.cuts = cuts, gates.pad = 0ull;
 }
@@ -830,12 +841,14 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
       for (int x = 0; x < kTiles; ++x) vn[x][0] = vx[x][0].get(), vn[x][1] = vx[x][1].get();
       if (!came) vn[0][0].x = __int_as_float(0x7fffffff);
       fetch_v(n + 1);
-      if (a.states) s.store(a.states + (((long long)n * a.B + b) * a.H + h) * DD, a, v0);
+      // S0 and Y for the backward pass
+      float* kept = a.states ? a.states + (((long long)n * a.B + b) * a.H + h) * (a.Dk + C) * a.Dv : nullptr;
+      if (kept) s.store(kept, a, v0);
       const unsigned long long cuts = gate.cuts;
 
       for (int lo = 0; lo < C;) {
         const int hi = piece_end(cuts, lo);
-        float x[kTiles][4];  // B X
+        float x[kTiles][4];  // X
         __syncwarp();
         {
           float d[kTiles][4] = {}, e[kTiles][4] = {};
@@ -847,9 +860,9 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
             const bool in = i >= lo && i < hi;
 #pragma unroll
             for (int c = 0; c < kTiles; ++c) {
-              x[c][2 * r] = in ? beta * (vn[c][r].x - gam * (d[c][2 * r] + e[c][2 * r])) : 0.0f;
-              x[c][2 * r + 1] = in ? beta * (vn[c][r].y - gam * (d[c][2 * r + 1] + e[c][2 * r + 1])) : 0.0f;
-              sh.X.put(i, cb + c * 8 + 2 * t, x[c][2 * r], x[c][2 * r + 1]);
+              x[c][2 * r] = vn[c][r].x - gam * (d[c][2 * r] + e[c][2 * r]);
+              x[c][2 * r + 1] = vn[c][r].y - gam * (d[c][2 * r + 1] + e[c][2 * r + 1]);
+              sh.X.put(i, cb + c * 8 + 2 * t, in ? beta * x[c][2 * r] : 0.0f, in ? beta * x[c][2 * r + 1] : 0.0f);
             }
           }
         }
@@ -865,8 +878,9 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
             const float beta = gate.beta[i], dec = gate.dec[i];
 #pragma unroll
             for (int c = 0; c < kTiles; ++c) {
-              const float p = in ? x[c][2 * r] - beta * (d[c][2 * r] + e[c][2 * r]) : 0.0f;
-              const float q = in ? x[c][2 * r + 1] - beta * (d[c][2 * r + 1] + e[c][2 * r + 1]) : 0.0f;
+              const float y = x[c][2 * r] - (d[c][2 * r] + e[c][2 * r]), z = x[c][2 * r + 1] - (d[c][2 * r + 1] + e[c][2 * r + 1]);
+              const float p = in ? beta * y : 0.0f, q = in ? beta * z : 0.0f;
+              if (kept && in) put2(kept + (long long)(a.Dk + i) * a.Dv, v0 + cb + c * 8 + 2 * t, a.Dv, a.even, y, z);
               sh.U.put(i, cb + c * 8 + 2 * t, p, q);
               if (hi == C) sh.Ud.put(i, cb + c * 8 + 2 * t, in ? dec * p : 0.0f, in ? dec * q : 0.0f);
             }
@@ -997,7 +1011,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
       const long long chunk = ((long long)n * a.B + b) * a.H + h;
       s.store(a.dS + chunk * DD, a, v0);
       StatePart<KD, NV> before;
-      before.load(a.states + chunk * DD, a, v0);
+      before.load(a.states + chunk * (a.Dk + C) * a.Dv, a, v0);
       const unsigned long long cuts = gate.cuts;
       float* R = a.R + chunk * C * a.Dv;
 
@@ -1168,27 +1182,26 @@ template <typename T, int KD>
 struct GradShared {
   static constexpr int W = kSlice<T, KD>, P = kParts<T>, kOut = kOutParts<T>;
   KeyMat<T, KD> K, Q;
-  SquareMat N;
   Gates* gates;
   float* sums;  // [3][4][C]
   float *next_S, *next_dS;  // the next round's, as they come
-  // one round's: S0, dS, dO, R, B X, U; after the last, P and E
+  // one round's: S0, dS, dO, R, U; after the last, P and E
   Mat<KD, W, 3> S;
   Mat<KD, W, kOut> dS;
   Mat<C, W, P> dO;
   Mat<C, W, kOut> R;
-  Mat<C, W, 3> X, U;
+  Mat<C, W, 3> U;
   SquareMat Pm;
   Mat<C, C, kOut> E;
-  static constexpr size_t kFixed = kKeysBytes<T, KD> + SquareMat::kBytes + sizeof(Gates) + 12 * C * 4 + 2 * KD * W * 4;
-  static constexpr size_t kRound = decltype(S)::kBytes + decltype(dS)::kBytes + decltype(dO)::kBytes + decltype(R)::kBytes + 2 * decltype(X)::kBytes;
+  static constexpr size_t kFixed = kKeysBytes<T, KD> + sizeof(Gates) + 12 * C * 4 + 2 * KD * W * 4;
+  static constexpr size_t kRound = decltype(S)::kBytes + decltype(dS)::kBytes + decltype(dO)::kBytes + decltype(R)::kBytes + decltype(U)::kBytes;
   static constexpr size_t kAfter = decltype(Pm)::kBytes + decltype(E)::kBytes;
   static constexpr size_t kBytes = kFixed + (kRound > kAfter ? kRound : kAfter);
   __device__ __forceinline__ explicit GradShared(unsigned char* p)
-      : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * P}, N{Q.p + Q.kSize * P}, gates(reinterpret_cast<Gates*>(N.p + N.kSize * 3)),
+      : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * P}, gates(reinterpret_cast<Gates*>(Q.p + Q.kSize * P)),
         sums(reinterpret_cast<float*>(gates + 1)), next_S(sums + 12 * C), next_dS(next_S + KD * W),
         S{reinterpret_cast<bf16*>(next_dS + KD * W)}, dS{S.p + S.kSize * 3}, dO{dS.p + dS.kSize * kOut}, R{dO.p + dO.kSize * P},
-        X{R.p + R.kSize * kOut}, U{X.p + X.kSize * 3}, Pm{S.p}, E{Pm.p + Pm.kSize * 3} {}
+        U{R.p + R.kSize * kOut}, Pm{S.p}, E{Pm.p + Pm.kSize * 3} {}
 };
 
 // [rows][W] values of a matrix [Dk][Dv] from column v0 on, as they come (zeros past its ends); `quads`: in 16-byte pieces.
@@ -1211,24 +1224,48 @@ __device__ __forceinline__ void fetch_slice(float* to, const float* from, int v0
   }
 }
 
-// acc += rows m0 of A (parts PA) times the transposed rows n0.. of B, over kLength columns; two tiles of 8 rows of B at a time,
-// summed apart first (an MMA's sum is cut, not rounded, to 24 bits).
-template <int kDepth, int PB, int kTiles, int kLength, int PA, typename MatB>
-__device__ __forceinline__ void add_rows(float (&acc)[kTiles][4], const uint32_t (&fa)[kLength / 16][PA][4], const MatB& B, int n0) {
+// x += A, y += B times the transposed rows n0.. of M (three parts), over kLength columns; two tiles of 8 rows
+// of M at a time, summed apart first (an MMA's sum is cut, not rounded, to 24 bits).
+template <int kDepth, int kTiles, int kLength, int PA, int PB, typename MatM>
+__device__ __forceinline__ void add_rows(float (&x)[kTiles][4], const uint32_t (&fa)[kLength / 16][PA][4], float (&y)[kTiles][4],
+                                         const uint32_t (&fb)[kLength / 16][PB][4], const MatM& M, int n0) {
 #pragma unroll
   for (int n = 0; n < kTiles; n += 2) {
-    float d[2][4] = {}, e[2][4] = {};
+    float d[2][4] = {}, e[2][4] = {}, f[2][4] = {};
 #pragma unroll
     for (int k = 0; k < kLength / 16; ++k) {
-      uint32_t fb[PB][2][2];
-      load_b<PB>(B, n0 + n * 8, k * 16, fb);
-      mma<kDepth>(d[0], e[0], fa[k], fb, 0);
-      mma<kDepth>(d[1], e[1], fa[k], fb, 1);
+      uint32_t m[3][2][2];
+      load_b<3>(M, n0 + n * 8, k * 16, m);
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        mma<2>(d[z], e[z], fa[k], m, z);
+        mma<kDepth>(f[z], f[z], fb[k], m, z);
+      }
     }
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int z = 0; z < 2; ++z)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) acc[n + x][r] += d[x][r] + e[x][r];
+      for (int r = 0; r < 4; ++r) x[n + z][r] += d[z][r] + e[z][r], y[n + z][r] += f[z][r];
+  }
+}
+// x += A times the transposed rows of M, in what goes into outputs alone.
+template <int kDepth, int kTiles, int kLength, int PA, int kHas, int kRows>
+__device__ __forceinline__ void add_rows(float (&x)[kTiles][4], const uint32_t (&fa)[kLength / 16][PA][4], const Mat<kRows, kLength, kHas>& M,
+                                         int n0) {
+#pragma unroll
+  for (int n = 0; n < kTiles; n += 2) {
+    float f[2][4] = {};
+#pragma unroll
+    for (int k = 0; k < kLength / 16; ++k) {
+      uint32_t m[kHas][2][2];
+      load_b<kHas>(M, n0 + n * 8, k * 16, m);
+      mma<kDepth>(f[0], f[0], fa[k], m, 0);
+      mma<kDepth>(f[1], f[1], fa[k], m, 1);
+    }
+#pragma unroll
+    for (int z = 0; z < 2; ++z)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[n + z][r] += f[z][r];
   }
 }
 
@@ -1266,10 +1303,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
     const long long chunk = ((long long)n * a.B + b) * a.H + h;
     const T* v = static_cast<const T*>(a.v) + t0 * a.vs.t + b * a.vs.b + h * a.vs.h;
     const T* d_o = static_cast<const T*>(a.d_o) + t0 * a.dos.t + b * a.dos.b + h * a.dos.h;
-    const float *S = a.states + chunk * DD, *dS = a.dS + chunk * DD, *R = a.R + chunk * C * a.Dv;
-    const unsigned char* head = a.heads + (size_t)chunk * kHeadBytes;
+    const float *S = a.states + chunk * (a.Dk + C) * a.Dv, *Y = S + DD, *dS = a.dS + chunk * DD, *R = a.R + chunk * C * a.Dv;
     __syncthreads();
-    fetch<(int)(SquareMat::kBytes + sizeof(Gates)), kGradThreads>(sh.N.p, head);
+    fetch<(int)sizeof(Gates), kGradThreads>(sh.gates, a.heads + (size_t)chunk * kHeadBytes + SquareMat::kBytes);
     if (h == hk * a.share) fetch<(int)kKeysBytes<T, KD>, kGradThreads>(sh.K.p, a.keys + where * kKeysBytes<T, KD>);
     fetch_slice<KD, W>(sh.next_S, S, 0, a.Dk, a.Dv, a.quads);
     fetch_slice<KD, W>(sh.next_dS, dS, 0, a.Dk, a.Dv, a.quads);
@@ -1300,7 +1336,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
       const bool mine = side < W / 8;  // this warp's 8 columns of a round's 16 or 32
       const int col = side * 8 + 2 * t;
       Raw2<T> vx[2], ox[2];
-      Raw2<float> rx[2];
+      Raw2<float> rx[2], yx[2];
       auto fetch_rows = [&](int v0) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -1308,6 +1344,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
           const bool in = mine && i >= lo && i < hi;
           vx[r].load(v + i * a.vs.t, v0 + col, a.Dv, a.pairs, in);
           rx[r].load(R + (long long)i * a.Dv, v0 + col, a.Dv, a.even, in);
+          yx[r].load(Y + (long long)i * a.Dv, v0 + col, a.Dv, a.even, in);
           ox[r].load(d_o + i * a.dos.t, v0 + col, a.Dv, a.pairs, in);
         }
       };
@@ -1324,12 +1361,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
           sh.S.put(r, c, x.x, x.y);
           sh.dS.put(r, c, y.x, y.y);
         }
-        float2 vn[2], rn[2];
+        if (mine) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          vn[r] = vx[r].get(), rn[r] = rx[r].get();
-          const float2 on = ox[r].get();
-          if (mine) sh.R.put(rb + g + 8 * r, col, rn[r].x, rn[r].y), sh.dO.put(rb + g + 8 * r, col, on.x, on.y);
+          for (int r = 0; r < 2; ++r) {
+            const int i = rb + g + 8 * r;
+            const bool in = i >= lo && i < hi;
+            const float beta = gate.beta[i];
+            const float2 vn = vx[r].get(), rn = rx[r].get(), yn = yx[r].get(), on = ox[r].get();
+            rv[r] = fmaf(rn.x, vn.x, fmaf(rn.y, vn.y, rv[r]));
+            ry[r] = fmaf(rn.x, yn.x, fmaf(rn.y, yn.y, ry[r]));
+            sh.R.put(i, col, rn.x, rn.y);
+            sh.dO.put(i, col, on.x, on.y);
+            sh.U.put(i, col, in ? beta * yn.x : 0.0f, in ? beta * yn.y : 0.0f);
+          }
         }
         __syncthreads();
         if (v0 + W < a.Dv) {
@@ -1338,58 +1382,23 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
           fetch_rows(v0 + W);
         }
         copies_commit();
-        float x[4];  // X
         __syncwarp();
-        if (mine) {
-          float d[1][4] = {}, e[1][4] = {};
-          if (!fresh) product<2, P, 3, 1, KD, false>(d, e, sh.K, rb, sh.S, side * 8, 0);
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const int i = rb + g + 8 * r;
-            const bool in = i >= lo && i < hi;
-            const float gam = gate.gam[i], beta = gate.beta[i];
-            x[2 * r] = in ? vn[r].x - gam * (d[0][2 * r] + e[0][2 * r]) : 0.0f;
-            x[2 * r + 1] = in ? vn[r].y - gam * (d[0][2 * r + 1] + e[0][2 * r + 1]) : 0.0f;
-            sh.X.put(i, col, in ? beta * x[2 * r] : 0.0f, in ? beta * x[2 * r + 1] : 0.0f);
-          }
-        }
-        __syncthreads();
-        if (mine) {
-          float d[1][4] = {}, e[1][4] = {};
-          product_lower<2, 3, 3, 1, false>(d, e, sh.N, rb, sh.X, side * 8);
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const int i = rb + g + 8 * r;
-            const bool in = i >= lo && i < hi;
-            const float beta = gate.beta[i];
-            const float y = in ? x[2 * r] - (d[0][2 * r] + e[0][2 * r]) : 0.0f;
-            const float z = in ? x[2 * r + 1] - (d[0][2 * r + 1] + e[0][2 * r + 1]) : 0.0f;
-            rv[r] = fmaf(rn[r].x, vn[r].x, fmaf(rn[r].y, vn[r].y, rv[r]));
-            ry[r] = fmaf(rn[r].x, y, fmaf(rn[r].y, z, ry[r]));
-            sh.U.put(i, col, in ? beta * y : 0.0f, in ? beta * z : 0.0f);
-          }
-        }
-        __syncthreads();
         const bool below = side * 16 <= rb;  // else the warp's part of P and E lies above the diagonal
         {
-          uint32_t fa[W / 16][P][4];
+          uint32_t fo[W / 16][P][4], fr[W / 16][kOut][4];
 #pragma unroll
-          for (int k = 0; k < W / 16; ++k) load_a<P>(sh.dO, rb, k * 16, fa[k]);
-          if (below) add_rows<2, 3, 2, W>(acc_p, fa, sh.U, side * 16);
-          if (!fresh) add_rows<2, 3, kTiles, W>(acc_q, fa, sh.S, side * kPart);
-        }
-        {
-          uint32_t fa[W / 16][kOut][4];
-#pragma unroll
-          for (int k = 0; k < W / 16; ++k) load_a<kOut>(sh.R, rb, k * 16, fa[k]);
-          if (below) add_rows<kDepth, kOut, 2, W>(acc_e, fa, sh.U, side * 16);
-          if (!fresh) add_rows<kDepth, kOut, kTiles, W>(acc_w, fa, sh.S, side * kPart);
+          for (int k = 0; k < W / 16; ++k) {
+            load_a<P>(sh.dO, rb, k * 16, fo[k]);
+            load_a<kOut>(sh.R, rb, k * 16, fr[k]);
+          }
+          if (below) add_rows<kDepth, 2, W>(acc_p, fo, acc_e, fr, sh.U, side * 16);
+          if (!fresh) add_rows<kDepth, kTiles, W>(acc_q, fo, acc_w, fr, sh.S, side * kPart);
         }
         if (last) {
           uint32_t fa[W / 16][kOut][4];
 #pragma unroll
           for (int k = 0; k < W / 16; ++k) load_a<kOut>(sh.U, rb, k * 16, fa[k]);
-          add_rows<kDepth, kOut, kTiles, W>(acc_t, fa, sh.dS, side * kPart);
+          add_rows<kDepth, kTiles, W>(acc_t, fa, sh.dS, side * kPart);
         }
       }
       __syncthreads();

@@ -580,7 +580,7 @@ PyObject* delta_scan(PyObject*, PyObject* const* a, Py_ssize_t) {
     const int32_t* lengths = static_cast<const int32_t*>(call.dense(a[7], "lengths", at::kInt, {B}));
     const unsigned char* reset = Sequence::resets(call, a[8], {T, B});
     float* states = static_cast<float*>(call.dense(
-        a[11], "states", at::kFloat, {(T + LSTM_APPROX_DELTA_CHUNK - 1) / LSTM_APPROX_DELTA_CHUNK, B, H, Dk, Dv}));
+        a[11], "states", at::kFloat, {(T + LSTM_APPROX_DELTA_CHUNK - 1) / LSTM_APPROX_DELTA_CHUNK, B, H, Dk + LSTM_APPROX_DELTA_CHUNK, Dv}));
     const float scale = heads.scale(a[6]);
     Tensor o = heads.out(call, a[9], "o", false);
     n = 9;
@@ -614,7 +614,7 @@ PyObject* delta_scan_backward(PyObject*, PyObject* const* a, Py_ssize_t) {
     const float* beta = heads.add_gate(call, tensor(a[5], "beta"), "beta", strides, n);
     const float* states = static_cast<const float*>(
         call.dense(tensor(a[6], "states"), "states", at::kFloat,
-                   {(T + LSTM_APPROX_DELTA_CHUNK - 1) / LSTM_APPROX_DELTA_CHUNK, B, H, Dk, Dv}));
+                   {(T + LSTM_APPROX_DELTA_CHUNK - 1) / LSTM_APPROX_DELTA_CHUNK, B, H, Dk + LSTM_APPROX_DELTA_CHUNK, Dv}));
     const float* dl = static_cast<const float*>(call.dense(a[7], "dh_last", at::kFloat, {B, H, Dk, Dv}));
     const int32_t* lengths = static_cast<const int32_t*>(call.dense(a[9], "lengths", at::kInt, {B}));
     const unsigned char* reset = Sequence::resets(call, a[10], {T, B});

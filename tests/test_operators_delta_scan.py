@@ -103,7 +103,7 @@ def test_backward(cuda_device, T, B, H, Hk, Dk, Dv, dtype):
     args = delta.tensors((T, B), H, Hk, Dk, Dv, dtype, 50 + T)
     do = torch.randn(T, B, H, Dv, device="cuda").to(args[0].dtype)
     states = delta_scan_states(args[0], args[2])
-    assert states.shape == (-(-T // 64), B, H, Dk, Dv)
+    assert states.shape == (-(-T // 64), B, H, Dk + 64, Dv)
     delta_scan(*args, states=states)
     compare_backward(do, args, delta_scan_backward(do, *args, states), dtype)
     lengths, reset = lengths_and_resets(T, B, T + 1)
@@ -168,7 +168,8 @@ def test_layouts(cuda_device, dtype, Dk, Dv):
         o = torch.full((B, H, T, Dv), float("nan"), dtype=v.dtype, device="cuda").permute(2, 0, 1, 3)
         other = torch.empty_like(states)
         got = delta_scan(q, k, v, g, beta, o=o, states=other)
-        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(other, states)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert torch.equal(other[0], states[0]) and torch.equal(other[1, :, :, :Dk + 26], states[1, :, :, :Dk + 26])
         dz = torch.full((T, B, 2 * Hk * Dk + H * Dv), float("nan"), dtype=v.dtype, device="cuda")
         dgates = torch.full((T, B, 2 * H), float("nan"), device="cuda")
         dq, dk, dv = dz.split((Hk * Dk, Hk * Dk, H * Dv), -1)
