@@ -312,6 +312,7 @@ def adamw_step(params, grads, state: AdamWState, step, *, lr, betas=(0.9, 0.999)
     CUDA bool of one value, where true nothing changes.
     """
     _need(len(betas) == 2, "betas must be two numbers")
+    _need(all(hasattr(x, "__iter__") for x in (params, grads)), "params and grads must be sequences of tensors")
     params, grads, copies = (x if x is None or isinstance(x, (list, tuple)) else list(x) for x in (params, grads, copies))
     args = (params, grads, state.exp_avg, state.exp_avg_sq, state.exp_avg_scale, state.exp_avg_sq_scale, copies, step, lr,
             betas[0], betas[1], eps, weight_decay, grad_scale, skip, seed)

@@ -6,8 +6,8 @@
 // Bound by memory: every value is read once and written once.  A warp takes
 // 256 neighbouring values of a tensor, which is also what shares a scale of
 // the 8-bit averages: their largest is one warp-wide maximum.  A block of 8
-// warps takes 2048 values; which tensor they belong to it finds in the table
-// that comes with the kernel's arguments (nothing is copied to the device
+// warps takes 2048 values at a time; which tensor they belong to it finds in the
+// table that comes with the kernel's arguments (nothing is copied to the device
 // before the launch, and a captured graph holds its own copy).
 //
 // The averages in 8 bits: m, and u = sqrt(v) (half the range of exponents), as
@@ -16,20 +16,30 @@
 // of their two neighbours with the chances that keep the mean: 16 bits from a
 // hash of seed, step and position for each.  A u above zero never becomes zero
 // (m / (0 + eps) would be a step of any size): it is at least the type's smallest.
+//
+// Measured, of the 6790 GB/s of a copy: 302 M parameters in 32 bits, gradients and
+// copies in 16: 1214 us (103%); the same with 8-bit averages 874 us (82%: the rounding
+// is 85 instructions a value, which with the waits fill the issue slots); 13 M in
+// 16 bits with 8-bit averages at odd addresses 62 us (31%: values one by one).
 #include <cuda_fp8.h>
 
 #include <cmath>
+#include <initializer_list>
+#include <type_traits>
 
 #include "ops_common.cuh"
+#include "ptx.cuh"
 
 namespace lstm_approx_impl {
 namespace {
+
+using namespace lstm_approx_dev;
 
 constexpr int kThreads = 256;
 constexpr int kTile = kThreads * 8;
 constexpr int kBlock = 256;  // values to a scale
 static_assert(kBlock == 32 * 8, "a warp's values share a scale");
-constexpr float kMost = 448.0f, kLeast = 1.953125e-3f, kMinScale = 1.17549435e-38f;  // of e4m3: largest, 2^-9; 2^-126
+constexpr float kMost = 448.0f, kMinScale = 1.17549435e-38f;  // of e4m3; 2^-126
 
 struct AdamWTensor {
   void *p, *m, *v, *copy;
@@ -38,16 +48,17 @@ struct AdamWTensor {
   long long n;
   unsigned long long first;  // of its values among those of all tensors
   unsigned tile;             // its first tile
-  unsigned char p_type, g_type, copy_type, wide;  // wide: 16 bytes (8-bit averages: 8) at a time
+  unsigned char p_type, g_type, copy_type;
 };
 
 struct AdamWShared {
   const int* step_at;
   const float *lr_at, *grad_scale;
   const unsigned char* skip;
-  float lr, log_b1, log_b2, b1, b1_rest, b2, b2_rest, eps, decay;
+  float lr, log_b1, log_b2, b1, b1_rest, b2, b2_rest, eps, decay, one;
   int step;
   unsigned seed;
+  int rounds;  // tiles to a block
 };
 
 // (The kernel's arguments may take 32764 bytes; few tensors get a small table, which is cheaper to launch.)
@@ -69,58 +80,66 @@ __device__ __forceinline__ unsigned mix(unsigned h) {
 }
 
 // Where a thread's e-th value lies in its warp's 256: 8 neighbours, or 32 apart.
-__device__ __forceinline__ int place(bool wide, int e) {
+__device__ __forceinline__ int place(bool near, int e) {
   const int lane = threadIdx.x & 31;
-  return wide ? lane * 8 + e : e * 32 + lane;
+  return near ? lane * 8 + e : e * 32 + lane;
 }
 
-// A thread's values of the 256 that begin at p; `left` of them lie in the tensor.
-template <typename T>
-__device__ __forceinline__ void get8(const T* p, bool wide, int left, float (&x)[8]) {
-  if (wide && left >= place(true, 8)) {
+// A thread's values of the 256 that begin at p, of a type known when the kernel runs.  kNear: p is a multiple of 16 bytes (of 8 for
+// 8-bit floats) and all of them lie in the tensor; else `left` do, and they are moved one by one.  (Whole pieces of 16 bytes shifted
+// into place between lanes took 80 us where this takes 62: 13 M parameters in 16 bits with 8-bit averages, at odd addresses.)
+template <bool kNear, typename T>
+__device__ __forceinline__ void get8(const T* p, int left, float (&x)[8]) {
+  if constexpr (kNear) {
     load8(p + place(true, 0), x);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = place(wide, e) < left ? to_f32(p[place(wide, e)]) : 0.0f;
+    for (int e = 0; e < 8; ++e) x[e] = place(false, e) < left ? to_f32(p[place(false, e)]) : 0.0f;
   }
 }
-template <typename T>
-__device__ __forceinline__ void put8(T* p, bool wide, int left, const float (&x)[8]) {
-  if (wide && left >= place(true, 8)) {
+template <bool kNear, typename T>
+__device__ __forceinline__ void put8(T* p, int left, const float (&x)[8]) {
+  if constexpr (kNear) {
     store8(p + place(true, 0), x);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (place(wide, e) < left) p[place(wide, e)] = from_f32<T>(x[e]);
+      if (place(false, e) < left) p[place(false, e)] = from_f32<T>(x[e]);
   }
 }
-__device__ __forceinline__ void get8(int type, const void* p, long long at, bool wide, int left, float (&x)[8]) {
-  if (type == LSTM_APPROX_OP_FP32) get8(static_cast<const float*>(p) + at, wide, left, x);
-  else if (type == LSTM_APPROX_OP_BF16) get8(static_cast<const __nv_bfloat16*>(p) + at, wide, left, x);
-  else get8(static_cast<const __half*>(p) + at, wide, left, x);
+template <bool kNear>
+__device__ __forceinline__ void get8(int type, const void* p, long long at, int left, float (&x)[8]) {
+  if (type == LSTM_APPROX_OP_FP32) get8<kNear>(static_cast<const float*>(p) + at, left, x);
+  else if (type == LSTM_APPROX_OP_BF16) get8<kNear>(static_cast<const __nv_bfloat16*>(p) + at, left, x);
+  else get8<kNear>(static_cast<const __half*>(p) + at, left, x);
 }
-__device__ __forceinline__ void put8(int type, void* p, long long at, bool wide, int left, const float (&x)[8]) {
-  if (type == LSTM_APPROX_OP_FP32) put8(static_cast<float*>(p) + at, wide, left, x);
-  else if (type == LSTM_APPROX_OP_BF16) put8(static_cast<__nv_bfloat16*>(p) + at, wide, left, x);
-  else put8(static_cast<__half*>(p) + at, wide, left, x);
+template <bool kNear>
+__device__ __forceinline__ void put8(int type, void* p, long long at, int left, const float (&x)[8]) {
+  if (type == LSTM_APPROX_OP_FP32) put8<kNear>(static_cast<float*>(p) + at, left, x);
+  else if (type == LSTM_APPROX_OP_BF16) put8<kNear>(static_cast<__nv_bfloat16*>(p) + at, left, x);
+  else put8<kNear>(static_cast<__half*>(p) + at, left, x);
 }
 
-// The same for 8-bit floats, as they lie in memory.
-__device__ __forceinline__ uint2 get8(const uint8_t* p, bool wide, int left) {
-  if (wide && left >= place(true, 8)) return *reinterpret_cast<const uint2*>(p + place(true, 0));
-  unsigned w[2] = {0u, 0u};
+// The same for 8-bit floats, four to a word.
+template <bool kNear>
+__device__ __forceinline__ uint2 get8(const uint8_t* p, int left) {
+  if constexpr (kNear) {
+    return *reinterpret_cast<const uint2*>(p + place(true, 0));
+  } else {
+    unsigned b[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (place(wide, e) < left) w[e / 4] |= (unsigned)p[place(wide, e)] << (8 * (e % 4));
-  return make_uint2(w[0], w[1]);
+    for (int e = 0; e < 8; ++e) b[e] = place(false, e) < left ? p[place(false, e)] : 0u;
+    return make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24);
+  }
 }
-__device__ __forceinline__ void put8(uint8_t* p, bool wide, int left, uint2 x) {
-  if (wide && left >= place(true, 8)) {
+template <bool kNear>
+__device__ __forceinline__ void put8(uint8_t* p, int left, uint2 x) {
+  if constexpr (kNear) {
     *reinterpret_cast<uint2*>(p + place(true, 0)) = x;
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (place(wide, e) < left) p[place(wide, e)] = (uint8_t)((e < 4 ? x.x : x.y) >> (8 * (e % 4)));
+      if (place(false, e) < left) p[place(false, e)] = (uint8_t)((e < 4 ? x.x : x.y) >> (8 * (e % 4)));
   }
 }
 __device__ __forceinline__ void from_e4m3(uint2 q, float (&x)[8]) {
@@ -133,38 +152,153 @@ __device__ __forceinline__ void from_e4m3(uint2 q, float (&x)[8]) {
     x[e + 1] = f.y;
   }
 }
-__device__ __forceinline__ uint2 to_e4m3(const float (&x)[8]) {  // (of values that the type holds)
-  unsigned w[2] = {0u, 0u};
-#pragma unroll
-  for (int e = 0; e < 8; e += 2)
-    w[e / 4] |= (unsigned)__nv_cvt_float2_to_fp8x2(make_float2(x[e], x[e + 1]), __NV_SATFINITE, __NV_E4M3) << (8 * (e % 4));
-  return make_uint2(w[0], w[1]);
+
+// x in [0, 448] as an e4m3 code in the upper byte, rounded to one of x's neighbours: the upper one if 16 random bits (bits 8 to 23
+// of `chance`) fall below x's share of the distance.  A code is a 32-bit float's exponent and upper 3 bits of fraction, less 960 (64
+// more, in 8 bits).  Below 2^-6 the type's values lie 2^-9 apart, as they do from 2^-6 to 2^-5: there x is taken 2^-6, 8 codes,
+// higher.  positive: not to zero.
+__device__ __forceinline__ unsigned code_of(float x, unsigned chance, bool positive) {
+  const bool small = x < 0.015625f;
+  if (small) x += 0.015625f;
+  unsigned c = __float_as_uint(x) * 16u + ((chance & 0xffff00u) | 0x40000080u);
+  if (small) c -= 8u << 24;
+  if (small && positive) c = max(c, 1u << 24);
+  return c;
+}
+// The upper bytes of four words.
+__device__ __forceinline__ unsigned upper_bytes(unsigned a, unsigned b, unsigned c, unsigned d) {
+  return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
 
-// x in [0, 448] to one of its neighbours in e4m3, the upper one if 16 random bits fall below its share of the distance.
-// Below 2^-6 the type's values lie 2^-9 apart, as they do from 2^-6 to 2^-5: there x is taken 2^-6 higher.
-__device__ __forceinline__ float to_neighbour(float x, unsigned bits16) {
-  const float up = x < 0.015625f ? 0.015625f : 0.0f;
-  const unsigned b = __float_as_uint(x + up) + (bits16 << 4) + 8u;
-  return __uint_as_float(b & ~0xfffffu) - up;
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
 }
-
 // The scale of a warp's 256 values (a NaN among them makes it one).
 __device__ __forceinline__ float scale_of(const float (&x)[8]) {
-  unsigned most = 0u;
+  float most = fabsf(x[0]);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(x[e]) & 0x7fffffffu);
-  const float s = __fdiv_rn(__uint_as_float(__reduce_max_sync(0xffffffffu, most)), kMost);
+  for (int e = 1; e < 8; ++e) most = max_or_nan(most, fabsf(x[e]));
+  const float s = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most) & 0x7fffffffu)) * (1.0f / kMost);
   return s < kMinScale ? kMinScale : s;
 }
 
+// sqrt x of two values: Newton's step on y = x^-1/2 with the exact remainder (P. Markstein, "Computation of elementary functions
+// on the IBM RISC System/6000 processor", 1990).  Rounded to the nearest for all of the 2^24 fractions and both parities of the
+// exponent; below 2^-126 x 2^63.
+__device__ __forceinline__ void roots_of(uint64_t x, float x0, float x1, float& u0, float& u1) {
+  float y0, y1;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(fmaxf(x0, kMinScale)));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(fmaxf(x1, kMinScale)));
+  const uint64_t y = f32x2(y0, y1), g = mul2(x, y), half = f32x2(0.5f, 0.5f), minus = f32x2(-1.0f, -1.0f);
+  f32x2_split(fma2(fma2(mul2(g, minus), g, x), mul2(y, half), g), u0, u1);
+}
+
 struct Rates {
-  float keep, step, root, eps;  // 1 - lr wd, lr / (1 - b1^t), (1 - b2^t)^-1/2
+  float keep, step, root, eps, one;  // 1 - lr wd, lr / (1 - b1^t), (1 - b2^t)^-1/2
 };
 
-template <int kBits, int kTensors>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ AdamWArgs<kTensors> a) {
-  __shared__ Rates rates_of_block;
+// What one tile needs beside its tensor.
+struct Update {
+  float clip, b1, b1_rest, b2, b2_rest;
+  unsigned key;  // of the random bits
+};
+
+// Loads, to be followed by update() when the rates are there.
+template <int kBits, bool kNear>
+struct Tile {
+  float p[8], g[8], m[8], v[8];
+  uint2 m8, v8;
+  float m_scale, v_scale;
+
+  __device__ __forceinline__ void load(const AdamWTensor& t, long long at, int left) {
+    get8<kNear>(t.p_type, t.p, at, left, p);
+    get8<kNear>(t.g_type, t.g, at, left, g);
+    if constexpr (kBits == 8) {
+      m8 = get8<kNear>(static_cast<const uint8_t*>(t.m) + at, left);
+      v8 = get8<kNear>(static_cast<const uint8_t*>(t.v) + at, left);
+      m_scale = t.m_scale[at / kBlock], v_scale = t.v_scale[at / kBlock];
+    } else {
+      get8<kNear>(static_cast<const float*>(t.m) + at, left, m);
+      get8<kNear>(static_cast<const float*>(t.v) + at, left, v);
+    }
+  }
+
+  // (Two values to an instruction; each operation rounded by itself, so that which neighbour an 8-bit average becomes follows from
+  // the formula alone.)
+  __device__ __forceinline__ void update(const AdamWTensor& t, long long at, int left, const Update& w, const Rates& r) {
+    float u[8];
+    if constexpr (kBits == 8) {
+      from_e4m3(m8, m);
+      from_e4m3(v8, v);
+    }
+    const uint64_t clip = f32x2(w.clip, w.clip), b1 = f32x2(w.b1, w.b1), b1_rest = f32x2(w.b1_rest, w.b1_rest);
+    const uint64_t b2 = f32x2(w.b2, w.b2), b2_rest = f32x2(w.b2_rest, w.b2_rest), keep = f32x2(r.keep, r.keep);
+    const uint64_t back = f32x2(-r.step, -r.step), root = f32x2(r.root, r.root), eps = f32x2(r.eps, r.eps), one = f32x2(r.one, r.one);
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const uint64_t gs = mul2(f32x2(g[e], g[e + 1]), clip);
+      uint64_t mm = f32x2(m[e], m[e + 1]), vv = f32x2(v[e], v[e + 1]);
+      if constexpr (kBits == 8) {
+        mm = mul2(mm, f32x2(m_scale, m_scale));
+        vv = mul2(vv, f32x2(v_scale, v_scale));
+        vv = mul2(vv, vv);
+      }
+      // (times one, which the compiler does not know: it would make one operation of a product and a sum)
+      mm = fma2(mul2(mm, b1), one, mul2(gs, b1_rest));
+      vv = fma2(mul2(vv, b2), one, mul2(mul2(gs, gs), b2_rest));
+      f32x2_split(mm, m[e], m[e + 1]);
+      f32x2_split(vv, v[e], v[e + 1]);
+      if constexpr (kBits == 8) {
+        roots_of(vv, v[e], v[e + 1], u[e], u[e + 1]);
+      } else {
+        asm("sqrt.approx.f32 %0, %1;" : "=f"(u[e]) : "f"(v[e]));
+        asm("sqrt.approx.f32 %0, %1;" : "=f"(u[e + 1]) : "f"(v[e + 1]));
+      }
+      float d0, d1;
+      f32x2_split(fma2(f32x2(u[e], u[e + 1]), root, eps), d0, d1);
+      const uint64_t ratio = mul2(mm, f32x2(rcp_approx(d0), rcp_approx(d1)));
+      f32x2_split(fma2(f32x2(p[e], p[e + 1]), keep, mul2(back, ratio)), p[e], p[e + 1]);
+    }
+    put8<kNear>(t.p_type, t.p, at, left, p);
+    if (t.copy) put8<kNear>(t.copy_type, t.copy, at, left, p);
+    if constexpr (kBits == 8) {
+      const float ms = scale_of(m), us = scale_of(u), m_inv = __frcp_rn(ms), u_inv = __frcp_rn(us);
+      const unsigned long long first = t.first + (unsigned long long)at;
+      const unsigned low = (unsigned)first, high = (unsigned)(first >> 32);
+      unsigned mc[8], uc[8], mq[2], uq[2];
+      auto round_all = [&](auto wraps) {
+        const unsigned key0 = w.key ^ high, key1 = w.key ^ (high + 1u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const unsigned where = low + place(kNear, e);
+          const unsigned chance = mix(where + (decltype(wraps)::value && where < low ? key1 : key0));
+          mc[e] = code_of(fminf(fabsf(m[e]) * m_inv, kMost), chance << 8, false);
+          uc[e] = code_of(fminf(u[e] * u_inv, kMost), chance >> 8, u[e] > 0.0f);
+        }
+      };
+      if (low > 0u - kBlock) round_all(std::true_type());  // positions pass a multiple of 2^32 among these
+      else round_all(std::false_type());
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const unsigned sign = upper_bytes(__float_as_uint(m[4 * x]), __float_as_uint(m[4 * x + 1]), __float_as_uint(m[4 * x + 2]),
+                                          __float_as_uint(m[4 * x + 3]));
+        mq[x] = upper_bytes(mc[4 * x], mc[4 * x + 1], mc[4 * x + 2], mc[4 * x + 3]) | (sign & 0x80808080u);
+        uq[x] = upper_bytes(uc[4 * x], uc[4 * x + 1], uc[4 * x + 2], uc[4 * x + 3]);
+      }
+      put8<kNear>(static_cast<uint8_t*>(t.m) + at, left, make_uint2(mq[0], mq[1]));
+      put8<kNear>(static_cast<uint8_t*>(t.v) + at, left, make_uint2(uq[0], uq[1]));
+      if ((threadIdx.x & 31) == 0) t.m_scale[at / kBlock] = ms, t.v_scale[at / kBlock] = us;
+    } else {
+      put8<kNear>(static_cast<float*>(t.m) + at, left, m);
+      put8<kNear>(static_cast<float*>(t.v) + at, left, v);
+    }
+  }
+};
+
+template <int kBits, int kTensors, bool kWide>
+__global__ void __launch_bounds__(kThreads, kBits == 8 ? 5 : 4) adamw_kernel(const __grid_constant__ AdamWArgs<kTensors> a) {
   begin_op();
   const AdamWShared& all = a.all;
   if (all.skip && *all.skip) return;
@@ -175,79 +309,33 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     else hi = mid - 1;
   }
   const AdamWTensor& t = a.t[lo];
-  const long long at = (long long)(blockIdx.x - t.tile) * kTile + (threadIdx.x >> 5) * kBlock;
-  const long long rest = t.n - at;
-  const int left = rest > kBlock ? kBlock : rest > 0 ? (int)rest : 0;
-  const bool wide = t.wide;
-
-  float p[8], g[8], m[8], v[8];
-  uint2 m8, v8;
-  float m_scale = 0.0f, v_scale = 0.0f;
-  get8(t.p_type, t.p, at, wide, left, p);
-  get8(t.g_type, t.g, at, wide, left, g);
-  if constexpr (kBits == 8) {
-    m8 = get8(static_cast<const uint8_t*>(t.m) + at, wide, left);
-    v8 = get8(static_cast<const uint8_t*>(t.v) + at, wide, left);
-    if (left > 0) m_scale = t.m_scale[at / kBlock], v_scale = t.v_scale[at / kBlock];
-  } else {
-    get8(static_cast<const float*>(t.m) + at, wide, left, m);
-    get8(static_cast<const float*>(t.v) + at, wide, left, v);
-  }
-  const float clip = all.grad_scale ? *all.grad_scale : 1.0f;
+  const long long tile = (long long)(blockIdx.x - t.tile) * all.rounds;
   const int step = all.step_at ? *all.step_at : all.step;
-  if (threadIdx.x == 0) {  // 1 - b^t = -(e^(t log b) - 1), without the cancellation of small t
-    const float lr = all.lr_at ? *all.lr_at : all.lr, n = (float)step;
-    rates_of_block = {1.0f - lr * all.decay, __fdiv_rn(lr, -expm1f(n * all.log_b1)),
-                      __frsqrt_rn(-expm1f(n * all.log_b2)), all.eps};
-  }
-  __syncthreads();
-  if (left == 0) return;
-  const Rates r = rates_of_block;
-
-  if constexpr (kBits == 8) {
-    from_e4m3(m8, m);
-    from_e4m3(v8, v);
-  }
-  float u[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float gs = g[e] * clip;
-    if constexpr (kBits == 8) {
-      m[e] *= m_scale;
-      v[e] *= v_scale;
-      v[e] *= v[e];
+  const Update w{all.grad_scale ? *all.grad_scale : 1.0f, all.b1, all.b1_rest, all.b2, all.b2_rest, mix(mix(all.seed + 1u) ^ (unsigned)step)};
+  Rates rates{};
+  auto run = [&](auto near, long long at, int left, bool first) {
+    Tile<kBits, decltype(near)::value> tile;
+    tile.load(t, at, left);
+    if (first) {  // 1 - b^t = -(e^(t log b) - 1), without the cancellation of small t; while the loads are under way
+      const float lr = all.lr_at ? *all.lr_at : all.lr, n = (float)step;
+      rates = {1.0f - lr * all.decay, __fdiv_rn(lr, -expm1f(n * all.log_b1)), __frsqrt_rn(-expm1f(n * all.log_b2)), all.eps, all.one};
     }
-    m[e] = fmaf(m[e], all.b1, gs * all.b1_rest);
-    v[e] = fmaf(v[e], all.b2, gs * gs * all.b2_rest);
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(u[e]) : "f"(v[e]));
-    p[e] = fmaf(p[e], r.keep, -r.step * __fdividef(m[e], fmaf(u[e], r.root, r.eps)));
-  }
-  put8(t.p_type, t.p, at, wide, left, p);
-  if (t.copy) put8(t.copy_type, t.copy, at, wide, left, p);
-  if constexpr (kBits == 8) {
-    const float ms = scale_of(m), us = scale_of(u), m_inv = __frcp_rn(ms), u_inv = __frcp_rn(us);
-    const unsigned key = mix(mix(all.seed + 1u) ^ (unsigned)step);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const unsigned long long where = t.first + (unsigned long long)(at + place(wide, e));
-      const unsigned chance = mix((unsigned)where + (key ^ (unsigned)(where >> 32)));
-      const float x = fabsf(m[e]) * m_inv, y = u[e] * u_inv;
-      m[e] = copysignf(to_neighbour(x > kMost ? kMost : x, chance & 0xffffu), m[e]);
-      const float z = to_neighbour(y > kMost ? kMost : y, chance >> 16);
-      u[e] = u[e] > 0.0f && z < kLeast ? kLeast : z;
-    }
-    put8(static_cast<uint8_t*>(t.m) + at, wide, left, to_e4m3(m));
-    put8(static_cast<uint8_t*>(t.v) + at, wide, left, to_e4m3(u));
-    if ((threadIdx.x & 31) == 0) t.m_scale[at / kBlock] = ms, t.v_scale[at / kBlock] = us;
-  } else {
-    put8(static_cast<float*>(t.m) + at, wide, left, m);
-    put8(static_cast<float*>(t.v) + at, wide, left, v);
+    tile.update(t, at, left, w, rates);
+  };
+#pragma unroll 1
+  for (int round = 0; round < all.rounds; ++round) {
+    const long long at = (tile + round) * kTile + (threadIdx.x >> 5) * kBlock, rest = t.n - at;
+    if (rest <= 0) return;
+    if (kWide && rest >= kBlock) run(std::true_type(), at, kBlock, round == 0);
+    else run(std::false_type(), at, rest < kBlock ? (int)rest : kBlock, round == 0);
   }
 }
 
 template <int kTensors>
-cudaError_t launch(int bits, const AdamWArgs<kTensors>& a, unsigned tiles, cudaStream_t s) {
-  return op_launch(bits == 8 ? adamw_kernel<8, kTensors> : adamw_kernel<32, kTensors>, dim3(tiles), dim3(kThreads), 0, s, a);
+cudaError_t launch(int bits, bool wide, const AdamWArgs<kTensors>& a, unsigned tiles, cudaStream_t s) {
+  auto kern = bits == 8 ? (wide ? adamw_kernel<8, kTensors, true> : adamw_kernel<8, kTensors, false>)
+                        : (wide ? adamw_kernel<32, kTensors, true> : adamw_kernel<32, kTensors, false>);
+  return op_launch(kern, dim3(tiles), dim3(kThreads), 0, s, a);
 }
 
 }  // namespace
@@ -285,45 +373,47 @@ extern "C" int lstm_approx_adamw_step(int count, const lstm_approx_adamw_tensor*
   if (int rc = op_check_device(msg, msg_len)) return rc;
 
   AdamWShared all{step_at, lr_at, grad_scale, skip, (float)lr, (float)std::log(beta1), (float)std::log(beta2), (float)beta1,
-                  (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, (float)weight_decay, step, seed};
+                  (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, (float)weight_decay, 1.0f, step, seed, 1};
   static thread_local AdamWArgs<kMany> args;  // (32 KB: not on the stack)
-  unsigned long long first = 0;
-  for (int i = 0; i < count;) {
-    args.count = 0;
-    long long tiles = 0;
-    for (; i < count && args.count < kMany; ++i) {
-      const lstm_approx_adamw_tensor& t = tensors[i];
-      const long long mine = (t.n + kTile - 1) / kTile;
-      const unsigned long long from = first;
-      if (t.n == 0 || !t.g) {
+  // What a block does once (its tensor, the rates) is a quarter of its instructions with one tile: four tiles to a block where
+  // there are enough of them for that (302 M parameters with 8-bit averages 1020 us with one, 890 with four).
+  long long all_tiles = 0;
+  for (int i = 0; i < count; ++i) all_tiles += (tensors[i].n + kTile - 1) / kTile;
+  all.rounds = all_tiles >= 152 * 32 ? 4 : 1;
+  const long long tile_values = (long long)kTile * all.rounds;
+  for (const bool wide : {true, false}) {  // those at multiples of 16 bytes (8, 8-bit averages), then the others
+    unsigned long long first = 0;
+    for (int i = 0; i < count;) {
+      args.count = 0;
+      long long tiles = 0;
+      for (; i < count && args.count < kMany; ++i) {
+        const lstm_approx_adamw_tensor& t = tensors[i];
+        const long long mine = (t.n + tile_values - 1) / tile_values;
+        const size_t state = bits == 8 ? 8 : 16;
+        const bool is_wide = op_aligned(t.p, 16) && op_aligned(t.g, 16) && op_aligned(t.m, state) && op_aligned(t.v, state) &&
+                             (!t.copy || op_aligned(t.copy, 16));
+        if (t.n > 0 && t.g && is_wide == wide) {
+          if (tiles + mine > 0x7fffffffll) break;  // (one tensor's are fewer)
+          args.t[args.count++] = {t.p, t.m, t.v, t.copy, t.g, t.m_scale, t.v_scale, t.n, first, (unsigned)tiles,
+                                  (unsigned char)t.p_dtype, (unsigned char)t.g_dtype, (unsigned char)t.copy_dtype};
+          tiles += mine;
+        }
         first += (unsigned long long)t.n;
-        continue;
       }
-      if (tiles + mine > 0x7fffffffll) {
-        if (args.count > 0) break;
-        return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "tensor %d: %lld values are too many", i, t.n);
+      if (args.count == 0) continue;
+      args.all = all;
+      cudaError_t e;
+      if (args.count <= kFew) {
+        AdamWArgs<kFew> few;
+        few.all = all;
+        few.count = args.count;
+        for (int k = 0; k < args.count; ++k) few.t[k] = args.t[k];
+        e = launch(bits, wide, few, (unsigned)tiles, static_cast<cudaStream_t>(cuda_stream));
+      } else {
+        e = launch(bits, wide, args, (unsigned)tiles, static_cast<cudaStream_t>(cuda_stream));
       }
-      first += (unsigned long long)t.n;
-      const size_t state = bits == 8 ? 8 : 16;
-      const bool wide = op_aligned(t.p, 16) && op_aligned(t.g, 16) && op_aligned(t.m, state) && op_aligned(t.v, state) &&
-                        (!t.copy || op_aligned(t.copy, 16));
-      args.t[args.count++] = {t.p, t.m, t.v, t.copy, t.g, t.m_scale, t.v_scale, t.n, from, (unsigned)tiles,
-                              (unsigned char)t.p_dtype, (unsigned char)t.g_dtype, (unsigned char)t.copy_dtype, wide};
-      tiles += mine;
+      if (int rc = op_launched(e, "adamw launch", msg, msg_len)) return rc;
     }
-    if (args.count == 0) continue;
-    args.all = all;
-    cudaError_t e;
-    if (args.count <= kFew) {
-      AdamWArgs<kFew> few;
-      few.all = all;
-      few.count = args.count;
-      for (int k = 0; k < args.count; ++k) few.t[k] = args.t[k];
-      e = launch(bits, few, (unsigned)tiles, static_cast<cudaStream_t>(cuda_stream));
-    } else {
-      e = launch(bits, args, (unsigned)tiles, static_cast<cudaStream_t>(cuda_stream));
-    }
-    if (int rc = op_launched(e, "adamw launch", msg, msg_len)) return rc;
   }
   return LSTM_APPROX_OK;
 }

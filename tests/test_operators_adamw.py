@@ -305,3 +305,33 @@ def test_refusals(lib):
                  dict(eps=float("inf")), dict(lr=float("inf")), dict(wd=float("nan")), dict(step_at=ctypes.c_void_p(2)),
                  dict(lr_at=ctypes.c_void_p(2))):
         assert call(**more) == EINVAL, more
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("dtype,gdtype", [("fp32", "fp32"), ("bf16", "fp16")])
+def test_every_alignment(cuda_device, bits, dtype, gdtype):
+    """Tensors that begin at any value of an allocation: the bits of the aligned ones, and nothing beside them is written."""
+    import torch
+    from paper_1905_00689_gb300 import AdamWState, adamw_step
+    n = 1000
+    base = make([n], dtype, gdtype, 11, 0, bits)
+    base = [x[0] for x in base if x is not None]
+    want = [t.clone() for t in base] + [torch.zeros(n, dtype=torch.float16, device="cuda")]
+    scales = lambda t: ([[t[4]], [t[5]]] if bits == 8 else [None, None])  # noqa: E731
+    adamw_step([want[0]], [want[1]], AdamWState([want[2]], [want[3]], *scales(want)), 3, lr=LR, copies=[want[-1]])
+    for shift in range(1, 17):
+        big = [torch.full((n + 40,), 1.0, device="cuda").to(t.dtype) for t in base[:4]] + \
+              [torch.ones(n + 40, dtype=torch.float16, device="cuda")]
+        # each of the five at a place of its own
+        at = [(shift * k) % 17 for k in (1, 3, 5, 7, 11)]
+        part = [b[a:a + n] for b, a in zip(big, at)]
+        for x, t in zip(part, base[:4]):
+            x.copy_(t)
+        own = [t.clone() for t in base[4:]]
+        adamw_step([part[0]], [part[1]], AdamWState([part[2]], [part[3]], *([[t] for t in own] if bits == 8 else [None, None])), 3,
+                   lr=LR, copies=[part[4]])
+        for k, (x, w) in enumerate(zip(part, want[:4] + want[-1:])):
+            assert torch.equal(x.view(torch.uint8), w.view(torch.uint8)), (shift, k)
+        for b, a in zip(big, at):
+            assert (b[:a].float() == 1).all() and (b[a + n:].float() == 1).all()
