@@ -55,8 +55,6 @@ using namespace lstm_approx_dev;
 constexpr int C = LSTM_APPROX_DELTA_CHUNK;
 static_assert(C == 64, "rows of a chunk");
 constexpr int kThreads = 256;
-constexpr int kPrepareThreads = 512;
-static_assert(kPrepareThreads == 2 * C * C / 16, "a pair of N's diagonal blocks to a thread");
 constexpr float kLeastG = -200.0f;
 
 using bf16 = __nv_bfloat16;
@@ -341,11 +339,11 @@ struct PrepareShared {
 // Rows of q or k as the MMAs read them: in parts, zeros past the stream's length and past Dk.
 template <typename T, int KD>
 __device__ __forceinline__ void fill_keys(const KeyMat<T, KD>& to, const T* p, long long t_stride, int rows, int Dk, bool wide) {
-  constexpr int kPer = 16 / (int)sizeof(T), kRounds = (C * (KD / kPer) + kPrepareThreads - 1) / kPrepareThreads;
+  constexpr int kPer = 16 / (int)sizeof(T), kRounds = C * (KD / kPer) / kThreads;
   uint4 raw[kRounds];
 #pragma unroll
   for (int x = 0; x < kRounds; ++x) {
-    const int i = threadIdx.x + x * kPrepareThreads, row = i / (KD / kPer), col = i % (KD / kPer) * kPer;
+    const int i = threadIdx.x + x * kThreads, row = i / (KD / kPer), col = i % (KD / kPer) * kPer;
     raw[x] = make_uint4(0u, 0u, 0u, 0u);
     if (row < rows && col < Dk) {
       if (wide) {
@@ -360,7 +358,7 @@ __device__ __forceinline__ void fill_keys(const KeyMat<T, KD>& to, const T* p, l
   }
 #pragma unroll
   for (int x = 0; x < kRounds; ++x) {
-    const int i = threadIdx.x + x * kPrepareThreads, row = i / (KD / kPer), col = i % (KD / kPer) * kPer;
+    const int i = threadIdx.x + x * kThreads, row = i / (KD / kPer), col = i % (KD / kPer) * kPer;
     if constexpr (std::is_same_v<T, bf16>) {
       *reinterpret_cast<uint4*>(to.p + to.at(row, col)) = raw[x];
     } else {
@@ -440,7 +438,7 @@ __device__ __forceinline__ void make_gates(const RawGates& raw, Gates& gates) {
 }
 
 template <typename T, int KD, bool kBackward>
-__global__ void __launch_bounds__(kPrepareThreads, 2) delta_prepare_kernel(const DeltaArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr int P = kParts<T>;
   using Sh = PrepareShared<T, KD, kBackward ? 3 : kOutParts<T>>;
@@ -452,35 +450,36 @@ __global__ void __launch_bounds__(kPrepareThreads, 2) delta_prepare_kernel(const
   const int t0 = n * C, rows = min(length_of(a, b) - t0, C);
   if (rows <= 0) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane_g(), t = lane_t();
-  const int i0 = (warp & 3) * 16, side = (warp >> 2) * 16;  // a warp's 16 rows and 16 columns
+  const int i0 = (warp & 3) * 16, side = (warp >> 2) * 32;  // a warp's 16 rows and 32 columns
   RawGates raw;
-  if (warp == kPrepareThreads / 32 - 1) raw.load(a, t0, rows, b, hk * a.share);
+  if (warp == 7) raw.load(a, t0, rows, b, hk * a.share);
   fill_keys<T, KD>(sh.K, static_cast<const T*>(a.k) + t0 * a.ks.t + b * a.ks.b + hk * a.ks.h, a.ks.t, rows, a.Dk, a.wide);
   fill_keys<T, KD>(sh.Q, static_cast<const T*>(a.q) + t0 * a.qs.t + b * a.qs.b + hk * a.qs.h, a.qs.t, rows, a.Dk, a.wide);
-  if (warp == kPrepareThreads / 32 - 1) make_gates(raw, gates);
+  if (warp == 7) make_gates(raw, gates);
   fence_proxy_async_shared();
   __syncthreads();
   if (threadIdx.x == 0)
     bulk_copy_s2g(a.keys + (size_t)blockIdx.x * kKeysBytes<T, KD>, smem_u32(smem), (uint32_t)kKeysBytes<T, KD>);
   __syncwarp();
 
-  float kk[2][4] = {}, qk[2][4] = {};  // K K^T and Q K^T
-  if (side <= i0) {
-    float ke[2][4] = {}, qe[2][4] = {};
+  float kk[4][4] = {}, qk[4][4] = {};  // K K^T and Q K^T
+  if (side < i0 + 16) {
+    float ke[4][4] = {}, qe[4][4] = {};
 #pragma unroll
     for (int k0 = 0; k0 < KD; k0 += 16) {
-      uint32_t fk[P][4], fq[P][4], fb[P][2][2];
+      uint32_t fk[P][4], fq[P][4], fb[2][P][2][2];
       load_a<P>(sh.K, i0, k0, fk);
       load_a<P>(sh.Q, i0, k0, fq);
-      load_b<P>(sh.K, side, k0, fb);
+      load_b<P>(sh.K, side, k0, fb[0]);
+      load_b<P>(sh.K, side + 16, k0, fb[1]);
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        mma<2>(kk[x], ke[x], fk, fb, x);
-        mma<2>(qk[x], qe[x], fq, fb, x);
+      for (int x = 0; x < 4; ++x) {
+        mma<2>(kk[x], ke[x], fk, fb[x >> 1], x & 1);
+        mma<2>(qk[x], qe[x], fq, fb[x >> 1], x & 1);
       }
     }
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < 4; ++x)
 #pragma unroll
       for (int r = 0; r < 4; ++r) kk[x][r] += ke[x][r], qk[x][r] += qe[x][r];
   }
@@ -489,7 +488,7 @@ __global__ void __launch_bounds__(kPrepareThreads, 2) delta_prepare_kernel(const
     if (threadIdx.x == 0) bulk_wait_read();  // of K and Q, or of the head before
     __syncthreads();
     if (h > hk * a.share) {
-      if (warp == kPrepareThreads / 32 - 1) {
+      if (warp == 7) {
         raw.load(a, t0, rows, b, h);
         make_gates(raw, gates);
       }
@@ -497,11 +496,11 @@ __global__ void __launch_bounds__(kPrepareThreads, 2) delta_prepare_kernel(const
     }
     const unsigned long long cuts = gates.cuts;
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < 4; ++x)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int i = i0 + g + 8 * r, j = side + x * 8 + 2 * t;
-        if (side > i0) {
+        if (side + x * 8 >= i0 + 16) {
           sh.M.put(i, j, 0.0f, 0.0f);
           sh.N.put(i, j, 0.0f, 0.0f);
           continue;
@@ -517,7 +516,7 @@ __global__ void __launch_bounds__(kPrepareThreads, 2) delta_prepare_kernel(const
           w[y] = v[y] != 0.0f ? v[y] * gates.beta[j + y] : 0.0f;  // (beta of another document: anything)
         }
         sh.M.put(i, j, m[0], m[1]);
-        if (side < i0) sh.AB.put(i, j, w[0], w[1]);
+        if (side + x * 8 < i0) sh.AB.put(i, j, w[0], w[1]);
         *reinterpret_cast<float2*>(sh.A + i * kPitch + j) = make_float2(v[0], v[1]);
       }
     __syncthreads();
@@ -544,8 +543,9 @@ __global__ void __launch_bounds__(kPrepareThreads, 2) delta_prepare_kernel(const
       if (cuts) x = cut_between(cuts, j, i) ? 0.0f : x, y = cut_between(cuts, j + 1, i) ? 0.0f : y;
       sh.N.put(i, j, x, y);
     };
-    {
-      const int p = threadIdx.x, o = p / 128 * 16, i = o + p % 128 / 8, j = o + p % 8 * 2;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int p = threadIdx.x + x * kThreads, o = p / 128 * 16, i = o + p % 128 / 8, j = o + p % 8 * 2;
       const float2 v = *reinterpret_cast<const float2*>(sh.A + i * kPitch + j);
       put_n(i, j, v.x, v.y);
     }
@@ -553,7 +553,7 @@ __global__ void __launch_bounds__(kPrepareThreads, 2) delta_prepare_kernel(const
     // for [L 0; X R]: N_X = H - N_R B H with H = X - X B N_L; tiles of 16 x 8
 #pragma unroll
     for (int half = 16; half < C; half *= 2) {
-      const bool mine = warp < (half == 32 ? 8 : 4);
+      const bool mine = half == 32 || warp < 4;
       const int o = half == 16 ? (warp >> 1 & 1) * 32 : 0;               // the block's first row
       const int r0 = half == 16 ? 0 : (warp & 1) * 16;                   // the tile in X
       const int c0 = half == 16 ? (warp & 1) * 8 : (warp >> 1) * 8;
@@ -1636,8 +1636,8 @@ cudaError_t prepare(int dtype, const DeltaArgs& a, bool backward, cudaStream_t s
     using T = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
     const dim3 grid((unsigned)blocks);
-    if (backward) return launch_big<delta_prepare_kernel<T, KD, true>>(grid, PrepareShared<T, KD, 3>::kBytes, s, a, 1, kPrepareThreads);
-    return launch_big<delta_prepare_kernel<T, KD, false>>(grid, PrepareShared<T, KD, kOutParts<T>>::kBytes, s, a, 1, kPrepareThreads);
+    if (backward) return launch_big<delta_prepare_kernel<T, KD, true>>(grid, PrepareShared<T, KD, 3>::kBytes, s, a);
+    return launch_big<delta_prepare_kernel<T, KD, false>>(grid, PrepareShared<T, KD, kOutParts<T>>::kBytes, s, a);
   });
 }
 
