@@ -55,16 +55,6 @@ __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Its two halves: every thread of the cluster arrives, and waits before it arrives again.
-__device__ __forceinline__ void cluster_arrive() {
-  __syncwarp();
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_wait() {
-  __syncwarp();
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
 __device__ __forceinline__ void fence_mbarrier_init_cluster() {
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 }
@@ -431,17 +421,6 @@ __device__ __forceinline__ void mma_16816_f16(float (&d)[4], uint32_t a0, uint32
                : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(kFirst ? 0.0f : d[0]), "f"(kFirst ? 0.0f : d[1]),
                  "f"(kFirst ? 0.0f : d[2]), "f"(kFirst ? 0.0f : d[3]));
-}
-
-// d += a b for a 16 x 8, b 8 x 8 and d 16 x 8 fp32, of 32-bit floats of which a sign, 8 bits of exponent and 10 of fraction
-// are read: a0 and a1 rows g and g + 8 of a column of a, b0 the same row of b; a2, a3 and b1 another one.
-template <bool kTogether>
-__device__ __forceinline__ void mma_1688_tf32(float (&d)[4], float a0, float a1, float a2, float a3, float b0, float b1) {
-  if constexpr (!kTogether) __syncwarp();
-  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(__float_as_uint(a0)), "r"(__float_as_uint(a1)), "r"(__float_as_uint(a2)), "r"(__float_as_uint(a3)),
-                 "r"(__float_as_uint(b0)), "r"(__float_as_uint(b1)));
 }
 
 // Four 8 x 8 matrices of 16-bit values, lane l giving the address of row l % 8 of matrix l / 8: a lane gets columns 2 t and
