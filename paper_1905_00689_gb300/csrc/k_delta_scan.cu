@@ -651,6 +651,12 @@ constexpr int kChainThreads = 256, kSideThreads = 128, kBothThreads = kChainThre
 constexpr uint32_t kChain = 1, kSide = 2, kToSide = 3, kToChain = 4, kStateToSide = 5;
 
 // Two rings of barriers of a block: a stage's chunk has come; all warps of the cluster have read it.
+//
+// A warp has read its own block's shared memory when it arrives at the other blocks' barriers, and a load that has its value does not
+// see what is copied there afterwards: the order within its block is all that an arrival has to give (what the warp wrote into the
+// stage is another matter).  One that orders for the cluster waits for all loads and stores of the warp under way, those of other
+// chunks' values among them, in the middle of a chunk: 8191 timesteps of 16 heads took 342 us instead of 292, 319 when every block's
+// warps arrived at home and the thread that asks for the copies at the cluster's barriers.
 template <int kN>
 struct Ring {
   uint32_t full, empty;  // addresses
@@ -664,7 +670,7 @@ struct Ring {
   }
   // The k-th chunk (once a wait has run out, no further one is waited for).
   __device__ __forceinline__ bool wait_full(int k) {
-    ok = ok && mbar_wait_bounded<true>(full + k % kN * 8, (uint32_t)(k / kN) & 1u, kWaitNs, &g_never);
+    ok = ok && mbar_wait_bounded<false>(full + k % kN * 8, (uint32_t)(k / kN) & 1u, kWaitNs, &g_never);
     return ok;
   }
   __device__ __forceinline__ bool wait_empty(int k) {
@@ -894,7 +900,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
           for (int i = threadIdx.x; i < lo * KD; i += kChainThreads)
 #pragma unroll
             for (int q = 0; q < P; ++q) now.K.p[q * now.K.kSize + i] = from_f32<bf16>(0.0f);
-          fence_proxy_async_shared();  // (before a copy overwrites them)
+          fence_proxy_async_shared(), fence_cluster();  // (before another block's copy overwrites them)
         }
         named_arrive(kToSide, kBothThreads);
         named_sync(kChain, kChainThreads);
@@ -1074,7 +1080,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
           for (int i = threadIdx.x + hi * KD; i < C * KD; i += kChainThreads)
 #pragma unroll
             for (int q = 0; q < P; ++q) now.K.p[q * now.K.kSize + i] = now.Q.p[q * now.Q.kSize + i] = from_f32<bf16>(0.0f);
-          fence_proxy_async_shared();
+          fence_proxy_async_shared(), fence_cluster();
         }
         named_sync(kChain, kChainThreads);
         if (lo > 0) named_arrive(kToSide, kBothThreads);  // L and Od have been read

@@ -71,9 +71,14 @@ __device__ __forceinline__ void mbar_arrive(uint32_t mb) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(mb) : "memory");
 }
 
-// At the barrier that a CTA of the cluster has at the same place (its address from mapa).
+// At the barrier that a CTA of the cluster has at the same place (its address from mapa): orders what went before for the thread's
+// own CTA alone.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t mb_cluster) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mb_cluster) : "memory");
+  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(mb_cluster) : "memory");
+}
+
+__device__ __forceinline__ void fence_cluster() {
+  asm volatile("fence.acq_rel.cluster;" ::: "memory");
 }
 
 // Barriers among some warps of a CTA (`threads` of them in all; 0 is __syncthreads'): with those that arrive, without waiting.
