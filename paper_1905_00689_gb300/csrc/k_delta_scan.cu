@@ -1190,11 +1190,11 @@ constexpr int kGradThreads = 512;
 
 template <typename T, int KD>
 struct GradShared {
-  static constexpr int W = kSlice<T, KD>, P = kParts<T>, kOut = kOutParts<T>;
+  static constexpr int W = kSlice<T, KD>, P = kParts<T>, kOut = kOutParts<T>, kPitch = W + 8;  // (of R and Y: a warp reads 8 rows)
   KeyMat<T, KD> K, Q;
   Gates* gates;
   float* sums;  // [3][4][C]
-  float *next_S, *next_dS;  // the next round's, as they come
+  float *next_S, *next_dS, *next_R, *next_Y;  // the next round's, as they come
   // one round's: S0, dS, dO, R, U; after the last, P and E
   Mat<KD, W, 3> S;
   Mat<KD, W, kOut> dS;
@@ -1203,33 +1203,34 @@ struct GradShared {
   Mat<C, W, 3> U;
   SquareMat Pm;
   Mat<C, C, kOut> E;
-  static constexpr size_t kFixed = kKeysBytes<T, KD> + sizeof(Gates) + 12 * C * 4 + 2 * KD * W * 4;
+  static constexpr size_t kFixed = kKeysBytes<T, KD> + sizeof(Gates) + 12 * C * 4 + 2 * KD * W * 4 + 2 * C * kPitch * 4;
   static constexpr size_t kRound = decltype(S)::kBytes + decltype(dS)::kBytes + decltype(dO)::kBytes + decltype(R)::kBytes + decltype(U)::kBytes;
   static constexpr size_t kAfter = decltype(Pm)::kBytes + decltype(E)::kBytes;
   static constexpr size_t kBytes = kFixed + (kRound > kAfter ? kRound : kAfter);
   __device__ __forceinline__ explicit GradShared(unsigned char* p)
       : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * P}, gates(reinterpret_cast<Gates*>(Q.p + Q.kSize * P)),
         sums(reinterpret_cast<float*>(gates + 1)), next_S(sums + 12 * C), next_dS(next_S + KD * W),
-        S{reinterpret_cast<bf16*>(next_dS + KD * W)}, dS{S.p + S.kSize * 3}, dO{dS.p + dS.kSize * kOut}, R{dO.p + dO.kSize * P},
+        next_R(next_dS + KD * W), next_Y(next_R + C * kPitch), S{reinterpret_cast<bf16*>(next_Y + C * kPitch)}, dS{S.p + S.kSize * 3},
+        dO{dS.p + dS.kSize * kOut}, R{dO.p + dO.kSize * P},
         U{R.p + R.kSize * kOut}, Pm{S.p}, E{Pm.p + Pm.kSize * 3} {}
 };
 
-// [rows][W] values of a matrix [Dk][Dv] from column v0 on, as they come (zeros past its ends); `quads`: in 16-byte pieces.
-template <int KD, int W>
-__device__ __forceinline__ void fetch_slice(float* to, const float* from, int v0, int Dk, int Dv, bool quads) {
+// [kRows][W] values of a matrix [rows][Dv] from column v0 on, as they come (zeros past its ends); `quads`: in 16-byte pieces.
+template <int kRows, int W, int kPitch>
+__device__ __forceinline__ void fetch_slice(float* to, const float* from, int v0, int rows, int Dv, bool quads) {
   if (quads) {
 #pragma unroll
-    for (int i = threadIdx.x; i < KD * W / 4; i += kGradThreads) {
+    for (int i = threadIdx.x; i < kRows * W / 4; i += kGradThreads) {
       const int r = i / (W / 4), c = i % (W / 4) * 4;
-      const bool in = r < Dk && v0 + c < Dv;
-      copy16(to + i * 4, in ? from + (long long)r * Dv + v0 + c : from, in ? 16 : 0);
+      const bool in = r < rows && v0 + c < Dv;
+      copy16(to + r * kPitch + c, in ? from + (long long)r * Dv + v0 + c : from, in ? 16 : 0);
     }
   } else {
 #pragma unroll 4
-    for (int i = threadIdx.x; i < KD * W; i += kGradThreads) {
+    for (int i = threadIdx.x; i < kRows * W; i += kGradThreads) {
       const int r = i / W, c = i % W;
-      const bool in = r < Dk && v0 + c < Dv;
-      copy4(to + i, in ? from + (long long)r * Dv + v0 + c : from, in ? 4 : 0);
+      const bool in = r < rows && v0 + c < Dv;
+      copy4(to + r * kPitch + c, in ? from + (long long)r * Dv + v0 + c : from, in ? 4 : 0);
     }
   }
 }
@@ -1284,7 +1285,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr int W = kSlice<T, KD>, P = kParts<T>, kOut = kOutParts<T>, kDepth = kOutDepth<T>;
   constexpr int kPart = KD / 4, kTiles = kPart / 8;  // a warp has 16 rows and a quarter of the columns
-  const GradShared<T, KD> sh(smem);
+  using Sh = GradShared<T, KD>;
+  const Sh sh(smem);
   const Gates& gate = *sh.gates;
   begin_op();
   const int Hk = a.H / a.share;
@@ -1317,9 +1319,29 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
     __syncthreads();
     fetch<(int)sizeof(Gates), kGradThreads>(sh.gates, a.heads + (size_t)chunk * kHeadBytes + SquareMat::kBytes);
     if (h == hk * a.share) fetch<(int)kKeysBytes<T, KD>, kGradThreads>(sh.K.p, a.keys + where * kKeysBytes<T, KD>);
-    fetch_slice<KD, W>(sh.next_S, S, 0, a.Dk, a.Dv, a.quads);
-    fetch_slice<KD, W>(sh.next_dS, dS, 0, a.Dk, a.Dv, a.quads);
-    copies_commit();
+    // (R and Y as copies too: held in registers while a round is multiplied, the forward and backward passes took 636 us, not 611,
+    // for 4 streams of 8 heads and 2048 timesteps.)
+    auto fetch_slices = [&](int v0) {
+      fetch_slice<KD, W, W>(sh.next_S, S, v0, a.Dk, a.Dv, a.quads);
+      fetch_slice<KD, W, W>(sh.next_dS, dS, v0, a.Dk, a.Dv, a.quads);
+      fetch_slice<C, W, Sh::kPitch>(sh.next_R, R, v0, rows, a.Dv, a.quads);
+      fetch_slice<C, W, Sh::kPitch>(sh.next_Y, Y, v0, rows, a.Dv, a.quads);
+      copies_commit();
+    };
+    fetch_slices(0);
+    const bool mine = side < W / 8;  // this warp's 8 columns of a round's 16 or 32
+    const int col = side * 8 + 2 * t;
+    Raw2<T> vx[2], ox[2];
+    auto fetch_rows = [&](int v0) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int i = rb + g + 8 * r;
+        const bool in = mine && i < rows;
+        vx[r].load(v + i * a.vs.t, v0 + col, a.Dv, a.pairs, in);
+        ox[r].load(d_o + i * a.dos.t, v0 + col, a.Dv, a.pairs, in);
+      }
+    };
+    fetch_rows(0);
     copies_wait<0>();
     __syncthreads();
     const unsigned long long cuts = gate.cuts;
@@ -1330,9 +1352,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
       if (cuts) {  // this piece's keys and the first slices anew
         __syncthreads();
         fetch<(int)kKeysBytes<T, KD>, kGradThreads>(sh.K.p, a.keys + where * kKeysBytes<T, KD>);
-        fetch_slice<KD, W>(sh.next_S, S, 0, a.Dk, a.Dv, a.quads);
-        fetch_slice<KD, W>(sh.next_dS, dS, 0, a.Dk, a.Dv, a.quads);
-        copies_commit();
+        fetch_slices(0);
         copies_wait<0>();
         __syncthreads();
         for (int i = threadIdx.x; i < C * KD; i += kGradThreads)
@@ -1343,22 +1363,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
       float acc_q[kTiles][4] = {}, acc_w[kTiles][4] = {}, acc_t[kTiles][4] = {};  // dO S0^T, R S0^T, U dS^T
       float acc_p[2][4] = {}, acc_e[2][4] = {};                                  // dO U^T, R U^T
       float rv[2] = {}, ry[2] = {};                                              // R . V, R . Y
-      const bool mine = side < W / 8;  // this warp's 8 columns of a round's 16 or 32
-      const int col = side * 8 + 2 * t;
-      Raw2<T> vx[2], ox[2];
-      Raw2<float> rx[2], yx[2];
-      auto fetch_rows = [&](int v0) {
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int i = rb + g + 8 * r;
-          const bool in = mine && i >= lo && i < hi;
-          vx[r].load(v + i * a.vs.t, v0 + col, a.Dv, a.pairs, in);
-          rx[r].load(R + (long long)i * a.Dv, v0 + col, a.Dv, a.even, in);
-          yx[r].load(Y + (long long)i * a.Dv, v0 + col, a.Dv, a.even, in);
-          ox[r].load(d_o + i * a.dos.t, v0 + col, a.Dv, a.pairs, in);
-        }
-      };
-      fetch_rows(0);
+      if (lo > 0) fetch_rows(0);
 
       for (int v0 = 0; v0 < a.Dv; v0 += W) {
         copies_wait<0>();
@@ -1377,7 +1382,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
             const int i = rb + g + 8 * r;
             const bool in = i >= lo && i < hi;
             const float beta = gate.beta[i];
-            const float2 vn = vx[r].get(), rn = rx[r].get(), yn = yx[r].get(), on = ox[r].get();
+            const float2 vn = in ? vx[r].get() : zero, on = in ? ox[r].get() : zero;
+            const float2 rn = in ? *reinterpret_cast<const float2*>(sh.next_R + i * Sh::kPitch + col) : zero;
+            const float2 yn = in ? *reinterpret_cast<const float2*>(sh.next_Y + i * Sh::kPitch + col) : zero;
             rv[r] = fmaf(rn.x, vn.x, fmaf(rn.y, vn.y, rv[r]));
             ry[r] = fmaf(rn.x, yn.x, fmaf(rn.y, yn.y, ry[r]));
             sh.R.put(i, col, rn.x, rn.y);
@@ -1387,11 +1394,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
         }
         __syncthreads();
         if (v0 + W < a.Dv) {
-          fetch_slice<KD, W>(sh.next_S, S, v0 + W, a.Dk, a.Dv, a.quads);
-          fetch_slice<KD, W>(sh.next_dS, dS, v0 + W, a.Dk, a.Dv, a.quads);
+          fetch_slices(v0 + W);
           fetch_rows(v0 + W);
         }
-        copies_commit();
         __syncwarp();
         const bool below = side * 16 <= rb;  // else the warp's part of P and E lies above the diagonal
         {
