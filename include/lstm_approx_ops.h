@@ -290,8 +290,8 @@ size_t lstm_approx_w4_workspace_bytes(int x_dtype, int M, int K);
  *   workspace at least lstm_approx_delta_scan_workspace_bytes(dtype, T, B, H,
  *             Hk, Dk, Dv, 0) bytes, 16-byte aligned, not shared by calls in flight
  *
- * Values that are not finite stay in their stream, head and (from the next
- * reset on) document, but reach earlier timesteps of their chunk.
+ * Values are finite and below 2^127.  Others stay in their stream, head and (from
+ * the next reset on) document, but reach earlier timesteps of their chunk.
  */
 #define LSTM_APPROX_DELTA_CHUNK 64
 int lstm_approx_delta_scan(int dtype, const void *q, const void *k, const void *v, const float *g,
@@ -312,7 +312,8 @@ size_t lstm_approx_delta_scan_workspace_bytes(int dtype, int T, int B, int H, in
  *             output
  *   dq, dk    [T][B][Hk][Dk] dtype, summed over the value heads that share
  *             them;  dv [T][B][H][Dv] dtype;  dg, dbeta [T][B][H] fp32
- *             (all zero past a stream's length);  dh0 [B][H][Dk][Dv] fp32
+ *             (all zero past a stream's length);  dh0 [B][H][Dk][Dv] fp32, may be
+ *             dh_last itself
  *   strides   HOST [29]: the t, b and head strides of d_o, q, k, v, dq, dk and dv,
  *             the t and b strides of g, beta, dg and dbeta, in this order; NULL:
  *             all contiguous

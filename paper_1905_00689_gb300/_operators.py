@@ -171,7 +171,8 @@ def delta_scan(q, k, v, g, beta, h0=None, *, scale=None, lengths=None, reset=Non
     scale: None for Dk ** -0.5.  h0 [B, H, Dk, Dv] fp32 or None; lengths [B]
     int32: the timesteps of each stream; reset [T, B] bool or uint8: where true, the
     state before counts as zero.  ``states`` (:func:`delta_scan_states`) receives
-    what :func:`delta_scan_backward` needs.
+    what :func:`delta_scan_backward` needs.  h_last may be h0 itself; no other output
+    shares memory with an input or another output.  Values are finite, below 2 ** 127.
     """
     args = (q, k, v, g, beta, h0, scale, lengths, reset, o, h_last, states, workspace)
     return _ops.delta_scan(*args) if stream is None else _on(stream, _ops.delta_scan, *args)
@@ -182,7 +183,8 @@ def delta_scan_backward(do, q, k, v, g, beta, states, dh_last=None, *, scale=Non
     """Gradients of :func:`delta_scan` (same q, k, v, g, beta, scale, lengths and
     reset; the states it wrote): (dq, dk, dv, dg, dbeta, dh0), those of q and k
     summed over the value heads that share them.  dq, dk and dv may be given with
-    any t, b and head strides, as slices of one projection's gradient.
+    any t, b and head strides, as slices of one projection's gradient.  No output
+    shares memory with an input or another output (dh0 may be dh_last itself).
     """
     args = (do, q, k, v, g, beta, states, dh_last, scale, lengths, reset, dq, dk, dv, dg, dbeta, dh0, workspace)
     return _ops.delta_scan_backward(*args) if stream is None else _on(stream, _ops.delta_scan_backward, *args)
@@ -193,7 +195,8 @@ def delta_step(q, k, v, g, beta, state, *, scale=None, slots=None, reset=None, o
     beta [B, H]: returns o [B, H, Dv] and updates state [n_slots, H, Dk, Dv]
     fp32 in place.  slots [B] int32: the row of
     state of each stream (None: row b); one outside [0, n_slots) marks an idle
-    stream, whose o is zero.  reset [B]: where true the state counts as zero.
+    stream, whose o is zero; those in range are distinct.  reset [B]: where true the
+    state counts as zero.
     """
     args = (q, k, v, g, beta, state, scale, slots, reset, o)
     return _ops.delta_step(*args) if stream is None else _on(stream, _ops.delta_step, *args)

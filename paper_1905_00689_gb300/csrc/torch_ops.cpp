@@ -553,11 +553,15 @@ struct Heads {
     for (size_t k = 0; k < lead.size(); ++k) strides[n++] = t.stride(k);
     return static_cast<float*>(p);
   }
-  Tensor out(const Call& call, PyObject* o, const char* name, bool keys) const {
-    if (o == Py_None) return call.out(o, name, type, shape(keys));
-    Call::written(tensor(o, name));
-    return tensor(o, name);
+  // The caller's tensor of any strides, no value of it at two places, or a new one.
+  static Tensor out(const Call& call, PyObject* o, const char* name, at::ScalarType type, const std::vector<int64_t>& shape) {
+    if (o == Py_None) return call.out(o, name, type, shape);
+    const Tensor& t = tensor(o, name);
+    for (int64_t k = 0; k < t.dim(); ++k) need(t.size(k) < 2 || t.stride(k) != 0, "an output must not be an expanded tensor");
+    Call::written(t);
+    return t;
   }
+  Tensor out(const Call& call, PyObject* o, const char* name, bool keys) const { return out(call, o, name, type, shape(keys)); }
   float scale(PyObject* o) const { return o == Py_None ? (float)(1.0 / std::sqrt((double)Dk)) : real(o); }
 };
 
@@ -620,12 +624,7 @@ PyObject* delta_scan_backward(PyObject*, PyObject* const* a, Py_ssize_t) {
     const unsigned char* reset = Sequence::resets(call, a[10], {T, B});
     const float scale = heads.scale(a[8]);
     Tensor dq = heads.out(call, a[11], "dq", true), dk = heads.out(call, a[12], "dk", true), dv = heads.out(call, a[13], "dv", false);
-    auto gate_out = [&](PyObject* o, const char* name) {
-      if (o == Py_None) return call.out(o, name, at::kFloat, heads.per_head());
-      Call::written(tensor(o, name));
-      return tensor(o, name);
-    };
-    Tensor dg = gate_out(a[14], "dg"), dbeta = gate_out(a[15], "dbeta");
+    Tensor dg = Heads::out(call, a[14], "dg", at::kFloat, heads.per_head()), dbeta = Heads::out(call, a[15], "dbeta", at::kFloat, heads.per_head());
     n = 12;
     void* pdq = heads.add(call, dq, "dq", true, strides, n);
     void* pdk = heads.add(call, dk, "dk", true, strides, n);

@@ -416,3 +416,45 @@ def test_refuses_tensors(cuda_device):
     wide = torch.zeros(4, 1, 1, 129, device="cuda")
     with pytest.raises((ValueError, RuntimeError)):
         delta_scan(wide, wide, wide, wide[..., 0], wide[..., 0])
+
+
+@pytest.mark.gpu
+def test_refuses_expanded_outputs(cuda_device):
+    """Several places of such an output would be one; inputs may be expanded, and count as their copies do."""
+    import torch
+    from paper_1905_00689_gb300 import delta_scan, delta_scan_backward, delta_scan_states, delta_step
+    T, B, H, Hk, Dk, Dv = 70, 2, 4, 2, 32, 16
+    q, k, v, g, beta = delta.tensors((T, B), H, Hk, Dk, Dv, "bf16", 1)
+    states, do = delta_scan_states(q, v), torch.randn(T, B, H, Dv, device="cuda").bfloat16()
+
+    def same(t):
+        return t[:, :1].expand(t.shape)
+    with pytest.raises(ValueError):
+        delta_scan(q, k, v, g, beta, o=same(torch.empty_like(v)))
+    with pytest.raises(ValueError):
+        delta_step(q[0], k[0], v[0], g[0], beta[0], torch.zeros(B, H, Dk, Dv, device="cuda"), o=torch.empty_like(v[0])[:1].expand(v[0].shape))
+    for name, like in (("dq", q), ("dk", k), ("dv", v), ("dg", g), ("dbeta", beta)):
+        with pytest.raises(ValueError):
+            delta_scan_backward(do, q, k, v, g, beta, states, **{name: same(torch.empty_like(like))})
+    args = [same(t) for t in (q, k, v, g, beta)]
+    got = delta_scan(*args, states=states)
+    grads = delta_scan_backward(same(do), *args, states)
+    args = [t.contiguous() for t in args]
+    want = delta_scan(*args, states=states)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert all(torch.equal(a, b) for a, b in zip(grads, delta_scan_backward(same(do).contiguous(), *args, states)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,B,H,Hk,Dk,Dv", [(130, 3, 4, 2, 64, 70), (0, 2, 2, 1, 16, 5)])
+def test_gradient_of_the_first_state_over_that_of_the_last(cuda_device, T, B, H, Hk, Dk, Dv):
+    import torch
+    from paper_1905_00689_gb300 import delta_scan, delta_scan_backward, delta_scan_states
+    args = delta.tensors((T, B), H, Hk, Dk, Dv, "bf16", 5)
+    states, do = delta_scan_states(args[0], args[2]), torch.randn(T, B, H, Dv, device="cuda").bfloat16()
+    lengths = torch.tensor([T, 0, 70][:B], dtype=torch.int32, device="cuda")
+    delta_scan(*args, states=states, lengths=lengths)
+    held = torch.randn(B, H, Dk, Dv, device="cuda")
+    want = delta_scan_backward(do, *args, states, held.clone(), lengths=lengths)
+    got = delta_scan_backward(do, *args, states, held, lengths=lengths, dh0=held)
+    assert got[5] is held and all(torch.equal(a, b) for a, b in zip(got, want))
