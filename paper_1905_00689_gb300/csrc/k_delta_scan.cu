@@ -40,6 +40,13 @@
 // used, in two parts of 11 bits on MMAs of 32-bit floats, these kernels executed
 // 4 times the instructions: a chunk of 64 x 128 x 16 took 5.1 us.)
 //
+// Measured, bf16 and 128 x 128 states: 8191 timesteps of 16 heads 368 us (77 the
+// chunks' matrices, 292 along them: 2.3 us a chunk, of which the products are 0.75
+// of the tensor pipes; 18 times the time of its bytes at a copy's rate), 4 streams of
+// 2048 timesteps and 8 heads forward and backward 611 us (44 + 142, 46 + 188 + 230;
+// 30 times).  Bound by what follows one another: three products of 64 x 128 x 16 and
+// four barriers to a chunk, T / 64 chunks.
+//
 // At a reset the state before counts as zero, and so does everything before it
 // in its chunk: a chunk with resets is taken piece by piece, and rows of other
 // pieces are left out, not multiplied by zero.
@@ -437,6 +444,8 @@ __device__ __forceinline__ void make_gates(const RawGates& raw, Gates& gates) {
   if (lane == 0) gates.cuts = cuts, gates.pad = 0ull;
 }
 
+// Two blocks to an SM, so that one's loads and barriers lie behind the other's products: 2048 chunks of 128 wide bf16 keys 77 us, in
+// which 284 MB move (43 us at a copy's rate).  (With 16 warps to a block registers spill: 88.)
 template <typename T, int KD, bool kBackward>
 __global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
@@ -614,7 +623,8 @@ __global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaA
 // ---- along the chunks -------------------------------------------------------------
 
 // What a chunk brings along: parts of K and Q, N, gates, M.  The blocks of a cluster have the same head: each asks for its share
-// and sends it to all (from L2, 16 heads of 8 blocks would otherwise take 73 KB to a block and chunk: 3400 cycles).
+// and sends it to all (from L2, 16 heads of 8 blocks would otherwise take 73 KB to a block and chunk, 9.4 MB to every
+// 2.3 us of the device).
 template <typename T, int KD, int kMParts>
 struct Stage {
   KeyMat<T, KD> K, Q;
@@ -793,8 +803,8 @@ struct ForwardShared {
   __device__ __forceinline__ SMat state(int n) const { return SMat{S.p + (n & 1) * S.kSize * 3}; }
 };
 
-// Warps 0 to 7: X, Y and the next state.  Warps 8 to 11: O, from the state and U.  (All of it by 8 warps: 0.6 us of 2.8 us to a
-// chunk of 64 x 128 x 16.)
+// Warps 0 to 7: X, Y and the next state.  Warps 8 to 11: O, from the state and U.  (When 8 warps did all of it, a chunk of 64 x 128
+// x 16 took 2.8 us instead of 2.2.)
 template <typename T, int KD, int NV>
 __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
@@ -1280,6 +1290,8 @@ __device__ __forceinline__ void add_rows(float (&x)[kTiles][4], const uint32_t (
   }
 }
 
+// By columns of S, 32 at a time: the next ones come as copies while 16 warps multiply.  1024 chunks of bf16, 128 x 128: 230 us, half
+// of it without the products (splitting, the first slices, barriers: one block fills an SM), which take 50 us of the tensor pipes.
 template <typename T, int KD>
 __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
