@@ -43,7 +43,7 @@
 // Measured, bf16 and 128 x 128 states: 8191 timesteps of 16 heads 368 us (77 the
 // chunks' matrices, 292 along them: 2.3 us a chunk, of which the products are 0.75
 // of the tensor pipes; 18 times the time of its bytes at a copy's rate), 4 streams of
-// 2048 timesteps and 8 heads forward and backward 611 us (44 + 142, 46 + 188 + 230;
+// 2048 timesteps and 8 heads forward and backward 602 us (44 + 142, 46 + 188 + 204;
 // 30 times).  Bound by what follows one another: three products of 64 x 128 x 16 and
 // four barriers to a chunk, T / 64 chunks.
 //
@@ -98,6 +98,19 @@ struct Mat {
         const float2 f = __bfloat1622float2(h);
         x -= f.x;
         y -= f.y;
+      }
+    }
+  }
+  // Four of them (col a multiple of 4).
+  __device__ __forceinline__ void put4(int row, int col, float4 x) const {
+    const int i = at(row, col);
+#pragma unroll
+    for (int q = 0; q < kP; ++q) {
+      const __nv_bfloat162 h[2] = {__floats2bfloat162_rn(x.x, x.y), __floats2bfloat162_rn(x.z, x.w)};
+      *reinterpret_cast<uint2*>(p + q * kSize + i) = *reinterpret_cast<const uint2*>(h);
+      if (q + 1 < kP) {
+        const float2 f = __bfloat1622float2(h[0]), g = __bfloat1622float2(h[1]);
+        x = make_float4(x.x - f.x, x.y - f.y, x.z - g.x, x.w - g.y);
       }
     }
   }
@@ -1200,12 +1213,13 @@ constexpr int kGradThreads = 512;
 
 template <typename T, int KD>
 struct GradShared {
-  static constexpr int W = kSlice<T, KD>, P = kParts<T>, kOut = kOutParts<T>, kPitch = W + 8;  // (of R and Y: a warp reads 8 rows)
+  static constexpr int W = kSlice<T, KD>, P = kParts<T>, kOut = kOutParts<T>;
   KeyMat<T, KD> K, Q;
   Gates* gates;
-  float* sums;  // [3][4][C]
+  float* sums;                                // [6][C]
   float *next_S, *next_dS, *next_R, *next_Y;  // the next round's, as they come
-  // one round's: S0, dS, dO, R, U; after the last, P and E
+  // one round's: S0, dS, dO, R, U; after the last, P and E.  (Two rounds in turn, so that a warp splits one while others multiply the
+  // one before, leave the L1 little: 612 us where this takes 602, forward and backward of 4 streams of 8 heads and 2048 timesteps.)
   Mat<KD, W, 3> S;
   Mat<KD, W, kOut> dS;
   Mat<C, W, P> dO;
@@ -1213,36 +1227,40 @@ struct GradShared {
   Mat<C, W, 3> U;
   SquareMat Pm;
   Mat<C, C, kOut> E;
-  static constexpr size_t kFixed = kKeysBytes<T, KD> + sizeof(Gates) + 12 * C * 4 + 2 * KD * W * 4 + 2 * C * kPitch * 4;
+  static constexpr size_t kFixed = kKeysBytes<T, KD> + sizeof(Gates) + 6 * C * 4 + 2 * (KD + C) * W * 4;
   static constexpr size_t kRound = decltype(S)::kBytes + decltype(dS)::kBytes + decltype(dO)::kBytes + decltype(R)::kBytes + decltype(U)::kBytes;
   static constexpr size_t kAfter = decltype(Pm)::kBytes + decltype(E)::kBytes;
   static constexpr size_t kBytes = kFixed + (kRound > kAfter ? kRound : kAfter);
   __device__ __forceinline__ explicit GradShared(unsigned char* p)
       : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * P}, gates(reinterpret_cast<Gates*>(Q.p + Q.kSize * P)),
-        sums(reinterpret_cast<float*>(gates + 1)), next_S(sums + 12 * C), next_dS(next_S + KD * W),
-        next_R(next_dS + KD * W), next_Y(next_R + C * kPitch), S{reinterpret_cast<bf16*>(next_Y + C * kPitch)}, dS{S.p + S.kSize * 3},
-        dO{dS.p + dS.kSize * kOut}, R{dO.p + dO.kSize * P},
-        U{R.p + R.kSize * kOut}, Pm{S.p}, E{Pm.p + Pm.kSize * 3} {}
+        sums(reinterpret_cast<float*>(gates + 1)), next_S(sums + 6 * C), next_dS(next_S + KD * W), next_R(next_dS + KD * W),
+        next_Y(next_R + C * W), S{reinterpret_cast<bf16*>(next_Y + C * W)}, dS{S.p + S.kSize * 3}, dO{dS.p + dS.kSize * kOut},
+        R{dO.p + dO.kSize * P}, U{R.p + R.kSize * kOut}, Pm{S.p}, E{Pm.p + Pm.kSize * 3} {}
 };
 
-// [kRows][W] values of a matrix [rows][Dv] from column v0 on, as they come (zeros past its ends); `quads`: in 16-byte pieces.
-template <int kRows, int W, int kPitch>
-__device__ __forceinline__ void fetch_slice(float* to, const float* from, int v0, int rows, int Dv, bool quads) {
-  if (quads) {
+// [kRows][W] values of a matrix [rows][Dv] from column v0 on, as they come (zeros past its ends).  Each thread asks for the four
+// neighbours that it reads itself; `quads`: as one piece of 16 bytes.
+template <int kRows, int W, typename F>
+__device__ __forceinline__ void each_piece(F f) {  // f(row, column)
 #pragma unroll
-    for (int i = threadIdx.x; i < kRows * W / 4; i += kGradThreads) {
-      const int r = i / (W / 4), c = i % (W / 4) * 4;
+  for (int i = threadIdx.x; i < kRows * W / 4; i += kGradThreads) f(i / (W / 4), i % (W / 4) * 4);
+}
+template <int kRows, int W>
+__device__ __forceinline__ void fetch_slice(float* to, const float* from, int v0, int rows, int Dv, bool quads) {
+  each_piece<kRows, W>([&](int r, int c) {
+    const float* at = from + (long long)r * Dv + v0 + c;
+    float* into = to + r * W + c;
+    if (quads) {
       const bool in = r < rows && v0 + c < Dv;
-      copy16(to + r * kPitch + c, in ? from + (long long)r * Dv + v0 + c : from, in ? 16 : 0);
+      copy16(into, in ? at : from, in ? 16 : 0);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool in = r < rows && v0 + c + e < Dv;
+        copy4(into + e, in ? at + e : from, in ? 4 : 0);
+      }
     }
-  } else {
-#pragma unroll 4
-    for (int i = threadIdx.x; i < kRows * W; i += kGradThreads) {
-      const int r = i / W, c = i % W;
-      const bool in = r < rows && v0 + c < Dv;
-      copy4(to + r * kPitch + c, in ? from + (long long)r * Dv + v0 + c : from, in ? 4 : 0);
-    }
-  }
+  });
 }
 
 // x += A, y += B times the transposed rows n0.. of M (three parts), over kLength columns; two tiles of 8 rows
@@ -1290,7 +1308,7 @@ __device__ __forceinline__ void add_rows(float (&x)[kTiles][4], const uint32_t (
   }
 }
 
-// By columns of S, 32 at a time: the next ones come as copies while 16 warps multiply.  1024 chunks of bf16, 128 x 128: 230 us, half
+// By columns of S, 32 at a time: the next ones come as copies while 16 warps multiply.  1024 chunks of bf16, 128 x 128: 204 us, half
 // of it without the products (splitting, the first slices, barriers: one block fills an SM), which take 50 us of the tensor pipes.
 template <typename T, int KD>
 __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const DeltaArgs a) {
@@ -1331,26 +1349,24 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
     __syncthreads();
     fetch<(int)sizeof(Gates), kGradThreads>(sh.gates, a.heads + (size_t)chunk * kHeadBytes + SquareMat::kBytes);
     if (h == hk * a.share) fetch<(int)kKeysBytes<T, KD>, kGradThreads>(sh.K.p, a.keys + where * kKeysBytes<T, KD>);
-    // (R and Y as copies too: held in registers while a round is multiplied, the forward and backward passes took 636 us, not 611,
-    // for 4 streams of 8 heads and 2048 timesteps.)
+    // (R and Y as copies too: held in registers while a round is multiplied, the forward and backward passes took 636 us, not 611.)
     auto fetch_slices = [&](int v0) {
-      fetch_slice<KD, W, W>(sh.next_S, S, v0, a.Dk, a.Dv, a.quads);
-      fetch_slice<KD, W, W>(sh.next_dS, dS, v0, a.Dk, a.Dv, a.quads);
-      fetch_slice<C, W, Sh::kPitch>(sh.next_R, R, v0, rows, a.Dv, a.quads);
-      fetch_slice<C, W, Sh::kPitch>(sh.next_Y, Y, v0, rows, a.Dv, a.quads);
+      fetch_slice<KD, W>(sh.next_S, S, v0, a.Dk, a.Dv, a.quads);
+      fetch_slice<KD, W>(sh.next_dS, dS, v0, a.Dk, a.Dv, a.quads);
+      fetch_slice<C, W>(sh.next_R, R, v0, rows, a.Dv, a.quads);
+      fetch_slice<C, W>(sh.next_Y, Y, v0, rows, a.Dv, a.quads);
       copies_commit();
     };
     fetch_slices(0);
-    const bool mine = side < W / 8;  // this warp's 8 columns of a round's 16 or 32
-    const int col = side * 8 + 2 * t;
+    // The same piece of v and dO as of R and Y.
+    const bool mine = threadIdx.x < C * W / 4;
+    const int row = threadIdx.x / (W / 4), col = threadIdx.x % (W / 4) * 4;
     Raw2<T> vx[2], ox[2];
     auto fetch_rows = [&](int v0) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int i = rb + g + 8 * r;
-        const bool in = mine && i < rows;
-        vx[r].load(v + i * a.vs.t, v0 + col, a.Dv, a.pairs, in);
-        ox[r].load(d_o + i * a.dos.t, v0 + col, a.Dv, a.pairs, in);
+      for (int x = 0; x < 2; ++x) {
+        vx[x].load(v + row * a.vs.t, v0 + col + 2 * x, a.Dv, a.pairs, mine && row < rows);
+        ox[x].load(d_o + row * a.dos.t, v0 + col + 2 * x, a.Dv, a.pairs, mine && row < rows);
       }
     };
     fetch_rows(0);
@@ -1374,35 +1390,29 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
       }
       float acc_q[kTiles][4] = {}, acc_w[kTiles][4] = {}, acc_t[kTiles][4] = {};  // dO S0^T, R S0^T, U dS^T
       float acc_p[2][4] = {}, acc_e[2][4] = {};                                  // dO U^T, R U^T
-      float rv[2] = {}, ry[2] = {};                                              // R . V, R . Y
+      float rv = 0.0f, ry = 0.0f;                                                // R . V, R . Y
       if (lo > 0) fetch_rows(0);
 
       for (int v0 = 0; v0 < a.Dv; v0 += W) {
         copies_wait<0>();
-        __syncthreads();  // the slices are there, and nobody reads the round before
-#pragma unroll
-        for (int i = threadIdx.x; i < KD * W / 2; i += kGradThreads) {
-          const int r = i / (W / 2), c = i % (W / 2) * 2;
-          const float2 x = fresh ? zero : reinterpret_cast<const float2*>(sh.next_S)[i];
-          const float2 y = last ? reinterpret_cast<const float2*>(sh.next_dS)[i] : zero;
-          sh.S.put(r, c, x.x, x.y);
-          sh.dS.put(r, c, y.x, y.y);
-        }
+        __syncthreads();  // nobody reads the round before
+        const float4 none = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        each_piece<KD, W>([&](int r, int c) {
+          sh.S.put4(r, c, fresh ? none : *reinterpret_cast<const float4*>(sh.next_S + r * W + c));
+          sh.dS.put4(r, c, last ? *reinterpret_cast<const float4*>(sh.next_dS + r * W + c) : none);
+        });
         if (mine) {
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const int i = rb + g + 8 * r;
-            const bool in = i >= lo && i < hi;
-            const float beta = gate.beta[i];
-            const float2 vn = in ? vx[r].get() : zero, on = in ? ox[r].get() : zero;
-            const float2 rn = in ? *reinterpret_cast<const float2*>(sh.next_R + i * Sh::kPitch + col) : zero;
-            const float2 yn = in ? *reinterpret_cast<const float2*>(sh.next_Y + i * Sh::kPitch + col) : zero;
-            rv[r] = fmaf(rn.x, vn.x, fmaf(rn.y, vn.y, rv[r]));
-            ry[r] = fmaf(rn.x, yn.x, fmaf(rn.y, yn.y, ry[r]));
-            sh.R.put(i, col, rn.x, rn.y);
-            sh.dO.put(i, col, on.x, on.y);
-            sh.U.put(i, col, in ? beta * yn.x : 0.0f, in ? beta * yn.y : 0.0f);
-          }
+          const bool in = row >= lo && row < hi;
+          const float beta = gate.beta[row];
+          const float2 va = vx[0].get(), vb = vx[1].get(), oa = ox[0].get(), ob = ox[1].get();
+          const float4 rn = in ? *reinterpret_cast<const float4*>(sh.next_R + row * W + col) : none;
+          const float4 yn = in ? *reinterpret_cast<const float4*>(sh.next_Y + row * W + col) : none;
+          const float4 vn = in ? make_float4(va.x, va.y, vb.x, vb.y) : none;
+          rv = fmaf(rn.x, vn.x, fmaf(rn.y, vn.y, fmaf(rn.z, vn.z, fmaf(rn.w, vn.w, rv))));
+          ry = fmaf(rn.x, yn.x, fmaf(rn.y, yn.y, fmaf(rn.z, yn.z, fmaf(rn.w, yn.w, ry))));
+          sh.R.put4(row, col, rn);
+          sh.dO.put4(row, col, in ? make_float4(oa.x, oa.y, ob.x, ob.y) : none);
+          sh.U.put4(row, col, in ? make_float4(beta * yn.x, beta * yn.y, beta * yn.z, beta * yn.w) : none);
         }
         __syncthreads();
         if (v0 + W < a.Dv) {
@@ -1537,25 +1547,21 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
           }
         }
       }
-      // sums over a row's columns: four lanes and four warps
-      auto row_sum = [&](int which, float (&x)[2]) {
+      // sums over a row's columns: of neighbouring lanes, and for dot_q of four warps
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          float y = x[r];
-          y += __shfl_xor_sync(0xffffffffu, y, 1);
-          y += __shfl_xor_sync(0xffffffffu, y, 2);
-          if (t == 0) sh.sums[(which * 4 + side) * C + rb + g + 8 * r] = y;
-        }
-      };
-      row_sum(0, rv);
-      row_sum(1, ry);
-      row_sum(2, dot_q);
+      for (int d = 1; d < W / 4; d *= 2) {
+        rv += __shfl_xor_sync(0xffffffffu, rv, d);
+        ry += __shfl_xor_sync(0xffffffffu, ry, d);
+      }
+      if (mine && col == 0) sh.sums[row] = rv, sh.sums[C + row] = ry;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        dot_q[r] += __shfl_xor_sync(0xffffffffu, dot_q[r], 1);
+        dot_q[r] += __shfl_xor_sync(0xffffffffu, dot_q[r], 2);
+        if (t == 0) sh.sums[(2 + side) * C + rb + g + 8 * r] = dot_q[r];
+      }
       __syncthreads();
       if (warp == 0) {  // dbeta, and dg: what the state before gives, less the rows before (rows lane and lane + 32)
-        auto sum_of = [&](int which, int row) {
-          const float* x = sh.sums + which * 4 * C + row;
-          return (x[0] + x[C]) + (x[2 * C] + x[3 * C]);
-        };
         float start = 0.0f;
         if (!fresh)
           for (int i = 0; i < a.tiles; ++i) start += a.dots[chunk * a.tiles + i];
@@ -1564,15 +1570,16 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
         for (int s = 0; s < 2; ++s) {
           const int row = lane + 32 * s;
           const bool in = row >= lo && row < hi;
-          own[s] = in ? sum_of(2, row) - gate.beta[row] * sum_of(0, row) : 0.0f;
-          if (in) a.dbeta[(long long)(t0 + row) * a.dbt + b * a.dbb + h] = sum_of(1, row);
-          float x = own[s];
+          const float* x = sh.sums + 2 * C + row;
+          own[s] = in ? ((x[0] + x[C]) + (x[2 * C] + x[3 * C])) - gate.beta[row] * sh.sums[row] : 0.0f;
+          if (in) a.dbeta[(long long)(t0 + row) * a.dbt + b * a.dbb + h] = sh.sums[C + row];
+          float sum = own[s];
 #pragma unroll
           for (int d = 1; d < 32; d *= 2) {
-            const float y = __shfl_up_sync(0xffffffffu, x, d);
-            if (lane >= d) x += y;
+            const float y = __shfl_up_sync(0xffffffffu, sum, d);
+            if (lane >= d) sum += y;
           }
-          G[s] = x;
+          G[s] = sum;
         }
         G[1] += __shfl_sync(0xffffffffu, G[0], 31);
 #pragma unroll
