@@ -458,3 +458,43 @@ def test_gradient_of_the_first_state_over_that_of_the_last(cuda_device, T, B, H,
     want = delta_scan_backward(do, *args, states, held.clone(), lengths=lengths)
     got = delta_scan_backward(do, *args, states, held, lengths=lengths, dh0=held)
     assert got[5] is held and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits(cuda_device):
+    """Timesteps that lie more than 2^31 values apart, read and written; a pool of more than 2^31 values."""
+    import torch
+    from paper_1905_00689_gb300 import delta_scan, delta_scan_backward, delta_scan_states, delta_step
+    T, B, H, Hk, Dk, Dv = 3, 2, 2, 1, 16, 24
+    args = delta.tensors((T, B), H, Hk, Dk, Dv, "bf16", 9)
+    do = torch.randn(T, B, H, Dv, device="cuda").bfloat16()
+    apart, states = 2 ** 30 + 64, delta_scan_states(args[0], args[2])
+    room = torch.empty(2 * apart + 4096, dtype=torch.bfloat16, device="cuda")
+
+    def far(like, at):  # places of their own within the first 4096 values of each timestep
+        n = like[0].numel()
+        return room[at:].as_strided(like.shape, (apart, *like[0].stride())), at + n
+    at, moved = 0, []
+    for t in args[:3]:
+        view, at = far(t, at)
+        moved.append(view.copy_(t))
+    o, at = far(args[2], at)
+    want = delta_scan(*args, states=states)
+    got = delta_scan(*moved, *args[3:], o=o)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    want = delta_scan_backward(do, *args, states)
+    outs = {}
+    for name, like in (("dq", args[0]), ("dk", args[1]), ("dv", args[2])):
+        outs[name], at = far(like, at)
+    got = delta_scan_backward(do, *moved, *args[3:], states, **outs)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    del room, moved, o, outs, got
+
+    slots = 2 ** 31 // (64 * 64) + 3
+    pool = torch.empty(slots, 1, 64, 64, device="cuda")
+    q, k, v, g, beta = delta.tensors((2,), 1, 1, 64, 64, "bf16", 10)
+    small = torch.randn(2, 1, 64, 64, device="cuda")
+    pool[0], pool[slots - 1] = small[0], small[1]
+    want = delta_step(q, k, v, g, beta, small)
+    got = delta_step(q, k, v, g, beta, pool, slots=torch.tensor([0, slots - 1], dtype=torch.int32, device="cuda"))
+    assert torch.equal(got, want) and torch.equal(pool[0], small[0]) and torch.equal(pool[slots - 1], small[1])
