@@ -231,7 +231,7 @@ struct DeltaArgs {
   const float* h0;
   const int32_t* lengths;
   const unsigned char* reset;
-  int T, B, H, share, Dk, Dv, tiles, cluster;
+  int T, B, H, share, Dk, Dv, tiles;
   bool wide;   // q, k, dq and dk in 16-byte pieces
   bool pairs;  // v, o, dO and dV two at a time
   bool even;   // states two at a time
@@ -635,9 +635,8 @@ __global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaA
 
 // ---- along the chunks -------------------------------------------------------------
 
-// What a chunk brings along: parts of K and Q, N, gates, M.  The blocks of a cluster have the same head: each asks for its share
-// and sends it to all (from L2, 16 heads of 8 blocks would otherwise take 73 KB to a block and chunk, 9.4 MB to every
-// 2.3 us of the device).
+// What a chunk brings along: parts of K and Q, N, gates, M.  Every block asks for its own copy: the blocks of a head read the same
+// 73 KB (bf16, 128 wide keys) from L2.
 template <typename T, int KD, int kMParts>
 struct Stage {
   KeyMat<T, KD> K, Q;
@@ -649,19 +648,12 @@ struct Stage {
   __device__ __forceinline__ explicit Stage(unsigned char* p)
       : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * kParts<T>}, N{Q.p + Q.kSize * kParts<T>},
         gates(reinterpret_cast<Gates*>(N.p + N.kSize * 3)), M{reinterpret_cast<bf16*>(gates + 1)} {}
-  __device__ __forceinline__ static void share(uint32_t to, const unsigned char* from, uint32_t bytes, int cluster, uint32_t rank, uint32_t bar) {
-    const uint32_t per = (bytes / 16 + cluster - 1) / cluster * 16, at = rank * per;
-    if (at >= bytes) return;
-    const uint32_t mine = min(per, bytes - at);
-    if (cluster == 1) bulk_copy_g2s(to + at, from + at, mine, bar);
-    else bulk_copy_g2cluster(to + at, from + at, mine, bar, (uint16_t)((1u << cluster) - 1u));
-  }
-  // One thread of every block of the cluster; no block reads its stage any more.
-  __device__ __forceinline__ void load(const DeltaArgs& a, int n, int b, int h, uint32_t rank, uint32_t bar) const {
+  // One thread; nobody reads the stage any more.
+  __device__ __forceinline__ void load(const DeltaArgs& a, int n, int b, int h, uint32_t bar) const {
     const size_t at = (size_t)n * a.B + b;
     mbar_arrive_expect_tx(bar, kKeys + kHead);
-    share(smem_u32(K.p), a.keys + (at * (a.H / a.share) + h / a.share) * kKeysBytes<T, KD>, kKeys, a.cluster, rank, bar);
-    share(smem_u32(N.p), a.heads + (at * a.H + h) * kHeadBytes, kHead, a.cluster, rank, bar);
+    bulk_copy_g2s(smem_u32(K.p), a.keys + (at * (a.H / a.share) + h / a.share) * kKeysBytes<T, KD>, kKeys, bar);
+    bulk_copy_g2s(smem_u32(N.p), a.heads + (at * a.H + h) * kHeadBytes, kHead, bar);
   }
 };
 // Chunks in shared memory at a time: two, or one where the parts of wide keys fill it.
@@ -673,22 +665,15 @@ constexpr int kStages = kParts<T> > 1 && KD == 128 ? 1 : 2;
 constexpr int kChainThreads = 256, kSideThreads = 128, kBothThreads = kChainThreads + kSideThreads, kAllThreads = kBothThreads + 32;
 constexpr uint32_t kChain = 1, kSide = 2, kToSide = 3, kToChain = 4, kStateToSide = 5;
 
-// Two rings of barriers of a block: a stage's chunk has come; all warps of the cluster have read it.
-//
-// A warp has read its own block's shared memory when it arrives at the other blocks' barriers, and a load that has its value does not
-// see what is copied there afterwards: the order within its block is all that an arrival has to give (what the warp wrote into the
-// stage is another matter).  One that orders for the cluster waits for all loads and stores of the warp under way, those of other
-// chunks' values among them, in the middle of a chunk: 8191 timesteps of 16 heads took 342 us instead of 292, 319 when every block's
-// warps arrived at home and the thread that asks for the copies at the cluster's barriers.
+// Two rings of barriers: a stage's chunk has come; all warps have read it.
 template <int kN>
 struct Ring {
   uint32_t full, empty;  // addresses
-  int cluster;
   bool ok;
-  __device__ __forceinline__ Ring(uint64_t* bars, int cluster_) : full(smem_u32(bars)), empty(smem_u32(bars + kN)), cluster(cluster_), ok(true) {}
+  __device__ __forceinline__ explicit Ring(uint64_t* bars) : full(smem_u32(bars)), empty(smem_u32(bars + kN)), ok(true) {}
   __device__ __forceinline__ void init() const {  // one thread
 #pragma unroll
-    for (int i = 0; i < kN; ++i) mbar_init(full + 8 * i, 1), mbar_init(empty + 8 * i, (kBothThreads / 32) * cluster);
+    for (int i = 0; i < kN; ++i) mbar_init(full + 8 * i, 1), mbar_init(empty + 8 * i, kBothThreads / 32);
     fence_mbarrier_init_cluster();
   }
   // The k-th chunk (once a wait has run out, no further one is waited for).
@@ -697,12 +682,12 @@ struct Ring {
     return ok;
   }
   __device__ __forceinline__ bool wait_empty(int k) {
-    ok = ok && (k < kN || mbar_wait_bounded<true>(empty + k % kN * 8, (uint32_t)(k / kN - 1) & 1u, kWaitNs, &g_never));
+    ok = ok && (k < kN || mbar_wait_bounded<false>(empty + k % kN * 8, (uint32_t)(k / kN - 1) & 1u, kWaitNs, &g_never));
     return ok;
   }
   __device__ __forceinline__ void release(int k) const {  // a whole warp
     __syncwarp();
-    if ((int)(threadIdx.x & 31) < cluster) mbar_arrive_cluster(mapa_shared(empty + k % kN * 8, threadIdx.x & 31));
+    if ((threadIdx.x & 31) == 0) mbar_arrive(empty + k % kN * 8);
   }
 };
 
@@ -832,7 +817,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
   const int warp = threadIdx.x >> 5, g = lane_g(), t = lane_t();
   const long long DD = (long long)a.Dk * a.Dv;
   T* o = static_cast<T*>(a.o) + b * a.os.b + h * a.os.h;
-  Ring<kN> ring(sh.bars, a.cluster);
+  Ring<kN> ring(sh.bars);
   StatePart<KD, NV> s;
   if (warp < 8) {
     s.load(a.h0 ? a.h0 + (long long)bh * DD : nullptr, a, v0);
@@ -840,12 +825,10 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
   }
   if (threadIdx.x == kBothThreads) ring.init();
   __syncthreads();
-  cluster_sync_all();  // barriers and buffers of all blocks are ready
 
   if (warp == kBothThreads / 32) {
     if (threadIdx.x == kBothThreads) {
-      const uint32_t rank = cluster_ctarank();
-      for (int n = 0; n < chunks && ring.wait_empty(n); ++n) St(smem + n % kN * St::kBytes).load(a, n, b, h, rank, ring.full + n % kN * 8);
+      for (int n = 0; n < chunks && ring.wait_empty(n); ++n) St(smem + n % kN * St::kBytes).load(a, n, b, h, ring.full + n % kN * 8);
     }
   } else if (warp < 8) {
     constexpr int kTiles = NV / 16;  // a warp's 16 rows of the chunk and half of the columns
@@ -923,7 +906,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
           for (int i = threadIdx.x; i < lo * KD; i += kChainThreads)
 #pragma unroll
             for (int q = 0; q < P; ++q) now.K.p[q * now.K.kSize + i] = from_f32<bf16>(0.0f);
-          fence_proxy_async_shared(), fence_cluster();  // (before another block's copy overwrites them)
+          fence_proxy_async_shared();  // (before a copy overwrites them)
         }
         named_arrive(kToSide, kBothThreads);
         named_sync(kChain, kChainThreads);
@@ -980,7 +963,6 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
       if (c < a.Dv) o[i / NV * a.os.t + c] = from_f32<T>(0.0f);
     }
   }
-  cluster_sync_all();  // nothing is sent to a block that has ended
 }
 
 template <typename T, int KD, int NV>
@@ -1015,7 +997,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
   const int len = length_of(a, b), chunks = (len + C - 1) / C;
   const int warp = threadIdx.x >> 5, g = lane_g(), t = lane_t();
   const long long DD = (long long)a.Dk * a.Dv;
-  Ring<kN> ring(sh.bars, a.cluster);
+  Ring<kN> ring(sh.bars);
   StatePart<KD, NV> s;
   if (warp < 8) {
     s.load(a.dh_last ? a.dh_last + (long long)bh * DD : nullptr, a, v0);
@@ -1023,13 +1005,11 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
   }
   if (threadIdx.x == kBothThreads) ring.init();
   __syncthreads();
-  cluster_sync_all();
 
   if (warp == kBothThreads / 32) {
     if (threadIdx.x == kBothThreads) {
-      const uint32_t rank = cluster_ctarank();
       for (int k = 0; k < chunks && ring.wait_empty(k); ++k)
-        St(smem + k % kN * St::kBytes).load(a, chunks - 1 - k, b, h, rank, ring.full + k % kN * 8);
+        St(smem + k % kN * St::kBytes).load(a, chunks - 1 - k, b, h, ring.full + k % kN * 8);
     }
   } else if (warp < 8) {
     constexpr int kTiles = NV / 16;
@@ -1103,7 +1083,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
           for (int i = threadIdx.x + hi * KD; i < C * KD; i += kChainThreads)
 #pragma unroll
             for (int q = 0; q < P; ++q) now.K.p[q * now.K.kSize + i] = now.Q.p[q * now.Q.kSize + i] = from_f32<bf16>(0.0f);
-          fence_proxy_async_shared(), fence_cluster();
+          fence_proxy_async_shared();
         }
         named_sync(kChain, kChainThreads);
         if (lo > 0) named_arrive(kToSide, kBothThreads);  // L and Od have been read
@@ -1201,7 +1181,6 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
       }
     }
   }
-  cluster_sync_all();
 }
 
 // ---- per chunk and key head: the gradients of q, k, g and beta ---------------------
@@ -1615,7 +1594,7 @@ Workspace workspace_of(size_t es, bool exact, long long T, long long B, long lon
   if (backward) {
     w.dS = take(chunks * H * Dk * Dv * 4);
     w.R = take(chunks * H * C * Dv * 4);
-    w.dots = take(chunks * H * ((Dv + 15) / 16 + 8) * 4);
+    w.dots = take(chunks * H * ((Dv + 15) / 16) * 4);
     if (H > Hk) {
       w.sum_q = take(chunks * Hk * C * KD * 4);
       w.sum_k = take(chunks * Hk * C * KD * 4);
@@ -1630,25 +1609,12 @@ int columns_of(long long heads, int Dv, size_t es) {
   return heads * ((Dv + 15) / 16) <= 152 || es == 4 ? 16 : 32;
 }
 
-// Blocks of a head (tiles of columns, with some that have none) and of a cluster: as large as few idle blocks allow, any number
-// of them while the device has room.
-void clusters_of(long long heads, DeltaArgs& a, int NV) {
-  const int tiles = (a.Dv + NV - 1) / NV;
-  for (int c = 4;; c /= 2) {
-    const int padded = (tiles + c - 1) / c * c;
-    if (c == 1 || (c < 2 * tiles && (heads * padded <= 152 || 4 * padded <= 5 * tiles))) {
-      a.cluster = c, a.tiles = padded;
-      return;
-    }
-  }
-}
-
 template <auto kKern>
-cudaError_t launch_big(dim3 grid, size_t smem, cudaStream_t s, const DeltaArgs& a, int cluster = 1, int threads = kThreads) {
+cudaError_t launch_big(dim3 grid, size_t smem, cudaStream_t s, const DeltaArgs& a, int threads = kThreads) {
   static thread_local DeviceSet ready;  // of this kernel
   const cudaError_t e =
       once_per_device(&ready, [&] { return cudaFuncSetAttribute(kKern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
-  return e != cudaSuccess ? e : op_launch_clusters(cluster, kKern, grid, dim3(threads), smem, s, a);
+  return e != cudaSuccess ? e : op_launch(kKern, grid, dim3(threads), smem, s, a);
 }
 
 template <typename F>
@@ -1684,7 +1650,7 @@ int check(int dtype, const void* q, const void* k, const void* v, const float* g
   if (!op_float_dtype(dtype)) return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "dtype %d", dtype);
   if (int rc = delta_check_sizes(T, B, H, Hk, Dk, Dv, msg, msg_len)) return rc;
   const long long tiles = (Dv + 15) / 16;
-  if ((long long)B * H > 0x7fffffffll / (tiles + 8) || (long long)((T + 63ll) / 64) * B > 0x7fffffffll / H)
+  if ((long long)B * H > 0x7fffffffll / tiles || (long long)((T + 63ll) / 64) * B > 0x7fffffffll / H)
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "B H ceil(Dv / 16) and ceil(T / 64) B H must be below 2^31");
   const size_t es = op_dtype_bytes(dtype);
   if (T > 0 && B > 0 && (!q || !k || !v || !g || !beta))
@@ -1743,14 +1709,14 @@ extern "C" int lstm_approx_delta_scan(int dtype, const void* q, const void* k, c
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   if (int rc = op_launched(prepare(dtype, a, false, s), "delta scan launch", msg, msg_len)) return rc;
   const int NV = columns_of((long long)B * H, Dv, es);
-  clusters_of((long long)B * H, a, NV);
+  a.tiles = (Dv + NV - 1) / NV;
   const dim3 grid((unsigned)(B * H * a.tiles));
   const cudaError_t e = for_shape(dtype, Dk, [&](auto* t, auto kd) {
     using Ty = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
     if constexpr (sizeof(Ty) == 2)
-      if (NV == 32) return launch_big<delta_forward_kernel<Ty, KD, 32>>(grid, ForwardShared<Ty, KD, 32>::kBytes, s, a, a.cluster, kAllThreads);
-    return launch_big<delta_forward_kernel<Ty, KD, 16>>(grid, ForwardShared<Ty, KD, 16>::kBytes, s, a, a.cluster, kAllThreads);
+      if (NV == 32) return launch_big<delta_forward_kernel<Ty, KD, 32>>(grid, ForwardShared<Ty, KD, 32>::kBytes, s, a, kAllThreads);
+    return launch_big<delta_forward_kernel<Ty, KD, 16>>(grid, ForwardShared<Ty, KD, 16>::kBytes, s, a, kAllThreads);
   });
   return op_launched(e, "delta scan launch", msg, msg_len);
 }
@@ -1799,14 +1765,14 @@ extern "C" int lstm_approx_delta_scan_backward(int dtype, const void* d_o, const
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   if (int rc = op_launched(prepare(dtype, a, true, s), "delta scan launch", msg, msg_len)) return rc;
   const int NV = columns_of((long long)B * H, Dv, es);
-  clusters_of((long long)B * H, a, NV);
+  a.tiles = (Dv + NV - 1) / NV;
   const dim3 grid((unsigned)(B * H * a.tiles));
   cudaError_t e = for_shape(dtype, Dk, [&](auto* t, auto kd) {
     using Ty = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
     if constexpr (sizeof(Ty) == 2)
-      if (NV == 32) return launch_big<delta_backward_kernel<Ty, KD, 32>>(grid, BackwardShared<Ty, KD, 32>::kBytes, s, a, a.cluster, kAllThreads);
-    return launch_big<delta_backward_kernel<Ty, KD, 16>>(grid, BackwardShared<Ty, KD, 16>::kBytes, s, a, a.cluster, kAllThreads);
+      if (NV == 32) return launch_big<delta_backward_kernel<Ty, KD, 32>>(grid, BackwardShared<Ty, KD, 32>::kBytes, s, a, kAllThreads);
+    return launch_big<delta_backward_kernel<Ty, KD, 16>>(grid, BackwardShared<Ty, KD, 16>::kBytes, s, a, kAllThreads);
   });
   if (int rc = op_launched(e, "delta scan backward launch", msg, msg_len)) return rc;
   if (T == 0) return LSTM_APPROX_OK;
@@ -1814,7 +1780,7 @@ extern "C" int lstm_approx_delta_scan_backward(int dtype, const void* d_o, const
   e = for_shape(dtype, Dk, [&](auto* t, auto kd) {
     using Ty = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
-    return launch_big<delta_gradients_kernel<Ty, KD>>(blocks, GradShared<Ty, KD>::kBytes, s, a, 1, kGradThreads);
+    return launch_big<delta_gradients_kernel<Ty, KD>>(blocks, GradShared<Ty, KD>::kBytes, s, a, kGradThreads);
   });
   return op_launched(e, "delta gradients launch", msg, msg_len);
 }

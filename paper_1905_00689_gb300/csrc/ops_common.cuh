@@ -158,26 +158,18 @@ inline int op_launched(cudaError_t e, const char* what, char* msg, int msg_len) 
 // which waits for it (and all that it waited for) to be complete and visible.
 // Back to back, small kernels then take 1.7 to 2.6 us each instead of 4.2.
 template <typename... KArgs, typename... Args>
-cudaError_t op_launch_clusters(int cluster, void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const Args&... args) {
+cudaError_t op_launch(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const Args&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  cudaLaunchAttribute attr[2];
+  cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kern, KArgs(args)...);
-}
-template <typename... KArgs, typename... Args>
-cudaError_t op_launch(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const Args&... args) {
-  return op_launch_clusters(1, kern, grid, block, smem, s, args...);
 }
 
 // The sizes of the gated delta rule's calls.

@@ -71,16 +71,6 @@ __device__ __forceinline__ void mbar_arrive(uint32_t mb) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(mb) : "memory");
 }
 
-// At the barrier that a CTA of the cluster has at the same place (its address from mapa): orders what went before for the thread's
-// own CTA alone.
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t mb_cluster) {
-  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(mb_cluster) : "memory");
-}
-
-__device__ __forceinline__ void fence_cluster() {
-  asm volatile("fence.acq_rel.cluster;" ::: "memory");
-}
-
 // Barriers among some warps of a CTA (`threads` of them in all; 0 is __syncthreads'): with those that arrive, without waiting.
 __device__ __forceinline__ void named_sync(uint32_t id, uint32_t threads) {
   __syncwarp();
@@ -174,14 +164,6 @@ __device__ __forceinline__ void bulk_copy_g2s(uint32_t dst, const void* src, uin
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                "l"(src), "r"(bytes), "r"(mb)
                : "memory");
-}
-
-// The same to the same place in every CTA of the cluster that `mask` names, completing on its mbarrier at the same place.
-__device__ __forceinline__ void bulk_copy_g2cluster(uint32_t dst, const void* src, uint32_t bytes, uint32_t mb, uint16_t mask) {
-  asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.multicast::cluster [%0], [%1], %2, [%3], %4;" ::"r"(dst),
-      "l"(src), "r"(bytes), "r"(mb), "h"(mask)
-      : "memory");
 }
 
 // From this CTA's shared memory to global memory; the waits are for all of this thread's copies before: until their source may be
