@@ -303,6 +303,10 @@ int lstm_approx_delta_scan(int dtype, const void *q, const void *k, const void *
 /* Workspace bytes of the call above, or (backward not 0) of the next; 0 for invalid sizes. */
 size_t lstm_approx_delta_scan_workspace_bytes(int dtype, int T, int B, int H, int Hk, int Dk,
                                               int Dv, int backward);
+/* For tests, process-wide: the kernels wait limit_us for a copy on the device (0: 2 s), after
+ * which the results that need it are NaN; the next call of either direction does not make the
+ * copy of chunk `withheld` (-1: makes all). */
+int lstm_approx_delta_scan_set_waits(int limit_us, int withheld);
 
 /*
  * Its gradients:

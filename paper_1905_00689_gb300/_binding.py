@@ -44,7 +44,7 @@ EXPORTS = (
     "lstm_approx_gated_scan_workspace_bytes", "lstm_approx_gated_step", "lstm_approx_w4_quantize",
     "lstm_approx_w4_matvec", "lstm_approx_w4_workspace_bytes",
     "lstm_approx_delta_scan", "lstm_approx_delta_scan_backward",
-    "lstm_approx_delta_scan_workspace_bytes", "lstm_approx_delta_step", "lstm_approx_adamw_step",
+    "lstm_approx_delta_scan_workspace_bytes", "lstm_approx_delta_scan_set_waits", "lstm_approx_delta_step", "lstm_approx_adamw_step",
 )
 
 _lib = None
@@ -104,6 +104,7 @@ def load(path: str = LIB_PATH):
     lib.lstm_approx_delta_scan.argtypes = [I, P, P, P, P, P, F, P, P, P, I, I, I, I, I, I, P, P, P, P, P, Z] + end
     lib.lstm_approx_delta_scan_backward.argtypes = ([I, P, P, P, P, P, P, P, F, P, P, P, I, I, I, I, I, I] + [P] * 8 + [Z] + end)
     lib.lstm_approx_delta_scan_workspace_bytes.argtypes = [I] * 8
+    lib.lstm_approx_delta_scan_set_waits.argtypes = [I, I]
     lib.lstm_approx_delta_step.argtypes = [I, P, P, P, P, P, F, P, I, P, P, I, I, I, I, I, P, P] + end
     lib.lstm_approx_adamw_step.argtypes = [I, P, I, I, P, D, P, D, D, D, D, P, P, ctypes.c_uint] + end
     for name in EXPORTS:

@@ -50,6 +50,9 @@
 // At a reset the state before counts as zero, and so does everything before it
 // in its chunk: a chunk with resets is taken piece by piece, and rows of other
 // pieces are left out, not multiplied by zero.
+#include <atomic>
+#include <cstddef>
+#include <limits>
 #include <type_traits>
 
 #include "ops_common.cuh"
@@ -63,6 +66,7 @@ constexpr int C = LSTM_APPROX_DELTA_CHUNK;
 static_assert(C == 64, "rows of a chunk");
 constexpr int kThreads = 256;
 constexpr float kLeastG = -200.0f;
+constexpr float kNaN = std::numeric_limits<float>::quiet_NaN();
 
 using bf16 = __nv_bfloat16;
 
@@ -206,8 +210,8 @@ __device__ __forceinline__ void mma(float (&d)[4], float (&e)[4], const uint32_t
 
 // ---- what the kernels share ----------------------------------------------------
 
-// A wait for a copy that a working device always completes; on one that does not the results are NaN.
-constexpr uint64_t kWaitNs = 2000000000ull;
+// A wait for a copy that a working device always completes lasts 2 s at the most; where it runs out the results are NaN.
+constexpr int kWaitUs = 2000000;
 __device__ const int g_never = 0;
 
 struct Gates {  // of a chunk and head
@@ -232,6 +236,8 @@ struct DeltaArgs {
   const int32_t* lengths;
   const unsigned char* reset;
   int T, B, H, share, Dk, Dv, tiles;
+  uint64_t wait_ns;
+  int withheld;  // a chunk that is not copied (its waits run out), or -1
   bool wide;   // q, k, dq and dk in 16-byte pieces
   bool pairs;  // v, o, dO and dV two at a time
   bool even;   // states two at a time
@@ -255,6 +261,14 @@ using SquareMat = Mat<C, C, 3>;
 template <typename T, int KD>
 constexpr size_t kKeysBytes = 2 * KeyMat<T, KD>::kBytes;
 constexpr size_t kHeadBytes = 2 * SquareMat::kBytes + sizeof(Gates);
+
+// The resets of a chunk, for the loops over its pieces.  They come from memory and not from the stage: what a stage holds after a wait
+// that has run out may change at any time, and these loops hold barriers.
+__device__ __forceinline__ unsigned long long cuts_of(const DeltaArgs& a, int n, int chunks, int b, int h) {
+  if (n < 0 || n >= chunks) return 0ull;
+  const unsigned char* head = a.heads + ((size_t)((long long)n * a.B + b) * a.H + h) * kHeadBytes;
+  return *reinterpret_cast<const unsigned long long*>(head + SquareMat::kBytes + offsetof(Gates, cuts));
+}
 
 __device__ __forceinline__ int length_of(const DeltaArgs& a, int b) {
   return a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
@@ -652,6 +666,7 @@ struct Stage {
   __device__ __forceinline__ void load(const DeltaArgs& a, int n, int b, int h, uint32_t bar) const {
     const size_t at = (size_t)n * a.B + b;
     mbar_arrive_expect_tx(bar, kKeys + kHead);
+    if (n == a.withheld) return;
     bulk_copy_g2s(smem_u32(K.p), a.keys + (at * (a.H / a.share) + h / a.share) * kKeysBytes<T, KD>, kKeys, bar);
     bulk_copy_g2s(smem_u32(N.p), a.heads + (at * a.H + h) * kHeadBytes, kHead, bar);
   }
@@ -669,21 +684,31 @@ constexpr uint32_t kChain = 1, kSide = 2, kToSide = 3, kToChain = 4, kStateToSid
 template <int kN>
 struct Ring {
   uint32_t full, empty;  // addresses
+  uint64_t limit;
   bool ok;
-  __device__ __forceinline__ explicit Ring(uint64_t* bars) : full(smem_u32(bars)), empty(smem_u32(bars + kN)), ok(true) {}
+  __device__ __forceinline__ Ring(uint64_t* bars, uint64_t limit_) : full(smem_u32(bars)), empty(smem_u32(bars + kN)), limit(limit_), ok(true) {}
   __device__ __forceinline__ void init() const {  // one thread
 #pragma unroll
     for (int i = 0; i < kN; ++i) mbar_init(full + 8 * i, 1), mbar_init(empty + 8 * i, kBothThreads / 32);
     fence_mbarrier_init_cluster();
   }
-  // The k-th chunk (once a wait has run out, no further one is waited for).
+  __device__ __forceinline__ bool full_by(int k) const {
+    return mbar_wait_bounded<false>(full + k % kN * 8, (uint32_t)(k / kN) & 1u, limit, &g_never);
+  }
+  // The k-th chunk (once a wait has run out, no further one is waited for).  What follows a wait takes the same branches either way:
+  // warps whose waits end differently meet at the same barriers.
   __device__ __forceinline__ bool wait_full(int k) {
-    ok = ok && mbar_wait_bounded<false>(full + k % kN * 8, (uint32_t)(k / kN) & 1u, kWaitNs, &g_never);
+    ok = ok && full_by(k);
     return ok;
   }
+  // The thread that asks for the chunks: the k-th one's stage has been read, and what was asked for last has come.
   __device__ __forceinline__ bool wait_empty(int k) {
-    ok = ok && (k < kN || mbar_wait_bounded<false>(empty + k % kN * 8, (uint32_t)(k / kN - 1) & 1u, kWaitNs, &g_never));
+    ok = ok && (k < kN || (mbar_wait_bounded<false>(empty + k % kN * 8, (uint32_t)(k / kN - 1) & 1u, limit, &g_never) && full_by(k - kN)));
     return ok;
+  }
+  // The same, when it has asked for `asked` of them: a block does not end while its copies are under way.
+  __device__ __forceinline__ void wait_rest(int asked) const {
+    for (int k = max(asked - kN, 0); k < asked; ++k) full_by(k);
   }
   __device__ __forceinline__ void release(int k) const {  // a whole warp
     __syncwarp();
@@ -817,7 +842,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
   const int warp = threadIdx.x >> 5, g = lane_g(), t = lane_t();
   const long long DD = (long long)a.Dk * a.Dv;
   T* o = static_cast<T*>(a.o) + b * a.os.b + h * a.os.h;
-  Ring<kN> ring(sh.bars);
+  Ring<kN> ring(sh.bars, a.wait_ns);
   StatePart<KD, NV> s;
   if (warp < 8) {
     s.load(a.h0 ? a.h0 + (long long)bh * DD : nullptr, a, v0);
@@ -828,7 +853,9 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
 
   if (warp == kBothThreads / 32) {
     if (threadIdx.x == kBothThreads) {
-      for (int n = 0; n < chunks && ring.wait_empty(n); ++n) St(smem + n % kN * St::kBytes).load(a, n, b, h, ring.full + n % kN * 8);
+      int n = 0;
+      for (; n < chunks && ring.wait_empty(n); ++n) St(smem + n % kN * St::kBytes).load(a, n, b, h, ring.full + n % kN * 8);
+      ring.wait_rest(n);
     }
   } else if (warp < 8) {
     constexpr int kTiles = NV / 16;  // a warp's 16 rows of the chunk and half of the columns
@@ -846,21 +873,27 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
         }
     };
     fetch_v(0);
+    unsigned long long cuts_ahead = cuts_of(a, 0, chunks, b, h);
     for (int n = 0; n < chunks; ++n) {
       const bool came = ring.wait_full(n);
       __syncwarp();
+      const unsigned long long cuts = cuts_ahead;
+      cuts_ahead = cuts_of(a, n + 1, chunks, b, h);
       const St now(smem + n % kN * St::kBytes);
       const auto S0 = sh.state(n);
       const Gates& gate = *now.gates;
       float2 vn[kTiles][2];
 #pragma unroll
-      for (int x = 0; x < kTiles; ++x) vn[x][0] = vx[x][0].get(), vn[x][1] = vx[x][1].get();
-      if (!came) vn[0][0].x = __int_as_float(0x7fffffff);
+      for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          vn[x][r] = vx[x][r].get();
+          if (!came) vn[x][r] = make_float2(kNaN, kNaN);
+        }
       fetch_v(n + 1);
       // S0 and Y for the backward pass
       float* kept = a.states ? a.states + (((long long)n * a.B + b) * a.H + h) * (a.Dk + C) * a.Dv : nullptr;
       if (kept) s.store(kept, a, v0);
-      const unsigned long long cuts = gate.cuts;
 
       for (int lo = 0; lo < C;) {
         const int hi = piece_end(cuts, lo);
@@ -924,12 +957,15 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
   } else {
     constexpr int kTiles = NV / 8;
     const int rb = (warp - 8) * 16;
+    unsigned long long cuts_ahead = cuts_of(a, 0, chunks, b, h);
     for (int n = 0; n < chunks; ++n) {
       const bool came = ring.wait_full(n);
+      __syncwarp();
+      const unsigned long long cuts = cuts_ahead;
+      cuts_ahead = cuts_of(a, n + 1, chunks, b, h);
       if (n > 0) named_sync(kStateToSide, kBothThreads);
       const St now(smem + n % kN * St::kBytes);
       const Gates& gate = *now.gates;
-      const unsigned long long cuts = gate.cuts;
       for (int lo = 0; lo < C;) {
         const int hi = piece_end(cuts, lo);
         float d[kTiles][4] = {}, e[kTiles][4] = {};
@@ -951,8 +987,8 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
           if (i < lo || i >= hi || time >= len) continue;
 #pragma unroll
           for (int c = 0; c < kTiles; ++c) {
-            const float p = came ? a.scale * (d[c][2 * r] + e[c][2 * r]) : __int_as_float(0x7fffffff);
-            put2(o + time * a.os.t, v0 + c * 8 + 2 * t, a.Dv, a.pairs, p, a.scale * (d[c][2 * r + 1] + e[c][2 * r + 1]));
+            const float p = a.scale * (d[c][2 * r] + e[c][2 * r]), q = a.scale * (d[c][2 * r + 1] + e[c][2 * r + 1]);
+            put2(o + time * a.os.t, v0 + c * 8 + 2 * t, a.Dv, a.pairs, came ? p : kNaN, came ? q : kNaN);
           }
         }
         lo = hi;
@@ -997,7 +1033,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
   const int len = length_of(a, b), chunks = (len + C - 1) / C;
   const int warp = threadIdx.x >> 5, g = lane_g(), t = lane_t();
   const long long DD = (long long)a.Dk * a.Dv;
-  Ring<kN> ring(sh.bars);
+  Ring<kN> ring(sh.bars, a.wait_ns);
   StatePart<KD, NV> s;
   if (warp < 8) {
     s.load(a.dh_last ? a.dh_last + (long long)bh * DD : nullptr, a, v0);
@@ -1008,24 +1044,28 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
 
   if (warp == kBothThreads / 32) {
     if (threadIdx.x == kBothThreads) {
-      for (int k = 0; k < chunks && ring.wait_empty(k); ++k)
+      int k = 0;
+      for (; k < chunks && ring.wait_empty(k); ++k)
         St(smem + k % kN * St::kBytes).load(a, chunks - 1 - k, b, h, ring.full + k % kN * 8);
+      ring.wait_rest(k);
     }
   } else if (warp < 8) {
     constexpr int kTiles = NV / 16;
     const int rb = (warp < 4 ? warp : 7 - warp) * 16, cb = (warp >> 2) * (NV / 2);
     T* dv = static_cast<T*>(a.dv) + b * a.dvs.b + h * a.dvs.h;
+    unsigned long long cuts_ahead = cuts_of(a, chunks - 1, chunks, b, h);
     for (int k = 0; k < chunks; ++k) {
       const int n = chunks - 1 - k;
       const bool came = ring.wait_full(k);
       __syncwarp();
+      const unsigned long long cuts = cuts_ahead;
+      cuts_ahead = cuts_of(a, n - 1, chunks, b, h);
       const St now(smem + k % kN * St::kBytes);
       const Gates& gate = *now.gates;
       const long long chunk = ((long long)n * a.B + b) * a.H + h;
       s.store(a.dS + chunk * DD, a, v0);
       StatePart<KD, NV> before;
       before.load(a.states + chunk * (a.Dk + C) * a.Dv, a, v0);
-      const unsigned long long cuts = gate.cuts;
       float* R = a.R + chunk * C * a.Dv;
 
       for (int hi = C; hi > 0;) {  // pieces, the last first
@@ -1049,9 +1089,8 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
 #pragma unroll
               for (int y = 0; y < 2; ++y) {
                 const float far = hi == C ? dec * (d[c][2 * r + y] + e[c][2 * r + y]) : 0.0f;
-                du[c][2 * r + y] = in ? (y ? l.y : l.x) + far : 0.0f;
+                du[c][2 * r + y] = in ? came ? (y ? l.y : l.x) + far : kNaN : 0.0f;
               }
-              if (!came) du[c][0] = __int_as_float(0x7fffffff);
               sh.Z.put(i, col, in ? beta * du[c][2 * r] : 0.0f, in ? beta * du[c][2 * r + 1] : 0.0f);
             }
           }
@@ -1135,13 +1174,15 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
         }
     };
     fetch_o(chunks - 1);
+    unsigned long long cuts_ahead = cuts_of(a, chunks - 1, chunks, b, h);
     for (int k = 0; k < chunks; ++k) {
       const int n = chunks - 1 - k;
-      ring.wait_full(k);
+      const bool came = ring.wait_full(k);
       __syncwarp();
+      const unsigned long long cuts = cuts_ahead;
+      cuts_ahead = cuts_of(a, n - 1, chunks, b, h);
       const St now(smem + k % kN * St::kBytes);
       const Gates& gate = *now.gates;
-      const unsigned long long cuts = gate.cuts;
       float2 on[kTiles][2];
 #pragma unroll
       for (int c = 0; c < kTiles; ++c) on[c][0] = ox[c][0].get(), on[c][1] = ox[c][1].get();
@@ -1167,12 +1208,12 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
         for (int r = 0; r < 2; ++r) {
           const int i = rb + g + 8 * r;
           const bool in = i >= lo && i < hi;
-          const float gam = in ? a.scale * gate.gam[i] : 0.0f;
+          const float scale = came ? a.scale : kNaN, gam = in ? scale * gate.gam[i] : 0.0f;
 #pragma unroll
           for (int c = 0; c < kTiles; ++c) {
             const int col = c * 8 + 2 * t;
             *reinterpret_cast<float2*>(sh.L + i * Sh::kLPitch + col) =
-                make_float2(a.scale * (d[c][2 * r] + e[c][2 * r]), a.scale * (d[c][2 * r + 1] + e[c][2 * r + 1]));
+                make_float2(scale * (d[c][2 * r] + e[c][2 * r]), scale * (d[c][2 * r + 1] + e[c][2 * r + 1]));
             if (lo == 0) sh.Od.put(i, col, in ? gam * on[c][r].x : 0.0f, in ? gam * on[c][r].y : 0.0f);
           }
         }
@@ -1577,6 +1618,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
 
 // ---- host ----------------------------------------------------------------------
 
+// For tests: how long a copy is waited for, and a chunk that the next call does not copy.
+std::atomic<int> g_wait_us{kWaitUs}, g_withheld{-1};
+
 struct Workspace {
   size_t keys, heads, dS, R, dots, sum_q, sum_k, bytes;
 };
@@ -1667,6 +1711,13 @@ int check(int dtype, const void* q, const void* k, const void* v, const float* g
 
 using namespace lstm_approx_impl;
 
+extern "C" int lstm_approx_delta_scan_set_waits(int limit_us, int withheld) {
+  if (limit_us < 0 || withheld < -1) return LSTM_APPROX_EINVAL;
+  g_wait_us = limit_us ? limit_us : kWaitUs;
+  g_withheld = withheld;
+  return LSTM_APPROX_OK;
+}
+
 extern "C" size_t lstm_approx_delta_scan_workspace_bytes(int dtype, int T, int B, int H, int Hk, int Dk, int Dv, int backward) {
   if (check(dtype, nullptr, nullptr, nullptr, nullptr, nullptr, 0, B, H, Hk, Dk, Dv, nullptr, 0, nullptr, 0) || T < 0 ||
       (long long)((T + 63ll) / 64) * B > 0x7fffffffll / H)
@@ -1704,6 +1755,7 @@ extern "C" int lstm_approx_delta_scan(int dtype, const void* q, const void* k, c
   a.pairs = pair_rows(v, a.vs, Dv, es) && pair_rows(o, a.os, Dv, es);
   a.even = Dv % 2 == 0 && op_aligned(h0, 8) && op_aligned(h_last, 8) && op_aligned(states, 8);
   a.h_last = h_last, a.states = states;
+  a.wait_ns = 1000ull * (uint64_t)g_wait_us.load(), a.withheld = g_withheld.exchange(-1);
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) / 256 * 256);
   a.keys = reinterpret_cast<unsigned char*>(ws + w.keys), a.heads = reinterpret_cast<unsigned char*>(ws + w.heads);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
@@ -1757,6 +1809,7 @@ extern "C" int lstm_approx_delta_scan_backward(int dtype, const void* d_o, const
   a.quads = Dv % 4 == 0 && op_aligned(states, 16);
   a.states = const_cast<float*>(states), a.dh_last = dh_last;
   a.dq = dq, a.dk = dk, a.dv = dv, a.dg = dg, a.dbeta = dbeta, a.dh0 = dh0;
+  a.wait_ns = 1000ull * (uint64_t)g_wait_us.load(), a.withheld = g_withheld.exchange(-1);
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) / 256 * 256);
   a.keys = reinterpret_cast<unsigned char*>(ws + w.keys), a.heads = reinterpret_cast<unsigned char*>(ws + w.heads);
   a.dS = reinterpret_cast<float*>(ws + w.dS), a.R = reinterpret_cast<float*>(ws + w.R);
