@@ -793,16 +793,23 @@ __device__ __forceinline__ void product(float (&d)[kTiles][4], float (&e)[kTiles
 #pragma unroll
     for (int r = 0; r < 4; ++r) e[0][r] += f[r];
 }
-// S += keys^T rows (P parts of the keys).
-template <int P, int KD, int NV, int kHas>
-__device__ __forceinline__ void add_keys(StatePart<KD, NV>& s, const Mat<C, KD, kHas>& keys, const Mat<C, NV, 3>& rows) {
-  float e[StatePart<KD, NV>::kTiles][4] = {};
-  product<2, P, 3, StatePart<KD, NV>::kTiles, C, true>(s.x, e, keys, s.row0(), rows, s.col0(), 0);
+// What a chunk adds to S, keys^T rows (P parts of the keys).  It is summed from zero and added once: an MMA's sum is cut, not rounded,
+// to 24 bits, and a state that went through the MMAs would drift towards zero by two units of its last place a chunk (4 MMAs).
+template <int KD, int NV>
+struct StateSum {
+  using Part = StatePart<KD, NV>;
+  float d[Part::kTiles][4] = {}, e[Part::kTiles][4] = {};
+  template <int P, int kHas>
+  __device__ __forceinline__ void add(const Mat<C, KD, kHas>& keys, const Mat<C, NV, 3>& rows) {
+    product<2, P, 3, Part::kTiles, C, true>(d, e, keys, Part::row0(), rows, Part::col0(), 0);
+  }
+  __device__ __forceinline__ void add_to(Part& s) const {
 #pragma unroll
-  for (int c = 0; c < s.kTiles; ++c)
+    for (int c = 0; c < Part::kTiles; ++c)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) s.x[c][r] += e[c][r];
-}
+      for (int r = 0; r < 4; ++r) s.x[c][r] += d[c][r] + e[c][r];
+  }
+};
 // The same for a matrix [64][64] that is zero above the diagonal.
 template <int kDepth, int PA, int PB, int kTiles, bool kTransA, typename MatA, typename MatB>
 __device__ __forceinline__ void product_lower(float (&d)[kTiles][4], float (&e)[kTiles][4], const MatA& A, int m0, const MatB& B, int n0) {
@@ -947,8 +954,10 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
       }
       const float keep = gate.gam[C - 1];
       s.each([&](int, int, float& p, float& q) { p = cuts ? 0.0f : keep * p, q = cuts ? 0.0f : keep * q; });
-      add_keys<P>(s, now.K, sh.Ud);
+      StateSum<KD, NV> more;
+      more.template add<P>(now.K, sh.Ud);
       ring.release(n);
+      more.add_to(s);
       s.split(sh.state(n + 1));
       if (n + 1 < chunks) named_arrive(kStateToSide, kBothThreads);
       named_sync(kChain, kChainThreads);
@@ -1131,11 +1140,13 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
       // dS = gam_63 dS + Q^T scale gam dO - K^T gam dV
       const float keep = gate.gam[C - 1];
       s.each([&](int, int, float& p, float& q) { p = cuts ? 0.0f : keep * p, q = cuts ? 0.0f : keep * q; });
+      StateSum<KD, NV> more;
       if (!(cuts & 1ull)) {
-        add_keys<P>(s, now.Q, sh.Od);
-        add_keys<P>(s, now.K, sh.Z);
+        more.template add<P>(now.Q, sh.Od);
+        more.template add<P>(now.K, sh.Z);
       }
       ring.release(k);
+      more.add_to(s);
       s.split(sh.S);
       float dot = 0.0f;
 #pragma unroll
