@@ -33,8 +33,8 @@
 // Products run on warp MMAs of bf16 with 32-bit sums.  An operand of 32 bits is
 // taken in three parts of 8 bits each (x = high + middle + low), one in fp16 in
 // two, and the products of parts down to 2^-16 of the largest are summed: 2^-24
-// of a factor is left out.  What only goes into a 16-bit output has two parts and
-// products down to 2^-8 (2^-16 left out).  A state carries thousands of
+// of a factor is left out.  So a 16-bit output differs from a 32-bit sum's, rounded,
+// where that lies next to a border alone.  A state carries thousands of
 // timesteps, so it is never rounded to 16 bits.  An operand is split once, where
 // it is made, and lies in shared memory as the MMA wants it.  (Split where it is
 // used, in two parts of 11 bits on MMAs of 32-bit floats, these kernels executed
@@ -70,27 +70,45 @@ constexpr float kNaN = std::numeric_limits<float>::quiet_NaN();
 
 using bf16 = __nv_bfloat16;
 
-// Parts of a value of T; of an operand of the sums that only a T is made of, and how far their products go (see `mma`).
+// Parts of a value of T.
 template <typename T>
 constexpr int kParts = sizeof(T) == 4 ? 3 : std::is_same_v<T, bf16> ? 1 : 2;
-template <typename T>
-constexpr int kOutParts = sizeof(T) == 4 ? 3 : 2;
-template <typename T>
-constexpr int kOutDepth = sizeof(T) == 4 ? 2 : 1;
 
 // ---- matrices in shared memory and the products of warps ---------------------
 
-// [kRows][W] values, kP parts of each, one matrix behind the other.  16-byte pieces of a row are exchanged by a rule on the row:
-// the same piece of eight neighbouring rows lies in different banks.
-template <int kRows, int W, int kP>
-struct Mat {
-  bf16* p;
-  static constexpr int kSize = kRows * W, kBytes = kSize * kP * 2;
+// Where a value of a matrix of W columns lies.  16-byte pieces of a row are exchanged by a rule on the row: the same piece of eight
+// neighbouring rows lies in different banks.
+template <int W>
+__device__ __forceinline__ int place(int row, int col) {
+  constexpr int kPieces = W / 8;
+  const int turn = kPieces >= 8 ? row & 7 : row / (8 / kPieces) & (kPieces - 1);
+  return row * W + (col ^ turn << 3);
+}
+// The layouts of matrices: all values;
+template <int kRows, int W>
+struct Whole {
+  static constexpr int kSize = kRows * W;
+  __device__ __forceinline__ static int at(int row, int col) { return place<W>(row, col); }
+};
+// those of a square one that is zero above the diagonal, without the upper right quarter, which nobody asks for (two stages of whole
+// ones do not fit beside 32 columns of S and 128 wide keys).
+template <int W>
+struct Lower {
+  static constexpr int kHalf = W / 2, kSize = kHalf * kHalf + kHalf * W;
+  __device__ __forceinline__ static bool has(int row, int col) { return row >= kHalf || col < kHalf; }
   __device__ __forceinline__ static int at(int row, int col) {
-    constexpr int kPieces = W / 8;
-    const int turn = kPieces >= 8 ? row & 7 : row / (8 / kPieces) & (kPieces - 1);
-    return row * W + (col ^ turn << 3);
+    return row < kHalf ? place<kHalf>(row, col) : kHalf * kHalf + place<W>(row - kHalf, col);
   }
+};
+
+// kP parts of each of its values, one matrix behind the other.
+template <typename Layout, int kP>
+struct MatOf : Layout {
+  bf16* p;
+  __device__ __forceinline__ explicit MatOf(bf16* p_) : p(p_) {}
+  using Layout::at;
+  using Layout::kSize;
+  static constexpr int kHas = kP, kBytes = kSize * kP * 2;
   // Columns col and col + 1 (col even).
   __device__ __forceinline__ void put(int row, int col, float x, float y) const {
     const int i = at(row, col);
@@ -130,6 +148,8 @@ struct Mat {
     return s;
   }
 };
+template <int kRows, int W, int kP>
+using Mat = MatOf<Whole<kRows, W>, kP>;
 
 // The loads and MMAs below are reached by whole warps: a barrier lies before each, and between that and the last of them only
 // branches that a warp's lanes take alike.  Lane = 4 g + t of an MMA has rows g and g + 8 and columns 2 t and 2 t + 1 of its
@@ -138,26 +158,26 @@ __device__ __forceinline__ int lane_g() { return (threadIdx.x & 31) >> 2; }
 __device__ __forceinline__ int lane_t() { return threadIdx.x & 3; }
 
 // A, 16 rows and 16 columns (k): kP parts of it, from rows that are A's; from rows that are A's columns.
-template <int kP, int kRows, int W, int kHas>
-__device__ __forceinline__ void load_a(const Mat<kRows, W, kHas>& m, int m0, int k0, uint32_t (&a)[kP][4]) {
-  static_assert(kP <= kHas, "parts");
+template <int kP, typename M>
+__device__ __forceinline__ void load_a(const M& m, int m0, int k0, uint32_t (&a)[kP][4]) {
+  static_assert(kP <= M::kHas, "parts");
   const int l = threadIdx.x & 31;
   const uint32_t addr = smem_u32(m.p + m.at(m0 + (l & 15), k0 + (l >> 4) * 8));
 #pragma unroll
   for (int q = 0; q < kP; ++q) ldmatrix4<true>(addr + q * m.kSize * 2, a[q]);
 }
-template <int kP, int kRows, int W, int kHas>
-__device__ __forceinline__ void load_at(const Mat<kRows, W, kHas>& m, int m0, int k0, uint32_t (&a)[kP][4]) {
-  static_assert(kP <= kHas, "parts");
+template <int kP, typename M>
+__device__ __forceinline__ void load_at(const M& m, int m0, int k0, uint32_t (&a)[kP][4]) {
+  static_assert(kP <= M::kHas, "parts");
   const int l = threadIdx.x & 31;
   const uint32_t addr = smem_u32(m.p + m.at(k0 + (l & 7) + (l >> 4) * 8, m0 + (l >> 3 & 1) * 8));
 #pragma unroll
   for (int q = 0; q < kP; ++q) ldmatrix4_trans<true>(addr + q * m.kSize * 2, a[q]);
 }
 // B, 16 rows (k) and 16 columns, [part][column / 8][k / 8]: from rows that are B's columns; from rows that are B's.
-template <int kP, int kRows, int W, int kHas>
-__device__ __forceinline__ void load_b(const Mat<kRows, W, kHas>& m, int n0, int k0, uint32_t (&b)[kP][2][2]) {
-  static_assert(kP <= kHas, "parts");
+template <int kP, typename M>
+__device__ __forceinline__ void load_b(const M& m, int n0, int k0, uint32_t (&b)[kP][2][2]) {
+  static_assert(kP <= M::kHas, "parts");
   const int l = threadIdx.x & 31;
   const uint32_t addr = smem_u32(m.p + m.at(n0 + (l & 7) + (l >> 4) * 8, k0 + (l >> 3 & 1) * 8));
 #pragma unroll
@@ -167,9 +187,9 @@ __device__ __forceinline__ void load_b(const Mat<kRows, W, kHas>& m, int n0, int
     b[q][0][0] = r[0], b[q][0][1] = r[1], b[q][1][0] = r[2], b[q][1][1] = r[3];
   }
 }
-template <int kP, int kRows, int W, int kHas>
-__device__ __forceinline__ void load_bt(const Mat<kRows, W, kHas>& m, int n0, int k0, uint32_t (&b)[kP][2][2]) {
-  static_assert(kP <= kHas, "parts");
+template <int kP, typename M>
+__device__ __forceinline__ void load_bt(const M& m, int n0, int k0, uint32_t (&b)[kP][2][2]) {
+  static_assert(kP <= M::kHas, "parts");
   const int l = threadIdx.x & 31;
   const uint32_t addr = smem_u32(m.p + m.at(k0 + (l & 15), n0 + (l >> 4) * 8));
 #pragma unroll
@@ -180,9 +200,9 @@ __device__ __forceinline__ void load_bt(const Mat<kRows, W, kHas>& m, int n0, in
   }
 }
 // The same of 32 rows of k and 8 columns: [part][k / 16][k / 8 % 2].
-template <int kP, int kRows, int W, int kHas>
-__device__ __forceinline__ void load_bt_tall(const Mat<kRows, W, kHas>& m, int n0, int k0, uint32_t (&b)[kP][2][2]) {
-  static_assert(kP <= kHas, "parts");
+template <int kP, typename M>
+__device__ __forceinline__ void load_bt_tall(const M& m, int n0, int k0, uint32_t (&b)[kP][2][2]) {
+  static_assert(kP <= M::kHas, "parts");
   const uint32_t addr = smem_u32(m.p + m.at(k0 + (threadIdx.x & 31), n0));
 #pragma unroll
   for (int q = 0; q < kP; ++q) {
@@ -192,20 +212,20 @@ __device__ __forceinline__ void load_bt_tall(const Mat<kRows, W, kHas>& m, int n
   }
 }
 
-// d + e (+ f) += a b, column tile x of b: part i of a with part j of b where i + j <= kDepth, to d, e and f by i + j.
-template <int kDepth, int kPA, int kPB>
+// d + e (+ f) += a b, column tile x of b: part i of a with part j of b where i + j <= 2, to d, e and f by i + j.
+template <int kPA, int kPB>
 __device__ __forceinline__ void mma(float (&d)[4], float (&e)[4], float (&f)[4], const uint32_t (&a)[kPA][4], const uint32_t (&b)[kPB][2][2],
                                     int x) {
 #pragma unroll
   for (int i = 0; i < kPA; ++i)
 #pragma unroll
-    for (int s = kDepth; s >= 0; --s)
+    for (int s = 2; s >= 0; --s)
       if (s - i >= 0 && s - i < kPB)
         mma_16816_bf16<true, false>(s == 0 ? d : s == 1 ? e : f, a[i][0], a[i][1], a[i][2], a[i][3], b[s - i][x][0], b[s - i][x][1]);
 }
-template <int kDepth, int kPA, int kPB>
+template <int kPA, int kPB>
 __device__ __forceinline__ void mma(float (&d)[4], float (&e)[4], const uint32_t (&a)[kPA][4], const uint32_t (&b)[kPB][2][2], int x) {
-  mma<kDepth>(d, e, e, a, b, x);
+  mma(d, e, e, a, b, x);
 }
 
 // ---- what the kernels share ----------------------------------------------------
@@ -254,20 +274,21 @@ struct DeltaArgs {
   long long dgt, dgb, dbt, dbb;
 };
 
-// The workspace's parts.  M has three parts where a backward pass reads it.
+// The workspace's parts.
 template <typename T, int KD>
 using KeyMat = Mat<C, KD, kParts<T>>;
 using SquareMat = Mat<C, C, 3>;
+using LowerMat = MatOf<Lower<C>, 3>;
 template <typename T, int KD>
 constexpr size_t kKeysBytes = 2 * KeyMat<T, KD>::kBytes;
-constexpr size_t kHeadBytes = 2 * SquareMat::kBytes + sizeof(Gates);
+constexpr size_t kHeadBytes = 2 * LowerMat::kBytes + sizeof(Gates);
 
 // The resets of a chunk, for the loops over its pieces.  They come from memory and not from the stage: what a stage holds after a wait
 // that has run out may change at any time, and these loops hold barriers.
 __device__ __forceinline__ unsigned long long cuts_of(const DeltaArgs& a, int n, int chunks, int b, int h) {
-  if (n < 0 || n >= chunks) return 0ull;
+  if (!a.reset || n < 0 || n >= chunks) return 0ull;
   const unsigned char* head = a.heads + ((size_t)((long long)n * a.B + b) * a.H + h) * kHeadBytes;
-  return *reinterpret_cast<const unsigned long long*>(head + SquareMat::kBytes + offsetof(Gates, cuts));
+  return *reinterpret_cast<const unsigned long long*>(head + LowerMat::kBytes + offsetof(Gates, cuts));
 }
 
 __device__ __forceinline__ int length_of(const DeltaArgs& a, int b) {
@@ -351,22 +372,22 @@ __device__ __forceinline__ bool cut_between(unsigned long long cuts, int j, int 
 
 // ---- per chunk and key head: copies of q and k, gates, N and M --------------------
 
-template <typename T, int KD, int kMParts>
+template <typename T, int KD>
 struct PrepareShared {
-  static constexpr size_t kFirst = kKeysBytes<T, KD> > SquareMat::kBytes ? kKeysBytes<T, KD> : SquareMat::kBytes;
+  static constexpr size_t kFirst = kKeysBytes<T, KD> > LowerMat::kBytes ? kKeysBytes<T, KD> : LowerMat::kBytes;
   static constexpr int kPitch = C + 4;
   KeyMat<T, KD> K, Q;
-  SquareMat N;  // where K and Q were
+  LowerMat N;  // where K and Q were
   Gates* gates;
-  Mat<C, C, kMParts> M;  // behind the gates, as in the workspace
-  SquareMat AB;          // A B
+  LowerMat M;    // behind the gates, as in the workspace
+  SquareMat AB;  // A B
   Mat<C / 2, C / 2, 3> BH;
   float* A;  // [C][kPitch]; then N's blocks on the diagonal
-  static constexpr uint32_t kTail = sizeof(Gates) + Mat<C, C, kMParts>::kBytes;
+  static constexpr uint32_t kTail = sizeof(Gates) + LowerMat::kBytes;
   static constexpr size_t kBytes = kFirst + kTail + SquareMat::kBytes + decltype(BH)::kBytes + C * kPitch * 4;
   __device__ __forceinline__ explicit PrepareShared(unsigned char* p)
       : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * kParts<T>}, N{K.p}, gates(reinterpret_cast<Gates*>(p + kFirst)),
-        M{reinterpret_cast<bf16*>(gates + 1)}, AB{M.p + M.kSize * kMParts}, BH{AB.p + AB.kSize * 3},
+        M{reinterpret_cast<bf16*>(gates + 1)}, AB{M.p + M.kSize * 3}, BH{AB.p + AB.kSize * 3},
         A(reinterpret_cast<float*>(BH.p + BH.kSize * 3)) {}
 };
 
@@ -473,11 +494,11 @@ __device__ __forceinline__ void make_gates(const RawGates& raw, Gates& gates) {
 
 // Two blocks to an SM, so that one's loads and barriers lie behind the other's products: 2048 chunks of 128 wide bf16 keys 77 us, in
 // which 284 MB move (43 us at a copy's rate).  (With 16 warps to a block registers spill: 88.)
-template <typename T, int KD, bool kBackward>
+template <typename T, int KD>
 __global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr int P = kParts<T>;
-  using Sh = PrepareShared<T, KD, kBackward ? 3 : kOutParts<T>>;
+  using Sh = PrepareShared<T, KD>;
   constexpr int kPitch = Sh::kPitch;
   const Sh sh(smem);
   Gates& gates = *sh.gates;
@@ -510,8 +531,8 @@ __global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaA
       load_b<P>(sh.K, side + 16, k0, fb[1]);
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        mma<2>(kk[x], ke[x], fk, fb[x >> 1], x & 1);
-        mma<2>(qk[x], qe[x], fq, fb[x >> 1], x & 1);
+        mma(kk[x], ke[x], fk, fb[x >> 1], x & 1);
+        mma(qk[x], qe[x], fq, fb[x >> 1], x & 1);
       }
     }
 #pragma unroll
@@ -536,6 +557,7 @@ __global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaA
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int i = i0 + g + 8 * r, j = side + x * 8 + 2 * t;
+        if (!LowerMat::has(i0, side)) continue;
         if (side + x * 8 >= i0 + 16) {
           sh.M.put(i, j, 0.0f, 0.0f);
           sh.N.put(i, j, 0.0f, 0.0f);
@@ -602,8 +624,8 @@ __global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaA
           uint32_t fa[3][4], fb[3][2][2];
           load_a<3>(sh.AB, o + half + r0, o + k0, fa);
           load_bt<3>(sh.N, o + (c0 & ~8), o + k0, fb);
-          if (c0 & 8) mma<2>(d, e, e2, fa, fb, 1);
-          else mma<2>(d, e, e2, fa, fb, 0);
+          if (c0 & 8) mma(d, e, e2, fa, fb, 1);
+          else mma(d, e, e2, fa, fb, 0);
         }
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -626,8 +648,8 @@ __global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaA
           uint32_t fa[3][4], fb[3][2][2];
           load_a<3>(sh.N, o + half + r0, o + half + k0, fa);
           load_bt<3>(sh.BH, c0 & ~8, h0 + k0, fb);
-          if (c0 & 8) mma<2>(d, e, e2, fa, fb, 1);
-          else mma<2>(d, e, e2, fa, fb, 0);
+          if (c0 & 8) mma(d, e, e2, fa, fb, 1);
+          else mma(d, e, e2, fa, fb, 0);
         }
 #pragma unroll
         for (int r = 0; r < 2; ++r)
@@ -640,8 +662,8 @@ __global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaA
     __syncthreads();
     if (threadIdx.x == 0) {
       unsigned char* head = a.heads + ((size_t)((long long)n * a.B + b) * a.H + h) * kHeadBytes;
-      bulk_copy_s2g(head, smem_u32(sh.N.p), SquareMat::kBytes);
-      bulk_copy_s2g(head + SquareMat::kBytes, smem_u32(sh.gates), Sh::kTail);
+      bulk_copy_s2g(head, smem_u32(sh.N.p), LowerMat::kBytes);
+      bulk_copy_s2g(head + LowerMat::kBytes, smem_u32(sh.gates), Sh::kTail);
     }
   }
   if (threadIdx.x == 0) bulk_wait_all();
@@ -650,14 +672,14 @@ __global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaA
 // ---- along the chunks -------------------------------------------------------------
 
 // What a chunk brings along: parts of K and Q, N, gates, M.  Every block asks for its own copy: the blocks of a head read the same
-// 73 KB (bf16, 128 wide keys) from L2.
-template <typename T, int KD, int kMParts>
+// 69 KB (bf16, 128 wide keys) from L2.
+template <typename T, int KD>
 struct Stage {
   KeyMat<T, KD> K, Q;
-  SquareMat N;
+  LowerMat N;
   Gates* gates;
-  Mat<C, C, kMParts> M;
-  static constexpr uint32_t kKeys = (uint32_t)kKeysBytes<T, KD>, kHead = SquareMat::kBytes + sizeof(Gates) + Mat<C, C, kMParts>::kBytes;
+  LowerMat M;
+  static constexpr uint32_t kKeys = (uint32_t)kKeysBytes<T, KD>, kHead = kHeadBytes;
   static constexpr size_t kBytes = kKeys + kHead;
   __device__ __forceinline__ explicit Stage(unsigned char* p)
       : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * kParts<T>}, N{Q.p + Q.kSize * kParts<T>},
@@ -766,18 +788,17 @@ struct Operands {
       for (int n = 0; n < kTiles / 2; ++n) load_bt<PB>(B, n0 + 16 * n, k0, b[n]);
     }
   }
-  template <int kDepth>
   __device__ __forceinline__ void multiply(float (&d)[kTiles][4], float (&e)[kTiles][4], float (&f)[4]) {
     if constexpr (kTiles == 1) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s) mma<kDepth>(d[0], e[0], f, a[s], b[0], s);
+      for (int s = 0; s < 2; ++s) mma(d[0], e[0], f, a[s], b[0], s);
     } else {
 #pragma unroll
-      for (int n = 0; n < kTiles; ++n) mma<kDepth>(d[n], e[n], a[0], b[n / 2], n & 1);
+      for (int n = 0; n < kTiles; ++n) mma(d[n], e[n], a[0], b[n / 2], n & 1);
     }
   }
 };
-template <int kDepth, int PA, int PB, int kTiles, int kLength, bool kTransA, typename MatA, typename MatB>
+template <int PA, int PB, int kTiles, int kLength, bool kTransA, typename MatA, typename MatB>
 __device__ __forceinline__ void product(float (&d)[kTiles][4], float (&e)[kTiles][4], const MatA& A, int m0, const MatB& B, int n0, int k0) {
   using Ops = Operands<PA, PB, kTiles, kTransA>;
   constexpr int kSteps = kLength / Ops::kDepthOf;
@@ -787,7 +808,7 @@ __device__ __forceinline__ void product(float (&d)[kTiles][4], float (&e)[kTiles
 #pragma unroll
   for (int k = 0; k < kSteps; ++k) {
     if (k + 1 < kSteps) ops[(k + 1) & 1].load(A, m0, B, n0, k0 + (k + 1) * Ops::kDepthOf);
-    ops[k & 1].template multiply<kDepth>(d, e, f);
+    ops[k & 1].multiply(d, e, f);
   }
   if constexpr (kTiles == 1)
 #pragma unroll
@@ -801,7 +822,7 @@ struct StateSum {
   float d[Part::kTiles][4] = {}, e[Part::kTiles][4] = {};
   template <int P, int kHas>
   __device__ __forceinline__ void add(const Mat<C, KD, kHas>& keys, const Mat<C, NV, 3>& rows) {
-    product<2, P, 3, Part::kTiles, C, true>(d, e, keys, Part::row0(), rows, Part::col0(), 0);
+    product<P, 3, Part::kTiles, C, true>(d, e, keys, Part::row0(), rows, Part::col0(), 0);
   }
   __device__ __forceinline__ void add_to(Part& s) const {
 #pragma unroll
@@ -811,25 +832,24 @@ struct StateSum {
   }
 };
 // The same for a matrix [64][64] that is zero above the diagonal.
-template <int kDepth, int PA, int PB, int kTiles, bool kTransA, typename MatA, typename MatB>
+template <int PA, int PB, int kTiles, bool kTransA, typename MatA, typename MatB>
 __device__ __forceinline__ void product_lower(float (&d)[kTiles][4], float (&e)[kTiles][4], const MatA& A, int m0, const MatB& B, int n0) {
-  if (kTransA ? m0 >= C / 2 : m0 < C / 2) product<kDepth, PA, PB, kTiles, C / 2, kTransA>(d, e, A, m0, B, n0, kTransA ? C / 2 : 0);
-  else product<kDepth, PA, PB, kTiles, C, kTransA>(d, e, A, m0, B, n0, 0);
+  if (kTransA ? m0 >= C / 2 : m0 < C / 2) product<PA, PB, kTiles, C / 2, kTransA>(d, e, A, m0, B, n0, kTransA ? C / 2 : 0);
+  else product<PA, PB, kTiles, C, kTransA>(d, e, A, m0, B, n0, 0);
 }
 
 template <typename T, int KD, int NV>
 struct ForwardShared {
-  static constexpr int kOut = kOutParts<T>, kN = kStages<T, KD>;
-  using St = Stage<T, KD, kOut>;
+  static constexpr int kN = kStages<T, KD>;
+  using St = Stage<T, KD>;
   using SMat = Mat<KD, NV, 3>;
   SMat S;  // before the chunk; the next one's behind it
-  Mat<C, NV, 3> X, Ud;
-  Mat<C, NV, kOut> U;
+  Mat<C, NV, 3> X, Ud, U;
   uint64_t* bars;  // [2 kN]
-  static constexpr size_t kBytes = kN * St::kBytes + 2 * SMat::kBytes + 2 * decltype(X)::kBytes + decltype(U)::kBytes + 16 * kN;
+  static constexpr size_t kBytes = kN * St::kBytes + 2 * SMat::kBytes + 3 * decltype(X)::kBytes + 16 * kN;
   __device__ __forceinline__ explicit ForwardShared(unsigned char* p)
       : S{reinterpret_cast<bf16*>(p + kN * St::kBytes)}, X{S.p + 2 * S.kSize * 3}, Ud{X.p + X.kSize * 3}, U{Ud.p + Ud.kSize * 3},
-        bars(reinterpret_cast<uint64_t*>(U.p + U.kSize * kOut)) {}
+        bars(reinterpret_cast<uint64_t*>(U.p + U.kSize * 3)) {}
   __device__ __forceinline__ SMat state(int n) const { return SMat{S.p + (n & 1) * S.kSize * 3}; }
 };
 
@@ -838,7 +858,7 @@ struct ForwardShared {
 template <typename T, int KD, int NV>
 __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
-  constexpr int P = kParts<T>, kOut = kOutParts<T>, kDepth = kOutDepth<T>;
+  constexpr int P = kParts<T>;
   using Sh = ForwardShared<T, KD, NV>;
   using St = typename Sh::St;
   constexpr int kN = Sh::kN;
@@ -908,7 +928,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
         __syncwarp();
         {
           float d[kTiles][4] = {}, e[kTiles][4] = {};
-          if (!cut_before(cuts, lo)) product<2, P, 3, kTiles, KD, false>(d, e, now.K, rb, S0, cb, 0);
+          if (!cut_before(cuts, lo)) product<P, 3, kTiles, KD, false>(d, e, now.K, rb, S0, cb, 0);
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
             const int i = rb + g + 8 * r;
@@ -925,7 +945,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
         named_sync(kChain, kChainThreads);
         {
           float d[kTiles][4] = {}, e[kTiles][4] = {};
-          product_lower<2, 3, 3, kTiles, false>(d, e, now.N, rb, sh.X, cb);
+          product_lower<3, 3, kTiles, false>(d, e, now.N, rb, sh.X, cb);
           named_sync(kToChain, kBothThreads);  // the U before has been read
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
@@ -980,7 +1000,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
         float d[kTiles][4] = {}, e[kTiles][4] = {};
         __syncwarp();
         if (!cut_before(cuts, lo)) {
-          product<kDepth, P, kOut, kTiles, KD, false>(d, e, now.Q, rb, sh.state(n), 0, 0);
+          product<P, 3, kTiles, KD, false>(d, e, now.Q, rb, sh.state(n), 0, 0);
 #pragma unroll
           for (int c = 0; c < kTiles; ++c)
 #pragma unroll
@@ -988,7 +1008,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
         }
         named_arrive(kToChain, kBothThreads);
         named_sync(kToSide, kBothThreads);
-        product_lower<kDepth, kOut, kOut, kTiles, false>(d, e, now.M, rb, sh.U, 0);
+        product_lower<3, 3, kTiles, false>(d, e, now.M, rb, sh.U, 0);
         if (hi == C) ring.release(n);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -1013,7 +1033,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_forward_kernel(const Del
 template <typename T, int KD, int NV>
 struct BackwardShared {
   static constexpr int kN = kStages<T, KD>, kLPitch = NV + 4;
-  using St = Stage<T, KD, 3>;
+  using St = Stage<T, KD>;
   Mat<KD, NV, 3> S;                // dS
   Mat<C, NV, 3> Od, Z;             // scale gam dO; B dU, then - gam B R
   Mat<C, NV, kParts<T>> O;         // dO
@@ -1084,7 +1104,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
         __syncwarp();
         {  // dU = scale M^T dO + dec K dS
           float d[kTiles][4] = {}, e[kTiles][4] = {};
-          if (hi == C) product<2, P, 3, kTiles, KD, false>(d, e, now.K, rb, sh.S, cb, 0);
+          if (hi == C) product<P, 3, kTiles, KD, false>(d, e, now.K, rb, sh.S, cb, 0);
           named_sync(kToChain, kBothThreads);  // this piece's L and Od
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
@@ -1107,7 +1127,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
         named_sync(kChain, kChainThreads);
         {  // R = dU - N^T B dU, dV = B R
           float d[kTiles][4] = {}, e[kTiles][4] = {};
-          product_lower<2, 3, 3, kTiles, true>(d, e, now.N, rb, sh.Z, cb);
+          product_lower<3, 3, kTiles, true>(d, e, now.N, rb, sh.Z, cb);
           named_sync(kChain, kChainThreads);
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
@@ -1211,7 +1231,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) delta_backward_kernel(const De
           }
         named_sync(kSide, kSideThreads);
         float d[kTiles][4] = {}, e[kTiles][4] = {};
-        product_lower<2, 3, P, kTiles, true>(d, e, now.M, rb, sh.O, 0);
+        product_lower<3, P, kTiles, true>(d, e, now.M, rb, sh.O, 0);
         if (lo == 0) ring.release(k);  // (the gates below are read before the chain is done with the chunk)
         if (k > 0 || hi < C) named_sync(kToSide, kBothThreads);  // the L and Od before have been read
         else named_sync(kSide, kSideThreads);                    // (O has been read by all, as behind the other barrier)
@@ -1244,20 +1264,17 @@ constexpr int kGradThreads = 512;
 
 template <typename T, int KD>
 struct GradShared {
-  static constexpr int W = kSlice<T, KD>, P = kParts<T>, kOut = kOutParts<T>;
+  static constexpr int W = kSlice<T, KD>, P = kParts<T>;
   KeyMat<T, KD> K, Q;
   Gates* gates;
   float* sums;                                // [6][C]
   float *next_S, *next_dS, *next_R, *next_Y;  // the next round's, as they come
   // one round's: S0, dS, dO, R, U; after the last, P and E.  (Two rounds in turn, so that a warp splits one while others multiply the
   // one before, leave the L1 little: 612 us where this takes 602, forward and backward of 4 streams of 8 heads and 2048 timesteps.)
-  Mat<KD, W, 3> S;
-  Mat<KD, W, kOut> dS;
+  Mat<KD, W, 3> S, dS;
   Mat<C, W, P> dO;
-  Mat<C, W, kOut> R;
-  Mat<C, W, 3> U;
-  SquareMat Pm;
-  Mat<C, C, kOut> E;
+  Mat<C, W, 3> R, U;
+  SquareMat Pm, E;
   static constexpr size_t kFixed = kKeysBytes<T, KD> + sizeof(Gates) + 6 * C * 4 + 2 * (KD + C) * W * 4;
   static constexpr size_t kRound = decltype(S)::kBytes + decltype(dS)::kBytes + decltype(dO)::kBytes + decltype(R)::kBytes + decltype(U)::kBytes;
   static constexpr size_t kAfter = decltype(Pm)::kBytes + decltype(E)::kBytes;
@@ -1265,8 +1282,8 @@ struct GradShared {
   __device__ __forceinline__ explicit GradShared(unsigned char* p)
       : K{reinterpret_cast<bf16*>(p)}, Q{K.p + K.kSize * P}, gates(reinterpret_cast<Gates*>(Q.p + Q.kSize * P)),
         sums(reinterpret_cast<float*>(gates + 1)), next_S(sums + 6 * C), next_dS(next_S + KD * W), next_R(next_dS + KD * W),
-        next_Y(next_R + C * W), S{reinterpret_cast<bf16*>(next_Y + C * W)}, dS{S.p + S.kSize * 3}, dO{dS.p + dS.kSize * kOut},
-        R{dO.p + dO.kSize * P}, U{R.p + R.kSize * kOut}, Pm{S.p}, E{Pm.p + Pm.kSize * 3} {}
+        next_Y(next_R + C * W), S{reinterpret_cast<bf16*>(next_Y + C * W)}, dS{S.p + S.kSize * 3}, dO{dS.p + dS.kSize * 3},
+        R{dO.p + dO.kSize * P}, U{R.p + R.kSize * 3}, Pm{S.p}, E{Pm.p + Pm.kSize * 3} {}
 };
 
 // [kRows][W] values of a matrix [rows][Dv] from column v0 on, as they come (zeros past its ends).  Each thread asks for the four
@@ -1294,49 +1311,34 @@ __device__ __forceinline__ void fetch_slice(float* to, const float* from, int v0
   });
 }
 
-// x += A, y += B times the transposed rows n0.. of M (three parts), over kLength columns; two tiles of 8 rows
-// of M at a time, summed apart first (an MMA's sum is cut, not rounded, to 24 bits).
-template <int kDepth, int kTiles, int kLength, int PA, int PB, typename MatM>
-__device__ __forceinline__ void add_rows(float (&x)[kTiles][4], const uint32_t (&fa)[kLength / 16][PA][4], float (&y)[kTiles][4],
-                                         const uint32_t (&fb)[kLength / 16][PB][4], const MatM& M, int n0) {
+// x += A times the transposed rows n0.. of M (three parts), over kLength columns; two tiles of 8 rows of M at a time, summed apart first
+// (an MMA's sum is cut, not rounded, to 24 bits).
+template <int kTiles, int kLength, int PA, typename MatM>
+__device__ __forceinline__ void add_rows(float (&x)[kTiles][4], const uint32_t (&fa)[kLength / 16][PA][4], const MatM& M, int n0) {
 #pragma unroll
   for (int n = 0; n < kTiles; n += 2) {
-    float d[2][4] = {}, e[2][4] = {}, f[2][4] = {};
+    float d[2][4] = {}, e[2][4] = {};
 #pragma unroll
     for (int k = 0; k < kLength / 16; ++k) {
       uint32_t m[3][2][2];
       load_b<3>(M, n0 + n * 8, k * 16, m);
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        mma<2>(d[z], e[z], fa[k], m, z);
-        mma<kDepth>(f[z], f[z], fb[k], m, z);
-      }
+      mma(d[0], e[0], fa[k], m, 0);
+      mma(d[1], e[1], fa[k], m, 1);
     }
 #pragma unroll
     for (int z = 0; z < 2; ++z)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x[n + z][r] += d[z][r] + e[z][r], y[n + z][r] += f[z][r];
+      for (int r = 0; r < 4; ++r) x[n + z][r] += d[z][r] + e[z][r];
   }
 }
-// x += A times the transposed rows of M, in what goes into outputs alone.
-template <int kDepth, int kTiles, int kLength, int PA, int kHas, int kRows>
-__device__ __forceinline__ void add_rows(float (&x)[kTiles][4], const uint32_t (&fa)[kLength / 16][PA][4], const Mat<kRows, kLength, kHas>& M,
-                                         int n0) {
+
+// x += a b, of 16 rows of k.
+template <int kPA, int kPB>
+__device__ __forceinline__ void add_mma(float (&x)[4], const uint32_t (&a)[kPA][4], const uint32_t (&b)[kPB][2][2], int tile) {
+  float d[4] = {}, e[4] = {};
+  mma(d, e, a, b, tile);
 #pragma unroll
-  for (int n = 0; n < kTiles; n += 2) {
-    float f[2][4] = {};
-#pragma unroll
-    for (int k = 0; k < kLength / 16; ++k) {
-      uint32_t m[kHas][2][2];
-      load_b<kHas>(M, n0 + n * 8, k * 16, m);
-      mma<kDepth>(f[0], f[0], fa[k], m, 0);
-      mma<kDepth>(f[1], f[1], fa[k], m, 1);
-    }
-#pragma unroll
-    for (int z = 0; z < 2; ++z)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) x[n + z][r] += f[z][r];
-  }
+  for (int r = 0; r < 4; ++r) x[r] += d[r] + e[r];
 }
 
 // By columns of S, 32 at a time: the next ones come as copies while 16 warps multiply.  1024 chunks of bf16, 128 x 128: 204 us, half
@@ -1344,7 +1346,7 @@ __device__ __forceinline__ void add_rows(float (&x)[kTiles][4], const uint32_t (
 template <typename T, int KD>
 __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
-  constexpr int W = kSlice<T, KD>, P = kParts<T>, kOut = kOutParts<T>, kDepth = kOutDepth<T>;
+  constexpr int W = kSlice<T, KD>, P = kParts<T>;
   constexpr int kPart = KD / 4, kTiles = kPart / 8;  // a warp has 16 rows and a quarter of the columns
   using Sh = GradShared<T, KD>;
   const Sh sh(smem);
@@ -1378,7 +1380,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
     const T* d_o = static_cast<const T*>(a.d_o) + t0 * a.dos.t + b * a.dos.b + h * a.dos.h;
     const float *S = a.states + chunk * (a.Dk + C) * a.Dv, *Y = S + DD, *dS = a.dS + chunk * DD, *R = a.R + chunk * C * a.Dv;
     __syncthreads();
-    fetch<(int)sizeof(Gates), kGradThreads>(sh.gates, a.heads + (size_t)chunk * kHeadBytes + SquareMat::kBytes);
+    fetch<(int)sizeof(Gates), kGradThreads>(sh.gates, a.heads + (size_t)chunk * kHeadBytes + LowerMat::kBytes);
     if (h == hk * a.share) fetch<(int)kKeysBytes<T, KD>, kGradThreads>(sh.K.p, a.keys + where * kKeysBytes<T, KD>);
     // (R and Y as copies too: held in registers while a round is multiplied, the forward and backward passes took 636 us, not 611.)
     auto fetch_slices = [&](int v0) {
@@ -1453,20 +1455,24 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
         __syncwarp();
         const bool below = side * 16 <= rb;  // else the warp's part of P and E lies above the diagonal
         {
-          uint32_t fo[W / 16][P][4], fr[W / 16][kOut][4];
+          uint32_t fa[W / 16][P][4];
 #pragma unroll
-          for (int k = 0; k < W / 16; ++k) {
-            load_a<P>(sh.dO, rb, k * 16, fo[k]);
-            load_a<kOut>(sh.R, rb, k * 16, fr[k]);
-          }
-          if (below) add_rows<kDepth, 2, W>(acc_p, fo, acc_e, fr, sh.U, side * 16);
-          if (!fresh) add_rows<kDepth, kTiles, W>(acc_q, fo, acc_w, fr, sh.S, side * kPart);
+          for (int k = 0; k < W / 16; ++k) load_a<P>(sh.dO, rb, k * 16, fa[k]);
+          if (below) add_rows<2, W>(acc_p, fa, sh.U, side * 16);
+          if (!fresh) add_rows<kTiles, W>(acc_q, fa, sh.S, side * kPart);
+        }
+        {
+          uint32_t fa[W / 16][3][4];
+#pragma unroll
+          for (int k = 0; k < W / 16; ++k) load_a<3>(sh.R, rb, k * 16, fa[k]);
+          if (below) add_rows<2, W>(acc_e, fa, sh.U, side * 16);
+          if (!fresh) add_rows<kTiles, W>(acc_w, fa, sh.S, side * kPart);
         }
         if (last) {
-          uint32_t fa[W / 16][kOut][4];
+          uint32_t fa[W / 16][3][4];
 #pragma unroll
-          for (int k = 0; k < W / 16; ++k) load_a<kOut>(sh.U, rb, k * 16, fa[k]);
-          add_rows<kDepth, kTiles, W>(acc_t, fa, sh.dS, side * kPart);
+          for (int k = 0; k < W / 16; ++k) load_a<3>(sh.U, rb, k * 16, fa[k]);
+          add_rows<kTiles, W>(acc_t, fa, sh.dS, side * kPart);
         }
       }
       __syncthreads();
@@ -1510,29 +1516,26 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
 #pragma unroll
       for (int k0 = 0; k0 < C; k0 += 16) {
         if (k0 > rb) continue;
-        uint32_t fp[3][4], fe[kOut][4];
+        uint32_t fp[3][4], fe[3][4];
         load_a<3>(sh.Pm, rb, k0, fp);
-        load_a<kOut>(sh.E, rb, k0, fe);
+        load_a<3>(sh.E, rb, k0, fe);
 #pragma unroll
         for (int x = 0; x < kTiles; x += 2) {
           uint32_t fb[P][2][2];
           load_bt<P>(sh.K, side * kPart + x * 8, k0, fb);
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            float d[4] = {}, e[4] = {};
-            mma<2>(d, e, fp, fb, y);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc_q[x + y][r] += d[r] + e[r];
-            mma<kDepth>(acc_w[x + y], acc_w[x + y], fe, fb, y);
+            add_mma(acc_q[x + y], fp, fb, y);
+            add_mma(acc_w[x + y], fe, fb, y);
           }
         }
       }
 #pragma unroll
       for (int k0 = 0; k0 < C; k0 += 16) {
         if (k0 < rb) continue;
-        uint32_t fp[kOut][4], fe[kOut][4];
-        load_at<kOut>(sh.Pm, rb, k0, fp);
-        load_at<kOut>(sh.E, rb, k0, fe);
+        uint32_t fp[3][4], fe[3][4];
+        load_at<3>(sh.Pm, rb, k0, fp);
+        load_at<3>(sh.E, rb, k0, fe);
 #pragma unroll
         for (int x = 0; x < kTiles; x += 2) {
           uint32_t fk[P][2][2], fq[P][2][2];
@@ -1540,8 +1543,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
           load_bt<P>(sh.Q, side * kPart + x * 8, k0, fq);
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            mma<kDepth>(acc_t[x + y], acc_t[x + y], fp, fq, y);
-            mma<kDepth>(acc_w[x + y], acc_w[x + y], fe, fk, y);
+            add_mma(acc_t[x + y], fp, fq, y);
+            add_mma(acc_w[x + y], fe, fk, y);
           }
         }
       }
@@ -1680,15 +1683,13 @@ cudaError_t for_shape(int dtype, int Dk, F f) {
   });
 }
 
-cudaError_t prepare(int dtype, const DeltaArgs& a, bool backward, cudaStream_t s) {
+cudaError_t prepare(int dtype, const DeltaArgs& a, cudaStream_t s) {
   const long long blocks = (long long)((a.T + C - 1) / C) * a.B * (a.H / a.share);
   if (blocks == 0) return cudaSuccess;
   return for_shape(dtype, a.Dk, [&](auto* t, auto kd) {
     using T = std::remove_pointer_t<decltype(t)>;
     constexpr int KD = decltype(kd)::value;
-    const dim3 grid((unsigned)blocks);
-    if (backward) return launch_big<delta_prepare_kernel<T, KD, true>>(grid, PrepareShared<T, KD, 3>::kBytes, s, a);
-    return launch_big<delta_prepare_kernel<T, KD, false>>(grid, PrepareShared<T, KD, kOutParts<T>>::kBytes, s, a);
+    return launch_big<delta_prepare_kernel<T, KD>>(dim3((unsigned)blocks), PrepareShared<T, KD>::kBytes, s, a);
   });
 }
 
@@ -1770,7 +1771,7 @@ extern "C" int lstm_approx_delta_scan(int dtype, const void* q, const void* k, c
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) / 256 * 256);
   a.keys = reinterpret_cast<unsigned char*>(ws + w.keys), a.heads = reinterpret_cast<unsigned char*>(ws + w.heads);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  if (int rc = op_launched(prepare(dtype, a, false, s), "delta scan launch", msg, msg_len)) return rc;
+  if (int rc = op_launched(prepare(dtype, a, s), "delta scan launch", msg, msg_len)) return rc;
   const int NV = columns_of((long long)B * H, Dv, es);
   a.tiles = (Dv + NV - 1) / NV;
   const dim3 grid((unsigned)(B * H * a.tiles));
@@ -1827,7 +1828,7 @@ extern "C" int lstm_approx_delta_scan_backward(int dtype, const void* d_o, const
   a.dots = reinterpret_cast<float*>(ws + w.dots);
   a.sum_q = reinterpret_cast<float*>(ws + w.sum_q), a.sum_k = reinterpret_cast<float*>(ws + w.sum_k);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  if (int rc = op_launched(prepare(dtype, a, true, s), "delta scan launch", msg, msg_len)) return rc;
+  if (int rc = op_launched(prepare(dtype, a, s), "delta scan launch", msg, msg_len)) return rc;
   const int NV = columns_of((long long)B * H, Dv, es);
   a.tiles = (Dv + NV - 1) / NV;
   const dim3 grid((unsigned)(B * H * a.tiles));
