@@ -355,9 +355,6 @@ __device__ __forceinline__ void put2(T* row, int col, int D, bool pairs, float x
   }
 }
 
-// e^x for x <= 0 from the hardware's 2^z: off by 2^-22 + |x| 2^-24 of it, which is under 2^-23 of 1.
-__device__ __forceinline__ float decay_of(float x) { return ex2_approx(x * kLog2E); }
-
 // The piece of a chunk that begins at row lo ends before this row.
 __device__ __forceinline__ int piece_end(unsigned long long cuts, int lo) {
   const unsigned long long behind = lo >= 63 ? 0ull : cuts >> (lo + 1);
@@ -568,7 +565,7 @@ __global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaA
         for (int y = 0; y < 2; ++y) {
           const float dist = (gates.g_high[i] - gates.g_high[j + y]) + (gates.g_low[i] - gates.g_low[j + y]);
           const bool same = i >= j + y && !(cuts && cut_between(cuts, j + y, i));
-          const float D = same ? decay_of(dist) : 0.0f;
+          const float D = same ? expf(dist) : 0.0f;
           m[y] = same ? D * qk[x][2 * r + y] : 0.0f;
           v[y] = same && i > j + y ? D * kk[x][2 * r + y] : 0.0f;
           w[y] = v[y] != 0.0f ? v[y] * gates.beta[j + y] : 0.0f;  // (beta of another document: anything)
@@ -1490,7 +1487,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const 
           for (int y = 0; y < 2; ++y) {
             const float dist = (gate.g_high[i] - gate.g_high[j + y]) + (gate.g_low[i] - gate.g_low[j + y]);
             const bool both = in && i >= j + y && j + y >= lo;
-            const float D = both ? decay_of(dist) : 0.0f;
+            const float D = both ? expf(dist) : 0.0f;
             p[y] = both ? a.scale * D * acc_p[x][2 * r + y] : 0.0f;
             e[y] = both && i > j + y ? beta * D * acc_e[x][2 * r + y] : 0.0f;
           }

@@ -66,3 +66,25 @@ def test_gradients_of_a_key(cuda_device, dtype):
              h0={(0, 0, 4, 2): X, (0, 0, 4, 9): Y})[3]
     want[0, 0, 0, 4] = -2.0 ** -20
     np.testing.assert_array_equal(dk, want)
+
+
+@pytest.mark.gpu
+def test_decays_inside_a_chunk(cuda_device):
+    """A value written at 0 and read at 1 along the same key, with nothing between but the decay g: o = e^g, within a unit of the
+    last place of expf, four parts' splits and products and the sum of each, half a unit: 2 + 10 half units.  (2^z of a rounded
+    z = g / ln 2 is off by |g| of them.)  The gradient of that value is the same number, made of the same parts."""
+    import torch
+    from paper_1905_00689_gb300 import delta_scan, delta_scan_backward, delta_scan_states
+    B, Dk, Dv = 400, 8, 1
+    g = torch.zeros(2, B, 1, device="cuda")
+    g[1, :, 0] = -20.0 - 20.0 * torch.rand(B, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    q, k, v = (torch.zeros(2, B, 1, d, device="cuda") for d in (Dk, Dk, Dv))
+    q[1, ..., 0], k[0, ..., 0], v[0] = 1.0, 1.0, 1.0
+    beta, do = torch.ones(2, B, 1, device="cuda"), torch.zeros(2, B, 1, Dv, device="cuda")
+    do[1] = 1.0
+    states = delta_scan_states(q, v)
+    o, _ = delta_scan(q, k, v, g, beta, states=states, scale=1.0)
+    grads = delta_scan_backward(do, q, k, v, g, beta, states, scale=1.0)
+    want = np.exp(ref.f64(g[1, :, 0]))
+    for got in (o[1, :, 0, 0], grads[2][0, :, 0, 0], grads[0][1, :, 0, 0]):
+        assert (np.abs(ref.f64(got) - want) <= 12 * 2.0 ** -24 * want).all()
