@@ -380,7 +380,8 @@ int lstm_approx_delta_step(int dtype, const void *q, const void *k, const void *
  *
  *   step      t >= 1, or step_at: a DEVICE int32 that holds it (for captured
  *             graphs; it is read, not changed);  lr, or lr_at: a DEVICE float
- *   beta1, beta2  in [0, 1);  eps >= 0
+ *   beta1, beta2  in [0, 1);  eps 0 (a value whose averages are zero is NaN then, 0 / 0) or
+ *             between 2^-126 and 2^126
  *   grad_scale  DEVICE float that multiplies every gradient, or NULL
  *   skip      DEVICE byte, or NULL: where not zero nothing changes
  * Several hundred tensors go into one launch.

@@ -306,7 +306,8 @@ def adamw_step(params, grads, state: AdamWState, step, *, lr, betas=(0.9, 0.999)
     state: :class:`AdamWState`; 8-bit averages are rounded at random (`seed`, step and
     position choose), so that they move on average by what they should.  copies: a
     list of tensors (or None) that receive the parameters in a type of their own, as
-    the next forward pass reads them.
+    the next forward pass reads them.  eps is 0 (where both averages are zero the parameter
+    becomes NaN then) or between 2 ** -126 and 2 ** 126.
 
     step: the number of this update, from 1; or a CUDA int32 tensor of one value that
     holds it, for captured graphs (read, not changed: count it up before the call, in

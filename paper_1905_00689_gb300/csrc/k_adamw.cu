@@ -355,6 +355,10 @@ extern "C" int lstm_approx_adamw_step(int count, const lstm_approx_adamw_tensor*
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "betas must lie in [0, 1)");
   if (!(eps >= 0.0) || !std::isfinite(eps) || !std::isfinite(weight_decay) || (!lr_at && !std::isfinite(lr)))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "lr and weight_decay must be finite, eps finite and not negative");
+  // (the reciprocal of what is below or above counts as that of zero or as zero: 0 / eps would not be 0)
+  const float least = 1.17549435e-38f, most = 8.50705917e37f;
+  if (eps != 0.0 && !((float)eps >= least && (float)eps <= most))
+    return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "eps must be 0 or between 2^-126 and 2^126");
   if (!op_aligned(step_at, 4) || !op_aligned(lr_at, 4) || !op_aligned(grad_scale, 4))
     return op_report(msg, msg_len, LSTM_APPROX_EINVAL, "a pointer not aligned to its type");
   for (int i = 0; i < count; ++i) {
