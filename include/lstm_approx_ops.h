@@ -374,7 +374,9 @@ int lstm_approx_delta_step(int dtype, const void *q, const void *k, const void *
  *             values: largest magnitude / 448, at least 2^-126.  They are
  *             rounded to either neighbour with the chances that keep the mean, by a
  *             hash of seed, step and the value's position among all tensors'; a
- *             sqrt(v) above zero does not become zero.
+ *             sqrt(v) above zero does not become zero.  Values that are not finite (a
+ *             gradient's, or its square) take the averages of their 256 along, from the
+ *             next step on.
  *   copy      n values of copy_dtype that receive p, or NULL
  * No two of the tensors overlap.
  *

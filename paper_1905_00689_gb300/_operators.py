@@ -304,7 +304,8 @@ def adamw_step(params, grads, state: AdamWState, step, *, lr, betas=(0.9, 0.999)
     fp16 each (a parameter in 16 bits is rounded to the nearest, so steps below
     half a unit of it are lost); a gradient of None leaves its tensor as it is.
     state: :class:`AdamWState`; 8-bit averages are rounded at random (`seed`, step and
-    position choose), so that they move on average by what they should.  copies: a
+    position choose), so that they move on average by what they should; one that is
+    not finite takes those of its 256 values along, from the next step on.  copies: a
     list of tensors (or None) that receive the parameters in a type of their own, as
     the next forward pass reads them.  eps is 0 (where both averages are zero the parameter
     becomes NaN then) or between 2 ** -126 and 2 ** 126.

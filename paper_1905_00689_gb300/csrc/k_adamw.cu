@@ -40,6 +40,7 @@ constexpr int kTile = kThreads * 8;
 constexpr int kBlock = 256;  // values to a scale
 static_assert(kBlock == 32 * 8, "a warp's values share a scale");
 constexpr float kMost = 448.0f, kMinScale = 1.17549435e-38f;  // of e4m3; 2^-126
+constexpr float kLeastY = 5.42101086e-20f;                     // 2^-64
 
 struct AdamWTensor {
   void *p, *m, *v, *copy;
@@ -185,14 +186,17 @@ __device__ __forceinline__ float scale_of(const float (&x)[8]) {
 }
 
 // sqrt x of two values: Newton's step on y = x^-1/2 with the exact remainder (P. Markstein, "Computation of elementary functions
-// on the IBM RISC System/6000 processor", 1990).  Rounded to the nearest for all of the 2^24 fractions and both parities of the
-// exponent; below 2^-126 x 2^63.
+// on the IBM RISC System/6000 processor", 1990), rounded as sqrtf's from 2^-126 on; below, about x 2^63.  Of infinity, where the
+// remainder has no value, x 2^-64, which is less than any other root.  (Without that 877 us, with it 883: 302 M parameters with
+// 8-bit averages.)
 __device__ __forceinline__ void roots_of(uint64_t x, float x0, float x1, float& u0, float& u1) {
-  float y0, y1;
+  float y0, y1, r0, r1, l0, l1;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(fmaxf(x0, kMinScale)));
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(fmaxf(x1, kMinScale)));
   const uint64_t y = f32x2(y0, y1), g = mul2(x, y), half = f32x2(0.5f, 0.5f), minus = f32x2(-1.0f, -1.0f);
-  f32x2_split(fma2(fma2(mul2(g, minus), g, x), mul2(y, half), g), u0, u1);
+  f32x2_split(fma2(fma2(mul2(g, minus), g, x), mul2(y, half), g), r0, r1);
+  f32x2_split(mul2(x, f32x2(kLeastY, kLeastY)), l0, l1);
+  u0 = fmaxf(r0, l0), u1 = fmaxf(r1, l1);  // (NaN in both of NaN)
 }
 
 struct Rates {
@@ -206,7 +210,8 @@ struct Update {
 };
 
 // Loads, to be followed by update() when the rates are there.
-template <int kBits, bool kNear>
+// kExact: roots by sqrtf's.
+template <int kBits, bool kNear, bool kExact>
 struct Tile {
   float p[8], g[8], m[8], v[8];
   uint2 m8, v8;
@@ -250,7 +255,9 @@ struct Tile {
       vv = fma2(mul2(vv, b2), one, mul2(mul2(gs, gs), b2_rest));
       f32x2_split(mm, m[e], m[e + 1]);
       f32x2_split(vv, v[e], v[e + 1]);
-      if constexpr (kBits == 8) {
+      if constexpr (kExact) {
+        u[e] = __fsqrt_rn(v[e]), u[e + 1] = __fsqrt_rn(v[e + 1]);
+      } else if constexpr (kBits == 8) {
         roots_of(vv, v[e], v[e + 1], u[e], u[e + 1]);
       } else {
         asm("sqrt.approx.f32 %0, %1;" : "=f"(u[e]) : "f"(v[e]));
@@ -297,7 +304,7 @@ struct Tile {
   }
 };
 
-template <int kBits, int kTensors, bool kWide>
+template <int kBits, int kTensors, bool kWide, bool kExact = false>
 __global__ void __launch_bounds__(kThreads, kBits == 8 ? 5 : 4) adamw_kernel(const __grid_constant__ AdamWArgs<kTensors> a) {
   begin_op();
   const AdamWShared& all = a.all;
@@ -314,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, kBits == 8 ? 5 : 4) adamw_kernel(con
   const Update w{all.grad_scale ? *all.grad_scale : 1.0f, all.b1, all.b1_rest, all.b2, all.b2_rest, mix(mix(all.seed + 1u) ^ (unsigned)step)};
   Rates rates{};
   auto run = [&](auto near, long long at, int left, bool first) {
-    Tile<kBits, decltype(near)::value> tile;
+    Tile<kBits, decltype(near)::value, kExact> tile;
     tile.load(t, at, left);
     if (first) {  // 1 - b^t = -(e^(t log b) - 1), without the cancellation of small t; while the loads are under way
       const float lr = all.lr_at ? *all.lr_at : all.lr, n = (float)step;
@@ -331,9 +338,12 @@ __global__ void __launch_bounds__(kThreads, kBits == 8 ? 5 : 4) adamw_kernel(con
   }
 }
 
+// Roots below 2^-63 by roots_of are too small, which beside an eps of 1e-9 nobody sees (1e-19, 1000 times that for a beta2 of
+// 0.999999); with a smaller eps, or none, 8-bit averages take sqrtf's (973 us where roots_of takes 883).
 template <int kTensors>
 cudaError_t launch(int bits, bool wide, const AdamWArgs<kTensors>& a, unsigned tiles, cudaStream_t s) {
-  auto kern = bits == 8 ? (wide ? adamw_kernel<8, kTensors, true> : adamw_kernel<8, kTensors, false>)
+  auto kern = bits == 8 && a.all.eps < 1e-9f ? (wide ? adamw_kernel<8, kTensors, true, true> : adamw_kernel<8, kTensors, false, true>)
+              : bits == 8 ? (wide ? adamw_kernel<8, kTensors, true> : adamw_kernel<8, kTensors, false>)
                         : (wide ? adamw_kernel<32, kTensors, true> : adamw_kernel<32, kTensors, false>);
   return op_launch(kern, dim3(tiles), dim3(kThreads), 0, s, a);
 }

@@ -38,3 +38,39 @@ def test_least_and_largest_eps(cuda_device, bits, eps):
     if eps < 1:
         want[256:] -= 0.25
     ref.check(p[0], want, 1.0, 32 * ref.U32, what="p")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("apart", [0, 1])
+@pytest.mark.parametrize("eps", [2.0 ** -100, 1e-8])
+def test_gradients_of_any_finite_size(cuda_device, bits, apart, eps):
+    """A gradient whose square is beyond the type: v is infinite, the parameter stays where its decay takes it, in this step and the
+    next, and its neighbours' step is theirs.  One whose square is below 2^-126 (few bits) or none: the step of those bits."""
+    import torch
+    from paper_1905_00689_gb300 import AdamWState, adamw_step
+    n = 600
+    p, g = [torch.ones(n + 1, device="cuda")[apart:apart + n]], [torch.zeros(n + 1, device="cuda")[apart:apart + n]]
+    g[0][:] = 0.5
+    sizes = {3: 1e20, 40: -3e38, 300: 2.0 ** -70, 301: -2.0 ** -73, 302: 2.0 ** -63, 303: 1.8e19}
+    for i, x in sizes.items():
+        g[0][i] = x
+    state = AdamWState.zeros(p, bits)
+    adamw_step(p, g, state, 1, lr=0.25, weight_decay=0.5, betas=(0.5, 0.5), eps=eps)
+    # the step of v in 32 bits as it is held: few bits below 2^-126
+    grad = ref.f64(g[0]).astype(np.float32)
+    with np.errstate(over="ignore"):
+        v = (grad * grad) * np.float32(0.5)
+    step = 0.25 * grad / (np.sqrt(v.astype(np.float64) * 2.0) + eps)
+    ref.check(p[0], 0.875 - step, 1.0 + np.abs(step), 32 * ref.U32, what="p")
+    v1 = ref.f64(state.exp_avg_sq[0])
+    if bits == 32:
+        ref.check(v1, v.astype(np.float64), np.where(np.isinf(v), 0.0, v), 8 * ref.U32, what="v")
+    else:
+        assert np.isinf(ref.f64(state.exp_avg_sq_scale[0])[0]) and np.isfinite(ref.f64(state.exp_avg_sq_scale[0])[1:]).all()
+        assert np.isfinite(ref.f64(state.exp_avg_scale[0])).all()
+    before = ref.f64(p[0])
+    adamw_step(p, [torch.zeros_like(p[0])], state, 2, lr=0.25, weight_decay=0.5, betas=(0.5, 0.5), eps=eps)
+    for i in (3, 40):
+        assert abs(float(p[0][i]) - before[i] * 0.875) <= 4 * ref.U32
+    assert torch.isfinite(p[0]).all()
