@@ -371,8 +371,8 @@ int lstm_approx_delta_step(int dtype, const void *q, const void *k, const void *
  *             tensor is left as it is.
  *   m, v      bits 32: the two averages, fp32.  bits 8: m and sqrt(v) as E4M3
  *             with scales m_scale, v_scale [ceil(n / 256)] fp32, one for each 256
- *             values: largest magnitude / 448, at least 2^-126.  They are
- *             rounded to either neighbour with the chances that keep the mean, by a
+ *             values: largest magnitude times 1 / 448 (the 32-bit number), at least
+ *             2^-126.  They are rounded to either neighbour with the chances that keep the mean, by a
  *             hash of seed, step and the value's position among all tensors'; a
  *             sqrt(v) above zero does not become zero.  Values that are not finite (a
  *             gradient's, or its square) take the averages of their 256 along, from the

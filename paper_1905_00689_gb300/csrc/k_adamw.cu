@@ -176,7 +176,8 @@ __device__ __forceinline__ float max_or_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-// The scale of a warp's 256 values (a NaN among them makes it one).
+// The scale of a warp's 256 values (a NaN among them makes it one).  Times the 32-bit number next to 1 / 448: a division by 448 is
+// off by half a unit instead of one, and took 914 us where this takes 891 (302 M parameters).
 __device__ __forceinline__ float scale_of(const float (&x)[8]) {
   float most = fabsf(x[0]);
 #pragma unroll

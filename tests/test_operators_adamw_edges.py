@@ -74,3 +74,26 @@ def test_gradients_of_any_finite_size(cuda_device, bits, apart, eps):
     for i in (3, 40):
         assert abs(float(p[0][i]) - before[i] * 0.875) <= 4 * ref.U32
     assert torch.isfinite(p[0]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("eps", [1e-8, 0.0])
+def test_scales_follow_from_the_formula_alone(cuda_device, eps):
+    """Each operation rounded by itself, the root as sqrtf's: the bits of the scales of 2^17 blocks, whose largest value an average
+    alone makes.  (eps of 0 takes other roots; a parameter whose averages are zero is NaN then.)"""
+    import torch
+    from paper_1905_00689_gb300 import AdamWState, adamw_step
+    blocks = 1 << 17
+    rng = np.random.default_rng(8)
+    scale = (rng.random(blocks) + 1).astype(np.float32) * np.float32(2.0) ** rng.integers(-20, 20, blocks).astype(np.float32)
+    codes = torch.zeros(blocks, 256, device="cuda")
+    codes[:, 77] = 448.0
+    codes = codes.to(torch.float8_e4m3fn).view(-1)
+    held = torch.tensor(scale, device="cuda")
+    state = AdamWState([codes.clone()], [codes.clone()], [held.clone()], [held.clone()])
+    p = [torch.zeros(blocks * 256, dtype=torch.bfloat16, device="cuda")]
+    adamw_step(p, [torch.zeros_like(p[0])], state, 5, lr=0.1, betas=(0.9, 0.7), eps=eps)
+    most, part = np.float32(448) * scale, np.float32(1) / np.float32(448)
+    m, u = most * np.float32(0.9), np.sqrt(most * most * np.float32(0.7))
+    np.testing.assert_array_equal(state.exp_avg_scale[0].cpu().numpy(), m * part)
+    np.testing.assert_array_equal(state.exp_avg_sq_scale[0].cpu().numpy(), u * part)
