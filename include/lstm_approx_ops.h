@@ -378,7 +378,8 @@ int lstm_approx_delta_step(int dtype, const void *q, const void *k, const void *
  *             gradient's, or its square) take the averages of their 256 along, from the
  *             next step on.
  *   copy      n values of copy_dtype that receive p, or NULL
- * No two of the tensors overlap.
+ * No two of the tensors overlap, but for gradients among themselves; g and copy may be
+ * p itself, of p's type.
  *
  *   step      t >= 1, or step_at: a DEVICE int32 that holds it (for captured
  *             graphs; it is read, not changed);  lr, or lr_at: a DEVICE float

@@ -303,6 +303,8 @@ def adamw_step(params, grads, state: AdamWState, step, *, lr, betas=(0.9, 0.999)
     params, grads: lists of contiguous CUDA tensors of one device, fp32, bf16 or
     fp16 each (a parameter in 16 bits is rounded to the nearest, so steps below
     half a unit of it are lost); a gradient of None leaves its tensor as it is.
+    What is written overlaps nothing else of the call (a gradient or copy may be the
+    parameter itself).
     state: :class:`AdamWState`; 8-bit averages are rounded at random (`seed`, step and
     position choose), so that they move on average by what they should; one that is
     not finite takes those of its 256 values along, from the next step on.  copies: a

@@ -689,6 +689,23 @@ struct Items {
   PyObject* operator[](Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(fast, i); }
 };
 
+// Memory that a call reads, or writes.
+struct Span {
+  uintptr_t at, end;
+  bool written;
+};
+// Whether none of it that is written is written or read by another's name.
+bool apart(std::vector<Span>& spans) {
+  std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.at < b.at; });
+  uintptr_t end = 0, written_end = 0;  // of those before
+  for (const Span& s : spans) {
+    if (s.at < (s.written ? end : written_end)) return false;
+    end = std::max(end, s.end);
+    if (s.written) written_end = std::max(written_end, s.end);
+  }
+  return true;
+}
+
 // adamw_step(params, grads, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale, copies, step, lr, beta1, beta2, eps,
 // weight_decay, grad_scale, skip, seed): the averages have 8 bits where there are scales
 PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t) {
@@ -707,8 +724,12 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t) {
     Call call(tensor(params[0], "params"), "params");
     const at::ScalarType kind = few_bits ? at::kFloat8_e4m3fn : at::kFloat;
     std::vector<lstm_approx_adamw_tensor> table((size_t)count);
-    std::vector<std::pair<uintptr_t, uintptr_t>> spans;
-    spans.reserve((size_t)count);
+    std::vector<Span> spans;
+    spans.reserve((size_t)count * 7);
+    auto span = [&](const void* p, size_t bytes, bool written) {
+      const auto at = reinterpret_cast<uintptr_t>(p);
+      if (p && bytes > 0) spans.push_back({at, at + bytes, written});
+    };
     for (Py_ssize_t i = 0; i < count; ++i) {
       const Tensor& p = tensor(params[i], "params");
       lstm_approx_adamw_tensor& t = table[(size_t)i];
@@ -734,13 +755,16 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t) {
         t.g_dtype = float_code(g, "grads");
         t.g = call.dense(g, "grads", g.scalar_type(), shape);
       }
-      if (t.n > 0) {
-        const auto at = reinterpret_cast<uintptr_t>(t.p);
-        spans.emplace_back(at, at + p.nbytes());
-      }
+      span(t.p, p.nbytes(), true);
+      if (!t.g) continue;
+      const size_t average = (size_t)t.n * (few_bits ? 1 : 4), scales = (size_t)((t.n + 255) / 256) * 4;
+      // (a copy or a gradient that is the parameter itself is read before, and written after, by who reads and writes that)
+      if (t.g != t.p || t.g_dtype != t.p_dtype) span(t.g, tensor(grads[i], "grads").nbytes(), false);
+      span(t.m, average, true), span(t.v, average, true);
+      span(t.m_scale, scales, true), span(t.v_scale, scales, true);
+      if (t.copy && (t.copy != t.p || t.copy_dtype != t.p_dtype)) span(t.copy, tensor((*copies)[i], "copies").nbytes(), true);
     }
-    std::sort(spans.begin(), spans.end());
-    for (size_t i = 1; i < spans.size(); ++i) need(spans[i].first >= spans[i - 1].second, "two of params overlap");
+    need(apart(spans), "params, averages, scales and copies must not overlap one another, nor a gradient");
     auto device_value = [&](PyObject* o, const char* name, at::ScalarType type) -> const void* {
       const Tensor& t = tensor(o, name);
       need(t.numel() == 1, "step, lr, grad_scale and skip must have one value");

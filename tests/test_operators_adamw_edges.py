@@ -97,3 +97,46 @@ def test_scales_follow_from_the_formula_alone(cuda_device, eps):
     m, u = most * np.float32(0.9), np.sqrt(most * most * np.float32(0.7))
     np.testing.assert_array_equal(state.exp_avg_scale[0].cpu().numpy(), m * part)
     np.testing.assert_array_equal(state.exp_avg_sq_scale[0].cpu().numpy(), u * part)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [8, 32])
+def test_tensors_that_overlap_are_refused(cuda_device, bits):
+    """A tensor under two names of which one is written; nothing has changed after a refusal.  Two parameters may share a gradient,
+    and tensors may lie one behind the other."""
+    import torch
+    from paper_1905_00689_gb300 import AdamWState, adamw_step
+    kind = torch.float32 if bits == 32 else torch.float8_e4m3fn
+    n = 256
+
+    def flat(count, dtype=torch.float32):
+        return torch.ones(count, device="cuda").to(dtype)
+
+    def lists(p=None, g=None, m=None, v=None, ms=None, vs=None, c=None):
+        pick = lambda given, make: given if given is not None else [make() for _ in range(2)]  # noqa: E731
+        ones = lambda: flat(1)  # noqa: E731
+        state = AdamWState(pick(m, lambda: flat(n, kind)), pick(v, lambda: flat(n, kind)),
+                           *((pick(ms, ones), pick(vs, ones)) if bits == 8 else ()))
+        return dict(params=pick(p, lambda: flat(n)), grads=pick(g, lambda: flat(n)), state=state, copies=c)
+
+    one, two, half = flat(n, kind), flat(n, kind), flat(n, torch.bfloat16)
+    p, long, scale = [flat(n), flat(n)], flat(2 * n), flat(1)
+    bad = [lists(m=[one, two], v=[flat(n, kind), one]), lists(m=[one, one]), lists(v=[one, one]), lists(c=[half, half]),
+           lists(p=p, c=[p[0].view(torch.bfloat16)[:n], None]), lists(p=p, c=[p[1], None]), lists(p=p, g=[flat(n), p[0]]),
+           lists(g=[long[:n], flat(n)], c=[long[n - 1:2 * n - 1], None]), lists(p=[long[:n], long[n - 1:-1]])]
+    if bits == 8:
+        bad += [lists(ms=[scale, scale]), lists(ms=[flat(1), scale], vs=[scale, flat(1)])]
+    for args in bad:
+        with pytest.raises(ValueError):
+            adamw_step(**args, step=1, lr=0.1)
+    assert all((x == 1).all() for x in p + [long, scale]) and (one.float() == 1).all() and (half == 1).all()
+    g = flat(n)
+    good = lists(p=[long[:n], long[n:]], g=[g, g], c=[half, None])
+    adamw_step(**good, step=1, lr=0.1)
+    assert torch.equal(long[:n], long[n:]) and torch.equal(half, long[:n].bfloat16()) and (long != 1).all()
+    good = lists(m=[one, one], g=[flat(n), None])  # (what has no gradient keeps its averages)
+    adamw_step(**good, step=1, lr=0.1)
+    good, want = lists(p=[flat(n), p[1]], g=[flat(n), p[1]], c=[None, p[1]]), lists()  # itself as its gradient and copy
+    adamw_step(**good, step=1, lr=0.1)
+    adamw_step(**want, step=1, lr=0.1)
+    assert torch.equal(p[1], want["params"][1]) and (p[1] != 1).all()
