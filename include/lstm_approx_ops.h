@@ -280,7 +280,7 @@ size_t lstm_approx_w4_workspace_bytes(int x_dtype, int M, int K);
  *             T) timesteps.  Nothing from later ones enters any result, whatever
  *             they hold; their o is zero.
  *   reset     [T][B] bytes, contiguous, or NULL: where not zero, S_{t-1} counts as
- *             zero (the first token of a packed document), whatever it holds
+ *             zero (the first token of a packed document), whatever it and g_t hold
  *   h_last    [B][H][Dk][Dv] fp32: the state after the stream's last timestep
  *             (h0 where it has none); may be h0 itself
  *   states    [ceil(T / LSTM_APPROX_DELTA_CHUNK)][B][H][Dk +
@@ -350,7 +350,7 @@ int lstm_approx_delta_scan_backward(int dtype, const void *d_o, const float *dh_
  *             outside [0, n_slots) is idle: no state changes, its o is zero.
  *             Slots in range are distinct.
  *   reset     [B] bytes, or NULL: where not zero the state counts as zero,
- *             whatever it holds
+ *             whatever it and g hold
  */
 int lstm_approx_delta_step(int dtype, const void *q, const void *k, const void *v, const float *g,
                            const float *beta, float scale, float *state, int n_slots,

@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kThreads) delta_step_kernel(const StepArgs a) 
   for (int e = 0; e < 4; ++e)
     vc[e] = column(e) < a.Dv ? to_f32(static_cast<const T*>(a.v)[b * a.vb + h * a.vh + column(e)]) : 0.0f;
 
-  const float decay = expf(g < kLeastG ? kLeastG : g);
+  const float decay = fresh ? 0.0f : expf(g < kLeastG ? kLeastG : g);  // (at a reset g may be anything)
   float part[9] = {};  // W^T k and W^T q of 4 columns, k . q
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
