@@ -18,9 +18,13 @@
 // (m / (0 + eps) would be a step of any size): it is at least the type's smallest.
 //
 // Measured, of the 6790 GB/s of a copy: 302 M parameters in 32 bits, gradients and
-// copies in 16: 1214 us (103%); the same with 8-bit averages 874 us (82%: the rounding
-// is 85 instructions a value, which with the waits fill the issue slots); 13 M in
-// 16 bits with 8-bit averages at odd addresses 62 us (31%: values one by one).
+// copies in 16: 1217 us (102%); the same with 8-bit averages 888 us (80%: the rounding
+// is 82 instructions a value, 69% of the issue slots); 13 M in 16 bits with 8-bit
+// averages at odd addresses 63 us (31%: values one by one).
+//
+// With 32-bit averages the root and the reciprocal are the hardware's, each off by one
+// unit of its last place, of a step that is a thousandth of p: 1217 us, 1229 with the
+// rounded ones.  m and v see neither.
 #include <cuda_fp8.h>
 
 #include <cmath>

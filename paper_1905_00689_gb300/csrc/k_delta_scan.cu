@@ -40,11 +40,11 @@
 // used, in two parts of 11 bits on MMAs of 32-bit floats, these kernels executed
 // 4 times the instructions: a chunk of 64 x 128 x 16 took 5.1 us.)
 //
-// Measured, bf16 and 128 x 128 states: 8191 timesteps of 16 heads 368 us (77 the
-// chunks' matrices, 292 along them: 2.3 us a chunk, of which the products are 0.75
-// of the tensor pipes; 18 times the time of its bytes at a copy's rate), 4 streams of
-// 2048 timesteps and 8 heads forward and backward 602 us (44 + 142, 46 + 188 + 204;
-// 30 times).  Bound by what follows one another: three products of 64 x 128 x 16 and
+// Measured, bf16 and 128 x 128 states: 8191 timesteps of 16 heads 416 us (82 the
+// chunks' matrices, 335 along them: 2.6 us a chunk, of which the products are 0.9
+// of the tensor pipes; 21 times the time of its bytes at a copy's rate), 4 streams of
+// 2048 timesteps and 8 heads forward and backward 724 us (47 + 162, 47 + 197 + 251,
+// each alone under a profiler; 36 times).  Bound by what follows one another: three products of 64 x 128 x 16 and
 // four barriers to a chunk, T / 64 chunks.
 //
 // At a reset the state before counts as zero, and so does everything before it
@@ -489,8 +489,8 @@ __device__ __forceinline__ void make_gates(const RawGates& raw, Gates& gates) {
   if (lane == 0) gates.cuts = cuts, gates.pad = 0ull;
 }
 
-// Two blocks to an SM, so that one's loads and barriers lie behind the other's products: 2048 chunks of 128 wide bf16 keys 77 us, in
-// which 284 MB move (43 us at a copy's rate).  (With 16 warps to a block registers spill: 88.)
+// Two blocks to an SM, so that one's loads and barriers lie behind the other's products: 2048 chunks of 128 wide bf16 keys 82 us, in
+// which 212 MB move (31 us at a copy's rate).  (With 16 warps to a block registers spill: 88 us where 8 took 77.)
 template <typename T, int KD>
 __global__ void __launch_bounds__(kThreads, 2) delta_prepare_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
@@ -1267,7 +1267,7 @@ struct GradShared {
   float* sums;                                // [6][C]
   float *next_S, *next_dS, *next_R, *next_Y;  // the next round's, as they come
   // one round's: S0, dS, dO, R, U; after the last, P and E.  (Two rounds in turn, so that a warp splits one while others multiply the
-  // one before, leave the L1 little: 612 us where this takes 602, forward and backward of 4 streams of 8 heads and 2048 timesteps.)
+  // one before, leave the L1 little: 612 us where this took 602, forward and backward of 4 streams of 8 heads and 2048 timesteps.)
   Mat<KD, W, 3> S, dS;
   Mat<C, W, P> dO;
   Mat<C, W, 3> R, U;
@@ -1338,8 +1338,9 @@ __device__ __forceinline__ void add_mma(float (&x)[4], const uint32_t (&a)[kPA][
   for (int r = 0; r < 4; ++r) x[r] += d[r] + e[r];
 }
 
-// By columns of S, 32 at a time: the next ones come as copies while 16 warps multiply.  1024 chunks of bf16, 128 x 128: 204 us, half
-// of it without the products (splitting, the first slices, barriers: one block fills an SM), which take 50 us of the tensor pipes.
+// By columns of S, 32 at a time: the next ones come as copies while 16 warps multiply.  1024 chunks of bf16, 128 x 128: 251 us, of
+// which the products take 90 of the tensor pipes; the rest is splitting, the first slices and barriers (one block fills an SM).  dO
+// and R each go through S by themselves: both at once, S read once, spills more registers and takes 10 us longer.
 template <typename T, int KD>
 __global__ void __launch_bounds__(kGradThreads, 1) delta_gradients_kernel(const DeltaArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];

@@ -10,8 +10,8 @@
 // S do not see one another: a block takes 32 of them, a thread 4 (16 bytes) of
 // every 16th row, all of them asked for at once.
 //
-// Measured, 16 heads of 128 x 128: 64 streams 24.4 us (82% of the 6790 GB/s of a
-// copy), one stream 4.7 us a call, the time of a launch.
+// Measured, 16 heads of 128 x 128: 64 streams 24.9 us (80% of the 6790 GB/s of a
+// copy), one stream 5.6 us a call, the time of a launch.
 #include "ops_common.cuh"
 
 namespace lstm_approx_impl {
